@@ -238,9 +238,9 @@ def prepare(case, seed):
         s["cache"] = E.make_cache(
             s["k"], s["v"], s["k_scale"], s["v_scale"], s["bounds"],
             s["table"], s["lengths"], H=Hkv * G, dtype=case["dtype"])
-        s["ws"] = E.new_cache_workspace(s["cache"], T=T,
-                                        weights=case["weights"],
-                                        keep=case["keep"])
+        s["ws"] = None if case["kind"] == "append" else \
+            E.new_cache_workspace(s["cache"], T=T, weights=case["weights"],
+                                  keep=case["keep"])
     return s
 
 
