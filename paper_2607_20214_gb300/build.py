@@ -41,8 +41,8 @@ def _sources():
 
 def _deps():
     return _sources() + sorted(glob.glob(os.path.join(CSRC, "*.h"))) + sorted(
-        glob.glob(os.path.join(CSRC, "*.cuh"))) + [
-            os.path.join(ROOT, "include", "elsaa.h")]
+        glob.glob(os.path.join(CSRC, "*.cuh"))) + sorted(
+            glob.glob(os.path.join(ROOT, "include", "*.h")))
 
 
 def up_to_date() -> bool:

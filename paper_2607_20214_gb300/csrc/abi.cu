@@ -11,6 +11,7 @@
 #include <string>
 #include <vector>
 
+#include "cache.h"
 #include "internal.h"
 
 namespace elsaa {
@@ -326,6 +327,11 @@ int set_last_error(int code, const char *fmt, ...) {
     vsnprintf(g_err, sizeof(g_err), fmt, ap);
     va_end(ap);
     return code;
+}
+
+cudaError_t timed_launch(const char *name, cudaStream_t st,
+                         cudaError_t (*fn)(void *), void *arg) {
+    return timed(name, st, [&] { return fn(arg); });
 }
 
 }  // namespace elsaa

@@ -1,0 +1,92 @@
+// Internal declarations of the cache operators (include/elsaa_cache.h): the
+// view of a cache that kernels take by value, the division of attention work
+// over CTAs, and the launchers.
+#pragma once
+
+#include "../../include/elsaa_cache.h"
+#include "internal.h"
+
+namespace elsaa {
+
+// Exponents of a page's scale, and of an 8-bit query in the page scores.
+constexpr int kCacheExpLow = -64, kCacheExpHigh = 120;
+constexpr int kQueryExpLow = -60;
+// Tokens per tile of the attention kernels: a whole number of pages.
+constexpr int kCacheTile = 128;
+// Sequences of a call: their tile counts are summed in shared memory.
+constexpr int kCacheMaxB = 4096;
+// In-band status codes and sites of the cache kernels.
+constexpr int kDevCachePage = 5;    // a page outside the pool was skipped
+constexpr int kDevCacheLength = 6;  // a length outside the table was clipped
+
+struct CacheView {
+    int B, H, Hkv, G, d, ps, num_pages, max_pages, T;
+    int dtype;
+    float scale;
+    uint8_t *k, *v;
+    float *ks, *vs;
+    int8_t *bounds;
+    const int32_t *table, *lengths, *new_len;
+    DeviceStatus *status;
+};
+
+// One attention call. Columns of an item: the G T queries of a K/V head, in
+// groups of `cols` (the last group may be smaller); column g T + t.
+struct CacheAttn {
+    CacheView c;
+    const void *q;
+    void *o;
+    float *lse;              // or NULL
+    const int32_t *pages;    // [B, Hkv, n_sel], or NULL
+    int n_sel;
+    const float *weight_in;
+    float *weight_out;       // or NULL: no weights
+    int cols, groups;        // columns per group, groups of a head
+    int ctas;                // CTAs that share the tiles
+    // workspace
+    float *part;             // [ctas][2][cols][d + 2]: O, max, sum of pieces
+    int *prefix;             // [B + 1] tiles of a head before sequence b
+    float *lse2;             // [B, Hkv, G T] log2 sums
+    float *scores;           // [B, Hkv, G T, slots] log2 scores (weights)
+    long slots;              // tokens (or listed rows) of a head's scores
+};
+
+// CTAs of the attention kernels on this chip's 152 SMs, and the columns that
+// one walks at a time.
+constexpr int kCacheSimtCtas = 152 * 3;
+constexpr int kCacheTcCtas = 152 * 2;
+constexpr int kCacheMaxCtas = kCacheSimtCtas;
+inline int cache_simt_cols(int gt) { return gt >= 3 ? 4 : gt; }
+inline int cache_tc_cols(int gt) {
+    int n = 1;
+    while (n < gt && n < 16) n *= 2;
+    return n;
+}
+
+bool cache_attn_tc_supported(const CacheView &c);
+cudaError_t launch_cache_attn_simt(CacheAttn &A, cudaStream_t st);
+cudaError_t launch_cache_attn_tc(CacheAttn &A, cudaStream_t st);
+cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st);
+cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st);
+
+cudaError_t launch_cache_append(const CacheView &c, const void *k,
+                                const void *v, cudaStream_t st);
+cudaError_t launch_cache_select(const CacheView &c, const void *q, int n_sel,
+                                int first, int last, int32_t *pages,
+                                float *scores, cudaStream_t st);
+// kept: [B, Hkv, keep]; count: [B] tokens kept.
+cudaError_t launch_cache_keep(const CacheView &c, const float *weight,
+                              int keep, int recent, int32_t *kept, int *count,
+                              cudaStream_t st);
+cudaError_t launch_cache_compact(const CacheView &c, const float *weight,
+                                 int keep, const int32_t *kept,
+                                 const int *count, const int32_t *dst_table,
+                                 int dst_pages, float *weight_out,
+                                 int32_t *lengths_out, cudaStream_t st);
+
+// Runs a launch under its name in the per-kernel timing of
+// elsaa_profile_start (abi.cu).
+cudaError_t timed_launch(const char *name, cudaStream_t st,
+                         cudaError_t (*fn)(void *), void *arg);
+
+}  // namespace elsaa

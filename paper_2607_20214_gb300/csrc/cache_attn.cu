@@ -1,0 +1,383 @@
+// Attention of new tokens over the 8-bit cache: the CUDA-core kernel, the
+// merge of items that several CTAs shared, and the accumulated weights.
+//
+// k_cache_attn_simt walks the tiles of its range once with a running maximum
+// and sum. A warp takes 32 tokens of a tile: the lanes of a row hold 16
+// channels each (one 16-byte load of codes), so a token's score is 16 products
+// a lane and a few shuffles, its value 16 products again, and O stays in
+// registers for all columns of the item. A cached byte is read once per group
+// of up to 4 columns and costs 2 conversions' share and 2 fp32 products per
+// column: with one column (ungrouped heads) that is below what the SMs have
+// to spare while HBM delivers the byte, with more the products bound it.
+#include "cache_common.cuh"
+
+namespace elsaa {
+
+namespace {
+
+using namespace cache;
+
+constexpr int kSaThreads = 128;
+constexpr float kLog2eF = 1.4426950408889634f;
+
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(kSaThreads)
+    k_cache_attn_simt(const CacheAttn A) {
+    wait_for_stream();
+    constexpr int LPR = D / 16;   // lanes per row
+    constexpr int R = 32 / LPR;   // rows per warp load
+    constexpr int S = 32 / R;     // loads per tile
+    extern __shared__ int prefix[];
+    __shared__ float accs[4][NG][D];
+    __shared__ float ms[4][NG], ls[4][NG];
+    const CacheView &c = A.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int sub = lane % LPR, rg = lane / LPR;
+    sum_tiles(A, prefix);
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int i = tid; i <= c.B; i += kSaThreads) A.prefix[i] = prefix[i];
+    const Range r = cta_range(A, prefix, blockIdx.x);
+    const float sl2 = c.scale * kLog2eF;
+    const int GT = c.G * c.T;
+
+    for (long t = r.t0; t < r.t1;) {
+        const Item it = find_item(A, prefix, t);
+        const long end = min(it.a + it.tiles, r.t1);
+        const size_t bh = (size_t)it.b * c.Hkv + it.h;
+        float qf[NG][16], acc[NG][16], m[NG], l[NG];
+        int limit[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            m[g] = -INFINITY;
+            l[g] = 0.0f;
+            limit[g] = g < it.cols ? last_seen(A, it, it.col0 + g) : -1;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) qf[g][i] = acc[g][i] = 0.0f;
+            if (limit[g] >= 0) {
+                const T *x = (const T *)A.q +
+                             query_row(A, it.b, it.h, it.col0 + g) * D +
+                             sub * 16;
+                load8(x, qf[g]);
+                load8(x + 8, qf[g] + 8);
+            }
+        }
+        for (; t < end; ++t) {
+            // lane i: token i of the warp's 32
+            const int w = (int)(t - it.a) * kCacheTile + warp * 32 + lane;
+            int id = -1, pos = 0;
+            float ks = 0.0f, vs = 0.0f;
+            if (w < it.walk) {
+                int p = w / c.ps;
+                if (A.pages) p = A.pages[bh * A.n_sel + p];
+                pos = p * c.ps + w % c.ps;
+                if (p >= 0 && p < c.max_pages && pos < it.len)
+                    id = page_id(c, it.b, p);
+                if (id >= 0) {
+                    const size_t ph = (size_t)id * c.Hkv + it.h;
+                    ks = c.ks[ph] * sl2;
+                    vs = c.vs[ph];
+                }
+            }
+            const int row = w % c.ps;
+            uint4 kr[S], vr[S];
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int tk = s * R + rg;
+                const int i = __shfl_sync(0xffffffffu, id, tk);
+                const int ro = __shfl_sync(0xffffffffu, row, tk);
+                kr[s] = vr[s] = make_uint4(0, 0, 0, 0);
+                if (i >= 0) {
+                    const size_t at =
+                        (((size_t)i * c.Hkv + it.h) * c.ps + ro) * D + sub * 16;
+                    kr[s] = *(const uint4 *)(c.k + at);
+                    vr[s] = *(const uint4 *)(c.v + at);
+                }
+            }
+            float sc[NG][S];
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                float x[16];
+                from_e4m3x4(kr[s].x, x);
+                from_e4m3x4(kr[s].y, x + 4);
+                from_e4m3x4(kr[s].z, x + 8);
+                from_e4m3x4(kr[s].w, x + 12);
+                const int tk = s * R + rg;
+                const float f = __shfl_sync(0xffffffffu, ks, tk);
+                const int po = __shfl_sync(0xffffffffu, pos, tk);
+                const bool in = __shfl_sync(0xffffffffu, id, tk) >= 0;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    float d = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) d = fmaf(qf[g][i], x[i], d);
+#pragma unroll
+                    for (int o = 1; o < LPR; o <<= 1)
+                        d += __shfl_xor_sync(0xffffffffu, d, o);
+                    sc[g][s] = in && po <= limit[g] ? d * f : -INFINITY;
+                }
+            }
+            if (A.scores) {
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    const long at = (t - it.a) * kCacheTile + warp * 32 +
+                                    s * R + rg;
+                    if (sub == 0 && at < it.walk)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g)
+                            if (g < it.cols)
+                                A.scores[(bh * GT + it.col0 + g) * A.slots +
+                                         at] = sc[g][s];
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                float mx = sc[g][0];
+#pragma unroll
+                for (int s = 1; s < S; ++s) mx = fmaxf(mx, sc[g][s]);
+#pragma unroll
+                for (int o = LPR; o < 32; o <<= 1)
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                mx = fmaxf(mx, m[g]);
+                const float ref = mx == -INFINITY ? 0.0f : mx;
+                const float al = tc::ex2_approx(m[g] - ref);
+                m[g] = mx;
+                l[g] *= al;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[g][i] *= al;
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    sc[g][s] = tc::ex2_approx(sc[g][s] - ref);
+                    l[g] += sc[g][s];
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                float x[16];
+                from_e4m3x4(vr[s].x, x);
+                from_e4m3x4(vr[s].y, x + 4);
+                from_e4m3x4(vr[s].z, x + 8);
+                from_e4m3x4(vr[s].w, x + 12);
+                const float f = __shfl_sync(0xffffffffu, vs, s * R + rg);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    // a token that a column does not see adds nothing,
+                    // whatever its codes are
+                    const float p = sc[g][s] * f;
+                    if (sc[g][s] != 0.0f)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[g][i] = fmaf(p, x[i], acc[g][i]);
+                }
+            }
+        }
+        // the warp's rows, then the four warps
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int o = LPR; o < 32; o <<= 1) {
+                l[g] += __shfl_xor_sync(0xffffffffu, l[g], o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    acc[g][i] += __shfl_xor_sync(0xffffffffu, acc[g][i], o);
+            }
+            if (rg == 0)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    accs[warp][g][sub * 16 + i] = acc[g][i];
+            if (lane == 0) {
+                ms[warp][g] = m[g];
+                ls[warp][g] = l[g];
+            }
+        }
+        __syncthreads();
+        const bool whole = it.a >= r.t0 && it.a + it.tiles <= r.t1;
+        const int slot = it.a < r.t0 ? 0 : 1;
+        for (int g = 0; g < it.cols; ++g) {
+            float M = ms[0][g], L = 0.0f, x = 0.0f;
+            for (int k = 1; k < 4; ++k) M = fmaxf(M, ms[k][g]);
+            const float ref = M == -INFINITY ? 0.0f : M;
+            for (int k = 0; k < 4; ++k) {
+                const float f = tc::ex2_approx(ms[k][g] - ref);
+                L += f * ls[k][g];
+                if (tid < D) x += f * accs[k][g][tid];
+            }
+            const int col = it.col0 + g;
+            if (!whole) {
+                float *at = piece(A, blockIdx.x, slot, g);
+                if (tid < D) at[tid] = x;
+                if (tid == 0) {
+                    at[D] = M;
+                    at[D + 1] = L;
+                }
+            } else {
+                if (tid == 0) store_lse(A, it, col, M, L);
+                if (tid < D && col % c.T < it.n)
+                    store_o(A, query_row(A, it.b, it.h, col), tid,
+                            L == 0.0f ? 0.0f : x / L);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------- merge
+//
+// A column of an item that several CTAs shared: their pieces in order, so the
+// result does not depend on which CTA was first. 256 threads: the channels,
+// times groups of pieces read at once.
+constexpr int kMgThreads = 512;
+
+__global__ void __launch_bounds__(kMgThreads)
+    k_cache_merge(const CacheAttn A) {
+    wait_for_stream();
+    __shared__ float f[kCacheMaxCtas], sum[kMgThreads], red[kMgThreads / 32];
+    const CacheView &c = A.c;
+    const int GT = c.G * c.T, HC = c.Hkv * A.groups;
+    const int b = blockIdx.y, h = blockIdx.x / GT, col = blockIdx.x % GT;
+    const int tid = threadIdx.x;
+    const int tiles = A.prefix[b + 1] - A.prefix[b];
+    const long total = (long)A.prefix[c.B] * HC;
+    const long n = min((long)A.ctas, total);
+    if (tiles == 0) return;
+    const int group = col / A.cols;
+    const long a = (long)A.prefix[b] * HC +
+                   (long)(h * A.groups + group) * tiles;
+    const long c0 = range_owner(a, total, n);
+    const int pieces = (int)(range_owner(a + tiles - 1, total, n) - c0) + 1;
+    if (pieces == 1) return;
+    Item it;
+    it.b = b;
+    it.h = h;
+    it.n = fresh(c, b);
+    const int d = c.d, g = col - group * A.cols;
+    auto at = [&](int i) { return piece(A, c0 + i, i == 0 ? 1 : 0, g); };
+    float M = -INFINITY;
+    for (int i = tid; i < pieces; i += kMgThreads) {
+        f[i] = at(i)[d];
+        M = fmaxf(M, f[i]);
+    }
+    M = warp_max(M);
+    if ((tid & 31) == 0) red[tid >> 5] = M;
+    __syncthreads();
+    for (int i = 0; i < kMgThreads / 32; ++i) M = fmaxf(M, red[i]);
+    const float ref = M == -INFINITY ? 0.0f : M;
+    for (int i = tid; i < pieces; i += kMgThreads) f[i] = exp2f(f[i] - ref);
+    __syncthreads();
+    const int ch = tid % d, part = tid / d, parts = kMgThreads / d;
+    float x = 0.0f, L = 0.0f;
+#pragma unroll 4
+    for (int i = part; i < pieces; i += parts) x += f[i] * at(i)[ch];
+    sum[tid] = x;
+    if (tid < 32) {
+        for (int i = tid; i < pieces; i += 32) L += f[i] * at(i)[d + 1];
+        L = warp_sum(L);
+        if (tid == 0) red[0] = L;
+    }
+    __syncthreads();
+    L = red[0];
+    if (tid == 0) store_lse(A, it, col, M, L);
+    if (part == 0 && col % c.T < it.n) {
+        for (int p = 1; p < parts; ++p) x += sum[p * d + ch];
+        store_o(A, query_row(A, b, h, col), ch, L == 0.0f ? 0.0f : x / L);
+    }
+}
+
+// ----------------------------------------------------------------- weights
+//
+// weight_out_j = weight_in_j + sum over the columns of 2^(s_j - lse), from
+// the scores that the attention kernel left: 4 bytes a token and column,
+// where a second walk over the keys would read d bytes.
+constexpr int kWtThreads = 128;
+
+__global__ void __launch_bounds__(kWtThreads)
+    k_cache_weights(const CacheAttn A) {
+    wait_for_stream();
+    __shared__ int slot[kWtThreads / 16];
+    __shared__ float lse[128];
+    const CacheView &c = A.c;
+    const int h = blockIdx.y, b = blockIdx.z, GT = c.G * c.T;
+    const size_t bh = (size_t)b * c.Hkv + h;
+    const int len = tokens(c, b), j0 = blockIdx.x * kWtThreads;
+    const int j = j0 + threadIdx.x;
+    if (j0 >= len) return;
+    const bool any = fresh(c, b) > 0;
+    if (any && threadIdx.x < GT) lse[threadIdx.x] = A.lse2[bh * GT + threadIdx.x];
+    long at = j;
+    if (A.pages) {
+        // the list entries of this block's pages
+        if (threadIdx.x < kWtThreads / 16) slot[threadIdx.x] = -1;
+        __syncthreads();
+        const int p0 = j0 / c.ps, np = kWtThreads / c.ps;
+        const int listed = min(A.n_sel, (len + c.ps - 1) / c.ps);
+        for (int e = threadIdx.x; e < listed; e += kWtThreads) {
+            const int p = A.pages[bh * A.n_sel + e] - p0;
+            if (p >= 0 && p < np) slot[p] = e;
+        }
+        __syncthreads();
+        const int e = slot[(j - j0) / c.ps];
+        at = e < 0 ? -1 : (long)e * c.ps + j % c.ps;
+    }
+    __syncthreads();
+    if (j >= len) return;
+    const size_t w = bh * c.max_pages * c.ps + j;
+    float x = 0.0f;
+    if (any && at >= 0) {
+        const float *s = A.scores + bh * GT * A.slots + at;
+        for (int col = 0; col < GT; ++col) {
+            const float v = s[(size_t)col * A.slots];
+            if (v != -INFINITY) x += exp2f(v - lse[col]);
+        }
+    }
+    A.weight_out[w] = (A.weight_in ? A.weight_in[w] : 0.0f) + x;
+}
+
+template <typename T, int D, int NG>
+cudaError_t launch_simt(const CacheAttn &A, cudaStream_t st) {
+    return launch_after(k_cache_attn_simt<T, D, NG>, dim3(A.ctas), kSaThreads,
+                        sizeof(int) * (A.c.B + 1), st, A);
+}
+
+template <typename T, int D>
+cudaError_t launch_simt_cols(const CacheAttn &A, cudaStream_t st) {
+    switch (A.cols) {
+        case 1: return launch_simt<T, D, 1>(A, st);
+        case 2: return launch_simt<T, D, 2>(A, st);
+        default: return launch_simt<T, D, 4>(A, st);
+    }
+}
+
+template <typename T>
+cudaError_t launch_simt_d(const CacheAttn &A, cudaStream_t st) {
+    switch (A.c.d) {
+        case 32: return launch_simt_cols<T, 32>(A, st);
+        case 64: return launch_simt_cols<T, 64>(A, st);
+        default: return launch_simt_cols<T, 128>(A, st);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_cache_attn_simt(CacheAttn &A, cudaStream_t st) {
+    const int GT = A.c.G * A.c.T;
+    A.cols = cache_simt_cols(GT);
+    A.groups = (GT + A.cols - 1) / A.cols;
+    A.ctas = kCacheSimtCtas;
+    return A.c.dtype == ELSAA_FP32 ? launch_simt_d<float>(A, st)
+                                   : launch_simt_d<__nv_bfloat16>(A, st);
+}
+
+cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st) {
+    return launch_after(k_cache_merge, dim3(A.c.Hkv * A.c.G * A.c.T, A.c.B),
+                        kMgThreads, 0, st, A);
+}
+
+cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st) {
+    const long cap = (long)A.c.max_pages * A.c.ps;
+    return launch_after(k_cache_weights,
+                        dim3((unsigned)((cap + kWtThreads - 1) / kWtThreads),
+                             A.c.Hkv, A.c.B),
+                        kWtThreads, 0, st, A);
+}
+
+}  // namespace elsaa

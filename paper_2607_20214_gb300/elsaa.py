@@ -1,4 +1,4 @@
-"""Python binding of the libelsaa C ABI (include/elsaa.h).
+"""Python binding of the libelsaa C ABI (include/elsaa.h, elsaa_cache.h).
 
 Argument marshalling only: every step of the operator runs in the CUDA
 kernels of libelsaa.so. PyTorch provides device memory and streams. The
@@ -34,7 +34,10 @@ SYMBOLS = ("elsaa_workspace_size", "elsaa_forward", "elsaa_check_status",
            "elsaa_check_status_noalloc",
            "elsaa_selftest_wait_timeout_noalloc", "elsaa_causal_levels",
            "elsaa_causal_index_lists", "elsaa_forward_selected_keys",
-           "elsaa_forward_gated_workspace_size", "elsaa_forward_gated")
+           "elsaa_forward_gated_workspace_size", "elsaa_forward_gated",
+           "elsaa_cache_workspace_size", "elsaa_cache_append",
+           "elsaa_cache_select", "elsaa_cache_attention",
+           "elsaa_cache_evict")
 # Size of the fixed scratch array behind elsaa_forward_noalloc.
 ELSAA_STATIC_WORKSPACE_BYTES = 64 << 20
 
@@ -71,6 +74,22 @@ class elsaa_gate_mlp(ctypes.Structure):
 class elsaa_kernel_stat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int),
                 ("total_ms", ctypes.c_double)]
+
+
+class elsaa_cache(ctypes.Structure):
+    """Mirror of struct elsaa_cache (include/elsaa_cache.h). make_cache fills
+    it from tensors and keeps them alive in `tensors`."""
+    _fields_ = [
+        ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
+        ("d_h", ctypes.c_int), ("dtype", ctypes.c_int),
+        ("page_size", ctypes.c_int), ("num_pages", ctypes.c_int),
+        ("max_pages", ctypes.c_int), ("scale", ctypes.c_float),
+        ("impl", ctypes.c_int), ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p), ("bounds", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+    ]
 
 
 class ElsaaError(RuntimeError):
@@ -155,6 +174,18 @@ def load_library(path: str = LIB) -> ctypes.CDLL:
     L.elsaa_check_status_noalloc.restype = ctypes.c_int
     L.elsaa_selftest_wait_timeout_noalloc.argtypes = [ctypes.c_int, vp]
     L.elsaa_selftest_wait_timeout_noalloc.restype = ctypes.c_int
+    pc, ci, sz = ctypes.POINTER(elsaa_cache), ctypes.c_int, ctypes.c_size_t
+    L.elsaa_cache_workspace_size.argtypes = [pc, ci, ci, ci,
+                                             ctypes.POINTER(sz)]
+    L.elsaa_cache_append.argtypes = [pc, ci, vp, vp, vp, vp]
+    L.elsaa_cache_select.argtypes = [pc, ci, vp, vp, ci, ci, ci, vp, vp, sz,
+                                     vp]
+    L.elsaa_cache_attention.argtypes = [pc, ci, vp, vp, vp, ci, vp, vp, vp,
+                                        vp, vp, sz, vp]
+    L.elsaa_cache_evict.argtypes = [pc, vp, ci, ci, vp, ci, vp, vp, vp, vp,
+                                    sz, vp]
+    for name in ("workspace_size", "append", "select", "attention", "evict"):
+        getattr(L, "elsaa_cache_" + name).restype = ci
     _lib = L
     return L
 
@@ -637,3 +668,187 @@ def elsaa_forward_gated(params: elsaa_params, mlp: dict, q, k, v, w_sort,
         ctypes.byref(params), ctypes.byref(m), *args,
         workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
     return o
+
+
+# ------------------------------------------------ the cache (elsaa_cache.h)
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def make_cache(k, v, k_scale, v_scale, bounds, page_table, lengths, H=None,
+               dtype="bf16", scale=0.0, impl=ELSAA_IMPL_AUTO,
+               status=None) -> elsaa_cache:
+    """The cache over these device tensors (layouts: include/elsaa_cache.h).
+
+    k, v [num_pages, H_kv, page_size, d_h] float8_e4m3fn (or its bytes);
+    k_scale, v_scale [num_pages, H_kv] fp32; bounds [num_pages, H_kv, 2, d_h]
+    int8; page_table [B, max_pages] and lengths [B] int32; H query heads
+    (default H_kv); status [4] int32 zeros (default: made here).
+    """
+    dev = k.device
+    if dev.type != "cuda":
+        raise ValueError("k must be a CUDA tensor")
+    if k.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k must have 4 dimensions and page_table 2")
+    num, hkv, ps, d = k.shape
+    B, width = page_table.shape
+    if k.dtype not in _CODES or v.dtype not in _CODES:
+        raise ValueError("k and v must be float8_e4m3fn or uint8")
+    if status is None:
+        status = torch.zeros(4, dtype=torch.int32, device=dev)
+    dt = {"bf16": ELSAA_BF16, "fp32": ELSAA_FP32}[dtype] if isinstance(
+        dtype, str) else int(dtype)
+    f32, i32 = torch.float32, torch.int32
+    c = elsaa_cache(
+        B, hkv if H is None else H, hkv, d, dt, ps, num, width, scale, impl,
+        _ptr(k, "k", None, k.numel(), dev), _ptr(v, "v", None, k.numel(), dev),
+        _ptr(k_scale, "k_scale", f32, num * hkv, dev),
+        _ptr(v_scale, "v_scale", f32, num * hkv, dev),
+        _ptr(bounds, "bounds", torch.int8, num * hkv * 2 * d, dev),
+        _ptr(page_table, "page_table", i32, B * width, dev),
+        _ptr(lengths, "lengths", i32, B, dev),
+        _ptr(status, "status", i32, 4, dev))
+    c.tensors = dict(k=k, v=v, k_scale=k_scale, v_scale=v_scale,
+                     bounds=bounds, page_table=page_table, lengths=lengths,
+                     status=status)
+    c.device = dev
+    c.torch_dtype = f32 if dt == ELSAA_FP32 else torch.bfloat16
+    return c
+
+
+def new_cache(B, H, H_kv, d_h, page_size, num_pages, max_pages,
+              dtype="bf16", scale=0.0, impl=ELSAA_IMPL_AUTO,
+              device="cuda") -> elsaa_cache:
+    """An empty cache: pools of num_pages pages, a page table of -1 and
+    lengths of 0 (in `tensors`, for the caller to fill)."""
+    def zeros(shape, dt):
+        return torch.zeros(shape, dtype=dt, device=device)
+    pool = (num_pages, H_kv, page_size, d_h)
+    return make_cache(
+        zeros(pool, torch.uint8).view(torch.float8_e4m3fn),
+        zeros(pool, torch.uint8).view(torch.float8_e4m3fn),
+        torch.ones((num_pages, H_kv), device=device),
+        torch.ones((num_pages, H_kv), device=device),
+        zeros((num_pages, H_kv, 2, d_h), torch.int8),
+        torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+        zeros((B,), torch.int32), H, dtype, scale, impl)
+
+
+def elsaa_cache_workspace_size(cache: elsaa_cache, T=1, weights=False,
+                               keep=0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().elsaa_cache_workspace_size(
+        ctypes.byref(cache), int(T), int(bool(weights)), int(keep),
+        ctypes.byref(n)))
+    return n.value
+
+
+def new_cache_workspace(cache: elsaa_cache, T=1, weights=False,
+                        keep=0) -> torch.Tensor:
+    """Scratch for the cache calls of up to T tokens a sequence (weights:
+    elsaa_cache_attention with weight_out; keep: elsaa_cache_evict)."""
+    n = elsaa_cache_workspace_size(cache, T, weights, keep)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.device)
+
+
+def _rows(t, name, cache, heads):
+    """(pointer, T) of [B, heads, T, d_h] rows."""
+    if t.dim() != 4 or t.shape[0] != cache.B or t.shape[1] != heads or \
+            t.shape[3] != cache.d_h:
+        raise ValueError("%s must be [%d, %d, T, %d] (got %s)" % (
+            name, cache.B, heads, cache.d_h, tuple(t.shape)))
+    return _ptr(t, name, cache.torch_dtype, None, cache.device), t.shape[2]
+
+
+def elsaa_cache_append(cache: elsaa_cache, k, v, new_len=None, stream=None):
+    """Enqueue elsaa_cache_append: rows k, v [B, H_kv, T, d_h] become the
+    newest tokens (lengths count them already)."""
+    dev = cache.device
+    kp, T = _rows(k, "k", cache, cache.H_kv)
+    vp = _ptr(v, "v", cache.torch_dtype, k.numel(), dev)
+    _check(load_library().elsaa_cache_append(
+        ctypes.byref(cache), T, kp, vp,
+        _ptr(new_len, "new_len", torch.int32, cache.B, dev),
+        _stream_of(stream, dev)))
+
+
+def elsaa_cache_select(cache: elsaa_cache, q, n_sel, first=1, last=1,
+                       new_len=None, pages=None, workspace=None,
+                       stream=None):
+    """Enqueue elsaa_cache_select for queries q [B, H, T, d_h]; returns pages
+    [B, H_kv, n_sel] int32 (allocated here when not given)."""
+    dev = cache.device
+    qp, T = _rows(q, "q", cache, cache.H)
+    if pages is None:
+        pages = torch.empty((cache.B, cache.H_kv, n_sel), dtype=torch.int32,
+                            device=dev)
+    if workspace is None:
+        workspace = new_cache_workspace(cache, T)
+    _check(load_library().elsaa_cache_select(
+        ctypes.byref(cache), T, qp,
+        _ptr(new_len, "new_len", torch.int32, cache.B, dev), n_sel, first,
+        last, _ptr(pages, "pages", torch.int32,
+                   cache.B * cache.H_kv * n_sel, dev),
+        _ptr(workspace, "workspace", None, None, dev),
+        workspace.numel() * workspace.element_size(),
+        _stream_of(stream, dev)))
+    return pages
+
+
+def elsaa_cache_attention(cache: elsaa_cache, q, pages=None, new_len=None,
+                          weight_in=None, weight_out=None, o=None, lse=None,
+                          workspace=None, stream=None):
+    """Enqueue elsaa_cache_attention for queries q [B, H, T, d_h]; returns o
+    (allocated here when not given, rows behind new_len then undefined).
+    pages: as elsaa_cache_select returns them, or None for all."""
+    dev = cache.device
+    qp, T = _rows(q, "q", cache, cache.H)
+    if o is None:
+        o = torch.empty_like(q)
+    if workspace is None:
+        workspace = new_cache_workspace(cache, T, weight_out is not None)
+    f32 = torch.float32
+    slots = cache.B * cache.H_kv * cache.max_pages * cache.page_size
+    n_sel = 0
+    if pages is not None:
+        n_sel = pages.shape[-1]
+    _check(load_library().elsaa_cache_attention(
+        ctypes.byref(cache), T, qp,
+        _ptr(new_len, "new_len", torch.int32, cache.B, dev),
+        _ptr(pages, "pages", torch.int32, cache.B * cache.H_kv * n_sel, dev),
+        n_sel, _ptr(weight_in, "weight_in", f32, slots, dev),
+        _ptr(weight_out, "weight_out", f32, slots, dev),
+        _ptr(o, "o", cache.torch_dtype, q.numel(), dev),
+        _ptr(lse, "lse", f32, cache.B * cache.H * T, dev),
+        _ptr(workspace, "workspace", None, None, dev),
+        workspace.numel() * workspace.element_size(),
+        _stream_of(stream, dev)))
+    return o
+
+
+def elsaa_cache_evict(cache: elsaa_cache, weight, keep, recent, dst_table,
+                      weight_out=None, lengths_out=None, kept=None,
+                      workspace=None, stream=None):
+    """Enqueue elsaa_cache_evict; returns (weight_out, lengths_out), allocated
+    here when not given. The kept tokens are in the pages of dst_table
+    [B, dst_pages] afterwards."""
+    dev, i32, f32 = cache.device, torch.int32, torch.float32
+    width, ps, bh = dst_table.shape[-1], cache.page_size, cache.B * cache.H_kv
+    if weight_out is None:
+        weight_out = torch.zeros((cache.B, cache.H_kv, width * ps),
+                                 device=dev)
+    if lengths_out is None:
+        lengths_out = torch.empty((cache.B,), dtype=i32, device=dev)
+    if workspace is None:
+        workspace = new_cache_workspace(cache, 1, False, keep)
+    _check(load_library().elsaa_cache_evict(
+        ctypes.byref(cache),
+        _ptr(weight, "weight", f32, bh * cache.max_pages * ps, dev), keep,
+        recent, _ptr(dst_table, "dst_table", i32, cache.B * width, dev),
+        width, _ptr(weight_out, "weight_out", f32, bh * width * ps, dev),
+        _ptr(lengths_out, "lengths_out", i32, cache.B, dev),
+        _ptr(kept, "kept", i32, bh * keep, dev),
+        _ptr(workspace, "workspace", None, None, dev),
+        workspace.numel() * workspace.element_size(),
+        _stream_of(stream, dev)))
+    return weight_out, lengths_out
