@@ -321,6 +321,15 @@ cudaError_t make_tma_map_bf16_narrow(CUtensorMap *map, const void *base,
                      cols, box_cols, box_rows, sw);
 }
 
+cudaError_t make_tma_map_u8(CUtensorMap *map, const void *base, uint64_t rows,
+                            uint64_t cols, uint32_t box_rows) {
+    if (cols != 64 && cols != 128) return cudaErrorInvalidValue;
+    return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, base, rows, cols,
+                     (uint32_t)cols, box_rows,
+                     cols == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                : CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
 int set_last_error(int code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);

@@ -257,7 +257,11 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
         A.slots = (long)c.max_pages * c.ps;
     }
     cudaStream_t st = (cudaStream_t)stream;
-    ELSAA_CACHE_LAUNCH("cache_attn_simt", st, launch_cache_attn_simt(A, st));
+    if (cache->impl == ELSAA_IMPL_AUTO && cache_attn_tc_supported(c))
+        ELSAA_CACHE_LAUNCH("cache_attn_tc", st, launch_cache_attn_tc(A, st));
+    else
+        ELSAA_CACHE_LAUNCH("cache_attn_simt", st,
+                           launch_cache_attn_simt(A, st));
     ELSAA_CACHE_LAUNCH("cache_merge", st, launch_cache_merge(A, st));
     if (weight_out)
         ELSAA_CACHE_LAUNCH("cache_weights", st, launch_cache_weights(A, st));

@@ -301,8 +301,13 @@ __global__ void __launch_bounds__(kWtThreads)
     const int len = tokens(c, b), j0 = blockIdx.x * kWtThreads;
     const int j = j0 + threadIdx.x;
     if (j0 >= len) return;
-    const bool any = fresh(c, b) > 0;
-    if (any && threadIdx.x < GT) lse[threadIdx.x] = A.lse2[bh * GT + threadIdx.x];
+    const int n = fresh(c, b);
+    const bool any = n > 0;
+    // a column that is no query adds nothing: 2^(s - inf)
+    if (any && threadIdx.x < GT)
+        lse[threadIdx.x] = (int)threadIdx.x % c.T < n
+                               ? A.lse2[bh * GT + threadIdx.x]
+                               : INFINITY;
     long at = j;
     if (A.pages) {
         // the list entries of this block's pages

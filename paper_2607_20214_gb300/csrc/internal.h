@@ -248,6 +248,11 @@ cudaError_t make_tma_map_bf16_narrow(CUtensorMap *map, const void *base,
                                      uint64_t rows, uint64_t cols,
                                      uint32_t box_cols, uint32_t box_rows);
 
+// Row-major bytes [rows x cols], cols 64 or 128, with boxes of whole rows and
+// the swizzle of their width.
+cudaError_t make_tma_map_u8(CUtensorMap *map, const void *base, uint64_t rows,
+                            uint64_t cols, uint32_t box_rows);
+
 // RACE planes as bf16 rows [H][Lg_pad][d] (rows >= L * gamma zero), the
 // operand image the tensor-core kernels load with TMA.
 cudaError_t launch_prep_planes(const Plan &P, const float *w_race,
