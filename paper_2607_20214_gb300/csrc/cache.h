@@ -30,6 +30,13 @@ struct CacheView {
     DeviceStatus *status;
 };
 
+// An item of the attention kernels that began in a CTA and went on in others.
+struct alignas(16) CacheSplit {
+    int b, hc;   // sequence; K/V head * groups + column group
+    int pieces;  // CTAs; 0: none such
+    int n;       // the sequence's new tokens
+};
+
 // One attention call. Columns of an item: the G T queries of a K/V head, in
 // groups of `cols` (the last group may be smaller); column g T + t.
 struct CacheAttn {
@@ -44,18 +51,20 @@ struct CacheAttn {
     int cols, groups;        // columns per group, groups of a head
     int ctas;                // CTAs that share the tiles
     // workspace
+    CacheSplit *split;       // [ctas]
     float *part;             // [ctas][2][cols][d + 2]: O, max, sum of pieces
-    int *prefix;             // [B + 1] tiles of a head before sequence b
     float *lse2;             // [B, Hkv, G T] log2 sums
     float *scores;           // [B, Hkv, G T, slots] log2 scores (weights)
-    long slots;              // tokens (or listed rows) of a head's scores
+    long slots;              // rows of a head's scores
 };
 
 // CTAs of the attention kernels on this chip's 152 SMs, and the columns that
 // one walks at a time.
 constexpr int kCacheSimtCtas = 152 * 3;
 constexpr int kCacheTcCtas = 152 * 2;
-constexpr int kCacheMaxCtas = kCacheSimtCtas;
+// CTAs that share one item at most: what the merge of an item costs grows with
+// them.
+constexpr int kCacheMaxPieces = 64;
 inline int cache_simt_cols(int gt) { return gt >= 3 ? 4 : gt; }
 inline int cache_tc_cols(int gt) {
     int n = 1;
@@ -64,8 +73,8 @@ inline int cache_tc_cols(int gt) {
 }
 
 bool cache_attn_tc_supported(const CacheView &c);
-cudaError_t launch_cache_attn_simt(CacheAttn &A, cudaStream_t st);
-cudaError_t launch_cache_attn_tc(CacheAttn &A, cudaStream_t st);
+cudaError_t launch_cache_attn_simt(const CacheAttn &A, cudaStream_t st);
+cudaError_t launch_cache_attn_tc(const CacheAttn &A, cudaStream_t st);
 cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st);
 cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st);
 

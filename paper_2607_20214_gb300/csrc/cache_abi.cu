@@ -93,29 +93,41 @@ int check_queries(const CacheView &c) {
         return set_last_error(ELSAA_ERR_UNSUPPORTED,
                               "T must be at most 64 and T * H / H_kv at most "
                               "128");
+    if ((long)c.B * c.H * c.T > 1L << 30)
+        return set_last_error(ELSAA_ERR_UNSUPPORTED,
+                              "B * H * T must be at most 2^30");
     return ELSAA_OK;
 }
 
-// Workspace of one call: tile counts | lse2 | pieces | scores (attention), or
+// Workspace of one call: split items | lse2 | pieces | scores (attention), or
 // page keys (select), or counts | kept (evict).
 struct Layout {
-    size_t prefix, lse2, part, scores, total;
+    size_t split, lse2, part, scores, total;
+    int cols, groups, ctas;
 };
-Layout attention_layout(const CacheView &c, int T, bool weights) {
-    const int gt = c.G * T;
-    size_t cols = (size_t)kCacheSimtCtas * cache_simt_cols(gt);
-    const size_t tc = (size_t)kCacheTcCtas * cache_tc_cols(gt);
-    if (tc > cols) cols = tc;
+Layout attention_layout(const CacheView &c, bool tc, bool weights) {
     Layout l;
-    l.prefix = 0;
-    l.lse2 = align256(sizeof(int) * ((size_t)c.B + 1));
-    l.part = l.lse2 + align256(sizeof(float) * (size_t)c.B * c.H * T);
-    l.scores = l.part + align256(sizeof(float) * 2 * cols * (c.d + 2));
-    l.total = l.scores;
+    const int gt = c.G * c.T;
+    l.cols = tc ? cache_tc_cols(gt) : cache_simt_cols(gt);
+    l.groups = (gt + l.cols - 1) / l.cols;
+    l.ctas = tc ? kCacheTcCtas : kCacheSimtCtas;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t was = at;
+        at += align256(bytes);
+        return was;
+    };
+    l.split = take(sizeof(CacheSplit) * l.ctas);
+    l.lse2 = take(sizeof(float) * (size_t)c.B * c.H * c.T);
+    l.part = take(sizeof(float) * 2 * l.ctas * l.cols * (c.d + 2));
+    l.scores = at;
     if (weights)
-        l.total += align256(sizeof(float) * (size_t)c.B * c.H * T *
-                            c.max_pages * c.ps);
+        take(sizeof(float) * (size_t)c.B * c.H * c.T * c.max_pages * c.ps);
+    l.total = at;
     return l;
+}
+bool on_tensor_cores(const elsaa_cache *cache, const CacheView &c) {
+    return cache->impl == ELSAA_IMPL_AUTO && cache_attn_tc_supported(c);
 }
 size_t select_bytes(const CacheView &c) {
     return align256(sizeof(uint32_t) * (size_t)c.B * c.Hkv * c.max_pages);
@@ -152,7 +164,9 @@ extern "C" int elsaa_cache_workspace_size(const elsaa_cache *cache, int T,
     if (rc != ELSAA_OK) return rc;
     if (keep < 0)
         return set_last_error(ELSAA_ERR_INVALID_ARG, "keep must be >= 0");
-    size_t n = attention_layout(c, T, weights != 0).total;
+    // columns come in powers of two: fewer tokens never need more
+    size_t n =
+        attention_layout(c, on_tensor_cores(cache, c), weights != 0).total;
     if (select_bytes(c) > n) n = select_bytes(c);
     if (evict_bytes(c, keep) > n) n = evict_bytes(c, keep);
     *bytes = n;
@@ -237,7 +251,8 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "n_sel must be positive and n_sel * page_size "
                               "fit in int32");
-    const Layout l = attention_layout(c, T, weight_out != nullptr);
+    const bool tc = on_tensor_cores(cache, c);
+    const Layout l = attention_layout(c, tc, weight_out != nullptr);
     rc = check_workspace(workspace, workspace_bytes, l.total);
     if (rc != ELSAA_OK) return rc;
     char *ws = (char *)workspace;
@@ -249,7 +264,10 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
     A.n_sel = pages ? n_sel : 0;
     A.weight_in = weight_in;
     A.weight_out = weight_out;
-    A.prefix = (int *)(ws + l.prefix);
+    A.cols = l.cols;
+    A.groups = l.groups;
+    A.ctas = l.ctas;
+    A.split = (CacheSplit *)(ws + l.split);
     A.part = (float *)(ws + l.part);
     if (weight_out) {
         A.lse2 = (float *)(ws + l.lse2);
@@ -257,7 +275,7 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
         A.slots = (long)c.max_pages * c.ps;
     }
     cudaStream_t st = (cudaStream_t)stream;
-    if (cache->impl == ELSAA_IMPL_AUTO && cache_attn_tc_supported(c))
+    if (tc)
         ELSAA_CACHE_LAUNCH("cache_attn_tc", st, launch_cache_attn_tc(A, st));
     else
         ELSAA_CACHE_LAUNCH("cache_attn_simt", st,

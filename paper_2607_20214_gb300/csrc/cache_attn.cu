@@ -22,28 +22,23 @@ constexpr float kLog2eF = 1.4426950408889634f;
 
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kSaThreads)
-    k_cache_attn_simt(const CacheAttn A) {
+    k_cache_attn_simt(const __grid_constant__ CacheAttn A) {
     wait_for_stream();
     constexpr int LPR = D / 16;   // lanes per row
     constexpr int R = 32 / LPR;   // rows per warp load
     constexpr int S = 32 / R;     // loads per tile
-    extern __shared__ int prefix[];
     __shared__ float accs[4][NG][D];
     __shared__ float ms[4][NG], ls[4][NG];
     const CacheView &c = A.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int sub = lane % LPR, rg = lane / LPR;
-    sum_tiles(A, prefix);
-    __syncthreads();
-    if (blockIdx.x == 0)
-        for (int i = tid; i <= c.B; i += kSaThreads) A.prefix[i] = prefix[i];
-    const Range r = cta_range(A, prefix, blockIdx.x);
+    extern __shared__ int prefix[];
+    Walk walk(divide<kSaThreads>(A, prefix));
     const float sl2 = c.scale * kLog2eF;
     const int GT = c.G * c.T;
 
-    for (long t = r.t0; t < r.t1;) {
-        const Item it = find_item(A, prefix, t);
-        const long end = min(it.a + it.tiles, r.t1);
+    while (walk.left > 0) {
+        const Item it = walk.next(A);
         const size_t bh = (size_t)it.b * c.Hkv + it.h;
         float qf[NG][16], acc[NG][16], m[NG], l[NG];
         int limit[NG];
@@ -51,7 +46,7 @@ __global__ void __launch_bounds__(kSaThreads)
         for (int g = 0; g < NG; ++g) {
             m[g] = -INFINITY;
             l[g] = 0.0f;
-            limit[g] = g < it.cols ? last_seen(A, it, it.col0 + g) : -1;
+            limit[g] = g < it.cols ? last_seen(A, it.len, it.n, it.col0 + g) : -1;
 #pragma unroll
             for (int i = 0; i < 16; ++i) qf[g][i] = acc[g][i] = 0.0f;
             if (limit[g] >= 0) {
@@ -62,9 +57,9 @@ __global__ void __launch_bounds__(kSaThreads)
                 load8(x + 8, qf[g] + 8);
             }
         }
-        for (; t < end; ++t) {
+        for (int t = it.off; t < it.off + it.count; ++t) {
             // lane i: token i of the warp's 32
-            const int w = (int)(t - it.a) * kCacheTile + warp * 32 + lane;
+            const int w = t * kCacheTile + warp * 32 + lane;
             int id = -1, pos = 0;
             float ks = 0.0f, vs = 0.0f;
             if (w < it.walk) {
@@ -120,8 +115,7 @@ __global__ void __launch_bounds__(kSaThreads)
             if (A.scores) {
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    const long at = (t - it.a) * kCacheTile + warp * 32 +
-                                    s * R + rg;
+                    const int at = t * kCacheTile + warp * 32 + s * R + rg;
                     if (sub == 0 && at < it.walk)
 #pragma unroll
                         for (int g = 0; g < NG; ++g)
@@ -191,8 +185,6 @@ __global__ void __launch_bounds__(kSaThreads)
             }
         }
         __syncthreads();
-        const bool whole = it.a >= r.t0 && it.a + it.tiles <= r.t1;
-        const int slot = it.a < r.t0 ? 0 : 1;
         for (int g = 0; g < it.cols; ++g) {
             float M = ms[0][g], L = 0.0f, x = 0.0f;
             for (int k = 1; k < 4; ++k) M = fmaxf(M, ms[k][g]);
@@ -203,15 +195,15 @@ __global__ void __launch_bounds__(kSaThreads)
                 if (tid < D) x += f * accs[k][g][tid];
             }
             const int col = it.col0 + g;
-            if (!whole) {
-                float *at = piece(A, blockIdx.x, slot, g);
+            if (it.slot >= 0) {
+                float *at = piece(A, blockIdx.x, it.slot, g);
                 if (tid < D) at[tid] = x;
                 if (tid == 0) {
                     at[D] = M;
                     at[D + 1] = L;
                 }
             } else {
-                if (tid == 0) store_lse(A, it, col, M, L);
+                if (tid == 0) store_lse(A, it.b, it.h, it.n, col, M, L);
                 if (tid < D && col % c.T < it.n)
                     store_o(A, query_row(A, it.b, it.h, col), tid,
                             L == 0.0f ? 0.0f : x / L);
@@ -223,64 +215,79 @@ __global__ void __launch_bounds__(kSaThreads)
 
 // ------------------------------------------------------------------- merge
 //
-// A column of an item that several CTAs shared: their pieces in order, so the
-// result does not depend on which CTA was first. 256 threads: the channels,
-// times groups of pieces read at once.
+// The columns of an item that began in CTA blockIdx.x and went on in others:
+// its pieces in order, so the result does not depend on which CTA was first.
+// A thread has a channel of a column; with few columns the pieces are shared
+// out among groups of threads, whose sums are added in order as well. A few
+// dependent reads of L2 is all it takes, so it is as short as its loads in
+// flight are many.
 constexpr int kMgThreads = 512;
+constexpr int kMgCols = 4;  // columns per block
 
 __global__ void __launch_bounds__(kMgThreads)
-    k_cache_merge(const CacheAttn A) {
+    k_cache_merge(const __grid_constant__ CacheAttn A) {
     wait_for_stream();
-    __shared__ float f[kCacheMaxCtas], sum[kMgThreads], red[kMgThreads / 32];
+    __shared__ float sm[kMgThreads], sl[kMgThreads], sx[kMgThreads];
+    const CacheSplit s = A.split[blockIdx.x];
+    if (s.pieces == 0) return;
     const CacheView &c = A.c;
-    const int GT = c.G * c.T, HC = c.Hkv * A.groups;
-    const int b = blockIdx.y, h = blockIdx.x / GT, col = blockIdx.x % GT;
-    const int tid = threadIdx.x;
-    const int tiles = A.prefix[b + 1] - A.prefix[b];
-    const long total = (long)A.prefix[c.B] * HC;
-    const long n = min((long)A.ctas, total);
-    if (tiles == 0) return;
-    const int group = col / A.cols;
-    const long a = (long)A.prefix[b] * HC +
-                   (long)(h * A.groups + group) * tiles;
-    const long c0 = range_owner(a, total, n);
-    const int pieces = (int)(range_owner(a + tiles - 1, total, n) - c0) + 1;
-    if (pieces == 1) return;
-    Item it;
-    it.b = b;
-    it.h = h;
-    it.n = fresh(c, b);
-    const int d = c.d, g = col - group * A.cols;
-    auto at = [&](int i) { return piece(A, c0 + i, i == 0 ? 1 : 0, g); };
-    float M = -INFINITY;
-    for (int i = tid; i < pieces; i += kMgThreads) {
-        f[i] = at(i)[d];
-        M = fmaxf(M, f[i]);
+    const int tid = threadIdx.x, d = c.d, ch = tid % d, group = tid / d;
+    const int cols = min(A.cols, kMgCols), parts = kMgThreads / d / cols;
+    const int g = blockIdx.y * kMgCols + group % cols, part = group / cols;
+    const int h = s.hc / A.groups, col = s.hc % A.groups * A.cols + g;
+    float M = -INFINITY, L = 0.0f, x = 0.0f;
+    if (part < parts) {
+        constexpr int U = 8;
+        for (int i0 = part; i0 < s.pieces; i0 += parts * U) {
+            float m[U], l[U], y[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * parts;
+                m[u] = -INFINITY;
+                l[u] = y[u] = 0.0f;
+                if (i < s.pieces) {
+                    const float *at = piece(A, blockIdx.x + i, i == 0, g);
+                    y[u] = at[ch];
+                    m[u] = at[d];
+                    l[u] = at[d + 1];
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            const float f = exp2f(M - ref);
+            x *= f;
+            L *= f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float e = exp2f(m[u] - ref);
+                x += e * y[u];
+                L += e * l[u];
+            }
+            M = top;
+        }
     }
-    M = warp_max(M);
-    if ((tid & 31) == 0) red[tid >> 5] = M;
-    __syncthreads();
-    for (int i = 0; i < kMgThreads / 32; ++i) M = fmaxf(M, red[i]);
-    const float ref = M == -INFINITY ? 0.0f : M;
-    for (int i = tid; i < pieces; i += kMgThreads) f[i] = exp2f(f[i] - ref);
-    __syncthreads();
-    const int ch = tid % d, part = tid / d, parts = kMgThreads / d;
-    float x = 0.0f, L = 0.0f;
-#pragma unroll 4
-    for (int i = part; i < pieces; i += parts) x += f[i] * at(i)[ch];
-    sum[tid] = x;
-    if (tid < 32) {
-        for (int i = tid; i < pieces; i += 32) L += f[i] * at(i)[d + 1];
-        L = warp_sum(L);
-        if (tid == 0) red[0] = L;
+    if (parts > 1) {
+        sm[tid] = M;
+        sl[tid] = L;
+        sx[tid] = x;
+        __syncthreads();
+        if (part > 0) return;
+        for (int p = 1; p < parts; ++p) {
+            const int o = tid + p * cols * d;
+            const float top = fmaxf(M, sm[o]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            const float f = exp2f(M - ref), e = exp2f(sm[o] - ref);
+            x = x * f + sx[o] * e;
+            L = L * f + sl[o] * e;
+            M = top;
+        }
     }
-    __syncthreads();
-    L = red[0];
-    if (tid == 0) store_lse(A, it, col, M, L);
-    if (part == 0 && col % c.T < it.n) {
-        for (int p = 1; p < parts; ++p) x += sum[p * d + ch];
-        store_o(A, query_row(A, b, h, col), ch, L == 0.0f ? 0.0f : x / L);
-    }
+    if (part > 0 || col >= c.G * c.T) return;
+    if (ch == 0) store_lse(A, s.b, h, s.n, col, M, L);
+    if (col % c.T < s.n)
+        store_o(A, query_row(A, s.b, h, col), ch, L == 0.0f ? 0.0f : x / L);
 }
 
 // ----------------------------------------------------------------- weights
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(kMgThreads)
 constexpr int kWtThreads = 128;
 
 __global__ void __launch_bounds__(kWtThreads)
-    k_cache_weights(const CacheAttn A) {
+    k_cache_weights(const __grid_constant__ CacheAttn A) {
     wait_for_stream();
     __shared__ int slot[kWtThreads / 16];
     __shared__ float lse[128];
@@ -363,17 +370,14 @@ cudaError_t launch_simt_d(const CacheAttn &A, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_cache_attn_simt(CacheAttn &A, cudaStream_t st) {
-    const int GT = A.c.G * A.c.T;
-    A.cols = cache_simt_cols(GT);
-    A.groups = (GT + A.cols - 1) / A.cols;
-    A.ctas = kCacheSimtCtas;
+cudaError_t launch_cache_attn_simt(const CacheAttn &A, cudaStream_t st) {
     return A.c.dtype == ELSAA_FP32 ? launch_simt_d<float>(A, st)
                                    : launch_simt_d<__nv_bfloat16>(A, st);
 }
 
 cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st) {
-    return launch_after(k_cache_merge, dim3(A.c.Hkv * A.c.G * A.c.T, A.c.B),
+    return launch_after(k_cache_merge,
+                        dim3(A.ctas, (A.cols + kMgCols - 1) / kMgCols),
                         kMgThreads, 0, st, A);
 }
 

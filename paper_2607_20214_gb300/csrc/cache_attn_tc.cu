@@ -28,8 +28,9 @@
 // added at the end.
 //
 // CTA: 4 softmax warps (a token a thread for S, a channel a thread for O), a
-// producer warp (page table, TMA of the pages' rows, scales) and a product
-// warp. The range's tiles run through rings of K and V buffers; S of tile
+// producer warp (page table, TMA of the pages' rows, scales), a product warp
+// and two query warps, which split the next item's queries while this one is
+// walked. The range's tiles run through rings of K and V buffers; S of tile
 // i + 1 is issued before O of tile i, so the softmax finds its next scores
 // ready. Two CTAs share an SM.
 #include "cache_common.cuh"
@@ -41,7 +42,10 @@ namespace {
 using namespace cache;
 using namespace tc;
 
-constexpr int kTaThreads = 192;
+constexpr int kTaThreads = 256;
+// Registers: 128 a thread at launch (two CTAs); the four softmax warps take
+// what the other four leave, 2 * 128 in all.
+constexpr int kTaRegsSoft = 184, kTaRegsOther = 72;
 constexpr float kLog2eF = 1.4426950408889634f;
 constexpr int kMaxPagesPerTile = kCacheTile / 16;
 
@@ -57,7 +61,7 @@ struct Cfg {
     static constexpr uint32_t kQ = N1 * D;
     static constexpr uint32_t kP = kCacheTile * W;
     static constexpr uint32_t kSmem =
-        1024 + (KS + VS) * kTile + kQ + 2 * kP;
+        1024 + (KS + VS) * kTile + 2 * kQ + 2 * kP;
     static constexpr uint32_t kCols = 2 * N1 + 2 * NO;
     static constexpr uint32_t kTmem = kCols <= 64    ? 64
                                       : kCols <= 128 ? 128
@@ -76,13 +80,6 @@ __device__ __forceinline__ uint64_t line_desc(uint32_t start, uint32_t line) {
     d |= (uint64_t)(line == 128 ? 2 : line == 64 ? 4 : 6) << 61;
     return d;
 }
-// Where the 16-byte chunk c of line r lies.
-template <int LINE>
-__device__ __forceinline__ uint32_t line_offset(int r, int c) {
-    constexpr int PER = LINE / 16;  // chunks of a line; 8 / PER lines a row
-    return (uint32_t)(r * LINE + ((c ^ ((r / (8 / PER)) & (PER - 1))) << 4));
-}
-
 // kind::f8f6f4 with e4m3 operands and fp32 sums.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N, bool a_mn,
                                                   bool b_mn) {
@@ -137,6 +134,24 @@ __device__ __forceinline__ void tmem_read(uint32_t t, float *x) {
     }
 }
 
+// V = 2 or 4 neighbouring bf16 values.
+template <int V>
+__device__ __forceinline__ void load_row(const __nv_bfloat16 *p, float *x) {
+    uint32_t w[V / 2];
+    if constexpr (V == 4) {
+        const uint2 a = *(const uint2 *)p;
+        w[0] = a.x;
+        w[1] = a.y;
+    } else {
+        w[0] = *(const uint32_t *)p;
+    }
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
 // Largest of the warp's values, in every lane.
 __device__ __forceinline__ float redux_max(float x) {
     float r;
@@ -155,7 +170,7 @@ struct TileMeta {
 
 struct Bars {
     uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], m_full[6];
-    uint64_t s_full[2], p_ready[2], o_full[2], q_ready, drain;
+    uint64_t s_full[2], p_ready[2], o_full[2], q_full[2], q_empty[2], drain;
 };
 
 template <int D, int NV>
@@ -163,33 +178,26 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     k_cache_attn_tc(const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV,
                     const __grid_constant__ CacheAttn A) {
-    wait_for_stream();
     using C = Cfg<D, NV>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Bars bars;
     __shared__ TileMeta meta[C::VS];
+    __shared__ Item items[2];
+    __shared__ float factors[2][NV];  // of an item's columns' scores
+    __shared__ int limits[2][NV];     // last positions that they see
     __shared__ uint32_t tbase;
     __shared__ int abort_flag;
     __shared__ __align__(16) float red[2][NV][4];
     __shared__ __align__(16) float fin[NV][4];
-    __shared__ float colscale[NV];
-    __shared__ int limit[NV];
     __shared__ float half[D == 64 ? NV * 64 : 1];
     volatile int *abort = &abort_flag;
     const CacheView &c = A.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t sK = base, sV = sK + C::KS * C::kTile;
-    const uint32_t sQ = sV + C::VS * C::kTile, sP = sQ + C::kQ;
-    int *prefix = (int *)(smem_raw + C::kSmem);
+    const uint32_t sQ = sV + C::VS * C::kTile, sP = sQ + 2 * C::kQ;
 
-    sum_tiles(A, prefix);
-    __syncthreads();
-    if (blockIdx.x == 0)
-        for (int i = tid; i <= c.B; i += kTaThreads) A.prefix[i] = prefix[i];
-    const Range r = cta_range(A, prefix, blockIdx.x);
-    if (r.t0 >= r.t1) return;
-
+    // set up while the kernel before ends
     if (warp == 5) tmem_alloc(&tbase, C::kTmem);
     if (tid == 0) {
         for (int s = 0; s < 6; ++s) {
@@ -203,8 +211,9 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             mbar_init(&bars.s_full[s], 1);
             mbar_init(&bars.p_ready[s], 128);
             mbar_init(&bars.o_full[s], 1);
+            mbar_init(&bars.q_full[s], 2);   // the query warps
+            mbar_init(&bars.q_empty[s], 5);  // products, four softmax warps
         }
-        mbar_init(&bars.q_ready, 128);
         mbar_init(&bars.drain, 1);
         abort_flag = 0;
         fence_mbar_init();
@@ -213,165 +222,257 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     __syncthreads();
     tc_fence_after();
     const uint32_t tm = tbase;
-    const int count = (int)(r.t1 - r.t0);
+    wait_for_stream();
+    const Start first =
+        divide<kTaThreads>(A, (int *)(smem_raw + C::kSmem));
+    const int count = first.count;
 
-    if (warp == 4) {
-        // ------------------------------------------------ pages and scales
-        const int pt = kCacheTile / c.ps;  // pages of a tile
-        Item it;
-        long end = r.t0;
-        bool ok = true;
-        int kn = 0, vn = 0;  // loads issued
-        for (int i = 0; i < count; ++i) {
-            const long t = r.t0 + i;
-            if (t == end) {
-                it = find_item(A, prefix, t);
-                end = min(it.a + it.tiles, r.t1);
-            }
-            // lane l: the tile's l-th page
-            const int e = (int)(t - it.a) * pt + lane;
-            int p = -1, id = -1, rows = 0;
-            if (lane < pt && (long)e * c.ps < it.walk)
-                p = A.pages
-                        ? A.pages[((size_t)it.b * c.Hkv + it.h) * A.n_sel + e]
-                        : e;
-            if (p >= 0 && p < c.max_pages) {
-                rows = min(it.len - p * c.ps, c.ps);
-                if (rows > 0) id = page_id(c, it.b, p);
-            }
-            if (id < 0) rows = 0;
-            const int ph = id * c.Hkv + it.h;  // fits: checked by the host
-            const uint32_t live = __ballot_sync(0xffffffffu, id >= 0);
-            const uint32_t bytes = __popc(live) * c.ps * D;
-            const int ks = i % C::KS, vs = i % C::VS;
-            if (i >= C::KS)
-                ok = __all_sync(0xffffffffu,
-                                mbar_wait_or_abort(&bars.k_empty[ks],
-                                                   (i / C::KS - 1) & 1, abort,
-                                                   c.status, 180));
-            if (!ok) break;
-            if (lane == 0) mbar_expect_tx(&bars.k_full[ks], bytes);
-            __syncwarp();
-            if (id >= 0)
-                tma_load_2d(sK + ks * C::kTile + lane * c.ps * D, &tmK, 0,
-                            ph * c.ps, &bars.k_full[ks]);
-            ++kn;
-            float k_sc = 0.0f, v_sc = 0.0f;
-            if (id >= 0) {
-                k_sc = c.ks[ph];
-                v_sc = c.vs[ph];
-            }
-            if (i >= C::VS)
-                ok = __all_sync(0xffffffffu,
-                                mbar_wait_or_abort(&bars.v_empty[vs],
-                                                   (i / C::VS - 1) & 1, abort,
-                                                   c.status, 181));
-            if (!ok) break;
-            if (lane == 0) mbar_expect_tx(&bars.v_full[vs], bytes);
-            __syncwarp();
-            if (id >= 0)
-                tma_load_2d(sV + vs * C::kTile + lane * c.ps * D, &tmV, 0,
-                            D == 128 ? ph * c.ps : ph * c.ps / 2,
-                            &bars.v_full[vs]);
-            ++vn;
-            const float vmax = warp_max(v_sc);
-            if (lane < pt) {
-                TileMeta &m = meta[vs];
-                m.ks[lane] = k_sc;
-                m.vs[lane] = vmax > 0.0f ? v_sc / vmax : 0.0f;
-                m.pos[lane] = p * c.ps;
-                m.rows[lane] = rows;
-                if (lane == 0) m.vmax = vmax;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.m_full[vs]);
-        }
-        // whatever was asked for has arrived before the CTA ends
-        for (int j = max(0, kn - C::KS); j < kn; ++j)
-            mbar_wait(&bars.k_full[j % C::KS], (j / C::KS) & 1, c.status,
-                      182);
-        for (int j = max(0, vn - C::VS); j < vn; ++j)
-            mbar_wait(&bars.v_full[j % C::VS], (j / C::VS) & 1, c.status,
-                      183);
-    } else if (warp == 5) {
-        // -------------------------------------------------------- products
-        const bool el = elect_one();
-        auto wait = [&](uint64_t *bar, uint32_t par, int site) {
-            return __all_sync(0xffffffffu,
-                              mbar_wait_or_abort(bar, par, abort, c.status,
-                                                 site));
-        };
-        const uint32_t id_s = idesc_e4m3(128, C::N1, false, false);
-        const uint32_t id_o = idesc_e4m3(128, C::NP, true, true);
-        const uint64_t dQ = line_desc(sQ, D);
-        long end = r.t0;
-        int item = 0;
-        bool ok = true;
-        auto values = [&](int j) {  // O of tile j
-            const int vs = j % C::VS, b = j & 1;
-            if (!wait(&bars.v_full[vs], (j / C::VS) & 1, 185)) return false;
-            if (!wait(&bars.p_ready[b], (j >> 1) & 1, 186)) return false;
-            tc_fence_after();
-            if (el) {
-                const uint64_t dV = line_desc(sV + vs * C::kTile, 128);
-                const uint64_t dP = line_desc(sP + b * C::kP, C::W);
-                const uint32_t o = tm + 2 * C::N1 + b * C::NO;
-                if (D == 128) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        mma_e4m3(o, desc_at(dV, x * 4096),
-                                 desc_at(dP, x * 32 * C::W), id_o, x > 0);
-                } else {
-#pragma unroll
-                    for (int par = 0; par < 2; ++par)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-                            mma_e4m3(o + par * C::NP, desc_at(dV, x * 4096),
-                                     desc_at(dP, (par * 64 + x * 32) * C::W),
-                                     id_o, x > 0);
+    if (warp >= 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
+            kTaRegsOther));
+        if (warp == 4) {
+            // ------------------------------------------------ pages and scales
+            const int pt = kCacheTile / c.ps;  // pages of a tile
+            Walk walk(first);
+            Item it;
+            it.count = it.off = 0;
+            bool ok = true;
+            int kn = 0, vn = 0;  // loads issued
+            int t = 0;           // tile within the item
+            for (int i = 0; i < count; ++i, ++t) {
+                if (t == it.off + it.count) {
+                    it = walk.next(A);
+                    t = it.off;
                 }
-                mma_commit(&bars.o_full[b]);
-                mma_commit(&bars.v_empty[vs]);
-            }
-            __syncwarp();
-            return true;
-        };
-        for (int i = 0; i < count && ok; ++i) {
-            const long t = r.t0 + i;
-            const bool next = t == end;
-            if (next) {
-                const Item it = find_item(A, prefix, t);
-                end = min(it.a + it.tiles, r.t1);
-                // the softmax ends an item before it splits the next one's
-                // queries: its last O goes first
-                if (i > 0) ok = values(i - 1);
+                // lane l: the tile's l-th page
+                const int e = t * pt + lane;
+                int p = -1, id = -1, rows = 0;
+                if (lane < pt && (long)e * c.ps < it.walk)
+                    p = A.pages ? A.pages[((size_t)it.b * c.Hkv + it.h) *
+                                              A.n_sel + e]
+                                : e;
+                if (p >= 0 && p < c.max_pages) {
+                    rows = min(it.len - p * c.ps, c.ps);
+                    if (rows > 0) id = page_id(c, it.b, p);
+                }
+                if (id < 0) rows = 0;
+                const int ph = id * c.Hkv + it.h;  // fits: checked by the host
+                const uint32_t live = __ballot_sync(0xffffffffu, id >= 0);
+                const uint32_t bytes = __popc(live) * c.ps * D;
+                const int ks = i % C::KS, vs = i % C::VS;
+                if (i >= C::KS)
+                    ok = __all_sync(0xffffffffu,
+                                    mbar_wait_or_abort(&bars.k_empty[ks],
+                                                       (i / C::KS - 1) & 1, abort,
+                                                       c.status, 180));
                 if (!ok) break;
-                ok = wait(&bars.q_ready, item & 1, 187);
-                ++item;
+                if (lane == 0) mbar_expect_tx(&bars.k_full[ks], bytes);
+                __syncwarp();
+                if (id >= 0)
+                    tma_load_2d(sK + ks * C::kTile + lane * c.ps * D, &tmK, 0,
+                                ph * c.ps, &bars.k_full[ks]);
+                ++kn;
+                float k_sc = 0.0f, v_sc = 0.0f;
+                if (id >= 0) {
+                    k_sc = c.ks[ph];
+                    v_sc = c.vs[ph];
+                }
+                if (i >= C::VS)
+                    ok = __all_sync(0xffffffffu,
+                                    mbar_wait_or_abort(&bars.v_empty[vs],
+                                                       (i / C::VS - 1) & 1, abort,
+                                                       c.status, 181));
                 if (!ok) break;
+                if (lane == 0) mbar_expect_tx(&bars.v_full[vs], bytes);
+                __syncwarp();
+                if (id >= 0)
+                    tma_load_2d(sV + vs * C::kTile + lane * c.ps * D, &tmV, 0,
+                                D == 128 ? ph * c.ps : ph * c.ps / 2,
+                                &bars.v_full[vs]);
+                ++vn;
+                const float vmax = warp_max(v_sc);
+                if (lane < pt) {
+                    TileMeta &m = meta[vs];
+                    m.ks[lane] = k_sc;
+                    m.vs[lane] = vmax > 0.0f ? v_sc / vmax : 0.0f;
+                    m.pos[lane] = p * c.ps;
+                    m.rows[lane] = rows;
+                    if (lane == 0) m.vmax = vmax;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.m_full[vs]);
             }
-            const int ks = i % C::KS, b = i & 1;
-            ok = wait(&bars.k_full[ks], (i / C::KS) & 1, 188);
-            if (!ok) break;
-            tc_fence_after();
-            if (el) {
-                const uint64_t dK = line_desc(sK + ks * C::kTile, D);
+            // whatever was asked for has arrived before the CTA ends
+            for (int j = max(0, kn - C::KS); j < kn; ++j)
+                mbar_wait(&bars.k_full[j % C::KS], (j / C::KS) & 1, c.status,
+                          182);
+            for (int j = max(0, vn - C::VS); j < vn; ++j)
+                mbar_wait(&bars.v_full[j % C::VS], (j / C::VS) & 1, c.status,
+                          183);
+        } else if (warp == 5) {
+            // -------------------------------------------------------- products
+            const bool el = elect_one();
+            auto wait = [&](uint64_t *bar, uint32_t par, int site) {
+                return __all_sync(0xffffffffu,
+                                  mbar_wait_or_abort(bar, par, abort, c.status,
+                                                     site));
+            };
+            const uint32_t id_s = idesc_e4m3(128, C::N1, false, false);
+            const uint32_t id_o = idesc_e4m3(128, C::NP, true, true);
+            bool ok = true;
+            auto values = [&](int j) {  // O of tile j
+                const int vs = j % C::VS, b = j & 1;
+                if (!wait(&bars.v_full[vs], (j / C::VS) & 1, 185)) return false;
+                if (!wait(&bars.p_ready[b], (j >> 1) & 1, 186)) return false;
+                tc_fence_after();
+                if (el) {
+                    const uint64_t dV = line_desc(sV + vs * C::kTile, 128);
+                    const uint64_t dP = line_desc(sP + b * C::kP, C::W);
+                    const uint32_t o = tm + 2 * C::N1 + b * C::NO;
+                    if (D == 128) {
 #pragma unroll
-                for (int x = 0; x < D / 32; ++x)
-                    mma_e4m3(tm + b * C::N1, desc_at(dK, x * 32),
-                             desc_at(dQ, x * 32), id_s, x > 0);
-                mma_commit(&bars.s_full[b]);
-                mma_commit(&bars.k_empty[ks]);
+                        for (int x = 0; x < 4; ++x)
+                            mma_e4m3(o, desc_at(dV, x * 4096),
+                                     desc_at(dP, x * 32 * C::W), id_o, x > 0);
+                    } else {
+#pragma unroll
+                        for (int par = 0; par < 2; ++par)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)
+                                mma_e4m3(o + par * C::NP, desc_at(dV, x * 4096),
+                                         desc_at(dP, (par * 64 + x * 32) * C::W),
+                                         id_o, x > 0);
+                    }
+                    mma_commit(&bars.o_full[b]);
+                    mma_commit(&bars.v_empty[vs]);
+                }
+                __syncwarp();
+                return true;
+            };
+            int item = 0, left = 0;  // tiles of the item
+            uint64_t dQ = 0;
+            for (int i = 0; i < count && ok; ++i) {
+                if (left == 0) {
+                    ok = wait(&bars.q_full[item & 1], (item >> 1) & 1, 187);
+                    if (!ok) break;
+                    left = items[item & 1].count;
+                    dQ = line_desc(sQ + (item & 1) * C::kQ, D);
+                    ++item;
+                }
+                --left;
+                const int ks = i % C::KS, b = i & 1;
+                ok = wait(&bars.k_full[ks], (i / C::KS) & 1, 188);
+                if (!ok) break;
+                tc_fence_after();
+                if (el) {
+                    const uint64_t dK = line_desc(sK + ks * C::kTile, D);
+#pragma unroll
+                    for (int x = 0; x < D / 32; ++x)
+                        mma_e4m3(tm + b * C::N1, desc_at(dK, x * 32),
+                                 desc_at(dQ, x * 32), id_s, x > 0);
+                    mma_commit(&bars.s_full[b]);
+                    mma_commit(&bars.k_empty[ks]);
+                    if (left == 0) mma_commit(&bars.q_empty[(item - 1) & 1]);
+                }
+                __syncwarp();
+                if (i > 0) ok = values(i - 1);
             }
+            if (ok && count > 0) values(count - 1);
+            // every product is complete before the tensor memory is given back
+            if (el) mma_commit(&bars.drain);
+            mbar_wait(&bars.drain, 0, c.status, 189);
             __syncwarp();
-            if (i > 0 && !next) ok = values(i - 1);
+        } else if (warp >= 6) {
+            // --------------------------------------------------------- queries
+            Walk walk(first);
+            constexpr int V = D / 32;  // elements a lane
+            for (int k = 0; walk.left > 0; ++k) {
+                const Item it = walk.next(A);
+                const int qs = k & 1;
+                bool ok = true;
+                // this warp's columns, a few at a time; the first are read before
+                // the buffer is free
+                constexpr int Z = (NV + 1) / 2, ZB = Z < 4 ? Z : 4;
+#pragma unroll 1
+                for (int z0 = 0; z0 < Z; z0 += ZB) {
+                    float x[ZB][V];
+                    int lim[ZB];
+#pragma unroll
+                    for (int z = 0; z < ZB; ++z) {
+                        const int g = 2 * (z0 + z) + warp - 6;
+                        lim[z] = g < it.cols
+                                     ? last_seen(A, it.len, it.n, it.col0 + g)
+                                     : -1;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) x[z][i] = 0.0f;
+                        if (lim[z] >= 0)
+                            load_row<V>((const __nv_bfloat16 *)A.q +
+                                            query_row(A, it.b, it.h, it.col0 + g) *
+                                                D + lane * V,
+                                        x[z]);
+                    }
+                    if (z0 == 0 && k >= 2)
+                        ok = __all_sync(0xffffffffu,
+                                        mbar_wait_or_abort(&bars.q_empty[qs],
+                                                           ((k >> 1) - 1) & 1,
+                                                           abort, c.status, 184));
+                    if (!ok) break;
+#pragma unroll
+                    for (int z = 0; z < ZB; ++z) {
+                        const int g = 2 * (z0 + z) + warp - 6;
+                        if (g >= NV) break;
+                        float amax = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < V; ++i)
+                            amax = fmaxf(amax, magnitude(x[z][i]));
+                        const int e = least_exponent(warp_max(amax), 0x600000u, 8,
+                                                     -100, kCacheExpHigh);
+                        const float f = pow2(-e);
+                        uint32_t w[2] = {0, 0};
+#pragma unroll
+                        for (int i = 0; i < V; i += 2) {
+                            // an infinity has no split: it counts as NaN
+                            const float y0 = isinf(x[z][i]) ? NAN : x[z][i] * f;
+                            const float y1 =
+                                isinf(x[z][i + 1]) ? NAN : x[z][i + 1] * f;
+                            const uint32_t hi = e4m3x2(y0, y1);
+                            const float2 u = from_e4m3x2(hi);
+                            w[0] |= hi << (8 * i);
+                            w[1] |= e4m3x2((y0 - u.x) * 16.0f,
+                                           (y1 - u.y) * 16.0f)
+                                    << (8 * i);
+                        }
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            const uint32_t at =
+                                sQ + qs * C::kQ +
+                                line_offset<D>(p * NV + g, (lane * V) >> 4) +
+                                ((lane * V) & 15);
+                            if (V == 4)
+                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(at),
+                                             "r"(w[p])
+                                             : "memory");
+                            else
+                                asm volatile("st.shared.u16 [%0], %1;" ::"r"(at),
+                                             "h"((uint16_t)w[p])
+                                             : "memory");
+                        }
+                        if (lane == 0) {
+                            factors[qs][g] = pow2(e) * (c.scale * kLog2eF);
+                            limits[qs][g] = lim[z];
+                        }
+                    }
+                }
+                if (!ok) break;
+                if (warp == 6 && lane == 0) items[qs] = it;
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.q_full[qs]);
+            }
         }
-        if (ok) values(count - 1);
-        // every product is complete before the tensor memory is given back
-        if (el) mma_commit(&bars.drain);
-        mbar_wait(&bars.drain, 0, c.status, 189);
-        __syncwarp();
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(
+            kTaRegsSoft));
         // --------------------------------------------------------- softmax
         auto wait = [&](uint64_t *bar, uint32_t par, int site) {
             return __all_sync(0xffffffffu,
@@ -380,10 +481,9 @@ __global__ void __launch_bounds__(kTaThreads, 2)
         };
         const int GT = c.G * c.T;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        const float sl2 = c.scale * kLog2eF;
         float acc[NV], l[NV], M[NV], al[NV], be[NV];
         Item it;
-        long end = r.t0;
+        int item = 0, t = 0, end = 0;
         bool ok = true;
         // acc of the current item takes tile j's O
         auto take = [&](int j) {
@@ -402,70 +502,14 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             tc_fence_before();
             return fine;
         };
-        for (int i = 0; i < count; ++i) {
-            const long t = r.t0 + i;
+        for (int i = 0; i < count; ++i, ++t) {
             if (t == end) {
-                it = find_item(A, prefix, t);
-                end = min(it.a + it.tiles, r.t1);
-                // every score of the item before is read, so its queries may
-                // go: a warp splits a query, D / 32 elements a lane
-                constexpr int V = D / 32;
-                for (int g = warp; g < NV; g += 4) {
-                    const int col = it.col0 + g;
-                    const int lim =
-                        g < it.cols ? last_seen(A, it, col) : -1;
-                    float x[V], amax = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < V; ++k) x[k] = 0.0f;
-                    if (lim >= 0) {
-                        const __nv_bfloat16 *src =
-                            (const __nv_bfloat16 *)A.q +
-                            query_row(A, it.b, it.h, col) * D + lane * V;
-#pragma unroll
-                        for (int k = 0; k < V; ++k) {
-                            x[k] = __bfloat162float(src[k]);
-                            amax = fmaxf(amax, magnitude(x[k]));
-                        }
-                    }
-                    const int e = least_exponent(warp_max(amax), 0x600000u, 8,
-                                                 -100, kCacheExpHigh);
-                    const float f = pow2(-e);
-                    uint32_t hi = 0, lo = 0;
-#pragma unroll
-                    for (int k = 0; k < V; k += 2) {
-                        // an infinity has no split: it counts as NaN
-                        const float a = isinf(x[k]) ? NAN : x[k] * f;
-                        const float b = isinf(x[k + 1]) ? NAN : x[k + 1] * f;
-                        const uint32_t h = e4m3x2(a, b);
-                        const float2 y = from_e4m3x2(h);
-                        hi |= h << (8 * k);
-                        lo |= e4m3x2((a - y.x) * 16.0f, (b - y.y) * 16.0f)
-                              << (8 * k);
-                    }
-                    const int byte = lane * V;
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const uint32_t at =
-                            sQ + line_offset<D>(z * NV + g, byte >> 4) +
-                            (byte & 15);
-                        const uint32_t w = z ? lo : hi;
-                        if (V == 4)
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at),
-                                         "r"(w)
-                                         : "memory");
-                        else
-                            asm volatile("st.shared.u16 [%0], %1;" ::"r"(at),
-                                         "h"((uint16_t)w)
-                                         : "memory");
-                    }
-                    if (lane == 0) {
-                        colscale[g] = pow2(e) * sl2;
-                        limit[g] = lim;
-                    }
-                }
-                fence_proxy_async_smem();
-                named_sync(1, 128);
-                mbar_arrive(&bars.q_ready);
+                const int qs = item & 1;
+                ok = wait(&bars.q_full[qs], (item >> 1) & 1, 195) && ok;
+                it = ok ? items[qs] : Item{};
+                t = it.off;
+                end = it.off + it.count;
+                ++item;
 #pragma unroll
                 for (int g = 0; g < NV; ++g) {
                     acc[g] = l[g] = al[g] = be[g] = 0.0f;
@@ -487,14 +531,21 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 tmem_read<2 * NV>(tm + lanes + b * C::N1, x);
                 tmem_wait_ld();
                 const bool all = pos <= it.len - it.n;
+                const float *factor = factors[(item - 1) & 1];
+                const int *limit = limits[(item - 1) & 1];
 #pragma unroll
                 for (int g = 0; g < NV; ++g) {
-                    s[g] = (x[g] + 0.0625f * x[NV + g]) * (ks * colscale[g]);
-                    if (!in || (!all && pos > limit[g])) s[g] = -INFINITY;
+                    s[g] = (x[g] + 0.0625f * x[NV + g]) * (ks * factor[g]);
+                    if (!in || (!all && pos > limit[g]))
+                        s[g] = -INFINITY;
                 }
             }
+            if (t + 1 == end) {  // the queries may go
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.q_empty[(item - 1) & 1]);
+            }
             if (A.scores) {
-                const long w = (t - it.a) * kCacheTile + tid;
+                const int w = t * kCacheTile + tid;
                 if (w < it.walk) {
                     float *at = A.scores +
                                 (((size_t)it.b * c.Hkv + it.h) * GT +
@@ -592,7 +643,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             fence_proxy_async_smem();
             tc_fence_before();
             mbar_arrive(&bars.p_ready[b]);
-            if (t > it.a && i > 0) ok = take(i - 1) && ok;
+            if (t > it.off) ok = take(i - 1) && ok;
 #pragma unroll
             for (int g = 0; g < NV; ++g) {
                 al[g] = al2[g];
@@ -610,8 +661,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             }
             ok = named_sync_and(1, 128, ok);
             if (!ok) break;
-            const bool whole = it.a >= r.t0 && it.a + it.tiles <= r.t1;
-            const int slot = it.a < r.t0 ? 0 : 1;
+            if (i + 1 == count && tid == 0) let_next_launch();
 #pragma unroll
             for (int g = 0; g < NV; ++g) {
                 if (g >= it.cols) break;
@@ -620,15 +670,16 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 const int col = it.col0 + g;
                 float x = acc[g];
                 if (D == 64 && tid < 64) x += half[g * 64 + tid];
-                if (!whole) {
-                    float *at = piece(A, blockIdx.x, slot, g);
+                if (it.slot >= 0) {
+                    float *at = piece(A, blockIdx.x, it.slot, g);
                     if (tid < D) at[tid] = x;
                     if (tid == 0) {
                         at[D] = M[g];
                         at[D + 1] = L;
                     }
                 } else {
-                    if (tid == 0) store_lse(A, it, col, M[g], L);
+                    if (tid == 0)
+                        store_lse(A, it.b, it.h, it.n, col, M[g], L);
                     if (tid < D && col % c.T < it.n)
                         store_o(A, query_row(A, it.b, it.h, col), tid,
                                 L == 0.0f ? 0.0f : x / L);
@@ -675,11 +726,7 @@ bool cache_attn_tc_supported(const CacheView &c) {
     return c.dtype == ELSAA_BF16 && (c.d == 64 || c.d == 128);
 }
 
-cudaError_t launch_cache_attn_tc(CacheAttn &A, cudaStream_t st) {
-    const int GT = A.c.G * A.c.T;
-    A.cols = cache_tc_cols(GT);
-    A.groups = (GT + A.cols - 1) / A.cols;
-    A.ctas = kCacheTcCtas;
+cudaError_t launch_cache_attn_tc(const CacheAttn &A, cudaStream_t st) {
     return A.c.d == 64 ? launch_cols<64>(A, st) : launch_cols<128>(A, st);
 }
 

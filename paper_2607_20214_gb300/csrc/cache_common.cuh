@@ -101,6 +101,14 @@ __device__ __forceinline__ void from_e4m3x4(uint32_t w, float *x) {
     x[3] = b.y;
 }
 
+// Shared-memory lines of LINE = 32, 64 or 128 bytes with the swizzle of that
+// width: where the 16-byte chunk c of line r lies.
+template <int LINE>
+__host__ __device__ __forceinline__ uint32_t line_offset(int r, int c) {
+    constexpr int PER = LINE / 16;  // chunks of a line; 8 / PER lines a row
+    return (uint32_t)(r * LINE + ((c ^ ((r / (8 / PER)) & (PER - 1))) << 4));
+}
+
 // Rows of 8 elements of the caller's type.
 __device__ __forceinline__ void load8(const float *p, float *x) {
     const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
@@ -120,99 +128,164 @@ __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *x) {
 // --------------------------------------------------- attention: the division
 //
 // Every K/V head and column group of a sequence is an item of
-// ceil(tokens / kCacheTile) tiles (one at least, so that a query without keys
+// ceil(rows / kCacheTile) tiles (one at least, so that a query without keys
 // gets its row). The tiles of all items, one after the other, are cut into
-// `ctas` equal ranges, so that ragged lengths load the SMs evenly; an item
-// that a cut crosses is written as pieces and merged afterwards.
+// equal ranges, one per CTA, so that ragged lengths load the SMs evenly; an
+// item that a cut crosses is written as pieces and merged afterwards. Every
+// CTA finds its range by itself from the lengths: a launch that did it for all
+// cost more than the B loads and the scan.
 
-// Tokens (or listed rows) that sequence b's heads walk, and its tiles.
-__device__ __forceinline__ int walk(const CacheAttn &A, int b) {
-    if (fresh(A.c, b) == 0) return -1;
-    const int n = tokens(A.c, b);
-    if (!A.pages) return n;
-    const int np = (n + A.c.ps - 1) / A.c.ps;
-    return min(np, A.n_sel) * A.c.ps;
-}
-__device__ __forceinline__ int walk_tiles(int n) {
-    return n < 0 ? 0 : max(1, (n + kCacheTile - 1) / kCacheTile);
+// What a sequence's heads walk.
+struct Seq {
+    int len, n;  // tokens held, new ones
+    int walk;    // tokens, or rows of listed pages
+    int tiles;   // of a head's item; 0 without queries
+};
+__device__ __forceinline__ Seq sequence(const CacheAttn &A, int b) {
+    Seq s;
+    s.len = tokens(A.c, b);
+    s.n = fresh(A.c, b);
+    s.walk = A.pages ? min((s.len + A.c.ps - 1) / A.c.ps, A.n_sel) * A.c.ps
+                     : s.len;
+    s.tiles =
+        s.n == 0 ? 0 : max(1, (s.walk + kCacheTile - 1) / kCacheTile);
+    return s;
 }
 
-// prefix[b] = tiles of one head's items of the sequences before b, by the
-// first warp; the CTA synchronises afterwards.
-__device__ __forceinline__ void sum_tiles(const CacheAttn &A, int *prefix) {
-    const int lane = threadIdx.x & 31;
-    if (threadIdx.x >= 32) return;
-    int base = 0;
-    for (int b0 = 0; b0 < A.c.B; b0 += 32) {
-        const int b = b0 + lane;
-        int x = b < A.c.B ? walk_tiles(walk(A, b)) : 0;
+struct Start {
+    int b, hc, off;  // sequence, head and group, first tile of that item
+    int count;       // tiles of this CTA
+};
+
+// All NT threads of the CTA; prefix: B + 1 ints of shared memory. Writes the
+// CTA's entry of A.split.
+template <int NT>
+__device__ __forceinline__ Start divide(const CacheAttn &A, int *prefix) {
+    __shared__ int warps[NT / 32], some[NT / 32];
+    __shared__ Start mine;
+    const CacheView &c = A.c;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int base = 0, items = 0;
+    for (int b0 = 0; b0 < c.B; b0 += NT) {
+        const int b = b0 + tid;
+        int x = b < c.B ? sequence(A, b).tiles : 0;
+        const int own = __popc(__ballot_sync(0xffffffffu, x > 0));
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        if (b < A.c.B) prefix[b + 1] = base + x;
-        base += __shfl_sync(0xffffffffu, x, 31);
+        if (lane == 31) {
+            warps[warp] = x;
+            some[warp] = own;
+        }
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) x += warps[w];
+        if (b < c.B) prefix[b + 1] = base + x;
+        for (int w = 0; w < NT / 32; ++w) {
+            base += warps[w];
+            items += some[w];
+        }
+        __syncthreads();
     }
-    if (lane == 0) prefix[0] = 0;
+    if (tid == 0) prefix[0] = 0;
+    __syncthreads();
+    const int HC = c.Hkv * A.groups, k = blockIdx.x;
+    const long total = (long)base * HC;
+    const long n =
+        min(min((long)A.ctas, total), (long)items * HC * kCacheMaxPieces);
+    // the sequence of tile t: prefix[b] HC <= t < prefix[b + 1] HC
+    auto find = [&](long t) {
+        int lo = 0, hi = c.B;
+        while (hi - lo > 1) {
+            const int m = (lo + hi) >> 1;
+            if ((long)prefix[m] * HC <= t)
+                lo = m;
+            else
+                hi = m;
+        }
+        return lo;
+    };
+    const long t0 = k < n ? total * k / n : 0;
+    const long t1 = k < n ? total * (k + 1) / n : 0;
+    if (tid == 0) {
+        Start s = {0, 0, 0, (int)(t1 - t0)};
+        if (k < n) {
+            s.b = find(t0);
+            const int tiles = prefix[s.b + 1] - prefix[s.b];
+            const int in = (int)(t0 - (long)prefix[s.b] * HC);
+            s.hc = in / tiles;
+            s.off = in % tiles;
+        }
+        mine = s;
+    } else if (tid == 32) {
+        // an item that begins here and goes on behind t1
+        CacheSplit s = {0, 0, 0, 0};
+        if (k < n) {
+            s.b = find(t1 - 1);
+            const int tiles = prefix[s.b + 1] - prefix[s.b];
+            const long first = (long)prefix[s.b] * HC;
+            s.hc = (int)(t1 - 1 - first) / tiles;
+            const long a = first + (long)s.hc * tiles;
+            if (a >= t0 && a + tiles > t1) {
+                s.pieces = (int)range_owner(a + tiles - 1, total, n) - k + 1;
+                s.n = fresh(c, s.b);
+            }
+        }
+        A.split[k] = s;
+    }
+    __syncthreads();
+    return mine;
 }
 
-struct Range {
-    long total, n;  // tiles of the call, CTAs that have some
-    long t0, t1;    // of this CTA
+// A CTA's share of one item.
+struct alignas(16) Item {
+    int b, h, col0, cols;   // sequence, K/V head, its columns of the G T
+    int len, n, walk;       // as in Seq
+    int off, count;         // tiles [off, off + count) of it
+    int slot;               // -1: the whole item; else 0 if it began in an
+                            // earlier CTA, 1 if here
 };
-__device__ __forceinline__ Range cta_range(const CacheAttn &A,
-                                           const int *prefix, int cta) {
-    Range r;
-    r.total = (long)prefix[A.c.B] * A.c.Hkv * A.groups;
-    r.n = min((long)A.ctas, r.total);
-    r.t0 = cta < r.n ? r.total * cta / r.n : r.total;
-    r.t1 = cta < r.n ? r.total * (cta + 1) / r.n : r.total;
-    return r;
-}
-
-// The item that tile t belongs to.
-struct Item {
-    int b, h, group;   // sequence, K/V head, column group
-    long a;            // its first tile
-    int tiles;
-    int len, n;        // tokens held, new ones
-    int walk;          // rows walked
-    int col0, cols;    // its columns of the head's G T
-};
-__device__ __forceinline__ Item find_item(const CacheAttn &A,
-                                          const int *prefix, long t) {
-    const int HC = A.c.Hkv * A.groups;
-    int lo = 0, hi = A.c.B;  // prefix[lo] HC <= t < prefix[hi] HC
-    while (hi - lo > 1) {
-        const int m = (lo + hi) >> 1;
-        if ((long)prefix[m] * HC <= t)
-            lo = m;
-        else
-            hi = m;
+// Walks the items of a CTA's range.
+struct Walk {
+    int b, hc, off, left;
+    __device__ __forceinline__ Walk(const Start &s)
+        : b(s.b), hc(s.hc), off(s.off), left(s.count) {}
+    __device__ __forceinline__ Item next(const CacheAttn &A) {
+        Seq s = sequence(A, b);
+        while (s.tiles == 0) s = sequence(A, ++b);  // left > 0: there is one
+        Item it;
+        it.b = b;
+        it.h = hc / A.groups;
+        it.col0 = hc % A.groups * A.cols;
+        it.cols = min(A.cols, A.c.G * A.c.T - it.col0);
+        it.len = s.len;
+        it.n = s.n;
+        it.walk = s.walk;
+        it.off = off;
+        it.count = min(s.tiles - off, left);
+        it.slot = it.count == s.tiles ? -1 : off > 0 ? 0 : 1;
+        left -= it.count;
+        off = 0;
+        if (++hc == A.c.Hkv * A.groups) {
+            hc = 0;
+            ++b;
+        }
+        return it;
     }
-    Item it;
-    it.b = lo;
-    it.tiles = prefix[lo + 1] - prefix[lo];
-    const long first = (long)prefix[lo] * HC;
-    const int hc = (int)((t - first) / it.tiles);
-    it.a = first + (long)hc * it.tiles;
-    it.h = hc / A.groups;
-    it.group = hc % A.groups;
-    it.n = fresh(A.c, lo);
-    it.len = tokens(A.c, lo);
-    it.walk = walk(A, lo);
-    it.col0 = it.group * A.cols;
-    it.cols = min(A.cols, A.c.G * A.c.T - it.col0);
-    return it;
+};
+
+// The dependent launch may be set up from here on.
+__device__ __forceinline__ void let_next_launch() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // The last position that column `col` (g T + t) of an item sees, -1 if none
 // or if the column is no query.
-__device__ __forceinline__ int last_seen(const CacheAttn &A, const Item &it,
+__device__ __forceinline__ int last_seen(const CacheAttn &A, int len, int n,
                                          int col) {
     const int t = col % A.c.T;
-    return t < it.n ? it.len - it.n + t : -1;
+    return t < n ? len - n + t : -1;
 }
 // Row of q, o and lse of column `col`.
 __device__ __forceinline__ size_t query_row(const CacheAttn &A, int b, int h,
@@ -221,8 +294,8 @@ __device__ __forceinline__ size_t query_row(const CacheAttn &A, int b, int h,
     return ((size_t)b * A.c.H + (size_t)h * A.c.G + g) * A.c.T + t;
 }
 
-__device__ __forceinline__ float *piece(const CacheAttn &A, long cta,
-                                        int slot, int col) {
+__device__ __forceinline__ float *piece(const CacheAttn &A, int cta, int slot,
+                                        int col) {
     return A.part + (((size_t)cta * 2 + slot) * A.cols + col) * (A.c.d + 2);
 }
 
@@ -234,13 +307,13 @@ __device__ __forceinline__ void store_o(const CacheAttn &A, size_t row, int i,
         ((__nv_bfloat16 *)A.o)[row * A.c.d + i] = __float2bfloat16_rn(x);
 }
 // lse of a finished column from its maximum (log2) and sum.
-__device__ __forceinline__ void store_lse(const CacheAttn &A, const Item &it,
-                                          int col, float m, float l) {
-    const float l2 = l > 0.0f ? m + log2f(l) : -INFINITY;
+__device__ __forceinline__ void store_lse(const CacheAttn &A, int b, int h,
+                                          int n, int col, float m, float l) {
+    const float l2 = l == 0.0f ? -INFINITY : m + log2f(l);
     if (A.lse2)
-        A.lse2[((size_t)it.b * A.c.Hkv + it.h) * A.c.G * A.c.T + col] = l2;
-    if (A.lse && col % A.c.T < it.n)
-        A.lse[query_row(A, it.b, it.h, col)] = l2 * 0.6931471805599453f;
+        A.lse2[((size_t)b * A.c.Hkv + h) * A.c.G * A.c.T + col] = l2;
+    if (A.lse && col % A.c.T < n)
+        A.lse[query_row(A, b, h, col)] = l2 * 0.6931471805599453f;
 }
 
 }  // namespace cache

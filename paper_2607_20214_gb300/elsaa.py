@@ -713,6 +713,7 @@ def make_cache(k, v, k_scale, v_scale, bounds, page_table, lengths, H=None,
                      status=status)
     c.device = dev
     c.torch_dtype = f32 if dt == ELSAA_FP32 else torch.bfloat16
+    c.ref = ctypes.byref(c)
     return c
 
 
@@ -753,11 +754,11 @@ def new_cache_workspace(cache: elsaa_cache, T=1, weights=False,
 
 def _rows(t, name, cache, heads):
     """(pointer, T) of [B, heads, T, d_h] rows."""
-    if t.dim() != 4 or t.shape[0] != cache.B or t.shape[1] != heads or \
-            t.shape[3] != cache.d_h:
+    s = t.shape
+    if len(s) != 4 or (s[0], s[1], s[3]) != (cache.B, heads, cache.d_h):
         raise ValueError("%s must be [%d, %d, T, %d] (got %s)" % (
-            name, cache.B, heads, cache.d_h, tuple(t.shape)))
-    return _ptr(t, name, cache.torch_dtype, None, cache.device), t.shape[2]
+            name, cache.B, heads, cache.d_h, tuple(s)))
+    return _ptr(t, name, cache.torch_dtype, None, cache.device), s[2]
 
 
 def elsaa_cache_append(cache: elsaa_cache, k, v, new_len=None, stream=None):
@@ -767,7 +768,7 @@ def elsaa_cache_append(cache: elsaa_cache, k, v, new_len=None, stream=None):
     kp, T = _rows(k, "k", cache, cache.H_kv)
     vp = _ptr(v, "v", cache.torch_dtype, k.numel(), dev)
     _check(load_library().elsaa_cache_append(
-        ctypes.byref(cache), T, kp, vp,
+        cache.ref, T, kp, vp,
         _ptr(new_len, "new_len", torch.int32, cache.B, dev),
         _stream_of(stream, dev)))
 
@@ -785,13 +786,12 @@ def elsaa_cache_select(cache: elsaa_cache, q, n_sel, first=1, last=1,
     if workspace is None:
         workspace = new_cache_workspace(cache, T)
     _check(load_library().elsaa_cache_select(
-        ctypes.byref(cache), T, qp,
+        cache.ref, T, qp,
         _ptr(new_len, "new_len", torch.int32, cache.B, dev), n_sel, first,
         last, _ptr(pages, "pages", torch.int32,
                    cache.B * cache.H_kv * n_sel, dev),
         _ptr(workspace, "workspace", None, None, dev),
-        workspace.numel() * workspace.element_size(),
-        _stream_of(stream, dev)))
+        workspace.nbytes, _stream_of(stream, dev)))
     return pages
 
 
@@ -813,7 +813,7 @@ def elsaa_cache_attention(cache: elsaa_cache, q, pages=None, new_len=None,
     if pages is not None:
         n_sel = pages.shape[-1]
     _check(load_library().elsaa_cache_attention(
-        ctypes.byref(cache), T, qp,
+        cache.ref, T, qp,
         _ptr(new_len, "new_len", torch.int32, cache.B, dev),
         _ptr(pages, "pages", torch.int32, cache.B * cache.H_kv * n_sel, dev),
         n_sel, _ptr(weight_in, "weight_in", f32, slots, dev),
@@ -821,8 +821,7 @@ def elsaa_cache_attention(cache: elsaa_cache, q, pages=None, new_len=None,
         _ptr(o, "o", cache.torch_dtype, q.numel(), dev),
         _ptr(lse, "lse", f32, cache.B * cache.H * T, dev),
         _ptr(workspace, "workspace", None, None, dev),
-        workspace.numel() * workspace.element_size(),
-        _stream_of(stream, dev)))
+        workspace.nbytes, _stream_of(stream, dev)))
     return o
 
 
@@ -842,13 +841,12 @@ def elsaa_cache_evict(cache: elsaa_cache, weight, keep, recent, dst_table,
     if workspace is None:
         workspace = new_cache_workspace(cache, 1, False, keep)
     _check(load_library().elsaa_cache_evict(
-        ctypes.byref(cache),
+        cache.ref,
         _ptr(weight, "weight", f32, bh * cache.max_pages * ps, dev), keep,
         recent, _ptr(dst_table, "dst_table", i32, cache.B * width, dev),
         width, _ptr(weight_out, "weight_out", f32, bh * width * ps, dev),
         _ptr(lengths_out, "lengths_out", i32, cache.B, dev),
         _ptr(kept, "kept", i32, bh * keep, dev),
         _ptr(workspace, "workspace", None, None, dev),
-        workspace.numel() * workspace.element_size(),
-        _stream_of(stream, dev)))
+        workspace.nbytes, _stream_of(stream, dev)))
     return weight_out, lengths_out
