@@ -32,8 +32,8 @@ __global__ void __launch_bounds__(kSaThreads)
     const CacheView &c = A.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int sub = lane % LPR, rg = lane / LPR;
-    extern __shared__ int prefix[];
-    Walk walk(divide<kSaThreads>(A, prefix));
+    __shared__ Seq near[kNearSeqs];
+    Walk walk(divide<kSaThreads>(A, near), near);
     const float sl2 = c.scale * kLog2eF;
     const int GT = c.G * c.T;
 
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kWtThreads)
 template <typename T, int D, int NG>
 cudaError_t launch_simt(const CacheAttn &A, cudaStream_t st) {
     return launch_after(k_cache_attn_simt<T, D, NG>, dim3(A.ctas), kSaThreads,
-                        sizeof(int) * (A.c.B + 1), st, A);
+                        0, st, A);
 }
 
 template <typename T, int D>

@@ -49,24 +49,29 @@ constexpr int kTaRegsSoft = 184, kTaRegsOther = 72;
 constexpr float kLog2eF = 1.4426950408889634f;
 constexpr int kMaxPagesPerTile = kCacheTile / 16;
 
+constexpr int kSub = 2;  // tiles of a softmax step
+
 template <int D, int NV>
 struct Cfg {
     static constexpr int N1 = 2 * NV < 16 ? 16 : 2 * NV;  // columns of S
     static constexpr int NP = (3 * NV + 15) / 16 * 16;    // of one P product
     static constexpr int NO = D == 128 ? NP : 2 * NP;     // of O
     static constexpr int W = NP <= 32 ? 32 : 64;  // bytes of a token's P row
-    static constexpr int KS = D == 64 ? (NV < 16 ? 6 : 5) : (NV < 16 ? 3 : 2);
-    static constexpr int VS = D == 64 ? (NV < 16 ? 6 : 5) : 3;
+    // K is free again as soon as S is made, V only when O is
+    static constexpr int KS = D == 64 ? 4 : 2;
+    static constexpr int VS = D == 64 ? (NV < 16 ? 8 : 6) : (NV < 16 ? 4 : 3);
+    // a tile's pages and scales are written before its V buffer is waited
+    // for: by then tile - 1 - VS is read
+    static constexpr int MS = VS + 1;
     static constexpr uint32_t kTile = kCacheTile * D;
     static constexpr uint32_t kQ = N1 * D;
     static constexpr uint32_t kP = kCacheTile * W;
     static constexpr uint32_t kSmem =
-        1024 + (KS + VS) * kTile + 2 * kQ + 2 * kP;
-    static constexpr uint32_t kCols = 2 * N1 + 2 * NO;
-    static constexpr uint32_t kTmem = kCols <= 64    ? 64
-                                      : kCols <= 128 ? 128
-                                                     : 256;
+        1024 + (KS + VS) * kTile + 2 * kQ + kSub * kP;
+    static constexpr uint32_t kCols = 2 * kSub * N1 + NO;
+    static constexpr uint32_t kTmem = kCols <= 128 ? 128 : 256;
     static_assert(kCols <= 256, "two CTAs share tensor memory");
+    static_assert(VS > kSub, "the next step's V has to fit");
 };
 
 // Shared-memory descriptor of an operand whose lines are `line` = 32, 64 or
@@ -134,24 +139,6 @@ __device__ __forceinline__ void tmem_read(uint32_t t, float *x) {
     }
 }
 
-// V = 2 or 4 neighbouring bf16 values.
-template <int V>
-__device__ __forceinline__ void load_row(const __nv_bfloat16 *p, float *x) {
-    uint32_t w[V / 2];
-    if constexpr (V == 4) {
-        const uint2 a = *(const uint2 *)p;
-        w[0] = a.x;
-        w[1] = a.y;
-    } else {
-        w[0] = *(const uint32_t *)p;
-    }
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-
 // Largest of the warp's values, in every lane.
 __device__ __forceinline__ float redux_max(float x) {
     float r;
@@ -162,15 +149,15 @@ __device__ __forceinline__ float redux_max(float x) {
 // The pages of one tile, written by the producer.
 struct TileMeta {
     float ks[kMaxPagesPerTile];   // key scale
-    float vs[kMaxPagesPerTile];   // value scale over the tile's largest
+    float vs[kMaxPagesPerTile];   // value scale
     int pos[kMaxPagesPerTile];    // first position
     int rows[kMaxPagesPerTile];   // rows that count
-    float vmax;
+    float vmax;                   // largest value scale
 };
 
 struct Bars {
-    uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6], m_full[6];
-    uint64_t s_full[2], p_ready[2], o_full[2], q_full[2], q_empty[2], drain;
+    uint64_t k_full[4], k_empty[4], v_full[8], v_empty[8], m_full[9];
+    uint64_t s_full[2], p_ready, o_full, q_full[2], q_empty[2], drain;
 };
 
 template <int D, int NV>
@@ -181,14 +168,19 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     using C = Cfg<D, NV>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Bars bars;
-    __shared__ TileMeta meta[C::VS];
+    __shared__ TileMeta meta[C::MS];
     __shared__ Item items[2];
+    __shared__ Seq near[kNearSeqs];
     __shared__ float factors[2][NV];  // of an item's columns' scores
     __shared__ int limits[2][NV];     // last positions that they see
     __shared__ uint32_t tbase;
     __shared__ int abort_flag;
-    __shared__ __align__(16) float red[2][NV][4];
-    __shared__ __align__(16) float fin[NV][4];
+    // per step parity: every warp's maxima, and for every warp a column's
+    // reference, factor of the sums so far, factor of the step's sum and of
+    // its O
+    __shared__ float red[2][4][NV];
+    __shared__ float4 stat[2][4][NV];
+    __shared__ float4 fin[2][NV];  // sums of the four warps' tokens
     __shared__ float half[D == 64 ? NV * 64 : 1];
     volatile int *abort = &abort_flag;
     const CacheView &c = A.c;
@@ -200,20 +192,22 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     // set up while the kernel before ends
     if (warp == 5) tmem_alloc(&tbase, C::kTmem);
     if (tid == 0) {
-        for (int s = 0; s < 6; ++s) {
+        for (int s = 0; s < C::KS; ++s) {
             mbar_init(&bars.k_full[s], 1);
             mbar_init(&bars.k_empty[s], 1);
+        }
+        for (int s = 0; s < C::VS; ++s) {
             mbar_init(&bars.v_full[s], 1);
             mbar_init(&bars.v_empty[s], 1);
-            mbar_init(&bars.m_full[s], 1);
         }
+        for (int s = 0; s < C::MS; ++s) mbar_init(&bars.m_full[s], 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.s_full[s], 1);
-            mbar_init(&bars.p_ready[s], 128);
-            mbar_init(&bars.o_full[s], 1);
             mbar_init(&bars.q_full[s], 2);   // the query warps
             mbar_init(&bars.q_empty[s], 5);  // products, four softmax warps
         }
+        mbar_init(&bars.p_ready, 128);
+        mbar_init(&bars.o_full, 1);
         mbar_init(&bars.drain, 1);
         abort_flag = 0;
         fence_mbar_init();
@@ -223,84 +217,117 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     tc_fence_after();
     const uint32_t tm = tbase;
     wait_for_stream();
-    const Start first =
-        divide<kTaThreads>(A, (int *)(smem_raw + C::kSmem));
+    const Start first = divide<kTaThreads>(A, near);
     const int count = first.count;
 
     if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
             kTaRegsOther));
+        auto wait = [&](uint64_t *bar, uint32_t par, int site) {
+            return __all_sync(0xffffffffu,
+                              mbar_wait_or_abort(bar, par, abort, c.status,
+                                                 site));
+        };
         if (warp == 4) {
-            // ------------------------------------------------ pages and scales
+            // -------------------------------------------- pages and scales
+            // A batch is the next 32 pages of an item, a page a lane; the next
+            // batch's table entries and scales are asked for as soon as this
+            // one's first tile is on its way.
             const int pt = kCacheTile / c.ps;  // pages of a tile
-            Walk walk(first);
-            Item it;
-            it.count = it.off = 0;
-            bool ok = true;
-            int kn = 0, vn = 0;  // loads issued
-            int t = 0;           // tile within the item
-            for (int i = 0; i < count; ++i, ++t) {
-                if (t == it.off + it.count) {
-                    it = walk.next(A);
-                    t = it.off;
-                }
-                // lane l: the tile's l-th page
-                const int e = t * pt + lane;
-                int p = -1, id = -1, rows = 0;
-                if (lane < pt && (long)e * c.ps < it.walk)
+            struct Page {
+                int id, pos, rows;
+                float ks, vs;
+            };
+            auto fetch = [&](const Item &it, int tile) {
+                Page g = {-1, 0, 0, 0.0f, 0.0f};
+                const int e = tile * pt + lane;
+                int p = -1;
+                if ((long)e * c.ps < it.walk)
                     p = A.pages ? A.pages[((size_t)it.b * c.Hkv + it.h) *
                                               A.n_sel + e]
                                 : e;
                 if (p >= 0 && p < c.max_pages) {
-                    rows = min(it.len - p * c.ps, c.ps);
-                    if (rows > 0) id = page_id(c, it.b, p);
+                    g.pos = p * c.ps;
+                    g.rows = min(it.len - g.pos, c.ps);
+                    if (g.rows > 0) g.id = page_id(c, it.b, p);
                 }
-                if (id < 0) rows = 0;
-                const int ph = id * c.Hkv + it.h;  // fits: checked by the host
-                const uint32_t live = __ballot_sync(0xffffffffu, id >= 0);
-                const uint32_t bytes = __popc(live) * c.ps * D;
-                const int ks = i % C::KS, vs = i % C::VS;
-                if (i >= C::KS)
-                    ok = __all_sync(0xffffffffu,
-                                    mbar_wait_or_abort(&bars.k_empty[ks],
-                                                       (i / C::KS - 1) & 1, abort,
-                                                       c.status, 180));
-                if (!ok) break;
-                if (lane == 0) mbar_expect_tx(&bars.k_full[ks], bytes);
-                __syncwarp();
-                if (id >= 0)
-                    tma_load_2d(sK + ks * C::kTile + lane * c.ps * D, &tmK, 0,
-                                ph * c.ps, &bars.k_full[ks]);
-                ++kn;
-                float k_sc = 0.0f, v_sc = 0.0f;
-                if (id >= 0) {
-                    k_sc = c.ks[ph];
-                    v_sc = c.vs[ph];
+                if (g.id >= 0) {
+                    const int ph = g.id * c.Hkv + it.h;  // fits: the host's
+                    g.ks = c.ks[ph];                     // check
+                    g.vs = c.vs[ph];
+                } else {
+                    g.rows = 0;
                 }
-                if (i >= C::VS)
-                    ok = __all_sync(0xffffffffu,
-                                    mbar_wait_or_abort(&bars.v_empty[vs],
-                                                       (i / C::VS - 1) & 1, abort,
-                                                       c.status, 181));
-                if (!ok) break;
-                if (lane == 0) mbar_expect_tx(&bars.v_full[vs], bytes);
-                __syncwarp();
-                if (id >= 0)
-                    tma_load_2d(sV + vs * C::kTile + lane * c.ps * D, &tmV, 0,
-                                D == 128 ? ph * c.ps : ph * c.ps / 2,
-                                &bars.v_full[vs]);
-                ++vn;
-                const float vmax = warp_max(v_sc);
-                if (lane < pt) {
-                    TileMeta &m = meta[vs];
-                    m.ks[lane] = k_sc;
-                    m.vs[lane] = vmax > 0.0f ? v_sc / vmax : 0.0f;
-                    m.pos[lane] = p * c.ps;
-                    m.rows[lane] = rows;
-                    if (lane == 0) m.vmax = vmax;
+                return g;
+            };
+            Walk walk(first, near);
+            Item it = {}, nit = {};
+            Page page = {}, next = {};
+            int tile = 0, ntile = 0;
+            bool ok = true;
+            int kn = 0, vn = 0;  // loads issued
+            if (count > 0) {
+                it = walk.next(A);
+                tile = it.off;
+                page = fetch(it, tile);
+            }
+            for (int i = 0; i < count && ok;) {
+                const int nt = min(32 / pt, it.off + it.count - tile);
+                for (int k = 0; k < nt; ++k, ++i) {
+                    const int src = (k * pt + lane) & 31;
+                    int id = __shfl_sync(0xffffffffu, page.id, src);
+                    if (lane >= pt) id = -1;
+                    const int row = (id * c.Hkv + it.h) * c.ps;
+                    const uint32_t bytes =
+                        __popc(__ballot_sync(0xffffffffu, id >= 0)) * c.ps * D;
+                    const int ks = i % C::KS, vs = i % C::VS;
+                    if (i >= C::KS)
+                        ok = wait(&bars.k_empty[ks], (i / C::KS - 1) & 1, 180);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(&bars.k_full[ks], bytes);
+                    __syncwarp();
+                    if (id >= 0)
+                        tma_load_2d(sK + ks * C::kTile + lane * c.ps * D, &tmK,
+                                    0, row, &bars.k_full[ks]);
+                    ++kn;
+                    float v = __shfl_sync(0xffffffffu, page.vs, src);
+                    const float vmax = warp_max(lane < pt ? v : 0.0f);
+                    const float kk = __shfl_sync(0xffffffffu, page.ks, src);
+                    const int pos = __shfl_sync(0xffffffffu, page.pos, src);
+                    const int rows = __shfl_sync(0xffffffffu, page.rows, src);
+                    if (lane < pt) {
+                        TileMeta &m = meta[i % C::MS];
+                        m.ks[lane] = kk;
+                        m.vs[lane] = v;
+                        m.pos[lane] = pos;
+                        m.rows[lane] = rows;
+                        if (lane == 0) m.vmax = vmax;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.m_full[i % C::MS]);
+                    if (i >= C::VS)
+                        ok = wait(&bars.v_empty[vs], (i / C::VS - 1) & 1, 181);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(&bars.v_full[vs], bytes);
+                    __syncwarp();
+                    if (id >= 0)
+                        tma_load_2d(sV + vs * C::kTile + lane * c.ps * D, &tmV,
+                                    0, D == 128 ? row : row / 2,
+                                    &bars.v_full[vs]);
+                    ++vn;
+                    if (k == 0) {
+                        nit = it;
+                        ntile = tile + nt;
+                        if (ntile == it.off + it.count && walk.left > 0) {
+                            nit = walk.next(A);
+                            ntile = nit.off;
+                        }
+                        if (i + nt < count) next = fetch(nit, ntile);
+                    }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.m_full[vs]);
+                it = nit;
+                tile = ntile;
+                page = next;
             }
             // whatever was asked for has arrived before the CTA ends
             for (int j = max(0, kn - C::KS); j < kn; ++j)
@@ -310,48 +337,55 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 mbar_wait(&bars.v_full[j % C::VS], (j / C::VS) & 1, c.status,
                           183);
         } else if (warp == 5) {
-            // -------------------------------------------------------- products
+            // ---------------------------------------------------- products
             const bool el = elect_one();
-            auto wait = [&](uint64_t *bar, uint32_t par, int site) {
-                return __all_sync(0xffffffffu,
-                                  mbar_wait_or_abort(bar, par, abort, c.status,
-                                                     site));
-            };
             const uint32_t id_s = idesc_e4m3(128, C::N1, false, false);
             const uint32_t id_o = idesc_e4m3(128, C::NP, true, true);
-            bool ok = true;
-            auto values = [&](int j) {  // O of tile j
-                const int vs = j % C::VS, b = j & 1;
-                if (!wait(&bars.v_full[vs], (j / C::VS) & 1, 185)) return false;
-                if (!wait(&bars.p_ready[b], (j >> 1) & 1, 186)) return false;
+            const uint32_t o = tm + 2 * kSub * C::N1;
+            // O of step j: `n` tiles from tile u on
+            auto values = [&](int j, int u, int n) {
+                for (int x = 0; x < n; ++x)
+                    if (!wait(&bars.v_full[(u + x) % C::VS],
+                              ((u + x) / C::VS) & 1, 185))
+                        return false;
+                if (!wait(&bars.p_ready, j & 1, 186)) return false;
                 tc_fence_after();
                 if (el) {
-                    const uint64_t dV = line_desc(sV + vs * C::kTile, 128);
-                    const uint64_t dP = line_desc(sP + b * C::kP, C::W);
-                    const uint32_t o = tm + 2 * C::N1 + b * C::NO;
-                    if (D == 128) {
+                    for (int x = 0; x < n; ++x) {
+                        const int vs = (u + x) % C::VS;
+                        const uint64_t dV = line_desc(sV + vs * C::kTile, 128);
+                        const uint64_t dP = line_desc(sP + x * C::kP, C::W);
+                        if (D == 128) {
 #pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            mma_e4m3(o, desc_at(dV, x * 4096),
-                                     desc_at(dP, x * 32 * C::W), id_o, x > 0);
-                    } else {
+                            for (int y = 0; y < 4; ++y)
+                                mma_e4m3(o, desc_at(dV, y * 4096),
+                                         desc_at(dP, y * 32 * C::W), id_o,
+                                         x + y > 0);
+                        } else {
 #pragma unroll
-                        for (int par = 0; par < 2; ++par)
+                            for (int par = 0; par < 2; ++par)
 #pragma unroll
-                            for (int x = 0; x < 2; ++x)
-                                mma_e4m3(o + par * C::NP, desc_at(dV, x * 4096),
-                                         desc_at(dP, (par * 64 + x * 32) * C::W),
-                                         id_o, x > 0);
+                                for (int y = 0; y < 2; ++y)
+                                    mma_e4m3(o + par * C::NP,
+                                             desc_at(dV, y * 4096),
+                                             desc_at(dP, (par * 64 + y * 32) *
+                                                             C::W),
+                                             id_o, x + y > 0);
+                        }
                     }
-                    mma_commit(&bars.o_full[b]);
-                    mma_commit(&bars.v_empty[vs]);
+                    mma_commit(&bars.o_full);
+                    for (int x = 0; x < n; ++x)
+                        mma_commit(&bars.v_empty[(u + x) % C::VS]);
                 }
                 __syncwarp();
                 return true;
             };
+            bool ok = true;
             int item = 0, left = 0;  // tiles of the item
+            int u0 = 0, n0 = 0;      // tiles of the step before
             uint64_t dQ = 0;
-            for (int i = 0; i < count && ok; ++i) {
+            int i = 0;
+            for (int u = 0; u < count; ++i) {
                 if (left == 0) {
                     ok = wait(&bars.q_full[item & 1], (item >> 1) & 1, 187);
                     if (!ok) break;
@@ -359,107 +393,105 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                     dQ = line_desc(sQ + (item & 1) * C::kQ, D);
                     ++item;
                 }
-                --left;
-                const int ks = i % C::KS, b = i & 1;
-                ok = wait(&bars.k_full[ks], (i / C::KS) & 1, 188);
-                if (!ok) break;
-                tc_fence_after();
-                if (el) {
-                    const uint64_t dK = line_desc(sK + ks * C::kTile, D);
+                const int n = min(left, kSub);
+                left -= n;
+                for (int x = 0; x < n && ok; ++x) {
+                    const int ks = (u + x) % C::KS;
+                    ok = wait(&bars.k_full[ks], ((u + x) / C::KS) & 1, 188);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (el) {
+                        const uint64_t dK = line_desc(sK + ks * C::kTile, D);
+                        const uint32_t s = tm + ((i & 1) * kSub + x) * C::N1;
 #pragma unroll
-                    for (int x = 0; x < D / 32; ++x)
-                        mma_e4m3(tm + b * C::N1, desc_at(dK, x * 32),
-                                 desc_at(dQ, x * 32), id_s, x > 0);
-                    mma_commit(&bars.s_full[b]);
-                    mma_commit(&bars.k_empty[ks]);
-                    if (left == 0) mma_commit(&bars.q_empty[(item - 1) & 1]);
+                        for (int y = 0; y < D / 32; ++y)
+                            mma_e4m3(s, desc_at(dK, y * 32),
+                                     desc_at(dQ, y * 32), id_s, y > 0);
+                        mma_commit(&bars.k_empty[ks]);
+                        if (x + 1 == n) {
+                            mma_commit(&bars.s_full[i & 1]);
+                            if (left == 0)
+                                mma_commit(&bars.q_empty[(item - 1) & 1]);
+                        }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
-                if (i > 0) ok = values(i - 1);
+                if (ok && i > 0) ok = values(i - 1, u0, n0);
+                if (!ok) break;
+                u0 = u;
+                n0 = n;
+                u += n;
             }
-            if (ok && count > 0) values(count - 1);
-            // every product is complete before the tensor memory is given back
+            if (ok && count > 0) values(i - 1, u0, n0);
+            // every product is complete before tensor memory is given back
             if (el) mma_commit(&bars.drain);
             mbar_wait(&bars.drain, 0, c.status, 189);
             __syncwarp();
-        } else if (warp >= 6) {
-            // --------------------------------------------------------- queries
-            Walk walk(first);
-            constexpr int V = D / 32;  // elements a lane
+        } else {
+            // ----------------------------------------------------- queries
+            // D / 16 lanes a column, 16 elements each: a line's 16-byte chunk
+            constexpr int LPC = D / 16, CPW = 32 / LPC;
+            const int ch = lane % LPC;
+            Walk walk(first, near);
+            bool ok = true;
             for (int k = 0; walk.left > 0; ++k) {
                 const Item it = walk.next(A);
                 const int qs = k & 1;
-                bool ok = true;
-                // this warp's columns, a few at a time; the first are read before
-                // the buffer is free
-                constexpr int Z = (NV + 1) / 2, ZB = Z < 4 ? Z : 4;
 #pragma unroll 1
-                for (int z0 = 0; z0 < Z; z0 += ZB) {
-                    float x[ZB][V];
-                    int lim[ZB];
+                for (int g0 = 0; g0 < NV; g0 += 2 * CPW) {
+                    const int g = g0 + (warp - 6) * CPW + lane / LPC;
+                    const int lim =
+                        g < it.cols
+                            ? last_seen(A, it.len, it.n, it.col0 + g)
+                            : -1;
+                    float x[16];
 #pragma unroll
-                    for (int z = 0; z < ZB; ++z) {
-                        const int g = 2 * (z0 + z) + warp - 6;
-                        lim[z] = g < it.cols
-                                     ? last_seen(A, it.len, it.n, it.col0 + g)
-                                     : -1;
-#pragma unroll
-                        for (int i = 0; i < V; ++i) x[z][i] = 0.0f;
-                        if (lim[z] >= 0)
-                            load_row<V>((const __nv_bfloat16 *)A.q +
-                                            query_row(A, it.b, it.h, it.col0 + g) *
-                                                D + lane * V,
-                                        x[z]);
+                    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+                    if (lim >= 0) {
+                        const __nv_bfloat16 *src =
+                            (const __nv_bfloat16 *)A.q +
+                            query_row(A, it.b, it.h, it.col0 + g) * D +
+                            ch * 16;
+                        load8(src, x);
+                        load8(src + 8, x + 8);
                     }
-                    if (z0 == 0 && k >= 2)
-                        ok = __all_sync(0xffffffffu,
-                                        mbar_wait_or_abort(&bars.q_empty[qs],
-                                                           ((k >> 1) - 1) & 1,
-                                                           abort, c.status, 184));
+                    // the first columns are read before the buffer is free
+                    if (g0 == 0 && k >= 2)
+                        ok = wait(&bars.q_empty[qs], ((k >> 1) - 1) & 1, 184);
                     if (!ok) break;
+                    float amax = 0.0f;
 #pragma unroll
-                    for (int z = 0; z < ZB; ++z) {
-                        const int g = 2 * (z0 + z) + warp - 6;
-                        if (g >= NV) break;
-                        float amax = 0.0f;
+                    for (int i = 0; i < 16; ++i)
+                        amax = fmaxf(amax, magnitude(x[i]));
 #pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            amax = fmaxf(amax, magnitude(x[z][i]));
-                        const int e = least_exponent(warp_max(amax), 0x600000u, 8,
-                                                     -100, kCacheExpHigh);
-                        const float f = pow2(-e);
-                        uint32_t w[2] = {0, 0};
+                    for (int o = 1; o < LPC; o <<= 1)
+                        amax = fmaxf(amax,
+                                     __shfl_xor_sync(0xffffffffu, amax, o));
+                    const int e = least_exponent(amax, 0x600000u, 8, -100,
+                                                 kCacheExpHigh);
+                    const float f = pow2(-e);
+                    uint32_t hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
 #pragma unroll
-                        for (int i = 0; i < V; i += 2) {
-                            // an infinity has no split: it counts as NaN
-                            const float y0 = isinf(x[z][i]) ? NAN : x[z][i] * f;
-                            const float y1 =
-                                isinf(x[z][i + 1]) ? NAN : x[z][i + 1] * f;
-                            const uint32_t hi = e4m3x2(y0, y1);
-                            const float2 u = from_e4m3x2(hi);
-                            w[0] |= hi << (8 * i);
-                            w[1] |= e4m3x2((y0 - u.x) * 16.0f,
-                                           (y1 - u.y) * 16.0f)
-                                    << (8 * i);
-                        }
-#pragma unroll
-                        for (int p = 0; p < 2; ++p) {
-                            const uint32_t at =
-                                sQ + qs * C::kQ +
-                                line_offset<D>(p * NV + g, (lane * V) >> 4) +
-                                ((lane * V) & 15);
-                            if (V == 4)
-                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(at),
-                                             "r"(w[p])
-                                             : "memory");
-                            else
-                                asm volatile("st.shared.u16 [%0], %1;" ::"r"(at),
-                                             "h"((uint16_t)w[p])
-                                             : "memory");
-                        }
-                        if (lane == 0) {
+                    for (int i = 0; i < 16; i += 2) {
+                        // an infinity has no split: it counts as NaN
+                        const float y0 = isinf(x[i]) ? NAN : x[i] * f;
+                        const float y1 = isinf(x[i + 1]) ? NAN : x[i + 1] * f;
+                        const uint32_t h = e4m3x2(y0, y1);
+                        const float2 z = from_e4m3x2(h);
+                        hi[i / 4] |= h << (8 * (i & 3));
+                        lo[i / 4] |= e4m3x2((y0 - z.x) * 16.0f,
+                                            (y1 - z.y) * 16.0f)
+                                     << (8 * (i & 3));
+                    }
+                    if (g < NV) {
+                        const uint32_t q = sQ + qs * C::kQ;
+                        st_shared_v4(q + line_offset<D>(g, ch), hi[0], hi[1],
+                                     hi[2], hi[3]);
+                        st_shared_v4(q + line_offset<D>(NV + g, ch), lo[0],
+                                     lo[1], lo[2], lo[3]);
+                        if (ch == 0) {
                             factors[qs][g] = pow2(e) * (c.scale * kLog2eF);
-                            limits[qs][g] = lim[z];
+                            limits[qs][g] = lim;
                         }
                     }
                 }
@@ -474,219 +506,289 @@ __global__ void __launch_bounds__(kTaThreads, 2)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(
             kTaRegsSoft));
         // --------------------------------------------------------- softmax
+        // A step is up to kSub tiles of an item: a thread has a token of each,
+        // so that what a step costs whatever it holds (waits, the maximum
+        // over the warps, O's way back) is paid once.
         auto wait = [&](uint64_t *bar, uint32_t par, int site) {
             return __all_sync(0xffffffffu,
                               mbar_wait_or_abort(bar, par, abort, c.status,
                                                  site));
         };
         const int GT = c.G * c.T;
+        const int shift = __ffs(c.ps) - 1;
+        const int slot = tid >> shift, row = tid & (c.ps - 1);
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        float acc[NV], l[NV], M[NV], al[NV], be[NV];
-        Item it;
+        float acc[NV], l[NV];
+        float M = -INFINITY;      // lane g: of column g
+        Item it = {}, last = {};  // this step's, the unfinished one before
+        float lastM = 0.0f;
         int item = 0, t = 0, end = 0;
-        bool ok = true;
-        // acc of the current item takes tile j's O
+        bool ok = true, fine = count > 0;
+#pragma unroll
+        for (int g = 0; g < NV; ++g) acc[g] = l[g] = 0.0f;
+        // acc takes step j's O
         auto take = [&](int j) {
-            const bool fine = wait(&bars.o_full[j & 1], (j >> 1) & 1, 190);
+            const bool done = wait(&bars.o_full, j & 1, 190);
             tc_fence_after();
             float o[C::NP];
-            uint32_t at = tm + lanes + 2 * C::N1 + (j & 1) * C::NO;
+            uint32_t at = tm + lanes + 2 * kSub * C::N1;
             if (D == 64 && warp >= 2) at += C::NP;
             tmem_read<C::NP>(at, o);
             tmem_wait_ld();
 #pragma unroll
-            for (int g = 0; g < NV; ++g)
-                acc[g] = acc[g] * al[g] +
-                         be[g] * (o[g] + 0.0625f * o[NV + g] +
-                                  0.00390625f * o[2 * NV + g]);
+            for (int g = 0; g < NV; ++g) {
+                const float4 f = stat[j & 1][warp][g];
+                acc[g] = acc[g] * f.y +
+                         f.w * (o[g] + 0.0625f * o[NV + g] +
+                                0.00390625f * o[2 * NV + g]);
+            }
             tc_fence_before();
-            return fine;
+            return done;
         };
-        for (int i = 0; i < count; ++i, ++t) {
-            if (t == end) {
+        // the sums of a finished item, where every warp finds them behind the
+        // next barrier
+        auto leave = [&](int k) {
+#pragma unroll
+            for (int g = 0; g < NV; ++g) {
+                const float x = warp_sum(l[g]);
+                if (lane == 0) ((float *)&fin[k & 1][g])[warp] = x;
+                l[g] = 0.0f;
+            }
+            last = it;
+            lastM = M;
+            M = -INFINITY;
+        };
+        // item k is complete in acc
+        auto finish = [&](int k) {
+            if (D == 64) {
+                if (tid >= 64)
+#pragma unroll
+                    for (int g = 0; g < NV; ++g)
+                        half[g * 64 + tid - 64] = acc[g];
+                named_sync(1, 128);
+            }
+            const bool all = last.n == c.T;
+            const size_t r0 = query_row(A, last.b, last.h, last.col0);
+#pragma unroll
+            for (int g = 0; g < NV; ++g) {
+                if (g >= last.cols) break;
+                float x = acc[g];
+                if (D == 64 && tid < 64) x += half[g * 64 + tid];
+                if (tid >= D) continue;
+                if (last.slot >= 0) {
+                    piece(A, blockIdx.x, last.slot, g)[tid] = x;
+                } else if (all || (last.col0 + g) % c.T < last.n) {
+                    const float4 w = fin[k & 1][g];
+                    const float L = (w.x + w.y) + (w.z + w.w);
+                    ((__nv_bfloat16 *)A.o)[(r0 + g) * D + tid] =
+                        __float2bfloat16_rn(L == 0.0f ? 0.0f : x / L);
+                }
+            }
+            if (tid < last.cols) {  // column `tid`
+                const float4 w = fin[k & 1][tid];
+                const float L = (w.x + w.y) + (w.z + w.w);
+                if (last.slot >= 0) {
+                    float *at = piece(A, blockIdx.x, last.slot, tid);
+                    at[D] = lastM;
+                    at[D + 1] = L;
+                } else {
+                    store_lse(A, last.b, last.h, last.n, last.col0 + tid,
+                              lastM, L);
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < NV; ++g) acc[g] = 0.0f;
+        };
+        int i = 0;
+        for (int u = 0; u < count; ++i) {
+            const bool begins = t == end;
+            if (begins) {
+                if (i > 0) leave(item - 1);
                 const int qs = item & 1;
                 ok = wait(&bars.q_full[qs], (item >> 1) & 1, 195) && ok;
                 it = ok ? items[qs] : Item{};
                 t = it.off;
                 end = it.off + it.count;
                 ++item;
+            }
+            const int n = min(end - t, kSub), b = i & 1;
+            const float *factor = factors[(item - 1) & 1];
+            const int *limit = limits[(item - 1) & 1];
+            float s[kSub][NV], vrel[kSub], vmax = 0.0f;
+            bool in[kSub];
+            int pos[kSub];
+            float ks[kSub];
 #pragma unroll
-                for (int g = 0; g < NV; ++g) {
-                    acc[g] = l[g] = al[g] = be[g] = 0.0f;
-                    M[g] = -INFINITY;
+            for (int x = 0; x < kSub; ++x) {
+                in[x] = true;
+                ks[x] = vrel[x] = 0.0f;
+                pos[x] = 0;
+                if (x < n) {
+                    const int ms = (u + x) % C::MS;
+                    ok = wait(&bars.m_full[ms], ((u + x) / C::MS) & 1, 191) &&
+                         ok;
+                    const TileMeta &m = meta[ms];
+                    in[x] = row < m.rows[slot];
+                    pos[x] = m.pos[slot] + row;
+                    ks[x] = m.ks[slot];
+                    vrel[x] = m.vs[slot];
+                    vmax = fmaxf(vmax, m.vmax);
                 }
             }
-            const int vs = i % C::VS, b = i & 1;
-            ok = wait(&bars.m_full[vs], (i / C::VS) & 1, 191) && ok;
-            const int j = tid / c.ps, row = tid % c.ps;
-            const TileMeta &m = meta[vs];
-            const bool in = row < m.rows[j];
-            const int pos = m.pos[j] + row;
-            const float ks = m.ks[j], vrel = m.vs[j], vmax = m.vmax;
             ok = wait(&bars.s_full[b], (i >> 1) & 1, 192) && ok;
             tc_fence_after();
-            float s[NV];
-            {
-                float x[2 * NV];
-                tmem_read<2 * NV>(tm + lanes + b * C::N1, x);
-                tmem_wait_ld();
-                const bool all = pos <= it.len - it.n;
-                const float *factor = factors[(item - 1) & 1];
-                const int *limit = limits[(item - 1) & 1];
 #pragma unroll
-                for (int g = 0; g < NV; ++g) {
-                    s[g] = (x[g] + 0.0625f * x[NV + g]) * (ks * factor[g]);
-                    if (!in || (!all && pos > limit[g]))
-                        s[g] = -INFINITY;
+            for (int x = 0; x < kSub; ++x) {
+                if (x < n) {
+                    float y[2 * NV];
+                    tmem_read<2 * NV>(tm + lanes + (b * kSub + x) * C::N1, y);
+                    tmem_wait_ld();
+                    const bool all = pos[x] <= it.len - it.n;
+#pragma unroll
+                    for (int g = 0; g < NV; ++g) {
+                        s[x][g] = (y[g] + 0.0625f * y[NV + g]) *
+                                  (ks[x] * factor[g]);
+                        if (!in[x] || (!all && pos[x] > limit[g]))
+                            s[x][g] = -INFINITY;
+                    }
+                } else {
+#pragma unroll
+                    for (int g = 0; g < NV; ++g) s[x][g] = -INFINITY;
                 }
             }
-            if (t + 1 == end) {  // the queries may go
+            tc_fence_before();
+            if (t + n == end) {  // the queries may go
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.q_empty[(item - 1) & 1]);
             }
             if (A.scores) {
-                const int w = t * kCacheTile + tid;
-                if (w < it.walk) {
-                    float *at = A.scores +
-                                (((size_t)it.b * c.Hkv + it.h) * GT +
-                                 it.col0) * A.slots + w;
 #pragma unroll
-                    for (int g = 0; g < NV; ++g)
-                        if (g < it.cols) at[(size_t)g * A.slots] = s[g];
-                }
-            }
+                for (int x = 0; x < kSub; ++x) {
+                    const int w = (t + x) * kCacheTile + tid;
+                    if (x < n && w < it.walk) {
+                        float *at = A.scores +
+                                    (((size_t)it.b * c.Hkv + it.h) * GT +
+                                     it.col0) * A.slots + w;
 #pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                const float x = redux_max(s[g]);
-                if (lane == 0) red[b][g][warp] = x;
-            }
-            // also agrees on whether every wait of the four warps ended well
-            ok = named_sync_and(1, 128, ok);
-            if (!ok) break;
-            // tile j's factors move on once its O is taken, which is after
-            // this tile's weights: keep both
-            float al2[NV], be2[NV];
-            uint32_t hi[(NV + 1) / 2], mid[(NV + 1) / 2], lo[(NV + 1) / 2];
-#pragma unroll
-            for (int g = 0; g < NV; g += 2) {
-                float y[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    y[k] = 0.0f;
-                    if (g + k >= NV) continue;
-                    const float4 w = *(const float4 *)red[b][g + k];
-                    const float mt = fmaxf(fmaxf(w.x, w.y), fmaxf(w.z, w.w));
-                    const float Mn = fmaxf(M[g + k], mt);
-                    const float ref = mt == -INFINITY ? 0.0f : mt;
-                    const float Mr = Mn == -INFINITY ? 0.0f : Mn;
-                    const float p = ex2_approx(s[g + k] - ref);
-                    const float a2 = ex2_approx(M[g + k] - Mr);
-                    const float b2 = ex2_approx(mt - Mr);
-                    M[g + k] = Mn;
-                    l[g + k] = l[g + k] * a2 + b2 * p;
-                    al2[g + k] = a2;
-                    be2[g + k] = b2 * vmax * 0.00390625f;
-                    y[k] = p * vrel * 256.0f;
-                }
-                const uint32_t h = e4m3x2(y[0], y[1]);
-                const float2 u = from_e4m3x2(h);
-                y[0] = (y[0] - u.x) * 16.0f;
-                y[1] = (y[1] - u.y) * 16.0f;
-                const uint32_t q = e4m3x2(y[0], y[1]);
-                const float2 v = from_e4m3x2(q);
-                hi[g / 2] = h;
-                mid[g / 2] = q;
-                lo[g / 2] = e4m3x2((y[0] - v.x) * 16.0f,
-                                   (y[1] - v.y) * 16.0f);
-            }
-            {
-                // the token's row of P: all hi, all mid, all lo
-                const int pr = D == 128 ? tid : tid >> 1;
-                const uint32_t at = sP + b * C::kP +
-                                    (D == 128 ? 0u : (tid & 1) * 64u * C::W);
-                uint32_t w[12];
-#pragma unroll
-                for (int k = 0; k < 12; ++k) w[k] = 0;
-                if constexpr (NV == 1) {
-                    w[0] = (hi[0] & 0xffu) | (mid[0] & 0xffu) << 8 |
-                           (lo[0] & 0xffu) << 16;
-                } else if constexpr (NV == 2) {
-                    w[0] = hi[0] | mid[0] << 16;
-                    w[1] = lo[0];
-                } else {
-#pragma unroll
-                    for (int k = 0; k < NV / 4; ++k) {
-                        w[k] = hi[2 * k] | hi[2 * k + 1] << 16;
-                        w[NV / 4 + k] = mid[2 * k] | mid[2 * k + 1] << 16;
-                        w[NV / 2 + k] = lo[2 * k] | lo[2 * k + 1] << 16;
+                        for (int g = 0; g < NV; ++g)
+                            if (g < it.cols) at[(size_t)g * A.slots] = s[x][g];
                     }
                 }
-#pragma unroll
-                for (int k = 0; k < (3 * NV + 15) / 16; ++k)
-                    st_shared_v4(at + line_offset<C::W>(pr, k), w[4 * k],
-                                 w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
             }
-            if (!in) {
-                // a row that does not count may hold anything, NaN too: its
-                // weight is 0, its values have to be
-                ok = mbar_wait_or_abort(&bars.v_full[vs], (i / C::VS) & 1,
-                                        abort, c.status, 193) &&
-                     ok;
-                const int vr = D == 128 ? tid : tid >> 1;
-                const int c0 = D == 128 ? 0 : (tid & 1) * 4;
+            // lane g keeps column g's maximum
+            float top = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    st_shared_zero16(sV + vs * C::kTile +
-                                     line_offset<128>(vr, c0 + k));
+            for (int g = 0; g < NV; ++g) {
+                const float x = redux_max(fmaxf(s[0][g], s[1][g]));
+                if (lane == g) top = x;
+            }
+            if (lane < NV) red[b][warp][lane] = top;
+            // also agrees on whether every wait of the four warps ended well
+            fine = named_sync_and(1, 128, ok);
+            if (!fine) break;
+            if (lane < NV) {
+                const float mt = fmaxf(fmaxf(red[b][0][lane], red[b][1][lane]),
+                                       fmaxf(red[b][2][lane], red[b][3][lane]));
+                const float Mn = fmaxf(M, mt);
+                const float Mr = Mn == -INFINITY ? 0.0f : Mn;
+                const float be = ex2_approx(mt - Mr);
+                stat[b][warp][lane] =
+                    make_float4(mt == -INFINITY ? 0.0f : mt,
+                                ex2_approx(M - Mr), be,
+                                be * vmax * 0.00390625f);
+                M = Mn;
+            }
+            __syncwarp();
+            const float inv = vmax > 0.0f ? 256.0f / vmax : 0.0f;
+#pragma unroll
+            for (int x = 0; x < kSub; ++x) vrel[x] *= inv;
+            // the tokens' rows of P: all hi, all mid, all lo
+            uint32_t w[kSub][4 * ((3 * NV + 15) / 16)];
+#pragma unroll
+            for (int x = 0; x < kSub; ++x)
+#pragma unroll
+                for (int k = 0; k < 4 * ((3 * NV + 15) / 16); ++k) w[x][k] = 0;
+#pragma unroll
+            for (int g = 0; g < NV; g += 2) {
+                float y[kSub][2] = {};
+#pragma unroll
+                for (int k = 0; k < 2 && g + k < NV; ++k) {
+                    const float4 f = stat[b][warp][g + k];
+                    float p = 0.0f;
+#pragma unroll
+                    for (int x = 0; x < kSub; ++x) {
+                        const float z = ex2_approx(s[x][g + k] - f.x);
+                        p += z;
+                        y[x][k] = z * vrel[x];
+                    }
+                    l[g + k] = l[g + k] * f.y + f.z * p;
+                }
+#pragma unroll
+                for (int x = 0; x < kSub; ++x) {
+                    float *z = y[x];
+                    uint32_t h[3];
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        h[k] = e4m3x2(z[0], z[1]);
+                        const float2 f = from_e4m3x2(h[k]);
+                        z[0] = (z[0] - f.x) * 16.0f;
+                        z[1] = (z[1] - f.y) * 16.0f;
+                    }
+                    if constexpr (NV == 1) {
+                        w[x][0] = (h[0] & 0xffu) | (h[1] & 0xffu) << 8 |
+                                  (h[2] & 0xffu) << 16;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 3; ++k)
+                            w[x][(k * NV + g) / 4] |=
+                                h[k] << (8 * ((k * NV + g) & 3));
+                    }
+                }
+            }
+            // the O of the step before; its products have read P by then
+            if (i > 0) ok = take(i - 1) && ok;
+            if (begins && i > 0) finish(item - 2);
+            const int pr = D == 128 ? tid : tid >> 1;
+#pragma unroll
+            for (int x = 0; x < kSub; ++x) {
+                if (x < n) {
+                    const uint32_t at =
+                        sP + x * C::kP +
+                        (D == 128 ? 0u : (tid & 1) * 64u * C::W);
+#pragma unroll
+                    for (int k = 0; k < (3 * NV + 15) / 16; ++k)
+                        st_shared_v4(at + line_offset<C::W>(pr, k),
+                                     w[x][4 * k], w[x][4 * k + 1],
+                                     w[x][4 * k + 2], w[x][4 * k + 3]);
+                }
+                if (!in[x]) {
+                    // a row that does not count may hold anything, NaN too:
+                    // its weight is 0, its values have to be
+                    const int vs = (u + x) % C::VS;
+                    ok = mbar_wait_or_abort(&bars.v_full[vs],
+                                            ((u + x) / C::VS) & 1, abort,
+                                            c.status, 193) &&
+                         ok;
+                    const int c0 = D == 128 ? 0 : (tid & 1) * 4;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        st_shared_zero16(sV + vs * C::kTile +
+                                         line_offset<128>(pr, c0 + k));
+                }
             }
             __syncwarp();
             fence_proxy_async_smem();
             tc_fence_before();
-            mbar_arrive(&bars.p_ready[b]);
-            if (t > it.off) ok = take(i - 1) && ok;
-#pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                al[g] = al2[g];
-                be[g] = be2[g];
-            }
-            if (t + 1 < end) continue;
-
-            // ------------------------------------------- the item's end
-            ok = take(i) && ok;
-#pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                const float x = warp_sum(l[g]);
-                if (lane == 0) fin[g][warp] = x;
-                if (D == 64 && tid >= 64) half[g * 64 + tid - 64] = acc[g];
-            }
+            mbar_arrive(&bars.p_ready);
+            t += n;
+            u += n;
+        }
+        if (fine) {
+            ok = take(i - 1) && ok;
+            leave(item - 1);
             ok = named_sync_and(1, 128, ok);
-            if (!ok) break;
-            if (i + 1 == count && tid == 0) let_next_launch();
-#pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                if (g >= it.cols) break;
-                const float4 w = *(const float4 *)fin[g];
-                const float L = (w.x + w.y) + (w.z + w.w);
-                const int col = it.col0 + g;
-                float x = acc[g];
-                if (D == 64 && tid < 64) x += half[g * 64 + tid];
-                if (it.slot >= 0) {
-                    float *at = piece(A, blockIdx.x, it.slot, g);
-                    if (tid < D) at[tid] = x;
-                    if (tid == 0) {
-                        at[D] = M[g];
-                        at[D + 1] = L;
-                    }
-                } else {
-                    if (tid == 0)
-                        store_lse(A, it.b, it.h, it.n, col, M[g], L);
-                    if (tid < D && col % c.T < it.n)
-                        store_o(A, query_row(A, it.b, it.h, col), tid,
-                                L == 0.0f ? 0.0f : x / L);
-                }
-            }
-            // fin and half are written again only behind the next tile's
-            // barrier
+            if (tid == 0) let_next_launch();
+            if (ok) finish(item - 1);
         }
     }
     tc_fence_before();
@@ -706,7 +808,7 @@ cudaError_t launch_tc(const CacheAttn &A, cudaStream_t st) {
                             D == 128 ? c.ps : c.ps / 2);
     if (e != cudaSuccess) return e;
     return launch_after(k_cache_attn_tc<D, NV>, dim3(A.ctas), kTaThreads,
-                        C::kSmem + sizeof(int) * (c.B + 1), st, tmK, tmV, A);
+                        C::kSmem, st, tmK, tmV, A);
 }
 
 template <int D>

@@ -157,85 +157,95 @@ struct Start {
     int count;       // tiles of this CTA
 };
 
-// All NT threads of the CTA; prefix: B + 1 ints of shared memory. Writes the
-// CTA's entry of A.split.
+// The sequences from the CTA's first on, as far as they fit.
+constexpr int kNearSeqs = 32;
+
+// All NT threads of the CTA; near: kNearSeqs entries. Writes the CTA's entry
+// of A.split. A thread has a sequence (several, one after the other, when B is
+// larger): whether a bound of the range lies in its tiles it sees by itself.
 template <int NT>
-__device__ __forceinline__ Start divide(const CacheAttn &A, int *prefix) {
+__device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near) {
     __shared__ int warps[NT / 32], some[NT / 32];
     __shared__ Start mine;
     const CacheView &c = A.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    int base = 0, items = 0;
-    for (int b0 = 0; b0 < c.B; b0 += NT) {
-        const int b = b0 + tid;
-        int x = b < c.B ? sequence(A, b).tiles : 0;
-        const int own = __popc(__ballot_sync(0xffffffffu, x > 0));
+    const int rounds = (c.B + NT - 1) / NT, HC = c.Hkv * A.groups;
+    Seq own = {0, 0, 0, 0};
+    // tiles of the sequences up to the thread's, from the round's first on
+    auto sum = [&](int round) {
+        const int b = round * NT + tid;
+        own = {0, 0, 0, 0};
+        if (b < c.B) own = sequence(A, b);
+        int x = own.tiles;
+        const int live = __popc(__ballot_sync(0xffffffffu, x > 0));
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
+        __syncthreads();  // the round before has read
         if (lane == 31) {
             warps[warp] = x;
-            some[warp] = own;
+            some[warp] = live;
         }
         __syncthreads();
         for (int w = 0; w < warp; ++w) x += warps[w];
-        if (b < c.B) prefix[b + 1] = base + x;
+        return x;
+    };
+    if (tid == 0) {
+        mine = {0, 0, 0, 0};
+        A.split[blockIdx.x] = {0, 0, 0, 0};
+    }
+    int tiles = 0, items = 0, upto = 0;
+    for (int r = 0; r < rounds; ++r) {
+        upto = sum(r);
         for (int w = 0; w < NT / 32; ++w) {
-            base += warps[w];
+            tiles += warps[w];
             items += some[w];
         }
-        __syncthreads();
     }
-    if (tid == 0) prefix[0] = 0;
-    __syncthreads();
-    const int HC = c.Hkv * A.groups, k = blockIdx.x;
-    const long total = (long)base * HC;
-    const long n =
-        min(min((long)A.ctas, total), (long)items * HC * kCacheMaxPieces);
-    // the sequence of tile t: prefix[b] HC <= t < prefix[b + 1] HC
-    auto find = [&](long t) {
-        int lo = 0, hi = c.B;
-        while (hi - lo > 1) {
-            const int m = (lo + hi) >> 1;
-            if ((long)prefix[m] * HC <= t)
-                lo = m;
-            else
-                hi = m;
+    // the host has checked that total fits
+    const unsigned total = (unsigned)tiles * HC, k = blockIdx.x;
+    const unsigned n = min(min((unsigned)A.ctas, total),
+                           (unsigned)min((long)items * HC * kCacheMaxPieces,
+                                         1L << 30));
+    const unsigned q = n ? total / n : 0, rest = n ? total - q * n : 0;
+    // total k / n without the large product
+    auto bound = [&](unsigned i) { return q * i + rest * i / n; };
+    const unsigned t0 = k < n ? bound(k) : 0, t1 = k < n ? bound(k + 1) : 0;
+    int base = 0;
+    for (int r = 0; r < rounds && k < n; ++r) {
+        if (rounds > 1) upto = sum(r);
+        const unsigned z = (unsigned)(base + upto) * HC;
+        const unsigned a = z - (unsigned)own.tiles * HC;
+        const int b = r * NT + tid;
+        if (a <= t0 && t0 < z) {
+            const int in = (int)(t0 - a);
+            mine = {b, in / own.tiles, in % own.tiles, (int)(t1 - t0)};
         }
-        return lo;
-    };
-    const long t0 = k < n ? total * k / n : 0;
-    const long t1 = k < n ? total * (k + 1) / n : 0;
-    if (tid == 0) {
-        Start s = {0, 0, 0, (int)(t1 - t0)};
-        if (k < n) {
-            s.b = find(t0);
-            const int tiles = prefix[s.b + 1] - prefix[s.b];
-            const int in = (int)(t0 - (long)prefix[s.b] * HC);
-            s.hc = in / tiles;
-            s.off = in % tiles;
-        }
-        mine = s;
-    } else if (tid == 32) {
-        // an item that begins here and goes on behind t1
-        CacheSplit s = {0, 0, 0, 0};
-        if (k < n) {
-            s.b = find(t1 - 1);
-            const int tiles = prefix[s.b + 1] - prefix[s.b];
-            const long first = (long)prefix[s.b] * HC;
-            s.hc = (int)(t1 - 1 - first) / tiles;
-            const long a = first + (long)s.hc * tiles;
-            if (a >= t0 && a + tiles > t1) {
-                s.pieces = (int)range_owner(a + tiles - 1, total, n) - k + 1;
-                s.n = fresh(c, s.b);
+        if (a < t1 && t1 <= z) {
+            // the item of the last tile: does it begin here and go on?
+            const int hc = (int)(t1 - 1 - a) / own.tiles;
+            const unsigned i0 = a + (unsigned)hc * own.tiles;
+            const unsigned i1 = i0 + own.tiles;
+            if (i0 >= t0 && i1 > t1) {
+                const int last = (int)range_owner(i1 - 1, total, n);
+                A.split[k] = {b, hc, last - (int)k + 1, own.n};
             }
         }
-        A.split[k] = s;
+        if (rounds > 1)
+            for (int w = 0; w < NT / 32; ++w) base += warps[w];
     }
     __syncthreads();
-    return mine;
+    const Start s = mine;
+    if (rounds == 1) {
+        if (tid < c.B && tid >= s.b && tid < s.b + kNearSeqs)
+            near[tid - s.b] = own;
+    } else if (tid < kNearSeqs && s.b + tid < c.B) {
+        near[tid] = sequence(A, s.b + tid);
+    }
+    __syncthreads();
+    return s;
 }
 
 // A CTA's share of one item.
@@ -248,12 +258,16 @@ struct alignas(16) Item {
 };
 // Walks the items of a CTA's range.
 struct Walk {
-    int b, hc, off, left;
-    __device__ __forceinline__ Walk(const Start &s)
-        : b(s.b), hc(s.hc), off(s.off), left(s.count) {}
+    const Seq *near;
+    int b0, b, hc, off, left;
+    __device__ __forceinline__ Walk(const Start &s, const Seq *n)
+        : near(n), b0(s.b), b(s.b), hc(s.hc), off(s.off), left(s.count) {}
+    __device__ __forceinline__ Seq at(const CacheAttn &A, int b) const {
+        return b - b0 < kNearSeqs ? near[b - b0] : sequence(A, b);
+    }
     __device__ __forceinline__ Item next(const CacheAttn &A) {
-        Seq s = sequence(A, b);
-        while (s.tiles == 0) s = sequence(A, ++b);  // left > 0: there is one
+        Seq s = at(A, b);
+        while (s.tiles == 0) s = at(A, ++b);  // left > 0: there is one
         Item it;
         it.b = b;
         it.h = hc / A.groups;
@@ -287,11 +301,10 @@ __device__ __forceinline__ int last_seen(const CacheAttn &A, int len, int n,
     const int t = col % A.c.T;
     return t < n ? len - n + t : -1;
 }
-// Row of q, o and lse of column `col`.
+// Row of q, o and lse of column `col`: a head's columns lie side by side.
 __device__ __forceinline__ size_t query_row(const CacheAttn &A, int b, int h,
                                             int col) {
-    const int g = col / A.c.T, t = col % A.c.T;
-    return ((size_t)b * A.c.H + (size_t)h * A.c.G + g) * A.c.T + t;
+    return ((size_t)b * A.c.H + (size_t)h * A.c.G) * A.c.T + col;
 }
 
 __device__ __forceinline__ float *piece(const CacheAttn &A, int cta, int slot,
