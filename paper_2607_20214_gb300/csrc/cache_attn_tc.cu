@@ -11,12 +11,12 @@
 // the remainder, at most half a step of it, again has 4 bits, so hi and lo
 // hold q exactly (elements below 2^-14 of the row's largest lose bits below
 // 2^-22 of it). Two columns a query; scores are as exact as fp32 products. A
-// softmax weight is an fp32 number; three e4m3 numbers (256, 16 and 1 times
-// the remainder so far) hold it to 2^-12 relative, and to 2^-26 of the
-// tile's largest where it is smaller: a bf16 weight would have 2^-9. Each
-// tile's weights are relative to the tile's own maximum, so that a flat tail
-// behind one large score keeps its bits; sums and O, in registers, are
-// rescaled in fp32.
+// softmax weight is rounded to fp16, whose 11 bits (2^-11 relative at most,
+// and 2^-33 of the step's largest) three e4m3 numbers hold exactly, down to
+// 2^-26 of the largest: a bf16 weight would have 8 bits. A step's weights are
+// relative to the step's own maximum, so that a flat tail behind one large
+// score keeps its bits; sums (of the weights before rounding) and O, in
+// registers, are rescaled in fp32.
 //
 // Scales: a page's key scale multiplies the score in fp32; its value scale,
 // relative to the tile's largest (both powers of two), goes into the weight
@@ -146,6 +146,53 @@ __device__ __forceinline__ float redux_max(float x) {
     return r;
 }
 
+// Sums of NV columns over the warp: in lane i, column i / (32 / NV)'s. Every
+// exchange halves the columns that a lane still holds.
+template <int NV>
+__device__ __forceinline__ float column_sums(const float *x) {
+    float v[NV];
+#pragma unroll
+    for (int g = 0; g < NV; ++g) v[g] = x[g];
+    const int lane = threadIdx.x & 31;
+    int o = 16;
+#pragma unroll
+    for (int n = NV / 2; n >= 1; n /= 2, o /= 2) {
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int g = 0; g < n; ++g) {
+            const float mine = up ? v[g + n] : v[g];
+            const float his = up ? v[g] : v[g + n];
+            v[g] = mine + __shfl_xor_sync(0xffffffffu, his, o);
+        }
+    }
+#pragma unroll
+    for (; o >= 1; o /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    return v[0];
+}
+
+// fp16 pairs (low half first) and their e4m3 roundings.
+__device__ __forceinline__ uint32_t e4m3x2_of(uint32_t h) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+    return r;
+}
+__device__ __forceinline__ uint32_t f16x2_of(uint32_t e) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)e));
+    return r;
+}
+// 16 (a - b), exact for a >= 0 and b its e4m3 rounding: a has 11 bits, b the
+// first four of them.
+__device__ __forceinline__ uint32_t rest16(uint32_t a, uint32_t b) {
+    uint32_t x, r;
+    constexpr uint32_t k16 = 0x4c004c00u, km16 = 0xcc00cc00u;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(k16));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;"
+        : "=r"(r)
+        : "r"(b), "r"(km16), "r"(x));
+    return r;
+}
+
 // The pages of one tile, written by the producer.
 struct TileMeta {
     float ks[kMaxPagesPerTile];   // key scale
@@ -176,12 +223,11 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     __shared__ uint32_t tbase;
     __shared__ int abort_flag;
     // per step parity: every warp's maxima, and for every warp a column's
-    // reference, factor of the sums so far, factor of the step's sum and of
-    // its O
+    // numbers: minus its reference, score factor, factor of the sums so far,
+    // factor of the step's
     __shared__ float red[2][4][NV];
-    __shared__ float4 stat[2][4][NV];
+    __shared__ __align__(16) float stat[2][4][4][NV];
     __shared__ float4 fin[2][NV];  // sums of the four warps' tokens
-    __shared__ float half[D == 64 ? NV * 64 : 1];
     volatile int *abort = &abort_flag;
     const CacheView &c = A.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -518,14 +564,21 @@ __global__ void __launch_bounds__(kTaThreads, 2)
         const int shift = __ffs(c.ps) - 1;
         const int slot = tid >> shift, row = tid & (c.ps - 1);
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        float acc[NV], l[NV];
-        float M = -INFINITY;      // lane g: of column g
+        constexpr int NH = (NV + 1) / 2;  // columns in pairs
+        constexpr int NW = 4 * ((3 * NV + 15) / 16);  // words of a P row
+        float2 acc[NH], l[NH];
+        float M = -INFINITY;      // lane g: of column g, in the scores' unit
         Item it = {}, last = {};  // this step's, the unfinished one before
-        float lastM = 0.0f;
+        float lastM = 0.0f, factor = 0.0f;
         int item = 0, t = 0, end = 0;
         bool ok = true, fine = count > 0;
 #pragma unroll
-        for (int g = 0; g < NV; ++g) acc[g] = l[g] = 0.0f;
+        for (int g = 0; g < NH; ++g) acc[g] = l[g] = make_float2(0.0f, 0.0f);
+        // column pair g of a row of stat
+        auto pair = [&](const float *p, int g) {
+            return NV == 1 ? make_float2(p[0], 0.0f)
+                           : *(const float2 *)(p + 2 * g);
+        };
         // acc takes step j's O
         auto take = [&](int j) {
             const bool done = wait(&bars.o_full, j & 1, 190);
@@ -535,12 +588,17 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             if (D == 64 && warp >= 2) at += C::NP;
             tmem_read<C::NP>(at, o);
             tmem_wait_ld();
+            const float(*f)[NV] = stat[j & 1][warp];
+            const float2 c1 = make_float2(0.0625f, 0.0625f);
+            const float2 c2 = make_float2(0.00390625f, 0.00390625f);
 #pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                const float4 f = stat[j & 1][warp][g];
-                acc[g] = acc[g] * f.y +
-                         f.w * (o[g] + 0.0625f * o[NV + g] +
-                                0.00390625f * o[2 * NV + g]);
+            for (int g = 0; g < NH; ++g) {
+                auto at = [&](int k) {
+                    return make_float2(o[k * NV + 2 * g],
+                                       NV == 1 ? 0.0f : o[k * NV + 2 * g + 1]);
+                };
+                const float2 x = fma2(c2, at(2), fma2(c1, at(1), at(0)));
+                acc[g] = fma2(pair(f[3], g), x, mul2(acc[g], pair(f[2], g)));
             }
             tc_fence_before();
             return done;
@@ -548,40 +606,45 @@ __global__ void __launch_bounds__(kTaThreads, 2)
         // the sums of a finished item, where every warp finds them behind the
         // next barrier
         auto leave = [&](int k) {
+            const float x = column_sums<NV>((const float *)l);
+            if (lane % (32 / NV) == 0)
+                ((float *)&fin[k & 1][lane / (32 / NV)])[warp] = x;
 #pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                const float x = warp_sum(l[g]);
-                if (lane == 0) ((float *)&fin[k & 1][g])[warp] = x;
-                l[g] = 0.0f;
-            }
+            for (int g = 0; g < NH; ++g) l[g] = make_float2(0.0f, 0.0f);
             last = it;
-            lastM = M;
+            lastM = M * factor;
             M = -INFINITY;
         };
-        // item k is complete in acc
+        // Item k is complete in acc: it leaves through the P buffer, which no
+        // product reads now, as whole rows.
         auto finish = [&](int k) {
-            if (D == 64) {
-                if (tid >= 64)
+            float *buf = (float *)(smem_raw + (sP - smem_u32(smem_raw)));
 #pragma unroll
-                    for (int g = 0; g < NV; ++g)
-                        half[g * 64 + tid - 64] = acc[g];
-                named_sync(1, 128);
-            }
-            const bool all = last.n == c.T;
+            for (int g = 0; g < NV; ++g)
+                buf[g * 128 + tid] = g & 1 ? acc[g / 2].y : acc[g / 2].x;
+#pragma unroll
+            for (int g = 0; g < NH; ++g) acc[g] = make_float2(0.0f, 0.0f);
+            named_sync(1, 128);
             const size_t r0 = query_row(A, last.b, last.h, last.col0);
-#pragma unroll
-            for (int g = 0; g < NV; ++g) {
-                if (g >= last.cols) break;
-                float x = acc[g];
-                if (D == 64 && tid < 64) x += half[g * 64 + tid];
-                if (tid >= D) continue;
+#pragma unroll 1
+            for (int e = tid; e < last.cols * (D / 4); e += 128) {
+                const int g = e / (D / 4), ch = e % (D / 4) * 4;
+                float4 x = *(const float4 *)(buf + g * 128 + ch);
+                if (D == 64) {
+                    const float4 y = *(const float4 *)(buf + g * 128 + 64 + ch);
+                    x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+                }
                 if (last.slot >= 0) {
-                    piece(A, blockIdx.x, last.slot, g)[tid] = x;
-                } else if (all || (last.col0 + g) % c.T < last.n) {
+                    float *at = piece(A, blockIdx.x, last.slot, g) + ch;
+                    *(float2 *)at = make_float2(x.x, x.y);
+                    *(float2 *)(at + 2) = make_float2(x.z, x.w);
+                } else if ((last.col0 + g) % c.T < last.n) {
                     const float4 w = fin[k & 1][g];
                     const float L = (w.x + w.y) + (w.z + w.w);
-                    ((__nv_bfloat16 *)A.o)[(r0 + g) * D + tid] =
-                        __float2bfloat16_rn(L == 0.0f ? 0.0f : x / L);
+                    const float f = L == 0.0f ? 0.0f : 1.0f / L;
+                    *(uint2 *)((__nv_bfloat16 *)A.o + (r0 + g) * D + ch) =
+                        make_uint2(pack_bf16x2(x.x * f, x.y * f),
+                                   pack_bf16x2(x.z * f, x.w * f));
                 }
             }
             if (tid < last.cols) {  // column `tid`
@@ -596,8 +659,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                               lastM, L);
                 }
             }
-#pragma unroll
-            for (int g = 0; g < NV; ++g) acc[g] = 0.0f;
+            named_sync(1, 128);
         };
         int i = 0;
         for (int u = 0; u < count; ++i) {
@@ -607,20 +669,20 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 const int qs = item & 1;
                 ok = wait(&bars.q_full[qs], (item >> 1) & 1, 195) && ok;
                 it = ok ? items[qs] : Item{};
+                factor = lane < NV ? factors[qs][lane] : 0.0f;
                 t = it.off;
                 end = it.off + it.count;
                 ++item;
             }
+            // a second tile that the item does not have counts as one without
+            // rows
             const int n = min(end - t, kSub), b = i & 1;
-            const float *factor = factors[(item - 1) & 1];
-            const int *limit = limits[(item - 1) & 1];
-            float s[kSub][NV], vrel[kSub], vmax = 0.0f;
+            float vrel[kSub], ks[kSub], vmax = 0.0f;
             bool in[kSub];
             int pos[kSub];
-            float ks[kSub];
 #pragma unroll
             for (int x = 0; x < kSub; ++x) {
-                in[x] = true;
+                in[x] = false;
                 ks[x] = vrel[x] = 0.0f;
                 pos[x] = 0;
                 if (x < n) {
@@ -635,31 +697,44 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                     vmax = fmaxf(vmax, m.vmax);
                 }
             }
+            const bool free = in[0] && in[1] &&
+                              max(pos[0], pos[1]) <= it.len - it.n;
             ok = wait(&bars.s_full[b], (i >> 1) & 1, 192) && ok;
             tc_fence_after();
+            float2 s[kSub][NH];
 #pragma unroll
             for (int x = 0; x < kSub; ++x) {
-                if (x < n) {
-                    float y[2 * NV];
-                    tmem_read<2 * NV>(tm + lanes + (b * kSub + x) * C::N1, y);
-                    tmem_wait_ld();
-                    const bool all = pos[x] <= it.len - it.n;
+                float y[2 * NV];
+                tmem_read<2 * NV>(tm + lanes + (b * kSub + x) * C::N1, y);
+                tmem_wait_ld();
+                const float2 c1 = make_float2(0.0625f, 0.0625f);
+                const float2 kk = make_float2(ks[x], ks[x]);
 #pragma unroll
-                    for (int g = 0; g < NV; ++g) {
-                        s[x][g] = (y[g] + 0.0625f * y[NV + g]) *
-                                  (ks[x] * factor[g]);
-                        if (!in[x] || (!all && pos[x] > limit[g]))
-                            s[x][g] = -INFINITY;
-                    }
-                } else {
-#pragma unroll
-                    for (int g = 0; g < NV; ++g) s[x][g] = -INFINITY;
+                for (int g = 0; g < NH; ++g) {
+                    const float2 hi = make_float2(y[2 * g],
+                                                  NV == 1 ? 0.0f
+                                                          : y[2 * g + 1]);
+                    const float2 lo = make_float2(y[NV + 2 * g],
+                                                  NV == 1 ? 0.0f
+                                                          : y[NV + 2 * g + 1]);
+                    s[x][g] = mul2(fma2(c1, lo, hi), kk);
                 }
             }
             tc_fence_before();
-            if (t + n == end) {  // the queries may go
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.q_empty[(item - 1) & 1]);
+            if (!__all_sync(0xffffffffu, free)) {
+                // rows that do not count, keys behind a query
+                const int *limit = limits[(item - 1) & 1];
+#pragma unroll
+                for (int x = 0; x < kSub; ++x)
+#pragma unroll
+                    for (int g = 0; g < NV; ++g)
+                        if (!in[x] || (pos[x] > it.len - it.n &&
+                                       pos[x] > limit[g])) {
+                            if (g & 1)
+                                s[x][g / 2].y = -INFINITY;
+                            else
+                                s[x][g / 2].x = -INFINITY;
+                        }
             }
             if (A.scores) {
 #pragma unroll
@@ -671,15 +746,24 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                                      it.col0) * A.slots + w;
 #pragma unroll
                         for (int g = 0; g < NV; ++g)
-                            if (g < it.cols) at[(size_t)g * A.slots] = s[x][g];
+                            if (g < it.cols)
+                                at[(size_t)g * A.slots] =
+                                    (g & 1 ? s[x][g / 2].y : s[x][g / 2].x) *
+                                    factors[(item - 1) & 1][g];
                     }
                 }
+            }
+            if (t + n == end) {  // the queries may go
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.q_empty[(item - 1) & 1]);
             }
             // lane g keeps column g's maximum
             float top = -INFINITY;
 #pragma unroll
             for (int g = 0; g < NV; ++g) {
-                const float x = redux_max(fmaxf(s[0][g], s[1][g]));
+                const float x =
+                    redux_max(g & 1 ? fmaxf(s[0][g / 2].y, s[1][g / 2].y)
+                                    : fmaxf(s[0][g / 2].x, s[1][g / 2].x));
                 if (lane == g) top = x;
             }
             if (lane < NV) red[b][warp][lane] = top;
@@ -691,59 +775,51 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                                        fmaxf(red[b][2][lane], red[b][3][lane]));
                 const float Mn = fmaxf(M, mt);
                 const float Mr = Mn == -INFINITY ? 0.0f : Mn;
-                const float be = ex2_approx(mt - Mr);
-                stat[b][warp][lane] =
-                    make_float4(mt == -INFINITY ? 0.0f : mt,
-                                ex2_approx(M - Mr), be,
-                                be * vmax * 0.00390625f);
+                float(*f)[NV] = stat[b][warp];
+                f[0][lane] = mt == -INFINITY ? 0.0f : -mt * factor;
+                f[1][lane] = factor;
+                f[2][lane] = ex2_approx((M - Mr) * factor);
+                f[3][lane] = ex2_approx((mt - Mr) * factor) * vmax *
+                             0.00390625f;
                 M = Mn;
             }
             __syncwarp();
             const float inv = vmax > 0.0f ? 256.0f / vmax : 0.0f;
+            const float2 inv2 = make_float2(inv, inv);
+            uint32_t w[kSub][NW];
 #pragma unroll
-            for (int x = 0; x < kSub; ++x) vrel[x] *= inv;
-            // the tokens' rows of P: all hi, all mid, all lo
-            uint32_t w[kSub][4 * ((3 * NV + 15) / 16)];
+            for (int x = 0; x < kSub; ++x) {
+                vrel[x] *= inv;
 #pragma unroll
-            for (int x = 0; x < kSub; ++x)
+                for (int k = 0; k < NW; ++k) w[x][k] = 0;
+            }
 #pragma unroll
-                for (int k = 0; k < 4 * ((3 * NV + 15) / 16); ++k) w[x][k] = 0;
-#pragma unroll
-            for (int g = 0; g < NV; g += 2) {
-                float y[kSub][2] = {};
-#pragma unroll
-                for (int k = 0; k < 2 && g + k < NV; ++k) {
-                    const float4 f = stat[b][warp][g + k];
-                    float p = 0.0f;
-#pragma unroll
-                    for (int x = 0; x < kSub; ++x) {
-                        const float z = ex2_approx(s[x][g + k] - f.x);
-                        p += z;
-                        y[x][k] = z * vrel[x];
-                    }
-                    l[g + k] = l[g + k] * f.y + f.z * p;
-                }
+            for (int g = 0; g < NH; ++g) {
+                const float(*f)[NV] = stat[b][warp];
+                const float2 nref = pair(f[0], g), fac = pair(f[1], g);
+                float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
                 for (int x = 0; x < kSub; ++x) {
-                    float *z = y[x];
-                    uint32_t h[3];
+                    float2 p = fma2(s[x][g], fac, nref);
+                    p.x = ex2_approx(p.x);
+                    if (NV > 1) p.y = ex2_approx(p.y);
+                    sum = add2(sum, p);
+                    p = mul2(p, make_float2(vrel[x], vrel[x]));
+                    // the pieces of the weights, hi, mid, lo
+                    uint32_t r = pack_f16x2(p.x, p.y);
 #pragma unroll
                     for (int k = 0; k < 3; ++k) {
-                        h[k] = e4m3x2(z[0], z[1]);
-                        const float2 f = from_e4m3x2(h[k]);
-                        z[0] = (z[0] - f.x) * 16.0f;
-                        z[1] = (z[1] - f.y) * 16.0f;
-                    }
-                    if constexpr (NV == 1) {
-                        w[x][0] = (h[0] & 0xffu) | (h[1] & 0xffu) << 8 |
-                                  (h[2] & 0xffu) << 16;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 3; ++k)
-                            w[x][(k * NV + g) / 4] |=
-                                h[k] << (8 * ((k * NV + g) & 3));
+                        const uint32_t e = e4m3x2_of(r);
+                        if (k < 2) r = rest16(r, f16x2_of(e));
+                        if constexpr (NV == 1)
+                            w[x][0] |= (e & 0xffu) << (8 * k);
+                        else
+                            w[x][(k * NV + 2 * g) / 4] |=
+                                e << (8 * ((k * NV + 2 * g) & 3));
                     }
                 }
+                l[g] = fma2(pair(f[3], g), mul2(sum, inv2),
+                            mul2(l[g], pair(f[2], g)));
             }
             // the O of the step before; its products have read P by then
             if (i > 0) ok = take(i - 1) && ok;
@@ -751,17 +827,14 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             const int pr = D == 128 ? tid : tid >> 1;
 #pragma unroll
             for (int x = 0; x < kSub; ++x) {
-                if (x < n) {
-                    const uint32_t at =
-                        sP + x * C::kP +
-                        (D == 128 ? 0u : (tid & 1) * 64u * C::W);
+                const uint32_t at = sP + x * C::kP +
+                                    (D == 128 ? 0u : (tid & 1) * 64u * C::W);
 #pragma unroll
-                    for (int k = 0; k < (3 * NV + 15) / 16; ++k)
-                        st_shared_v4(at + line_offset<C::W>(pr, k),
-                                     w[x][4 * k], w[x][4 * k + 1],
-                                     w[x][4 * k + 2], w[x][4 * k + 3]);
-                }
-                if (!in[x]) {
+                for (int k = 0; k < NW / 4; ++k)
+                    st_shared_v4(at + line_offset<C::W>(pr, k), w[x][4 * k],
+                                 w[x][4 * k + 1], w[x][4 * k + 2],
+                                 w[x][4 * k + 3]);
+                if (!in[x] && x < n) {
                     // a row that does not count may hold anything, NaN too:
                     // its weight is 0, its values have to be
                     const int vs = (u + x) % C::VS;

@@ -9,11 +9,18 @@
 namespace elsaa {
 namespace cache {
 
+// Out of line: faults are rare, and the code before a kernel's first loads is
+// fetched while nothing else runs.
+static __device__ __noinline__ void report_rare(DeviceStatus *st, int code,
+                                                int where, int a, int b) {
+    report(st, code, where, a, b);
+}
+
 // Tokens of sequence b, clipped to its table row.
 __device__ __forceinline__ int tokens(const CacheView &c, int b) {
     const int n = c.lengths[b], cap = c.max_pages * c.ps;
     if (n < 0 || n > cap) {
-        report(c.status, kDevCacheLength, b, n, cap);
+        report_rare(c.status, kDevCacheLength, b, n, cap);
         return n < 0 ? 0 : cap;
     }
     return n;
@@ -24,7 +31,7 @@ __device__ __forceinline__ int fresh(const CacheView &c, int b) {
     if (!c.new_len) return c.T;
     const int n = c.new_len[b];
     if (n < 0 || n > c.T) {
-        report(c.status, kDevCacheLength, b, n, c.T);
+        report_rare(c.status, kDevCacheLength, b, n, c.T);
         return n < 0 ? 0 : c.T;
     }
     return n;
@@ -34,7 +41,7 @@ __device__ __forceinline__ int fresh(const CacheView &c, int b) {
 __device__ __forceinline__ int checked_page(const CacheView &c, int id, int b,
                                             int p) {
     if ((unsigned)id < (unsigned)c.num_pages) return id;
-    report(c.status, kDevCachePage, b, p, id);
+    report_rare(c.status, kDevCachePage, b, p, id);
     return -1;
 }
 __device__ __forceinline__ int page_id(const CacheView &c, int b, int p) {
