@@ -83,14 +83,21 @@ cudaError_t launch_cache_append(const CacheView &c, const void *k,
 cudaError_t launch_cache_select(const CacheView &c, const void *q, int n_sel,
                                 int first, int last, int32_t *pages,
                                 float *scores, cudaStream_t st);
-// kept: [B, Hkv, keep]; count: [B] tokens kept.
+// rows: [B, Hkv, keep] pool rows of the kept tokens (page * page_size + row;
+// -1: their page is outside the pool), kept: their positions, or NULL;
+// count: [B] tokens kept.
+struct CacheKept {
+    int32_t *rows, *kept;
+    int *count;
+    float *weight_out;
+    int dst_pages;
+};
 cudaError_t launch_cache_keep(const CacheView &c, const float *weight,
-                              int keep, int recent, int32_t *kept, int *count,
+                              int keep, int recent, const CacheKept &out,
                               cudaStream_t st);
-cudaError_t launch_cache_compact(const CacheView &c, const float *weight,
-                                 int keep, const int32_t *kept,
-                                 const int *count, const int32_t *dst_table,
-                                 int dst_pages, float *weight_out,
+cudaError_t launch_cache_compact(const CacheView &c, int keep,
+                                 const int32_t *rows, const int *count,
+                                 const int32_t *dst_table, int dst_pages,
                                  int32_t *lengths_out, cudaStream_t st);
 
 // Runs a launch under its name in the per-kernel timing of

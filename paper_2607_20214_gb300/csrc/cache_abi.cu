@@ -105,7 +105,7 @@ int check_queries(const CacheView &c) {
 }
 
 // Workspace of one call: split items | lse2 | pieces | scores (attention), or
-// page keys (select), or counts | kept (evict).
+// page keys (select), or counts | pool rows (evict).
 struct Layout {
     size_t split, lse2, part, scores, total;
     int cols, groups, ctas;
@@ -314,20 +314,21 @@ extern "C" int elsaa_cache_evict(const elsaa_cache *cache,
     if (dst_pages <= 0 || (long)dst_pages * c.ps < keep)
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "dst_pages * page_size must be at least keep");
-    const size_t need = evict_bytes(c, kept ? 0 : keep);
-    rc = check_workspace(workspace, workspace_bytes, need);
+    rc = check_workspace(workspace, workspace_bytes, evict_bytes(c, keep));
     if (rc != ELSAA_OK) return rc;
-    int *count = (int *)workspace;
-    if (!kept)
-        kept = (int32_t *)((char *)workspace +
+    CacheKept out;
+    out.count = (int *)workspace;
+    out.rows = (int32_t *)((char *)workspace +
                            align256(sizeof(int) * (size_t)c.B));
+    out.kept = kept;
+    out.weight_out = weight_out;
+    out.dst_pages = dst_pages;
     cudaStream_t st = (cudaStream_t)stream;
     ELSAA_CACHE_LAUNCH("cache_keep", st,
-                       launch_cache_keep(c, weight, keep, recent, kept, count,
-                                         st));
+                       launch_cache_keep(c, weight, keep, recent, out, st));
     ELSAA_CACHE_LAUNCH("cache_compact", st,
-                       launch_cache_compact(c, weight, keep, kept, count,
-                                            dst_table, dst_pages, weight_out,
-                                            lengths_out, st));
+                       launch_cache_compact(c, keep, out.rows, out.count,
+                                            dst_table, dst_pages, lengths_out,
+                                            st));
     return ELSAA_OK;
 }

@@ -100,11 +100,11 @@ __device__ __forceinline__ void find_threshold(K key, int n, int m,
     ties = left;
 }
 
-// Writes the selected indices, increasing, to out[0 .. m).
-template <int NT, typename K>
+// put(k, i) for the k-th selected index i, increasing.
+template <int NT, typename K, typename P>
 __device__ __forceinline__ void write_selected(K key, int n, uint32_t thr,
                                                int ties, TopkShared<NT> &S,
-                                               int32_t *out) {
+                                               P put) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int W = NT / 32;
     const int run = ((n + W - 1) / W + 31) & ~31;
@@ -135,36 +135,57 @@ __device__ __forceinline__ void write_selected(K key, int n, uint32_t thr,
         const bool take = in && (u > thr || (u == thr &&
                                              eq + __popc(me & below) < ties));
         const uint32_t mt = __ballot_sync(0xffffffffu, take);
-        if (take) out[at + __popc(mt & below)] = i + lane;
+        if (take) put(at + __popc(mt & below), i + lane);
         at += __popc(mt);
         eq += __popc(me);
     }
 }
 
 // -------------------------------------------------------------- page scores
+//
+// A cluster per sequence and head: its CTAs score the pages, one a thread (the
+// bounds of a page are 2 d bytes, sixteen 16-byte loads in flight a thread at
+// d = 128), and leave the keys in the first CTA's shared memory, which
+// selects. One launch; with the keys in HBM between two it was 10 us longer.
+constexpr int kScThreads = 512;
+constexpr int kScShared = 32768;  // keys that fit there
+// Up to as many pages the rank of every key is counted directly.
+constexpr int kScDirect = 128;
 
-constexpr int kScThreads = 128;  // one page a thread
+__device__ __forceinline__ void put_remote(uint32_t addr, uint32_t v) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(addr));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v)
+                 : "memory");
+}
 
 // Queries as pairs of 8-bit rows max(qhat, 0), min(qhat, 0): with hi >= lo,
 // max(q hi, q lo) = max(q, 0) hi + min(q, 0) lo.
 template <typename T, int D>
-__global__ void __launch_bounds__(kScThreads)
-    k_cache_scores(CacheView c, const T *__restrict__ q, int first, int last,
-                   uint32_t *__restrict__ keys) {
+__global__ void __launch_bounds__(kScThreads, 1)
+    k_cache_select(const __grid_constant__ CacheView c,
+                   const T *__restrict__ q, int n_sel, int first, int last,
+                   int32_t *__restrict__ pages, uint32_t *__restrict__ keys,
+                   int shared_keys) {
     wait_for_stream();
-    extern __shared__ uint4 sq[];  // [queries][2][D / 16]
+    extern __shared__ uint4 sq[];  // [queries][2][D / 16], then the keys
+    __shared__ TopkShared<kScThreads> S;
     __shared__ float qscale[128];
+    // a CTA's shared memory is written only once it runs
+    if (gridDim.x > 1) tc::cluster_sync();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int h = blockIdx.y, b = blockIdx.z;
+    const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const size_t bh = (size_t)b * c.Hkv + h;
     const int n = fresh(c, b), len = tokens(c, b);
-    const int pages = (len + c.ps - 1) / c.ps;
-    const int p = blockIdx.x * kScThreads + tid;
-    if (n == 0 || blockIdx.x * kScThreads >= pages) return;
-    const int id = p < pages ? page_id(c, b, p) : -1;
+    const int np = n == 0 ? 0 : (len + c.ps - 1) / c.ps;
     constexpr int W = D / 16;
+    uint32_t *own = (uint32_t *)(sq + (size_t)c.G * c.T * 2 * W);
     uint4 hi[W], lo[W];
     float ks = 0.0f;
-    if (id >= 0) {
+    int id = -1;
+    auto fetch = [&](int p) {
+        id = p < np ? page_id(c, b, p) : -1;
+        if (id < 0) return;
         const size_t ph = (size_t)id * c.Hkv + h;
         const uint4 *at = (const uint4 *)(c.bounds + ph * 2 * D);
 #pragma unroll
@@ -173,14 +194,15 @@ __global__ void __launch_bounds__(kScThreads)
             lo[i] = at[W + i];
         }
         ks = 4.0f * c.ks[ph];
-    }
-    // a warp quantises a query: D / 32 values a lane
-    constexpr int V = D / 32;
-    int rows = 0;
-    for (int g = 0; g < c.G; ++g)
-        for (int t = 0; t < n; ++t, ++rows) {
-            if (rows % (kScThreads / 32) != warp) continue;
-            const T *x = q + (((size_t)b * c.H + (size_t)h * c.G + g) * c.T + t) * D + lane * V;
+    };
+    int p = rank * kScThreads + tid;
+    const int step = gridDim.x * kScThreads;
+    if (rank * kScThreads < np) {
+        fetch(p);
+        // a warp quantises a query: D / 32 values a lane
+        constexpr int V = D / 32;
+        for (int r = warp; r < c.G * c.T; r += kScThreads / 32) {
+            const T *x = q + ((bh * c.G) * c.T + r) * D + lane * V;
             float y[V], amax = 0.0f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -189,7 +211,7 @@ __global__ void __launch_bounds__(kScThreads)
             }
             const int e = query_exponent(warp_max(amax));
             const float f = pow2(-e);
-            int8_t *at = (int8_t *)&sq[rows * 2 * W] + lane * V;
+            int8_t *at = (int8_t *)&sq[r * 2 * W] + lane * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int v = __float2int_rn(
@@ -198,88 +220,176 @@ __global__ void __launch_bounds__(kScThreads)
                 at[i] = (int8_t)max(z, 0);
                 at[D + i] = (int8_t)min(z, 0);
             }
-            if (lane == 0) qscale[rows] = pow2(e);
+            if (lane == 0) qscale[r] = r % c.T < n ? pow2(e) : -1.0f;
         }
-    __syncthreads();
-    if (p >= pages) return;
-    float best = -INFINITY;
-    if (id >= 0) {
-        for (int r = 0; r < rows; ++r) {
-            int s = 0;
-            const uint4 *a = sq + r * 2 * W;
+        __syncthreads();
+        while (p < np) {
+            float best = -INFINITY;
+            if (id >= 0) {
+                for (int r = 0; r < c.G * c.T; ++r) {
+                    const float f = qscale[r];
+                    if (f < 0.0f) continue;  // no query
+                    int s = 0;
+                    const uint4 *a = sq + r * 2 * W;
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                const uint4 u = a[i], v = a[W + i];
-                s = __dp4a((int)u.x, (int)hi[i].x, s);
-                s = __dp4a((int)u.y, (int)hi[i].y, s);
-                s = __dp4a((int)u.z, (int)hi[i].z, s);
-                s = __dp4a((int)u.w, (int)hi[i].w, s);
-                s = __dp4a((int)v.x, (int)lo[i].x, s);
-                s = __dp4a((int)v.y, (int)lo[i].y, s);
-                s = __dp4a((int)v.z, (int)lo[i].z, s);
-                s = __dp4a((int)v.w, (int)lo[i].w, s);
+                    for (int i = 0; i < W; ++i) {
+                        const uint4 u = a[i], v = a[W + i];
+                        s = __dp4a((int)u.x, (int)hi[i].x, s);
+                        s = __dp4a((int)u.y, (int)hi[i].y, s);
+                        s = __dp4a((int)u.z, (int)hi[i].z, s);
+                        s = __dp4a((int)u.w, (int)hi[i].w, s);
+                        s = __dp4a((int)v.x, (int)lo[i].x, s);
+                        s = __dp4a((int)v.y, (int)lo[i].y, s);
+                        s = __dp4a((int)v.z, (int)lo[i].z, s);
+                        s = __dp4a((int)v.w, (int)lo[i].w, s);
+                    }
+                    best = fmaxf(best, (float)s * f * ks);
+                }
             }
-            best = fmaxf(best, (float)s * qscale[r] * ks);
+            const bool must = p < first || p >= np - last;
+            const uint32_t key = must ? kKeyFirst : order_key(best);
+            if (!shared_keys)
+                keys[bh * c.max_pages + p] = key;
+            else if (rank == 0)
+                own[p] = key;
+            else
+                put_remote(tc::smem_u32(own + p), key);
+            p += step;
+            fetch(p);
         }
     }
-    const bool must = p < first || p >= pages - last;
-    keys[((size_t)b * c.Hkv + h) * c.max_pages + p] =
-        must ? kKeyFirst : order_key(best);
-}
-
-constexpr int kSpThreads = 256;
-
-__global__ void __launch_bounds__(kSpThreads)
-    k_cache_pages(CacheView c, const uint32_t *__restrict__ keys, int n_sel,
-                  int32_t *__restrict__ pages) {
-    wait_for_stream();
-    __shared__ TopkShared<kSpThreads> S;
-    const int h = blockIdx.x, b = blockIdx.y;
-    const size_t bh = (size_t)b * c.Hkv + h;
-    const int n = fresh(c, b) > 0 ? (tokens(c, b) + c.ps - 1) / c.ps : 0;
-    const int m = min(n, n_sel);
+    if (gridDim.x > 1)
+        tc::cluster_sync();
+    else
+        __syncthreads();
+    if (rank > 0) return;
+    const int m = min(np, n_sel);
     int32_t *out = pages + bh * n_sel;
-    for (int i = m + threadIdx.x; i < n_sel; i += kSpThreads) out[i] = -1;
+    for (int i = m + tid; i < n_sel; i += kScThreads) out[i] = -1;
     if (m == 0) return;
-    const uint32_t *kk = keys + bh * c.max_pages;
-    if (m == n) {
-        for (int i = threadIdx.x; i < n; i += kSpThreads) out[i] = i;
+    if (m == np) {
+        for (int i = tid; i < np; i += kScThreads) out[i] = i;
         return;
     }
+    const uint32_t *kk = shared_keys ? own : keys + bh * c.max_pages;
     auto key = [=](int i) { return kk[i]; };
+    if (np <= kScDirect) {
+        // rank of every key: the larger ones, and the equal ones before it
+        bool take = false;
+        if (tid < np) {
+            const uint32_t mine = kk[tid];
+            int above = 0;
+            for (int i = 0; i < np; ++i) {
+                const uint32_t x = kk[i];
+                above += x > mine || (x == mine && i < tid);
+            }
+            take = above < m;
+        }
+        const uint32_t votes = __ballot_sync(0xffffffffu, take);
+        if (lane == 0) S.warps[warp][0] = __popc(votes);
+        __syncthreads();
+        int at = __popc(votes & ((1u << lane) - 1));
+        for (int w = 0; w < warp; ++w) at += S.warps[w][0];
+        if (take) out[at] = tid;
+        return;
+    }
     uint32_t thr;
     int ties;
-    find_threshold<kSpThreads>(key, n, m, S, thr, ties);
-    write_selected<kSpThreads>(key, n, thr, ties, S, out);
+    find_threshold<kScThreads>(key, np, m, S, thr, ties);
+    write_selected<kScThreads>(key, np, thr, ties, S,
+                               [=](int k, int i) { out[k] = i; });
 }
 
 // ------------------------------------------------------------- kept tokens
-
+//
+// A CTA per sequence and head. The weights are read once, as many at a time
+// as there are registers for, and their keys kept in shared memory (up to
+// kKpShared tokens; longer rows are read again by every pass).
 constexpr int kKpThreads = 1024;
+constexpr int kKpShared = 49152;
 
 __global__ void __launch_bounds__(kKpThreads)
-    k_cache_keep(CacheView c, const float *__restrict__ weight, int keep,
-                 int recent, int32_t *__restrict__ kept,
-                 int *__restrict__ count) {
+    k_cache_keep(const __grid_constant__ CacheView c,
+                 const float *__restrict__ weight, int keep, int recent,
+                 const CacheKept out, int shared_keys) {
     wait_for_stream();
+    extern __shared__ uint32_t own[];
     __shared__ TopkShared<kKpThreads> S;
-    const int h = blockIdx.x, b = blockIdx.y;
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const size_t bh = (size_t)b * c.Hkv + h;
     const int n = tokens(c, b), m = min(n, keep), safe = n - recent;
-    int32_t *out = kept + bh * keep;
-    if (h == 0 && threadIdx.x == 0) count[b] = m;
-    for (int i = m + threadIdx.x; i < keep; i += kKpThreads) out[i] = -1;
+    const float *w = weight + bh * c.max_pages * c.ps;
+    int32_t *kept = out.kept ? out.kept + bh * keep : nullptr;
+    int32_t *rows = out.rows + bh * keep;
+    float *wout = out.weight_out + bh * out.dst_pages * c.ps;
+    if (h == 0 && tid == 0) out.count[b] = m;
+    if (kept)
+        for (int i = m + tid; i < keep; i += kKpThreads) kept[i] = -1;
     if (m == 0) return;
+    // the rows' places are found here, where the reads of the table overlap
+    auto put = [&](int k, int i) {
+        const int id = page_id(c, b, i / c.ps);
+        rows[k] = id < 0 ? -1 : id * c.ps + i % c.ps;
+        wout[k] = w[i];
+        if (kept) kept[k] = i;
+    };
     if (m == n) {
-        for (int i = threadIdx.x; i < n; i += kKpThreads) out[i] = i;
+        for (int i = tid; i < n; i += kKpThreads) put(i, i);
         return;
     }
-    const float *w = weight + bh * c.max_pages * c.ps;
-    auto key = [=](int i) { return i < safe ? order_key(w[i]) : kKeyFirst; };
     uint32_t thr;
     int ties;
-    find_threshold<kKpThreads>(key, n, m, S, thr, ties);
-    write_selected<kKpThreads>(key, n, thr, ties, S, out);
+    if (shared_keys) {
+        constexpr int U = 8;
+        for (int i0 = tid; i0 < n; i0 += U * kKpThreads) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kKpThreads;
+                x[u] = i < n ? w[i] : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * kKpThreads;
+                if (i < n) own[i] = i < safe ? order_key(x[u]) : kKeyFirst;
+            }
+        }
+        __syncthreads();
+        const uint32_t *kk = own;
+        auto key = [=](int i) { return kk[i]; };
+        find_threshold<kKpThreads>(key, n, m, S, thr, ties);
+        write_selected<kKpThreads>(key, n, thr, ties, S, put);
+    } else {
+        auto key = [=](int i) {
+            return i < safe ? order_key(w[i]) : kKeyFirst;
+        };
+        find_threshold<kKpThreads>(key, n, m, S, thr, ties);
+        write_selected<kKpThreads>(key, n, thr, ties, S, put);
+    }
+}
+
+// launch_after with clusters of `cluster` CTAs along x.
+template <typename... K, typename... A>
+cudaError_t launch_clusters(void (*kern)(K...), dim3 grid, int threads,
+                            size_t smem, int cluster, cudaStream_t st,
+                            A... args) {
+    cudaError_t e = cudaFuncSetAttribute(
+        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return taken(e);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return taken(cudaLaunchKernelEx(&cfg, kern, K(args)...));
 }
 
 }  // namespace
@@ -287,14 +397,20 @@ __global__ void __launch_bounds__(kKpThreads)
 cudaError_t launch_cache_select(const CacheView &c, const void *q, int n_sel,
                                 int first, int last, int32_t *pages,
                                 float *scores, cudaStream_t st) {
-    const dim3 grid((c.max_pages + kScThreads - 1) / kScThreads, c.Hkv, c.B);
-    const size_t smem = (size_t)c.G * c.T * 2 * c.d;
-    uint32_t *keys = (uint32_t *)scores;
+    // as many CTAs as have pages and SMs
+    int cluster = 1;
+    while (cluster < 8 && cluster * kScThreads < c.max_pages &&
+           2L * cluster * c.B * c.Hkv <= 152)
+        cluster *= 2;
+    const int shared_keys = c.max_pages <= kScShared;
+    const size_t smem = (size_t)c.G * c.T * 2 * c.d +
+                        (shared_keys ? sizeof(uint32_t) * c.max_pages : 0);
     auto go = [&](auto t, auto dd) {
         using T = decltype(t);
-        return launch_after(k_cache_scores<T, decltype(dd)::value>, grid,
-                            kScThreads, smem, st, c, (const T *)q, first,
-                            last, keys);
+        return launch_clusters(k_cache_select<T, decltype(dd)::value>,
+                               dim3(cluster, c.Hkv, c.B), kScThreads, smem,
+                               cluster, st, c, (const T *)q, n_sel, first,
+                               last, pages, (uint32_t *)scores, shared_keys);
     };
     auto by_d = [&](auto t) {
         switch (c.d) {
@@ -303,18 +419,17 @@ cudaError_t launch_cache_select(const CacheView &c, const void *q, int n_sel,
             default: return go(t, std::integral_constant<int, 128>{});
         }
     };
-    const cudaError_t e =
-        c.dtype == ELSAA_FP32 ? by_d(0.0f) : by_d(__nv_bfloat16{});
-    if (e != cudaSuccess) return e;
-    return launch_after(k_cache_pages, dim3(c.Hkv, c.B), kSpThreads, 0, st, c,
-                        (const uint32_t *)keys, n_sel, pages);
+    return c.dtype == ELSAA_FP32 ? by_d(0.0f) : by_d(__nv_bfloat16{});
 }
 
 cudaError_t launch_cache_keep(const CacheView &c, const float *weight,
-                              int keep, int recent, int32_t *kept, int *count,
+                              int keep, int recent, const CacheKept &out,
                               cudaStream_t st) {
-    return launch_after(k_cache_keep, dim3(c.Hkv, c.B), kKpThreads, 0, st, c,
-                        weight, keep, recent, kept, count);
+    const long slots = (long)c.max_pages * c.ps;
+    const int shared_keys = slots <= kKpShared;
+    return launch_clusters(k_cache_keep, dim3(c.Hkv, c.B), kKpThreads,
+                           shared_keys ? sizeof(uint32_t) * slots : 0, 1, st,
+                           c, weight, keep, recent, out, shared_keys);
 }
 
 }  // namespace elsaa

@@ -1,11 +1,15 @@
 // Writes into the 8-bit cache: elsaa_cache_append (rows of new tokens) and
 // the second half of elsaa_cache_evict (the kept rows to other pages).
 //
-// A CTA owns one page of one head, keys or values, so the page's exponent is
-// one block reduction away and every byte moves once: the page's new rows are
-// read into registers (at most 32 KB a CTA), their largest magnitude gives
-// the exponent e, and codes e4m3(x 2^-e) go out. Scaling by a power of two is
-// exact, so the only rounding is the conversion's.
+// A page of one head, keys or values, belongs to ps d / 64 threads of a CTA,
+// each with 8 channels of 8 rows, so the page's exponent is one reduction
+// away and every byte moves once: rows are read into registers, their largest
+// magnitude gives the exponent e, and codes e4m3(x 2^-e) go out (16 channels a
+// thread, read in two loads, took 99 us instead of 81 for a prompt of 2 x 16
+// heads x 16384 rows of 128). Scaling by a power of two is exact, so the only
+// rounding is the conversion's. What bounds it is HBM, if enough pages are in
+// flight: small pages share a CTA, and every dependent read (length, table
+// entry, position) is issued for all four rows before one is used.
 #include "cache_common.cuh"
 
 namespace elsaa {
@@ -13,283 +17,471 @@ namespace elsaa {
 namespace {
 
 using namespace cache;
+using tc::pack_bf16x2;
+using tc::pack_f16x2;
+using tc::unpack_f16x2;
 
 constexpr int kWrThreads = 256;
 
-// Largest of all threads' x.
-__device__ __forceinline__ float block_max(float x, float *tmp) {
-    x = warp_max(x);
-    if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = x;
-    __syncthreads();
-    float m = tmp[0];
+// The threads of a page.
+template <int D>
+struct Page {
+    static constexpr int C = D / 8;  // threads of a row
+    static constexpr int ROWS = 8;   // rows of a thread
+    int size;                        // threads of the page
+    int t;                           // this one
+    int ch, row, step;               // channels from 8 ch, rows row + i step
+    int index;                       // which of the CTA's pages
+    __device__ __forceinline__ explicit Page(int ps) {
+        size = ps * D / 64;
+        t = threadIdx.x & (size - 1);
+        index = threadIdx.x / size;
+        ch = t % C;
+        row = t / C;
+        step = ps / ROWS;
+    }
+};
+
+// Extremes of 8 channels, in the type that the rows come in (rounding is
+// monotonous, so the extremes of the codes are the codes of the extremes).
+// NaN is left out.
+#define ELSAA_EXTREME_OPS(NAME, TYPE)                                       \
+    __device__ __forceinline__ uint32_t NAME##_max(uint32_t a, uint32_t b) { \
+        uint32_t r;                                                         \
+        asm("max." TYPE " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));        \
+        return r;                                                           \
+    }                                                                       \
+    __device__ __forceinline__ uint32_t NAME##_min(uint32_t a, uint32_t b) { \
+        uint32_t r;                                                         \
+        asm("min." TYPE " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));        \
+        return r;                                                           \
+    }
+ELSAA_EXTREME_OPS(bf16x2, "bf16x2")
+ELSAA_EXTREME_OPS(f16x2, "f16x2")
+#undef ELSAA_EXTREME_OPS
+
+struct Bf16Rows {  // bf16 pairs
+    static constexpr int P = 4;
+    static constexpr uint32_t kNoHigh = 0xff80ff80u, kNoLow = 0x7f807f80u;
+    static constexpr uint32_t kAbs = 0x7fff7fffu;
+    static __device__ uint32_t max2(uint32_t a, uint32_t b) {
+        return bf16x2_max(a, b);
+    }
+    static __device__ uint32_t min2(uint32_t a, uint32_t b) {
+        return bf16x2_min(a, b);
+    }
+    static __device__ float2 get(uint32_t w) {
+        return make_float2(__uint_as_float(w << 16),
+                           __uint_as_float(w & 0xffff0000u));
+    }
+};
+struct F16Rows {  // fp16 pairs
+    static constexpr int P = 4;
+    static constexpr uint32_t kNoHigh = 0xfc00fc00u, kNoLow = 0x7c007c00u;
+    static constexpr uint32_t kAbs = 0x7fff7fffu;
+    static __device__ uint32_t max2(uint32_t a, uint32_t b) {
+        return f16x2_max(a, b);
+    }
+    static __device__ uint32_t min2(uint32_t a, uint32_t b) {
+        return f16x2_min(a, b);
+    }
+    static __device__ float2 get(uint32_t w) {
+        float2 x;
+        unpack_f16x2(w, x.x, x.y);
+        return x;
+    }
+};
+struct F32Rows {
+    static constexpr int P = 8;
+    static constexpr uint32_t kNoHigh = 0xff800000u, kNoLow = 0x7f800000u;
+    static constexpr uint32_t kAbs = 0x7fffffffu;
+    static __device__ uint32_t max2(uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }
+    static __device__ uint32_t min2(uint32_t a, uint32_t b) {
+        return __float_as_uint(fminf(__uint_as_float(a), __uint_as_float(b)));
+    }
+    static __device__ float2 get(uint32_t w) {
+        return make_float2(__uint_as_float(w), __uint_as_float(w));
+    }
+};
+
+// Largest magnitude in the P words of a row (any sign), joined with `m`.
+template <typename R>
+__device__ __forceinline__ uint32_t abs_max(uint32_t m, const uint32_t *w) {
 #pragma unroll
-    for (int i = 1; i < kWrThreads / 32; ++i) m = fmaxf(m, tmp[i]);
+    for (int i = 0; i < R::P; ++i) m = R::max2(m, w[i] & R::kAbs);
     return m;
 }
 
-// Channel extremes of the codes: thread (row group, chunk of 8 channels)
-// holds hi[8], lo[8] of its rows; afterwards thread i < D has channel i's.
+// Largest x of the page's threads. All threads of the CTA.
 template <int D>
-__device__ __forceinline__ void channel_extremes(float *hi, float *lo,
-                                                 float (*sh)[2][D], float &h,
-                                                 float &l) {
-    constexpr int C = D / 8;
-    const int tid = threadIdx.x;
+__device__ __forceinline__ float page_max(const Page<D> &g, float x,
+                                          float *tmp) {
+    for (int o = 1; o < min(g.size, 32); o <<= 1)
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    if (g.size > 32) {
+        if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = x;
+        __syncthreads();
+        const int w0 = g.index * g.size / 32;
+        for (int w = 0; w < g.size / 32; ++w) x = fmaxf(x, tmp[w0 + w]);
+    }
+    return x;
+}
+
+// The page's channel extremes, in its first C threads. All threads of the
+// CTA; sh: [warps][C][2 P] words.
+template <typename R, int D>
+__device__ __forceinline__ void page_extremes(const Page<D> &g, uint32_t *hi,
+                                              uint32_t *lo, uint32_t *sh) {
+    constexpr int C = Page<D>::C, P = R::P;
+    for (int o = C; o < min(g.size, 32); o <<= 1) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-#pragma unroll
-        for (int o = C; o < 32; o <<= 1) {
-            hi[i] = fmaxf(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
-            lo[i] = fminf(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
+        for (int i = 0; i < P; ++i) {
+            hi[i] = R::max2(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
+            lo[i] = R::min2(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
         }
     }
-    if ((tid & 31) < C) {
+    if (g.size > 32) {
+        const int lane = threadIdx.x & 31;
+        if (lane < C) {
+            uint32_t *at = sh + ((threadIdx.x >> 5) * C + lane) * 2 * P;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sh[tid >> 5][0][(tid & 31) * 8 + i] = hi[i];
-            sh[tid >> 5][1][(tid & 31) * 8 + i] = lo[i];
+            for (int i = 0; i < P; ++i) {
+                at[i] = hi[i];
+                at[P + i] = lo[i];
+            }
         }
-    }
-    __syncthreads();
-    h = -INFINITY;
-    l = INFINITY;
-    if (tid < D) {
+        __syncthreads();
+        if (g.t < C) {
+            const int w0 = g.index * g.size / 32;
+            for (int w = 1; w < g.size / 32; ++w) {
+                const uint32_t *at = sh + ((w0 + w) * C + g.t) * 2 * P;
 #pragma unroll
-        for (int w = 0; w < kWrThreads / 32; ++w) {
-            h = fmaxf(h, sh[w][0][tid]);
-            l = fminf(l, sh[w][1][tid]);
+                for (int i = 0; i < P; ++i) {
+                    hi[i] = R::max2(hi[i], at[i]);
+                    lo[i] = R::min2(lo[i], at[P + i]);
+                }
+            }
         }
     }
 }
 
-// One byte of bounds: a whole number in [-112, 112] (448 / 4) wherever the
-// channel has a number; clipped for one that has none.
-__device__ __forceinline__ int8_t bound(float x) {
-    return (int8_t)fminf(fmaxf(x, -112.0f), 112.0f);
-}
-
-// 8 values times f as codes; extremes of what the codes stand for.
-__device__ __forceinline__ uint2 encode8(const float *x, float f, bool ext,
-                                         float *hi, float *lo) {
-    uint2 w;
-    w.x = e4m3x4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-    w.y = e4m3x4(x[4] * f, x[5] * f, x[6] * f, x[7] * f);
-    if (ext) {
-        float y[8];
-        from_e4m3x4(w.x, y);
-        from_e4m3x4(w.y, y + 4);
+// Bytes of bounds for 8 channels: the extremes' codes (of x f) over 4, rounded
+// outwards, joined with the page's older ones times `drop`. Whole numbers in
+// [-112, 112] (448 / 4), clipped for a channel without a number.
+template <typename R>
+__device__ __forceinline__ void write_bounds(int8_t *at, int d,
+                                             const uint32_t *hi,
+                                             const uint32_t *lo, float f,
+                                             bool had, float drop) {
+    uint32_t *const to[2] = {(uint32_t *)at, (uint32_t *)(at + d)};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {  // NaN is left out
-            hi[i] = fmaxf(hi[i], y[i]);
-            lo[i] = fminf(lo[i], y[i]);
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t old[2] = {had ? to[0][k] : 0u, had ? to[1][k] : 0u};
+        uint32_t out[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int ch = 4 * k + i;
+            const float2 h = R::get(hi[R::P == 8 ? ch : ch / 2]);
+            const float2 l = R::get(lo[R::P == 8 ? ch : ch / 2]);
+            const float2 x = from_e4m3x2(e4m3x2((i & 1 ? h.y : h.x) * f,
+                                                (i & 1 ? l.y : l.x) * f));
+            float u = ceilf(x.x * 0.25f), v = floorf(x.y * 0.25f);
+            if (had) {
+                u = fmaxf(u, ceilf((float)(int8_t)(old[0] >> 8 * i) * drop));
+                v = fminf(v, floorf((float)(int8_t)(old[1] >> 8 * i) * drop));
+            }
+            out[0] |= ((uint32_t)(int)u & 0xffu) << 8 * i;
+            out[1] |= ((uint32_t)(int)v & 0xffu) << 8 * i;
         }
+        to[0][k] = out[0];
+        to[1][k] = out[1];
     }
-    return w;
 }
 
+// 8 neighbouring elements as read, and times f as codes.
 template <typename T>
-struct Raw8 {
-    uint4 w[sizeof(T) * 8 / 16];
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    using Rows = Bf16Rows;
+    uint4 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) {
+        a = *(const uint4 *)p;
+    }
+    __device__ __forceinline__ const uint32_t *words() const { return &a.x; }
+    __device__ __forceinline__ uint2 codes(float f) const {
+        // a power of two times a bf16 number is a bf16 number (or far too
+        // small for a code)
+        const uint32_t ff = pack_bf16x2(f, f);
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t y;
+            asm("mul.rn.bf16x2 %0, %1, %2;"
+                : "=r"(y)
+                : "r"(words()[i]), "r"(ff));
+            const float2 x = Bf16Rows::get(y);
+            c[i] = e4m3x2(x.x, x.y);
+        }
+        return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    }
+};
+template <>
+struct Raw8<float> {
+    using Rows = F32Rows;
+    uint4 a[2];
+    __device__ __forceinline__ void load(const float *p) {
+        a[0] = ((const uint4 *)p)[0];
+        a[1] = ((const uint4 *)p)[1];
+    }
+    __device__ __forceinline__ const uint32_t *words() const {
+        return &a[0].x;
+    }
+    __device__ __forceinline__ uint2 codes(float f) const {
+        const float *x = (const float *)a;
+        return make_uint2(e4m3x4(x[0] * f, x[1] * f, x[2] * f, x[3] * f),
+                          e4m3x4(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
+    }
 };
 
+// blockIdx: (pages of the window, keys and values in turn; head; sequence)
 template <typename T, int D>
-__global__ void __launch_bounds__(kWrThreads)
-    k_cache_append(CacheView c, const T *__restrict__ kn,
-                   const T *__restrict__ vn) {
+__global__ void __launch_bounds__(kWrThreads, sizeof(T) == 2 ? 4 : 2)
+    k_cache_append(const __grid_constant__ CacheView c,
+                   const T *__restrict__ kn, const T *__restrict__ vn) {
     wait_for_stream();
-    constexpr int C = D / 8, R = kWrThreads / C, NP = kCacheTile / R;
+    using G = Page<D>;
+    using R = typename Raw8<T>::Rows;
     __shared__ float tmp[kWrThreads / 32];
-    __shared__ float sh[kWrThreads / 32][2][D];
-    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z >> 1;
-    const bool keys = (blockIdx.z & 1) == 0;
+    __shared__ uint32_t sh[kWrThreads / 32 * G::C * 2 * R::P];
+    const G g(c.ps);
+    const int h = blockIdx.y, b = blockIdx.z;
+    const int q = blockIdx.x * (kWrThreads / g.size) + g.index;
+    const bool keys = (q & 1) == 0;
     const int end = tokens(c, b), start = end - fresh(c, b);
-    const int p = max(start, 0) / c.ps + blockIdx.x, p0 = p * c.ps;
-    if (p0 >= end || start >= end) return;
-    // rows [r0, r1) of the page are new, [0, r0) older
-    const int r0 = max(max(start, 0) - p0, 0), r1 = min(c.ps, end - p0);
-    const int id = page_id(c, b, p);
-    if (id < 0) return;
-    const size_t ph = (size_t)id * c.Hkv + h;
-    uint8_t *codes = (keys ? c.k : c.v) + ph * c.ps * D;
+    const int p = max(start, 0) / c.ps + (q >> 1), p0 = p * c.ps;
+    // rows [r0, r1) of the page are new, [0, r0) older; they are read while
+    // the table entry is on its way
+    const int r0 = max(max(start, 0) - p0, 0);
+    const int r1 = p0 < end && start < end ? min(c.ps, end - p0) : 0;
+    const int entry = r1 > 0 ? c.table[(size_t)b * c.max_pages + p] : -1;
+    const T *x = (keys ? kn : vn) + ((size_t)b * c.Hkv + h) * c.T * D +
+                 g.ch * 8;
+    Raw8<T> raw[G::ROWS];
+#pragma unroll
+    for (int i = 0; i < G::ROWS; ++i) {
+        const int r = g.row + i * g.step;
+        if (r >= r0 && r < r1)
+            raw[i].load(x + (size_t)(p0 + r - start) * D);
+    }
+    const int id = r1 > 0 ? checked_page(c, entry, b, p) : -1;
+    const bool had = id >= 0 && r0 > 0;
+    const size_t ph = (size_t)max(id, 0) * c.Hkv + h;
+    uint8_t *codes = (keys ? c.k : c.v) + ph * c.ps * D + g.ch * 8;
     float *scale = (keys ? c.ks : c.vs) + ph;
-    const T *x = (keys ? kn : vn) + ((size_t)b * c.Hkv + h) * c.T * D;
-    const int ch = tid % C, rr = tid / C;
-
-    Raw8<T> raw[NP];
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * R + rr;
-        if (r >= r0 && r < r1) {
-            const uint4 *src =
-                (const uint4 *)(x + (size_t)(p0 + r - start) * D + ch * 8);
-#pragma unroll
-            for (int j = 0; j < (int)(sizeof(T) / 2); ++j) raw[i].w[j] = src[j];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * R + rr;
-        if (r >= r0 && r < r1) {
-            float y[8];
-            load8((const T *)&raw[i], y);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) amax = fmaxf(amax, magnitude(y[j]));
-        }
-    }
-    const bool had = r0 > 0;
     const int e_old =
         had ? min(max(scale_exponent(*scale), kCacheExpLow), kCacheExpHigh)
             : kCacheExpLow;
-    int e = page_exponent(block_max(amax, tmp));
-    if (had) e = max(e, e_old);
-    const float f = pow2(-e);
-    float hi[8], lo[8];
+    uint32_t hi[R::P], lo[R::P], top = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        hi[j] = -INFINITY;
-        lo[j] = INFINITY;
+    for (int j = 0; j < R::P; ++j) {
+        hi[j] = R::kNoHigh;
+        lo[j] = R::kNoLow;
     }
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * R + rr;
+    for (int i = 0; i < G::ROWS; ++i) {
+        const int r = g.row + i * g.step;
         if (r >= r0 && r < r1) {
-            float y[8];
-            load8((const T *)&raw[i], y);
-            *(uint2 *)(codes + (size_t)r * D + ch * 8) =
-                encode8(y, f, keys, hi, lo);
+            const uint32_t *w = raw[i].words();
+            if (keys) {
+#pragma unroll
+                for (int j = 0; j < R::P; ++j) {
+                    hi[j] = R::max2(hi[j], w[j]);
+                    lo[j] = R::min2(lo[j], w[j]);
+                }
+            } else {
+                top = abs_max<R>(top, w);
+            }
         }
+    }
+    if (keys) {
+        // a channel without a number holds infinities of the wrong sign
+#pragma unroll
+        for (int j = 0; j < R::P; ++j)
+            top = R::max2(top, R::max2(R::max2(hi[j], 0u),
+                                       R::min2(lo[j], 0u) & R::kAbs));
+    }
+    const float2 t2 = R::get(top);
+    int e = page_exponent(page_max(g, magnitude(fmaxf(t2.x, t2.y)), tmp));
+    if (had) e = max(e, e_old);
+    const float f = pow2(-e);
+#pragma unroll
+    for (int i = 0; i < G::ROWS; ++i) {
+        const int r = g.row + i * g.step;
+        if (r >= r0 && r < r1 && id >= 0)
+            *(uint2 *)(codes + (size_t)r * D) = raw[i].codes(f);
     }
     // older rows move to the larger exponent; 2^(e_old - e) may be far below
     // the smallest code, whose product is then 0
     const float drop = exp2f((float)(e_old - e));
     if (had && e != e_old) {
-        for (int r = rr; r < r0; r += R) {
-            uint2 *at = (uint2 *)(codes + (size_t)r * D + ch * 8);
-            const uint2 w = *at;
+        for (int r = g.row; r < r0; r += g.step) {
+            uint2 *at = (uint2 *)(codes + (size_t)r * D);
+            const uint2 old = *at;
             float y[8];
-            from_e4m3x4(w.x, y);
-            from_e4m3x4(w.y, y + 4);
-            *at = encode8(y, drop, false, nullptr, nullptr);
+            from_e4m3x4(old.x, y);
+            from_e4m3x4(old.y, y + 4);
+            *at = make_uint2(e4m3x4(y[0] * drop, y[1] * drop, y[2] * drop,
+                                    y[3] * drop),
+                             e4m3x4(y[4] * drop, y[5] * drop, y[6] * drop,
+                                    y[7] * drop));
         }
     }
-    if (keys) {
-        float u, l;
-        channel_extremes<D>(hi, lo, sh, u, l);
-        if (tid < D) {
-            int8_t *at = c.bounds + ph * 2 * D + tid;
-            u = ceilf(u * 0.25f);
-            l = floorf(l * 0.25f);
-            if (had) {
-                u = fmaxf(u, ceilf((float)at[0] * drop));
-                l = fminf(l, floorf((float)at[D] * drop));
-            }
-            at[0] = bound(u);
-            at[D] = bound(l);
-        }
-    }
-    // block_max's barrier lies between every thread's read of it and this
-    if (tid == 0) *scale = pow2(e);
+    page_extremes<R>(g, hi, lo, sh);
+    if (id < 0) return;
+    if (keys && g.t < G::C)
+        write_bounds<R>(c.bounds + ph * 2 * D + g.ch * 8, D, hi, lo, f, had,
+                        drop);
+    // every thread of the page has read the scale: page_extremes' barrier (or
+    // the warp's exchange) lies between
+    __syncwarp();
+    if (g.t == 0) *scale = pow2(e);
 }
 
-// Page j of sequence b's kept rows, one head, keys or values.
+__device__ __forceinline__ uint32_t h2_of_e4m3(uint32_t w) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+    return r;
+}
+// 2^k as an fp16 pair, 0 below 2^-24.
+__device__ __forceinline__ uint32_t pow2_h2(int k) {
+    const float x = k < -24 ? 0.0f : pow2(min(k, 15));
+    return pack_f16x2(x, x);
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// blockIdx: (pages of the kept rows, keys and values in turn; head; sequence)
 template <int D>
-__global__ void __launch_bounds__(kWrThreads)
-    k_cache_compact(CacheView c, const float *__restrict__ weight, int keep,
-                    const int32_t *__restrict__ kept,
+__global__ void __launch_bounds__(kWrThreads, 4)
+    k_cache_compact(const __grid_constant__ CacheView c, int keep,
+                    const int32_t *__restrict__ rows,
                     const int *__restrict__ count,
                     const int32_t *__restrict__ dst_table, int dst_pages,
-                    float *__restrict__ weight_out,
                     int32_t *__restrict__ lengths_out) {
     wait_for_stream();
-    constexpr int C = D / 8, R = kWrThreads / C, NP = kCacheTile / R;
+    using G = Page<D>;
+    using R = F16Rows;
     __shared__ float tmp[kWrThreads / 32];
-    __shared__ float sh[kWrThreads / 32][2][D];
-    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z >> 1;
-    const bool keys = (blockIdx.z & 1) == 0;
-    const int n = count[b], p = blockIdx.x, p0 = p * c.ps;
-    if (keys && p == 0 && h == 0 && tid == 0) lengths_out[b] = n;
-    if (p0 >= n) return;
-    const size_t bh = (size_t)b * c.Hkv + h;
-    const int rows = min(c.ps, n - p0);
-    const int32_t *from = kept + bh * keep + p0;
-    const size_t cap = (size_t)c.max_pages * c.ps;
-    if (!keys && tid < rows)
-        weight_out[bh * dst_pages * c.ps + p0 + tid] =
-            weight[bh * cap + from[tid]];
-    const int id =
-        checked_page(c, dst_table[(size_t)b * dst_pages + p], b, p);
-    if (id < 0) return;
-    const size_t ph = (size_t)id * c.Hkv + h;
+    __shared__ uint32_t sh[kWrThreads / 32 * G::C * 2 * R::P];
+    const G g(c.ps);
+    const int h = blockIdx.y, b = blockIdx.z;
+    const int q = blockIdx.x * (kWrThreads / g.size) + g.index;
+    const bool keys = (q & 1) == 0;
+    const int p = q >> 1, p0 = p * c.ps;
+    const int32_t *from = rows + ((size_t)b * c.Hkv + h) * keep + p0;
     const uint8_t *pool = keys ? c.k : c.v;
     const float *scales = keys ? c.ks : c.vs;
-    const int ch = tid % C, rr = tid / C;
-
-    uint2 raw[NP];
-    float sc[NP];
+    // where the rows are, then codes and scales, each read for all of them
+    // before one is used
+    int src[G::ROWS];
+    uint2 raw[G::ROWS];
+    int ex[G::ROWS];  // exponents
+#pragma unroll
+    for (int i = 0; i < G::ROWS; ++i) {
+        const int r = g.row + i * g.step;
+        src[i] = p0 + r < keep ? from[r] : -1;
+    }
+    const int n = count[b];
+    const int entry =
+        p < dst_pages ? dst_table[(size_t)b * dst_pages + p] : -1;
+    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) lengths_out[b] = n;
+    const int held = max(0, min(c.ps, n - p0));
+    const int shift = __ffs(c.ps) - 1;
+#pragma unroll
+    for (int i = 0; i < G::ROWS; ++i) {
+        raw[i] = make_uint2(0, 0);
+        ex[i] = 0;
+        if (g.row + i * g.step < held && src[i] >= 0) {
+            const size_t sp = (size_t)(src[i] >> shift) * c.Hkv + h;
+            const size_t at = (sp << shift) + (src[i] & (c.ps - 1));
+            raw[i] = *(const uint2 *)(pool + at * D + g.ch * 8);
+            ex[i] = __float_as_int(scales[sp]);
+        }
+    }
+    const int id = held > 0 ? checked_page(c, entry, b, p) : -1;
     float amax = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * R + rr;
-        raw[i] = make_uint2(0, 0);
-        sc[i] = 0.0f;
-        if (r < rows) {
-            const int j = from[r], src = page_id(c, b, j / c.ps);
-            if (src >= 0) {
-                const size_t sh_ = (size_t)src * c.Hkv + h;
-                raw[i] = *(const uint2 *)(pool +
-                                          (sh_ * c.ps + j % c.ps) * D + ch * 8);
-                sc[i] = scales[sh_];
+    for (int i = 0; i < G::ROWS; ++i) {
+        // the largest code of the row's 8 times its scale
+        const uint32_t w[4] = {h2_of_e4m3(raw[i].x), h2_of_e4m3(raw[i].x >> 16),
+                               h2_of_e4m3(raw[i].y),
+                               h2_of_e4m3(raw[i].y >> 16)};
+        const float2 x = R::get(abs_max<R>(0u, w));
+        const float sc = __int_as_float(ex[i]);
+        amax = fmaxf(amax, magnitude(fmaxf(x.x, x.y) * sc));
+        ex[i] = scale_exponent(sc);
+    }
+    const int e = page_exponent(page_max(g, amax, tmp));
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        hi[k] = R::kNoHigh;
+        lo[k] = R::kNoLow;
+    }
+    const size_t ph = (size_t)max(id, 0) * c.Hkv + h;
+    uint8_t *codes = (keys ? c.k : c.v) + ph * c.ps * D + g.ch * 8;
+#pragma unroll
+    for (int i = 0; i < G::ROWS; ++i) {
+        const int r = g.row + i * g.step;
+        if (r < held && id >= 0) {
+            // code 2^k in fp16, in two factors: exact wherever it does not
+            // end below half the smallest code (448 2^-9 2^17 is the other
+            // end)
+            const int k = ex[i] - e;
+            const uint32_t f1 = pow2_h2(k), f2 = pow2_h2(max(k - 15, 0));
+            uint32_t o[2] = {0, 0};
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const uint32_t w = (m < 2 ? raw[i].x : raw[i].y) >> 16 * (m & 1);
+                const uint32_t x = mul_h2(mul_h2(h2_of_e4m3(w), f1), f2);
+                if (keys) {
+                    hi[m] = R::max2(hi[m], x);
+                    lo[m] = R::min2(lo[m], x);
+                }
+                uint16_t z;
+                asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(z) : "r"(x));
+                o[m / 2] |= (uint32_t)z << 16 * (m & 1);
             }
+            *(uint2 *)(codes + (size_t)r * D) = make_uint2(o[0], o[1]);
         }
     }
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        float y[8];
-        from_e4m3x4(raw[i].x, y);
-        from_e4m3x4(raw[i].y, y + 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            amax = fmaxf(amax, magnitude(y[j] * sc[i]));
-    }
-    const int e = page_exponent(block_max(amax, tmp));
-    float hi[8], lo[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        hi[j] = -INFINITY;
-        lo[j] = INFINITY;
-    }
-    uint8_t *codes = (keys ? c.k : c.v) + ph * c.ps * D;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * R + rr;
-        if (r < rows) {
-            float y[8];
-            from_e4m3x4(raw[i].x, y);
-            from_e4m3x4(raw[i].y, y + 4);
-            // a code that is not 0 has sc 2^-e <= 2^17; the clip keeps 0 from
-            // meeting an infinity
-            *(uint2 *)(codes + (size_t)r * D + ch * 8) =
-                encode8(y, fminf(sc[i] * pow2(-e), 0x1p20f), keys, hi, lo);
-        }
-    }
-    if (keys) {
-        float u, l;
-        channel_extremes<D>(hi, lo, sh, u, l);
-        if (tid < D) {
-            int8_t *at = c.bounds + ph * 2 * D + tid;
-            at[0] = bound(ceilf(u * 0.25f));
-            at[D] = bound(floorf(l * 0.25f));
-        }
-    }
-    if (tid == 0) (keys ? c.ks : c.vs)[ph] = pow2(e);
+    page_extremes<R>(g, hi, lo, sh);
+    if (id < 0) return;
+    if (keys && g.t < G::C)
+        write_bounds<R>(c.bounds + ph * 2 * D + g.ch * 8, D, hi, lo, 1.0f,
+                        false, 1.0f);
+    if (g.t == 0) (keys ? c.ks : c.vs)[ph] = pow2(e);
+}
+
+// CTAs for `pages` pages of keys and of values.
+unsigned page_ctas(const CacheView &c, long pages) {
+    const int per = kWrThreads / (c.ps * c.d / 64);
+    return (unsigned)((2 * pages + per - 1) / per);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_append(const CacheView &c, const void *k,
                                 const void *v, cudaStream_t st) {
-    const dim3 grid((c.T + c.ps - 2) / c.ps + 1, c.Hkv, 2 * c.B);
+    // T rows touch at most this many pages
+    const dim3 grid(page_ctas(c, ((long)c.T + c.ps - 2) / c.ps + 1), c.Hkv,
+                    c.B);
     auto go = [&](auto t, auto dd) {
         using T = decltype(t);
         return launch_after(k_cache_append<T, decltype(dd)::value>, grid,
@@ -305,16 +497,15 @@ cudaError_t launch_cache_append(const CacheView &c, const void *k,
     return c.dtype == ELSAA_FP32 ? by_d(0.0f) : by_d(__nv_bfloat16{});
 }
 
-cudaError_t launch_cache_compact(const CacheView &c, const float *weight,
-                                 int keep, const int32_t *kept,
-                                 const int *count, const int32_t *dst_table,
-                                 int dst_pages, float *weight_out,
+cudaError_t launch_cache_compact(const CacheView &c, int keep,
+                                 const int32_t *rows, const int *count,
+                                 const int32_t *dst_table, int dst_pages,
                                  int32_t *lengths_out, cudaStream_t st) {
-    const dim3 grid((keep + c.ps - 1) / c.ps, c.Hkv, 2 * c.B);
+    const dim3 grid(page_ctas(c, ((long)keep + c.ps - 1) / c.ps), c.Hkv, c.B);
     auto go = [&](auto dd) {
         return launch_after(k_cache_compact<decltype(dd)::value>, grid,
-                            kWrThreads, 0, st, c, weight, keep, kept, count,
-                            dst_table, dst_pages, weight_out, lengths_out);
+                            kWrThreads, 0, st, c, keep, rows, count,
+                            dst_table, dst_pages, lengths_out);
     };
     switch (c.d) {
         case 32: return go(std::integral_constant<int, 32>{});
