@@ -137,7 +137,8 @@ int elsaa_cache_select(const elsaa_cache *cache, int T, const void *q,
  * pages     [B, H_kv, n_sel] as elsaa_cache_select writes them (distinct;
  *           entries outside the sequence's pages count as none), or NULL for
  *           all (n_sel is then ignored).
- * weight_in, weight_out  [B, H_kv, max_pages * page_size] fp32, or both NULL:
+ * weight_in, weight_out  [B, H_kv, max_pages * page_size] fp32, 16-byte
+ *           aligned, or both NULL:
  *           weight_out_j = weight_in_j + sum of exp(s_j - lse) over the K/V
  *           head's queries, for j < lengths[b]; entries behind keep what they
  *           held. weight_in may be weight_out, or NULL for zeros.

@@ -249,6 +249,10 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
     if (misaligned(q, 16) || misaligned(o, 16))
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "q and o must be 16-byte aligned");
+    if (misaligned(weight_in, 16) || misaligned(weight_out, 16))
+        return set_last_error(ELSAA_ERR_INVALID_ARG,
+                              "weight_in and weight_out must be 16-byte "
+                              "aligned");
     if (weight_in && !weight_out)
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "weight_in needs weight_out");

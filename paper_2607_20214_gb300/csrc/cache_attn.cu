@@ -294,35 +294,36 @@ __global__ void __launch_bounds__(kMgThreads)
 //
 // weight_out_j = weight_in_j + sum over the columns of 2^(s_j - lse), from
 // the scores that the attention kernel left: 4 bytes a token and column,
-// where a second walk over the keys would read d bytes.
+// where a second walk over the keys would read d bytes. Four neighbouring
+// tokens a thread (they share a page), a column's in one load.
 constexpr int kWtThreads = 128;
+constexpr int kWtTokens = 4 * kWtThreads;
 
 __global__ void __launch_bounds__(kWtThreads)
     k_cache_weights(const __grid_constant__ CacheAttn A) {
     wait_for_stream();
-    __shared__ int slot[kWtThreads / 16];
+    __shared__ int slot[kWtTokens / 16];
     __shared__ float lse[128];
     const CacheView &c = A.c;
     const int h = blockIdx.y, b = blockIdx.z, GT = c.G * c.T;
+    const int tid = threadIdx.x;
     const size_t bh = (size_t)b * c.Hkv + h;
-    const int len = tokens(c, b), j0 = blockIdx.x * kWtThreads;
-    const int j = j0 + threadIdx.x;
+    const int len = tokens(c, b), j0 = blockIdx.x * kWtTokens;
+    const int j = j0 + 4 * tid;
     if (j0 >= len) return;
     const int n = fresh(c, b);
     const bool any = n > 0;
     // a column that is no query adds nothing: 2^(s - inf)
-    if (any && threadIdx.x < GT)
-        lse[threadIdx.x] = (int)threadIdx.x % c.T < n
-                               ? A.lse2[bh * GT + threadIdx.x]
-                               : INFINITY;
+    if (any && tid < GT)
+        lse[tid] = tid % c.T < n ? A.lse2[bh * GT + tid] : INFINITY;
     long at = j;
     if (A.pages) {
         // the list entries of this block's pages
-        if (threadIdx.x < kWtThreads / 16) slot[threadIdx.x] = -1;
+        if (tid < kWtTokens / 16) slot[tid] = -1;
         __syncthreads();
-        const int p0 = j0 / c.ps, np = kWtThreads / c.ps;
+        const int p0 = j0 / c.ps, np = kWtTokens / c.ps;
         const int listed = min(A.n_sel, (len + c.ps - 1) / c.ps);
-        for (int e = threadIdx.x; e < listed; e += kWtThreads) {
+        for (int e = tid; e < listed; e += kWtThreads) {
             const int p = A.pages[bh * A.n_sel + e] - p0;
             if (p >= 0 && p < np) slot[p] = e;
         }
@@ -332,16 +333,35 @@ __global__ void __launch_bounds__(kWtThreads)
     }
     __syncthreads();
     if (j >= len) return;
+    // a row of weights is a whole number of pages long, so whole fours can be
+    // read; only tokens that are held are written
     const size_t w = bh * c.max_pages * c.ps + j;
-    float x = 0.0f;
+    const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float4 was = A.weight_in ? *(const float4 *)(A.weight_in + w) : z;
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (any && at >= 0) {
         const float *s = A.scores + bh * GT * A.slots + at;
+#pragma unroll 4
         for (int col = 0; col < GT; ++col) {
-            const float v = s[(size_t)col * A.slots];
-            if (v != -INFINITY) x += exp2f(v - lse[col]);
+            const float4 v = *(const float4 *)(s + (size_t)col * A.slots);
+            const float l = lse[col];
+            // a masked score beside an empty row's -inf is not a number
+            const float y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (y[i] != -INFINITY) x[i] += tc::ex2_approx(y[i] - l);
         }
     }
-    A.weight_out[w] = (A.weight_in ? A.weight_in[w] : 0.0f) + x;
+    float *out = A.weight_out + w;
+    const float4 sum =
+        make_float4(was.x + x[0], was.y + x[1], was.z + x[2], was.w + x[3]);
+    if (j + 3 < len) {
+        *(float4 *)out = sum;
+    } else {
+        out[0] = sum.x;
+        if (j + 1 < len) out[1] = sum.y;
+        if (j + 2 < len) out[2] = sum.z;
+    }
 }
 
 template <typename T, int D, int NG>
@@ -384,7 +404,7 @@ cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st) {
 cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st) {
     const long cap = (long)A.c.max_pages * A.c.ps;
     return launch_after(k_cache_weights,
-                        dim3((unsigned)((cap + kWtThreads - 1) / kWtThreads),
+                        dim3((unsigned)((cap + kWtTokens - 1) / kWtTokens),
                              A.c.Hkv, A.c.B),
                         kWtThreads, 0, st, A);
 }

@@ -2,7 +2,7 @@
 // the second half of elsaa_cache_evict (the kept rows to other pages).
 //
 // A page of one head, keys or values, belongs to ps d / 64 threads of a CTA,
-// each with 8 channels of 8 rows, so the page's exponent is one reduction
+// each with E channels of 64 / E rows, so the page's exponent is one reduction
 // away and every byte moves once: rows are read into registers, their largest
 // magnitude gives the exponent e, and codes e4m3(x 2^-e) go out (16 channels a
 // thread, read in two loads, took 99 us instead of 81 for a prompt of 2 x 16
@@ -23,15 +23,15 @@ using tc::unpack_f16x2;
 
 constexpr int kWrThreads = 256;
 
-// The threads of a page.
-template <int D>
+// The threads of a page: E channels each, in 64 / E rows.
+template <int D, int E>
 struct Page {
-    static constexpr int C = D / 8;  // threads of a row
-    static constexpr int ROWS = 8;   // rows of a thread
-    int size;                        // threads of the page
-    int t;                           // this one
-    int ch, row, step;               // channels from 8 ch, rows row + i step
-    int index;                       // which of the CTA's pages
+    static constexpr int C = D / E;      // threads of a row
+    static constexpr int ROWS = 64 / E;  // rows of a thread
+    int size;                            // threads of the page
+    int t;                               // this one
+    int ch, row, step;                   // channels from E ch, rows row + i step
+    int index;                           // which of the CTA's pages
     __device__ __forceinline__ explicit Page(int ps) {
         size = ps * D / 64;
         t = threadIdx.x & (size - 1);
@@ -42,7 +42,7 @@ struct Page {
     }
 };
 
-// Extremes of 8 channels, in the type that the rows come in (rounding is
+// Extremes of neighbouring channels, in the type that the rows come in (rounding is
 // monotonous, so the extremes of the codes are the codes of the extremes).
 // NaN is left out.
 #define ELSAA_EXTREME_OPS(NAME, TYPE)                                       \
@@ -60,8 +60,8 @@ ELSAA_EXTREME_OPS(bf16x2, "bf16x2")
 ELSAA_EXTREME_OPS(f16x2, "f16x2")
 #undef ELSAA_EXTREME_OPS
 
-struct Bf16Rows {  // bf16 pairs
-    static constexpr int P = 4;
+struct Bf16Rows {  // 8 channels, bf16 pairs
+    static constexpr int P = 4, PER = 2;  // words, channels a word
     static constexpr uint32_t kNoHigh = 0xff80ff80u, kNoLow = 0x7f807f80u;
     static constexpr uint32_t kAbs = 0x7fff7fffu;
     static __device__ uint32_t max2(uint32_t a, uint32_t b) {
@@ -75,8 +75,8 @@ struct Bf16Rows {  // bf16 pairs
                            __uint_as_float(w & 0xffff0000u));
     }
 };
-struct F16Rows {  // fp16 pairs
-    static constexpr int P = 4;
+struct F16Rows {  // 16 channels, fp16 pairs
+    static constexpr int P = 8, PER = 2;
     static constexpr uint32_t kNoHigh = 0xfc00fc00u, kNoLow = 0x7c007c00u;
     static constexpr uint32_t kAbs = 0x7fff7fffu;
     static __device__ uint32_t max2(uint32_t a, uint32_t b) {
@@ -91,8 +91,8 @@ struct F16Rows {  // fp16 pairs
         return x;
     }
 };
-struct F32Rows {
-    static constexpr int P = 8;
+struct F32Rows {  // 8 channels
+    static constexpr int P = 8, PER = 1;
     static constexpr uint32_t kNoHigh = 0xff800000u, kNoLow = 0x7f800000u;
     static constexpr uint32_t kAbs = 0x7fffffffu;
     static __device__ uint32_t max2(uint32_t a, uint32_t b) {
@@ -115,8 +115,8 @@ __device__ __forceinline__ uint32_t abs_max(uint32_t m, const uint32_t *w) {
 }
 
 // Largest x of the page's threads. All threads of the CTA.
-template <int D>
-__device__ __forceinline__ float page_max(const Page<D> &g, float x,
+template <int D, int E>
+__device__ __forceinline__ float page_max(const Page<D, E> &g, float x,
                                           float *tmp) {
     for (int o = 1; o < min(g.size, 32); o <<= 1)
         x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
@@ -131,10 +131,11 @@ __device__ __forceinline__ float page_max(const Page<D> &g, float x,
 
 // The page's channel extremes, in its first C threads. All threads of the
 // CTA; sh: [warps][C][2 P] words.
-template <typename R, int D>
-__device__ __forceinline__ void page_extremes(const Page<D> &g, uint32_t *hi,
-                                              uint32_t *lo, uint32_t *sh) {
-    constexpr int C = Page<D>::C, P = R::P;
+template <typename R, int D, int E>
+__device__ __forceinline__ void page_extremes(const Page<D, E> &g,
+                                              uint32_t *hi, uint32_t *lo,
+                                              uint32_t *sh) {
+    constexpr int C = Page<D, E>::C, P = R::P;
     for (int o = C; o < min(g.size, 32); o <<= 1) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -167,7 +168,7 @@ __device__ __forceinline__ void page_extremes(const Page<D> &g, uint32_t *hi,
     }
 }
 
-// Bytes of bounds for 8 channels: the extremes' codes (of x f) over 4, rounded
+// Bytes of bounds for the channels: the extremes' codes (of x f) over 4, rounded
 // outwards, joined with the page's older ones times `drop`. Whole numbers in
 // [-112, 112] (448 / 4), clipped for a channel without a number.
 template <typename R>
@@ -177,14 +178,14 @@ __device__ __forceinline__ void write_bounds(int8_t *at, int d,
                                              bool had, float drop) {
     uint32_t *const to[2] = {(uint32_t *)at, (uint32_t *)(at + d)};
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < R::P * R::PER / 4; ++k) {
         const uint32_t old[2] = {had ? to[0][k] : 0u, had ? to[1][k] : 0u};
         uint32_t out[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int ch = 4 * k + i;
-            const float2 h = R::get(hi[R::P == 8 ? ch : ch / 2]);
-            const float2 l = R::get(lo[R::P == 8 ? ch : ch / 2]);
+            const float2 h = R::get(hi[ch / R::PER]);
+            const float2 l = R::get(lo[ch / R::PER]);
             const float2 x = from_e4m3x2(e4m3x2((i & 1 ? h.y : h.x) * f,
                                                 (i & 1 ? l.y : l.x) * f));
             float u = ceilf(x.x * 0.25f), v = floorf(x.y * 0.25f);
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(kWrThreads, sizeof(T) == 2 ? 4 : 2)
     k_cache_append(const __grid_constant__ CacheView c,
                    const T *__restrict__ kn, const T *__restrict__ vn) {
     wait_for_stream();
-    using G = Page<D>;
+    using G = Page<D, 8>;
     using R = typename Raw8<T>::Rows;
     __shared__ float tmp[kWrThreads / 32];
     __shared__ uint32_t sh[kWrThreads / 32 * G::C * 2 * R::P];
@@ -366,6 +367,10 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
     return r;
 }
 
+__device__ __forceinline__ uint32_t word(const uint4 &w, int m) {
+    return m == 0 ? w.x : m == 1 ? w.y : m == 2 ? w.z : w.w;
+}
+
 // blockIdx: (pages of the kept rows, keys and values in turn; head; sequence)
 template <int D>
 __global__ void __launch_bounds__(kWrThreads, 4)
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(kWrThreads, 4)
                     const int32_t *__restrict__ dst_table, int dst_pages,
                     int32_t *__restrict__ lengths_out) {
     wait_for_stream();
-    using G = Page<D>;
+    using G = Page<D, 16>;
     using R = F16Rows;
     __shared__ float tmp[kWrThreads / 32];
     __shared__ uint32_t sh[kWrThreads / 32 * G::C * 2 * R::P];
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(kWrThreads, 4)
     // where the rows are, then codes and scales, each read for all of them
     // before one is used
     int src[G::ROWS];
-    uint2 raw[G::ROWS];
+    uint4 raw[G::ROWS];
     int ex[G::ROWS];  // exponents
 #pragma unroll
     for (int i = 0; i < G::ROWS; ++i) {
@@ -405,12 +410,12 @@ __global__ void __launch_bounds__(kWrThreads, 4)
     const int shift = __ffs(c.ps) - 1;
 #pragma unroll
     for (int i = 0; i < G::ROWS; ++i) {
-        raw[i] = make_uint2(0, 0);
+        raw[i] = make_uint4(0, 0, 0, 0);
         ex[i] = 0;
         if (g.row + i * g.step < held && src[i] >= 0) {
             const size_t sp = (size_t)(src[i] >> shift) * c.Hkv + h;
             const size_t at = (sp << shift) + (src[i] & (c.ps - 1));
-            raw[i] = *(const uint2 *)(pool + at * D + g.ch * 8);
+            raw[i] = *(const uint4 *)(pool + at * D + g.ch * 16);
             ex[i] = __float_as_int(scales[sp]);
         }
     }
@@ -418,53 +423,65 @@ __global__ void __launch_bounds__(kWrThreads, 4)
     float amax = 0.0f;
 #pragma unroll
     for (int i = 0; i < G::ROWS; ++i) {
-        // the largest code of the row's 8 times its scale
-        const uint32_t w[4] = {h2_of_e4m3(raw[i].x), h2_of_e4m3(raw[i].x >> 16),
-                               h2_of_e4m3(raw[i].y),
-                               h2_of_e4m3(raw[i].y >> 16)};
-        const float2 x = R::get(abs_max<R>(0u, w));
+        // the largest code of the row's 16 times its scale
+        uint32_t top = 0;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const uint32_t w = word(raw[i], m);
+            top = R::max2(top, h2_of_e4m3(w) & R::kAbs);
+            top = R::max2(top, h2_of_e4m3(w >> 16) & R::kAbs);
+        }
+        const float2 x = R::get(top);
         const float sc = __int_as_float(ex[i]);
         amax = fmaxf(amax, magnitude(fmaxf(x.x, x.y) * sc));
         ex[i] = scale_exponent(sc);
     }
     const int e = page_exponent(page_max(g, amax, tmp));
-    uint32_t hi[4], lo[4];
+    uint32_t hi[R::P], lo[R::P];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < R::P; ++k) {
         hi[k] = R::kNoHigh;
         lo[k] = R::kNoLow;
     }
     const size_t ph = (size_t)max(id, 0) * c.Hkv + h;
-    uint8_t *codes = (keys ? c.k : c.v) + ph * c.ps * D + g.ch * 8;
+    uint8_t *codes = (keys ? c.k : c.v) + ph * c.ps * D + g.ch * 16;
 #pragma unroll
     for (int i = 0; i < G::ROWS; ++i) {
         const int r = g.row + i * g.step;
         if (r < held && id >= 0) {
-            // code 2^k in fp16, in two factors: exact wherever it does not
-            // end below half the smallest code (448 2^-9 2^17 is the other
-            // end)
+            // code 2^k in fp16: exact wherever it does not end below half
+            // the smallest code
             const int k = ex[i] - e;
-            const uint32_t f1 = pow2_h2(k), f2 = pow2_h2(max(k - 15, 0));
-            uint32_t o[2] = {0, 0};
+            const uint32_t f = pow2_h2(k);
+            uint32_t o[4];
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
-                const uint32_t w = (m < 2 ? raw[i].x : raw[i].y) >> 16 * (m & 1);
-                const uint32_t x = mul_h2(mul_h2(h2_of_e4m3(w), f1), f2);
-                if (keys) {
-                    hi[m] = R::max2(hi[m], x);
-                    lo[m] = R::min2(lo[m], x);
+                uint32_t x[2] = {h2_of_e4m3(word(raw[i], m)),
+                                 h2_of_e4m3(word(raw[i], m) >> 16)};
+                uint16_t z[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    x[y] = mul_h2(x[y], f);
+                    // beyond 2^15 (448 is 2^-9 2^17 at most) a second factor
+                    if (k > 15) x[y] = mul_h2(x[y], pow2_h2(k - 15));
+                    if (keys) {
+                        hi[2 * m + y] = R::max2(hi[2 * m + y], x[y]);
+                        lo[2 * m + y] = R::min2(lo[2 * m + y], x[y]);
+                    }
+                    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;"
+                        : "=h"(z[y])
+                        : "r"(x[y]));
                 }
-                uint16_t z;
-                asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(z) : "r"(x));
-                o[m / 2] |= (uint32_t)z << 16 * (m & 1);
+                o[m] = (uint32_t)z[0] | (uint32_t)z[1] << 16;
             }
-            *(uint2 *)(codes + (size_t)r * D) = make_uint2(o[0], o[1]);
+            *(uint4 *)(codes + (size_t)r * D) =
+                make_uint4(o[0], o[1], o[2], o[3]);
         }
     }
     page_extremes<R>(g, hi, lo, sh);
     if (id < 0) return;
     if (keys && g.t < G::C)
-        write_bounds<R>(c.bounds + ph * 2 * D + g.ch * 8, D, hi, lo, 1.0f,
+        write_bounds<R>(c.bounds + ph * 2 * D + g.ch * 16, D, hi, lo, 1.0f,
                         false, 1.0f);
     if (g.t == 0) (keys ? c.ks : c.vs)[ph] = pow2(e);
 }

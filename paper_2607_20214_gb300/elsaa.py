@@ -714,6 +714,8 @@ def make_cache(k, v, k_scale, v_scale, bounds, page_table, lengths, H=None,
     c.device = dev
     c.torch_dtype = f32 if dt == ELSAA_FP32 else torch.bfloat16
     c.ref = ctypes.byref(c)
+    c.index = k.get_device()
+    c.slots = B * hkv * width * ps
     return c
 
 
@@ -752,25 +754,43 @@ def new_cache_workspace(cache: elsaa_cache, T=1, weights=False,
     return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.device)
 
 
+def _cptr(t, name, dtype, numel, cache):
+    """_ptr for the cache's device; the checks that pass cost least (a step
+    of decoding makes a dozen of them)."""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and \
+            t.get_device() == cache.index and t.numel() == numel and \
+            t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t, name, dtype, numel, cache.device)
+
+
 def _rows(t, name, cache, heads):
     """(pointer, T) of [B, heads, T, d_h] rows."""
     s = t.shape
     if len(s) != 4 or (s[0], s[1], s[3]) != (cache.B, heads, cache.d_h):
         raise ValueError("%s must be [%d, %d, T, %d] (got %s)" % (
             name, cache.B, heads, cache.d_h, tuple(s)))
-    return _ptr(t, name, cache.torch_dtype, None, cache.device), s[2]
+    return _cptr(t, name, cache.torch_dtype, t.numel(), cache), s[2]
+
+
+def _scratch(workspace, cache):
+    """(pointer, bytes) of a workspace."""
+    if workspace.get_device() != cache.index or \
+            not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on %s" % cache.device)
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def elsaa_cache_append(cache: elsaa_cache, k, v, new_len=None, stream=None):
     """Enqueue elsaa_cache_append: rows k, v [B, H_kv, T, d_h] become the
     newest tokens (lengths count them already)."""
-    dev = cache.device
     kp, T = _rows(k, "k", cache, cache.H_kv)
-    vp = _ptr(v, "v", cache.torch_dtype, k.numel(), dev)
     _check(load_library().elsaa_cache_append(
-        cache.ref, T, kp, vp,
-        _ptr(new_len, "new_len", torch.int32, cache.B, dev),
-        _stream_of(stream, dev)))
+        cache.ref, T, kp, _cptr(v, "v", cache.torch_dtype, k.numel(), cache),
+        _cptr(new_len, "new_len", torch.int32, cache.B, cache),
+        _stream_of(stream, cache.device)))
 
 
 def elsaa_cache_select(cache: elsaa_cache, q, n_sel, first=1, last=1,
@@ -778,20 +798,18 @@ def elsaa_cache_select(cache: elsaa_cache, q, n_sel, first=1, last=1,
                        stream=None):
     """Enqueue elsaa_cache_select for queries q [B, H, T, d_h]; returns pages
     [B, H_kv, n_sel] int32 (allocated here when not given)."""
-    dev = cache.device
     qp, T = _rows(q, "q", cache, cache.H)
     if pages is None:
         pages = torch.empty((cache.B, cache.H_kv, n_sel), dtype=torch.int32,
-                            device=dev)
+                            device=cache.device)
     if workspace is None:
         workspace = new_cache_workspace(cache, T)
+    ws, nbytes = _scratch(workspace, cache)
     _check(load_library().elsaa_cache_select(
-        cache.ref, T, qp,
-        _ptr(new_len, "new_len", torch.int32, cache.B, dev), n_sel, first,
-        last, _ptr(pages, "pages", torch.int32,
-                   cache.B * cache.H_kv * n_sel, dev),
-        _ptr(workspace, "workspace", None, None, dev),
-        workspace.nbytes, _stream_of(stream, dev)))
+        cache.ref, T, qp, _cptr(new_len, "new_len", torch.int32, cache.B,
+                                cache), n_sel, first, last,
+        _cptr(pages, "pages", torch.int32, cache.B * cache.H_kv * n_sel,
+              cache), ws, nbytes, _stream_of(stream, cache.device)))
     return pages
 
 
@@ -801,27 +819,22 @@ def elsaa_cache_attention(cache: elsaa_cache, q, pages=None, new_len=None,
     """Enqueue elsaa_cache_attention for queries q [B, H, T, d_h]; returns o
     (allocated here when not given, rows behind new_len then undefined).
     pages: as elsaa_cache_select returns them, or None for all."""
-    dev = cache.device
     qp, T = _rows(q, "q", cache, cache.H)
     if o is None:
         o = torch.empty_like(q)
     if workspace is None:
         workspace = new_cache_workspace(cache, T, weight_out is not None)
-    f32 = torch.float32
-    slots = cache.B * cache.H_kv * cache.max_pages * cache.page_size
-    n_sel = 0
-    if pages is not None:
-        n_sel = pages.shape[-1]
+    f32, i32, B = torch.float32, torch.int32, cache.B
+    n_sel = 0 if pages is None else pages.shape[-1]
+    ws, nbytes = _scratch(workspace, cache)
     _check(load_library().elsaa_cache_attention(
-        cache.ref, T, qp,
-        _ptr(new_len, "new_len", torch.int32, cache.B, dev),
-        _ptr(pages, "pages", torch.int32, cache.B * cache.H_kv * n_sel, dev),
-        n_sel, _ptr(weight_in, "weight_in", f32, slots, dev),
-        _ptr(weight_out, "weight_out", f32, slots, dev),
-        _ptr(o, "o", cache.torch_dtype, q.numel(), dev),
-        _ptr(lse, "lse", f32, cache.B * cache.H * T, dev),
-        _ptr(workspace, "workspace", None, None, dev),
-        workspace.nbytes, _stream_of(stream, dev)))
+        cache.ref, T, qp, _cptr(new_len, "new_len", i32, B, cache),
+        _cptr(pages, "pages", i32, B * cache.H_kv * n_sel, cache), n_sel,
+        _cptr(weight_in, "weight_in", f32, cache.slots, cache),
+        _cptr(weight_out, "weight_out", f32, cache.slots, cache),
+        _cptr(o, "o", cache.torch_dtype, q.numel(), cache),
+        _cptr(lse, "lse", f32, B * cache.H * T, cache), ws, nbytes,
+        _stream_of(stream, cache.device)))
     return o
 
 
@@ -831,22 +844,21 @@ def elsaa_cache_evict(cache: elsaa_cache, weight, keep, recent, dst_table,
     """Enqueue elsaa_cache_evict; returns (weight_out, lengths_out), allocated
     here when not given. The kept tokens are in the pages of dst_table
     [B, dst_pages] afterwards."""
-    dev, i32, f32 = cache.device, torch.int32, torch.float32
-    width, ps, bh = dst_table.shape[-1], cache.page_size, cache.B * cache.H_kv
+    i32, f32, B = torch.int32, torch.float32, cache.B
+    width, ps, bh = dst_table.shape[-1], cache.page_size, B * cache.H_kv
     if weight_out is None:
-        weight_out = torch.zeros((cache.B, cache.H_kv, width * ps),
-                                 device=dev)
+        weight_out = torch.zeros((B, cache.H_kv, width * ps),
+                                 device=cache.device)
     if lengths_out is None:
-        lengths_out = torch.empty((cache.B,), dtype=i32, device=dev)
+        lengths_out = torch.empty((B,), dtype=i32, device=cache.device)
     if workspace is None:
         workspace = new_cache_workspace(cache, 1, False, keep)
+    ws, nbytes = _scratch(workspace, cache)
     _check(load_library().elsaa_cache_evict(
-        cache.ref,
-        _ptr(weight, "weight", f32, bh * cache.max_pages * ps, dev), keep,
-        recent, _ptr(dst_table, "dst_table", i32, cache.B * width, dev),
-        width, _ptr(weight_out, "weight_out", f32, bh * width * ps, dev),
-        _ptr(lengths_out, "lengths_out", i32, cache.B, dev),
-        _ptr(kept, "kept", i32, bh * keep, dev),
-        _ptr(workspace, "workspace", None, None, dev),
-        workspace.nbytes, _stream_of(stream, dev)))
+        cache.ref, _cptr(weight, "weight", f32, cache.slots, cache), keep,
+        recent, _cptr(dst_table, "dst_table", i32, B * width, cache), width,
+        _cptr(weight_out, "weight_out", f32, bh * width * ps, cache),
+        _cptr(lengths_out, "lengths_out", i32, B, cache),
+        _cptr(kept, "kept", i32, bh * keep, cache), ws, nbytes,
+        _stream_of(stream, cache.device)))
     return weight_out, lengths_out

@@ -118,6 +118,8 @@ def test_bad_caches_are_refused_everywhere(lib, over, code, text):
     ("attention", dict(o=None), INV, "non-NULL"),
     ("attention", dict(q=P + 4), INV, "aligned"),
     ("attention", dict(win=P), INV, "weight_out"),
+    ("attention", dict(wout=P + 4), INV, "aligned"),
+    ("attention", dict(win=P + 8, wout=P), INV, "aligned"),
     ("attention", dict(n_sel=0), INV, "n_sel"),
     ("attention", dict(n_sel=1 << 28), INV, "n_sel"),
     ("attention", dict(bytes=0), WS, "small"),
