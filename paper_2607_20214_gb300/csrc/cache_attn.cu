@@ -33,7 +33,9 @@ __global__ void __launch_bounds__(kSaThreads)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int sub = lane % LPR, rg = lane / LPR;
     __shared__ Seq near[kNearSeqs];
-    Walk walk(divide<kSaThreads>(A, near), near);
+    Seq own;
+    const Start first = divide<kSaThreads>(A, near, own);
+    Walk walk(first, near, own);
     const float sl2 = c.scale * kLog2eF;
     const int GT = c.G * c.T;
 

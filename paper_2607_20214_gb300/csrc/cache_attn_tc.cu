@@ -263,7 +263,8 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     tc_fence_after();
     const uint32_t tm = tbase;
     wait_for_stream();
-    const Start first = divide<kTaThreads>(A, near);
+    Seq own;
+    const Start first = divide<kTaThreads>(A, near, own);
     const int count = first.count;
 
     if (warp >= 4) {
@@ -306,7 +307,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 }
                 return g;
             };
-            Walk walk(first, near);
+            Walk walk(first, near, own);
             Item it = {}, nit = {};
             Page page = {}, next = {};
             int tile = 0, ntile = 0;
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             // D / 16 lanes a column, 16 elements each: a line's 16-byte chunk
             constexpr int LPC = D / 16, CPW = 32 / LPC;
             const int ch = lane % LPC;
-            Walk walk(first, near);
+            Walk walk(first, near, own);
             bool ok = true;
             for (int k = 0; walk.left > 0; ++k) {
                 const Item it = walk.next(A);

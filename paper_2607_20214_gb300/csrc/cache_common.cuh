@@ -167,29 +167,76 @@ struct Start {
 // The sequences from the CTA's first on, as far as they fit.
 constexpr int kNearSeqs = 32;
 
-// All NT threads of the CTA; near: kNearSeqs entries. Writes the CTA's entry
-// of A.split. A thread has a sequence (several, one after the other, when B is
-// larger): whether a bound of the range lies in its tiles it sees by itself.
+// The range [t0, t1) of CTA k of n, each with total / n tiles or one more,
+// without a product that needs 64 bits; the host has checked that total fits.
+struct Cut {
+    unsigned total, n, q, rest;
+    __device__ __forceinline__ Cut(const CacheAttn &A, int tiles, int items) {
+        const int HC = A.c.Hkv * A.groups;
+        total = (unsigned)tiles * HC;
+        const unsigned live = (unsigned)items * HC;
+        n = min((unsigned)A.ctas, total);
+        if (live * kCacheMaxPieces < n) n = live * kCacheMaxPieces;
+        q = n ? total / n : 0;
+        rest = total - q * n;
+    }
+    __device__ __forceinline__ unsigned at(unsigned k) const {
+        return q * k + rest * k / n;
+    }
+    // the CTA that has tile t
+    __device__ __forceinline__ unsigned owner(unsigned t) const {
+        unsigned k = min((unsigned)((float)t * ((float)n / (float)total)),
+                         n - 1);
+        while (k > 0 && at(k) > t) --k;
+        while (at(k + 1) <= t) ++k;
+        return k;
+    }
+};
+// Where the range begins, for the thread whose sequence's tiles [a, z) hold
+// its first one.
+__device__ __forceinline__ Start start_in(int b, int tiles, unsigned a,
+                                          unsigned t0, unsigned t1) {
+    const unsigned in = t0 - a, hc = in / tiles;
+    return {b, (int)hc, (int)(in - hc * tiles), (int)(t1 - t0)};
+}
+// The item of the range's last tile, if it begins in the range and goes on.
+__device__ __forceinline__ CacheSplit split_in(const Cut &cut, int b,
+                                               const Seq &s, unsigned a,
+                                               unsigned t0, unsigned t1) {
+    const unsigned hc = (t1 - 1 - a) / s.tiles;
+    const unsigned i0 = a + hc * s.tiles, i1 = i0 + s.tiles;
+    if (i0 < t0 || i1 <= t1) return {0, 0, 0, 0};
+    return {b, (int)hc, (int)(cut.owner(i1 - 1) - blockIdx.x) + 1, s.n};
+}
+// Sums up to the lane's, over the warp.
+__device__ __forceinline__ int upto_lane(int x) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+
+// More than 32 sequences: all NT threads of the CTA together, a sequence a
+// thread (several, one after the other, beyond NT); near: kNearSeqs entries.
 template <int NT>
-__device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near) {
+__device__ __noinline__ Start divide_many(const CacheAttn &A, Seq *near) {
     __shared__ int warps[NT / 32], some[NT / 32];
     __shared__ Start mine;
     const CacheView &c = A.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rounds = (c.B + NT - 1) / NT, HC = c.Hkv * A.groups;
     Seq own = {0, 0, 0, 0};
-    // tiles of the sequences up to the thread's, from the round's first on
+    // tiles of the round's sequences up to the thread's
     auto sum = [&](int round) {
         const int b = round * NT + tid;
         own = {0, 0, 0, 0};
         if (b < c.B) own = sequence(A, b);
         int x = own.tiles;
         const int live = __popc(__ballot_sync(0xffffffffu, x > 0));
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
+        x = upto_lane(x);
         __syncthreads();  // the round before has read
         if (lane == 31) {
             warps[warp] = x;
@@ -211,48 +258,55 @@ __device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near) {
             items += some[w];
         }
     }
-    // the host has checked that total fits
-    const unsigned total = (unsigned)tiles * HC, k = blockIdx.x;
-    const unsigned n = min(min((unsigned)A.ctas, total),
-                           (unsigned)min((long)items * HC * kCacheMaxPieces,
-                                         1L << 30));
-    const unsigned q = n ? total / n : 0, rest = n ? total - q * n : 0;
-    // total k / n without the large product
-    auto bound = [&](unsigned i) { return q * i + rest * i / n; };
-    const unsigned t0 = k < n ? bound(k) : 0, t1 = k < n ? bound(k + 1) : 0;
+    const Cut cut(A, tiles, items);
+    const unsigned k = blockIdx.x;
+    const unsigned t0 = k < cut.n ? cut.at(k) : 0;
+    const unsigned t1 = k < cut.n ? cut.at(k + 1) : 0;
     int base = 0;
-    for (int r = 0; r < rounds && k < n; ++r) {
+    for (int r = 0; r < rounds && k < cut.n; ++r) {
         if (rounds > 1) upto = sum(r);
         const unsigned z = (unsigned)(base + upto) * HC;
         const unsigned a = z - (unsigned)own.tiles * HC;
         const int b = r * NT + tid;
-        if (a <= t0 && t0 < z) {
-            const int in = (int)(t0 - a);
-            mine = {b, in / own.tiles, in % own.tiles, (int)(t1 - t0)};
-        }
-        if (a < t1 && t1 <= z) {
-            // the item of the last tile: does it begin here and go on?
-            const int hc = (int)(t1 - 1 - a) / own.tiles;
-            const unsigned i0 = a + (unsigned)hc * own.tiles;
-            const unsigned i1 = i0 + own.tiles;
-            if (i0 >= t0 && i1 > t1) {
-                const int last = (int)range_owner(i1 - 1, total, n);
-                A.split[k] = {b, hc, last - (int)k + 1, own.n};
-            }
-        }
+        if (a <= t0 && t0 < z) mine = start_in(b, own.tiles, a, t0, t1);
+        if (a < t1 && t1 <= z) A.split[k] = split_in(cut, b, own, a, t0, t1);
         if (rounds > 1)
             for (int w = 0; w < NT / 32; ++w) base += warps[w];
     }
     __syncthreads();
     const Start s = mine;
-    if (rounds == 1) {
-        if (tid < c.B && tid >= s.b && tid < s.b + kNearSeqs)
-            near[tid - s.b] = own;
-    } else if (tid < kNearSeqs && s.b + tid < c.B) {
-        near[tid] = sequence(A, s.b + tid);
-    }
+    if (tid < kNearSeqs && s.b + tid < c.B) near[tid] = sequence(A, s.b + tid);
     __syncthreads();
     return s;
+}
+
+// The CTA's range; its entry of A.split is written. Up to 32 sequences every
+// warp finds it by itself, a sequence a lane (`own`, which Walk asks), so that
+// no warp waits for another.
+template <int NT>
+__device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near,
+                                        Seq &own) {
+    const CacheView &c = A.c;
+    own = {0, 0, 0, 0};
+    if (c.B > 32) return divide_many<NT>(A, near);
+    const int lane = threadIdx.x & 31, HC = c.Hkv * A.groups;
+    if (lane < c.B) own = sequence(A, lane);
+    const int upto = upto_lane(own.tiles);
+    const Cut cut(A, __shfl_sync(0xffffffffu, upto, 31),
+                  __popc(__ballot_sync(0xffffffffu, own.tiles > 0)));
+    const unsigned k = blockIdx.x;
+    if (k >= cut.n) {
+        if (threadIdx.x == 0) A.split[k] = {0, 0, 0, 0};
+        return {0, 0, 0, 0};
+    }
+    const unsigned t0 = cut.at(k), t1 = cut.at(k + 1);
+    const unsigned z = (unsigned)upto * HC, a = z - (unsigned)own.tiles * HC;
+    if (threadIdx.x < 32 && a < t1 && t1 <= z)
+        A.split[k] = split_in(cut, lane, own, a, t0, t1);
+    const int b =
+        __ffs(__ballot_sync(0xffffffffu, a <= t0 && t0 < z)) - 1;
+    return start_in(b, __shfl_sync(0xffffffffu, own.tiles, b),
+                    __shfl_sync(0xffffffffu, a, b), t0, t1);
 }
 
 // A CTA's share of one item.
@@ -263,13 +317,20 @@ struct alignas(16) Item {
     int slot;               // -1: the whole item; else 0 if it began in an
                             // earlier CTA, 1 if here
 };
-// Walks the items of a CTA's range.
+// Walks the items of a CTA's range. Whole warps.
 struct Walk {
     const Seq *near;
+    Seq own;
     int b0, b, hc, off, left;
-    __device__ __forceinline__ Walk(const Start &s, const Seq *n)
-        : near(n), b0(s.b), b(s.b), hc(s.hc), off(s.off), left(s.count) {}
+    __device__ __forceinline__ Walk(const Start &s, const Seq *n, const Seq &o)
+        : near(n), own(o), b0(s.b), b(s.b), hc(s.hc), off(s.off),
+          left(s.count) {}
     __device__ __forceinline__ Seq at(const CacheAttn &A, int b) const {
+        if (A.c.B <= 32)
+            return {__shfl_sync(0xffffffffu, own.len, b),
+                    __shfl_sync(0xffffffffu, own.n, b),
+                    __shfl_sync(0xffffffffu, own.walk, b),
+                    __shfl_sync(0xffffffffu, own.tiles, b)};
         return b - b0 < kNearSeqs ? near[b - b0] : sequence(A, b);
     }
     __device__ __forceinline__ Item next(const CacheAttn &A) {

@@ -129,75 +129,87 @@ __device__ __forceinline__ float page_max(const Page<D, E> &g, float x,
     return x;
 }
 
-// The page's channel extremes, in its first C threads. All threads of the
-// CTA; sh: [warps][C][2 P] words.
-template <typename R, int D, int E>
-__device__ __forceinline__ void page_extremes(const Page<D, E> &g,
-                                              uint32_t *hi, uint32_t *lo,
-                                              uint32_t *sh) {
-    constexpr int C = Page<D, E>::C, P = R::P;
-    for (int o = C; o < min(g.size, 32); o <<= 1) {
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            hi[i] = R::max2(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
-            lo[i] = R::min2(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
-        }
-    }
-    if (g.size > 32) {
-        const int lane = threadIdx.x & 31;
-        if (lane < C) {
-            uint32_t *at = sh + ((threadIdx.x >> 5) * C + lane) * 2 * P;
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                at[i] = hi[i];
-                at[P + i] = lo[i];
-            }
-        }
-        __syncthreads();
-        if (g.t < C) {
-            const int w0 = g.index * g.size / 32;
-            for (int w = 1; w < g.size / 32; ++w) {
-                const uint32_t *at = sh + ((w0 + w) * C + g.t) * 2 * P;
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    hi[i] = R::max2(hi[i], at[i]);
-                    lo[i] = R::min2(lo[i], at[P + i]);
-                }
-            }
-        }
-    }
-}
-
-// Bytes of bounds for the channels: the extremes' codes (of x f) over 4, rounded
+// Bytes of bounds for 4 channels: the extremes' codes (of x f) over 4, rounded
 // outwards, joined with the page's older ones times `drop`. Whole numbers in
 // [-112, 112] (448 / 4), clipped for a channel without a number.
 template <typename R>
-__device__ __forceinline__ void write_bounds(int8_t *at, int d,
+__device__ __forceinline__ void write_bounds(uint32_t *hi_at, uint32_t *lo_at,
                                              const uint32_t *hi,
                                              const uint32_t *lo, float f,
                                              bool had, float drop) {
-    uint32_t *const to[2] = {(uint32_t *)at, (uint32_t *)(at + d)};
+    const uint32_t old[2] = {had ? *hi_at : 0u, had ? *lo_at : 0u};
+    uint32_t out[2] = {0, 0};
 #pragma unroll
-    for (int k = 0; k < R::P * R::PER / 4; ++k) {
-        const uint32_t old[2] = {had ? to[0][k] : 0u, had ? to[1][k] : 0u};
-        uint32_t out[2] = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int ch = 4 * k + i;
-            const float2 h = R::get(hi[ch / R::PER]);
-            const float2 l = R::get(lo[ch / R::PER]);
-            const float2 x = from_e4m3x2(e4m3x2((i & 1 ? h.y : h.x) * f,
-                                                (i & 1 ? l.y : l.x) * f));
-            float u = ceilf(x.x * 0.25f), v = floorf(x.y * 0.25f);
-            if (had) {
-                u = fmaxf(u, ceilf((float)(int8_t)(old[0] >> 8 * i) * drop));
-                v = fminf(v, floorf((float)(int8_t)(old[1] >> 8 * i) * drop));
-            }
-            out[0] |= ((uint32_t)(int)u & 0xffu) << 8 * i;
-            out[1] |= ((uint32_t)(int)v & 0xffu) << 8 * i;
+    for (int i = 0; i < 4; ++i) {
+        const float2 h = R::get(hi[i / R::PER]), l = R::get(lo[i / R::PER]);
+        const float2 x = from_e4m3x2(
+            e4m3x2((i & 1 ? h.y : h.x) * f, (i & 1 ? l.y : l.x) * f));
+        float u = ceilf(x.x * 0.25f), v = floorf(x.y * 0.25f);
+        if (had) {
+            u = fmaxf(u, ceilf((float)(int8_t)(old[0] >> 8 * i) * drop));
+            v = fminf(v, floorf((float)(int8_t)(old[1] >> 8 * i) * drop));
         }
-        to[0][k] = out[0];
-        to[1][k] = out[1];
+        out[0] |= ((uint32_t)(int)u & 0xffu) << 8 * i;
+        out[1] |= ((uint32_t)(int)v & 0xffu) << 8 * i;
+    }
+    *hi_at = out[0];
+    *lo_at = out[1];
+}
+
+// The page's channel extremes into its bounds (`bounds`: where the page's
+// begin, or NULL: values, or nothing to write). All threads of the CTA; sh:
+// [warps][C][2 P] words. The threads of a page that share channels write four
+// of them each.
+template <typename R, int D, int E>
+__device__ __forceinline__ void page_bounds(const Page<D, E> &g, uint32_t *hi,
+                                            uint32_t *lo, uint32_t *sh,
+                                            int8_t *bounds, float f, bool had,
+                                            float drop) {
+    constexpr int C = Page<D, E>::C, P = R::P, PARTS = E / 4, W = P / PARTS;
+    static_assert(P * R::PER == E && PARTS <= 32 / C, "channels");
+    const int lane = threadIdx.x & 31;
+    // a whole warp without keys has nothing to exchange
+    if (__any_sync(0xffffffffu, bounds != nullptr)) {
+        for (int o = C; o < min(g.size, 32); o <<= 1) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                hi[i] = R::max2(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
+                lo[i] = R::min2(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
+            }
+        }
+    }
+    const int part = (g.size > 32 ? lane : g.t) / C;
+    uint32_t h[W], l[W];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k)
+        if (k == 0 || part == k)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                h[i] = hi[k * W + i];
+                l[i] = lo[k * W + i];
+            }
+    if (g.size > 32) {
+        uint32_t *at = sh + ((threadIdx.x >> 5) * C + lane % C) * 2 * P;
+        if (part < PARTS)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                at[part * W + i] = h[i];
+                at[P + part * W + i] = l[i];
+            }
+        __syncthreads();
+        if (g.t >= 32 || part >= PARTS) return;
+        for (int w = 1; w < g.size / 32; ++w) {
+            at += C * 2 * P;  // the page's next warp
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                h[i] = R::max2(h[i], at[part * W + i]);
+                l[i] = R::min2(l[i], at[P + part * W + i]);
+            }
+        }
+    }
+    if (bounds && part < PARTS) {
+        uint32_t *to = (uint32_t *)(bounds + g.ch * E) + part;
+        write_bounds<R>(to, to + D / 4, h, l, f, had, drop);
     }
 }
 
@@ -340,15 +352,12 @@ __global__ void __launch_bounds__(kWrThreads, sizeof(T) == 2 ? 4 : 2)
                                     y[7] * drop));
         }
     }
-    page_extremes<R>(g, hi, lo, sh);
-    if (id < 0) return;
-    if (keys && g.t < G::C)
-        write_bounds<R>(c.bounds + ph * 2 * D + g.ch * 8, D, hi, lo, f, had,
-                        drop);
-    // every thread of the page has read the scale: page_extremes' barrier (or
-    // the warp's exchange) lies between
-    __syncwarp();
-    if (g.t == 0) *scale = pow2(e);
+    page_bounds<R>(g, hi, lo, sh,
+                   keys && id >= 0 ? c.bounds + ph * 2 * D : nullptr, f, had,
+                   drop);
+    // every thread of the page has read the scale: page_max's exchange lies
+    // between
+    if (id >= 0 && g.t == 0) *scale = pow2(e);
 }
 
 __device__ __forceinline__ uint32_t h2_of_e4m3(uint32_t w) {
@@ -478,12 +487,10 @@ __global__ void __launch_bounds__(kWrThreads, 4)
                 make_uint4(o[0], o[1], o[2], o[3]);
         }
     }
-    page_extremes<R>(g, hi, lo, sh);
-    if (id < 0) return;
-    if (keys && g.t < G::C)
-        write_bounds<R>(c.bounds + ph * 2 * D + g.ch * 16, D, hi, lo, 1.0f,
-                        false, 1.0f);
-    if (g.t == 0) (keys ? c.ks : c.vs)[ph] = pow2(e);
+    page_bounds<R>(g, hi, lo, sh,
+                   keys && id >= 0 ? c.bounds + ph * 2 * D : nullptr, 1.0f,
+                   false, 1.0f);
+    if (id >= 0 && g.t == 0) (keys ? c.ks : c.vs)[ph] = pow2(e);
 }
 
 // CTAs for `pages` pages of keys and of values.
