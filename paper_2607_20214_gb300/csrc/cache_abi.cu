@@ -96,11 +96,13 @@ int check_queries(const CacheView &c) {
     if ((long)c.B * c.H * c.T > 1L << 30)
         return set_last_error(ELSAA_ERR_UNSUPPORTED,
                               "B * H * T must be at most 2^30");
-    const long tiles = ((long)c.max_pages * c.ps + kCacheTile - 1) / kCacheTile;
-    if (tiles * c.B > (1L << 30) / ((long)c.H * c.T))
+    // the tiles of all columns, with a few more for every item
+    const long tiles =
+        ((long)c.max_pages * c.ps + kCacheTile - 1) / kCacheTile + 7;
+    if (tiles * c.B > (1L << 31) / ((long)c.H * c.T))
         return set_last_error(ELSAA_ERR_UNSUPPORTED,
                               "B * H * T * max_pages * page_size must be at "
-                              "most 2^37");
+                              "most about 2^38");
     return ELSAA_OK;
 }
 

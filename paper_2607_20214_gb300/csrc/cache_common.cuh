@@ -136,9 +136,13 @@ __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *x) {
 //
 // Every K/V head and column group of a sequence is an item of
 // ceil(rows / kCacheTile) tiles (one at least, so that a query without keys
-// gets its row). The tiles of all items, one after the other, are cut into
-// equal ranges, one per CTA, so that ragged lengths load the SMs evenly; an
-// item that a cut crosses is written as pieces and merged afterwards. Every
+// gets its row). An item costs its tiles and, for its queries and its end,
+// about as much as kItemCost more (8000 cycles where a tile of 16 columns
+// takes 2000): 8 drafted sequences, some of a single token, took 35 us with
+// ranges of equal tiles, whose slowest CTA had six items. So the units tiles +
+// kItemCost of all items, one after the other, are cut into equal ranges, one
+// per CTA; an item that a cut crosses is written as pieces and merged
+// afterwards. Every
 // CTA finds its range by itself from the lengths: a launch that did it for all
 // cost more than the B loads and the scan.
 
@@ -159,6 +163,11 @@ __device__ __forceinline__ Seq sequence(const CacheAttn &A, int b) {
     return s;
 }
 
+constexpr int kItemCost = 3;
+__device__ __forceinline__ int units(const Seq &s) {
+    return s.tiles ? s.tiles + kItemCost : 0;
+}
+
 struct Start {
     int b, hc, off;  // sequence, head and group, first tile of that item
     int count;       // tiles of this CTA
@@ -167,15 +176,16 @@ struct Start {
 // The sequences from the CTA's first on, as far as they fit.
 constexpr int kNearSeqs = 32;
 
-// The range [t0, t1) of CTA k of n, each with total / n tiles or one more,
-// without a product that needs 64 bits; the host has checked that total fits.
+// The units of CTA k of n, total / n or one more, without a product that needs
+// 64 bits; the host has checked that total fits.
 struct Cut {
     unsigned total, n, q, rest;
-    __device__ __forceinline__ Cut(const CacheAttn &A, int tiles, int items) {
+    __device__ __forceinline__ Cut(const CacheAttn &A, int sum, int items) {
         const int HC = A.c.Hkv * A.groups;
-        total = (unsigned)tiles * HC;
         const unsigned live = (unsigned)items * HC;
-        n = min((unsigned)A.ctas, total);
+        total = (unsigned)sum * HC;
+        // no more CTAs than tiles
+        n = min((unsigned)A.ctas, total - live * kItemCost);
         if (live * kCacheMaxPieces < n) n = live * kCacheMaxPieces;
         q = n ? total / n : 0;
         rest = total - q * n;
@@ -183,30 +193,41 @@ struct Cut {
     __device__ __forceinline__ unsigned at(unsigned k) const {
         return q * k + rest * k / n;
     }
-    // the CTA that has tile t
-    __device__ __forceinline__ unsigned owner(unsigned t) const {
-        unsigned k = min((unsigned)((float)t * ((float)n / (float)total)),
+    // the CTA that has unit u
+    __device__ __forceinline__ unsigned owner(unsigned u) const {
+        unsigned k = min((unsigned)((float)u * ((float)n / (float)total)),
                          n - 1);
-        while (k > 0 && at(k) > t) --k;
-        while (at(k + 1) <= t) ++k;
+        while (k > 0 && at(k) > u) --k;
+        while (at(k + 1) <= u) ++k;
         return k;
     }
 };
-// Where the range begins, for the thread whose sequence's tiles [a, z) hold
-// its first one.
-__device__ __forceinline__ Start start_in(int b, int tiles, unsigned a,
-                                          unsigned t0, unsigned t1) {
-    const unsigned in = t0 - a, hc = in / tiles;
-    return {b, (int)hc, (int)(in - hc * tiles), (int)(t1 - t0)};
-}
-// The item of the range's last tile, if it begins in the range and goes on.
+// Unit u in the sequence of the thread that calls, whose units begin at a:
+// its item there (HC: the one behind the last), tiles of that item before u,
+// and tiles of all items before u; `before`: those of the sequences before.
+struct Place {
+    unsigned hc, off, tiles;
+    __device__ __forceinline__ Place(const Seq &s, unsigned a, unsigned u,
+                                     unsigned before) {
+        const unsigned each = s.tiles + kItemCost, in = u - a;
+        hc = in / each;
+        const unsigned r = in - hc * each;
+        off = r > kItemCost ? r - kItemCost : 0;
+        tiles = before + hc * s.tiles + off;
+    }
+};
+// The item that goes on behind the range, if it begins in it: the thread's
+// sequence has the range's end u1 (a < u1 <= its end), the range begins at u0.
 __device__ __forceinline__ CacheSplit split_in(const Cut &cut, int b,
                                                const Seq &s, unsigned a,
-                                               unsigned t0, unsigned t1) {
-    const unsigned hc = (t1 - 1 - a) / s.tiles;
-    const unsigned i0 = a + hc * s.tiles, i1 = i0 + s.tiles;
-    if (i0 < t0 || i1 <= t1) return {0, 0, 0, 0};
-    return {b, (int)hc, (int)(cut.owner(i1 - 1) - blockIdx.x) + 1, s.n};
+                                               unsigned u0, unsigned u1) {
+    const Place end(s, a, u1, 0);
+    const unsigned each = s.tiles + kItemCost, i0 = a + end.hc * each;
+    // its first tile is unit i0 + kItemCost; a range that begins before it
+    // begins the item
+    if (end.off == 0 || u0 > i0 + kItemCost) return {0, 0, 0, 0};
+    return {b, (int)end.hc,
+            (int)(cut.owner(i0 + each - 1) - blockIdx.x) + 1, s.n};
 }
 // Sums up to the lane's, over the warp.
 __device__ __forceinline__ int upto_lane(int x) {
@@ -224,57 +245,74 @@ __device__ __forceinline__ int upto_lane(int x) {
 template <int NT>
 __device__ __noinline__ Start divide_many(const CacheAttn &A, Seq *near) {
     __shared__ int warps[NT / 32], some[NT / 32];
-    __shared__ Start mine;
+    __shared__ Start mine;  // its count: tiles before the range
+    __shared__ int to;      // and before its end
     const CacheView &c = A.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rounds = (c.B + NT - 1) / NT, HC = c.Hkv * A.groups;
     Seq own = {0, 0, 0, 0};
-    // tiles of the round's sequences up to the thread's
+    int done = 0;  // tiles of the round's sequences up to the thread's
+    // their units
     auto sum = [&](int round) {
         const int b = round * NT + tid;
         own = {0, 0, 0, 0};
         if (b < c.B) own = sequence(A, b);
-        int x = own.tiles;
-        const int live = __popc(__ballot_sync(0xffffffffu, x > 0));
-        x = upto_lane(x);
+        const int live = __popc(__ballot_sync(0xffffffffu, own.tiles > 0));
+        int x = upto_lane(units(own));
+        done = upto_lane(own.tiles);
         __syncthreads();  // the round before has read
         if (lane == 31) {
             warps[warp] = x;
             some[warp] = live;
         }
         __syncthreads();
-        for (int w = 0; w < warp; ++w) x += warps[w];
+        for (int w = 0; w < warp; ++w) {
+            x += warps[w];
+            done += warps[w] - some[w] * kItemCost;
+        }
         return x;
     };
     if (tid == 0) {
         mine = {0, 0, 0, 0};
+        to = 0;
         A.split[blockIdx.x] = {0, 0, 0, 0};
     }
-    int tiles = 0, items = 0, upto = 0;
+    int total = 0, items = 0, upto = 0;
     for (int r = 0; r < rounds; ++r) {
         upto = sum(r);
         for (int w = 0; w < NT / 32; ++w) {
-            tiles += warps[w];
+            total += warps[w];
             items += some[w];
         }
     }
-    const Cut cut(A, tiles, items);
+    const Cut cut(A, total, items);
     const unsigned k = blockIdx.x;
-    const unsigned t0 = k < cut.n ? cut.at(k) : 0;
-    const unsigned t1 = k < cut.n ? cut.at(k + 1) : 0;
-    int base = 0;
+    const unsigned u0 = k < cut.n ? cut.at(k) : 0;
+    const unsigned u1 = k < cut.n ? cut.at(k + 1) : 0;
+    int base = 0, tiles = 0;
     for (int r = 0; r < rounds && k < cut.n; ++r) {
         if (rounds > 1) upto = sum(r);
         const unsigned z = (unsigned)(base + upto) * HC;
-        const unsigned a = z - (unsigned)own.tiles * HC;
+        const unsigned a = z - (unsigned)units(own) * HC;
+        const unsigned before = (unsigned)(tiles + done - own.tiles) * HC;
         const int b = r * NT + tid;
-        if (a <= t0 && t0 < z) mine = start_in(b, own.tiles, a, t0, t1);
-        if (a < t1 && t1 <= z) A.split[k] = split_in(cut, b, own, a, t0, t1);
+        if (a <= u0 && u0 < z) {
+            const Place p(own, a, u0, before);
+            mine = {b, (int)p.hc, (int)p.off, (int)p.tiles};
+        }
+        if (a < u1 && u1 <= z) {
+            to = (int)Place(own, a, u1, before).tiles;
+            A.split[k] = split_in(cut, b, own, a, u0, u1);
+        }
         if (rounds > 1)
-            for (int w = 0; w < NT / 32; ++w) base += warps[w];
+            for (int w = 0; w < NT / 32; ++w) {
+                base += warps[w];
+                tiles += warps[w] - some[w] * kItemCost;
+            }
     }
     __syncthreads();
-    const Start s = mine;
+    Start s = mine;
+    s.count = to - s.count;
     if (tid < kNearSeqs && s.b + tid < c.B) near[tid] = sequence(A, s.b + tid);
     __syncthreads();
     return s;
@@ -291,7 +329,8 @@ __device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near,
     if (c.B > 32) return divide_many<NT>(A, near);
     const int lane = threadIdx.x & 31, HC = c.Hkv * A.groups;
     if (lane < c.B) own = sequence(A, lane);
-    const int upto = upto_lane(own.tiles);
+    const int upto = upto_lane(units(own));
+    const int done = upto_lane(own.tiles);
     const Cut cut(A, __shfl_sync(0xffffffffu, upto, 31),
                   __popc(__ballot_sync(0xffffffffu, own.tiles > 0)));
     const unsigned k = blockIdx.x;
@@ -299,14 +338,21 @@ __device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near,
         if (threadIdx.x == 0) A.split[k] = {0, 0, 0, 0};
         return {0, 0, 0, 0};
     }
-    const unsigned t0 = cut.at(k), t1 = cut.at(k + 1);
-    const unsigned z = (unsigned)upto * HC, a = z - (unsigned)own.tiles * HC;
-    if (threadIdx.x < 32 && a < t1 && t1 <= z)
-        A.split[k] = split_in(cut, lane, own, a, t0, t1);
-    const int b =
-        __ffs(__ballot_sync(0xffffffffu, a <= t0 && t0 < z)) - 1;
-    return start_in(b, __shfl_sync(0xffffffffu, own.tiles, b),
-                    __shfl_sync(0xffffffffu, a, b), t0, t1);
+    const unsigned u0 = cut.at(k), u1 = cut.at(k + 1);
+    const unsigned z = (unsigned)upto * HC, a = z - (unsigned)units(own) * HC;
+    const unsigned before = (unsigned)(done - own.tiles) * HC;
+    if (threadIdx.x < 32 && a < u1 && u1 <= z)
+        A.split[k] = split_in(cut, lane, own, a, u0, u1);
+    // every lane evaluates both ends in the sequence that has them
+    auto place = [&](unsigned u, int b) {
+        const Seq s = {0, 0, 0, __shfl_sync(0xffffffffu, own.tiles, b)};
+        return Place(s, __shfl_sync(0xffffffffu, a, b), u,
+                     __shfl_sync(0xffffffffu, before, b));
+    };
+    const int b0 = __ffs(__ballot_sync(0xffffffffu, a <= u0 && u0 < z)) - 1;
+    const int b1 = __ffs(__ballot_sync(0xffffffffu, a < u1 && u1 <= z)) - 1;
+    const Place p0 = place(u0, b0), p1 = place(u1, b1);
+    return {b0, (int)p0.hc, (int)p0.off, (int)(p1.tiles - p0.tiles)};
 }
 
 // A CTA's share of one item.
