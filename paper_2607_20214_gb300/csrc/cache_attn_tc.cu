@@ -277,17 +277,18 @@ __global__ void __launch_bounds__(kTaThreads, 2)
         };
         if (warp == 4) {
             // -------------------------------------------- pages and scales
-            // A batch is the next 32 pages of an item, a page a lane; the next
-            // batch's table entries and scales are asked for as soon as this
-            // one's first tile is on its way.
-            const int pt = kCacheTile / c.ps;  // pages of a tile
+            // A batch is the next 32 pages of an item, a page a lane, which
+            // loads it; the next batch's table entries and scales are asked
+            // for as soon as this one's first tile is on its way.
+            const int lp = __ffs(kCacheTile / c.ps) - 1;  // pages of a tile
+            const int pt = 1 << lp, slot = lane & (pt - 1);
             struct Page {
                 int id, pos, rows;
                 float ks, vs;
             };
             auto fetch = [&](const Item &it, int tile) {
                 Page g = {-1, 0, 0, 0.0f, 0.0f};
-                const int e = tile * pt + lane;
+                const int e = (tile << lp) + lane;
                 int p = -1;
                 if ((long)e * c.ps < it.walk)
                     p = A.pages ? A.pages[((size_t)it.b * c.Hkv + it.h) *
@@ -319,48 +320,49 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 page = fetch(it, tile);
             }
             for (int i = 0; i < count && ok;) {
-                const int nt = min(32 / pt, it.off + it.count - tile);
+                const int nt = min(32 >> lp, it.off + it.count - tile);
+                // of the lane's tile: bytes to come, largest value scale
+                const uint32_t live =
+                    __ballot_sync(0xffffffffu, page.id >= 0) >>
+                    (lane & ~(pt - 1));
+                const uint32_t bytes =
+                    __popc(live & ((1u << pt) - 1)) * c.ps * D;
+                float vmax = page.vs;
+                for (int o = 1; o < pt; o <<= 1)
+                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
+                const int row = (page.id * c.Hkv + it.h) * c.ps;
+                const uint32_t to = slot * c.ps * D;
                 for (int k = 0; k < nt; ++k, ++i) {
-                    const int src = (k * pt + lane) & 31;
-                    int id = __shfl_sync(0xffffffffu, page.id, src);
-                    if (lane >= pt) id = -1;
-                    const int row = (id * c.Hkv + it.h) * c.ps;
-                    const uint32_t bytes =
-                        __popc(__ballot_sync(0xffffffffu, id >= 0)) * c.ps * D;
-                    const int ks = i % C::KS, vs = i % C::VS;
+                    const bool mine = lane >> lp == k;
+                    const int ks = i % C::KS, vs = i % C::VS, ms = i % C::MS;
                     if (i >= C::KS)
                         ok = wait(&bars.k_empty[ks], (i / C::KS - 1) & 1, 180);
                     if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(&bars.k_full[ks], bytes);
-                    __syncwarp();
-                    if (id >= 0)
-                        tma_load_2d(sK + ks * C::kTile + lane * c.ps * D, &tmK,
-                                    0, row, &bars.k_full[ks]);
-                    ++kn;
-                    float v = __shfl_sync(0xffffffffu, page.vs, src);
-                    const float vmax = warp_max(lane < pt ? v : 0.0f);
-                    const float kk = __shfl_sync(0xffffffffu, page.ks, src);
-                    const int pos = __shfl_sync(0xffffffffu, page.pos, src);
-                    const int rows = __shfl_sync(0xffffffffu, page.rows, src);
-                    if (lane < pt) {
-                        TileMeta &m = meta[i % C::MS];
-                        m.ks[lane] = kk;
-                        m.vs[lane] = v;
-                        m.pos[lane] = pos;
-                        m.rows[lane] = rows;
-                        if (lane == 0) m.vmax = vmax;
+                    if (mine) {
+                        if (slot == 0) mbar_expect_tx(&bars.k_full[ks], bytes);
+                        if (page.id >= 0)
+                            tma_load_2d(sK + ks * C::kTile + to, &tmK, 0, row,
+                                        &bars.k_full[ks]);
+                        TileMeta &m = meta[ms];
+                        m.ks[slot] = page.ks;
+                        m.vs[slot] = page.vs;
+                        m.pos[slot] = page.pos;
+                        m.rows[slot] = page.rows;
+                        m.vmax = vmax;
                     }
+                    ++kn;
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&bars.m_full[i % C::MS]);
+                    if (lane == 0) mbar_arrive(&bars.m_full[ms]);
                     if (i >= C::VS)
                         ok = wait(&bars.v_empty[vs], (i / C::VS - 1) & 1, 181);
                     if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(&bars.v_full[vs], bytes);
-                    __syncwarp();
-                    if (id >= 0)
-                        tma_load_2d(sV + vs * C::kTile + lane * c.ps * D, &tmV,
-                                    0, D == 128 ? row : row / 2,
-                                    &bars.v_full[vs]);
+                    if (mine) {
+                        if (slot == 0) mbar_expect_tx(&bars.v_full[vs], bytes);
+                        if (page.id >= 0)
+                            tma_load_2d(sV + vs * C::kTile + to, &tmV, 0,
+                                        D == 128 ? row : row / 2,
+                                        &bars.v_full[vs]);
+                    }
                     ++vn;
                     if (k == 0) {
                         nit = it;
@@ -376,6 +378,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 tile = ntile;
                 page = next;
             }
+            __syncwarp();
             // whatever was asked for has arrived before the CTA ends
             for (int j = max(0, kn - C::KS); j < kn; ++j)
                 mbar_wait(&bars.k_full[j % C::KS], (j / C::KS) & 1, c.status,
