@@ -338,6 +338,8 @@ int set_last_error(int code, const char *fmt, ...) {
     return code;
 }
 
+void clear_last_error() { g_err[0] = 0; }
+
 cudaError_t timed_launch(const char *name, cudaStream_t st,
                          cudaError_t (*fn)(void *), void *arg) {
     return timed(name, st, [&] { return fn(arg); });

@@ -162,7 +162,7 @@ int check_workspace(const void *ws, size_t bytes, size_t need) {
 extern "C" int elsaa_cache_workspace_size(const elsaa_cache *cache, int T,
                                           int weights, int keep,
                                           size_t *bytes) {
-    set_last_error(0, "");
+    clear_last_error();
     if (!bytes)
         return set_last_error(ELSAA_ERR_INVALID_ARG, "bytes is NULL");
     CacheView c;
@@ -183,7 +183,7 @@ extern "C" int elsaa_cache_workspace_size(const elsaa_cache *cache, int T,
 extern "C" int elsaa_cache_append(const elsaa_cache *cache, int T,
                                   const void *k, const void *v,
                                   const int32_t *new_len, void *stream) {
-    set_last_error(0, "");
+    clear_last_error();
     CacheView c;
     const int rc = make_view(cache, T, &c);
     if (rc != ELSAA_OK) return rc;
@@ -206,7 +206,7 @@ extern "C" int elsaa_cache_select(const elsaa_cache *cache, int T,
                                   int n_sel, int first, int last,
                                   int32_t *pages, void *workspace,
                                   size_t workspace_bytes, void *stream) {
-    set_last_error(0, "");
+    clear_last_error();
     CacheView c;
     int rc = make_view(cache, T, &c);
     if (rc == ELSAA_OK) rc = check_queries(c);
@@ -239,7 +239,7 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
                                      float *weight_out, void *o, float *lse,
                                      void *workspace, size_t workspace_bytes,
                                      void *stream) {
-    set_last_error(0, "");
+    clear_last_error();
     CacheAttn A = {};
     int rc = make_view(cache, T, &A.c);
     if (rc == ELSAA_OK) rc = check_queries(A.c);
@@ -303,7 +303,7 @@ extern "C" int elsaa_cache_evict(const elsaa_cache *cache,
                                  float *weight_out, int32_t *lengths_out,
                                  int32_t *kept, void *workspace,
                                  size_t workspace_bytes, void *stream) {
-    set_last_error(0, "");
+    clear_last_error();
     CacheView c;
     int rc = make_view(cache, 0, &c);
     if (rc != ELSAA_OK) return rc;

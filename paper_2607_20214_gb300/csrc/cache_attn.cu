@@ -368,8 +368,8 @@ __global__ void __launch_bounds__(kWtThreads)
 
 template <typename T, int D, int NG>
 cudaError_t launch_simt(const CacheAttn &A, cudaStream_t st) {
-    return launch_after(k_cache_attn_simt<T, D, NG>, dim3(A.ctas), kSaThreads,
-                        0, st, A);
+    return launch_cache<k_cache_attn_simt<T, D, NG>>(
+        dim3(A.ctas), kSaThreads, 0, 0, 1, st, A);
 }
 
 template <typename T, int D>
@@ -398,17 +398,16 @@ cudaError_t launch_cache_attn_simt(const CacheAttn &A, cudaStream_t st) {
 }
 
 cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st) {
-    return launch_after(k_cache_merge,
-                        dim3(A.ctas, (A.cols + kMgCols - 1) / kMgCols),
-                        kMgThreads, 0, st, A);
+    return launch_cache<k_cache_merge>(
+        dim3(A.ctas, (A.cols + kMgCols - 1) / kMgCols), kMgThreads, 0, 0, 1,
+        st, A);
 }
 
 cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st) {
     const long cap = (long)A.c.max_pages * A.c.ps;
-    return launch_after(k_cache_weights,
-                        dim3((unsigned)((cap + kWtTokens - 1) / kWtTokens),
-                             A.c.Hkv, A.c.B),
-                        kWtThreads, 0, st, A);
+    return launch_cache<k_cache_weights>(
+        dim3((unsigned)((cap + kWtTokens - 1) / kWtTokens), A.c.Hkv, A.c.B),
+        kWtThreads, 0, 0, 1, st, A);
 }
 
 }  // namespace elsaa

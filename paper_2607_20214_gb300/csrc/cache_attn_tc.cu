@@ -884,8 +884,8 @@ cudaError_t launch_tc(const CacheAttn &A, cudaStream_t st) {
         e = make_tma_map_u8(&tmV, c.v, D == 128 ? rows : rows / 2, 128,
                             D == 128 ? c.ps : c.ps / 2);
     if (e != cudaSuccess) return e;
-    return launch_after(k_cache_attn_tc<D, NV>, dim3(A.ctas), kTaThreads,
-                        C::kSmem, st, tmK, tmV, A);
+    return launch_cache<k_cache_attn_tc<D, NV>>(
+        dim3(A.ctas), kTaThreads, C::kSmem, C::kSmem, 1, st, tmK, tmV, A);
 }
 
 template <int D>

@@ -2,12 +2,49 @@
 // them, powers of two, e4m3 conversions, the division of tiles over CTAs.
 #pragma once
 
+#include <atomic>
+
 #include "cache.h"
 #include "device_common.cuh"
 #include "tc_common.cuh"
 
 namespace elsaa {
 namespace cache {
+
+// Launch of kernel K as launch_after does it, in clusters of `cluster` CTAs
+// along x. `most`: the largest dynamic shared memory that it is launched with,
+// allowed once for every device (asking each time is a tenth of a launch).
+template <auto K, typename... A>
+cudaError_t launch_cache(dim3 grid, int threads, size_t smem, size_t most,
+                         int cluster, cudaStream_t st, A... args) {
+    static std::atomic<unsigned long long> allowed{0};
+    if (most > 0) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return taken(e);
+        const unsigned long long bit = 1ull << (dev & 63);
+        if (dev > 63 || !(allowed.load(std::memory_order_relaxed) & bit)) {
+            e = cudaFuncSetAttribute(
+                K, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+            if (e != cudaSuccess) return taken(e);
+            allowed.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return taken(cudaLaunchKernelEx(&cfg, K, args...));
+}
 
 // Out of line: faults are rare, and the code before a kernel's first loads is
 // fetched while nothing else runs.

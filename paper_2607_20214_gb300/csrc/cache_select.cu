@@ -557,30 +557,6 @@ __global__ void __launch_bounds__(kKpThreads)
     if (cs > 1) tc::cluster_sync();
 }
 
-// launch_after with clusters of `cluster` CTAs along x.
-template <typename... K, typename... A>
-cudaError_t launch_clusters(void (*kern)(K...), dim3 grid, int threads,
-                            size_t smem, int cluster, cudaStream_t st,
-                            A... args) {
-    cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return taken(e);
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return taken(cudaLaunchKernelEx(&cfg, kern, K(args)...));
-}
-
 }  // namespace
 
 cudaError_t launch_cache_select(const CacheView &c, const void *q, int n_sel,
@@ -597,10 +573,12 @@ cudaError_t launch_cache_select(const CacheView &c, const void *q, int n_sel,
                         (shared_keys ? sizeof(uint32_t) * c.max_pages : 0);
     auto go = [&](auto t, auto dd) {
         using T = decltype(t);
-        return launch_clusters(k_cache_select<T, decltype(dd)::value>,
-                               dim3(cluster, c.Hkv, c.B), kScThreads, smem,
-                               cluster, st, c, (const T *)q, n_sel, first,
-                               last, pages, (uint32_t *)scores, shared_keys);
+        constexpr int D = decltype(dd)::value;
+        return launch_cache<k_cache_select<T, D>>(
+            dim3(cluster, c.Hkv, c.B), kScThreads, smem,
+            (128 + kScPages) * score_row(D) + sizeof(uint32_t) * kScShared,
+            cluster, st, c, (const T *)q, n_sel, first, last, pages,
+            (uint32_t *)scores, shared_keys);
     };
     auto by_d = [&](auto t) {
         switch (c.d) {
@@ -622,9 +600,10 @@ cudaError_t launch_cache_keep(const CacheView &c, const float *weight,
         cluster *= 2;
     const long run = ((slots + cluster - 1) / cluster + 31) / 32 * 32;
     const int shared_keys = run <= kKpShared;
-    return launch_clusters(k_cache_keep, dim3(cluster, c.Hkv, c.B), kKpThreads,
-                           shared_keys ? sizeof(uint32_t) * run : 0, cluster,
-                           st, c, weight, keep, recent, out, shared_keys);
+    return launch_cache<k_cache_keep>(
+        dim3(cluster, c.Hkv, c.B), kKpThreads,
+        shared_keys ? sizeof(uint32_t) * run : 0, sizeof(uint32_t) * kKpShared,
+        cluster, st, c, weight, keep, recent, out, shared_keys);
 }
 
 }  // namespace elsaa

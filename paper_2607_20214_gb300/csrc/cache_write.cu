@@ -508,8 +508,8 @@ cudaError_t launch_cache_append(const CacheView &c, const void *k,
                     c.B);
     auto go = [&](auto t, auto dd) {
         using T = decltype(t);
-        return launch_after(k_cache_append<T, decltype(dd)::value>, grid,
-                            kWrThreads, 0, st, c, (const T *)k, (const T *)v);
+        return launch_cache<k_cache_append<T, decltype(dd)::value>>(
+            grid, kWrThreads, 0, 0, 1, st, c, (const T *)k, (const T *)v);
     };
     auto by_d = [&](auto t) {
         switch (c.d) {
@@ -527,9 +527,9 @@ cudaError_t launch_cache_compact(const CacheView &c, int keep,
                                  int32_t *lengths_out, cudaStream_t st) {
     const dim3 grid(page_ctas(c, ((long)keep + c.ps - 1) / c.ps), c.Hkv, c.B);
     auto go = [&](auto dd) {
-        return launch_after(k_cache_compact<decltype(dd)::value>, grid,
-                            kWrThreads, 0, st, c, keep, rows, count,
-                            dst_table, dst_pages, lengths_out);
+        return launch_cache<k_cache_compact<decltype(dd)::value>>(
+            grid, kWrThreads, 0, 0, 1, st, c, keep, rows, count, dst_table,
+            dst_pages, lengths_out);
     };
     switch (c.d) {
         case 32: return go(std::integral_constant<int, 32>{});

@@ -62,6 +62,7 @@ struct Plan {
 
 // Records a one-line error for elsaa_last_error() and returns `code`.
 int set_last_error(int code, const char *fmt, ...);
+void clear_last_error();
 
 // Fills `plan` from validated parameters. Returns ELSAA_OK or an error code
 // and message (no CUDA calls).
