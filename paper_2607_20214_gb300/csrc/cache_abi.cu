@@ -117,7 +117,13 @@ Layout attention_layout(const CacheView &c, bool tc, bool weights) {
     const int gt = c.G * c.T;
     l.cols = tc ? cache_tc_cols(gt) : cache_simt_cols(gt);
     l.groups = (gt + l.cols - 1) / l.cols;
+    // no more than the table has tiles for, or than may share the items
+    const long tiles =
+        ((long)c.max_pages * c.ps + kCacheTile - 1) / kCacheTile;
+    const long share = tiles < kCacheMaxPieces ? tiles : kCacheMaxPieces;
+    const long most = (long)c.B * c.Hkv * l.groups * share;
     l.ctas = tc ? kCacheTcCtas : kCacheSimtCtas;
+    if (most < l.ctas) l.ctas = (int)most;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;

@@ -219,23 +219,28 @@ __global__ void __launch_bounds__(kSaThreads)
 //
 // The columns of an item that began in CTA blockIdx.x and went on in others:
 // its pieces in order, so the result does not depend on which CTA was first.
-// A thread has a channel of a column; with few columns the pieces are shared
-// out among groups of threads, whose sums are added in order as well. A few
-// dependent reads of L2 is all it takes, so it is as short as its loads in
-// flight are many.
+// A thread has a channel of a column; with few columns a block the pieces are
+// shared out among groups of threads, whose sums are added in order as well. A
+// few dependent reads of L2 is all it takes, 700 cycles for 8 pieces a thread,
+// so it is as short as its loads in flight are many: with few items, whose
+// pieces are many, a block has one column (64 pieces of 4 columns: 9 us less
+// than with 4 columns a block), else 4, for fewer blocks.
 constexpr int kMgThreads = 512;
-constexpr int kMgCols = 4;  // columns per block
+int merge_cols(const CacheAttn &A) {
+    const long items = (long)A.c.B * A.c.Hkv * A.groups;
+    return A.cols < 4 || 8 * items <= A.ctas ? 1 : 4;
+}
 
 __global__ void __launch_bounds__(kMgThreads)
-    k_cache_merge(const __grid_constant__ CacheAttn A) {
+    k_cache_merge(const __grid_constant__ CacheAttn A, int cols) {
     wait_for_stream();
     __shared__ float sm[kMgThreads], sl[kMgThreads], sx[kMgThreads];
     const CacheSplit s = A.split[blockIdx.x];
     if (s.pieces == 0) return;
     const CacheView &c = A.c;
     const int tid = threadIdx.x, d = c.d, ch = tid % d, group = tid / d;
-    const int cols = min(A.cols, kMgCols), parts = kMgThreads / d / cols;
-    const int g = blockIdx.y * kMgCols + group % cols, part = group / cols;
+    const int parts = kMgThreads / d / cols;
+    const int g = blockIdx.y * cols + group % cols, part = group / cols;
     const int h = s.hc / A.groups, col = s.hc % A.groups * A.cols + g;
     float M = -INFINITY, L = 0.0f, x = 0.0f;
     if (part < parts) {
@@ -398,9 +403,9 @@ cudaError_t launch_cache_attn_simt(const CacheAttn &A, cudaStream_t st) {
 }
 
 cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st) {
-    return launch_cache<k_cache_merge>(
-        dim3(A.ctas, (A.cols + kMgCols - 1) / kMgCols), kMgThreads, 0, 0, 1,
-        st, A);
+    const int cols = merge_cols(A);
+    return launch_cache<k_cache_merge>(dim3(A.ctas, A.cols / cols),
+                                       kMgThreads, 0, 0, 1, st, A, cols);
 }
 
 cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st) {
