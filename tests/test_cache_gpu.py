@@ -586,3 +586,146 @@ def test_other_stream_and_offsets_past_32_bits():
     oc.evict(zero, w.cpu().numpy(), 100, 10, dst6, wz)
     for x in "kv":
         assert np.array_equal(oc.E4M3[got[x][6:8]], oc.E4M3[zero[x][6:8]])
+
+
+# ---------------------------------------------------- the rules' other sides
+
+@pytest.mark.parametrize("impl", IMPL)
+@pytest.mark.parametrize("B", [32, 33, 300, 700])
+def test_attention_many_sequences(impl, B):
+    """The division with a sequence a lane, a sequence a thread, several a
+    thread; most sequences short or empty, a few long."""
+    g = np.random.default_rng(B)
+    lengths = g.choice([0, 1, 2, 15, 40], B)
+    lengths[g.integers(0, B, 3)] = 900
+    new = np.minimum(lengths, 1)
+    run_attention(Case([int(x) for x in lengths], 2, 1, 64, 16, seed=B),
+                  new_len=[int(x) for x in new], impl=impl)
+
+
+@pytest.mark.parametrize("impl", IMPL)
+@pytest.mark.parametrize("H,hkv,T", [(1, 1, 1), (16, 1, 1), (4, 4, 1),
+                                     (20, 2, 2)])
+def test_attention_one_sequence_shared_by_the_most_ctas(impl, H, hkv, T):
+    run_attention(Case([9000], H, hkv, 128, 128, seed=H), T=T, impl=impl)
+
+
+@pytest.mark.parametrize("impl", IMPL)
+def test_queries_that_are_no_numbers_stay_alone(impl):
+    """NaN and infinities in one query reach no other query's row."""
+    case = Case([300, 40], 8, 2, 64, 32, seed=17)
+    _, q = case.rows(8, 2)
+    clean = E.elsaa_cache_attention(case.device(E, impl), q)
+    q[0, 1, 0, 5] = float("nan")
+    q[1, 6, 1, 0] = float("inf")
+    o = E.elsaa_cache_attention(case.device(E, impl), q)
+    bad = torch.isnan(o).any(3)
+    assert bad[0, 1, 0] and bad[1, 6, 1] and bad.sum() == 2
+    assert torch.equal(o[~bad], clean[~bad])
+
+
+def big_cache(pages_of_pool, ps, d, lengths, max_pages, H, hkv, seed):
+    """A cache whose table names the pool's pages many times over (reading a
+    page for several places is allowed)."""
+    case = Case([pages_of_pool * ps], H, hkv, d, ps, seed=seed, extra_pages=0)
+    c = case.c
+    B = len(lengths)
+    c["table"] = case.rng.integers(0, pages_of_pool, (B, max_pages)).astype(
+        np.int32)
+    c["lengths"] = np.array(lengths, np.int32)
+    case.B, case.max_pages = B, max_pages
+    return case
+
+
+def test_select_from_more_pages_than_shared_memory_holds():
+    case = big_cache(40, 16, 32, [20011 * 16 - 3, 700], 20011, 2, 1, 18)
+    # scores that differ: every place has its own page, of 40 boxes; ties go
+    # to the lower place
+    q, qd = case.rows(2, 1)
+    got = E.elsaa_cache_select(case.device(E), qd, 600, 2, 3)
+    ref = oc.select(case.c, q, [1, 1], 600, 2, 3)
+    assert np.array_equal(got.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("n", [16385, 60000, 400000])
+def test_evict_long_rows(n):
+    """Rows of one CTA, of a cluster, and of a cluster without room for their
+    keys."""
+    pages = -(-n // 16)
+    case = big_cache(60, 16, 32, [n, 100], pages, 1, 1, 19)
+    keep = 1000
+    width = -(-keep // 16)
+    num = len(case.c["k"])
+    for x in ("k", "v", "k_scale", "v_scale", "bounds"):  # room for the kept
+        a = case.c[x]
+        case.c[x] = np.concatenate([a, np.zeros((2 * width,) + a.shape[1:],
+                                                a.dtype)])
+    dst = (num + np.arange(2 * width, dtype=np.int32)).reshape(2, width)
+    w = np.exp(2 * case.rng.standard_normal((2, 1, pages * 16))).astype(
+        np.float32)
+    w[case.rng.random(w.shape) < 0.3] = 0.25
+    cache = case.device(E)
+    kept = torch.empty((2, 1, keep), dtype=torch.int32, device="cuda")
+    wout = torch.zeros((2, 1, width * 16), device="cuda")
+    _, lens = E.elsaa_cache_evict(cache, torch.tensor(w).cuda(), keep, 17,
+                                  int_tensor(dst), weight_out=wout, kept=kept)
+    ref_w = np.zeros((2, 1, width * 16))
+    ref_len, ref_kept = oc.evict(case.c, w, keep, 17, dst, ref_w)
+    assert np.array_equal(kept.cpu().numpy(), ref_kept)
+    assert np.array_equal(lens.cpu().numpy(), ref_len)
+    assert np.array_equal(wout.double().cpu().numpy(), ref_w)
+    assert case.same_bytes(cache) == []
+
+
+def test_two_graphs_share_a_workspace_and_two_streams_do_not():
+    """Graphs of different sizes replayed in turn over one workspace; two
+    calls at once on streams and workspaces of their own."""
+    a, b = Case([3000, 10], 8, 2, 128, 64, seed=20), Case([70, 900, 5], 4, 4,
+                                                        64, 16, seed=21)
+    ca, cb = a.device(E), b.device(E)
+    _, qa = a.rows(8, 1)
+    _, qb = b.rows(4, 3)
+    want = [E.elsaa_cache_attention(ca, qa), E.elsaa_cache_attention(cb, qb)]
+    n = max(E.elsaa_cache_workspace_size(ca, 1),
+            E.elsaa_cache_workspace_size(cb, 3))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros_like(qa), torch.zeros_like(qb)]
+    graphs = []
+    side = torch.cuda.Stream()
+    for c, q, o in ((ca, qa, outs[0]), (cb, qb, outs[1])):
+        g = torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(g, stream=side):
+            E.elsaa_cache_attention(c, q, o=o, workspace=ws)
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1, 0, 0):
+        outs[i].zero_()
+        graphs[i].replay()
+        assert torch.equal(outs[i], want[i])
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    w1 = E.new_cache_workspace(ca, 1)
+    w2 = E.new_cache_workspace(cb, 3)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        outs[0].zero_(), outs[1].zero_()
+        torch.cuda.synchronize()
+        E.elsaa_cache_attention(ca, qa, o=outs[0], workspace=w1, stream=s1)
+        E.elsaa_cache_attention(cb, qb, o=outs[1], workspace=w2, stream=s2)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_the_timing_tool_names_the_cache_kernels():
+    case = Case([500], 4, 2, 64, 32, seed=22)
+    cache = case.device(E)
+    _, q = case.rows(4, 1)
+    _, k = case.rows(2, 1)
+    w = torch.zeros((1, 2, case.max_pages * 32), device="cuda")
+    E.elsaa_profile_start()
+    E.elsaa_cache_append(cache, k, k)
+    pages = E.elsaa_cache_select(cache, q, 4)
+    E.elsaa_cache_attention(cache, q, pages=pages, weight_out=w)
+    E.elsaa_cache_evict(cache, w, 32, 1, int_tensor([[case.free[0]]]))
+    got = E.elsaa_profile_stop()
+    assert {"cache_append", "cache_select", "cache_attn_tc", "cache_merge",
+            "cache_weights", "cache_keep", "cache_compact"} <= set(got)
