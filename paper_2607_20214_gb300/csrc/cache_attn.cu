@@ -143,8 +143,10 @@ __global__ void __launch_bounds__(kSaThreads)
                 for (int i = 0; i < 16; ++i) acc[g][i] *= al;
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
-                    sc[g][s] = tc::ex2_approx(sc[g][s] - ref);
-                    l[g] += sc[g][s];
+                    const bool seen = sc[g][s] != -INFINITY;
+                    const float p = tc::ex2_approx(sc[g][s] - ref);
+                    l[g] += p;
+                    sc[g][s] = seen ? p : -1.0f;
                 }
             }
 #pragma unroll
@@ -160,7 +162,7 @@ __global__ void __launch_bounds__(kSaThreads)
                     // a token that a column does not see adds nothing,
                     // whatever its codes are
                     const float p = sc[g][s] * f;
-                    if (sc[g][s] != 0.0f)
+                    if (!(sc[g][s] < 0.0f))
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             acc[g][i] = fmaf(p, x[i], acc[g][i]);

@@ -33,6 +33,8 @@
 // walked. The range's tiles run through rings of K and V buffers; S of tile
 // i + 1 is issued before O of tile i, so the softmax finds its next scores
 // ready. Two CTAs share an SM.
+#include <limits.h>
+
 #include "cache_common.cuh"
 
 namespace elsaa {
@@ -193,6 +195,35 @@ __device__ __forceinline__ uint32_t rest16(uint32_t a, uint32_t b) {
     return r;
 }
 
+// 0x80 in every byte whose low 7 bits are all set: e4m3's NaN.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+    return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t at) {
+    uint4 r;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+                 : "r"(at)
+                 : "memory");
+    return r;
+}
+// The NaN codes among 16 in shared memory become 0; their channels' `from`
+// falls to pos.
+static __device__ __noinline__ void drop_nan(uint32_t at, int *from,
+                                             int pos) {
+    const uint4 q = ld_shared_v4(at);
+    uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t bad = nan_bytes(w[i]);
+        for (int k = 0; k < 4; ++k)
+            if (bad >> (8 * k) & 0x80u) {
+                w[i] &= ~(0xffu << (8 * k));
+                atomicMin(from + 4 * i + k, pos);
+            }
+    }
+    st_shared_v4(at, w[0], w[1], w[2], w[3]);
+}
+
 // The pages of one tile, written by the producer.
 struct TileMeta {
     float ks[kMaxPagesPerTile];   // key scale
@@ -228,6 +259,8 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     __shared__ float red[2][4][NV];
     __shared__ __align__(16) float stat[2][4][4][NV];
     __shared__ float4 fin[2][NV];  // sums of the four warps' tokens
+    // of an item, by channel: the first new token whose value is no number
+    __shared__ int nan_from[D];
     volatile int *abort = &abort_flag;
     const CacheView &c = A.c;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -576,6 +609,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
         float lastM = 0.0f, factor = 0.0f;
         int item = 0, t = 0, end = 0;
         bool ok = true, fine = count > 0;
+        if (tid < D) nan_from[tid] = INT_MAX;
 #pragma unroll
         for (int g = 0; g < NH; ++g) acc[g] = l[g] = make_float2(0.0f, 0.0f);
         // column pair g of a row of stat
@@ -628,6 +662,13 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                 buf[g * 128 + tid] = g & 1 ? acc[g / 2].y : acc[g / 2].x;
 #pragma unroll
             for (int g = 0; g < NH; ++g) acc[g] = make_float2(0.0f, 0.0f);
+            if (tid < D && nan_from[tid] != INT_MAX) {
+                for (int g = 0; g < last.cols; ++g)
+                    if (nan_from[tid] <=
+                        last_seen(A, last.len, last.n, last.col0 + g))
+                        buf[g * 128 + tid] = NAN;
+                nan_from[tid] = INT_MAX;
+            }
             named_sync(1, 128);
             const size_t r0 = query_row(A, last.b, last.h, last.col0);
 #pragma unroll 1
@@ -838,19 +879,36 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                     st_shared_v4(at + line_offset<C::W>(pr, k), w[x][4 * k],
                                  w[x][4 * k + 1], w[x][4 * k + 2],
                                  w[x][4 * k + 3]);
-                if (!in[x] && x < n) {
-                    // a row that does not count may hold anything, NaN too:
-                    // its weight is 0, its values have to be
+                if (x < n && (!in[x] || pos[x] > it.len - it.n)) {
+                    // A row that does not count may hold anything, NaN too:
+                    // its weight is 0, its values have to be. A new token's
+                    // weight is 0 for the queries before it: values that are
+                    // no numbers become 0 and are kept for the others.
                     const int vs = (u + x) % C::VS;
-                    ok = mbar_wait_or_abort(&bars.v_full[vs],
-                                            ((u + x) / C::VS) & 1, abort,
-                                            c.status, 193) &&
-                         ok;
+                    const bool there = mbar_wait_or_abort(
+                        &bars.v_full[vs], ((u + x) / C::VS) & 1, abort,
+                        c.status, 193);
+                    ok = there && ok;
+                    const uint32_t line = sV + vs * C::kTile;
                     const int c0 = D == 128 ? 0 : (tid & 1) * 4;
+                    if (!in[x]) {
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        st_shared_zero16(sV + vs * C::kTile +
-                                         line_offset<128>(pr, c0 + k));
+                        for (int k = 0; k < D / 16; ++k)
+                            st_shared_zero16(line +
+                                             line_offset<128>(pr, c0 + k));
+                    } else if (there) {
+                        uint32_t bad = 0;
+#pragma unroll 4
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint4 q = ld_shared_v4(
+                                line + line_offset<128>(pr, c0 + k));
+                            bad |= nan_bytes(q.x) | nan_bytes(q.y) |
+                                   nan_bytes(q.z) | nan_bytes(q.w);
+                        }
+                        for (int k = 0; bad != 0 && k < D / 16; ++k)
+                            drop_nan(line + line_offset<128>(pr, c0 + k),
+                                     nan_from + 16 * k, pos[x]);
+                    }
                 }
             }
             __syncwarp();

@@ -729,3 +729,41 @@ def test_the_timing_tool_names_the_cache_kernels():
     got = E.elsaa_profile_stop()
     assert {"cache_append", "cache_select", "cache_attn_tc", "cache_merge",
             "cache_weights", "cache_keep", "cache_compact"} <= set(got)
+
+
+@pytest.mark.parametrize("impl", IMPL)
+@pytest.mark.parametrize("d,ps,T,G", [(64, 16, 5, 1), (128, 128, 5, 2),
+                                      (64, 64, 6, 16), (128, 16, 3, 4)])
+def test_nan_of_a_later_token_stays_unseen(impl, d, ps, T, G):
+    """A value or a key that is no number reaches the new tokens from its own
+    on, its own channel, and no other; the new tokens lie in two tiles."""
+    case = Case([130, 66, 258], 2 * G, 2, d, ps, seed=23)
+    _, q = case.rows(2 * G, T)
+    clean = E.elsaa_cache_attention(case.device(E, impl), q)
+    want = torch.zeros(clean.shape, dtype=torch.bool, device="cuda")
+    for b, h, t, ch in ((0, 0, 1, 5), (0, 0, 2, d - 1), (0, 1, T - 1, 0),
+                        (1, 0, 0, d // 2), (2, 1, 2, 7), (2, 1, 1, 7)):
+        pos = int(case.c["lengths"][b]) - T + t
+        case.c["v"][case.c["table"][b, pos // ps], h, pos % ps, ch] = NAN
+        want[b, h * G:(h + 1) * G, t:, ch] = True
+    pos = 258 - 2
+    case.c["k"][case.c["table"][2, pos // ps], 0, pos % ps, 1] = NAN
+    want[2, :G, T - 2:] = True
+    o = E.elsaa_cache_attention(case.device(E, impl), q)
+    assert torch.equal(torch.isnan(o), want)
+    assert torch.equal(o[~want], clean[~want])
+
+
+@pytest.mark.parametrize("impl", IMPL)
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_values_of_the_least_weights_are_seen(impl, d):
+    """A weight too small for a float is not zero."""
+    case = Case([500], 4, 2, d, 32, seed=24)
+    _, q = case.rows(4, 1, 60.0)
+    for h in range(2):
+        for p in range(0, 500, 37):
+            case.c["v"][case.c["table"][0, p // 32], h, p % 32, p % d] = NAN
+    want = torch.zeros(d, dtype=torch.bool, device="cuda")
+    want[[p % d for p in range(0, 500, 37)]] = True
+    o = E.elsaa_cache_attention(case.device(E, impl), q)
+    assert torch.equal(torch.isnan(o), want.expand(1, 4, 1, d))
