@@ -84,8 +84,9 @@ int elsaa_cache_workspace_size(const elsaa_cache *cache, int T, int weights,
  * k, v      [B, H_kv, T, d_h] of cache->dtype, 16-byte aligned.
  * new_len   [B] int32 in [0, T]: sequence b's new tokens n_b, or NULL for T
  *           each. Row t < n_b is token lengths[b] - n_b + t: advance lengths
- *           first. Rows t >= n_b are not read, and rows of a page behind
- *           lengths[b] keep what they held.
+ *           first. Rows t >= n_b, and those of a token before the first,
+ *           are not read, and rows of a page behind lengths[b] keep what they
+ *           held.
  *
  * With e_new the least e in [-64, 120] with |x| <= 448 2^e for every new x of
  * a page and head, the page's exponent becomes e_new if it held no older
@@ -130,7 +131,9 @@ int elsaa_cache_select(const elsaa_cache *cache, int T, const void *q,
  *     O = sum_j exp(s_j - lse) v_j
  * for query t < n_b of sequence b over the tokens j <= lengths[b] - n_b + t
  * (of the pages listed, if any). The rows just appended are in the cache, as
- * every other in 8 bits. A query without a key gets O = 0, lse = -inf.
+ * every other in 8 bits. A query without a key gets O = 0, lse = -inf. A NaN
+ * code reaches the queries that see its token (a value's: that channel of
+ * theirs) and no other.
  *
  * q, o      [B, H, T, d_h] of cache->dtype, 16-byte aligned. Rows t >= n_b of
  *           o and lse keep what they held.

@@ -13,7 +13,7 @@ constexpr int kCacheExpLow = -64, kCacheExpHigh = 120;
 constexpr int kQueryExpLow = -60;
 // Tokens per tile of the attention kernels: a whole number of pages.
 constexpr int kCacheTile = 128;
-// Sequences of a call: their tile counts are summed in shared memory.
+// Sequences of a call: every CTA of the attention kernels reads all lengths.
 constexpr int kCacheMaxB = 4096;
 // In-band status codes and sites of the cache kernels.
 constexpr int kDevCachePage = 5;    // a page outside the pool was skipped
@@ -62,8 +62,8 @@ struct CacheAttn {
 // one walks at a time.
 constexpr int kCacheSimtCtas = 152 * 3;
 constexpr int kCacheTcCtas = 152 * 2;
-// CTAs that share one item at most: what the merge of an item costs grows with
-// them.
+// CTAs that share the items at most, an item on average: what the merge costs
+// grows with them (128 and 304 were slower).
 constexpr int kCacheMaxPieces = 64;
 inline int cache_simt_cols(int gt) { return gt >= 3 ? 4 : gt; }
 inline int cache_tc_cols(int gt) {

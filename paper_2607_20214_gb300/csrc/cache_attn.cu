@@ -48,7 +48,8 @@ __global__ void __launch_bounds__(kSaThreads)
         for (int g = 0; g < NG; ++g) {
             m[g] = -INFINITY;
             l[g] = 0.0f;
-            limit[g] = g < it.cols ? last_seen(A, it.len, it.n, it.col0 + g) : -1;
+            limit[g] =
+                g < it.cols ? last_seen(A, it.len, it.n, it.col0 + g) : -1;
 #pragma unroll
             for (int i = 0; i < 16; ++i) qf[g][i] = acc[g][i] = 0.0f;
             if (limit[g] >= 0) {

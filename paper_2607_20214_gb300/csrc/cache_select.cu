@@ -27,7 +27,7 @@ struct TopkShared {
     alignas(16) int hist[2][kBins];  // of a pass, and of the next
     int warps[NT / 32][2];
     int bin, above;
-    alignas(8) int taken[2];  // keys above the threshold and equal to it in this CTA
+    alignas(8) int taken[2];  // this CTA's keys above the threshold, equal
 };
 
 // Two neighbouring words of CTA `rank`'s shared memory.

@@ -30,7 +30,7 @@ struct Page {
     static constexpr int ROWS = 64 / E;  // rows of a thread
     int size;                            // threads of the page
     int t;                               // this one
-    int ch, row, step;                   // channels from E ch, rows row + i step
+    int ch, row, step;                   // channels E ch.., rows row + i step
     int index;                           // which of the CTA's pages
     __device__ __forceinline__ explicit Page(int ps) {
         size = ps * D / 64;
@@ -42,23 +42,20 @@ struct Page {
     }
 };
 
-// Extremes of neighbouring channels, in the type that the rows come in (rounding is
-// monotonous, so the extremes of the codes are the codes of the extremes).
-// NaN is left out.
-#define ELSAA_EXTREME_OPS(NAME, TYPE)                                       \
-    __device__ __forceinline__ uint32_t NAME##_max(uint32_t a, uint32_t b) { \
-        uint32_t r;                                                         \
-        asm("max." TYPE " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));        \
-        return r;                                                           \
-    }                                                                       \
-    __device__ __forceinline__ uint32_t NAME##_min(uint32_t a, uint32_t b) { \
-        uint32_t r;                                                         \
-        asm("min." TYPE " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));        \
-        return r;                                                           \
+// Extremes of neighbouring channels, in the type that the rows come in
+// (rounding is monotonous, so the extremes of the codes are the codes of the
+// extremes). NaN is left out.
+#define ELSAA_EXTREME(NAME, OP)                                       \
+    __device__ __forceinline__ uint32_t NAME(uint32_t a, uint32_t b) { \
+        uint32_t r;                                                   \
+        asm(OP " %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));            \
+        return r;                                                     \
     }
-ELSAA_EXTREME_OPS(bf16x2, "bf16x2")
-ELSAA_EXTREME_OPS(f16x2, "f16x2")
-#undef ELSAA_EXTREME_OPS
+ELSAA_EXTREME(bf16x2_max, "max.bf16x2")
+ELSAA_EXTREME(bf16x2_min, "min.bf16x2")
+ELSAA_EXTREME(f16x2_max, "max.f16x2")
+ELSAA_EXTREME(f16x2_min, "min.f16x2")
+#undef ELSAA_EXTREME
 
 struct Bf16Rows {  // 8 channels, bf16 pairs
     static constexpr int P = 4, PER = 2;  // words, channels a word

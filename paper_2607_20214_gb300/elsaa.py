@@ -7,6 +7,7 @@ raises RuntimeError; there is no fallback implementation.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -262,6 +263,8 @@ def _ptr(t, name, dtype=None, numel=None, device=None):
 # torch.cuda.current_stream builds a Stream object (2 us, as much as a kernel
 # launch); the raw handle is all that is needed
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice",
+                          torch.cuda.current_device)
 
 
 def _stream_of(stream, dev):
@@ -775,6 +778,26 @@ def _rows(t, name, cache, heads):
     return _cptr(t, name, cache.torch_dtype, t.numel(), cache), s[2]
 
 
+def _own(stream, cache):
+    """Memory that a call makes for itself belongs to the call's stream, or it
+    could be given out again while the call still runs there."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream_of(stream, None),
+                                           cache.device)
+    return torch.cuda.stream(stream)
+
+
+def _stream_for(stream, cache):
+    """_stream_of, for a cache on the current device: on another one the
+    kernels would follow pointers that are not its own."""
+    if _current_device() != cache.index:
+        raise ValueError("the cache is on %s, which is not the current "
+                         "device" % cache.device)
+    return _stream_of(stream, cache.device)
+
+
 def _scratch(workspace, cache):
     """(pointer, bytes) of a workspace."""
     if workspace.get_device() != cache.index or \
@@ -790,7 +813,7 @@ def elsaa_cache_append(cache: elsaa_cache, k, v, new_len=None, stream=None):
     _check(load_library().elsaa_cache_append(
         cache.ref, T, kp, _cptr(v, "v", cache.torch_dtype, k.numel(), cache),
         _cptr(new_len, "new_len", torch.int32, cache.B, cache),
-        _stream_of(stream, cache.device)))
+        _stream_for(stream, cache)))
 
 
 def elsaa_cache_select(cache: elsaa_cache, q, n_sel, first=1, last=1,
@@ -799,17 +822,19 @@ def elsaa_cache_select(cache: elsaa_cache, q, n_sel, first=1, last=1,
     """Enqueue elsaa_cache_select for queries q [B, H, T, d_h]; returns pages
     [B, H_kv, n_sel] int32 (allocated here when not given)."""
     qp, T = _rows(q, "q", cache, cache.H)
-    if pages is None:
-        pages = torch.empty((cache.B, cache.H_kv, n_sel), dtype=torch.int32,
-                            device=cache.device)
-    if workspace is None:
-        workspace = new_cache_workspace(cache, T)
+    if pages is None or workspace is None:
+        with _own(stream, cache):
+            if pages is None:
+                pages = torch.empty((cache.B, cache.H_kv, n_sel),
+                                    dtype=torch.int32, device=cache.device)
+            if workspace is None:
+                workspace = new_cache_workspace(cache, T)
     ws, nbytes = _scratch(workspace, cache)
     _check(load_library().elsaa_cache_select(
         cache.ref, T, qp, _cptr(new_len, "new_len", torch.int32, cache.B,
                                 cache), n_sel, first, last,
         _cptr(pages, "pages", torch.int32, cache.B * cache.H_kv * n_sel,
-              cache), ws, nbytes, _stream_of(stream, cache.device)))
+              cache), ws, nbytes, _stream_for(stream, cache)))
     return pages
 
 
@@ -820,10 +845,13 @@ def elsaa_cache_attention(cache: elsaa_cache, q, pages=None, new_len=None,
     (allocated here when not given, rows behind new_len then undefined).
     pages: as elsaa_cache_select returns them, or None for all."""
     qp, T = _rows(q, "q", cache, cache.H)
-    if o is None:
-        o = torch.empty_like(q)
-    if workspace is None:
-        workspace = new_cache_workspace(cache, T, weight_out is not None)
+    if o is None or workspace is None:
+        with _own(stream, cache):
+            if o is None:
+                o = torch.empty_like(q)
+            if workspace is None:
+                workspace = new_cache_workspace(cache, T,
+                                                weight_out is not None)
     f32, i32, B = torch.float32, torch.int32, cache.B
     n_sel = 0 if pages is None else pages.shape[-1]
     ws, nbytes = _scratch(workspace, cache)
@@ -834,7 +862,7 @@ def elsaa_cache_attention(cache: elsaa_cache, q, pages=None, new_len=None,
         _cptr(weight_out, "weight_out", f32, cache.slots, cache),
         _cptr(o, "o", cache.torch_dtype, q.numel(), cache),
         _cptr(lse, "lse", f32, B * cache.H * T, cache), ws, nbytes,
-        _stream_of(stream, cache.device)))
+        _stream_for(stream, cache)))
     return o
 
 
@@ -846,13 +874,16 @@ def elsaa_cache_evict(cache: elsaa_cache, weight, keep, recent, dst_table,
     [B, dst_pages] afterwards."""
     i32, f32, B = torch.int32, torch.float32, cache.B
     width, ps, bh = dst_table.shape[-1], cache.page_size, B * cache.H_kv
-    if weight_out is None:
-        weight_out = torch.zeros((B, cache.H_kv, width * ps),
-                                 device=cache.device)
-    if lengths_out is None:
-        lengths_out = torch.empty((B,), dtype=i32, device=cache.device)
-    if workspace is None:
-        workspace = new_cache_workspace(cache, 1, False, keep)
+    if weight_out is None or lengths_out is None or workspace is None:
+        with _own(stream, cache):
+            if weight_out is None:
+                weight_out = torch.zeros((B, cache.H_kv, width * ps),
+                                         device=cache.device)
+            if lengths_out is None:
+                lengths_out = torch.empty((B,), dtype=i32,
+                                          device=cache.device)
+            if workspace is None:
+                workspace = new_cache_workspace(cache, 1, False, keep)
     ws, nbytes = _scratch(workspace, cache)
     _check(load_library().elsaa_cache_evict(
         cache.ref, _cptr(weight, "weight", f32, cache.slots, cache), keep,
@@ -860,5 +891,5 @@ def elsaa_cache_evict(cache: elsaa_cache, weight, keep, recent, dst_table,
         _cptr(weight_out, "weight_out", f32, bh * width * ps, cache),
         _cptr(lengths_out, "lengths_out", i32, B, cache),
         _cptr(kept, "kept", i32, bh * keep, cache), ws, nbytes,
-        _stream_of(stream, cache.device)))
+        _stream_for(stream, cache)))
     return weight_out, lengths_out

@@ -767,3 +767,51 @@ def test_nan_values_of_the_least_weights_are_seen(impl, d):
     want[[p % d for p in range(0, 500, 37)]] = True
     o = E.elsaa_cache_attention(case.device(E, impl), q)
     assert torch.equal(torch.isnan(o), want.expand(1, 4, 1, d))
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_what_a_call_allocates_belongs_to_its_stream(monkeypatch, raw):
+    """Not to the current one, which could give it out again meanwhile."""
+    case = Case([200, 30], 4, 2, 64, 32, seed=25)
+    cache = case.device(E)
+    _, q = case.rows(4, 1)
+    made = []
+    new = E.new_cache_workspace
+    monkeypatch.setattr(E, "new_cache_workspace", lambda *a: made.append(
+        torch.cuda.current_stream().cuda_stream) or new(*a))
+    want = E.elsaa_cache_attention(cache, q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    st = side.cuda_stream if raw else side
+    pages = E.elsaa_cache_select(cache, q, 8, stream=st)
+    o = E.elsaa_cache_attention(cache, q, pages=pages, stream=st)
+    w = torch.ones((2, 2, case.max_pages * 32), device="cuda")
+    dst = int_tensor([[case.free[0]], [case.free[1]]])
+    torch.cuda.synchronize()
+    wout, _ = E.elsaa_cache_evict(cache, w, 20, 4, dst, stream=st)
+    side.synchronize()
+    assert made == [0] + 3 * [side.cuda_stream]
+    assert torch.equal(o, want)
+    assert (wout.cpu()[:, :, :20] == 1).all() and wout.sum() == 80
+
+
+def test_a_cache_of_another_device_is_refused(monkeypatch):
+    case = Case([20], 4, 2, 64, 32, seed=26)
+    cache = case.device(E)
+    _, q = case.rows(4, 1)
+    _, k = case.rows(2, 1)
+    w = torch.zeros((1, 2, case.max_pages * 32), device="cuda")
+    dst = int_tensor([[case.free[0]]])
+    ws = E.new_cache_workspace(cache, 1, True, 8)
+    out = torch.zeros((1, 2, 32), device="cuda"), int_tensor([0])
+    pages = int_tensor([[[0, 0]]] * 2).reshape(1, 2, 2)
+    monkeypatch.setattr(E, "_current_device", lambda: 1)
+    for call in (lambda: E.elsaa_cache_append(cache, k, k),
+                 lambda: E.elsaa_cache_select(cache, q, 2, pages=pages,
+                                              workspace=ws),
+                 lambda: E.elsaa_cache_attention(cache, q, o=q,
+                                                 workspace=ws),
+                 lambda: E.elsaa_cache_evict(cache, w, 8, 1, dst, *out,
+                                             workspace=ws)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
