@@ -318,10 +318,9 @@ __global__ void __launch_bounds__(kWtThreads)
     const int h = blockIdx.y, b = blockIdx.z, GT = c.G * c.T;
     const int tid = threadIdx.x;
     const size_t bh = (size_t)b * c.Hkv + h;
-    const int len = tokens(c, b), j0 = blockIdx.x * kWtTokens;
-    const int j = j0 + 4 * tid;
+    const int j0 = blockIdx.x * kWtTokens, j = j0 + 4 * tid;
+    const auto [len, n] = lengths(c, b);
     if (j0 >= len) return;
-    const int n = fresh(c, b);
     const bool any = n > 0;
     // a column that is no query adds nothing: 2^(s - inf)
     if (any && tid < GT)

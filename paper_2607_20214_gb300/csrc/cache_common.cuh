@@ -53,25 +53,24 @@ static __device__ __noinline__ void report_rare(DeviceStatus *st, int code,
     report(st, code, where, a, b);
 }
 
-// Tokens of sequence b, clipped to its table row.
-__device__ __forceinline__ int tokens(const CacheView &c, int b) {
-    const int n = c.lengths[b], cap = c.max_pages * c.ps;
-    if (n < 0 || n > cap) {
-        report_rare(c.status, kDevCacheLength, b, n, cap);
-        return n < 0 ? 0 : cap;
+// Tokens of sequence b, clipped to its table row, and its new tokens. Both
+// loads are issued before one is looked at: a kernel's first loads are on its
+// critical path.
+struct Lengths {
+    int len, n;
+};
+__device__ __forceinline__ Lengths lengths(const CacheView &c, int b) {
+    Lengths x = {c.lengths[b], c.new_len ? c.new_len[b] : c.T};
+    const int cap = c.max_pages * c.ps;
+    if (x.len < 0 || x.len > cap) {
+        report_rare(c.status, kDevCacheLength, b, x.len, cap);
+        x.len = x.len < 0 ? 0 : cap;
     }
-    return n;
-}
-
-// New tokens of sequence b.
-__device__ __forceinline__ int fresh(const CacheView &c, int b) {
-    if (!c.new_len) return c.T;
-    const int n = c.new_len[b];
-    if (n < 0 || n > c.T) {
-        report_rare(c.status, kDevCacheLength, b, n, c.T);
-        return n < 0 ? 0 : c.T;
+    if (x.n < 0 || x.n > c.T) {
+        report_rare(c.status, kDevCacheLength, b, x.n, c.T);
+        x.n = x.n < 0 ? 0 : c.T;
     }
-    return n;
+    return x;
 }
 
 // A page of the pool, or -1.
@@ -190,9 +189,10 @@ struct Seq {
     int tiles;   // of a head's item; 0 without queries
 };
 __device__ __forceinline__ Seq sequence(const CacheAttn &A, int b) {
+    const Lengths x = lengths(A.c, b);
     Seq s;
-    s.len = tokens(A.c, b);
-    s.n = fresh(A.c, b);
+    s.len = x.len;
+    s.n = x.n;
     s.walk = A.pages ? min((s.len + A.c.ps - 1) / A.c.ps, A.n_sel) * A.c.ps
                      : s.len;
     s.tiles =

@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kScThreads, 2)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
     const size_t bh = (size_t)b * c.Hkv + h;
-    const int n = fresh(c, b), len = tokens(c, b);
+    const auto [len, n] = lengths(c, b);
     const int np = n == 0 ? 0 : (len + c.ps - 1) / c.ps;
     constexpr int W = D / 16, ROW = score_row(D) / 16;  // 16-byte pieces
     const int GT = c.G * c.T, GT8 = (GT + 7) & ~7;
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(kKpThreads)
     const int cs = gridDim.x, rank = blockIdx.x;
     const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
     const size_t bh = (size_t)b * c.Hkv + h;
-    const int n = tokens(c, b), m = min(n, keep);
+    const int n = lengths(c, b).len, m = min(n, keep);
     const float *w = weight + bh * c.max_pages * c.ps;
     int32_t *kept = out.kept ? out.kept + bh * keep : nullptr;
     int32_t *rows = out.rows + bh * keep;

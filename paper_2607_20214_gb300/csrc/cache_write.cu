@@ -270,7 +270,8 @@ __global__ void __launch_bounds__(kWrThreads, sizeof(T) == 2 ? 4 : 2)
     const int h = blockIdx.y, b = blockIdx.z;
     const int q = blockIdx.x * (kWrThreads / g.size) + g.index;
     const bool keys = (q & 1) == 0;
-    const int end = tokens(c, b), start = end - fresh(c, b);
+    const auto [end, fresh] = lengths(c, b);
+    const int start = end - fresh;
     const int p = max(start, 0) / c.ps + (q >> 1), p0 = p * c.ps;
     // rows [r0, r1) of the page are new, [0, r0) older; they are read while
     // the table entry is on its way
