@@ -26,7 +26,7 @@ template <int NT>
 struct TopkShared {
     alignas(16) int hist[2][kBins];  // of a pass, and of the next
     int warps[NT / 32][2];
-    int bin, above;
+    int bin, above, count;  // the threshold's bin, keys above it and in it
     alignas(8) int taken[2];  // this CTA's keys above the threshold, equal
 };
 
@@ -147,6 +147,7 @@ __device__ __forceinline__ void find_threshold(K key, int n, int m, int cs,
                 if (a < left && left <= a + bins[i]) {
                     S.bin = kBins - 1 - (tid * PER + i);
                     S.above = a;
+                    S.count = bins[i];
                 }
                 a += bins[i];
             }
@@ -155,6 +156,13 @@ __device__ __forceinline__ void find_threshold(K key, int n, int m, int cs,
         prefix |= (uint32_t)S.bin << shift;
         mask |= digit << shift;
         left -= S.above;
+        if (S.count == left) {
+            // the whole bin is selected: with distinct keys nearly always
+            // before the last pass (there are other keys below: m < all)
+            thr = prefix - 1;
+            ties = 0;
+            return;
+        }
         __syncthreads();
     }
     thr = prefix;

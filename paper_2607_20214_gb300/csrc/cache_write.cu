@@ -55,6 +55,8 @@ ELSAA_EXTREME(bf16x2_max, "max.bf16x2")
 ELSAA_EXTREME(bf16x2_min, "min.bf16x2")
 ELSAA_EXTREME(f16x2_max, "max.f16x2")
 ELSAA_EXTREME(f16x2_min, "min.f16x2")
+// of the magnitudes; the sign means nothing
+ELSAA_EXTREME(f16x2_abs_max, "max.xorsign.abs.f16x2")
 #undef ELSAA_EXTREME
 
 struct Bf16Rows {  // 8 channels, bf16 pairs
@@ -374,6 +376,24 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
     return r;
 }
 
+// The codes of four fp16 numbers.
+__device__ __forceinline__ uint32_t e4m3x4_of(uint32_t a, uint32_t b) {
+    uint16_t x, y;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(x) : "r"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(y) : "r"(b));
+    return (uint32_t)x | (uint32_t)y << 16;
+}
+
+// Codes times 4, for a factor beyond fp16's 2^15 (448 is 2^-9 2^17 at most).
+static __device__ __noinline__ uint4 times_four(uint4 w) {
+    const uint32_t f = pow2_h2(2);
+    auto four = [=](uint32_t c) {
+        return e4m3x4_of(mul_h2(h2_of_e4m3(c), f),
+                         mul_h2(h2_of_e4m3(c >> 16), f));
+    };
+    return make_uint4(four(w.x), four(w.y), four(w.z), four(w.w));
+}
+
 __device__ __forceinline__ uint32_t word(const uint4 &w, int m) {
     return m == 0 ? w.x : m == 1 ? w.y : m == 2 ? w.z : w.w;
 }
@@ -435,10 +455,10 @@ __global__ void __launch_bounds__(kWrThreads, 4)
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const uint32_t w = word(raw[i], m);
-            top = R::max2(top, h2_of_e4m3(w) & R::kAbs);
-            top = R::max2(top, h2_of_e4m3(w >> 16) & R::kAbs);
+            top = f16x2_abs_max(top, h2_of_e4m3(w));
+            top = f16x2_abs_max(top, h2_of_e4m3(w >> 16));
         }
-        const float2 x = R::get(top);
+        const float2 x = R::get(top & R::kAbs);
         const float sc = __int_as_float(ex[i]);
         amax = fmaxf(amax, magnitude(fmaxf(x.x, x.y) * sc));
         ex[i] = scale_exponent(sc);
@@ -459,27 +479,23 @@ __global__ void __launch_bounds__(kWrThreads, 4)
             // code 2^k in fp16: exact wherever it does not end below half
             // the smallest code
             const int k = ex[i] - e;
-            const uint32_t f = pow2_h2(k);
-            uint32_t o[4];
+            if (k > 15) raw[i] = times_four(raw[i]);
+            // the page's own exponent, that of most rows: the codes stay
+            uint32_t o[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            if (keys || k != 0) {
+                const uint32_t f = pow2_h2(k > 15 ? k - 2 : k);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                uint32_t x[2] = {h2_of_e4m3(word(raw[i], m)),
-                                 h2_of_e4m3(word(raw[i], m) >> 16)};
-                uint16_t z[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    x[y] = mul_h2(x[y], f);
-                    // beyond 2^15 (448 is 2^-9 2^17 at most) a second factor
-                    if (k > 15) x[y] = mul_h2(x[y], pow2_h2(k - 15));
+                for (int m = 0; m < 4; ++m) {
+                    const uint32_t x = mul_h2(h2_of_e4m3(o[m]), f);
+                    const uint32_t y = mul_h2(h2_of_e4m3(o[m] >> 16), f);
                     if (keys) {
-                        hi[2 * m + y] = R::max2(hi[2 * m + y], x[y]);
-                        lo[2 * m + y] = R::min2(lo[2 * m + y], x[y]);
+                        hi[2 * m] = R::max2(hi[2 * m], x);
+                        lo[2 * m] = R::min2(lo[2 * m], x);
+                        hi[2 * m + 1] = R::max2(hi[2 * m + 1], y);
+                        lo[2 * m + 1] = R::min2(lo[2 * m + 1], y);
                     }
-                    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;"
-                        : "=h"(z[y])
-                        : "r"(x[y]));
+                    o[m] = e4m3x4_of(x, y);
                 }
-                o[m] = (uint32_t)z[0] | (uint32_t)z[1] << 16;
             }
             *(uint4 *)(codes + (size_t)r * D) =
                 make_uint4(o[0], o[1], o[2], o[3]);
