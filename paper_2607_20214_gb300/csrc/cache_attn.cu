@@ -237,6 +237,7 @@ int merge_cols(const CacheAttn &A) {
 __global__ void __launch_bounds__(kMgThreads)
     k_cache_merge(const __grid_constant__ CacheAttn A, int cols) {
     wait_for_stream();
+    let_next_launch();
     __shared__ float sm[kMgThreads], sl[kMgThreads], sx[kMgThreads];
     const CacheSplit s = A.split[blockIdx.x];
     if (s.pieces == 0) return;
@@ -312,6 +313,7 @@ constexpr int kWtTokens = 4 * kWtThreads;
 __global__ void __launch_bounds__(kWtThreads)
     k_cache_weights(const __grid_constant__ CacheAttn A) {
     wait_for_stream();
+    let_next_launch();
     __shared__ int slot[kWtTokens / 16];
     __shared__ float lse[128];
     const CacheView &c = A.c;

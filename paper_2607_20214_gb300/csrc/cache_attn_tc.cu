@@ -296,6 +296,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
     tc_fence_after();
     const uint32_t tm = tbase;
     wait_for_stream();
+    let_next_launch();
     Seq own;
     const Start first = divide<kTaThreads>(A, near, own);
     const int count = first.count;
@@ -936,7 +937,6 @@ __global__ void __launch_bounds__(kTaThreads, 2)
             ok = take(i - 1) && ok;
             leave(item - 1);
             ok = named_sync_and(1, 128, ok);
-            if (tid == 0) let_next_launch();
             if (ok) finish(item - 1);
         }
     }

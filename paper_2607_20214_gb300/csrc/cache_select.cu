@@ -305,6 +305,7 @@ __global__ void __launch_bounds__(kScThreads, 2)
     // the other CTAs' shared memory is written only once they run
     if (gridDim.x > 1) cluster_arrive();
     wait_for_stream();
+    let_next_launch();
     // queries, a tile of bounds (rows of 2 D bytes), keys
     extern __shared__ uint4 sq[];
     __shared__ TopkShared<kScThreads> S;
@@ -479,6 +480,7 @@ __global__ void __launch_bounds__(kKpThreads)
                  const float *__restrict__ weight, int keep, int recent,
                  const CacheKept out, int shared_keys) {
     wait_for_stream();
+    let_next_launch();
     extern __shared__ uint32_t own[];
     __shared__ TopkShared<kKpThreads> S;
     const int cs = gridDim.x, rank = blockIdx.x;

@@ -407,6 +407,7 @@ __global__ void __launch_bounds__(kWrThreads, 4)
                     const int32_t *__restrict__ dst_table, int dst_pages,
                     int32_t *__restrict__ lengths_out) {
     wait_for_stream();
+    let_next_launch();
     using G = Page<D, 16>;
     using R = F16Rows;
     __shared__ float tmp[kWrThreads / 32];
