@@ -117,98 +117,127 @@ __device__ __forceinline__ uint32_t abs_max(uint32_t m, const uint32_t *w) {
 template <int D, int E>
 __device__ __forceinline__ float page_max(const Page<D, E> &g, float x,
                                           float *tmp) {
-    for (int o = 1; o < min(g.size, 32); o <<= 1)
-        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+    // x >= 0: its bits are in the same order
+    if (g.size >= 32)
+        x = __uint_as_float(
+            __reduce_max_sync(0xffffffffu, __float_as_uint(x)));
+    else
+        for (int o = 1; o < g.size; o <<= 1)
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
     if (g.size > 32) {
         if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = x;
         __syncthreads();
-        const int w0 = g.index * g.size / 32;
-        for (int w = 0; w < g.size / 32; ++w) x = fmaxf(x, tmp[w0 + w]);
+        const float *at = tmp + g.index * g.size / 32;
+#pragma unroll
+        for (int w = 0; w < kWrThreads / 32; ++w)
+            if (w < g.size / 32) x = fmaxf(x, at[w]);
     }
     return x;
 }
 
-// Bytes of bounds for 4 channels: the extremes' codes (of x f) over 4, rounded
-// outwards, joined with the page's older ones times `drop`. Whole numbers in
-// [-112, 112] (448 / 4), clipped for a channel without a number.
+// Four bytes of bounds: the extremes' codes (of x f) over 4, rounded outwards,
+// joined with the page's older ones times `drop`. sign: 1 for the largest, -1
+// for the smallest. Whole numbers in [-112, 112] (448 / 4), clipped for a
+// channel without a number.
 template <typename R>
-__device__ __forceinline__ void write_bounds(uint32_t *hi_at, uint32_t *lo_at,
-                                             const uint32_t *hi,
-                                             const uint32_t *lo, float f,
-                                             bool had, float drop) {
-    const uint32_t old[2] = {had ? *hi_at : 0u, had ? *lo_at : 0u};
-    uint32_t out[2] = {0, 0};
+__device__ __forceinline__ uint32_t bound_word(const uint32_t *x, float sign,
+                                               float f, bool had,
+                                               uint32_t old, float drop) {
+    uint32_t out = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 h = R::get(hi[i / R::PER]), l = R::get(lo[i / R::PER]);
-        const float2 x = from_e4m3x2(
-            e4m3x2((i & 1 ? h.y : h.x) * f, (i & 1 ? l.y : l.x) * f));
-        float u = ceilf(x.x * 0.25f), v = floorf(x.y * 0.25f);
-        if (had) {
-            u = fmaxf(u, ceilf((float)(int8_t)(old[0] >> 8 * i) * drop));
-            v = fminf(v, floorf((float)(int8_t)(old[1] >> 8 * i) * drop));
+    for (int i = 0; i < 4; i += 2) {
+        const float2 a = R::get(x[i / R::PER]);
+        const float b = R::PER == 2 ? a.y : R::get(x[(i + 1) / R::PER]).x;
+        const float2 c = from_e4m3x2(e4m3x2(a.x * f, b * f));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float u = ceilf((k ? c.y : c.x) * 0.25f * sign);
+            if (had)
+                u = fmaxf(u, ceilf((float)(int8_t)(old >> 8 * (i + k)) * drop *
+                                   sign));
+            out |= ((uint32_t)(int)(u * sign) & 0xffu) << 8 * (i + k);
         }
-        out[0] |= ((uint32_t)(int)u & 0xffu) << 8 * i;
-        out[1] |= ((uint32_t)(int)v & 0xffu) << 8 * i;
     }
-    *hi_at = out[0];
-    *lo_at = out[1];
+    return out;
 }
 
 // The page's channel extremes into its bounds (`bounds`: where the page's
 // begin, or NULL: values, or nothing to write). All threads of the CTA; sh:
-// [warps][C][2 P] words. The threads of a page that share channels write four
-// of them each.
+// [warps][2][D / 4][W] words. The lanes that share channels exchange halves of
+// them, so that each ends with four channels; then two warps of the page, one
+// for the largest and one for the smallest, join the warps' (one warp for both,
+// and whole rows exchanged: a prompt 68 us instead of 65, a step 4.6 instead
+// of 4.0, eviction 31 instead of 29.6).
 template <typename R, int D, int E>
 __device__ __forceinline__ void page_bounds(const Page<D, E> &g, uint32_t *hi,
                                             uint32_t *lo, uint32_t *sh,
                                             int8_t *bounds, float f, bool had,
                                             float drop) {
     constexpr int C = Page<D, E>::C, P = R::P, PARTS = E / 4, W = P / PARTS;
-    static_assert(P * R::PER == E && PARTS <= 32 / C, "channels");
-    const int lane = threadIdx.x & 31;
+    constexpr int N = D / 4;  // words of bounds
+    static_assert(P * R::PER == E && PARTS <= 32 / C && N <= 32, "channels");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // a whole warp without keys has nothing to exchange
-    if (__any_sync(0xffffffffu, bounds != nullptr)) {
-        for (int o = C; o < min(g.size, 32); o <<= 1) {
+    const bool any = __any_sync(0xffffffffu, bounds != nullptr);
+    int o = min(g.size, 32) / 2, part = 0;
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
+    for (int n = P / 2; n >= W; n /= 2, o /= 2) {
+        const bool up = (g.t & o) != 0;
+        part = 2 * part + up;
+        if (any)
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const uint32_t h = up ? hi[i] : hi[n + i];
+                const uint32_t l = up ? lo[i] : lo[n + i];
+                hi[i] = R::max2(up ? hi[n + i] : hi[i],
+                                __shfl_xor_sync(0xffffffffu, h, o));
+                lo[i] = R::min2(up ? lo[n + i] : lo[i],
+                                __shfl_xor_sync(0xffffffffu, l, o));
+            }
+    }
+    const bool writes = bounds && (g.t & (2 * o - 1)) < C;
+    for (; o >= C; o >>= 1)
+        if (any)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
                 hi[i] = R::max2(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
                 lo[i] = R::min2(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
             }
-        }
-    }
-    const int part = (g.size > 32 ? lane : g.t) / C;
-    uint32_t h[W], l[W];
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k)
-        if (k == 0 || part == k)
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                h[i] = hi[k * W + i];
-                l[i] = lo[k * W + i];
-            }
+    const int word = g.ch * PARTS + part;
+    uint32_t *to = (uint32_t *)bounds;
     if (g.size > 32) {
-        uint32_t *at = sh + ((threadIdx.x >> 5) * C + lane % C) * 2 * P;
-        if (part < PARTS)
+        uint32_t *at = sh + warp * 2 * N * W;
+        if (writes)
 #pragma unroll
             for (int i = 0; i < W; ++i) {
-                at[part * W + i] = h[i];
-                at[P + part * W + i] = l[i];
+                at[word * W + i] = hi[i];
+                at[(N + word) * W + i] = lo[i];
             }
+        const bool low = g.t >= 32, mine = bounds && g.t < 64 && lane < N;
+        to += low * N + lane;
+        const uint32_t old = mine && had ? *to : 0u;
         __syncthreads();
-        if (g.t >= 32 || part >= PARTS) return;
-        for (int w = 1; w < g.size / 32; ++w) {
-            at += C * 2 * P;  // the page's next warp
+        if (!mine) return;
+        // the page's first warp
+        const uint32_t *from =
+            sh + (warp - low) * 2 * N * W + (low * N + lane) * W;
+        uint32_t x[W];
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                h[i] = R::max2(h[i], at[part * W + i]);
-                l[i] = R::min2(l[i], at[P + part * W + i]);
-            }
-        }
-    }
-    if (bounds && part < PARTS) {
-        uint32_t *to = (uint32_t *)(bounds + g.ch * E) + part;
-        write_bounds<R>(to, to + D / 4, h, l, f, had, drop);
+        for (int w = 0; w < kWrThreads / 32; ++w)
+            if (w < g.size / 32)
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const uint32_t y = from[w * 2 * N * W + i];
+                    x[i] = w == 0 ? y
+                           : low  ? R::min2(x[i], y)
+                                  : R::max2(x[i], y);
+                }
+        *to = bound_word<R>(x, low ? -1.0f : 1.0f, f, had, old, drop);
+    } else if (writes) {
+        to += word;
+        const uint32_t old[2] = {had ? to[0] : 0u, had ? to[N] : 0u};
+        to[0] = bound_word<R>(hi, 1.0f, f, had, old[0], drop);
+        to[N] = bound_word<R>(lo, -1.0f, f, had, old[1], drop);
     }
 }
 
@@ -441,9 +470,10 @@ __global__ void __launch_bounds__(kWrThreads, 4)
         raw[i] = make_uint4(0, 0, 0, 0);
         ex[i] = 0;
         if (g.row + i * g.step < held && src[i] >= 0) {
-            const size_t sp = (size_t)(src[i] >> shift) * c.Hkv + h;
-            const size_t at = (sp << shift) + (src[i] & (c.ps - 1));
-            raw[i] = *(const uint4 *)(pool + at * D + g.ch * 16);
+            // rows of the pool fit in an int: the host's check
+            const int sp = (src[i] >> shift) * c.Hkv + h;
+            const int at = (sp << shift) + (src[i] & (c.ps - 1));
+            raw[i] = *(const uint4 *)(pool + (size_t)at * D + g.ch * 16);
             ex[i] = __float_as_int(scales[sp]);
         }
     }
@@ -495,7 +525,7 @@ __global__ void __launch_bounds__(kWrThreads, 4)
                         hi[2 * m + 1] = R::max2(hi[2 * m + 1], y);
                         lo[2 * m + 1] = R::min2(lo[2 * m + 1], y);
                     }
-                    o[m] = e4m3x4_of(x, y);
+                    if (k != 0) o[m] = e4m3x4_of(x, y);
                 }
             }
             *(uint4 *)(codes + (size_t)r * D) =
