@@ -75,7 +75,8 @@ inline int cache_tc_cols(int gt) {
 bool cache_attn_tc_supported(const CacheView &c);
 cudaError_t launch_cache_attn_simt(const CacheAttn &A, cudaStream_t st);
 cudaError_t launch_cache_attn_tc(const CacheAttn &A, cudaStream_t st);
-cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st);
+cudaError_t launch_cache_merge(const CacheAttn &A, bool tensor_cores,
+                               cudaStream_t st);
 cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st);
 
 cudaError_t launch_cache_append(const CacheView &c, const void *k,

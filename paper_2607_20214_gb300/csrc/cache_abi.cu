@@ -297,7 +297,7 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
     else
         ELSAA_CACHE_LAUNCH("cache_attn_simt", st,
                            launch_cache_attn_simt(A, st));
-    ELSAA_CACHE_LAUNCH("cache_merge", st, launch_cache_merge(A, st));
+    ELSAA_CACHE_LAUNCH("cache_merge", st, launch_cache_merge(A, tc, st));
     if (weight_out)
         ELSAA_CACHE_LAUNCH("cache_weights", st, launch_cache_weights(A, st));
     return ELSAA_OK;

@@ -235,9 +235,10 @@ int merge_cols(const CacheAttn &A) {
 }
 
 __global__ void __launch_bounds__(kMgThreads)
-    k_cache_merge(const __grid_constant__ CacheAttn A, int cols) {
+    k_cache_merge(const __grid_constant__ CacheAttn A, int cols,
+                  bool tensor_cores) {
     wait_for_stream();
-    let_next_launch();
+    if (tensor_cores) let_next_launch();
     __shared__ float sm[kMgThreads], sl[kMgThreads], sx[kMgThreads];
     const CacheSplit s = A.split[blockIdx.x];
     if (s.pieces == 0) return;
@@ -406,10 +407,12 @@ cudaError_t launch_cache_attn_simt(const CacheAttn &A, cudaStream_t st) {
                                    : launch_simt_d<__nv_bfloat16>(A, st);
 }
 
-cudaError_t launch_cache_merge(const CacheAttn &A, cudaStream_t st) {
+cudaError_t launch_cache_merge(const CacheAttn &A, bool tensor_cores,
+                               cudaStream_t st) {
     const int cols = merge_cols(A);
     return launch_cache<k_cache_merge>(dim3(A.ctas, A.cols / cols),
-                                       kMgThreads, 0, 0, 1, st, A, cols);
+                                       kMgThreads, 0, 0, 1, st, A, cols,
+                                       tensor_cores);
 }
 
 cudaError_t launch_cache_weights(const CacheAttn &A, cudaStream_t st) {

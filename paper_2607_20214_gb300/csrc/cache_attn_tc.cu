@@ -373,9 +373,9 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                     }
                     ++kn;
                 };
-                // the first tiles' K need not wait for the scales (2 sequences
-                // of 300 tokens: 8.8 -> 8.4 us; with V's as well d = 64 lost
-                // that again)
+                // the first tiles' K need not wait for the scales (12 heads of
+                // 700 tokens, d = 64: 8.8 -> 8.4 us; with V's as well long
+                // sequences lost that again)
                 if (i == 0)
                     for (int k = 0; k < min(nt, C::KS); ++k) load_k(k, k);
                 // largest value scale of the lane's tile

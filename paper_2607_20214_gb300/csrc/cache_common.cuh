@@ -47,11 +47,11 @@ cudaError_t launch_cache(dim3 grid, int threads, size_t smem, size_t most,
 }
 
 // The launch behind this one may be set up once every CTA of this one runs: it
-// finds what this one left behind its own wait_for_stream(). Every kernel but
-// two begins with it (one sequence of 16384 tokens: 11.6 -> 11.2 us, page
-// selection with its attention 23.8 -> 23.1, eviction 32.4 -> 31.1); behind
-// k_cache_append and k_cache_attn_simt the waiting CTAs cost more than their
-// start (attention in fp32: 10.2 -> 10.9).
+// finds what this one left behind its own wait_for_stream(). The kernels begin
+// with it (one K/V head of 16384 tokens: 11.6 -> 11.2 us, page selection with
+// its attention 23.8 -> 23.1, eviction 32.4 -> 31.1), except k_cache_append,
+// and k_cache_attn_simt with its merge: behind those the waiting CTAs cost more
+// than their start (append 4.6 -> 4.7, fp32 attention 10.2 -> 10.9).
 __device__ __forceinline__ void let_next_launch() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
