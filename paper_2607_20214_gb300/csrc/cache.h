@@ -50,6 +50,8 @@ struct CacheAttn {
     float *weight_out;       // or NULL: no weights
     int cols, groups;        // columns per group, groups of a head
     int ctas;                // CTAs that share the tiles
+    bool whole;              // no item is shared: an item a CTA
+    unsigned per_t;          // col / T is col * per_t >> 16
     // workspace
     CacheSplit *split;       // [ctas]
     float *part;             // [ctas][2][cols][d + 2]: O, max, sum of pieces
@@ -65,8 +67,26 @@ constexpr int kCacheTcCtas = 152 * 2;
 // CTAs that share the items at most, an item on average: what the merge costs
 // grows with them (128 and 304 were slower).
 constexpr int kCacheMaxPieces = 64;
+// The tensor-core kernel's CTAs take whole items, and nothing is merged, where
+// an item (of the table, or of the pages listed) has kCacheWhole tiles at most,
+// every one finds a CTA, and a CTA gets at most kCacheMore tiles more than it
+// would get of items that are shared. Sharing gives every CTA two beginnings
+// and ends, and the merge is a launch: 8 sequences with 32 heads of 1024 tokens
+// 15.8 us shared, 12.0 whole; 8 with 8 heads, 4 x 5 queries each, 512 tokens
+// 19.0 and 11.2; 12 heads of 700 tokens (6 tiles more) 8.2 and 8.4, with a
+// launch less; 8 heads of 1024 tokens (8 more) 7.9 and 9.8. Behind more than
+// kCacheWholeSeqs sequences (a warp's lanes) the division counts tiles.
+constexpr int kCacheWhole = 16, kCacheMore = 6;
+constexpr int kCacheWholeSeqs = 32;
 inline int cache_simt_cols(int gt) { return gt >= 3 ? 4 : gt; }
-inline int cache_tc_cols(int gt) {
+// A step of 16 columns costs as much as nearly two of 8, whether they are used
+// or not, so 17 to 24 are three groups of 8 as long as the third reading of K
+// and V finds them in L2 (129 MB; `bytes`: what the table can hold): with 20,
+// 8 sequences of 8 heads and 2000 tokens on average 23.5 -> 20.1 us, one of 8192
+// tokens 22.0 -> 17.8; 32 of 8192 tokens (537 MB) 212 and 247.
+constexpr long kCacheRereads = 96L << 20;
+inline int cache_tc_cols(int gt, long bytes) {
+    if (gt > 16 && gt <= 24 && bytes <= kCacheRereads) return 8;
     int n = 1;
     while (n < gt && n < 16) n *= 2;
     return n;

@@ -115,15 +115,17 @@ struct Layout {
 Layout attention_layout(const CacheView &c, bool tc, bool weights) {
     Layout l;
     const int gt = c.G * c.T;
-    l.cols = tc ? cache_tc_cols(gt) : cache_simt_cols(gt);
+    const long heads = (long)c.B * c.Hkv;
+    const long held = heads * c.max_pages * c.ps * 2 * c.d;
+    l.cols = tc ? cache_tc_cols(gt, held) : cache_simt_cols(gt);
     l.groups = (gt + l.cols - 1) / l.cols;
     // no more than the table has tiles for, or than may share the items
     const long tiles =
         ((long)c.max_pages * c.ps + kCacheTile - 1) / kCacheTile;
     const long share = tiles < kCacheMaxPieces ? tiles : kCacheMaxPieces;
-    const long most = (long)c.B * c.Hkv * l.groups * share;
-    l.ctas = tc ? kCacheTcCtas : kCacheSimtCtas;
-    if (most < l.ctas) l.ctas = (int)most;
+    const long full = tc ? kCacheTcCtas : kCacheSimtCtas;
+    const long most = heads * share;  // in one group
+    l.ctas = (int)(most * l.groups < full ? most * l.groups : full);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t was = at;
@@ -132,7 +134,11 @@ Layout attention_layout(const CacheView &c, bool tc, bool weights) {
     };
     l.split = take(sizeof(CacheSplit) * l.ctas);
     l.lse2 = take(sizeof(float) * (size_t)c.B * c.H * c.T);
-    l.part = take(sizeof(float) * 2 * l.ctas * l.cols * (c.d + 2));
+    // a workspace for T tokens serves fewer, which may be one wider group
+    long rows = (long)l.ctas * l.cols;
+    if (tc && gt > 16 && rows < 16 * (most < full ? most : full))
+        rows = 16 * (most < full ? most : full);
+    l.part = take(sizeof(float) * 2 * rows * (c.d + 2));
     l.scores = at;
     if (weights)
         take(sizeof(float) * (size_t)c.B * c.H * c.T * c.max_pages * c.ps);
@@ -177,7 +183,7 @@ extern "C" int elsaa_cache_workspace_size(const elsaa_cache *cache, int T,
     if (rc != ELSAA_OK) return rc;
     if (keep < 0)
         return set_last_error(ELSAA_ERR_INVALID_ARG, "keep must be >= 0");
-    // columns come in powers of two: fewer tokens never need more
+    // fewer tokens never need more
     size_t n =
         attention_layout(c, on_tensor_cores(cache, c), weights != 0).total;
     if (select_bytes(c) > n) n = select_bytes(c);
@@ -284,6 +290,16 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
     A.cols = l.cols;
     A.groups = l.groups;
     A.ctas = l.ctas;
+    const long items = (long)c.B * c.Hkv * l.groups;
+    const long table = (long)c.max_pages * c.ps;
+    const long listed = pages ? (long)n_sel * c.ps : table;
+    const long tiles =
+        ((listed < table ? listed : table) + kCacheTile - 1) / kCacheTile;
+    A.whole = tc && c.B <= kCacheWholeSeqs && items <= kCacheTcCtas &&
+              tiles <= kCacheWhole &&
+              tiles - items * tiles / kCacheTcCtas <= kCacheMore;
+    A.per_t = (65535u + T) / T;
+    if (A.whole) A.ctas = (int)items;
     A.split = (CacheSplit *)(ws + l.split);
     A.part = (float *)(ws + l.part);
     if (weight_out) {
@@ -297,7 +313,8 @@ extern "C" int elsaa_cache_attention(const elsaa_cache *cache, int T,
     else
         ELSAA_CACHE_LAUNCH("cache_attn_simt", st,
                            launch_cache_attn_simt(A, st));
-    ELSAA_CACHE_LAUNCH("cache_merge", st, launch_cache_merge(A, tc, st));
+    if (!A.whole)
+        ELSAA_CACHE_LAUNCH("cache_merge", st, launch_cache_merge(A, tc, st));
     if (weight_out)
         ELSAA_CACHE_LAUNCH("cache_weights", st, launch_cache_weights(A, st));
     return ELSAA_OK;

@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kSaThreads)
                 }
             } else {
                 if (tid == 0) store_lse(A, it.b, it.h, it.n, col, M, L);
-                if (tid < D && col % c.T < it.n)
+                if (tid < D && token_of(A, col) < it.n)
                     store_o(A, query_row(A, it.b, it.h, col), tid,
                             L == 0.0f ? 0.0f : x / L);
             }
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kMgThreads)
     }
     if (part > 0 || col >= c.G * c.T) return;
     if (ch == 0) store_lse(A, s.b, h, s.n, col, M, L);
-    if (col % c.T < s.n)
+    if (token_of(A, col) < s.n)
         store_o(A, query_row(A, s.b, h, col), ch, L == 0.0f ? 0.0f : x / L);
 }
 
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kWtThreads)
     const bool any = n > 0;
     // a column that is no query adds nothing: 2^(s - inf)
     if (any && tid < GT)
-        lse[tid] = tid % c.T < n ? A.lse2[bh * GT + tid] : INFINITY;
+        lse[tid] = token_of(A, tid) < n ? A.lse2[bh * GT + tid] : INFINITY;
     long at = j;
     if (A.pages) {
         // the list entries of this block's pages

@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                     float *at = piece(A, blockIdx.x, last.slot, g) + ch;
                     *(float2 *)at = make_float2(x.x, x.y);
                     *(float2 *)(at + 2) = make_float2(x.z, x.w);
-                } else if ((last.col0 + g) % c.T < last.n) {
+                } else if (token_of(A, last.col0 + g) < last.n) {
                     const float4 w = fin[k & 1][g];
                     const float L = (w.x + w.y) + (w.z + w.w);
                     const float f = L == 0.0f ? 0.0f : 1.0f / L;

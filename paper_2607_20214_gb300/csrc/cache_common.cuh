@@ -211,8 +211,9 @@ __device__ __forceinline__ Seq sequence(const CacheAttn &A, int b) {
 }
 
 constexpr int kItemCost = 3;
-__device__ __forceinline__ int units(const Seq &s) {
-    return s.tiles ? s.tiles + kItemCost : 0;
+// Whole items (A.whole) are a unit each instead, and none is cut.
+__device__ __forceinline__ int units(const CacheAttn &A, int tiles) {
+    return tiles == 0 ? 0 : A.whole ? 1 : tiles + kItemCost;
 }
 
 struct Start {
@@ -232,7 +233,8 @@ struct Cut {
         const unsigned live = (unsigned)items * HC;
         total = (unsigned)sum * HC;
         // no more CTAs than tiles
-        n = min((unsigned)A.ctas, total - live * kItemCost);
+        n = min((unsigned)A.ctas,
+                A.whole ? live : total - live * kItemCost);
         if (live * kCacheMaxPieces < n) n = live * kCacheMaxPieces;
         q = n ? total / n : 0;
         rest = total - q * n;
@@ -249,27 +251,28 @@ struct Cut {
         return k;
     }
 };
-// Unit u in the sequence of the thread that calls, whose units begin at a:
+// Unit u in a sequence with items of n > 0 tiles, whose units begin at a:
 // its item there (HC: the one behind the last), tiles of that item before u,
 // and tiles of all items before u; `before`: those of the sequences before.
 struct Place {
     unsigned hc, off, tiles;
-    __device__ __forceinline__ Place(const Seq &s, unsigned a, unsigned u,
-                                     unsigned before) {
-        const unsigned each = s.tiles + kItemCost, in = u - a;
+    __device__ __forceinline__ Place(const CacheAttn &A, int n, unsigned a,
+                                     unsigned u, unsigned before) {
+        const unsigned each = units(A, n), in = u - a;
         hc = in / each;
         const unsigned r = in - hc * each;
         off = r > kItemCost ? r - kItemCost : 0;
-        tiles = before + hc * s.tiles + off;
+        tiles = before + hc * n + off;
     }
 };
 // The item that goes on behind the range, if it begins in it: the thread's
 // sequence has the range's end u1 (a < u1 <= its end), the range begins at u0.
-__device__ __forceinline__ CacheSplit split_in(const Cut &cut, int b,
+__device__ __forceinline__ CacheSplit split_in(const CacheAttn &A,
+                                               const Cut &cut, int b,
                                                const Seq &s, unsigned a,
                                                unsigned u0, unsigned u1) {
-    const Place end(s, a, u1, 0);
-    const unsigned each = s.tiles + kItemCost, i0 = a + end.hc * each;
+    const Place end(A, s.tiles, a, u1, 0);
+    const unsigned each = units(A, s.tiles), i0 = a + end.hc * each;
     // its first tile is unit i0 + kItemCost; a range that begins before it
     // begins the item
     if (end.off == 0 || u0 > i0 + kItemCost) return {0, 0, 0, 0};
@@ -305,7 +308,7 @@ __device__ __noinline__ Start divide_many(const CacheAttn &A, Seq *near) {
         own = {0, 0, 0, 0};
         if (b < c.B) own = sequence(A, b);
         const int live = __popc(__ballot_sync(0xffffffffu, own.tiles > 0));
-        int x = upto_lane(units(own));
+        int x = upto_lane(units(A, own.tiles));
         done = upto_lane(own.tiles);
         __syncthreads();  // the round before has read
         if (lane == 31) {
@@ -340,16 +343,16 @@ __device__ __noinline__ Start divide_many(const CacheAttn &A, Seq *near) {
     for (int r = 0; r < rounds && k < cut.n; ++r) {
         if (rounds > 1) upto = sum(r);
         const unsigned z = (unsigned)(base + upto) * HC;
-        const unsigned a = z - (unsigned)units(own) * HC;
+        const unsigned a = z - (unsigned)units(A, own.tiles) * HC;
         const unsigned before = (unsigned)(tiles + done - own.tiles) * HC;
         const int b = r * NT + tid;
         if (a <= u0 && u0 < z) {
-            const Place p(own, a, u0, before);
+            const Place p(A, own.tiles, a, u0, before);
             mine = {b, (int)p.hc, (int)p.off, (int)p.tiles};
         }
         if (a < u1 && u1 <= z) {
-            to = (int)Place(own, a, u1, before).tiles;
-            A.split[k] = split_in(cut, b, own, a, u0, u1);
+            to = (int)Place(A, own.tiles, a, u1, before).tiles;
+            A.split[k] = split_in(A, cut, b, own, a, u0, u1);
         }
         if (rounds > 1)
             for (int w = 0; w < NT / 32; ++w) {
@@ -376,7 +379,7 @@ __device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near,
     if (c.B > 32) return divide_many<NT>(A, near);
     const int lane = threadIdx.x & 31, HC = c.Hkv * A.groups;
     if (lane < c.B) own = sequence(A, lane);
-    const int upto = upto_lane(units(own));
+    const int upto = upto_lane(units(A, own.tiles));
     const int done = upto_lane(own.tiles);
     const Cut cut(A, __shfl_sync(0xffffffffu, upto, 31),
                   __popc(__ballot_sync(0xffffffffu, own.tiles > 0)));
@@ -386,14 +389,15 @@ __device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near,
         return {0, 0, 0, 0};
     }
     const unsigned u0 = cut.at(k), u1 = cut.at(k + 1);
-    const unsigned z = (unsigned)upto * HC, a = z - (unsigned)units(own) * HC;
+    const unsigned z = (unsigned)upto * HC;
+    const unsigned a = z - (unsigned)units(A, own.tiles) * HC;
     const unsigned before = (unsigned)(done - own.tiles) * HC;
     if (threadIdx.x < 32 && a < u1 && u1 <= z)
-        A.split[k] = split_in(cut, lane, own, a, u0, u1);
+        A.split[k] = split_in(A, cut, lane, own, a, u0, u1);
     // every lane evaluates both ends in the sequence that has them
     auto place = [&](unsigned u, int b) {
-        const Seq s = {0, 0, 0, __shfl_sync(0xffffffffu, own.tiles, b)};
-        return Place(s, __shfl_sync(0xffffffffu, a, b), u,
+        return Place(A, __shfl_sync(0xffffffffu, own.tiles, b),
+                     __shfl_sync(0xffffffffu, a, b), u,
                      __shfl_sync(0xffffffffu, before, b));
     };
     const int b0 = __ffs(__ballot_sync(0xffffffffu, a <= u0 && u0 < z)) - 1;
@@ -450,11 +454,16 @@ struct Walk {
     }
 };
 
+// The new token of column `col` < 128 (T at most 64: the product's error stays
+// below 1 / T).
+__device__ __forceinline__ int token_of(const CacheAttn &A, int col) {
+    return col - A.c.T * (int)((unsigned)col * A.per_t >> 16);
+}
 // The last position that column `col` (g T + t) of an item sees, -1 if none
 // or if the column is no query.
 __device__ __forceinline__ int last_seen(const CacheAttn &A, int len, int n,
                                          int col) {
-    const int t = col % A.c.T;
+    const int t = token_of(A, col);
     return t < n ? len - n + t : -1;
 }
 // Row of q, o and lse of column `col`: a head's columns lie side by side.
@@ -481,7 +490,7 @@ __device__ __forceinline__ void store_lse(const CacheAttn &A, int b, int h,
     const float l2 = l == 0.0f ? -INFINITY : m + log2f(l);
     if (A.lse2)
         A.lse2[((size_t)b * A.c.Hkv + h) * A.c.G * A.c.T + col] = l2;
-    if (A.lse && col % A.c.T < n)
+    if (A.lse && token_of(A, col) < n)
         A.lse[query_row(A, b, h, col)] = l2 * 0.6931471805599453f;
 }
 

@@ -156,3 +156,19 @@ def test_binding_checks_shapes():
     with pytest.raises(ValueError, match="CUDA"):
         E.make_cache(*[torch.zeros((2, 1, 16, 32), dtype=torch.uint8)] * 2,
                      None, None, None, torch.zeros((1, 1)), None)
+
+
+@pytest.mark.parametrize("impl", [0, 1])
+@pytest.mark.parametrize("B,H,H_kv,max_pages", [
+    (1, 1, 1, 1), (1, 4, 1, 7), (2, 8, 2, 40), (8, 8, 8, 3), (40, 16, 8, 64),
+    (3, 24, 3, 2000), (9, 20, 4, 1), (33, 12, 12, 2)])
+def test_a_workspace_serves_fewer_tokens_too(lib, impl, B, H, H_kv,
+                                             max_pages):
+    """Whatever groups the columns of a smaller call come in."""
+    for d in (64, 128):
+        for weights in (False, True):
+            sizes = [E.elsaa_cache_workspace_size(
+                cache(B=B, H=H, H_kv=H_kv, max_pages=max_pages, d_h=d,
+                      impl=impl), T, weights)
+                for T in range(1, min(64, 128 * H_kv // H) + 1)]
+            assert sizes == sorted(sizes)

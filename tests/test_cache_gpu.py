@@ -716,14 +716,14 @@ def test_two_graphs_share_a_workspace_and_two_streams_do_not():
 
 
 def test_the_timing_tool_names_the_cache_kernels():
-    case = Case([500], 4, 2, 64, 32, seed=22)
+    case = Case([2000], 4, 2, 64, 32, seed=22)
     cache = case.device(E)
     _, q = case.rows(4, 1)
     _, k = case.rows(2, 1)
     w = torch.zeros((1, 2, case.max_pages * 32), device="cuda")
     E.elsaa_profile_start()
     E.elsaa_cache_append(cache, k, k)
-    pages = E.elsaa_cache_select(cache, q, 4)
+    pages = E.elsaa_cache_select(cache, q, 40)
     E.elsaa_cache_attention(cache, q, pages=pages, weight_out=w)
     E.elsaa_cache_evict(cache, w, 32, 1, int_tensor([[case.free[0]]]))
     got = E.elsaa_profile_stop()
@@ -815,3 +815,24 @@ def test_a_cache_of_another_device_is_refused(monkeypatch):
                                              workspace=ws)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("T,G,ps", [(5, 4, 16), (17, 1, 64), (6, 4, 128),
+                                    (9, 2, 32)])
+@pytest.mark.parametrize("lengths", [[700, 90, 0], [6000, 33]])
+def test_attention_in_three_groups_of_columns(T, G, ps, lengths, weights):
+    """17 to 24 queries a head, in whole items and in shared ones."""
+    run_attention(Case(lengths, 2 * G, 2, 128, ps, seed=T), T=T,
+                  weights=weights)
+
+
+@pytest.mark.parametrize("B,H,hkv,n", [(32, 9, 9, 500), (32, 10, 10, 500),
+                                       (31, 2, 2, 2040), (2, 1, 1, 900),
+                                       (2, 1, 1, 500), (33, 4, 2, 500)])
+def test_attention_on_both_sides_of_whole_items(B, H, hkv, n):
+    """A CTA an item; more items than CTAs; items too long; more sequences
+    than a warp has lanes."""
+    g = np.random.default_rng(n + B)
+    lengths = [n] + [int(x) for x in g.integers(0, n, B - 1)]
+    run_attention(Case(lengths, H, hkv, 64, 64, seed=B, spare=0))
