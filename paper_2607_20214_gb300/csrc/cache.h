@@ -64,7 +64,7 @@ struct CacheAttn {
 // one walks at a time.
 constexpr int kCacheSimtCtas = 152 * 3;
 constexpr int kCacheTcCtas = 152 * 2;
-// CTAs that share the items at most, an item on average: what the merge costs
+// CTAs per shared item at most, on average over the items: the merge's cost
 // grows with them (128 and 304 were slower).
 constexpr int kCacheMaxPieces = 64;
 // The tensor-core kernel's CTAs take whole items, and nothing is merged, where

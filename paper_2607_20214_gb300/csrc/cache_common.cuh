@@ -188,9 +188,10 @@ __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *x) {
 // ranges of equal tiles, whose slowest CTA had six items. So the units tiles +
 // kItemCost of all items, one after the other, are cut into equal ranges, one
 // per CTA; an item that a cut crosses is written as pieces and merged
-// afterwards. Every
-// CTA finds its range by itself from the lengths: a launch that did it for all
-// cost more than the B loads and the scan.
+// afterwards. Every CTA finds its range by itself from the lengths: a launch
+// that did it for all cost more than the B loads and the scan. (Cuts at whole
+// steps of two tiles only were a wash: 8 heads of 1024 tokens 8.9 -> 8.5 us, 32
+// of 16384 tokens 30.1 -> 30.4.)
 
 // What a sequence's heads walk.
 struct Seq {
