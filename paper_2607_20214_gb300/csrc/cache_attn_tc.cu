@@ -33,6 +33,12 @@
 // walked. The range's tiles run through rings of K and V buffers; S of tile
 // i + 1 is issued before O of tile i, so the softmax finds its next scores
 // ready. Two CTAs share an SM.
+//
+// Measured with the merge: 16 sequences, 8 heads of 128, 4 queries a head,
+// 65536 tokens 324 us (6.6 TB/s, 0.98 of a copy); 2 x 16 heads of 16384 tokens
+// 30 us, of which 24 at 5.6 TB/s, the rest its start (lengths, table, first
+// tile: 5000 cycles) and the merge. From 16 columns on the softmax's arithmetic
+// bounds it, 2000 cycles a tile.
 #include <limits.h>
 
 #include "cache_common.cuh"
@@ -973,11 +979,11 @@ cudaError_t launch_cols(const CacheAttn &A, cudaStream_t st) {
 
 }  // namespace
 
-// Whatever the size: the CUDA cores are faster in caches of one tile only
-// (bf16, one query a head, one sequence of 40 tokens: 6.0 us against 6.5),
-// where setting up tensor memory and barriers shows; 2 sequences of 300 tokens
-// take 8.7 us here and 9.8 there, with 4 queries a head 9.1 and 14.8, 16
-// sequences of 4096 tokens 32 and 42.
+// Whatever the size: the CUDA cores are faster in the smallest caches only
+// (bf16, a head of 64 with 16 tokens: 4.8 us against 5.3), where setting up
+// tensor memory and barriers shows; 8 heads of 40 tokens take 5.3 us here and
+// 5.9 there, 2 sequences with 8 heads of 300 tokens 6.7 and 9.7, with 4 queries
+// a head 7.0 and 14.7, 16 sequences of 4096 tokens 30 and 42.
 bool cache_attn_tc_supported(const CacheView &c) {
     return c.dtype == ELSAA_BF16 && (c.d == 64 || c.d == 128);
 }

@@ -237,10 +237,12 @@ __device__ __forceinline__ void write_selected(K key, int n, uint32_t thr,
 //
 // A cluster per sequence and head: its CTAs score the pages, kScPages at a
 // time, and leave the keys in the first CTA's shared memory, which selects.
-// One launch; with the keys in HBM between two it was 10 us longer. The bounds
-// of a page are 2 d neighbouring bytes: they come by 16-byte asynchronous
-// copies, so that a warp reads whole lines (a page a thread, straight into
-// registers, took 7000 cycles for 512 pages instead of 2000).
+// One launch, 9 us for 1024 pages of 64 heads of 128 (17 MB: dependent loads,
+// the cluster's barrier and the counting bound it); with the keys in HBM
+// between two launches it was 10 us longer. The bounds of a page are 2 d
+// neighbouring bytes: they come by 16-byte asynchronous copies, so that a warp
+// reads whole lines (a page a thread, straight into registers, took 7000
+// cycles for 512 pages instead of 2000).
 //
 // The sums are small matrix products (16 pages x 8 queries x 2 d) of fp16
 // numbers, which hold 8-bit ones and add up exactly in fp32: 4-byte integer
@@ -471,7 +473,8 @@ __global__ void __launch_bounds__(kScThreads, 2)
 // cycles a pass, as much as the keys of 16384 tokens by itself, so only longer
 // rows are shared. The weights are read once, as many at a time as
 // there are registers for, and their keys kept in shared memory (up to
-// kKpShared a CTA; longer runs are read again by every pass).
+// kKpShared a CTA; longer runs are read again by every pass). 32 rows of 16384
+// weights take 13 us, a chain of barriers and dependent shared-memory reads.
 constexpr int kKpThreads = 1024;
 constexpr int kKpShared = 49152;
 
