@@ -82,8 +82,8 @@ inline int cache_simt_cols(int gt) { return gt >= 3 ? 4 : gt; }
 // A step of 16 columns costs as much as nearly two of 8, whether they are used
 // or not, so 17 to 24 are three groups of 8 as long as the third reading of K
 // and V finds them in L2 (129 MB; `bytes`: what the table can hold): with 20,
-// 8 sequences of 8 heads and 2000 tokens on average 23.5 -> 20.1 us, one of 8192
-// tokens 22.0 -> 17.8; 32 of 8192 tokens (537 MB) 212 and 247.
+// 8 sequences of 8 heads and 2000 tokens on average 23.5 -> 20.1 us, one of
+// 8192 tokens 22.0 -> 17.8; 32 of 8192 tokens (537 MB) 212 and 247.
 constexpr long kCacheRereads = 96L << 20;
 inline int cache_tc_cols(int gt, long bytes) {
     if (gt > 16 && gt <= 24 && bytes <= kCacheRereads) return 8;
