@@ -4,6 +4,7 @@
 #pragma once
 
 #include "../../include/elsaa_cache.h"
+#include "cache_division.h"
 #include "internal.h"
 
 namespace elsaa {
@@ -64,9 +65,6 @@ struct CacheAttn {
 // one walks at a time.
 constexpr int kCacheSimtCtas = 152 * 3;
 constexpr int kCacheTcCtas = 152 * 2;
-// CTAs per shared item at most, on average over the items: the merge's cost
-// grows with them (128 and 304 were slower).
-constexpr int kCacheMaxPieces = 64;
 // The tensor-core kernel's CTAs take whole items, and nothing is merged, where
 // an item (of the table, or of the pages listed) has kCacheWhole tiles at most,
 // every one finds a CTA, and a CTA gets at most kCacheMore tiles more than it

@@ -5,6 +5,7 @@
 #include <atomic>
 
 #include "cache.h"
+#include "cache_division.h"
 #include "device_common.cuh"
 #include "tc_common.cuh"
 
@@ -211,7 +212,6 @@ __device__ __forceinline__ Seq sequence(const CacheAttn &A, int b) {
     return s;
 }
 
-constexpr int kItemCost = 3;
 // Whole items (A.whole) are a unit each instead, and none is cut.
 __device__ __forceinline__ int units(const CacheAttn &A, int tiles) {
     return tiles == 0 ? 0 : A.whole ? 1 : tiles + kItemCost;
@@ -225,33 +225,12 @@ struct Start {
 // The sequences from the CTA's first on, as far as they fit.
 constexpr int kNearSeqs = 32;
 
-// The units of CTA k of n, total / n or one more, without a product that needs
-// 64 bits; the host has checked that total fits.
-struct Cut {
-    unsigned total, n, q, rest;
-    __device__ __forceinline__ Cut(const CacheAttn &A, int sum, int items) {
-        const int HC = A.c.Hkv * A.groups;
-        const unsigned live = (unsigned)items * HC;
-        total = (unsigned)sum * HC;
-        // no more CTAs than tiles
-        n = min((unsigned)A.ctas,
-                A.whole ? live : total - live * kItemCost);
-        if (live * kCacheMaxPieces < n) n = live * kCacheMaxPieces;
-        q = n ? total / n : 0;
-        rest = total - q * n;
-    }
-    __device__ __forceinline__ unsigned at(unsigned k) const {
-        return q * k + rest * k / n;
-    }
-    // the CTA that has unit u
-    __device__ __forceinline__ unsigned owner(unsigned u) const {
-        unsigned k = min((unsigned)((float)u * ((float)n / (float)total)),
-                         n - 1);
-        while (k > 0 && at(k) > u) --k;
-        while (at(k + 1) <= u) ++k;
-        return k;
-    }
-};
+// The cuts of a call whose sequences have `sum` units in all for each of their
+// items, `items` of them some.
+__device__ __forceinline__ Cut cuts(const CacheAttn &A, int sum, int items) {
+    return Cut((unsigned)sum, (unsigned)items,
+               (unsigned)(A.c.Hkv * A.groups), (unsigned)A.ctas, A.whole);
+}
 // Unit u in a sequence with items of n > 0 tiles, whose units begin at a:
 // its item there (HC: the one behind the last), tiles of that item before u,
 // and tiles of all items before u; `before`: those of the sequences before.
@@ -336,7 +315,7 @@ __device__ __noinline__ Start divide_many(const CacheAttn &A, Seq *near) {
             items += some[w];
         }
     }
-    const Cut cut(A, total, items);
+    const Cut cut = cuts(A, total, items);
     const unsigned k = blockIdx.x;
     const unsigned u0 = k < cut.n ? cut.at(k) : 0;
     const unsigned u1 = k < cut.n ? cut.at(k + 1) : 0;
@@ -382,8 +361,8 @@ __device__ __forceinline__ Start divide(const CacheAttn &A, Seq *near,
     if (lane < c.B) own = sequence(A, lane);
     const int upto = upto_lane(units(A, own.tiles));
     const int done = upto_lane(own.tiles);
-    const Cut cut(A, __shfl_sync(0xffffffffu, upto, 31),
-                  __popc(__ballot_sync(0xffffffffu, own.tiles > 0)));
+    const Cut cut = cuts(A, __shfl_sync(0xffffffffu, upto, 31),
+                         __popc(__ballot_sync(0xffffffffu, own.tiles > 0)));
     const unsigned k = blockIdx.x;
     if (k >= cut.n) {
         if (threadIdx.x == 0) A.split[k] = {0, 0, 0, 0};

@@ -1,0 +1,129 @@
+"""The cache operators on the GPU at the edges of their definitions, against
+the 64-bit oracle (oracle/cache.py).
+
+Bounds of O and lse. A score is a sum of d fp32 products and a few more
+roundings: at most (d + 8) 2^-24 of sum_i |q_i k_i| scale off, with 2^-21 for
+the power of two and its argument; a weight is off by that share e. A sum over
+the tokens has fewer than `depth` additions one after the other, for O and for
+the weights each: a lane of the CUDA-core kernel adds 16 tokens of a tile of
+128, then come the warp's rows (5 steps), four warps and the item's pieces (64
+on average at most; a long one of few items has more, and its tests state
+them). So O, a mean of values, is off by (2 e + 2 depth 2^-24) max|v| and half
+a step of its type, lse by e + depth 2^-24 + 2^-22 |lse|. Only the tensor-core
+kernel rounds a weight to fp16: 2^-11 of it, and 2^-18 in all for the pieces.
+"""
+import numpy as np
+import pytest
+import torch
+
+from cache_cases import NAN, Case, int_tensor
+from oracle import cache as oc
+from paper_2607_20214_gb300 import build
+from paper_2607_20214_gb300 import elsaa as E
+
+pytestmark = pytest.mark.gpu
+
+IMPL = [pytest.param(0, id="auto"), pytest.param(1, id="simt")]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build()
+    E.load_library()
+
+
+def on_tensor_cores(case, impl):
+    return impl == 0 and case.dtype == "bf16" and case.d in (64, 128)
+
+
+def bounds_of(case, ref, impl):
+    """(bound of O without its type's rounding, bound of lse, of a weight)."""
+    size, vmax = ref[3], ref[4]
+    e = (case.d + 8) * 2.0 ** -24 * size + 2.0 ** -21
+    depth = 16 * (-(-int(max(case.c["lengths"])) // 128)) + 80
+    tol = (2 * e + 2 * depth * 2.0 ** -24) * vmax
+    if on_tensor_cores(case, impl):
+        tol = tol + (2.0 ** -11 + 2.0 ** -18) * vmax
+    return tol, e + depth * 2.0 ** -24, e.max() + 2 * depth * 2.0 ** -24
+
+
+def check(case, o, lse, ref, new, impl=0):
+    half = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}[case.dtype]
+    tol, el, _ = bounds_of(case, ref, impl)
+    o, lse = o.double().cpu().numpy(), lse.double().cpu().numpy()
+    for b in range(case.B):
+        n = new[b]
+        ro, rl = ref[0][b, :, :n], ref[1][b, :, :n]
+        empty = np.isneginf(rl)
+        assert np.array_equal(np.isneginf(lse[b, :, :n]), empty)
+        assert np.all(o[b, :, :n][empty] == 0)
+        lim = tol[b, :, :n, None] + half * np.abs(ro)
+        assert np.all(np.abs(o[b, :, :n] - ro) <= lim), b
+        some = ~empty
+        lim = (el[b, :, :n] + 2.0 ** -22 * np.abs(rl))[some]
+        assert np.all(np.abs(lse[b, :, :n] - rl)[some] <= lim), b
+
+
+def attend(case, q, qd, new, impl, pages=None, scale=0.0, weights=False):
+    """Runs the call and checks all that it writes."""
+    T = qd.shape[2]
+    cache = case.device(E, impl, scale=scale)
+    o = torch.full_like(qd, 7.0)
+    lse = torch.full((case.B, case.H, T), 7.0, device="cuda")
+    win = wout = None
+    if weights:
+        slots = case.max_pages * case.ps
+        win = torch.rand((case.B, case.hkv, slots), device="cuda")
+        wout = torch.full_like(win, -3.0)
+    ws = torch.full((E.elsaa_cache_workspace_size(cache, T, weights),), 0xC7,
+                    dtype=torch.uint8, device="cuda")
+    E.elsaa_cache_attention(
+        cache, qd, pages=None if pages is None else int_tensor(pages), o=o,
+        lse=lse, weight_in=win, weight_out=wout, new_len=int_tensor(new),
+        workspace=ws)
+    E.elsaa_check_status(cache.tensors["status"])
+    ref = oc.attention(case.c, q, new, scale or case.d ** -0.5, pages)
+    check(case, o, lse, ref, new, impl)
+    for b, n in enumerate(new):
+        assert (o[b, :, n:] == 7).all() and (lse[b, :, n:] == 7).all()
+    if weights:
+        e = bounds_of(case, ref, impl)[2]
+        GT = case.H // case.hkv * T
+        got, w0 = wout.double().cpu().numpy(), win.double().cpu().numpy()
+        for b, n in enumerate(case.c["lengths"]):
+            want = (w0[b] + ref[2][b])[:, :n]
+            lim = 2 * e * ref[2][b][:, :n] + (GT + 1) * 2.0 ** -24 * want
+            assert np.all(np.abs(got[b][:, :n] - want) <= lim), b
+            assert np.all(got[b][:, n:] == -3.0)
+
+
+@pytest.mark.parametrize("impl", IMPL)
+def test_attention_with_the_most_heads(impl):
+    """2^26 items, one key each: their number times the CTAs that may share
+    one does not fit in 32 bits. O is the key's value."""
+    B, H, d, ps = 4096, 16384, 64, 16
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough memory")
+    cache = E.new_cache(B, H, H, d, ps, 1, 1, impl=impl)
+    t = cache.tensors
+    gen = torch.Generator(device="cuda").manual_seed(40)
+    t["page_table"].zero_()
+    t["lengths"].fill_(1)
+    v = torch.randn((1, H, ps, d), generator=gen, device="cuda")
+    t["v"].copy_(v)
+    t["k"].copy_(v)
+    t["v_scale"].fill_(0.25)
+    q = torch.empty((B, H, 1, d), dtype=torch.bfloat16, device="cuda")
+    q.normal_(generator=gen)
+    o = torch.full_like(q, 7.0)
+    lse = torch.full((B, H, 1), 7.0, device="cuda")
+    E.elsaa_cache_attention(cache, q, o=o, lse=lse)
+    E.elsaa_check_status(t["status"])
+    want = (t["v"][0, :, :1].float() * 0.25).to(torch.bfloat16)  # [H, 1, d]
+    key = t["k"][0, :, 0].float()
+    for b in range(0, B, 256):
+        assert (o[b:b + 256] == want).all()
+        x = q[b:b + 256, :, 0].float() * key
+        s, size = x.sum(2) / 8, x.abs().sum(2) / 8
+        assert ((lse[b:b + 256, :, 0] - s).abs() <=
+                3 * (d + 8) * 2.0 ** -24 * size + 2.0 ** -21).all()
