@@ -46,7 +46,8 @@ typedef struct elsaa_cache {
                         elsaa_cache_append, of the queries and of O          */
     int page_size;   /* tokens per page: 16, 32, 64 or 128                   */
     int num_pages;   /* pages of the pool                                    */
-    int max_pages;   /* entries of a page-table row                          */
+    int max_pages;   /* entries of a page-table row; max_pages * page_size at
+                        most 2^31 - 2^16                                     */
     float scale;     /* score scale; 0 -> 1/sqrt(d_h)                        */
     int impl;        /* ELSAA_IMPL_AUTO or ELSAA_IMPL_SIMT                   */
     void *k, *v;     /* [num_pages, H_kv, page_size, d_h] e4m3 codes,

@@ -16,6 +16,9 @@ constexpr int kQueryExpLow = -60;
 constexpr int kCacheTile = 128;
 // Sequences of a call: every CTA of the attention kernels reads all lengths.
 constexpr int kCacheMaxB = 4096;
+// Tokens that a table row may hold: positions are ints, and the kernels' loops
+// and tiles step beyond the last one, by 8192 at most.
+constexpr long kCacheMaxSlots = (1L << 31) - (1L << 16);
 // In-band status codes and sites of the cache kernels.
 constexpr int kDevCachePage = 5;    // a page outside the pool was skipped
 constexpr int kDevCacheLength = 6;  // a length outside the table was clipped

@@ -51,8 +51,8 @@ int make_view(const elsaa_cache *p, int T, CacheView *v) {
         return no("page_size must be 16, 32, 64 or 128");
     if (p->B > kCacheMaxB) return no("B must be at most 4096");
     if (p->H > 65535) return no("H must be at most 65535");
-    if ((long)p->max_pages * p->page_size > 0x7fffffffL)
-        return no("max_pages * page_size must fit in int32");
+    if ((long)p->max_pages * p->page_size > kCacheMaxSlots)
+        return no("max_pages * page_size must be at most 2^31 - 2^16");
     if ((long)p->num_pages * p->H_kv > 0x7fffffffL / p->page_size)
         return no("num_pages * H_kv * page_size must fit in int32");
     if (!p->k || !p->v || !p->k_scale || !p->v_scale || !p->bounds ||

@@ -1,0 +1,33 @@
+"""The cache operators at the largest sizes: what the kernels' 32-bit positions
+do not hold is refused on the host (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from paper_2607_20214_gb300 import build
+from paper_2607_20214_gb300 import elsaa as E
+from test_cache_abi import cache, calls
+
+UNS, WS = E.ELSAA_ERR_UNSUPPORTED, E.ELSAA_ERR_WORKSPACE
+MOST = 2 ** 31 - 2 ** 16
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return E.load_library()
+
+
+@pytest.mark.parametrize("ps", [16, 32, 64, 128])
+def test_tables_of_nearly_2_31_tokens_are_refused_everywhere(lib, ps):
+    for pages in (2 ** 31 // ps - 1, MOST // ps + 1):
+        c = cache(max_pages=pages, page_size=ps, H=2, H_kv=2, B=1)
+        for name, call in calls(lib, c).items():
+            assert call() == UNS, name
+            assert "max_pages * page_size" in E.elsaa_last_error(), name
+    # one page fewer: the next check speaks
+    c = cache(max_pages=MOST // ps, page_size=ps, H=2, H_kv=2, B=1)
+    for name, call in calls(lib, c, ws=None, keep=16).items():
+        if name in ("select", "attention", "evict"):
+            assert call() == WS, name
+    assert calls(lib, c)["size"]() == E.ELSAA_OK
