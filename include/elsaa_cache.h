@@ -161,10 +161,10 @@ int elsaa_cache_attention(const elsaa_cache *cache, int T, const void *q,
                           void *stream);
 
 /*
- * Cuts every sequence to at most `keep` tokens, for each K/V head its own:
- * the last `recent` ones (recent <= keep), and of the others those of largest
- * weight (equal: lower position; NaN below every number). They keep their
- * order.
+ * Cuts every sequence to at most `keep` tokens (keep <= 2^31 - 2^16), for each
+ * K/V head its own: the last `recent` ones (recent <= keep), and of the others
+ * those of largest weight (equal: lower position; NaN below every number).
+ * They keep their order.
  *
  * weight     [B, H_kv, max_pages * page_size] fp32, as accumulated by
  *            elsaa_cache_attention.

@@ -106,6 +106,13 @@ int check_queries(const CacheView &c) {
     return ELSAA_OK;
 }
 
+int check_keep(int keep) {
+    if (keep > kCacheMaxSlots)
+        return set_last_error(ELSAA_ERR_UNSUPPORTED,
+                              "keep must be at most 2^31 - 2^16");
+    return ELSAA_OK;
+}
+
 // Workspace of one call: split items | lse2 | pieces | scores (attention), or
 // page keys (select), or counts | pool rows (evict).
 struct Layout {
@@ -183,6 +190,8 @@ extern "C" int elsaa_cache_workspace_size(const elsaa_cache *cache, int T,
     if (rc != ELSAA_OK) return rc;
     if (keep < 0)
         return set_last_error(ELSAA_ERR_INVALID_ARG, "keep must be >= 0");
+    rc = check_keep(keep);
+    if (rc != ELSAA_OK) return rc;
     // fewer tokens never need more
     size_t n =
         attention_layout(c, on_tensor_cores(cache, c), weights != 0).total;
@@ -340,6 +349,8 @@ extern "C" int elsaa_cache_evict(const elsaa_cache *cache,
     if (keep <= 0 || recent < 0 || recent > keep)
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "keep must be positive and recent in [0, keep]");
+    rc = check_keep(keep);
+    if (rc != ELSAA_OK) return rc;
     if (dst_pages <= 0 || (long)dst_pages * c.ps < keep)
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "dst_pages * page_size must be at least keep");

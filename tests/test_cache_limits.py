@@ -31,3 +31,14 @@ def test_tables_of_nearly_2_31_tokens_are_refused_everywhere(lib, ps):
         if name in ("select", "attention", "evict"):
             assert call() == WS, name
     assert calls(lib, c)["size"]() == E.ELSAA_OK
+
+
+def test_eviction_to_nearly_2_31_tokens_is_refused(lib):
+    for keep in (2 ** 31 - 1, MOST + 1):
+        c = calls(lib, cache(), keep=keep, dst_pages=2 ** 31 - 1)
+        for name in ("size", "evict"):
+            assert c[name]() == UNS, name
+            assert "keep" in E.elsaa_last_error(), name
+    c = calls(lib, cache(), keep=MOST, dst_pages=2 ** 31 - 1, ws=None)
+    assert c["size"]() == E.ELSAA_OK
+    assert c["evict"]() == WS
