@@ -120,6 +120,7 @@ int elsaa_cache_append(const elsaa_cache *cache, int T, const void *k,
  * Taken are the first `first` pages, the last `last` and then those of
  * largest u (equal: lower p), n_sel in all or as many as the sequence has; a
  * sequence with n_b = 0 gets none. first, last >= 0 and first + last <= n_sel.
+ * n_sel * page_size <= 2^31 - 2^16.
  */
 int elsaa_cache_select(const elsaa_cache *cache, int T, const void *q,
                        const int32_t *new_len, int n_sel, int first, int last,

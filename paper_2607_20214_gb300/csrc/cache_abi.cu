@@ -243,6 +243,9 @@ extern "C" int elsaa_cache_select(const elsaa_cache *cache, int T,
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "n_sel must be positive, first and last >= 0 "
                               "and first + last at most n_sel");
+    if (n_sel > kCacheMaxSlots / c.ps)
+        return set_last_error(ELSAA_ERR_UNSUPPORTED,
+                              "n_sel * page_size must be at most 2^31 - 2^16");
     rc = check_workspace(workspace, workspace_bytes, select_bytes(c));
     if (rc != ELSAA_OK) return rc;
     c.new_len = new_len;

@@ -42,3 +42,13 @@ def test_eviction_to_nearly_2_31_tokens_is_refused(lib):
     c = calls(lib, cache(), keep=MOST, dst_pages=2 ** 31 - 1, ws=None)
     assert c["size"]() == E.ELSAA_OK
     assert c["evict"]() == WS
+
+
+@pytest.mark.parametrize("ps", [16, 128])
+def test_selecting_nearly_2_31_pages_is_refused(lib, ps):
+    for n_sel in (2 ** 31 - 1, MOST // ps + 1):
+        c = calls(lib, cache(page_size=ps), n_sel=n_sel)
+        assert c["select"]() == UNS
+        assert "n_sel" in E.elsaa_last_error()
+    c = calls(lib, cache(page_size=ps), n_sel=MOST // ps, ws=None)
+    assert c["select"]() == WS
