@@ -82,7 +82,8 @@ int elsaa_cache_workspace_size(const elsaa_cache *cache, int T, int weights,
 /*
  * Writes the newest tokens' rows into their pages.
  *
- * k, v      [B, H_kv, T, d_h] of cache->dtype, 16-byte aligned.
+ * k, v      [B, H_kv, T, d_h] of cache->dtype, 16-byte aligned;
+ *           T + max_pages * page_size <= 2^31 - 2^16.
  * new_len   [B] int32 in [0, T]: sequence b's new tokens n_b, or NULL for T
  *           each. Row t < n_b is token lengths[b] - n_b + t: advance lengths
  *           first. Rows t >= n_b, and those of a token before the first,

@@ -210,6 +210,12 @@ extern "C" int elsaa_cache_append(const elsaa_cache *cache, int T,
     if (rc != ELSAA_OK) return rc;
     if (T <= 0)
         return set_last_error(ELSAA_ERR_INVALID_ARG, "T must be positive");
+    // a sequence with few of the T rows may be at the end of its table already:
+    // the pages that all T would take from there on are numbered too
+    if (T > kCacheMaxSlots - (long)c.max_pages * c.ps)
+        return set_last_error(ELSAA_ERR_UNSUPPORTED,
+                              "T + max_pages * page_size must be at most "
+                              "2^31 - 2^16");
     if (!k || !v)
         return set_last_error(ELSAA_ERR_INVALID_ARG,
                               "k and v must be non-NULL");

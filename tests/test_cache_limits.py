@@ -52,3 +52,16 @@ def test_selecting_nearly_2_31_pages_is_refused(lib, ps):
         assert "n_sel" in E.elsaa_last_error()
     c = calls(lib, cache(page_size=ps), n_sel=MOST // ps, ws=None)
     assert c["select"]() == WS
+
+
+def test_appending_beyond_2_31_positions_is_refused(lib):
+    """What the table holds and what the call may bring together: a sequence
+    with fewer new rows than T may stand at its table's end."""
+    for pages, ps, T in ((2 ** 24, 64, 2 ** 30), (4, 32, 2 ** 31 - 1),
+                         (MOST // 128, 128, 128), (1, 16, MOST - 15)):
+        c = cache(max_pages=pages, page_size=ps)
+        assert calls(lib, c, T=T)["append"]() == UNS
+        assert "T + max_pages * page_size" in E.elsaa_last_error()
+    c = cache(max_pages=2 ** 24, page_size=64)
+    assert calls(lib, c, T=2 ** 30 - 2 ** 16,
+                 k=None)["append"]() == E.ELSAA_ERR_INVALID_ARG
