@@ -594,7 +594,12 @@ __global__ void __launch_bounds__(kTaThreads, 2)
                         st_shared_v4(q + line_offset<D>(NV + g, ch), lo[0],
                                      lo[1], lo[2], lo[3]);
                         if (ch == 0) {
-                            factors[qs][g] = pow2(e) * (c.scale * kLog2eF);
+                            // A masked score is -inf in any unit, and
+                            // -inf times 0 is no number: a factor below
+                            // fp32's least, of a small scale, becomes that
+                            // (2^-149 of a score of less than 2^128).
+                            factors[qs][g] = fmaxf(
+                                pow2(e) * (c.scale * kLog2eF), 1.4e-45f);
                             limits[qs][g] = lim;
                         }
                     }

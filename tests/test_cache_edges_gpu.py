@@ -98,6 +98,21 @@ def attend(case, q, qd, new, impl, pages=None, scale=0.0, weights=False):
 
 
 @pytest.mark.parametrize("impl", IMPL)
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("T,G", [(1, 1), (3, 2), (5, 4)])
+def test_queries_of_zeros_at_the_smallest_scales(impl, weights, T, G):
+    """Every key counts the same for a query of zeros, whatever the scale;
+    rows behind new_len, which are taken as zeros, reach no weight."""
+    for scale in (1e-30, 1e-45, 1e-3):
+        case = Case([300, 40, 5, 0, 128], 2 * G, 2, 64, 16, seed=T)
+        q, qd = case.rows(2 * G, T)
+        q[0], q[1, 0], q[2, :, T - 1] = 0, 0, 0
+        qd.copy_(torch.tensor(q))
+        new = [T, max(T - 1, 1), min(T, 2), 0, 1]
+        attend(case, q, qd, new, impl, scale=scale, weights=weights)
+
+
+@pytest.mark.parametrize("impl", IMPL)
 def test_attention_with_the_most_heads(impl):
     """2^26 items, one key each: their number times the CTAs that may share
     one does not fit in 32 bits. O is the key's value."""
