@@ -95,8 +95,9 @@ int elsaa_cache_workspace_size(const elsaa_cache *cache, int T, int weights,
  * token, else max(e_old, e_new), and its older codes move to it, rounded to
  * nearest even. bounds follows: hi = max(ceil(hi_old 2^(e_old - e)),
  * ceil(max code / 4)), lo likewise with min and floor. NaN stays NaN and is
- * left out of e and of bounds; an infinity counts as the type's largest value
- * and is stored as the page's largest, 448 2^e.
+ * left out of e and of bounds (a channel without a number in the page has the
+ * widest, hi = 112 and lo = -112); an infinity counts as the type's largest
+ * value and is stored as the page's largest, 448 2^e.
  *
  * A page that is written may be in one sequence's table only.
  */

@@ -73,6 +73,12 @@ def _extremes(codes):
     return np.ceil(hi / 4), np.floor(lo / 4)
 
 
+def _box(hi, lo):
+    """The bounds of a page; a channel without a number may hold anything."""
+    none = hi < lo
+    return np.stack([np.where(none, 112, hi), np.where(none, -112, lo)])
+
+
 def append(c, k, v, new_len):
     """Updates c in place with rows k, v [B, H_kv, T, d]; lengths count
     them already."""
@@ -102,8 +108,7 @@ def append(c, k, v, new_len):
                             was = np.float64(c["bounds"][i, h]) * drop
                             hi = np.maximum(hi, np.ceil(was[0]))
                             lo = np.minimum(lo, np.floor(was[1]))
-                        c["bounds"][i, h] = np.clip(np.stack([hi, lo]), -112,
-                                                    112)
+                        c["bounds"][i, h] = _box(hi, lo)
 
 
 def _rows(c, x, b, h, pos):
@@ -215,6 +220,5 @@ def evict(c, weight, keep, recent, dst, weight_out):
                     c[x + "_scale"][i, h] = 2.0 ** e
                     if x == "k":
                         hi, lo = _extremes(c[x][i, h, :len(r)])
-                        c["bounds"][i, h] = np.clip(np.stack([hi, lo]), -112,
-                                                    112)
+                        c["bounds"][i, h] = _box(hi, lo)
     return counts, kept

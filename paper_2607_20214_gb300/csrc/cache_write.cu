@@ -139,8 +139,7 @@ __device__ __forceinline__ float page_max(const Page<D, E> &g, float x,
 
 // Four bytes of bounds: the extremes' codes (of x f) over 4, rounded outwards,
 // joined with the page's older ones times `drop`. sign: 1 for the largest, -1
-// for the smallest. Whole numbers in [-112, 112] (448 / 4), clipped for a
-// channel without a number.
+// for the smallest. Whole numbers in [-112, 112] (448 / 4).
 template <typename R>
 __device__ __forceinline__ uint32_t bound_word(const uint32_t *x, float sign,
                                                float f, bool had,
@@ -161,6 +160,34 @@ __device__ __forceinline__ uint32_t bound_word(const uint32_t *x, float sign,
         }
     }
     return out;
+}
+
+// A channel in which the page holds no number may hold anything: its bounds are
+// the widest. It has both extremes' first values, -inf for the largest and
+// inf for the smallest (one of them may be a key's). `out`: the four bytes as
+// bound_word has them, from the extremes `own`; `other`: the other side's.
+template <int W>
+struct Words {
+    uint32_t w[W];
+};
+template <typename R, int W>
+__device__ __noinline__ uint32_t widest(uint32_t out, Words<W> own,
+                                        Words<W> other, bool low) {
+    const float no = low ? INFINITY : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 a = R::get(own.w[k / R::PER]);
+        const float2 b = R::get(other.w[k / R::PER]);
+        const bool y = R::PER == 2 && (k & 1);
+        if ((y ? a.y : a.x) == no && (y ? b.y : b.x) == -no)
+            out = (out & ~(0xffu << 8 * k)) | (low ? 0x90u : 0x70u) << 8 * k;
+    }
+    return out;
+}
+// Whether one of the four bytes is what bound_word makes of such an extreme.
+__device__ __forceinline__ bool may_be_none(uint32_t out, bool low) {
+    const uint32_t z = out ^ (low ? 0x70707070u : 0x90909090u);
+    return ((z - 0x01010101u) & ~z & 0x80808080u) != 0;
 }
 
 // The page's channel extremes into its bounds (`bounds`: where the page's
@@ -221,25 +248,44 @@ __device__ __forceinline__ void page_bounds(const Page<D, E> &g, uint32_t *hi,
         __syncthreads();
         if (!mine) return;
         // the page's first warp
-        const uint32_t *from =
-            sh + (warp - low) * 2 * N * W + (low * N + lane) * W;
-        uint32_t x[W];
+        const uint32_t *from = sh + (warp - low) * 2 * N * W + lane * W;
+        auto join = [&](bool l) {
+            Words<W> x;
 #pragma unroll
-        for (int w = 0; w < kWrThreads / 32; ++w)
-            if (w < g.size / 32)
+            for (int w = 0; w < kWrThreads / 32; ++w)
+                if (w < g.size / 32)
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    const uint32_t y = from[w * 2 * N * W + i];
-                    x[i] = w == 0 ? y
-                           : low  ? R::min2(x[i], y)
-                                  : R::max2(x[i], y);
-                }
-        *to = bound_word<R>(x, low ? -1.0f : 1.0f, f, had, old, drop);
+                    for (int i = 0; i < W; ++i) {
+                        const uint32_t y = from[(w * 2 + l) * N * W + i];
+                        x.w[i] = w == 0 ? y
+                                 : l    ? R::min2(x.w[i], y)
+                                        : R::max2(x.w[i], y);
+                    }
+            return x;
+        };
+        const Words<W> x = join(low);
+        uint32_t out =
+            bound_word<R>(x.w, low ? -1.0f : 1.0f, f, had, old, drop);
+        if (!had && may_be_none(out, low))
+            out = widest<R, W>(out, x, join(!low), low);
+        *to = out;
     } else if (writes) {
         to += word;
         const uint32_t old[2] = {had ? to[0] : 0u, had ? to[N] : 0u};
-        to[0] = bound_word<R>(hi, 1.0f, f, had, old[0], drop);
-        to[N] = bound_word<R>(lo, -1.0f, f, had, old[1], drop);
+        uint32_t out[2] = {bound_word<R>(hi, 1.0f, f, had, old[0], drop),
+                           bound_word<R>(lo, -1.0f, f, had, old[1], drop)};
+        if (!had && may_be_none(out[0], false)) {
+            Words<W> h, l;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                h.w[i] = hi[i];
+                l.w[i] = lo[i];
+            }
+            out[0] = widest<R, W>(out[0], h, l, false);
+            out[1] = widest<R, W>(out[1], l, h, true);
+        }
+        to[0] = out[0];
+        to[N] = out[1];
     }
 }
 

@@ -112,6 +112,57 @@ def test_queries_of_zeros_at_the_smallest_scales(impl, weights, T, G):
         attend(case, q, qd, new, impl, scale=scale, weights=weights)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("ps", [16, 32, 128])
+def test_channels_that_hold_no_number_count_as_the_widest(dtype, d, ps):
+    """Pages whose keys are all NaN in some channels, in a channel of
+    infinities, everywhere; they grow, are selected from and evicted from."""
+    case = Case([30 * ps, 9 * ps], 4, 2, d, ps, dtype, seed=d + ps,
+                spread=0.3, extra_pages=12)
+    k = case.rng.standard_normal((2, 2, 30 * ps, d))
+    for p in range(0, 30, 3):
+        k[:, :, p * ps:(p + 1) * ps, case.rng.permutation(d)[:d // 3]] = np.nan
+    k[0, 0, 5 * ps:6 * ps] = np.nan
+    k[0, 1, 7 * ps:8 * ps, :5] = -np.inf
+    k[0, 1, 7 * ps:8 * ps, 5:9] = np.inf
+    k[0, 1, 7 * ps:8 * ps:2, 3:7] = np.nan
+    cache = case.device(E)
+    kd = torch.tensor(k).cuda().to(cache.torch_dtype)
+    k = kd.double().cpu().numpy()
+    # the last page in two parts, then whole
+    for end in (30 * ps - ps // 2, 30 * ps - 1, 30 * ps):
+        n = [30 * ps - ps // 2 if end < 30 * ps - 1 else
+             end - (30 * ps - ps // 2) if end < 30 * ps else 1, 0]
+        t0 = end - n[0]
+        if t0 == 0:
+            n[1] = 9 * ps
+        rows = max(n)
+        part = np.zeros((2, 2, rows, d))
+        part[0, :, :n[0]] = k[0, :, t0:end]
+        part[1, :, :n[1]] = k[1, :, :n[1]]
+        case.c["lengths"][0] = end
+        cache.tensors["lengths"][0] = end
+        pd = torch.tensor(part).cuda().to(cache.torch_dtype)
+        E.elsaa_cache_append(cache, pd, pd, new_len=int_tensor(n))
+        oc.append(case.c, part, part, n)
+        assert case.same_bytes(cache) == []
+    assert (case.c["bounds"][:, :, 0] >= case.c["bounds"][:, :, 1]).all()
+    q, qd = case.rows(4, 1)
+    for n_sel, first, last in ((8, 0, 0), (13, 1, 1)):
+        got = E.elsaa_cache_select(cache, qd, n_sel, first, last)
+        assert np.array_equal(got.cpu().numpy(),
+                              oc.select(case.c, q, [1, 1], n_sel, first, last))
+    keep = 3 * ps + 1
+    w = np.zeros((2, 2, case.max_pages * ps), np.float32)
+    w[:, :, :ps], w[:, :, 5 * ps:6 * ps], w[:, :, 7 * ps:8 * ps] = 3, 2, 1
+    dst = case.free[:8].reshape(2, 4).astype(np.int32)
+    E.elsaa_cache_evict(cache, torch.tensor(w).cuda(), keep, 1,
+                        int_tensor(dst))
+    oc.evict(case.c, w, keep, 1, dst, np.zeros((2, 2, 4 * ps)))
+    assert case.same_bytes(cache) == []
+
+
 @pytest.mark.parametrize("impl", IMPL)
 def test_attention_with_the_most_heads(impl):
     """2^26 items, one key each: their number times the CTAs that may share
