@@ -119,6 +119,7 @@ int elsaa_cache_append(const elsaa_cache *cache, int T, const void *k,
  *           (sum_i max(qhat_i hi_i, qhat_i lo_i)) 2^e 4 k_scale_p.
  * The sum is a whole number below 2^24 and its factors powers of two, so u is
  * exact in fp32 and the selection does not depend on the order of summation.
+ * (From 2^128 on it counts as infinite, and such pages are equal.)
  * Taken are the first `first` pages, the last `last` and then those of
  * largest u (equal: lower p), n_sel in all or as many as the sequence has; a
  * sequence with n_b = 0 gets none. first, last >= 0 and first + last <= n_sel.

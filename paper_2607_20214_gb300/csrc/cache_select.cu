@@ -396,10 +396,13 @@ __global__ void __launch_bounds__(kScThreads, 2)
                 for (int j = 0; j < 4; ++j) {
                     const int r = r0 + 2 * t + (j & 1);
                     const float f = r < GT ? qscale[r] : -1.0f;
+                    // the smaller factor first: what overflows then is larger
+                    // than fp32 holds as a whole
+                    const float s = pscale[row + 8 * (j >> 1)];
                     if (f >= 0.0f)
-                        best[j >> 1] = fmaxf(
-                            best[j >> 1],
-                            acc[j] * f * pscale[row + 8 * (j >> 1)]);
+                        best[j >> 1] =
+                            fmaxf(best[j >> 1],
+                                  acc[j] * fminf(f, s) * fmaxf(f, s));
                 }
             }
         }

@@ -163,6 +163,28 @@ def test_channels_that_hold_no_number_count_as_the_widest(dtype, d, ps):
     assert case.same_bytes(cache) == []
 
 
+def test_select_with_large_queries_and_small_keys():
+    """The score fits fp32 where the query's part of it does not."""
+    case = Case([600], 2, 1, 64, 16, seed=31)
+    case.c["k_scale"][:] = 2.0 ** case.rng.integers(
+        -60, -50, case.c["k_scale"].shape)
+    q, qd = case.rows(2, 1, size=2.0 ** 125)
+    got = E.elsaa_cache_select(case.device(E), qd, 9, 0, 0)
+    ref = oc.select(case.c, q, [1], 9, 0, 0)
+    assert np.array_equal(got.cpu().numpy(), ref)
+
+
+def test_select_scores_beyond_fp32_tie():
+    case = Case([600], 1, 1, 64, 16, seed=32)
+    case.c["bounds"][:, :, 0], case.c["bounds"][:, :, 1] = 100, -100
+    case.c["k_scale"][:] = 2.0 ** 119
+    case.c["k_scale"][case.c["table"][0, 20]] = 2.0 ** 120
+    qd = torch.full((1, 1, 1, 64), 2.0 ** 100, device="cuda",
+                    dtype=torch.bfloat16)
+    got = E.elsaa_cache_select(case.device(E), qd, 5, 0, 0)
+    assert got[0, 0].tolist() == [0, 1, 2, 3, 4]
+
+
 @pytest.mark.parametrize("impl", IMPL)
 def test_attention_with_the_most_heads(impl):
     """2^26 items, one key each: their number times the CTAs that may share
