@@ -432,8 +432,9 @@ __global__ void __launch_bounds__(kWrThreads, sizeof(T) == 2 ? 4 : 2)
     page_bounds<R>(g, hi, lo, sh,
                    keys && id >= 0 ? c.bounds + ph * 2 * D : nullptr, f, had,
                    drop);
-    // every thread of the page has read the scale: page_max's exchange lies
-    // between
+    // every thread of the page has read the scale: a barrier of page_max's lies
+    // between, or the page is in one warp
+    __syncwarp();
     if (id >= 0 && g.t == 0) *scale = pow2(e);
 }
 
