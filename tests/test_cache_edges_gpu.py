@@ -97,6 +97,17 @@ def attend(case, q, qd, new, impl, pages=None, scale=0.0, weights=False):
             assert np.all(got[b][:, n:] == -3.0)
 
 
+def table_case(pool, ps, d, lengths, max_pages, H, hkv, dtype, seed):
+    """A cache whose table names the pool's pages many times over (reading a
+    page for several places is allowed)."""
+    case = Case([pool * ps], H, hkv, d, ps, dtype, seed=seed, extra_pages=0)
+    case.B, case.max_pages = len(lengths), max_pages
+    case.c["table"] = case.rng.integers(
+        0, pool, (case.B, max_pages)).astype(np.int32)
+    case.c["lengths"] = np.array(lengths, np.int32)
+    return case
+
+
 @pytest.mark.parametrize("impl", IMPL)
 @pytest.mark.parametrize("weights", [False, True])
 @pytest.mark.parametrize("T,G", [(1, 1), (3, 2), (5, 4)])
@@ -183,6 +194,29 @@ def test_select_scores_beyond_fp32_tie():
                     dtype=torch.bfloat16)
     got = E.elsaa_cache_select(case.device(E), qd, 5, 0, 0)
     assert got[0, 0].tolist() == [0, 1, 2, 3, 4]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64),
+                                     ("bf16", 32)])
+@pytest.mark.parametrize("B,max_pages", [(5, 257), (5, 1024), (3, 5000),
+                                         (2, 16384), (40, 1024), (76, 300)])
+def test_select_by_clusters(dtype, d, B, max_pages):
+    """Several CTAs score the pages of a sequence and head and leave the keys
+    with the first: all of them with pages, some without, several rounds
+    each; sequences full, empty and in between; clusters smaller than the
+    pages ask for."""
+    lengths = [max_pages * 16, 0, 16 * 255 + 3, 1, 16 * 256 + 1] + 71 * [70]
+    case = table_case(50, 16, d, [min(n, max_pages * 16) for n in lengths[:B]],
+                      max_pages, 4, 2, dtype, seed=max_pages)
+    new = ([1, 1, 2, 1, 2] + 71 * [1])[:B]
+    q, qd = case.rows(4, 2)
+    cache = case.device(E)
+    for n_sel, first, last in ((40, 1, 1), (300, 0, 3)):
+        got = E.elsaa_cache_select(cache, qd, n_sel, first, last,
+                                   new_len=int_tensor(new))
+        E.elsaa_check_status(cache.tensors["status"])
+        ref = oc.select(case.c, q, new, n_sel, first, last)
+        assert np.array_equal(got.cpu().numpy(), ref), (n_sel, first, last)
 
 
 @pytest.mark.parametrize("impl", IMPL)
