@@ -177,6 +177,9 @@ int elsaa_cache_attention(const elsaa_cache *cache, int T, const void *q,
  *            in use, by this call or by another. The old pages are free
  *            afterwards. A page's exponent and bounds are those that
  *            elsaa_cache_append gives to the values held.
+ *            A page of it outside the pool is not written. Of a page of
+ *            page_table outside the pool, whose tokens attention skips, the
+ *            kept tokens become rows of zeros, which later calls do see.
  * weight_out [B, H_kv, dst_pages * page_size] fp32: the kept tokens' weights;
  *            entries behind them keep what they held. Not weight itself.
  * lengths_out [B] int32: min(lengths, keep); may be cache->lengths.

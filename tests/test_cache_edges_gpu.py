@@ -219,6 +219,73 @@ def test_select_by_clusters(dtype, d, B, max_pages):
         assert np.array_equal(got.cpu().numpy(), ref), (n_sel, first, last)
 
 
+def test_select_passes_over_pages_outside_the_pool():
+    """They rank behind every page, and are recorded."""
+    case = Case([600, 300], 2, 2, 64, 16, seed=33, extra_pages=4)
+    q, qd = case.rows(2, 1)
+    cache = case.device(E)
+    num = len(case.c["k"])
+    for b, p, bad in ((0, 3, num), (0, 36, -7), (1, 0, 2 ** 31 - 1)):
+        cache.tensors["page_table"][b, p] = bad
+        case.c["table"][b, p] = case.free[0]
+    # in the oracle: a page of score -inf
+    i = case.free[0]
+    case.c["k_scale"][i] = -np.inf
+    case.c["bounds"][i, :, 0], case.c["bounds"][i, :, 1] = 1, -1
+    for n_sel, first, last in ((9, 0, 0), (35, 0, 1), (60, 1, 1)):
+        got = E.elsaa_cache_select(cache, qd, n_sel, first, last)
+        ref = oc.select(case.c, q, [1, 1], n_sel, first, last)
+        assert np.array_equal(got.cpu().numpy(), ref)
+    with pytest.raises(E.ElsaaError, match="status 5"):
+        E.elsaa_check_status(cache.tensors["status"])
+
+
+@pytest.mark.parametrize("d,ps", [(64, 16), (128, 128), (32, 32)])
+def test_evict_with_pages_outside_the_pool(d, ps):
+    """Tokens kept from such a page become zeros, pages that should go to
+    one are not written, and the first is recorded."""
+    lengths = [20 * ps + 3, 7 * ps]
+    keep = 3 * ps
+    case = Case(lengths, 2, 2, d, ps, seed=34, extra_pages=9)
+    w = np.exp(case.rng.standard_normal((2, 2, case.max_pages * ps)))
+    w = w.astype(np.float32)
+    w[0, :, 5 * ps:5 * ps + 9] = 1e9
+    w[1, 1, 2 * ps:3 * ps:2] = 1e9
+    dst = case.free[:6].reshape(2, 3).astype(np.int32)
+    cache = case.device(E)
+    num = len(case.c["k"])
+    zero = case.free[6]
+    for b, p, bad in ((0, 5, num), (0, 20, -1), (1, 2, 2 ** 31 - 1)):
+        cache.tensors["page_table"][b, p] = bad
+        case.c["table"][b, p] = zero
+    for x in "kv":  # in the oracle: a page of zeros
+        case.c[x][zero] = 0
+        case.c[x + "_scale"][zero] = 2.0 ** -64
+    on_device = dst.copy()
+    on_device[1, 1] = num + 5
+    spare = dst[1, 1]
+    was = {x: case.c[x][[zero, spare]].copy() for x in
+           ("k", "v", "k_scale", "v_scale", "bounds")}
+    for x in ("k", "v"):  # the device's page was not touched above
+        was[x][0] = NAN
+        was[x + "_scale"][0] = np.nan
+    kept = torch.empty((2, 2, keep), dtype=torch.int32, device="cuda")
+    wout = torch.zeros((2, 2, 3 * ps), device="cuda")
+    _, lens = E.elsaa_cache_evict(cache, torch.tensor(w).cuda(), keep, 5,
+                                  int_tensor(on_device), weight_out=wout,
+                                  kept=kept)
+    with pytest.raises(E.ElsaaError, match="status 5"):
+        E.elsaa_check_status(cache.tensors["status"])
+    ref_w = np.zeros((2, 2, 3 * ps))
+    ref_len, ref_kept = oc.evict(case.c, w, keep, 5, dst, ref_w)
+    assert np.array_equal(lens.cpu().numpy(), ref_len)
+    assert np.array_equal(kept.cpu().numpy(), ref_kept)
+    assert np.array_equal(wout.double().cpu().numpy(), ref_w)
+    for x in was:
+        case.c[x][[zero, spare]] = was[x]
+    assert case.same_bytes(cache) == []
+
+
 @pytest.mark.parametrize("impl", IMPL)
 def test_attention_with_the_most_heads(impl):
     """2^26 items, one key each: their number times the CTAs that may share
