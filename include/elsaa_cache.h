@@ -142,9 +142,12 @@ int elsaa_cache_select(const elsaa_cache *cache, int T, const void *q,
  *
  * q, o      [B, H, T, d_h] of cache->dtype, 16-byte aligned. Rows t >= n_b of
  *           o and lse keep what they held.
- * pages     [B, H_kv, n_sel] as elsaa_cache_select writes them (distinct;
- *           entries outside the sequence's pages count as none), or NULL for
- *           all (n_sel is then ignored).
+ * pages     [B, H_kv, n_sel] as elsaa_cache_select writes them, or NULL for
+ *           all (n_sel is then ignored). Lists of the caller's own: distinct
+ *           pages of the sequence first, in any order; entries outside its
+ *           pages count as none and come behind them. Of a sequence of m
+ *           pages the first min(m, n_sel) entries are read, so that pages
+ *           behind others' entries may be missed.
  * weight_in, weight_out  [B, H_kv, max_pages * page_size] fp32, 16-byte
  *           aligned, or both NULL:
  *           weight_out_j = weight_in_j + sum of exp(s_j - lse) over the K/V
