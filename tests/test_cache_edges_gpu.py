@@ -307,6 +307,101 @@ def test_lists_in_any_order_with_others_behind(impl, weights):
     attend(case, q, qd, [3, 2, 1, 3], impl, pages=pages, weights=weights)
 
 
+@pytest.mark.parametrize("dtype,d,impl", [
+    ("fp32", 32, 0), ("fp32", 64, 0), ("fp32", 128, 0), ("bf16", 32, 0),
+    ("bf16", 64, 1), ("bf16", 128, 1), ("bf16", 64, 0), ("bf16", 128, 0)])
+@pytest.mark.parametrize("T,G,ps", [(1, 1, 16), (1, 4, 64), (2, 3, 32),
+                                    (5, 4, 16), (7, 1, 128), (16, 8, 32)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_within_its_kernels_own_bound(dtype, d, impl, T, G, ps,
+                                                weights):
+    """Every type and head size with several tokens and weights; short
+    sequences, where a weight in half precision would show, and longer."""
+    case = Case([9, 130, 0, 1000, 128, 1, 16], 2 * G, 2, d, ps, dtype,
+                seed=d + T)
+    q, qd = case.rows(2 * G, T)
+    new = [T, max(T - 1, 1), min(T, 2), T, T, 1, 0]
+    attend(case, q, qd, new, impl, weights=weights)
+
+
+@pytest.mark.parametrize("dtype,d", [("fp32", 32), ("fp32", 64),
+                                     ("fp32", 128), ("bf16", 32)])
+@pytest.mark.parametrize("T,G", [(1, 1), (1, 6), (4, 2)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_listed_pages_on_cuda_cores(dtype, d, T, G, weights):
+    case = Case([700, 40, 0, 300], 3 * G, 3, d, 32, dtype, seed=36)
+    pages = np.full((4, 3, 9), -1, np.int32)
+    for b, n in enumerate([700, 40, 0, 300]):
+        for h in range(3):
+            take = sorted(case.rng.permutation(-(-n // 32))[:9 - h])
+            pages[b, h, :len(take)] = take
+    q, qd = case.rows(3 * G, T)
+    attend(case, q, qd, [T, 1, 0, T], 0, pages=pages, weights=weights)
+
+
+@pytest.mark.parametrize("impl", IMPL)
+def test_lengths_outside_the_table_are_clipped(impl):
+    """A negative length is none, one beyond the table is the table's, whose
+    entries behind the last page are skipped; the others are as ever."""
+    case = Case([100, 90], 4, 2, 64, 16, seed=37)
+    q, qd = case.rows(4, 1)
+    for bad in (-1, -2 ** 31, 10 ** 6, 2 ** 31 - 1):
+        cache = case.device(E, impl)
+        cache.tensors["lengths"][1] = bad
+        # six pages of the second sequence are whole but for 6 rows, which
+        # hold NaN: numbers, so that the clipped length can be compared
+        k = {x: case.c[x].copy() for x in "kv"}
+        last = case.c["table"][1, 5]
+        for x in "kv":
+            case.c[x][last, :, 10:] = 0x30
+            cache.tensors[x].copy_(torch.tensor(case.c[x]))
+        lse = torch.empty((2, 4, 1), device="cuda")
+        o = E.elsaa_cache_attention(cache, qd, lse=lse)
+        with pytest.raises(E.ElsaaError, match="status"):
+            E.elsaa_check_status(cache.tensors["status"])
+        was = case.c["lengths"].copy()
+        case.c["lengths"][1] = 0 if bad < 0 else 96
+        ref = oc.attention(case.c, q, [1, 1], 0.125)
+        check(case, o, lse, ref, [1, 1], impl)
+        case.c["lengths"][:] = was
+        case.c.update(k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_decoding_step_by_step(dtype, d):
+    """Append, select, attend over the selected pages with weights, in every
+    step all that is written against the oracle, lse too."""
+    case = Case([200, 33, 94], 4, 2, d, 32, dtype, seed=38, extra_pages=20,
+                spare=3)
+    for b in range(3):
+        t = case.c["table"][b]
+        gaps = np.flatnonzero(t < 0)
+        t[gaps] = case.free[3 * b:3 * b + len(gaps)]
+    cache = case.device(E)
+    w = torch.zeros((3, 2, case.max_pages * 32), device="cuda")
+    total = 0.0
+    for step in range(6):
+        case.c["lengths"] += 1
+        cache.tensors["lengths"] += 1
+        (k, kd), (v, vd) = case.rows(2, 1), case.rows(2, 1)
+        q, qd = case.rows(4, 1)
+        E.elsaa_cache_append(cache, kd, vd)
+        oc.append(case.c, k, v, [1] * 3)
+        pages = E.elsaa_cache_select(cache, qd, 5)
+        ref = oc.select(case.c, q, [1] * 3, 5, 1, 1)
+        assert np.array_equal(pages.cpu().numpy(), ref)
+        lse = torch.full((3, 4, 1), 7.0, device="cuda")
+        o = E.elsaa_cache_attention(cache, qd, pages=pages, lse=lse,
+                                    weight_in=w, weight_out=w)
+        ref = oc.attention(case.c, q, [1] * 3, d ** -0.5, ref)
+        check(case, o, lse, ref, [1] * 3)
+        total = total + ref[2]
+    E.elsaa_check_status(cache.tensors["status"])
+    assert case.same_bytes(cache) == []
+    assert np.abs(w.double().cpu().numpy() - total).max() <= 6 * 2.0 ** -17
+
+
 @pytest.mark.parametrize("impl", IMPL)
 def test_attention_with_the_most_heads(impl):
     """2^26 items, one key each: their number times the CTAs that may share
