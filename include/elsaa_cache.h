@@ -11,6 +11,10 @@
  *   elsaa_cache_evict      the tokens of least accumulated attention weight
  *                          leave
  *
+ * This is exact softmax attention over the cached tokens, or over selected
+ * pages of them: elsaa.h's low-rank branch, fusion weight and gates have no
+ * part in it.
+ *
  * The conventions of elsaa.h hold: device pointers owned by the caller, no
  * allocation, asynchronous on the caller's stream, arguments validated on the
  * host before any launch, ELSAA_* return codes, elsaa_last_error(). Every call
@@ -158,7 +162,12 @@ int elsaa_cache_select(const elsaa_cache *cache, int T, const void *q,
  * T at most 64 and T * H / H_kv at most 128 (longer runs of queries are
  * prompts). bf16 with d_h 64 or 128 runs on the tensor cores, which take the
  * codes as they are: a query is split into two e4m3 numbers that hold its 8
- * bits, a weight into three. fp32 and d_h = 32 run on CUDA cores.
+ * bits, a weight, rounded to fp16, into three. fp32 and d_h = 32 run on CUDA
+ * cores, and with impl = ELSAA_IMPL_SIMT everything does: weights and values
+ * are multiplied in fp32 there. The tensor cores multiply keys by queries that
+ * are scaled to at most 448: keys from 2^112 on may overflow, queries whose
+ * largest element lies below 2^-92 lose bits below 2^-113. The row of a query
+ * that holds a NaN or an infinity is not defined; it reaches no other row.
  */
 int elsaa_cache_attention(const elsaa_cache *cache, int T, const void *q,
                           const int32_t *new_len, const int32_t *pages,

@@ -74,9 +74,16 @@ constexpr int kCacheTcCtas = 152 * 2;
 // would get of items that are shared. Sharing gives every CTA two beginnings
 // and ends, and the merge is a launch: 8 sequences with 32 heads of 1024 tokens
 // 15.8 us shared, 12.0 whole; 8 with 8 heads, 4 x 5 queries each, 512 tokens
-// 19.0 and 11.2; 12 heads of 700 tokens (6 tiles more) 8.2 and 8.4, with a
-// launch less; 8 heads of 1024 tokens (8 more) 7.9 and 9.8. Behind more than
-// kCacheWholeSeqs sequences (a warp's lanes) the division counts tiles.
+// 19.0 and 11.2. Shared and whole, in a graph, by tiles more:
+//                                    2     3     4     5     6     7     8
+// 12 heads of 64, a sequence  shared 7.0   8.0   8.1   8.2   7.9   8.4   8.2
+//                             whole  5.8   6.8   7.3   8.2   8.4   9.2   9.5
+// 8 heads of 4 queries, 4 s.  shared 7.5   9.0   8.3   9.6   10.4  10.6  11.6
+//                             whole  6.2   7.2   7.5   8.4   8.9   9.8   10.2
+// One by one from Python a launch less counts too (12 heads, 6 tiles: 8.8 to
+// 9.2 and 8.8; 7: 9.0 and 9.6): at 6 the rule gives away half a microsecond of
+// the GPU's time with few items for the host's, and wins with many. Behind more
+// than kCacheWholeSeqs sequences (a warp's lanes) the division counts tiles.
 constexpr int kCacheWhole = 16, kCacheMore = 6;
 constexpr int kCacheWholeSeqs = 32;
 inline int cache_simt_cols(int gt) { return gt >= 3 ? 4 : gt; }

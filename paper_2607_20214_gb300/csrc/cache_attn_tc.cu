@@ -35,10 +35,13 @@
 // ready. Two CTAs share an SM.
 //
 // Measured with the merge: 16 sequences, 8 heads of 128, 4 queries a head,
-// 65536 tokens 324 us (6.6 TB/s, 0.98 of a copy); 2 x 16 heads of 16384 tokens
-// 30 us, of which 24 at 5.6 TB/s, the rest its start (lengths, table, first
-// tile: 5000 cycles) and the merge. From 16 columns on the softmax's arithmetic
-// bounds it, 2000 cycles a tile.
+// 65536 tokens 324 to 328 us (6.6 TB/s, 0.97 to 0.98 of a copy); 2 x 16 heads
+// of 16384 tokens 30 us, of which 24 at 5.6 TB/s, the rest its start (lengths,
+// table, first tile: 5000 cycles) and the merge. With more columns a tile takes
+// longer (8 sequences, 8 heads, 8192 tokens: 1 column 31 us, 8 33, 16 40, about
+// 2000 cycles a tile) without a unit being full: with 16 columns 24 % of the
+// issue slots, 18 % of the ALU, 42 % of DRAM, 6 % of the tensor pipe. Its warps
+// wait, for loads and at barriers above all.
 #include <limits.h>
 
 #include "cache_common.cuh"

@@ -8,7 +8,7 @@
 // power of two is exact, so the only rounding is the conversion's. What bounds
 // it is HBM, if enough pages are in flight: small pages share a CTA, and every
 // dependent read (length, table entry, position) is issued for all four rows
-// before one is used. A prompt of 2 x 16 heads x 16384 rows of 128: 65 us, 6.2
+// before one is used. A prompt of 2 x 16 heads x 16384 rows of 128: 65 us, 6.1
 // TB/s (8 channels a thread; with 16, read in two loads, 99 when this took 81).
 // Compaction of 2 x 16 heads to 4096 rows: 16 us, bound by its issue slots
 // (decoding, extremes) and by the reads that wait for one another.
