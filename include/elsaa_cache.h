@@ -164,11 +164,12 @@ int elsaa_cache_select(const elsaa_cache *cache, int T, const void *q,
  * codes as they are: a query is split into two e4m3 numbers that hold its 8
  * bits, a weight, rounded to fp16, into three. fp32 and d_h = 32 run on CUDA
  * cores, and with impl = ELSAA_IMPL_SIMT everything does: weights and values
- * are multiplied in fp32 there. Exponentials are the hardware's, 2^-21 off at
- * most with their arguments' rounding. The tensor cores multiply keys by queries that
- * are scaled to at most 448: keys from 2^112 on may overflow, queries whose
- * largest element lies below 2^-92 lose bits below 2^-113. The row of a query
- * that holds a NaN or an infinity is not defined; it reaches no other row.
+ * are multiplied in fp32 there. Exponentials are the hardware's, 2^-22 off
+ * beside the rounding of their arguments. The tensor cores multiply keys by
+ * queries that are scaled to at most 448: keys from 2^112 on may overflow,
+ * queries whose largest element lies below 2^-92 lose bits below 2^-113. The
+ * row of a query that holds a NaN or an infinity is not defined; it reaches no
+ * other row.
  */
 int elsaa_cache_attention(const elsaa_cache *cache, int T, const void *q,
                           const int32_t *new_len, const int32_t *pages,
