@@ -1,0 +1,60 @@
+// Exact attention (include/elsaa_exact.h): what a call is about, and how the
+// kernels see it.
+#pragma once
+
+#include "../../include/elsaa_exact.h"
+#include "cache.h"
+
+namespace elsaa {
+
+struct ExactView {
+    int B, H, Hkv, G, Nq, Nk, d, dtype, causal;
+    float scale;
+    const void *q, *k, *v, *o, *d_o;
+    const int32_t *q_len, *k_len;
+    float *lse;    // forward: written, or NULL; backward: read
+    float *delta;  // [B, H, Nq] scratch of the backward pass
+    void *out, *dq, *dk, *dv;
+    DeviceStatus *status;
+};
+
+#ifdef __CUDACC__
+// Sequence b's lengths, and how many keys query row i sees: the first seen(i).
+struct ExactSeq {
+    int ql, kl, causal;
+    __device__ __forceinline__ ExactSeq(const ExactView &a, int b)
+        : ql(a.Nq), kl(a.Nk), causal(a.causal) {
+        if (a.q_len) ql = min(max(a.q_len[b], 0), a.Nq);
+        if (a.k_len) kl = min(max(a.k_len[b], 0), a.Nk);
+    }
+    __device__ __forceinline__ int seen(int i) const {
+        if (i >= ql) return 0;
+        return causal ? max(0, min(kl, i + 1 + kl - ql)) : kl;
+    }
+    // the first query row that sees key row j (ql: none)
+    __device__ __forceinline__ int first_row(int j) const {
+        if (j >= kl) return ql;
+        return causal ? min(ql, max(0, j + ql - kl)) : 0;
+    }
+};
+
+// Rows of the query heads that share a K/V head, counted through: row r is row
+// r mod N of head r / N of the group. `most` is the largest seen() among rows
+// [r0, r1).
+__device__ __forceinline__ int exact_most(const ExactSeq &s, int r0, int r1,
+                                          int N) {
+    if (r0 >= r1 || s.ql == 0) return 0;
+    const int i0 = r0 % N, i1 = (r1 - 1) % N;
+    // the last rows of a head are among them
+    if (r0 / N != (r1 - 1) / N)
+        return i0 < s.ql ? s.seen(s.ql - 1) : s.seen(min(i1, s.ql - 1));
+    return i0 < s.ql ? s.seen(min(i1, s.ql - 1)) : 0;
+}
+#endif
+
+// CUDA cores (fp32, and bf16 with impl = SIMT)
+cudaError_t launch_exact_fwd_simt(const ExactView &a, cudaStream_t st);
+cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys,
+                                  cudaStream_t st);
+
+}  // namespace elsaa

@@ -1,4 +1,5 @@
-"""Python binding of the libelsaa C ABI (include/elsaa.h, elsaa_cache.h).
+"""Python binding of the libelsaa C ABI (include/elsaa.h, elsaa_cache.h,
+elsaa_heads.h, elsaa_exact.h).
 
 Argument marshalling only: every step of the operator runs in the CUDA
 kernels of libelsaa.so. PyTorch provides device memory and streams. The
@@ -38,7 +39,10 @@ SYMBOLS = ("elsaa_workspace_size", "elsaa_forward", "elsaa_check_status",
            "elsaa_forward_gated_workspace_size", "elsaa_forward_gated",
            "elsaa_cache_workspace_size", "elsaa_cache_append",
            "elsaa_cache_select", "elsaa_cache_attention",
-           "elsaa_cache_evict")
+           "elsaa_cache_evict", "elsaa_heads_workspace_size",
+           "elsaa_heads_forward", "elsaa_heads_backward",
+           "elsaa_exact_workspace_size", "elsaa_exact_forward",
+           "elsaa_exact_backward")
 # Size of the fixed scratch array behind elsaa_forward_noalloc.
 ELSAA_STATIC_WORKSPACE_BYTES = 64 << 20
 
@@ -90,6 +94,42 @@ class elsaa_cache(ctypes.Structure):
         ("v_scale", ctypes.c_void_p), ("bounds", ctypes.c_void_p),
         ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
         ("status", ctypes.c_void_p),
+    ]
+
+
+class elsaa_rotary(ctypes.Structure):
+    """Mirror of struct elsaa_rotary; make_rotary fills it."""
+    _fields_ = [
+        ("dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+        ("axes", ctypes.c_int), ("reserved", ctypes.c_int),
+        ("turns", ctypes.c_uint64 * 64), ("axis", ctypes.c_uint8 * 64),
+    ]
+
+
+class elsaa_heads(ctypes.Structure):
+    """Mirror of struct elsaa_heads; make_heads fills it."""
+    _fields_ = [
+        ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
+        ("N", ctypes.c_int), ("d_h", ctypes.c_int), ("dtype", ctypes.c_int),
+        ("norm", ctypes.c_int), ("expand", ctypes.c_int),
+        ("grad_fp32", ctypes.c_int), ("eps", ctypes.c_float),
+        ("rotary", elsaa_rotary),
+    ]
+
+
+class elsaa_rows(ctypes.Structure):
+    """Mirror of struct elsaa_rows (strides in elements)."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64),
+                ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class elsaa_exact(ctypes.Structure):
+    """Mirror of struct elsaa_exact; make_exact fills it."""
+    _fields_ = [
+        ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
+        ("N_q", ctypes.c_int), ("N_k", ctypes.c_int), ("d_h", ctypes.c_int),
+        ("dtype", ctypes.c_int), ("causal", ctypes.c_int),
+        ("scale", ctypes.c_float), ("impl", ctypes.c_int),
     ]
 
 
@@ -187,6 +227,18 @@ def load_library(path: str = LIB) -> ctypes.CDLL:
                                     sz, vp]
     for name in ("workspace_size", "append", "select", "attention", "evict"):
         getattr(L, "elsaa_cache_" + name).restype = ci
+    ph, pr = ctypes.POINTER(elsaa_heads), ctypes.POINTER(elsaa_rows)
+    pe = ctypes.POINTER(elsaa_exact)
+    L.elsaa_heads_workspace_size.argtypes = [ph, ctypes.POINTER(sz)]
+    L.elsaa_heads_forward.argtypes = [ph] + [pr] * 3 + [vp] * 9
+    L.elsaa_heads_backward.argtypes = [ph] + [vp] * 3 + [pr] * 2 + [
+        vp] * 5 + [pr] * 3 + [vp] * 3 + [sz, vp]
+    L.elsaa_exact_workspace_size.argtypes = [pe, ci, ctypes.POINTER(sz)]
+    L.elsaa_exact_forward.argtypes = [pe] + [vp] * 8 + [sz, vp]
+    L.elsaa_exact_backward.argtypes = [pe] + [vp] * 12 + [sz, vp]
+    for name in ("heads_workspace_size", "heads_forward", "heads_backward",
+                 "exact_workspace_size", "exact_forward", "exact_backward"):
+        getattr(L, "elsaa_" + name).restype = ci
     _lib = L
     return L
 
@@ -893,3 +945,324 @@ def elsaa_cache_evict(cache: elsaa_cache, weight, keep, recent, dst_table,
         _cptr(kept, "kept", i32, bh * keep, cache), ws, nbytes,
         _stream_for(stream, cache)))
     return weight_out, lengths_out
+
+
+# --------------------------- rows and heads (elsaa_heads.h), exact attention
+# (elsaa_exact.h)
+
+_DTYPES = {"bf16": ELSAA_BF16, "fp32": ELSAA_FP32}
+
+
+def _dtype_code(dtype):
+    return _DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+
+
+def _torch_dtype(code):
+    return torch.float32 if code == ELSAA_FP32 else torch.bfloat16
+
+
+def _turns(radians):
+    """A frequency (a double, radians per position) as turns * 2^64."""
+    import decimal
+    with decimal.localcontext() as ctx:
+        ctx.prec = 60
+        two_pi = decimal.Decimal("6.28318530717958647692528676655900576839433"
+                                 "879875021")
+        x = decimal.Decimal(float(radians)) / two_pi * (1 << 64)
+        return int(x.to_integral_value()) % (1 << 64)
+
+
+def make_rotary(dim, base=10000.0, interleaved=False, sections=None,
+                in_turn=False, frequencies=None) -> elsaa_rotary:
+    """The rotation of a head's first `dim` channels.
+
+    frequencies: radians per position of the dim / 2 pairs (default:
+    base^(-2 i / dim)). sections: pairs of every position axis (default: one
+    axis); in_turn=False gives the first pairs to the first axis, the next to
+    the second; True deals them out in turn while an axis has any left.
+    """
+    n = dim // 2
+    if dim < 0 or dim > 128 or dim % 2:
+        raise ValueError("dim must be even, 0 to 128")
+    if frequencies is None:
+        frequencies = [float(base) ** (-i / n) for i in range(n)]
+    if len(frequencies) != n:
+        raise ValueError("frequencies must have dim / 2 = %d entries" % n)
+    left = [n] if sections is None else [int(x) for x in sections]
+    if not 1 <= len(left) <= 4 or min(left) < 0 or sum(left) != n:
+        raise ValueError("sections must be 1 to 4 counts that add up to "
+                         "dim / 2 = %d" % n)
+    axes, axis = len(left), []
+    if in_turn:
+        while sum(left):
+            for i in range(axes):
+                if left[i]:
+                    left[i] -= 1
+                    axis.append(i)
+    else:
+        axis = [i for i, x in enumerate(left) for _ in range(x)]
+    r = elsaa_rotary(dim, int(bool(interleaved)), axes, 0)
+    for i in range(n):
+        r.turns[i] = _turns(frequencies[i])
+        r.axis[i] = axis[i]
+    return r
+
+
+def make_heads(B, H, H_kv, N, d_h, dtype="bf16", norm=True, rotary=None,
+               expand=False, grad_fp32=False, eps=1e-6) -> elsaa_heads:
+    """What elsaa_heads_forward and elsaa_heads_backward are about (fields:
+    include/elsaa_heads.h). rotary: as make_rotary returns it, or None."""
+    code = _dtype_code(dtype)
+    h = elsaa_heads(B, H, H_kv, N, d_h, code, int(bool(norm)),
+                    int(bool(expand)), int(bool(grad_fp32)), eps,
+                    make_rotary(0) if rotary is None else rotary)
+    h.ref = ctypes.byref(h)
+    h.torch_dtype = _torch_dtype(code)
+    h.grad_dtype = torch.float32 if grad_fp32 else h.torch_dtype
+    kv = H if expand else H_kv
+    h.rows = (B, N, H, d_h), (B, N, H_kv, d_h)
+    h.out = (B, H, N, d_h), (B, kv, N, d_h)
+    h.axes = h.rotary.axes
+    return h
+
+
+def elsaa_heads_workspace_size(heads: elsaa_heads) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().elsaa_heads_workspace_size(heads.ref,
+                                                     ctypes.byref(n)))
+    return n.value
+
+
+def new_heads_workspace(heads: elsaa_heads, device) -> torch.Tensor:
+    """Scratch for elsaa_heads_backward."""
+    return torch.empty(max(elsaa_heads_workspace_size(heads), 256),
+                       dtype=torch.uint8, device=device)
+
+
+class _On:
+    """The device of a call's tensors, which must be the current one."""
+
+    def __init__(self, t, name):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if not t.is_cuda:
+            raise ValueError("%s must be a CUDA tensor" % name)
+        self.device, self.index = t.device, t.get_device()
+        if _current_device() != self.index:
+            raise ValueError("%s is on %s, which is not the current device"
+                             % (name, self.device))
+
+
+def _whole(t, name, dtype, shape, on):
+    """Pointer of a contiguous tensor of this type and shape; None stays."""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and \
+            t.get_device() == on.index and t.shape == shape and \
+            t.is_contiguous():
+        return t.data_ptr()
+    n = 1
+    for x in shape:
+        n *= x
+    _ptr(t, name, dtype, n, on.device)
+    raise ValueError("%s must be %s (got %s)" % (name, list(shape),
+                                                 list(t.shape)))
+
+
+def _strided(t, name, dtype, shape, on):
+    """elsaa_rows of [B, N, heads, d_h], whose channels lie side by side."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.get_device() != on.index:
+        raise ValueError("%s must be on %s (got %s)" % (name, on.device,
+                                                        t.device))
+    if t.dtype is not dtype:
+        raise ValueError("%s must be %s (got %s)" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must be %s (got %s)" % (name, list(shape),
+                                                     list(t.shape)))
+    sb, sn, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError("%s must have its channels side by side" % name)
+    return elsaa_rows(t.data_ptr(), sb, sn, sh)
+
+
+def _tokens(heads, positions, lengths, new_len, on):
+    """Pointers of positions, lengths, new_len."""
+    i32, B = torch.int32, (heads.B,)
+    if positions is not None:
+        shape = (heads.axes, heads.B, heads.N)
+        if heads.axes == 1 and positions.dim() == 2:
+            shape = shape[1:]
+        positions = _whole(positions, "positions", i32, shape, on)
+    return (positions, _whole(lengths, "lengths", i32, B, on),
+            _whole(new_len, "new_len", i32, B, on))
+
+
+def elsaa_heads_forward(heads: elsaa_heads, q=None, k=None, v=None, w_q=None,
+                        w_k=None, positions=None, lengths=None, new_len=None,
+                        q_out=None, k_out=None, v_out=None, stream=None):
+    """Enqueue elsaa_heads_forward: rows q [B, N, H, d_h] and k, v
+    [B, N, H_kv, d_h] (strided views of a projection's output; None: not
+    wanted) to normed and rotated heads. Returns (q_out, k_out, v_out),
+    allocated here when not given (rows behind new_len then undefined)."""
+    first = q if q is not None else k if k is not None else v
+    on = _On(first, "q")
+    dt, f32, w = heads.torch_dtype, torch.float32, (heads.d_h,)
+    rq, rk = heads.rows
+    oq, ok = heads.out
+    rows = (_strided(q, "q", dt, rq, on), _strided(k, "k", dt, rk, on),
+            _strided(v, "v", dt, rk, on))
+    if (q is not None and q_out is None) or (
+            k is not None and k_out is None) or (
+            v is not None and v_out is None):
+        with _own(stream, on):
+            def new(x, out, shape):
+                if x is None or out is not None:
+                    return out
+                return torch.empty(shape, dtype=dt, device=on.device)
+            q_out, k_out, v_out = (new(q, q_out, oq), new(k, k_out, ok),
+                                   new(v, v_out, ok))
+    _check(load_library().elsaa_heads_forward(
+        heads.ref, *rows, _whole(w_q, "w_q", f32, w, on),
+        _whole(w_k, "w_k", f32, w, on),
+        *_tokens(heads, positions, lengths, new_len, on),
+        _whole(q_out, "q_out", dt, oq, on), _whole(k_out, "k_out", dt, ok, on),
+        _whole(v_out, "v_out", dt, ok, on), _stream_of(stream, on.device)))
+    return q_out, k_out, v_out
+
+
+def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
+                         q=None, k=None, w_q=None, w_k=None, positions=None,
+                         lengths=None, new_len=None, dq_rows=None,
+                         dk_rows=None, dv_rows=None, dw_q=None, dw_k=None,
+                         workspace=None, stream=None):
+    """Enqueue elsaa_heads_backward: gradients of the heads to those of the
+    rows and of the norm's weights. Returns (dq_rows, dk_rows, dv_rows, dw_q,
+    dw_k): the rows of the gradients given, allocated here when not given
+    (rows behind new_len then undefined); dw_q and dw_k likewise where the
+    weights are given."""
+    first = dq if dq is not None else dk if dk is not None else dv
+    on = _On(first, "dq")
+    dt, gt, f32 = heads.torch_dtype, heads.grad_dtype, torch.float32
+    w = (heads.d_h,)
+    rq, rk = heads.rows
+    oq, ok = heads.out
+    if w_q is not None and dw_q is None and dq is not None or \
+            w_k is not None and dw_k is None and dk is not None or \
+            dq is not None and dq_rows is None or \
+            dk is not None and dk_rows is None or \
+            dv is not None and dv_rows is None or \
+            workspace is None and not (dw_q is None and dw_k is None):
+        with _own(stream, on):
+            def new(x, out, shape, t):
+                if x is None or out is not None:
+                    return out
+                return torch.empty(shape, dtype=t, device=on.device)
+            dq_rows, dk_rows, dv_rows = (
+                new(dq, dq_rows, rq, dt), new(dk, dk_rows, rk, dt),
+                new(dv, dv_rows, rk, dt))
+            if dq is not None:
+                dw_q = new(w_q, dw_q, w, f32)
+            if dk is not None:
+                dw_k = new(w_k, dw_k, w, f32)
+            if workspace is None:
+                workspace = new_heads_workspace(heads, on.device)
+    ws, nbytes = (None, 0) if workspace is None else _scratch(workspace, on)
+    _check(load_library().elsaa_heads_backward(
+        heads.ref, _whole(dq, "dq", gt, oq, on), _whole(dk, "dk", gt, ok, on),
+        _whole(dv, "dv", gt, ok, on), _strided(q, "q", dt, rq, on),
+        _strided(k, "k", dt, rk, on), _whole(w_q, "w_q", f32, w, on),
+        _whole(w_k, "w_k", f32, w, on),
+        *_tokens(heads, positions, lengths, new_len, on),
+        _strided(dq_rows, "dq_rows", dt, rq, on),
+        _strided(dk_rows, "dk_rows", dt, rk, on),
+        _strided(dv_rows, "dv_rows", dt, rk, on),
+        _whole(dw_q, "dw_q", f32, w, on), _whole(dw_k, "dw_k", f32, w, on),
+        ws, nbytes, _stream_of(stream, on.device)))
+    return dq_rows, dk_rows, dv_rows, dw_q, dw_k
+
+
+def make_exact(B, H, H_kv, N_q, N_k, d_h, dtype="bf16", causal=False,
+               scale=0.0, impl=ELSAA_IMPL_AUTO) -> elsaa_exact:
+    """What elsaa_exact_forward and elsaa_exact_backward are about (fields:
+    include/elsaa_exact.h)."""
+    code = _dtype_code(dtype)
+    e = elsaa_exact(B, H, H_kv, N_q, N_k, d_h, code, int(bool(causal)), scale,
+                    impl)
+    e.ref = ctypes.byref(e)
+    e.torch_dtype = _torch_dtype(code)
+    e.q, e.kv, e.rows = ((B, H, N_q, d_h), (B, H_kv, N_k, d_h), (B, H, N_q))
+    return e
+
+
+def elsaa_exact_workspace_size(exact: elsaa_exact, backward=False) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().elsaa_exact_workspace_size(
+        exact.ref, int(bool(backward)), ctypes.byref(n)))
+    return n.value
+
+
+def new_exact_workspace(exact: elsaa_exact, device,
+                        backward=False) -> torch.Tensor:
+    """Scratch for elsaa_exact_forward (backward: for both calls).
+    elsaa_check_status(workspace) reads the status of the last call on it."""
+    return torch.empty(max(elsaa_exact_workspace_size(exact, backward), 256),
+                       dtype=torch.uint8, device=device)
+
+
+def elsaa_exact_forward(exact: elsaa_exact, q, k, v, q_len=None, k_len=None,
+                        o=None, lse=None, workspace=None, stream=None):
+    """Enqueue elsaa_exact_forward: q [B, H, N_q, d_h] over k, v
+    [B, H_kv, N_k, d_h]. Returns o (allocated here when not given, rows behind
+    q_len then undefined); lse [B, H, N_q] fp32 is written when given."""
+    on = _On(q, "q")
+    dt, i32, B = exact.torch_dtype, torch.int32, (exact.B,)
+    if o is None or workspace is None:
+        with _own(stream, on):
+            if o is None:
+                o = torch.empty(exact.q, dtype=dt, device=on.device)
+            if workspace is None:
+                workspace = new_exact_workspace(exact, on.device)
+    ws, nbytes = _scratch(workspace, on)
+    _check(load_library().elsaa_exact_forward(
+        exact.ref, _whole(q, "q", dt, exact.q, on),
+        _whole(k, "k", dt, exact.kv, on), _whole(v, "v", dt, exact.kv, on),
+        _whole(q_len, "q_len", i32, B, on), _whole(k_len, "k_len", i32, B, on),
+        _whole(o, "o", dt, exact.q, on),
+        _whole(lse, "lse", torch.float32, exact.rows, on), ws, nbytes,
+        _stream_of(stream, on.device)))
+    return o
+
+
+def elsaa_exact_backward(exact: elsaa_exact, q, k, v, o, lse, d_o, q_len=None,
+                         k_len=None, dq=None, dk=None, dv=None,
+                         workspace=None, stream=None):
+    """Enqueue elsaa_exact_backward: the gradients of q, k and v from d_o, with
+    o and lse of elsaa_exact_forward. Returns (dq, dk, dv), allocated here when
+    not given (rows behind q_len and k_len then undefined)."""
+    on = _On(q, "q")
+    dt, i32, B = exact.torch_dtype, torch.int32, (exact.B,)
+    if dq is None or dk is None or dv is None or workspace is None:
+        with _own(stream, on):
+            def new(out, shape):
+                return out if out is not None else torch.empty(
+                    shape, dtype=dt, device=on.device)
+            dq, dk, dv = (new(dq, exact.q), new(dk, exact.kv),
+                          new(dv, exact.kv))
+            if workspace is None:
+                workspace = new_exact_workspace(exact, on.device, True)
+    ws, nbytes = _scratch(workspace, on)
+    _check(load_library().elsaa_exact_backward(
+        exact.ref, _whole(q, "q", dt, exact.q, on),
+        _whole(k, "k", dt, exact.kv, on), _whole(v, "v", dt, exact.kv, on),
+        _whole(o, "o", dt, exact.q, on),
+        _whole(lse, "lse", torch.float32, exact.rows, on),
+        _whole(d_o, "d_o", dt, exact.q, on),
+        _whole(q_len, "q_len", i32, B, on), _whole(k_len, "k_len", i32, B, on),
+        _whole(dq, "dq", dt, exact.q, on), _whole(dk, "dk", dt, exact.kv, on),
+        _whole(dv, "dv", dt, exact.kv, on), ws, nbytes,
+        _stream_of(stream, on.device)))
+    return dq, dk, dv
