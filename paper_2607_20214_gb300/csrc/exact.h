@@ -52,6 +52,9 @@ __device__ __forceinline__ int exact_most(const ExactSeq &s, int r0, int r1,
 }
 #endif
 
+// bf16 on the tensor cores; next_item: an int of scratch
+cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
+                                cudaStream_t st);
 // CUDA cores (fp32, and bf16 with impl = SIMT)
 cudaError_t launch_exact_fwd_simt(const ExactView &a, cudaStream_t st);
 cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys,

@@ -63,12 +63,18 @@ int make_view(const elsaa_exact *p, ExactView *a) {
     return ELSAA_OK;
 }
 
+bool on_tensor_cores(const elsaa_exact *p) {
+    return p->dtype == ELSAA_BF16 && p->impl == ELSAA_IMPL_AUTO;
+}
+
+// status and a work counter | D_i
 struct Layout {
-    size_t delta, total;
+    size_t next_item, delta, total;
 };
 Layout layout(const ExactView &a, bool backward) {
     Layout l;
-    l.delta = align256(sizeof(DeviceStatus));
+    l.next_item = sizeof(DeviceStatus);
+    l.delta = align256(l.next_item + sizeof(int));
     l.total = l.delta;
     if (backward)
         l.total += align256(sizeof(float) * (size_t)a.B * a.H * a.Nq);
@@ -125,7 +131,14 @@ extern "C" int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
     a.lse = lse;
     a.status = (DeviceStatus *)workspace;
     cudaStream_t st = (cudaStream_t)stream;
-    ELSAA_EXACT_LAUNCH("exact_fwd_simt", st, launch_exact_fwd_simt(a, st));
+    int *next_item =
+        (int *)((char *)workspace + layout(a, false).next_item);
+    if (on_tensor_cores(exact))
+        ELSAA_EXACT_LAUNCH("exact_fwd_tc", st,
+                           launch_exact_fwd_tc(a, next_item, st));
+    else
+        ELSAA_EXACT_LAUNCH("exact_fwd_simt", st,
+                           launch_exact_fwd_simt(a, st));
     return ELSAA_OK;
 }
 

@@ -1,0 +1,943 @@
+// The backward pass of exact attention on the tensor cores
+// (include/elsaa_exact.h), bf16. With s = scale Q K^T, P = exp(s - lse),
+// D_i = <dO_i, O_i>, dS = P (dO V^T - D):
+//     dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K.
+// Two kernels compute P and dS again, each for sums of its own: k_exact_dq_tc
+// holds 128 query rows and walks the keys, k_exact_dkv_tc holds 128 keys and
+// walks the query rows of every head that reads them. That is seven products
+// instead of five, but every sum stays in tensor memory, in one order: no fp32
+// dQ in memory, no atomics, the same bits on every call.
+#include <type_traits>
+
+#include "device_common.cuh"
+#include "exact.h"
+#include "tc_common.cuh"
+#include "tc_race.cuh"
+
+namespace elsaa {
+
+namespace {
+
+using namespace tc;
+
+// 384 x 168 registers at launch = 256 x 208 (weights) + 128 x 88
+constexpr int kEbThreads = 384;
+constexpr int kEbRegsSoft = 208, kEbRegsOther = 88;
+static_assert(256 * kEbRegsSoft + 128 * kEbRegsOther <= kEbThreads * 168,
+              "register shares within the launch's total");
+
+template <int D>
+constexpr int kPanels = D > 64 ? 2 : 1;
+template <int D>
+constexpr uint32_t kTileBytes = kPanels<D> * 16384;  // 128 rows
+
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t par,
+                                          volatile int *abort,
+                                          DeviceStatus *st, int site) {
+    return __all_sync(0xffffffffu,
+                      mbar_wait_or_abort(bar, par, abort, st, site));
+}
+
+// 64 columns of tensor memory
+__device__ __forceinline__ void load64(uint32_t t, float2 (&x)[32]) {
+    uint32_t a[32], b[32];
+    tmem_ld32(t, a);
+    tmem_ld32(t + 32, b);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        x[i] = make_float2(__uint_as_float(a[2 * i]),
+                           __uint_as_float(a[2 * i + 1]));
+        x[16 + i] = make_float2(__uint_as_float(b[2 * i]),
+                                __uint_as_float(b[2 * i + 1]));
+    }
+}
+// as bf16 (rounded to nearest) in 32 columns
+__device__ __forceinline__ void store64(uint32_t t, const float2 (&x)[32]) {
+    uint32_t y[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) y[i] = pack_bf16x2(x[i].x, x[i].y);
+    tmem_st32(t, y);
+    tmem_wait_st();
+}
+
+// One operand's product of K = D (both K-major) and of K = 128 (A from tensor
+// memory: columns 0..31 and 64..95, as the two halves' threads write them; B
+// MN-major), issued by one lane.
+template <int D>
+__device__ __forceinline__ void mma_scores(uint32_t dst, uint64_t a,
+                                           uint64_t b) {
+    const uint32_t id = idesc_bf16(128, 128, false, false);
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+        const uint32_t o = (x >> 2) * 1024 + (x & 3) * 2;
+        mma_ss(dst, a + o, b + o, id, x > 0);
+    }
+}
+template <int D>
+__device__ __forceinline__ void mma_sums(uint32_t dst, uint32_t a, uint64_t b,
+                                         bool more) {
+    const uint32_t id = idesc_bf16(128, D, false, true);
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+        mma_ts(dst, a + (x >> 2) * 64 + (x & 3) * 8, b + 128 * x, id,
+               x > 0 || more);
+}
+
+// Rows [part, 128) of a tile in shared memory become zeros (all lanes).
+template <int D>
+__device__ __forceinline__ void zero_rows(uint32_t tile, int part,
+                                          int lane_id) {
+    for (int i = max(part, 0) * 8 + lane_id; i < 1024; i += 32)
+        for (int p = 0; p < kPanels<D>; ++p)
+            st_shared_zero16(tile + p * 16384 + i * 16);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// D / 2 columns of sums in tensor memory, times f, to a row of bf16.
+template <int D>
+__device__ __forceinline__ void store_sums(uint32_t t, float f, uint16_t *o,
+                                           bool valid) {
+#pragma unroll
+    for (int c = 0; c < D / 2; c += 16) {
+        uint32_t x[16], y[8];
+        tmem_ld16(t + c, x);
+        tmem_wait_ld();
+        if (!valid) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            y[e] = pack_bf16x2(__uint_as_float(x[2 * e]) * f,
+                               __uint_as_float(x[2 * e + 1]) * f);
+        reinterpret_cast<uint4 *>(o + c)[0] =
+            make_uint4(y[0], y[1], y[2], y[3]);
+        reinterpret_cast<uint4 *>(o + c)[1] =
+            make_uint4(y[4], y[5], y[6], y[7]);
+    }
+}
+template <int D>
+__device__ __forceinline__ void store_zeros(uint16_t *o) {
+#pragma unroll
+    for (int c = 0; c < D / 2; c += 8)
+        *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
+}
+
+// D_i = <dO_i, O_i>, D / 8 lanes a row; clears the status and two counters.
+template <int D>
+__global__ void __launch_bounds__(256)
+    k_exact_delta(const __grid_constant__ ExactView a, int *counters) {
+    wait_for_stream();
+    constexpr int L = D / 8;
+    if (blockIdx.x == 0 && threadIdx.x < 6)
+        (threadIdx.x < 4 ? &a.status->code + threadIdx.x
+                         : counters + threadIdx.x - 4)[0] = 0;
+    const long row = ((long)blockIdx.x * 256 + threadIdx.x) / L;
+    const int c = threadIdx.x % L * 8;
+    if (row >= (long)a.B * a.H * a.Nq) return;
+    const int b = (int)(row / ((long)a.H * a.Nq)), i = (int)(row % a.Nq);
+    float t = 0.0f;
+    if (i < ExactSeq(a, b).ql) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(
+            (const uint16_t *)a.d_o + row * D + c);
+        const uint4 y = *reinterpret_cast<const uint4 *>(
+            (const uint16_t *)a.o + row * D + c);
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            t = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(w[e] << 16),
+                     t);
+            t = fmaf(__uint_as_float(u[e] & 0xffff0000u),
+                     __uint_as_float(w[e] & 0xffff0000u), t);
+        }
+    }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1)
+        t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (c == 0) a.delta[row] = t;
+}
+
+// ------------------------------------------------------------------- dQ
+
+constexpr int kDqK = 3, kDqV = 2;  // key and value tiles held
+
+struct DqBars {
+    uint64_t item_full[2], item_empty[2], q_full, q_empty;
+    uint64_t k_full[kDqK], k_empty[kDqK], v_full[kDqV], v_empty[kDqV];
+    uint64_t s_full[2], dp_full, dp_read, ds_full[2], dq_full, dq_empty;
+};
+struct BwdItem {
+    int item;  // -1: no more
+    int b, kvh, r0;
+    int ql, kl;
+    int n;     // tiles to walk
+    int first; // keys held: the first query row that sees one
+};
+
+// A CTA holds Q and dO of 128 rows (of the heads that share a K/V head,
+// counted through) and walks key tiles. Warps 0-7: weights, two threads a row,
+// one for keys 0..63 of a tile, one for 64..127; warp 8 issues the products;
+// warp 9 takes the items and loads. Tensor memory: S of two tiles, dP, dQ; dS
+// goes over the S it came from.
+template <int D>
+__global__ void __launch_bounds__(kEbThreads, 1)
+    k_exact_dq_tc(const __grid_constant__ CUtensorMap tmQ,
+                  const __grid_constant__ CUtensorMap tmG,
+                  const __grid_constant__ CUtensorMap tmK,
+                  const __grid_constant__ CUtensorMap tmV,
+                  const __grid_constant__ ExactView a, int per_head,
+                  int tiles, int items, int *__restrict__ next_item) {
+    wait_for_stream();
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ DqBars bars;
+    __shared__ uint32_t tbase;
+    __shared__ int abort_flag;
+    __shared__ BwdItem item_s[2];
+    volatile int *abort = &abort_flag;
+    constexpr uint32_t kTile = kTileBytes<D>;
+    constexpr uint32_t kS = 0, kP = 256, kO = 384;  // tensor memory columns
+    const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
+    const uint32_t sQ = align1k(smem_u32(smem_raw)), sG = sQ + kTile;
+    const uint32_t sK = sG + kTile, sV = sK + kDqK * kTile;
+    DeviceStatus *status = a.status;
+
+    if (warp == 8) tmem_alloc(&tbase, 512);
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&bars.item_full[s], 1);
+            mbar_init(&bars.item_empty[s], 9);
+            mbar_init(&bars.s_full[s], 1);
+            mbar_init(&bars.ds_full[s], 256);
+        }
+        for (int s = 0; s < kDqK; ++s) {
+            mbar_init(&bars.k_full[s], 1);
+            mbar_init(&bars.k_empty[s], 1);
+        }
+        for (int s = 0; s < kDqV; ++s) {
+            mbar_init(&bars.v_full[s], 1);
+            mbar_init(&bars.v_empty[s], 1);
+        }
+        mbar_init(&bars.q_full, 1);
+        mbar_init(&bars.q_empty, 1);
+        mbar_init(&bars.dp_full, 1);
+        mbar_init(&bars.dp_read, 256);
+        mbar_init(&bars.dq_full, 1);
+        mbar_init(&bars.dq_empty, 256);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tm = tbase;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
+            kEbRegsOther));
+        if (warp == 9 && lane_id == 0) {
+            // ---------------------------------------------- items and loads
+            int c = 0, qs = 0;  // key tiles and items loaded so far
+            bool ok = true;
+            const int heads = a.B * a.Hkv, rows = a.G * a.Nq;
+            auto tile = [&](uint64_t *full, uint32_t dst,
+                            const CUtensorMap *map, int row) {
+                for (int p = 0; p < kPanels<D>; ++p)
+                    tma_load_2d(dst + p * 16384, map, 64 * p, row, full);
+            };
+            for (int it = 0; ok; ++it) {
+                const long item =
+                    it == 0 ? blockIdx.x
+                            : (long)gridDim.x + atomicAdd(next_item, 1);
+                if (it >= 2 && !mbar_wait_or_abort(&bars.item_empty[it & 1],
+                                                   ((it >> 1) - 1) & 1, abort,
+                                                   status, 420))
+                    break;
+                BwdItem w = {-1};
+                if (item < items) {
+                    // the last rows of every query head, which see most, first
+                    const int h = (int)(item % heads);
+                    const int t = (int)(item / heads);
+                    const int x = t % a.G * per_head + per_head - 1 - t / a.G;
+                    w.item = (int)item;
+                    w.r0 = x * 128;
+                    w.b = h / a.Hkv;
+                    w.kvh = h - w.b * a.Hkv;
+                    const ExactSeq seq(a, w.b);
+                    w.ql = seq.ql;
+                    w.kl = seq.kl;
+                    if (x < tiles)
+                        w.n = (exact_most(seq, w.r0, min(w.r0 + 128, rows),
+                                          a.Nq) + 127) / 128;
+                }
+                item_s[it & 1] = w;
+                mbar_arrive(&bars.item_full[it & 1]);
+                if (w.item < 0) break;
+                if (w.n == 0) continue;
+                if (qs >= 1 && !mbar_wait_or_abort(&bars.q_empty, (qs - 1) & 1,
+                                                   abort, status, 421))
+                    break;
+                ++qs;
+                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq + w.r0;
+                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
+                mbar_expect_tx(&bars.q_full, 2 * kTile);
+                tile(&bars.q_full, sQ, &tmQ, q0);
+                tile(&bars.q_full, sG, &tmG, q0);
+                for (int kt = 0; kt < w.n; ++kt, ++c) {
+                    const int ks = c % kDqK, vs = c % kDqV;
+                    if (c >= kDqK &&
+                        !(ok = mbar_wait_or_abort(&bars.k_empty[ks],
+                                                  (c / kDqK - 1) & 1, abort,
+                                                  status, 422)))
+                        break;
+                    mbar_expect_tx(&bars.k_full[ks], kTile);
+                    tile(&bars.k_full[ks], sK + ks * kTile, &tmK,
+                         k0 + 128 * kt);
+                    if (c >= kDqV &&
+                        !(ok = mbar_wait_or_abort(&bars.v_empty[vs],
+                                                  (c / kDqV - 1) & 1, abort,
+                                                  status, 423)))
+                        break;
+                    mbar_expect_tx(&bars.v_full[vs], kTile);
+                    tile(&bars.v_full[vs], sV + vs * kTile, &tmV,
+                         k0 + 128 * kt);
+                }
+            }
+        } else if (warp == 8) {
+            // ---------------------------------------------------- MMA issue
+            // In the order S(j+2), dP(j+1), dQ(j): the weights of tile j are
+            // made while the products around them run. S(j+2) goes over dS(j)
+            // behind dQ(j), which reads it: products of one thread run in the
+            // order of their issue.
+            const bool el = elect_one();
+            auto wait = [&](uint64_t *bar, uint32_t par, int site) {
+                return warp_wait(bar, par, abort, status, site);
+            };
+            const uint64_t dQ = smem_desc(sQ, 16, 1024);
+            const uint64_t dG = smem_desc(sG, 16, 1024);
+            const uint64_t dK = smem_desc(sK, 16, 1024);
+            const uint64_t dKm = smem_desc(sK, 16384, 1024);
+            const uint64_t dV = smem_desc(sV, 16, 1024);
+            int c = 0, qs = 0;  // tiles of earlier items, items
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 424)) break;
+                const BwdItem w = item_s[it & 1];
+                __syncwarp();
+                if (el) mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int n = w.n;
+                if (n == 0) continue;
+                if (!wait(&bars.q_full, qs & 1, 425)) break;
+                auto scores = [&](int j) {
+                    const int x = c + j, ks = x % kDqK;
+                    if (!wait(&bars.k_full[ks], x / kDqK & 1, 426))
+                        return false;
+                    // keys that the sequence does not have count with dS = 0
+                    // in dQ and must be numbers
+                    if (w.kl - 128 * j < 128)
+                        zero_rows<D>(sK + ks * kTile, w.kl - 128 * j, lane_id);
+                    tc_fence_after();
+                    if (el) {
+                        mma_scores<D>(tm + kS + 128 * (x & 1), dQ,
+                                      desc_at(dK, ks * kTile));
+                        mma_commit(&bars.s_full[x & 1]);
+                    }
+                    return true;
+                };
+                auto products = [&](int j) {
+                    const int x = c + j, vs = x % kDqV;
+                    if (!wait(&bars.v_full[vs], x / kDqV & 1, 427))
+                        return false;
+                    if (x > 0 && !wait(&bars.dp_read, (x - 1) & 1, 428))
+                        return false;
+                    tc_fence_after();
+                    if (el) {
+                        mma_scores<D>(tm + kP, dG, desc_at(dV, vs * kTile));
+                        mma_commit(&bars.dp_full);
+                        mma_commit(&bars.v_empty[vs]);
+                        if (j == n - 1) mma_commit(&bars.q_empty);
+                    }
+                    return true;
+                };
+                ok = scores(0) && (n < 2 || scores(1)) && products(0);
+                if (ok && qs > 0)
+                    ok = wait(&bars.dq_empty, (qs - 1) & 1, 429);
+                for (int j = 0; j < n && ok; ++j) {
+                    const int x = c + j, ks = x % kDqK;
+                    if (j + 1 < n && !(ok = products(j + 1))) break;
+                    ok = wait(&bars.ds_full[x & 1], x / 2 & 1, 430);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (el) {
+                        mma_sums<D>(tm + kO, tm + kS + 128 * (x & 1),
+                                    desc_at(dKm, ks * kTile), j > 0);
+                        mma_commit(&bars.k_empty[ks]);
+                        if (j == n - 1) mma_commit(&bars.dq_full);
+                    }
+                    if (j + 2 < n) ok = scores(j + 2);
+                }
+                c += n;
+                ++qs;
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------- weights
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEbRegsSoft));
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane_id;
+        const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t0 = tm + lane + 64 * half;
+        const float sl2 = a.scale * kLog2e;
+        const float2 sl22 = make_float2(sl2, sl2);
+        int c = 0, qs = 0;
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            if (!warp_wait(&bars.item_full[it & 1], (it >> 1) & 1, abort,
+                           status, 431))
+                break;
+            const BwdItem w = item_s[it & 1];
+            __syncwarp();
+            if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
+            if (w.item < 0) break;
+            const int r = w.r0 + row, i = r % a.Nq;
+            const bool valid = r < a.G * a.Nq && i < w.ql;
+            const size_t at = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq + r;
+            uint16_t *o = (uint16_t *)a.dq + at * D + D / 2 * half;
+            if (w.n == 0) {
+                if (valid) store_zeros<D>(o);
+                continue;
+            }
+            int seen = 0;
+            float nl = 0.0f, nd = 0.0f;
+            if (valid) {
+                seen = a.causal ? max(0, min(w.kl, i + 1 + w.kl - w.ql))
+                                : w.kl;
+                nl = -a.lse[at] * kLog2e;
+                nd = -a.delta[at];
+            }
+            const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(nd, nd);
+            for (int j = 0; j < w.n; ++j, ++c) {
+                if (!(ok = warp_wait(&bars.s_full[c & 1], c / 2 & 1, abort,
+                                     status, 432)))
+                    break;
+                tc_fence_after();
+                const uint32_t tS = t0 + kS + 128 * (c & 1);
+                float2 p[32], g[32];
+                load64(tS, p);
+#pragma unroll
+                for (int q = 0; q < 32; ++q) {
+                    p[q] = fma2(p[q], sl22, nl2);
+                    p[q] = make_float2(ex2_approx(p[q].x), ex2_approx(p[q].y));
+                }
+                if (!(ok = warp_wait(&bars.dp_full, c & 1, abort, status,
+                                     433)))
+                    break;
+                tc_fence_after();
+                load64(t0 + kP, g);
+                tc_fence_before();
+                mbar_arrive(&bars.dp_read);
+#pragma unroll
+                for (int q = 0; q < 32; ++q)
+                    g[q] = mul2(p[q], add2(g[q], nd2));
+                const int lim = seen - 128 * j - 64 * half;
+                if (__any_sync(0xffffffffu, lim < 64)) {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {
+                        if (2 * q >= lim) g[q].x = 0.0f;
+                        if (2 * q + 1 >= lim) g[q].y = 0.0f;
+                    }
+                }
+                store64(tS, g);
+                tc_fence_before();
+                mbar_arrive(&bars.ds_full[c & 1]);
+            }
+            if (!ok) break;
+            if (!(ok = warp_wait(&bars.dq_full, qs & 1, abort, status, 434)))
+                break;
+            ++qs;
+            tc_fence_after();
+            store_sums<D>(tm + lane + kO + D / 2 * half, a.scale, o, valid);
+            tc_fence_before();
+            mbar_arrive(&bars.dq_empty);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tm, 512);
+}
+
+// --------------------------------------------------------------- dK and dV
+
+template <int D>
+struct Dkv {
+    static constexpr int kS = D > 64 ? 1 : 2;  // S in tensor memory
+    // query tiles and dO tiles held: Q(j) serves S(j) and dK(j), behind
+    // S(j + kS)
+    static constexpr int kQ = D > 64 ? 2 : 4, kG = 2;
+    static constexpr uint32_t cS = 0, cP = 128 * kS, cV = cP + 128,
+                              cK = cV + D;
+};
+template <int D>
+struct DkvBars {
+    uint64_t item_full[2], item_empty[2], kv_full, kv_empty;
+    uint64_t q_full[Dkv<D>::kQ], q_empty[Dkv<D>::kQ];
+    uint64_t g_full[2], g_empty[2], l_full[2], l_empty[2];
+    uint64_t s_full[2], p_full[2], dp_full, ds_full, sum_full, sum_empty;
+};
+
+// A CTA holds K and V of 128 rows and walks tiles of 128 query rows of every
+// head that reads them; scores and weights stand transposed, a key a lane.
+// Warps 0-7: weights, two threads a key, for queries 0..63 and 64..127 of a
+// tile; warp 8 issues the products; warp 9 takes the items and loads; warp 10
+// fetches the rows' lse and D. Tensor memory: S^T (two for D <= 64), dP^T, dV,
+// dK; P^T and dS^T go over the S^T and dP^T that they came from.
+template <int D>
+__global__ void __launch_bounds__(kEbThreads, 1)
+    k_exact_dkv_tc(const __grid_constant__ CUtensorMap tmQ,
+                   const __grid_constant__ CUtensorMap tmG,
+                   const __grid_constant__ CUtensorMap tmK,
+                   const __grid_constant__ CUtensorMap tmV,
+                   const __grid_constant__ ExactView a, int items,
+                   int *__restrict__ next_item) {
+    wait_for_stream();
+    using X = Dkv<D>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ DkvBars<D> bars;
+    __shared__ uint32_t tbase;
+    __shared__ int abort_flag;
+    __shared__ BwdItem item_s[2];
+    __shared__ __align__(16) float row_l[2][128], row_d[2][128];
+    volatile int *abort = &abort_flag;
+    constexpr uint32_t kTile = kTileBytes<D>;
+    const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
+    const uint32_t sK = align1k(smem_u32(smem_raw)), sV = sK + kTile;
+    const uint32_t sQ = sV + kTile, sG = sQ + X::kQ * kTile;
+    DeviceStatus *status = a.status;
+
+    if (warp == 8) tmem_alloc(&tbase, 512);
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&bars.item_full[s], 1);
+            mbar_init(&bars.item_empty[s], 10);
+            mbar_init(&bars.g_full[s], 1);
+            mbar_init(&bars.g_empty[s], 1);
+            mbar_init(&bars.l_full[s], 32);
+            mbar_init(&bars.l_empty[s], 8);
+            mbar_init(&bars.s_full[s], 1);
+            mbar_init(&bars.p_full[s], 256);
+        }
+        for (int s = 0; s < X::kQ; ++s) {
+            mbar_init(&bars.q_full[s], 1);
+            mbar_init(&bars.q_empty[s], 1);
+        }
+        mbar_init(&bars.kv_full, 1);
+        mbar_init(&bars.kv_empty, 1);
+        mbar_init(&bars.dp_full, 1);
+        mbar_init(&bars.ds_full, 256);
+        mbar_init(&bars.sum_full, 1);
+        mbar_init(&bars.sum_empty, 256);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tm = tbase;
+    // tile t of an item: rows of the query head t / per, from row i0
+    auto tiles_of = [](const BwdItem &w) {
+        return (w.ql - w.first + 127) / 128;
+    };
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
+            kEbRegsOther));
+        if (warp == 9 && lane_id == 0) {
+            // ---------------------------------------------- items and loads
+            int c = 0, ks = 0;  // query tiles and items loaded so far
+            bool ok = true;
+            const int heads = a.B * a.Hkv;
+            auto tile = [&](uint64_t *full, uint32_t dst,
+                            const CUtensorMap *map, int row) {
+                for (int p = 0; p < kPanels<D>; ++p)
+                    tma_load_2d(dst + p * 16384, map, 64 * p, row, full);
+            };
+            for (int it = 0; ok; ++it) {
+                const long item =
+                    it == 0 ? blockIdx.x
+                            : (long)gridDim.x + atomicAdd(next_item, 1);
+                if (it >= 2 && !mbar_wait_or_abort(&bars.item_empty[it & 1],
+                                                   ((it >> 1) - 1) & 1, abort,
+                                                   status, 440))
+                    break;
+                BwdItem w = {-1};
+                if (item < items) {
+                    // the first keys, which are seen most, first
+                    const int h = (int)(item % heads);
+                    w.item = (int)item;
+                    w.r0 = (int)(item / heads) * 128;
+                    w.b = h / a.Hkv;
+                    w.kvh = h - w.b * a.Hkv;
+                    const ExactSeq seq(a, w.b);
+                    w.ql = seq.ql;
+                    w.kl = seq.kl;
+                    w.first = seq.first_row(w.r0);
+                    w.n = a.G * tiles_of(w);
+                }
+                item_s[it & 1] = w;
+                mbar_arrive(&bars.item_full[it & 1]);
+                if (w.item < 0) break;
+                if (w.n == 0) continue;
+                if (ks >= 1 && !mbar_wait_or_abort(&bars.kv_empty,
+                                                   (ks - 1) & 1, abort,
+                                                   status, 441))
+                    break;
+                ++ks;
+                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk + w.r0;
+                mbar_expect_tx(&bars.kv_full, 2 * kTile);
+                tile(&bars.kv_full, sK, &tmK, k0);
+                tile(&bars.kv_full, sV, &tmV, k0);
+                const int per = tiles_of(w);
+                for (int t = 0; t < w.n; ++t, ++c) {
+                    const int qs = c % X::kQ, gs = c % X::kG;
+                    const int row =
+                        (w.b * a.H + w.kvh * a.G + t / per) * a.Nq + w.first +
+                        t % per * 128;
+                    if (c >= X::kQ &&
+                        !(ok = mbar_wait_or_abort(&bars.q_empty[qs],
+                                                  (c / X::kQ - 1) & 1, abort,
+                                                  status, 442)))
+                        break;
+                    mbar_expect_tx(&bars.q_full[qs], kTile);
+                    tile(&bars.q_full[qs], sQ + qs * kTile, &tmQ, row);
+                    if (c >= X::kG &&
+                        !(ok = mbar_wait_or_abort(&bars.g_empty[gs],
+                                                  (c / X::kG - 1) & 1, abort,
+                                                  status, 443)))
+                        break;
+                    mbar_expect_tx(&bars.g_full[gs], kTile);
+                    tile(&bars.g_full[gs], sG + gs * kTile, &tmG, row);
+                }
+            }
+        } else if (warp == 8) {
+            // ---------------------------------------------------- MMA issue
+            // In the order dV(t), S(t + kS), dK(t), dP(t + 1): P(t + 1) is
+            // made during dK(t) and dP(t + 1), dS(t) during dV(t) and
+            // S(t + kS). Products of one thread run in the order of their
+            // issue, which S over P and dP over dS rely on.
+            const bool el = elect_one();
+            auto wait = [&](uint64_t *bar, uint32_t par, int site) {
+                return warp_wait(bar, par, abort, status, site);
+            };
+            const uint64_t dK = smem_desc(sK, 16, 1024);
+            const uint64_t dV = smem_desc(sV, 16, 1024);
+            const uint64_t dQ = smem_desc(sQ, 16, 1024);
+            const uint64_t dQm = smem_desc(sQ, 16384, 1024);
+            const uint64_t dG = smem_desc(sG, 16, 1024);
+            const uint64_t dGm = smem_desc(sG, 16384, 1024);
+            int c = 0, ks = 0;
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 444)) break;
+                const BwdItem w = item_s[it & 1];
+                __syncwarp();
+                if (el) mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int n = w.n;
+                if (n == 0) continue;
+                if (!wait(&bars.kv_full, ks & 1, 445)) break;
+                const int per = tiles_of(w);
+                // rows that the sequence does not have count with weights of
+                // 0 and must be numbers
+                auto part = [&](int t) {
+                    return w.ql - w.first - t % per * 128;
+                };
+                auto scores = [&](int t) {
+                    const int x = c + t, qs = x % X::kQ;
+                    if (!wait(&bars.q_full[qs], x / X::kQ & 1, 446))
+                        return false;
+                    if (part(t) < 128)
+                        zero_rows<D>(sQ + qs * kTile, part(t), lane_id);
+                    tc_fence_after();
+                    if (el) {
+                        mma_scores<D>(tm + X::cS + 128 * (x % X::kS), dK,
+                                      desc_at(dQ, qs * kTile));
+                        mma_commit(&bars.s_full[x % X::kS]);
+                    }
+                    return true;
+                };
+                auto products = [&](int t) {
+                    const int x = c + t, gs = x % X::kG;
+                    if (!wait(&bars.g_full[gs], x / X::kG & 1, 447))
+                        return false;
+                    if (part(t) < 128)
+                        zero_rows<D>(sG + gs * kTile, part(t), lane_id);
+                    tc_fence_after();
+                    if (el) {
+                        mma_scores<D>(tm + X::cP, dV, desc_at(dG, gs * kTile));
+                        mma_commit(&bars.dp_full);
+                        if (t == n - 1) mma_commit(&bars.kv_empty);
+                    }
+                    return true;
+                };
+                ok = scores(0) && products(0) &&
+                     (X::kS < 2 || n < 2 || scores(1));
+                if (ok && ks > 0)
+                    ok = wait(&bars.sum_empty, (ks - 1) & 1, 448);
+                for (int t = 0; t < n && ok; ++t) {
+                    const int x = c + t, qs = x % X::kQ, gs = x % X::kG;
+                    ok = wait(&bars.p_full[x % X::kS], x / X::kS & 1, 449);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (el) {
+                        mma_sums<D>(tm + X::cV,
+                                    tm + X::cS + 128 * (x % X::kS),
+                                    desc_at(dGm, gs * kTile), t > 0);
+                        mma_commit(&bars.g_empty[gs]);
+                    }
+                    if (t + X::kS < n && !(ok = scores(t + X::kS))) break;
+                    ok = wait(&bars.ds_full, x & 1, 450);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (el) {
+                        mma_sums<D>(tm + X::cK, tm + X::cP,
+                                    desc_at(dQm, qs * kTile), t > 0);
+                        mma_commit(&bars.q_empty[qs]);
+                        if (t == n - 1) mma_commit(&bars.sum_full);
+                    }
+                    if (t + 1 < n) ok = products(t + 1);
+                }
+                c += n;
+                ++ks;
+            }
+        } else if (warp == 10) {
+            // ------------------------------------------------- lse and D
+            int c = 0;
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!warp_wait(&bars.item_full[it & 1], (it >> 1) & 1, abort,
+                               status, 451))
+                    break;
+                const BwdItem w = item_s[it & 1];
+                __syncwarp();
+                if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int per = tiles_of(w);
+                for (int t = 0; t < w.n; ++t, ++c) {
+                    const int i0 = w.first + t % per * 128;
+                    const size_t at =
+                        (size_t)(w.b * a.H + w.kvh * a.G + t / per) * a.Nq +
+                        i0;
+                    float l[4], d[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int i = lane_id + 32 * q;
+                        l[q] = d[q] = 0.0f;
+                        if (i0 + i < w.ql) {
+                            l[q] = a.lse[at + i];
+                            d[q] = a.delta[at + i];
+                        }
+                    }
+                    if (c >= 2 && !(ok = warp_wait(&bars.l_empty[c & 1],
+                                                   (c / 2 - 1) & 1, abort,
+                                                   status, 452)))
+                        break;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        row_l[c & 1][lane_id + 32 * q] = -l[q] * kLog2e;
+                        row_d[c & 1][lane_id + 32 * q] = -d[q];
+                    }
+                    mbar_arrive(&bars.l_full[c & 1]);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------- weights
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEbRegsSoft));
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane_id;
+        const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t0 = tm + lane + 64 * half;
+        const float sl2 = a.scale * kLog2e;
+        const float2 sl22 = make_float2(sl2, sl2);
+        int c = 0, ks = 0;
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            if (!warp_wait(&bars.item_full[it & 1], (it >> 1) & 1, abort,
+                           status, 453))
+                break;
+            const BwdItem w = item_s[it & 1];
+            __syncwarp();
+            if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
+            if (w.item < 0) break;
+            const int j = w.r0 + row;
+            const bool valid = j < w.kl;
+            const size_t at =
+                ((size_t)(w.b * a.Hkv + w.kvh) * a.Nk + j) * D + D / 2 * half;
+            uint16_t *ok_ = (uint16_t *)a.dk + at, *ov = (uint16_t *)a.dv + at;
+            if (w.n == 0) {
+                if (valid) {
+                    store_zeros<D>(ok_);
+                    store_zeros<D>(ov);
+                }
+                continue;
+            }
+            // the first query row that sees the key, none: ql
+            const int first = !valid ? w.ql
+                              : a.causal ? min(w.ql, max(0, j + w.ql - w.kl))
+                                         : 0;
+            const int per = tiles_of(w);
+            for (int t = 0; t < w.n; ++t, ++c) {
+                const int i0 = w.first + t % per * 128 + 64 * half;
+                const int lo = first - i0, hi = w.ql - i0;
+                const bool edge =
+                    __any_sync(0xffffffffu, lo > 0 || hi < 64);
+                if (!(ok = warp_wait(&bars.l_full[c & 1], c / 2 & 1, abort,
+                                     status, 454)) ||
+                    !(ok = warp_wait(&bars.s_full[c % X::kS], c / X::kS & 1,
+                                     abort, status, 455)))
+                    break;
+                tc_fence_after();
+                const uint32_t tS = t0 + X::cS + 128 * (c % X::kS);
+                const float4 *nl = reinterpret_cast<const float4 *>(
+                    &row_l[c & 1][64 * half]);
+                const float4 *nd = reinterpret_cast<const float4 *>(
+                    &row_d[c & 1][64 * half]);
+                float2 p[32], g[32];
+                load64(tS, p);
+#pragma unroll
+                for (int q = 0; q < 32; q += 2) {
+                    const float4 l = nl[q / 2];
+                    p[q] = fma2(p[q], sl22, make_float2(l.x, l.y));
+                    p[q + 1] = fma2(p[q + 1], sl22, make_float2(l.z, l.w));
+                }
+#pragma unroll
+                for (int q = 0; q < 32; ++q)
+                    p[q] = make_float2(ex2_approx(p[q].x), ex2_approx(p[q].y));
+                if (edge) {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {
+                        if (2 * q < lo || 2 * q >= hi) p[q].x = 0.0f;
+                        if (2 * q + 1 < lo || 2 * q + 1 >= hi) p[q].y = 0.0f;
+                    }
+                }
+                store64(tS, p);
+                tc_fence_before();
+                mbar_arrive(&bars.p_full[c % X::kS]);
+                if (!(ok = warp_wait(&bars.dp_full, c & 1, abort, status,
+                                     456)))
+                    break;
+                tc_fence_after();
+                load64(t0 + X::cP, g);
+#pragma unroll
+                for (int q = 0; q < 32; q += 2) {
+                    const float4 d = nd[q / 2];
+                    g[q] = mul2(p[q], add2(g[q], make_float2(d.x, d.y)));
+                    g[q + 1] =
+                        mul2(p[q + 1], add2(g[q + 1], make_float2(d.z, d.w)));
+                }
+                if (edge) {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {
+                        if (2 * q < lo || 2 * q >= hi) g[q].x = 0.0f;
+                        if (2 * q + 1 < lo || 2 * q + 1 >= hi) g[q].y = 0.0f;
+                    }
+                }
+                store64(t0 + X::cP, g);
+                tc_fence_before();
+                mbar_arrive(&bars.ds_full);
+                __syncwarp();
+                if (lane_id == 0) mbar_arrive(&bars.l_empty[c & 1]);
+            }
+            if (!ok) break;
+            if (!(ok = warp_wait(&bars.sum_full, ks & 1, abort, status, 457)))
+                break;
+            ++ks;
+            tc_fence_after();
+            const uint32_t t = tm + lane + D / 2 * half;
+            store_sums<D>(t + X::cV, 1.0f, ov, valid);
+            store_sums<D>(t + X::cK, a.scale, ok_, valid);
+            tc_fence_before();
+            mbar_arrive(&bars.sum_empty);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tm, 512);
+}
+
+struct Maps {
+    CUtensorMap q, g, k, v;
+};
+cudaError_t make_maps(const ExactView &a, Maps *m) {
+    const uint64_t nq = (uint64_t)a.B * a.H * a.Nq;
+    const uint64_t nk = (uint64_t)a.B * a.Hkv * a.Nk;
+    cudaError_t e = make_tma_map_bf16(&m->q, a.q, nq, a.d, 128);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&m->g, a.d_o, nq, a.d, 128);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&m->k, a.k, nk, a.d, 128);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&m->v, a.v, nk, a.d, 128);
+    return e;
+}
+int sm_count() {
+    int dev = 0, sms = 152;
+    if (cudaGetDevice(&dev) == cudaSuccess)
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return sms;
+}
+template <typename F>
+cudaError_t by_width(int d, F f) {
+    return d == 128  ? f(std::integral_constant<int, 128>{})
+           : d == 64 ? f(std::integral_constant<int, 64>{})
+                     : f(std::integral_constant<int, 32>{});
+}
+
+}  // namespace
+
+cudaError_t launch_exact_delta(const ExactView &a, int *counters,
+                               cudaStream_t st) {
+    const long threads = (long)a.B * a.H * a.Nq * (a.d / 8);
+    return by_width(a.d, [&](auto dim) {
+        return launch_after(k_exact_delta<decltype(dim)::value>,
+                            dim3((unsigned)((threads + 255) / 256)), 256, 0,
+                            st, a, counters);
+    });
+}
+
+cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
+                               cudaStream_t st) {
+    const int tiles = (int)(((long)a.G * a.Nq + 127) / 128);
+    const int per_head = (tiles + a.G - 1) / a.G;
+    const long items = (long)per_head * a.G * a.B * a.Hkv;
+    const int sms = sm_count();
+    Maps m;
+    const cudaError_t e = make_maps(a, &m);
+    if (e != cudaSuccess) return e;
+    return by_width(a.d, [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        const size_t smem =
+            1024 + (size_t)(2 + kDqK + kDqV) * kTileBytes<D>;
+        return launch_after(
+            k_exact_dq_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
+            kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, per_head, tiles,
+            (int)items, next_item);
+    });
+}
+
+cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
+                                cudaStream_t st) {
+    const long items = (long)((a.Nk + 127) / 128) * a.B * a.Hkv;
+    const int sms = sm_count();
+    Maps m;
+    const cudaError_t e = make_maps(a, &m);
+    if (e != cudaSuccess) return e;
+    return by_width(a.d, [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        const size_t smem =
+            1024 + (size_t)(2 + Dkv<D>::kQ + Dkv<D>::kG) * kTileBytes<D>;
+        return launch_after(
+            k_exact_dkv_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
+            kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, (int)items,
+            next_item);
+    });
+}
+
+}  // namespace elsaa

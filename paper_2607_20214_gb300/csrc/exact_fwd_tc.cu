@@ -1,0 +1,514 @@
+// Exact attention on the tensor cores (include/elsaa_exact.h), bf16: one pass
+// over the keys with the running maximum and sum of the softmax.
+//
+// The query rows of the heads that share a K/V head are counted through (row r
+// is row r mod N of head r / N), so that a tile of short sequences is filled by
+// several heads. An item is 256 such rows, two slots of 128, over the keys that
+// they see; the slots share every key and value tile. Roles:
+//   warps 0-3, 4-7  softmax of slot 0 / 1: one thread per query row holds all
+//                   128 scores of a key tile in registers, so neither the row
+//                   maximum nor the sum needs another thread
+//   warp 8          issues every MMA: S = Q K^T, O += P V (P from TMEM)
+//   warp 9          takes the items, TMA loads of Q, K and V
+// TMEM: S_s at 128 s, O_s at 256 + 128 s, P_s behind O_s for D <= 64, over S_s
+// at D = 128. O stays in tensor memory; a softmax warp rescales it when the
+// maximum of one of its rows grows.
+#include <type_traits>
+
+#include "device_common.cuh"
+#include "exact.h"
+#include "tc_common.cuh"
+#include "tc_race.cuh"
+
+namespace elsaa {
+
+namespace {
+
+using namespace tc;
+
+// 384 x 168 registers at launch = 256 x 208 (softmax) + 128 x 88
+constexpr int kEfThreads = 384;
+constexpr int kEfRegsSoft = 208, kEfRegsOther = 88;
+static_assert(256 * kEfRegsSoft + 128 * kEfRegsOther <= kEfThreads * 168,
+              "register shares within the launch's total");
+constexpr int kEfStages = 2;  // key and value tiles held
+// a maximum below every score of a finite product
+constexpr float kLowest = -1e38f;
+
+struct EfBars {
+    uint64_t item_full[2], item_empty[2], q_full, q_empty;
+    uint64_t k_full[kEfStages], k_empty[kEfStages];
+    uint64_t v_full[kEfStages], v_empty[kEfStages];
+    uint64_t s_full[2], p_full[2], o_done[2], o_empty[2];
+};
+
+// What the roles know of an item.
+struct EfItem {
+    int item;   // -1: no more
+    int b, kvh, r0;
+    int ql, kl;
+    int n[2];   // key tiles of each slot
+};
+
+template <int D>
+__global__ void __launch_bounds__(kEfThreads, 1)
+    k_exact_fwd_tc(const __grid_constant__ CUtensorMap tmQ,
+                   const __grid_constant__ CUtensorMap tmK,
+                   const __grid_constant__ CUtensorMap tmV,
+                   const __grid_constant__ ExactView a, int tiles, int items,
+                   int *__restrict__ next_item) {
+    wait_for_stream();
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ EfBars bars;
+    __shared__ uint32_t tbase;
+    __shared__ int abort_flag;
+    __shared__ EfItem item_s[2];
+    volatile int *abort = &abort_flag;
+    // a row is D <= 64 elements of one 128-byte line, or two lines
+    constexpr int kPanels = D > 64 ? 2 : 1;
+    constexpr uint32_t kTileB = kPanels * 16384;
+    const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
+    const uint32_t sQ = align1k(smem_u32(smem_raw));
+    const uint32_t sK = sQ + 2 * kTileB, sV = sK + kEfStages * kTileB;
+    DeviceStatus *status = a.status;
+
+    if (!next_item && blockIdx.x == 0 && tid < 4)
+        (&status->code)[tid] = 0;  // a wait runs out much later
+    if (warp == 8) tmem_alloc(&tbase, 512);
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&bars.item_full[s], 1);
+            mbar_init(&bars.item_empty[s], 9);  // eight softmax warps, MMA
+            mbar_init(&bars.s_full[s], 1);
+            mbar_init(&bars.p_full[s], 128);
+            mbar_init(&bars.o_done[s], 1);
+            mbar_init(&bars.o_empty[s], 128);
+        }
+        for (int s = 0; s < kEfStages; ++s) {
+            mbar_init(&bars.k_full[s], 1);
+            mbar_init(&bars.k_empty[s], 1);
+            mbar_init(&bars.v_full[s], 1);
+            mbar_init(&bars.v_empty[s], 1);
+        }
+        mbar_init(&bars.q_full, 1);
+        mbar_init(&bars.q_empty, 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tm = tbase;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
+            kEfRegsOther));
+        if (warp == 9 && lane_id == 0) {
+            // ---------------------------------------------- items and loads
+            int c = 0;   // key tiles loaded so far
+            int qs = 0;  // items whose queries were loaded
+            bool ok = true;
+            auto load = [&](uint64_t *full, uint64_t *empty, uint32_t dst,
+                            const CUtensorMap *map, int row, int site) {
+                const int st = c % kEfStages;
+                if (c >= kEfStages &&
+                    !mbar_wait_or_abort(&empty[st], (c / kEfStages - 1) & 1,
+                                        abort, status, site))
+                    return false;
+                mbar_expect_tx(&full[st], kTileB);
+                for (int p = 0; p < kPanels; ++p)
+                    tma_load_2d(dst + st * kTileB + p * 16384, map, 64 * p,
+                                row, &full[st]);
+                return true;
+            };
+            const int heads = a.B * a.Hkv, rows = a.G * a.Nq;
+            for (int it = 0; ok; ++it) {
+                long item = blockIdx.x;
+                if (it > 0)
+                    item = next_item
+                               ? (long)gridDim.x + atomicAdd(next_item, 1)
+                               : items;
+                if (it >= 2 && !mbar_wait_or_abort(&bars.item_empty[it & 1],
+                                                   ((it >> 1) - 1) & 1, abort,
+                                                   status, 400))
+                    break;
+                EfItem w = {-1};
+                if (item < items) {
+                    // the last rows of every head, which see most, first
+                    const int h = (int)(item % heads);
+                    w.item = (int)item;
+                    w.r0 = (tiles - 1 - (int)(item / heads)) * 256;
+                    w.b = h / a.Hkv;
+                    w.kvh = h - w.b * a.Hkv;
+                    const ExactSeq seq(a, w.b);
+                    w.ql = seq.ql;
+                    w.kl = seq.kl;
+                    for (int s = 0; s < 2; ++s)
+                        w.n[s] = (exact_most(seq, w.r0 + 128 * s,
+                                             min(w.r0 + 128 * s + 128, rows),
+                                             a.Nq) + 127) / 128;
+                }
+                item_s[it & 1] = w;
+                mbar_arrive(&bars.item_full[it & 1]);
+                if (w.item < 0) break;
+                const int nk = max(w.n[0], w.n[1]);
+                if (nk == 0) continue;
+                if (qs >= 1 && !mbar_wait_or_abort(&bars.q_empty, (qs - 1) & 1,
+                                                   abort, status, 401))
+                    break;
+                ++qs;
+                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq + w.r0;
+                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
+                mbar_expect_tx(&bars.q_full,
+                               ((w.n[0] > 0) + (w.n[1] > 0)) * kTileB);
+                for (int s = 0; s < 2; ++s)
+                    for (int p = 0; p < kPanels && w.n[s] > 0; ++p)
+                        tma_load_2d(sQ + s * kTileB + p * 16384, &tmQ, 64 * p,
+                                    q0 + 128 * s, &bars.q_full);
+                for (int kt = 0; kt < nk && ok; ++kt, ++c)
+                    ok = load(bars.k_full, bars.k_empty, sK, &tmK,
+                              k0 + 128 * kt, 402) &&
+                         load(bars.v_full, bars.v_empty, sV, &tmV,
+                              k0 + 128 * kt, 403);
+            }
+        } else if (warp == 8) {
+            // ---------------------------------------------------- MMA issue
+            // Whenever a slot's P is ready: its P V product, and right behind
+            // it the scores of its next key tile; the softmax sees these only
+            // when both are complete (a commit covers all that was issued
+            // before it). At D = 128 the scores go over P, which relies on
+            // products of one thread running in the order of their issue.
+            // The whole warp runs the loop, so that its state and the
+            // operands' descriptors are warp-uniform; one lane issues.
+            const bool el = elect_one();
+            auto test = [&](uint64_t *bar, uint32_t par) -> bool {
+                return __all_sync(0xffffffffu, mbar_test(bar, par));
+            };
+            auto wait = [&](uint64_t *bar, uint32_t par, int site) -> bool {
+                return __all_sync(0xffffffffu,
+                                  mbar_wait_or_abort(bar, par, abort, status,
+                                                     site));
+            };
+            const uint32_t id_s = idesc_bf16(128, 128, false, false);
+            const uint32_t id_o = idesc_bf16(128, D, false, true);
+            const uint64_t dQ = smem_desc(sQ, 16, 1024);
+            const uint64_t dK = smem_desc(sK, 16, 1024);
+            const uint64_t dV = smem_desc(sV, 16384, 1024);
+            constexpr uint32_t kTile = kTileB >> 4;  // in descriptor units
+            int c0 = 0;                // key tiles of earlier items
+            int qs = 0;
+            int gp0 = 0, gp1 = 0;      // P V products issued per slot
+            int go0 = 0, go1 = 0;      // items finished per slot
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                ok = wait(&bars.item_full[it & 1], (it >> 1) & 1, 404);
+                if (!ok) break;
+                const EfItem w = item_s[it & 1];
+                __syncwarp();
+                if (el) mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int n0 = w.n[0], n1 = w.n[1], nk = max(n0, n1);
+                if (nk == 0) continue;
+                ok = wait(&bars.q_full, qs & 1, 405);
+                if (!ok) break;
+                ++qs;
+                int us0 = 0, us1 = 0, up0 = 0, up1 = 0;
+                // keys of the last tile that the sequence has: values of
+                // others count with weights of 0 and must be numbers
+                int part = w.kl - 128 * (nk - 1);
+                // the scores of slot s's next key tile
+                auto scores = [&](auto slot, int &us, int n, int us_o,
+                                  int n_o) {
+                    constexpr int s = decltype(slot)::value;
+                    const int st = (c0 + us) % kEfStages;
+                    if (!wait(&bars.k_full[st], (c0 + us) / kEfStages & 1,
+                              406))
+                        return false;
+                    tc_fence_after();
+                    const uint64_t q = dQ + s * kTile, k = dK + st * kTile;
+                    if (el) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const uint32_t o = (x >> 2) * 1024 + (x & 3) * 2;
+                            mma_ss(tm + 128u * s, q + o, k + o, id_s, x > 0);
+                        }
+                        mma_commit(&bars.s_full[s]);
+                        // both slots have used the tile
+                        if (us >= n_o || us_o > us)
+                            mma_commit(&bars.k_empty[st]);
+                        if (us + 1 == n && us_o == n_o)
+                            mma_commit(&bars.q_empty);
+                    }
+                    ++us;
+                    return true;
+                };
+                auto step = [&](auto slot, int &us, int &up, int &gp, int go,
+                                int n, int us_o, int up_o, int n_o) {
+                    constexpr int s = decltype(slot)::value;
+                    constexpr uint32_t cO = 128u * s + 256u;
+                    constexpr uint32_t cP = D <= 64 ? cO + 64 : 128u * s;
+                    const int st = (c0 + up) % kEfStages;
+                    if (up == us || !test(&bars.p_full[s], gp & 1) ||
+                        !test(&bars.v_full[st],
+                              (c0 + up) / kEfStages & 1) ||
+                        (up == 0 && go > 0 &&
+                         !test(&bars.o_empty[s], (go - 1) & 1)))
+                        return false;
+                    if (up == nk - 1 && part < 128) {
+                        const uint32_t v = sV + st * kTileB;
+                        for (int i = part * 8 + lane_id; i < 1024; i += 32)
+                            for (int p = 0; p < kPanels; ++p)
+                                st_shared_zero16(v + p * 16384 + i * 16);
+                        part = 128;  // once for both slots
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    tc_fence_after();
+                    const uint64_t v = dV + st * kTile;
+                    const uint32_t more = up > 0;
+                    if (el) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            mma_ts(tm + cO, tm + cP + 8 * x, v + 128 * x, id_o,
+                                   x > 0 ? 1u : more);
+                        mma_commit(&bars.o_done[s]);
+                        if (up >= n_o || up_o > up)
+                            mma_commit(&bars.v_empty[st]);
+                    }
+                    ++up;
+                    ++gp;
+                    if (us < n) ok = scores(slot, us, n, us_o, n_o);
+                    return true;
+                };
+                using S0 = std::integral_constant<int, 0>;
+                using S1 = std::integral_constant<int, 1>;
+                if (n0 > 0) ok = scores(S0{}, us0, n0, us1, n1);
+                if (ok && n1 > 0) ok = scores(S1{}, us1, n1, us0, n0);
+                unsigned long long t_last = 0;
+                uint32_t idle = 0;
+                while (ok && (up0 < n0 || up1 < n1)) {
+                    const bool x = step(S0{}, us0, up0, gp0, go0, n0, us1,
+                                        up1, n1);
+                    const bool y = ok && step(S1{}, us1, up1, gp1, go1, n1,
+                                              us0, up0, n0);
+                    if (x || y) {
+                        idle = 0;
+                    } else if ((++idle & 255u) == 0) {
+                        if (idle == 256u) t_last = global_ns();
+                        const bool late = global_ns() - t_last > kWaitLimitNs;
+                        if (late) {
+                            *abort = 1;
+                            record_timeout(status, 407);
+                        }
+                        ok = !__any_sync(0xffffffffu, late || *abort);
+                    }
+                }
+                c0 += nk;
+                go0 += n0 > 0;
+                go1 += n1 > 0;
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEfRegsSoft));
+        const int s = warp >> 2, row = (warp & 3) * 32 + lane_id;
+        const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t tS = tm + lane + 128u * s, tO = tS + 256u;
+        const uint32_t tP = D <= 64 ? tO + 64 : tS;
+        const float sl2 = a.scale * kLog2e;
+        const float2 sl22 = make_float2(sl2, sl2);
+        auto wwait = [=](uint64_t *bar, uint32_t par, int site) {
+            return __all_sync(0xffffffffu,
+                              mbar_wait_or_abort(bar, par, abort, status,
+                                                 site));
+        };
+        int g = 0;  // key tiles of this slot so far
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+            ok = wwait(&bars.item_full[it & 1], (it >> 1) & 1, 408);
+            if (!ok) break;
+            const EfItem w = item_s[it & 1];
+            __syncwarp();
+            if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
+            if (w.item < 0) break;
+            const int n = w.n[s];
+            const int r = w.r0 + 128 * s + row, i = r % a.Nq;
+            const bool valid = r < a.G * a.Nq && i < w.ql;
+            int seen = 0;
+            if (valid)
+                seen = a.causal ? max(0, min(w.kl, i + 1 + w.kl - w.ql))
+                                : w.kl;
+            float mref = kLowest, lsum = 0.0f;
+            for (int kt = 0; kt < n; ++kt, ++g) {
+                ok = wwait(&bars.s_full[s], g & 1, 409);
+                if (!ok) break;
+                tc_fence_after();
+                float v[128];
+                {
+                    uint32_t x[32], b[32], c[32], e[32];
+                    tmem_ld32(tS, x);
+                    tmem_ld32(tS + 32, b);
+                    tmem_ld32(tS + 64, c);
+                    tmem_ld32(tS + 96, e);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {
+                        v[q] = __uint_as_float(x[q]);
+                        v[32 + q] = __uint_as_float(b[q]);
+                        v[64 + q] = __uint_as_float(c[q]);
+                        v[96 + q] = __uint_as_float(e[q]);
+                    }
+                }
+                const int lim = seen - 128 * kt;
+                if (__any_sync(0xffffffffu, lim < 128)) {
+#pragma unroll
+                    for (int q = 0; q < 128; ++q)
+                        if (q >= lim) v[q] = -INFINITY;
+                }
+                float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                for (int q = 4; q < 124; q += 8)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        mx[x] = max3(mx[x], v[q + 2 * x], v[q + 2 * x + 1]);
+                mx[0] = max3(mx[0], v[124], v[125]);
+                mx[1] = max3(mx[1], v[126], v[127]);
+                const float z =
+                    fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
+                if (kt == 0) {
+                    mref = fmaxf(z, kLowest);
+                } else {
+                    // these scores were issued behind the last tile's P V
+                    // product: it is complete when they are
+                    const bool need = z > mref;
+                    if (__any_sync(0xffffffffu, need)) {
+                        const float f = need ? ex2_approx(mref - z) : 1.0f;
+                        const float2 f2 = make_float2(f, f);
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int q = 0; q < 16; q += 2) {
+                                const float2 y =
+                                    mul2(make_float2(__uint_as_float(o[q]),
+                                                     __uint_as_float(
+                                                         o[q + 1])),
+                                         f2);
+                                o[q] = __float_as_uint(y.x);
+                                o[q + 1] = __float_as_uint(y.y);
+                            }
+                            tmem_st16(tO + c, o);
+                        }
+                        lsum *= f;
+                        if (need) mref = z;
+                    }
+                }
+                const float2 nm = make_float2(-mref, -mref);
+                float2 ls[2] = {make_float2(0.0f, 0.0f),
+                                make_float2(0.0f, 0.0f)};
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) {
+                    uint32_t pw[16];
+#pragma unroll
+                    for (int q = 0; q < 32; q += 2) {
+                        const float2 x = fma2(
+                            make_float2(v[c + q], v[c + q + 1]), sl22, nm);
+                        const float2 p =
+                            make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        ls[(q >> 1) & 1] = add2(ls[(q >> 1) & 1], p);
+                        pw[q >> 1] = pack_bf16x2(p.x, p.y);
+                    }
+                    tmem_st16(tP + c / 2, pw);
+                }
+                lsum += (ls[0].x + ls[1].x) + (ls[0].y + ls[1].y);
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&bars.p_full[s]);
+            }
+            if (!ok) break;
+            const size_t at =
+                (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq + r;
+            uint16_t *o = (uint16_t *)a.out + at * D;
+            if (n > 0) {
+                ok = wwait(&bars.o_done[s], (g - 1) & 1, 410);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            // a row that sees nothing, or only scores of -inf: zeros
+            const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                uint32_t x[32];
+                if (n > 0) {
+                    tmem_ld32(tO + c, x);
+                    tmem_wait_ld();
+                    if (c + 32 == D) {
+                        tc_fence_before();
+                        mbar_arrive(&bars.o_empty[s]);
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) x[q] = 0;
+                }
+                if (!valid) continue;
+#pragma unroll
+                for (int q = 0; q < 32; q += 16) {
+                    uint32_t y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        y[e] = pack_bf16x2(
+                            __uint_as_float(x[q + 2 * e]) * inv,
+                            __uint_as_float(x[q + 2 * e + 1]) * inv);
+                    reinterpret_cast<uint4 *>(o + c + q)[0] =
+                        make_uint4(y[0], y[1], y[2], y[3]);
+                    reinterpret_cast<uint4 *>(o + c + q)[1] =
+                        make_uint4(y[4], y[5], y[6], y[7]);
+                }
+            }
+            if (valid && a.lse)
+                a.lse[at] = lsum == 0.0f ? -INFINITY
+                                         : (mref + log2f(lsum)) * kLn2;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tm, 512);
+}
+
+}  // namespace
+
+cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
+                                cudaStream_t st) {
+    const int tiles = (int)(((long)a.G * a.Nq + 255) / 256);
+    const long items = (long)tiles * a.B * a.Hkv;
+    int dev = 0, sms = 152;
+    if (cudaGetDevice(&dev) == cudaSuccess)
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    CUtensorMap tmQ, tmK, tmV;
+    const uint64_t nq = (uint64_t)a.B * a.H * a.Nq;
+    const uint64_t nk = (uint64_t)a.B * a.Hkv * a.Nk;
+    cudaError_t e = make_tma_map_bf16(&tmQ, a.q, nq, a.d, 128);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&tmK, a.k, nk, a.d, 128);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&tmV, a.v, nk, a.d, 128);
+    // more items than CTAs: they are taken from a counter
+    if (e == cudaSuccess && items > sms)
+        e = launch_clear(a.status, next_item, 1, st);
+    if (e != cudaSuccess) return e;
+    auto launch = [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        const size_t smem =
+            1024 + (size_t)(2 + 2 * kEfStages) * (D > 64 ? 2 : 1) * 16384;
+        return launch_after(
+            k_exact_fwd_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
+            kEfThreads, smem, st, tmQ, tmK, tmV, a, tiles, (int)items,
+            items > sms ? next_item : nullptr);
+    };
+    return a.d == 128  ? launch(std::integral_constant<int, 128>{})
+           : a.d == 64 ? launch(std::integral_constant<int, 64>{})
+                       : launch(std::integral_constant<int, 32>{});
+}
+
+}  // namespace elsaa
