@@ -55,6 +55,14 @@ __device__ __forceinline__ int exact_most(const ExactSeq &s, int r0, int r1,
 // bf16 on the tensor cores; next_item: an int of scratch
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
                                 cudaStream_t st);
+// Its backward pass: D_i first (which also clears the status and two work
+// counters), then dQ, and dK with dV.
+cudaError_t launch_exact_delta(const ExactView &a, int *counters,
+                               cudaStream_t st);
+cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
+                               cudaStream_t st);
+cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
+                                cudaStream_t st);
 // CUDA cores (fp32, and bf16 with impl = SIMT)
 cudaError_t launch_exact_fwd_simt(const ExactView &a, cudaStream_t st);
 cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys,

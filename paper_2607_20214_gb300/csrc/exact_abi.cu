@@ -67,14 +67,14 @@ bool on_tensor_cores(const elsaa_exact *p) {
     return p->dtype == ELSAA_BF16 && p->impl == ELSAA_IMPL_AUTO;
 }
 
-// status and a work counter | D_i
+// status and two work counters | D_i
 struct Layout {
     size_t next_item, delta, total;
 };
 Layout layout(const ExactView &a, bool backward) {
     Layout l;
     l.next_item = sizeof(DeviceStatus);
-    l.delta = align256(l.next_item + sizeof(int));
+    l.delta = align256(l.next_item + 2 * sizeof(int));
     l.total = l.delta;
     if (backward)
         l.total += align256(sizeof(float) * (size_t)a.B * a.H * a.Nq);
@@ -174,6 +174,16 @@ extern "C" int elsaa_exact_backward(
     a.status = (DeviceStatus *)workspace;
     a.delta = (float *)((char *)workspace + l.delta);
     cudaStream_t st = (cudaStream_t)stream;
+    if (on_tensor_cores(exact)) {
+        int *next_item = (int *)((char *)workspace + l.next_item);
+        ELSAA_EXACT_LAUNCH("exact_delta", st,
+                           launch_exact_delta(a, next_item, st));
+        ELSAA_EXACT_LAUNCH("exact_dq_tc", st,
+                           launch_exact_dq_tc(a, next_item, st));
+        ELSAA_EXACT_LAUNCH("exact_dkv_tc", st,
+                           launch_exact_dkv_tc(a, next_item + 1, st));
+        return ELSAA_OK;
+    }
     ELSAA_EXACT_LAUNCH("exact_dq_simt", st,
                        launch_exact_bwd_simt(a, false, st));
     ELSAA_EXACT_LAUNCH("exact_dkv_simt", st,
