@@ -2,10 +2,11 @@
 // (include/elsaa_heads.h): the norm of every query and key head, the rotation
 // by position and the change of layout in one pass; kernels and C ABI.
 //
-// A warp takes one token's row; D / VE lanes of 16 bytes hold a head, so that
-// it works on 32 VE / D heads at once, which lie side by side in the row. What
-// belongs to the token alone is made once: two pairs' sine and cosine a lane,
-// handed round, and multiplied by the norm's weights:
+// A warp takes one token's heads of one kind (queries, keys or values);
+// D / VE lanes of 16 bytes hold a head, so that it works on 32 VE / D heads at
+// once, which lie side by side in the row. What belongs to the token alone is
+// made once: two pairs' sine and cosine a lane, handed round, and multiplied
+// by the norm's weights:
 //     out = r (x A + x' B),  A = w cos a,  B = +-w' sin a,
 // x' the pair's other channel (of lane +- dim / 2 VE, or next to x), r the
 // head's 1 / sqrt(mean x^2 + eps). Memory bound: every row is read once and
@@ -25,9 +26,10 @@ namespace elsaa {
 namespace {
 
 constexpr int kHeadWarps = 8;
-// CTAs of the backward kernel at most: three of 8 warps on each of the 152 SMs
-// of a GB300. Fixed, so that the workspace does not depend on the device.
-constexpr int kHeadCtas = 456;
+// CTAs of the backward kernel at most, each of which leaves a partial of dw:
+// eight of 8 warps on each of the 152 SMs of a GB300. Fixed, so that the
+// workspace does not depend on the device.
+constexpr int kHeadCtas = 1216;
 
 struct RowsView {
     char *p;
@@ -39,15 +41,16 @@ struct HeadsArgs {
     int heads[3];   // of q, k, v that the call handles: H, Hkv, Hkv or 0
     int copies;     // of a K/V head: G with expand
     int norm, grad_fp32;
-    int groups;     // groups of heads that a warp handles at a time
-    int per_split;  // groups of one unit
+    // a warp handles a group of heads at a time; the groups of each kind are
+    // divided among splits[kind] CTAs of per_split each
+    int groups[3], splits[3], per_split;
     float eps;
     RowsView x[3];  // rows (forward), rows of q and k (backward)
     RowsView dx[3];
     char *out[3];   // heads, or their gradients
     const float *w[2];
     const int32_t *positions, *lengths, *new_len;
-    float *part;    // [CTAs][2][D]
+    float *part;    // [CTAs of queries, then of keys][D]
     int dim;
     uint64_t turns[ELSAA_MAX_PAIRS];
     uint8_t axis[ELSAA_MAX_PAIRS];
@@ -166,19 +169,23 @@ __device__ __forceinline__ uint4 shfl4(const uint4 &u, int src) {
                       __shfl_sync(~0u, u.z, src), __shfl_sync(~0u, u.w, src));
 }
 
-// Head hh of a unit's list is head h of q, k or v (kind 0, 1, 2; 3: none).
-__device__ __forceinline__ int which_head(const HeadsArgs &a, int hh,
-                                          int &h) {
-    h = hh;
-    if (h < a.heads[0]) return 0;
-    h -= a.heads[0];
-    if (h < a.heads[1]) return 1;
-    h -= a.heads[1];
-    return h < a.heads[2] ? 2 : 3;
+// blockIdx.y: kind (0 queries, 1 keys, 2 values) and split of its groups.
+__device__ __forceinline__ int which_kind(const HeadsArgs &a, int &split) {
+    int y = blockIdx.y, kind = 0;
+    while (kind < 2 && y >= a.splits[kind]) y -= a.splits[kind++];
+    split = y;
+    return kind;
 }
 
+// Pairs of channels as packed fp32.
+template <int VE>
+__device__ __forceinline__ float2 two(const float (&x)[VE], int i) {
+    return make_float2(x[2 * i], x[2 * i + 1]);
+}
+
+// __launch_bounds__: four CTAs an SM
 template <typename T, int D, bool IL>
-__global__ void __launch_bounds__(kHeadWarps * 32)
+__global__ void __launch_bounds__(kHeadWarps * 32, 4)
     k_heads_forward(const __grid_constant__ HeadsArgs a) {
     wait_for_stream();
     using V = Vec<T>;
@@ -189,89 +196,112 @@ __global__ void __launch_bounds__(kHeadWarps * 32)
     const int b = (int)(row / a.N), n = (int)(row - (long)b * a.N);
     const int n_new = a.new_len ? min(max(a.new_len[b], 0), a.N) : a.N;
     if (n >= n_new) return;
+    int split;
+    const int kind = which_kind(a, split);
     const int ch = (lane % LPH) * VE;
-    const int g0 = blockIdx.y * a.per_split;
-    const int g1 = min(g0 + a.per_split, a.groups);
+    const int heads = a.heads[kind], cp = kind ? a.copies : 1;
+    // this lane's head of group g is g HPW + lane / LPH
+    const int h0 = split * a.per_split * HPW + lane / LPH;
+    const int h1 = min(heads, (split + 1) * a.per_split * HPW);
+    const RowsView &X = a.x[kind];
+    const int64_t in_step = X.head * HPW;
+    const char *in = X.p + b * X.batch + n * X.row + h0 * X.head + ch * sizeof(T);
+    const size_t out_head = (size_t)a.N * D * sizeof(T);
+    const size_t out_step = out_head * HPW * cp;
+    char *out = a.out[kind] +
+                ((((size_t)b * heads + h0) * cp * a.N + n) * D + ch) *
+                    sizeof(T);
 
-    Turn<VE> t;
-    make_turn<VE, LPH, IL>(a, b, n, n_new, lane, t);
-    // A = w cos a, B = +-w' sin a for queries and keys
-    float A[2][VE], Bs[2][VE];
+    if (kind == 2) {  // values are copied
+        for (int h = h0; h < h1; h += HPW * U) {
+            uint4 raw[U];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+            for (int u = 0; u < U; ++u)
+                if (h + u * HPW < h1)
+                    raw[u] = *reinterpret_cast<const uint4 *>(in +
+                                                              u * in_step);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (h + u * HPW < h1)
+                    for (int i = 0; i < cp; ++i)
+                        *reinterpret_cast<uint4 *>(out + u * out_step +
+                                                   i * out_head) = raw[u];
+            in += U * in_step;
+            out += U * out_step;
+        }
+        return;
+    }
+    // A = w cos a, B = +-w' sin a
+    float A[VE], Bs[VE];
+    int partner;
+    bool rot;
+    {
+        Turn<VE> t;
+        make_turn<VE, LPH, IL>(a, b, n, n_new, lane, t);
         float w[VE];
 #pragma unroll
         for (int e = 0; e < VE; ++e)
-            w[e] = a.norm && a.w[k] ? a.w[k][ch + e] : 1.0f;
+            w[e] = a.norm && a.w[kind] ? a.w[kind][ch + e] : 1.0f;
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
             const float wp =
                 IL ? w[e ^ 1] : __shfl_sync(~0u, w[e], t.partner);
-            A[k][e] = w[e] * t.c[e];
-            Bs[k][e] = wp * t.s[e];
+            A[e] = w[e] * t.c[e];
+            Bs[e] = wp * t.s[e];
         }
+        partner = t.partner;
+        rot = t.on;
     }
-    for (int g = g0; g < g1; g += U) {
+    // lanes take part in the shuffles until the warp's last head is done
+    const int warp_h = split * a.per_split * HPW;
+    for (int g = 0; warp_h + g < h1; g += HPW * U) {
         uint4 raw[U];
-        int kind[U], h[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            kind[u] = g + u < g1
-                          ? which_head(a, (g + u) * HPW + lane / LPH, h[u])
-                          : 3;
             raw[u] = make_uint4(0, 0, 0, 0);
-            if (kind[u] < 3) {
-                const RowsView &x = a.x[kind[u]];
-                raw[u] = *reinterpret_cast<const uint4 *>(
-                    x.p + b * x.batch + n * x.row + h[u] * x.head +
-                    lane % LPH * 16);
-            }
+            if (h0 + g + u * HPW < h1)
+                raw[u] = *reinterpret_cast<const uint4 *>(in + u * in_step);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (g + u >= g1) break;
-            // a group of values only is copied
-            const bool copy = __all_sync(~0u, kind[u] >= 2);
-            uint4 y4 = raw[u];
-            if (!copy) {
-                float x[VE], xp[VE], y[VE];
-                V::unpack(raw[u], x);
-                float r = 1.0f;
-                if (a.norm) {
-                    float ss = 0.0f;
+            if (warp_h + g + u * HPW >= h1) break;
+            float x[VE], xp[VE], y[VE];
+            V::unpack(raw[u], x);
+            float r = 1.0f;
+            if (a.norm) {
+                float2 ss = make_float2(0.0f, 0.0f);
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) ss = fmaf(x[e], x[e], ss);
-                    r = inv_sqrt(fmaf(head_sum<LPH>(ss), 1.0f / D, a.eps));
-                }
-                if (IL) {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) xp[e] = x[e ^ 1];
-                } else {
-                    V::unpack(shfl4(raw[u], t.partner), xp);
-                }
-                const bool isk = kind[u] == 1;
-#pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    const float ae = isk ? A[1][e] : A[0][e];
-                    const float be = isk ? Bs[1][e] : Bs[0][e];
-                    const bool rot = IL ? ch + e < a.dim : t.on;
-                    // no product with a sine of 0: x' may be infinite
-                    const float z = x[e] * ae;
-                    y[e] = (rot ? fmaf(xp[e], be, z) : z) * r;
-                }
-                if (kind[u] < 2) y4 = V::pack(y);
+                for (int e = 0; e < VE / 2; ++e)
+                    ss = tc::fma2(two(x, e), two(x, e), ss);
+                r = inv_sqrt(
+                    fmaf(head_sum<LPH>(ss.x + ss.y), 1.0f / D, a.eps));
             }
-            if (kind[u] < 3) {
-                const int cp = kind[u] ? a.copies : 1;
-                const int heads = kind[u] ? a.Hkv * cp : a.H;
-                char *o = a.out[kind[u]] +
-                          ((((size_t)b * heads + h[u] * cp) * a.N + n) * D +
-                           ch) * sizeof(T);
+            if (IL) {
+#pragma unroll
+                for (int e = 0; e < VE; ++e) xp[e] = x[e ^ 1];
+            } else {
+                V::unpack(shfl4(raw[u], partner), xp);
+            }
+            const float2 rr = make_float2(r, r);
+#pragma unroll
+            for (int e = 0; e < VE / 2; ++e) {
+                const float2 z = tc::mul2(two(x, e), two(A, e));
+                float2 o = tc::fma2(two(xp, e), two(Bs, e), z);
+                // no product with a sine of 0: x' may be infinite
+                if (IL ? ch + 2 * e >= a.dim : !rot) o = z;
+                o = tc::mul2(o, rr);
+                y[2 * e] = o.x;
+                y[2 * e + 1] = o.y;
+            }
+            if (h0 + g + u * HPW < h1) {
+                const uint4 y4 = V::pack(y);
                 for (int i = 0; i < cp; ++i)
-                    *reinterpret_cast<uint4 *>(
-                        o + (size_t)i * a.N * D * sizeof(T)) = y4;
+                    *reinterpret_cast<uint4 *>(out + u * out_step +
+                                               i * out_head) = y4;
             }
         }
+        in += U * in_step;
+        out += U * out_step;
     }
 }
 
@@ -289,75 +319,75 @@ __device__ __forceinline__ void load_grad(const char *p, float *g) {
 // registers, then over the CTA's warps, and leaves as one partial of the CTA
 // that k_heads_weights adds up in order.
 template <typename T, typename GT, int D, bool IL>
-__global__ void __launch_bounds__(kHeadWarps * 32)
+__global__ void __launch_bounds__(kHeadWarps * 32, 2)
     k_heads_backward(const __grid_constant__ HeadsArgs a) {
     wait_for_stream();
     using V = Vec<T>;
-    constexpr int VE = V::n, LPH = D / VE, HPW = 32 / LPH;
-    constexpr int U = sizeof(GT) * VE > 16 ? 2 : 4;
-    __shared__ float sums[kHeadWarps][2][D];
+    constexpr int VE = V::n, LPH = D / VE, HPW = 32 / LPH, U = 2;
+    __shared__ float sums[kHeadWarps][D];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ch = (lane % LPH) * VE;
     const long rows = (long)a.B * a.N;
-    const int g0 = blockIdx.y * a.per_split;
-    const int g1 = min(g0 + a.per_split, a.groups);
-    float w[2][VE], dw[2][VE];
+    int split;
+    const int kind = which_kind(a, split);
+    const int heads = a.heads[kind], cp = kind ? a.copies : 1;
+    const int warp_h = split * a.per_split * HPW, h0 = warp_h + lane / LPH;
+    const int h1 = min(heads, (split + 1) * a.per_split * HPW);
+    const bool norm = a.norm && kind < 2;
+    const RowsView &X = a.x[norm ? kind : 0], &Y = a.dx[kind];
+    const size_t g_head = (size_t)a.N * D * sizeof(GT);
+    const size_t g_step = g_head * HPW * cp;
+    float w[VE], dw[VE];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            w[k][e] = a.norm && a.w[k] ? a.w[k][ch + e] : 1.0f;
-            dw[k][e] = 0.0f;
-        }
+    for (int e = 0; e < VE; ++e) {
+        w[e] = norm && a.w[kind] ? a.w[kind][ch + e] : 1.0f;
+        dw[e] = 0.0f;
+    }
     for (long row = (long)blockIdx.x * kHeadWarps + warp; row < rows;
          row += (long)gridDim.x * kHeadWarps) {
         const int b = (int)(row / a.N), n = (int)(row - (long)b * a.N);
         const int n_new = a.new_len ? min(max(a.new_len[b], 0), a.N) : a.N;
         if (n >= n_new) continue;
         Turn<VE> t;
-        make_turn<VE, LPH, IL>(a, b, n, n_new, lane, t);
-        for (int g = g0; g < g1; g += U) {
+        if (kind < 2) make_turn<VE, LPH, IL>(a, b, n, n_new, lane, t);
+        const char *gp = a.out[kind] +
+                         ((((size_t)b * heads + h0) * cp * a.N + n) * D + ch) *
+                             sizeof(GT);
+        const char *xp = X.p + b * X.batch + n * X.row + h0 * X.head +
+                         ch * sizeof(T);
+        char *yp = Y.p + b * Y.batch + n * Y.row + h0 * Y.head +
+                   ch * sizeof(T);
+        for (int g = 0; warp_h + g < h1; g += HPW * U) {
             float gr[U][VE];
             uint4 raw[U];
-            int kind[U], h[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                kind[u] = g + u < g1
-                              ? which_head(a, (g + u) * HPW + lane / LPH, h[u])
-                              : 3;
                 raw[u] = make_uint4(0, 0, 0, 0);
 #pragma unroll
                 for (int e = 0; e < VE; ++e) gr[u][e] = 0.0f;
-                if (kind[u] < 3) {
-                    const int cp = kind[u] ? a.copies : 1;
-                    const int heads = kind[u] ? a.Hkv * cp : a.H;
-                    const char *p =
-                        a.out[kind[u]] +
-                        ((((size_t)b * heads + h[u] * cp) * a.N + n) * D +
-                         ch) * sizeof(GT);
-                    load_grad<T, GT>(p, gr[u]);
-                    for (int i = 1; i < cp; ++i) {
-                        float more[VE];
-                        load_grad<T, GT>(
-                            p + (size_t)i * a.N * D * sizeof(GT), more);
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) gr[u][e] += more[e];
-                    }
-                    if (a.norm && kind[u] < 2) {
-                        const RowsView &x = a.x[kind[u]];
+                if (h0 + g + u * HPW < h1) {
+                    load_grad<T, GT>(gp + u * g_step, gr[u]);
+                    if (norm)
                         raw[u] = *reinterpret_cast<const uint4 *>(
-                            x.p + b * x.batch + n * x.row + h[u] * x.head +
-                            lane % LPH * 16);
-                    }
+                            xp + u * X.head * HPW);
                 }
+            }
+            if (cp > 1) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (h0 + g + u * HPW < h1)
+                        for (int i = 1; i < cp; ++i) {
+                            float more[VE];
+                            load_grad<T, GT>(gp + u * g_step + i * g_head,
+                                             more);
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) gr[u][e] += more[e];
+                        }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (g + u >= g1) break;
-                float y[VE];
-#pragma unroll
-                for (int e = 0; e < VE; ++e) y[e] = gr[u][e];
-                if (!__all_sync(~0u, kind[u] >= 2)) {
+                if (warp_h + g + u * HPW >= h1) break;
+                if (kind < 2) {
                     float uu[VE];
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
@@ -365,87 +395,83 @@ __global__ void __launch_bounds__(kHeadWarps * 32)
                             IL ? gr[u][e ^ 1]
                                : __shfl_sync(~0u, gr[u][e], t.partner);
                         const bool rot = IL ? ch + e < a.dim : t.on;
-                        uu[e] = rot ? fmaf(-p, t.s[e], gr[u][e] * t.c[e])
-                                    : gr[u][e];
+                        const float z = gr[u][e] * t.c[e];
+                        uu[e] = rot ? fmaf(-p, t.s[e], z) : z;
                     }
-                    if (a.norm) {
-                        const bool isk = kind[u] == 1;
-                        float x[VE], ss = 0.0f, tx = 0.0f;
+                    if (norm) {
+                        float x[VE];
+                        float2 s2 = make_float2(0.0f, 0.0f), t2 = s2;
                         V::unpack(raw[u], x);
 #pragma unroll
-                        for (int e = 0; e < VE; ++e)
-                            ss = fmaf(x[e], x[e], ss);
-                        const float r = inv_sqrt(
-                            fmaf(head_sum<LPH>(ss), 1.0f / D, a.eps));
-                        float tt[VE];
+                        for (int e = 0; e < VE / 2; ++e) {
+                            s2 = tc::fma2(two(x, e), two(x, e), s2);
+                            t2 = tc::fma2(tc::mul2(two(uu, e), two(w, e)),
+                                          two(x, e), t2);
+                        }
+                        const float ss = head_sum<LPH>(s2.x + s2.y);
+                        const float tx = head_sum<LPH>(t2.x + t2.y);
+                        const float r = inv_sqrt(fmaf(ss, 1.0f / D, a.eps));
+                        // of xh = x r: mean(t xh) = r mean(t x)
+                        const float m = tx * (1.0f / D) * r;
 #pragma unroll
                         for (int e = 0; e < VE; ++e) {
-                            x[e] *= r;
-                            tt[e] = uu[e] * (isk ? w[1][e] : w[0][e]);
-                            tx = fmaf(tt[e], x[e], tx);
-                        }
-                        const float m = head_sum<LPH>(tx) * (1.0f / D);
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) {
-                            const float d = uu[e] * x[e];
-                            if (kind[u] == 0) dw[0][e] += d;
-                            if (kind[u] == 1) dw[1][e] += d;
-                            uu[e] = r * fmaf(-x[e], m, tt[e]);
+                            const float xh = x[e] * r;
+                            dw[e] = fmaf(uu[e], xh, dw[e]);
+                            uu[e] = r * fmaf(-xh, m, uu[e] * w[e]);
                         }
                     }
-                    if (kind[u] < 2) {
 #pragma unroll
-                        for (int e = 0; e < VE; ++e) y[e] = uu[e];
-                    }
+                    for (int e = 0; e < VE; ++e) gr[u][e] = uu[e];
                 }
-                if (kind[u] < 3) {
-                    const RowsView &x = a.dx[kind[u]];
-                    *reinterpret_cast<uint4 *>(x.p + b * x.batch + n * x.row +
-                                               h[u] * x.head +
-                                               lane % LPH * 16) = V::pack(y);
-                }
+                if (h0 + g + u * HPW < h1)
+                    *reinterpret_cast<uint4 *>(yp + u * Y.head * HPW) =
+                        V::pack(gr[u]);
             }
+            gp += U * g_step;
+            xp += U * X.head * HPW;
+            yp += U * Y.head * HPW;
         }
     }
-    if (!a.part) return;
+    if (!a.part || kind == 2) return;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int e = 0; e < VE; ++e) {
+        float v = dw[e];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            float v = dw[k][e];
-#pragma unroll
-            for (int o = LPH; o < 32; o <<= 1)
-                v += __shfl_xor_sync(~0u, v, o);
-            if (lane < LPH) sums[warp][k][ch + e] = v;
-        }
+        for (int o = LPH; o < 32; o <<= 1) v += __shfl_xor_sync(~0u, v, o);
+        if (lane < LPH) sums[warp][ch + e] = v;
+    }
     __syncthreads();
-    const long cta = (long)blockIdx.y * gridDim.x + blockIdx.x;
-    for (int i = threadIdx.x; i < 2 * D; i += kHeadWarps * 32) {
+    const long cta =
+        (long)((kind ? a.splits[0] : 0) + split) * gridDim.x + blockIdx.x;
+    for (int i = threadIdx.x; i < D; i += kHeadWarps * 32) {
         float v = 0.0f;
 #pragma unroll
-        for (int q = 0; q < kHeadWarps; ++q) v += (&sums[q][0][0])[i];
-        a.part[cta * 2 * D + i] = v;
+        for (int q = 0; q < kHeadWarps; ++q) v += sums[q][i];
+        a.part[cta * D + i] = v;
     }
 }
 
 // dw: 32 columns of the partials a CTA, 32 rows of threads, in one order.
 __global__ void __launch_bounds__(1024)
-    k_heads_weights(const float *__restrict__ part, int ctas, int d,
-                    float *__restrict__ dw_q, float *__restrict__ dw_k) {
+    k_heads_weights(const float *__restrict__ part, int ctas_q, int ctas_k,
+                    int d, float *__restrict__ dw_q,
+                    float *__restrict__ dw_k) {
     wait_for_stream();
     __shared__ float s[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int col = blockIdx.x * 32 + x;
+    const bool keys = (int)blockIdx.x * 32 >= d;
+    const int col = blockIdx.x * 32 + x - (keys ? d : 0);
+    const int first = keys ? ctas_q : 0, last = first + (keys ? ctas_k : ctas_q);
     float v = 0.0f;
-    for (int c = y; c < ctas; c += 32) v += part[(size_t)c * 2 * d + col];
+    for (int c = first + y; c < last; c += 32) v += part[(size_t)c * d + col];
     s[y][x] = v;
     __syncthreads();
     if (y > 0) return;
     v = 0.0f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) v += s[i][x];
-    float *o = col < d ? dw_q : dw_k;
-    if (o) o[col < d ? col : col - d] = v;
+    float *o = keys ? dw_k : dw_q;
+    if (o) o[col] = v;
 }
 
 int bad(const char *m) {
@@ -547,17 +573,31 @@ void fill(const elsaa_heads *p, HeadsArgs *a) {
     }
 }
 
-// Groups of heads of a unit, so that few tokens still give every SM's warps a
-// unit each.
-int divide_groups(HeadsArgs *a, int d, int el, long tokens) {
+// Groups of heads of a CTA: those of one K/V set, four at least (the token's
+// sines are made for each), fewer where the tokens alone do not give every
+// SM's warps work. Returns the CTAs of a token, at most `most`.
+int divide_groups(HeadsArgs *a, int d, int el, long tokens, int most) {
     const int per_warp = 32 / (d * el / 16);
-    const int heads = a->heads[0] + a->heads[1] + a->heads[2];
-    a->groups = (heads + per_warp - 1) / per_warp;
+    int all = 0, least = 0;
+    for (int i = 0; i < 3; ++i) {
+        a->groups[i] = (a->heads[i] + per_warp - 1) / per_warp;
+        all += a->groups[i];
+        if (a->groups[i] && (!least || a->groups[i] < least))
+            least = a->groups[i];
+    }
     const long units = 152 * 16;
-    long splits = (units + tokens - 1) / tokens;
-    if (splits > a->groups) splits = a->groups;
-    a->per_split = (int)((a->groups + splits - 1) / splits);
-    return (a->groups + a->per_split - 1) / a->per_split;
+    long per = tokens * all / units;
+    if (per > least) per = least > 4 ? least : (per < 4 ? per : 4);
+    if (per < 1) per = 1;
+    for (;; per *= 2) {
+        int n = 0;
+        for (int i = 0; i < 3; ++i) {
+            a->splits[i] = (int)((a->groups[i] + per - 1) / per);
+            n += a->splits[i];
+        }
+        a->per_split = (int)per;
+        if (n <= most) return n;
+    }
 }
 
 int bwd_ctas(long tokens, int splits) {
@@ -601,8 +641,7 @@ extern "C" int elsaa_heads_workspace_size(const elsaa_heads *heads,
     if (!bytes) return bad("bytes is NULL");
     const int rc = check_heads(heads);
     if (rc != ELSAA_OK) return rc;
-    // at most one partial for each of kHeadCtas CTAs, or for each split
-    *bytes = sizeof(float) * 2 * heads->d_h * kHeadCtas;
+    *bytes = sizeof(float) * heads->d_h * kHeadCtas;
     return ELSAA_OK;
 }
 
@@ -638,7 +677,8 @@ extern "C" int elsaa_heads_forward(
     a.new_len = new_len;
     const bool f32 = heads->dtype == ELSAA_FP32;
     const long tokens = (long)a.B * a.N;
-    const int splits = divide_groups(&a, heads->d_h, f32 ? 4 : 2, tokens);
+    const int splits =
+        divide_groups(&a, heads->d_h, f32 ? 4 : 2, tokens, 65535);
     const dim3 grid((unsigned)((tokens + kHeadWarps - 1) / kHeadWarps),
                     splits);
     const bool il = heads->rotary.interleaved != 0;
@@ -708,7 +748,7 @@ extern "C" int elsaa_heads_backward(
         if (misaligned(workspace, 256))
             return set_last_error(ELSAA_ERR_WORKSPACE,
                                   "workspace must be 256-byte aligned");
-        const size_t need = sizeof(float) * 2 * d * kHeadCtas;
+        const size_t need = sizeof(float) * d * kHeadCtas;
         if (workspace_bytes < need)
             return set_last_error(ELSAA_ERR_WORKSPACE,
                                   "workspace too small: %zu bytes given, %zu "
@@ -724,11 +764,8 @@ extern "C" int elsaa_heads_backward(
     const bool f32 = heads->dtype == ELSAA_FP32;
     const bool g32 = f32 || heads->grad_fp32;
     const long tokens = (long)a.B * a.N;
-    int splits = divide_groups(&a, d, f32 ? 4 : 2, tokens);
-    if (splits > kHeadCtas) {
-        a.per_split = (a.groups + kHeadCtas - 1) / kHeadCtas;
-        splits = (a.groups + a.per_split - 1) / a.per_split;
-    }
+    const int splits =
+        divide_groups(&a, d, f32 ? 4 : 2, tokens, kHeadCtas);
     const dim3 grid(bwd_ctas(tokens, splits), splits);
     const bool il = heads->rotary.interleaved != 0;
     cudaStream_t st = (cudaStream_t)stream;
@@ -748,7 +785,8 @@ extern "C" int elsaa_heads_backward(
         e = timed("heads_weights", st, [&] {
             return launch_after(k_heads_weights, dim3(2 * d / 32), 1024, 0,
                                 st, (const float *)a.part,
-                                (int)(grid.x * grid.y), d, dw_q, dw_k);
+                                (int)grid.x * a.splits[0],
+                                (int)grid.x * a.splits[1], d, dw_q, dw_k);
         });
     if (e != cudaSuccess)
         return set_last_error(ELSAA_ERR_CUDA, "heads_backward: %s",

@@ -267,8 +267,8 @@ def test_together_with_attention():
                           (O, X.grad, W[0].grad, W[1].grad)):
         # fp32 throughout: chains of below 2^9 roundings of numbers that add
         # up to at most 2^4 times the largest result
-        tol = 2.0 ** (9 + 4 - 24) * float(r.abs().max())
-        assert float((g.double() - r).abs().max()) <= tol, name
+        tol = 2.0 ** (9 + 4 - 24) * float(r.detach().abs().max())
+        assert float((g.double() - r.detach()).abs().max()) <= tol, name
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         again = layer(x)
