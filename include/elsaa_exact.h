@@ -30,7 +30,7 @@ extern "C" {
 
 typedef struct elsaa_exact {
     int B;           /* sequences                                            */
-    int H;           /* query heads                                          */
+    int H;           /* query heads, at most 65535                           */
     int H_kv;        /* K/V heads; H a multiple of it: query head h reads
                         K/V head h / (H / H_kv)                              */
     int N_q, N_k;    /* rows of q and of k, v; B * H * N_q and

@@ -51,9 +51,9 @@ typedef struct elsaa_rotary {
 
 typedef struct elsaa_heads {
     int B;           /* sequences                                            */
-    int H;           /* query heads                                          */
+    int H;           /* query heads, at most 65535                           */
     int H_kv;        /* key and value heads; H a multiple of it              */
-    int N;           /* rows of every sequence                               */
+    int N;           /* rows of every sequence; B * N at most 2^30           */
     int d_h;         /* 32, 64 or 128                                        */
     int dtype;       /* ELSAA_BF16 or ELSAA_FP32: type of rows and heads     */
     int norm;        /* 1: queries and keys are normed                       */

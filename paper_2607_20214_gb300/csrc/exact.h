@@ -18,6 +18,38 @@ struct ExactView {
     DeviceStatus *status;
 };
 
+// How the rows of the query heads that share a K/V head are laid on tiles of
+// `tile` rows, and the order in which the tiles are taken: the last one of
+// every head (with causal = 1 it sees most) before the one before it, as far as
+// heads and tiles coincide. Row r is row r mod pitch of head r / pitch. Heads
+// follow one another without a gap (pitch = N_q), so that several short ones
+// fill a tile; but a padded batch of longer rows begins every head with a tile,
+// or tiles would hold the padding between two heads. Some of the tiles given
+// are past the last row.
+struct ExactOrder {
+    int pitch, rows, groups, per;
+    ExactOrder(const ExactView &a, int tile) {
+        pitch = a.Nq;
+        if (a.q_len && a.Nq > 128) pitch = (a.Nq + 127) / 128 * 128;
+        rows = a.G * pitch;
+        const int tiles = (rows + tile - 1) / tile;
+        groups = tiles < a.G ? 1 : a.G;
+        per = (tiles + groups - 1) / groups;
+    }
+    long items(const ExactView &a) const {
+        return (long)groups * per * a.B * a.Hkv;
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int tile(int t) const {
+        return t % groups * per + per - 1 - t / groups;
+    }
+    // where row r lies in memory, from the first head on
+    __device__ __forceinline__ int row(int r, int N) const {
+        return r / pitch * N + r % pitch;
+    }
+#endif
+};
+
 #ifdef __CUDACC__
 // Sequence b's lengths, and how many keys query row i sees: the first seen(i).
 struct ExactSeq {
@@ -52,9 +84,11 @@ __device__ __forceinline__ int exact_most(const ExactSeq &s, int r0, int r1,
 }
 #endif
 
-// bf16 on the tensor cores; next_item: an int of scratch
+// bf16 on the tensor cores; next_item: an int of scratch; part:
+// exact_split_bytes(a) of it, 256-byte aligned
+size_t exact_split_bytes(const ExactView &a);
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
-                                cudaStream_t st);
+                                float *part, cudaStream_t st);
 // Its backward pass: D_i first (which also clears the status and two work
 // counters), then dQ, and dK with dV.
 cudaError_t launch_exact_delta(const ExactView &a, int *counters,

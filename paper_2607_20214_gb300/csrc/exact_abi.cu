@@ -46,6 +46,7 @@ int make_view(const elsaa_exact *p, ExactView *a) {
         return bad("scale must be finite and >= 0");
     if (p->d_h != 32 && p->d_h != 64 && p->d_h != 128)
         return no("d_h must be 32, 64 or 128");
+    if (p->H > 65535) return no("H must be at most 65535");
     const long most = 1L << 30;
     if (p->N_q > most / p->B / p->H || p->N_k > most / p->B / p->H_kv)
         return no("B * H * N_q and B * H_kv * N_k must be at most 2^30");
@@ -67,17 +68,18 @@ bool on_tensor_cores(const elsaa_exact *p) {
     return p->dtype == ELSAA_BF16 && p->impl == ELSAA_IMPL_AUTO;
 }
 
-// status and two work counters | D_i
+// status and two work counters | D_i, or what the chunks of split keys leave
 struct Layout {
-    size_t next_item, delta, total;
+    size_t next_item, scratch, total;
 };
-Layout layout(const ExactView &a, bool backward) {
+Layout layout(const ExactView &a, bool tensor, bool backward) {
     Layout l;
     l.next_item = sizeof(DeviceStatus);
-    l.delta = align256(l.next_item + 2 * sizeof(int));
-    l.total = l.delta;
-    if (backward)
-        l.total += align256(sizeof(float) * (size_t)a.B * a.H * a.Nq);
+    l.scratch = align256(l.next_item + 2 * sizeof(int));
+    size_t most = tensor ? exact_split_bytes(a) : 0;
+    const size_t delta = sizeof(float) * (size_t)a.B * a.H * a.Nq;
+    if (backward && delta > most) most = delta;
+    l.total = l.scratch + align256(most);
     return l;
 }
 
@@ -103,7 +105,7 @@ extern "C" int elsaa_exact_workspace_size(const elsaa_exact *exact,
     ExactView a;
     const int rc = make_view(exact, &a);
     if (rc != ELSAA_OK) return rc;
-    *bytes = layout(a, backward != 0).total;
+    *bytes = layout(a, on_tensor_cores(exact), backward != 0).total;
     return ELSAA_OK;
 }
 
@@ -120,7 +122,9 @@ extern "C" int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
     if (!q || !k || !v || !o) return bad("q, k, v and o must be non-NULL");
     for (const void *p : {q, k, v, (const void *)o, (const void *)lse})
         if (misaligned(p)) return bad("tensors must be 16-byte aligned");
-    rc = check_workspace(workspace, workspace_bytes, layout(a, false).total);
+    const bool tensor = on_tensor_cores(exact);
+    const Layout l = layout(a, tensor, false);
+    rc = check_workspace(workspace, workspace_bytes, l.total);
     if (rc != ELSAA_OK) return rc;
     a.q = q;
     a.k = k;
@@ -131,11 +135,12 @@ extern "C" int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
     a.lse = lse;
     a.status = (DeviceStatus *)workspace;
     cudaStream_t st = (cudaStream_t)stream;
-    int *next_item =
-        (int *)((char *)workspace + layout(a, false).next_item);
-    if (on_tensor_cores(exact))
+    char *ws = (char *)workspace;
+    if (tensor)
         ELSAA_EXACT_LAUNCH("exact_fwd_tc", st,
-                           launch_exact_fwd_tc(a, next_item, st));
+                           launch_exact_fwd_tc(a, (int *)(ws + l.next_item),
+                                               (float *)(ws + l.scratch),
+                                               st));
     else
         ELSAA_EXACT_LAUNCH("exact_fwd_simt", st,
                            launch_exact_fwd_simt(a, st));
@@ -157,7 +162,8 @@ extern "C" int elsaa_exact_backward(
                           (const void *)dq, (const void *)dk,
                           (const void *)dv})
         if (misaligned(p)) return bad("tensors must be 16-byte aligned");
-    const Layout l = layout(a, true);
+    const bool tensor = on_tensor_cores(exact);
+    const Layout l = layout(a, tensor, true);
     rc = check_workspace(workspace, workspace_bytes, l.total);
     if (rc != ELSAA_OK) return rc;
     a.q = q;
@@ -172,9 +178,9 @@ extern "C" int elsaa_exact_backward(
     a.dk = dk;
     a.dv = dv;
     a.status = (DeviceStatus *)workspace;
-    a.delta = (float *)((char *)workspace + l.delta);
+    a.delta = (float *)((char *)workspace + l.scratch);
     cudaStream_t st = (cudaStream_t)stream;
-    if (on_tensor_cores(exact)) {
+    if (tensor) {
         int *next_item = (int *)((char *)workspace + l.next_item);
         ELSAA_EXACT_LAUNCH("exact_delta", st,
                            launch_exact_delta(a, next_item, st));

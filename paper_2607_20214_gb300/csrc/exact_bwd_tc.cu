@@ -159,11 +159,17 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------------------------- dQ
 
-constexpr int kDqK = 3, kDqV = 2;  // key and value tiles held
+// Key and value tiles held: K(j) serves S(j) and dQ(j), behind S(j + 2).
+template <int D>
+constexpr int kDqK = D > 64 ? 3 : 6;
+template <int D>
+constexpr int kDqV = D > 64 ? 2 : 4;
 
+template <int D>
 struct DqBars {
     uint64_t item_full[2], item_empty[2], q_full, q_empty;
-    uint64_t k_full[kDqK], k_empty[kDqK], v_full[kDqV], v_empty[kDqV];
+    uint64_t k_full[kDqK<D>], k_empty[kDqK<D>];
+    uint64_t v_full[kDqV<D>], v_empty[kDqV<D>];
     uint64_t s_full[2], dp_full, dp_read, ds_full[2], dq_full, dq_empty;
 };
 struct BwdItem {
@@ -177,19 +183,21 @@ struct BwdItem {
 // A CTA holds Q and dO of 128 rows (of the heads that share a K/V head,
 // counted through) and walks key tiles. Warps 0-7: weights, two threads a row,
 // one for keys 0..63 of a tile, one for 64..127; warp 8 issues the products;
-// warp 9 takes the items and loads. Tensor memory: S of two tiles, dP, dQ; dS
-// goes over the S it came from.
+// warp 9 takes the items and loads Q, dO and K, warp 10 V. Tensor memory: S of
+// two tiles, dP, dQ; dS goes over the S it came from.
 template <int D>
 __global__ void __launch_bounds__(kEbThreads, 1)
     k_exact_dq_tc(const __grid_constant__ CUtensorMap tmQ,
                   const __grid_constant__ CUtensorMap tmG,
                   const __grid_constant__ CUtensorMap tmK,
                   const __grid_constant__ CUtensorMap tmV,
-                  const __grid_constant__ ExactView a, int per_head,
-                  int tiles, int items, int *__restrict__ next_item) {
+                  const __grid_constant__ ExactView a,
+                  const __grid_constant__ ExactOrder order, int items,
+                  int *__restrict__ next_item) {
     wait_for_stream();
     extern __shared__ unsigned char smem_raw[];
-    __shared__ DqBars bars;
+    __shared__ DqBars<D> bars;
+    constexpr int kK = kDqK<D>, kV = kDqV<D>;
     __shared__ uint32_t tbase;
     __shared__ int abort_flag;
     __shared__ BwdItem item_s[2];
@@ -198,22 +206,22 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     constexpr uint32_t kS = 0, kP = 256, kO = 384;  // tensor memory columns
     const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
     const uint32_t sQ = align1k(smem_u32(smem_raw)), sG = sQ + kTile;
-    const uint32_t sK = sG + kTile, sV = sK + kDqK * kTile;
+    const uint32_t sK = sG + kTile, sV = sK + kK * kTile;
     DeviceStatus *status = a.status;
 
     if (warp == 8) tmem_alloc(&tbase, 512);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], 9);
+            mbar_init(&bars.item_empty[s], 10);
             mbar_init(&bars.s_full[s], 1);
             mbar_init(&bars.ds_full[s], 256);
         }
-        for (int s = 0; s < kDqK; ++s) {
+        for (int s = 0; s < kK; ++s) {
             mbar_init(&bars.k_full[s], 1);
             mbar_init(&bars.k_empty[s], 1);
         }
-        for (int s = 0; s < kDqV; ++s) {
+        for (int s = 0; s < kV; ++s) {
             mbar_init(&bars.v_full[s], 1);
             mbar_init(&bars.v_empty[s], 1);
         }
@@ -238,7 +246,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             // ---------------------------------------------- items and loads
             int c = 0, qs = 0;  // key tiles and items loaded so far
             bool ok = true;
-            const int heads = a.B * a.Hkv, rows = a.G * a.Nq;
+            const int heads = a.B * a.Hkv, rows = order.rows;
             auto tile = [&](uint64_t *full, uint32_t dst,
                             const CUtensorMap *map, int row) {
                 for (int p = 0; p < kPanels<D>; ++p)
@@ -256,18 +264,15 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 if (item < items) {
                     // the last rows of every query head, which see most, first
                     const int h = (int)(item % heads);
-                    const int t = (int)(item / heads);
-                    const int x = t % a.G * per_head + per_head - 1 - t / a.G;
                     w.item = (int)item;
-                    w.r0 = x * 128;
+                    w.r0 = order.tile((int)(item / heads)) * 128;
                     w.b = h / a.Hkv;
                     w.kvh = h - w.b * a.Hkv;
                     const ExactSeq seq(a, w.b);
                     w.ql = seq.ql;
                     w.kl = seq.kl;
-                    if (x < tiles)
-                        w.n = (exact_most(seq, w.r0, min(w.r0 + 128, rows),
-                                          a.Nq) + 127) / 128;
+                    w.n = (exact_most(seq, w.r0, min(w.r0 + 128, rows),
+                                      order.pitch) + 127) / 128;
                 }
                 item_s[it & 1] = w;
                 mbar_arrive(&bars.item_full[it & 1]);
@@ -277,29 +282,47 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                                    abort, status, 421))
                     break;
                 ++qs;
-                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq + w.r0;
+                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq +
+                               order.row(w.r0, a.Nq);
                 const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
                 mbar_expect_tx(&bars.q_full, 2 * kTile);
                 tile(&bars.q_full, sQ, &tmQ, q0);
                 tile(&bars.q_full, sG, &tmG, q0);
                 for (int kt = 0; kt < w.n; ++kt, ++c) {
-                    const int ks = c % kDqK, vs = c % kDqV;
-                    if (c >= kDqK &&
+                    const int ks = c % kK;
+                    if (c >= kK &&
                         !(ok = mbar_wait_or_abort(&bars.k_empty[ks],
-                                                  (c / kDqK - 1) & 1, abort,
+                                                  (c / kK - 1) & 1, abort,
                                                   status, 422)))
                         break;
                     mbar_expect_tx(&bars.k_full[ks], kTile);
                     tile(&bars.k_full[ks], sK + ks * kTile, &tmK,
                          k0 + 128 * kt);
-                    if (c >= kDqV &&
+                }
+            }
+        } else if (warp == 10 && lane_id == 0) {
+            // ------------------------------------------ loads of the values
+            int c = 0;
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!mbar_wait_or_abort(&bars.item_full[it & 1], (it >> 1) & 1,
+                                        abort, status, 423))
+                    break;
+                const BwdItem w = item_s[it & 1];
+                mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
+                for (int kt = 0; kt < w.n; ++kt, ++c) {
+                    const int vs = c % kV;
+                    if (c >= kV &&
                         !(ok = mbar_wait_or_abort(&bars.v_empty[vs],
-                                                  (c / kDqV - 1) & 1, abort,
-                                                  status, 423)))
+                                                  (c / kV - 1) & 1, abort,
+                                                  status, 435)))
                         break;
                     mbar_expect_tx(&bars.v_full[vs], kTile);
-                    tile(&bars.v_full[vs], sV + vs * kTile, &tmV,
-                         k0 + 128 * kt);
+                    for (int p = 0; p < kPanels<D>; ++p)
+                        tma_load_2d(sV + vs * kTile + p * 16384, &tmV, 64 * p,
+                                    k0 + 128 * kt, &bars.v_full[vs]);
                 }
             }
         } else if (warp == 8) {
@@ -329,8 +352,8 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 if (n == 0) continue;
                 if (!wait(&bars.q_full, qs & 1, 425)) break;
                 auto scores = [&](int j) {
-                    const int x = c + j, ks = x % kDqK;
-                    if (!wait(&bars.k_full[ks], x / kDqK & 1, 426))
+                    const int x = c + j, ks = x % kK;
+                    if (!wait(&bars.k_full[ks], x / kK & 1, 426))
                         return false;
                     // keys that the sequence does not have count with dS = 0
                     // in dQ and must be numbers
@@ -345,8 +368,8 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     return true;
                 };
                 auto products = [&](int j) {
-                    const int x = c + j, vs = x % kDqV;
-                    if (!wait(&bars.v_full[vs], x / kDqV & 1, 427))
+                    const int x = c + j, vs = x % kV;
+                    if (!wait(&bars.v_full[vs], x / kV & 1, 427))
                         return false;
                     if (x > 0 && !wait(&bars.dp_read, (x - 1) & 1, 428))
                         return false;
@@ -363,7 +386,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 if (ok && qs > 0)
                     ok = wait(&bars.dq_empty, (qs - 1) & 1, 429);
                 for (int j = 0; j < n && ok; ++j) {
-                    const int x = c + j, ks = x % kDqK;
+                    const int x = c + j, ks = x % kK;
                     if (j + 1 < n && !(ok = products(j + 1))) break;
                     ok = wait(&bars.ds_full[x & 1], x / 2 & 1, 430);
                     if (!ok) break;
@@ -399,9 +422,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
             if (w.item < 0) break;
-            const int r = w.r0 + row, i = r % a.Nq;
-            const bool valid = r < a.G * a.Nq && i < w.ql;
-            const size_t at = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq + r;
+            const int r = w.r0 + row, i = r % order.pitch;
+            const bool valid = r < order.rows && i < w.ql;
+            const size_t at = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq +
+                              order.row(r, a.Nq);
             uint16_t *o = (uint16_t *)a.dq + at * D + D / 2 * half;
             if (w.n == 0) {
                 if (valid) store_zeros<D>(o);
@@ -473,7 +497,7 @@ struct Dkv {
     static constexpr int kS = D > 64 ? 1 : 2;  // S in tensor memory
     // query tiles and dO tiles held: Q(j) serves S(j) and dK(j), behind
     // S(j + kS)
-    static constexpr int kQ = D > 64 ? 2 : 4, kG = 2;
+    static constexpr int kQ = D > 64 ? 3 : 4, kG = D > 64 ? 2 : 4;
     static constexpr uint32_t cS = 0, cP = 128 * kS, cV = cP + 128,
                               cK = cV + D;
 };
@@ -481,16 +505,28 @@ template <int D>
 struct DkvBars {
     uint64_t item_full[2], item_empty[2], kv_full, kv_empty;
     uint64_t q_full[Dkv<D>::kQ], q_empty[Dkv<D>::kQ];
-    uint64_t g_full[2], g_empty[2], l_full[2], l_empty[2];
-    uint64_t s_full[2], p_full[2], dp_full, ds_full, sum_full, sum_empty;
+    uint64_t g_full[Dkv<D>::kG], g_empty[Dkv<D>::kG];
+    uint64_t l_full[2], l_empty[2], s_full[2], p_full[2];
+    uint64_t dp_full, ds_full, sum_full, sum_empty;
+};
+
+// What lies behind the tiles in shared memory (there are 3 KB).
+template <int D>
+struct DkvShared {
+    float row_l[2][128], row_d[2][128];  // -lse (base 2) and -D of the rows
+    DkvBars<D> bars;
+    BwdItem item[2];
+    uint32_t tbase;
+    int abort_flag;
 };
 
 // A CTA holds K and V of 128 rows and walks tiles of 128 query rows of every
 // head that reads them; scores and weights stand transposed, a key a lane.
 // Warps 0-7: weights, two threads a key, for queries 0..63 and 64..127 of a
-// tile; warp 8 issues the products; warp 9 takes the items and loads; warp 10
-// fetches the rows' lse and D. Tensor memory: S^T (two for D <= 64), dP^T, dV,
-// dK; P^T and dS^T go over the S^T and dP^T that they came from.
+// tile; warp 8 issues the products; warp 9 takes the items and loads K, V and
+// Q, warp 11 dO; warp 10 fetches the rows' lse and D. Tensor memory: S^T (two
+// for D <= 64), dP^T, dV, dK; P^T and dS^T go over the S^T and dP^T that they
+// came from.
 template <int D>
 __global__ void __launch_bounds__(kEbThreads, 1)
     k_exact_dkv_tc(const __grid_constant__ CUtensorMap tmQ,
@@ -502,29 +538,38 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     wait_for_stream();
     using X = Dkv<D>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ DkvBars<D> bars;
-    __shared__ uint32_t tbase;
-    __shared__ int abort_flag;
-    __shared__ BwdItem item_s[2];
-    __shared__ __align__(16) float row_l[2][128], row_d[2][128];
-    volatile int *abort = &abort_flag;
     constexpr uint32_t kTile = kTileBytes<D>;
+    constexpr uint32_t kTiles = (2 + X::kQ + X::kG) * kTile;
+    // there is no room for a whole KB of padding: dynamic shared memory begins
+    // on one, as the kernel has no other
+    const uint32_t pad = align1k(smem_u32(smem_raw)) - smem_u32(smem_raw);
+    if (pad > 0) {
+        report(a.status, kDevLayout, 459, (int)pad, 0);
+        return;
+    }
+    DkvShared<D> &sh = *reinterpret_cast<DkvShared<D> *>(smem_raw + kTiles);
+    auto &bars = sh.bars;
+    auto &item_s = sh.item;
+    auto &row_l = sh.row_l, &row_d = sh.row_d;
+    volatile int *abort = &sh.abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
-    const uint32_t sK = align1k(smem_u32(smem_raw)), sV = sK + kTile;
+    const uint32_t sK = smem_u32(smem_raw), sV = sK + kTile;
     const uint32_t sQ = sV + kTile, sG = sQ + X::kQ * kTile;
     DeviceStatus *status = a.status;
 
-    if (warp == 8) tmem_alloc(&tbase, 512);
+    if (warp == 8) tmem_alloc(&sh.tbase, 512);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], 10);
-            mbar_init(&bars.g_full[s], 1);
-            mbar_init(&bars.g_empty[s], 1);
+            mbar_init(&bars.item_empty[s], 11);
             mbar_init(&bars.l_full[s], 32);
             mbar_init(&bars.l_empty[s], 8);
             mbar_init(&bars.s_full[s], 1);
             mbar_init(&bars.p_full[s], 256);
+        }
+        for (int s = 0; s < X::kG; ++s) {
+            mbar_init(&bars.g_full[s], 1);
+            mbar_init(&bars.g_empty[s], 1);
         }
         for (int s = 0; s < X::kQ; ++s) {
             mbar_init(&bars.q_full[s], 1);
@@ -536,14 +581,14 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         mbar_init(&bars.ds_full, 256);
         mbar_init(&bars.sum_full, 1);
         mbar_init(&bars.sum_empty, 256);
-        abort_flag = 0;
+        sh.abort_flag = 0;
         fence_mbar_init();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tm = tbase;
-    // tile t of an item: rows of the query head t / per, from row i0
+    const uint32_t tm = sh.tbase;
+    // tiles of a query head's rows, walked head by head
     auto tiles_of = [](const BwdItem &w) {
         return (w.ql - w.first + 127) / 128;
     };
@@ -596,27 +641,46 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 mbar_expect_tx(&bars.kv_full, 2 * kTile);
                 tile(&bars.kv_full, sK, &tmK, k0);
                 tile(&bars.kv_full, sV, &tmV, k0);
-                const int per = tiles_of(w);
-                for (int t = 0; t < w.n; ++t, ++c) {
-                    const int qs = c % X::kQ, gs = c % X::kG;
-                    const int row =
-                        (w.b * a.H + w.kvh * a.G + t / per) * a.Nq + w.first +
-                        t % per * 128;
-                    if (c >= X::kQ &&
-                        !(ok = mbar_wait_or_abort(&bars.q_empty[qs],
-                                                  (c / X::kQ - 1) & 1, abort,
-                                                  status, 442)))
-                        break;
-                    mbar_expect_tx(&bars.q_full[qs], kTile);
-                    tile(&bars.q_full[qs], sQ + qs * kTile, &tmQ, row);
-                    if (c >= X::kG &&
-                        !(ok = mbar_wait_or_abort(&bars.g_empty[gs],
-                                                  (c / X::kG - 1) & 1, abort,
-                                                  status, 443)))
-                        break;
-                    mbar_expect_tx(&bars.g_full[gs], kTile);
-                    tile(&bars.g_full[gs], sG + gs * kTile, &tmG, row);
-                }
+                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
+                for (int g = 0; g < a.G && ok; ++g)
+                    for (int i = w.first; i < w.ql; i += 128, ++c) {
+                        const int qs = c % X::kQ;
+                        if (c >= X::kQ &&
+                            !(ok = mbar_wait_or_abort(&bars.q_empty[qs],
+                                                      (c / X::kQ - 1) & 1,
+                                                      abort, status, 442)))
+                            break;
+                        mbar_expect_tx(&bars.q_full[qs], kTile);
+                        tile(&bars.q_full[qs], sQ + qs * kTile, &tmQ,
+                             q0 + g * a.Nq + i);
+                    }
+            }
+        } else if (warp == 11 && lane_id == 0) {
+            // ---------------------------------------------- loads of dO
+            int c = 0;
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!mbar_wait_or_abort(&bars.item_full[it & 1], (it >> 1) & 1,
+                                        abort, status, 443))
+                    break;
+                const BwdItem w = item_s[it & 1];
+                mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
+                for (int g = 0; g < a.G && ok; ++g)
+                    for (int i = w.first; i < w.ql; i += 128, ++c) {
+                        const int gs = c % X::kG;
+                        if (c >= X::kG &&
+                            !(ok = mbar_wait_or_abort(&bars.g_empty[gs],
+                                                      (c / X::kG - 1) & 1,
+                                                      abort, status, 458)))
+                            break;
+                        mbar_expect_tx(&bars.g_full[gs], kTile);
+                        for (int p = 0; p < kPanels<D>; ++p)
+                            tma_load_2d(sG + gs * kTile + p * 16384, &tmG,
+                                        64 * p, q0 + g * a.Nq + i,
+                                        &bars.g_full[gs]);
+                    }
             }
         } else if (warp == 8) {
             // ---------------------------------------------------- MMA issue
@@ -645,18 +709,18 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 const int n = w.n;
                 if (n == 0) continue;
                 if (!wait(&bars.kv_full, ks & 1, 445)) break;
-                const int per = tiles_of(w);
-                // rows that the sequence does not have count with weights of
-                // 0 and must be numbers
-                auto part = [&](int t) {
-                    return w.ql - w.first - t % per * 128;
-                };
+                // Rows that the sequence does not have count with weights of
+                // 0 and must be numbers: rows of the next Q and dO tile that
+                // it has.
+                const int all = w.ql - w.first;
+                int left_q = all, left_g = all;
                 auto scores = [&](int t) {
                     const int x = c + t, qs = x % X::kQ;
                     if (!wait(&bars.q_full[qs], x / X::kQ & 1, 446))
                         return false;
-                    if (part(t) < 128)
-                        zero_rows<D>(sQ + qs * kTile, part(t), lane_id);
+                    if (left_q < 128)
+                        zero_rows<D>(sQ + qs * kTile, left_q, lane_id);
+                    left_q = left_q > 128 ? left_q - 128 : all;
                     tc_fence_after();
                     if (el) {
                         mma_scores<D>(tm + X::cS + 128 * (x % X::kS), dK,
@@ -669,8 +733,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     const int x = c + t, gs = x % X::kG;
                     if (!wait(&bars.g_full[gs], x / X::kG & 1, 447))
                         return false;
-                    if (part(t) < 128)
-                        zero_rows<D>(sG + gs * kTile, part(t), lane_id);
+                    if (left_g < 128)
+                        zero_rows<D>(sG + gs * kTile, left_g, lane_id);
+                    left_g = left_g > 128 ? left_g - 128 : all;
                     tc_fence_after();
                     if (el) {
                         mma_scores<D>(tm + X::cP, dV, desc_at(dG, gs * kTile));
@@ -721,12 +786,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 __syncwarp();
                 if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
                 if (w.item < 0) break;
-                const int per = tiles_of(w);
+                size_t head = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq;
+                int i0 = w.first;
                 for (int t = 0; t < w.n; ++t, ++c) {
-                    const int i0 = w.first + t % per * 128;
-                    const size_t at =
-                        (size_t)(w.b * a.H + w.kvh * a.G + t / per) * a.Nq +
-                        i0;
+                    const size_t at = head + i0;
                     float l[4], d[4];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -747,6 +810,11 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         row_d[c & 1][lane_id + 32 * q] = -d[q];
                     }
                     mbar_arrive(&bars.l_full[c & 1]);
+                    i0 += 128;
+                    if (i0 >= w.ql) {
+                        i0 = w.first;
+                        head += a.Nq;
+                    }
                 }
             }
         }
@@ -785,10 +853,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             const int first = !valid ? w.ql
                               : a.causal ? min(w.ql, max(0, j + w.ql - w.kl))
                                          : 0;
-            const int per = tiles_of(w);
+            const int lo0 = first - w.first - 64 * half;
+            const int hi0 = w.ql - w.first - 64 * half;
+            int lo = lo0, hi = hi0;  // columns of this half that see the key
             for (int t = 0; t < w.n; ++t, ++c) {
-                const int i0 = w.first + t % per * 128 + 64 * half;
-                const int lo = first - i0, hi = w.ql - i0;
                 const bool edge =
                     __any_sync(0xffffffffu, lo > 0 || hi < 64);
                 if (!(ok = warp_wait(&bars.l_full[c & 1], c / 2 & 1, abort,
@@ -847,6 +915,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 mbar_arrive(&bars.ds_full);
                 __syncwarp();
                 if (lane_id == 0) mbar_arrive(&bars.l_empty[c & 1]);
+                lo -= 128;
+                hi -= 128;
+                if (hi + 64 * half <= 0) {  // the next head
+                    lo = lo0;
+                    hi = hi0;
+                }
             }
             if (!ok) break;
             if (!(ok = warp_wait(&bars.sum_full, ks & 1, abort, status, 457)))
@@ -904,9 +978,8 @@ cudaError_t launch_exact_delta(const ExactView &a, int *counters,
 
 cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
                                cudaStream_t st) {
-    const int tiles = (int)(((long)a.G * a.Nq + 127) / 128);
-    const int per_head = (tiles + a.G - 1) / a.G;
-    const long items = (long)per_head * a.G * a.B * a.Hkv;
+    const ExactOrder order(a, 128);
+    const long items = order.items(a);
     const int sms = sm_count();
     Maps m;
     const cudaError_t e = make_maps(a, &m);
@@ -914,11 +987,11 @@ cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
     return by_width(a.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         const size_t smem =
-            1024 + (size_t)(2 + kDqK + kDqV) * kTileBytes<D>;
+            1024 + (size_t)(2 + kDqK<D> + kDqV<D>) * kTileBytes<D>;
         return launch_after(
             k_exact_dq_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
-            kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, per_head, tiles,
-            (int)items, next_item);
+            kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, order, (int)items,
+            next_item);
     });
 }
 
@@ -931,8 +1004,10 @@ cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
     if (e != cudaSuccess) return e;
     return by_width(a.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
-        const size_t smem =
-            1024 + (size_t)(2 + Dkv<D>::kQ + Dkv<D>::kG) * kTileBytes<D>;
+        constexpr size_t smem =
+            sizeof(DkvShared<D>) +
+            (size_t)(2 + Dkv<D>::kQ + Dkv<D>::kG) * kTileBytes<D>;
+        static_assert(smem <= 232448, "shared memory of a CTA");
         return launch_after(
             k_exact_dkv_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
             kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, (int)items,

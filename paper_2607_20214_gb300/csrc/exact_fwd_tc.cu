@@ -10,9 +10,11 @@
 //                   maximum nor the sum needs another thread
 //   warp 8          issues every MMA: S = Q K^T, O += P V (P from TMEM)
 //   warp 9          takes the items, TMA loads of Q, K and V
+// With few items the keys are split too: an item is then a chunk of the key
+// tiles, and k_exact_merge joins what the chunks of a row leave.
 // TMEM: S_s at 128 s, O_s at 256 + 128 s, P_s behind O_s for D <= 64, over S_s
 // at D = 128. O stays in tensor memory; a softmax warp rescales it when the
-// maximum of one of its rows grows.
+// maximum of one of its rows has grown much.
 #include <type_traits>
 
 #include "device_common.cuh"
@@ -28,9 +30,15 @@ using namespace tc;
 
 // 384 x 168 registers at launch = 256 x 208 (softmax) + 128 x 88
 constexpr int kEfThreads = 384;
-constexpr int kEfRegsSoft = 208, kEfRegsOther = 88;
+constexpr int kEfRegsSoft = 200, kEfRegsOther = 104;
 static_assert(256 * kEfRegsSoft + 128 * kEfRegsOther <= kEfThreads * 168,
               "register shares within the launch's total");
+// O is rescaled when the maximum of one of a warp's rows has grown by more than
+// this (base 2) since it last was: weights are up to 2^8, which costs neither
+// them nor their sum any precision, but for the largest, which bf16 then rounds
+// too. Rescaling for every new maximum: 753 us instead of 710 (B1 H16 H_kv4
+// N16384 d128 causal), since among 32 rows there is one in nearly every tile.
+constexpr float kGrown = 8.0f;
 constexpr int kEfStages = 2;  // key and value tiles held
 // a maximum below every score of a finite product
 constexpr float kLowest = -1e38f;
@@ -39,7 +47,7 @@ struct EfBars {
     uint64_t item_full[2], item_empty[2], q_full, q_empty;
     uint64_t k_full[kEfStages], k_empty[kEfStages];
     uint64_t v_full[kEfStages], v_empty[kEfStages];
-    uint64_t s_full[2], p_full[2], o_done[2], o_empty[2];
+    uint64_t s_full[2], p_half[2], p_full[2], o_done[2], o_empty[2];
 };
 
 // What the roles know of an item.
@@ -47,15 +55,33 @@ struct EfItem {
     int item;   // -1: no more
     int b, kvh, r0;
     int ql, kl;
-    int n[2];   // key tiles of each slot
+    int kt0;    // the first key tile
+    int n[2];   // key tiles of each slot, from kt0 on
+    int parts[2];  // chunks that each slot's rows are split into
+    int sp;     // which of them this is
 };
+
+// How the keys are split: `splits` chunks at most, of `chunk` tiles. What a
+// chunk leaves of row r (over all heads): the sums of e^(z - m) v in
+// o[sp][r][D], and (m, sum of e^(z - m)) in ml[sp][r], z and m base 2.
+struct EfSplit {
+    int splits, chunk;
+    float *o;
+    float2 *ml;
+    size_t rows;
+};
+__device__ __forceinline__ int chunks_of(const EfSplit &p, int tiles) {
+    return (tiles + p.chunk - 1) / p.chunk;
+}
 
 template <int D>
 __global__ void __launch_bounds__(kEfThreads, 1)
     k_exact_fwd_tc(const __grid_constant__ CUtensorMap tmQ,
                    const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV,
-                   const __grid_constant__ ExactView a, int tiles, int items,
+                   const __grid_constant__ ExactView a,
+                   const __grid_constant__ EfSplit split,
+                   const __grid_constant__ ExactOrder order, int items,
                    int *__restrict__ next_item) {
     wait_for_stream();
     extern __shared__ unsigned char smem_raw[];
@@ -80,6 +106,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             mbar_init(&bars.item_full[s], 1);
             mbar_init(&bars.item_empty[s], 9);  // eight softmax warps, MMA
             mbar_init(&bars.s_full[s], 1);
+            mbar_init(&bars.p_half[s], 128);
             mbar_init(&bars.p_full[s], 128);
             mbar_init(&bars.o_done[s], 1);
             mbar_init(&bars.o_empty[s], 128);
@@ -121,7 +148,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                                 row, &full[st]);
                 return true;
             };
-            const int heads = a.B * a.Hkv, rows = a.G * a.Nq;
+            const int heads = a.B * a.Hkv, rows = order.rows;
             for (int it = 0; ok; ++it) {
                 long item = blockIdx.x;
                 if (it > 0)
@@ -134,19 +161,27 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     break;
                 EfItem w = {-1};
                 if (item < items) {
-                    // the last rows of every head, which see most, first
+                    // the last rows of every query head, which see most,
+                    // first
                     const int h = (int)(item % heads);
+                    const int t = (int)(item / heads);
                     w.item = (int)item;
-                    w.r0 = (tiles - 1 - (int)(item / heads)) * 256;
+                    w.sp = t % split.splits;
+                    w.kt0 = w.sp * split.chunk;
+                    w.r0 = order.tile(t / split.splits) * 256;
                     w.b = h / a.Hkv;
                     w.kvh = h - w.b * a.Hkv;
                     const ExactSeq seq(a, w.b);
                     w.ql = seq.ql;
                     w.kl = seq.kl;
-                    for (int s = 0; s < 2; ++s)
-                        w.n[s] = (exact_most(seq, w.r0 + 128 * s,
-                                             min(w.r0 + 128 * s + 128, rows),
-                                             a.Nq) + 127) / 128;
+                    for (int s = 0; s < 2; ++s) {
+                        const int r = w.r0 + 128 * s;
+                        const int n =
+                            (exact_most(seq, r, min(r + 128, rows),
+                                        order.pitch) + 127) / 128;
+                        w.parts[s] = chunks_of(split, n);
+                        w.n[s] = max(0, min(n - w.kt0, split.chunk));
+                    }
                 }
                 item_s[it & 1] = w;
                 mbar_arrive(&bars.item_full[it & 1]);
@@ -157,14 +192,16 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                                                    abort, status, 401))
                     break;
                 ++qs;
-                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq + w.r0;
-                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
+                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
+                const int k0 =
+                    (w.b * a.Hkv + w.kvh) * a.Nk + 128 * w.kt0;
                 mbar_expect_tx(&bars.q_full,
                                ((w.n[0] > 0) + (w.n[1] > 0)) * kTileB);
                 for (int s = 0; s < 2; ++s)
                     for (int p = 0; p < kPanels && w.n[s] > 0; ++p)
                         tma_load_2d(sQ + s * kTileB + p * 16384, &tmQ, 64 * p,
-                                    q0 + 128 * s, &bars.q_full);
+                                    q0 + order.row(w.r0 + 128 * s, a.Nq),
+                                    &bars.q_full);
                 for (int kt = 0; kt < nk && ok; ++kt, ++c)
                     ok = load(bars.k_full, bars.k_empty, sK, &tmK,
                               k0 + 128 * kt, 402) &&
@@ -173,8 +210,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             }
         } else if (warp == 8) {
             // ---------------------------------------------------- MMA issue
-            // Whenever a slot's P is ready: its P V product, and right behind
-            // it the scores of its next key tile; the softmax sees these only
+            // Whenever half of a slot's P is ready: that half of its P V
+            // product; then the other half, and right behind it the scores of its next key tile; the softmax sees these only
             // when both are complete (a commit covers all that was issued
             // before it). At D = 128 the scores go over P, which relies on
             // products of one thread running in the order of their issue.
@@ -215,7 +252,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 int us0 = 0, us1 = 0, up0 = 0, up1 = 0;
                 // keys of the last tile that the sequence has: values of
                 // others count with weights of 0 and must be numbers
-                int part = w.kl - 128 * (nk - 1);
+                int part = w.kl - 128 * (w.kt0 + nk - 1);
+                bool half0 = false, half1 = false;  // P V begun
                 // the scores of slot s's next key tile
                 auto scores = [&](auto slot, int &us, int n, int us_o,
                                   int n_o) {
@@ -242,35 +280,52 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     ++us;
                     return true;
                 };
-                auto step = [&](auto slot, int &us, int &up, int &gp, int go,
-                                int n, int us_o, int up_o, int n_o) {
+                auto step = [&](auto slot, int &us, int &up, bool &half,
+                                int &gp, int go, int n, int us_o, int up_o,
+                                int n_o) {
                     constexpr int s = decltype(slot)::value;
                     constexpr uint32_t cO = 128u * s + 256u;
                     constexpr uint32_t cP = D <= 64 ? cO + 64 : 128u * s;
                     const int st = (c0 + up) % kEfStages;
-                    if (up == us || !test(&bars.p_full[s], gp & 1) ||
-                        !test(&bars.v_full[st],
-                              (c0 + up) / kEfStages & 1) ||
-                        (up == 0 && go > 0 &&
-                         !test(&bars.o_empty[s], (go - 1) & 1)))
-                        return false;
-                    if (up == nk - 1 && part < 128) {
-                        const uint32_t v = sV + st * kTileB;
-                        for (int i = part * 8 + lane_id; i < 1024; i += 32)
-                            for (int p = 0; p < kPanels; ++p)
-                                st_shared_zero16(v + p * 16384 + i * 16);
-                        part = 128;  // once for both slots
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                    }
-                    tc_fence_after();
+                    if (up == us) return false;
                     const uint64_t v = dV + st * kTile;
-                    const uint32_t more = up > 0;
+                    if (!half) {
+                        if (!test(&bars.p_half[s], gp & 1) ||
+                            !test(&bars.v_full[st],
+                                  (c0 + up) / kEfStages & 1) ||
+                            (up == 0 && go > 0 &&
+                             !test(&bars.o_empty[s], (go - 1) & 1)))
+                            return false;
+                        if (up == nk - 1 && part < 128) {
+                            const uint32_t x = sV + st * kTileB;
+                            for (int i = part * 8 + lane_id; i < 1024;
+                                 i += 32)
+                                for (int p = 0; p < kPanels; ++p)
+                                    st_shared_zero16(x + p * 16384 + i * 16);
+                            part = 128;  // once for both slots
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                        }
+                        tc_fence_after();
+                        const uint32_t more = up > 0;
+                        if (el) {
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                mma_ts(tm + cO, tm + cP + 8 * x, v + 128 * x,
+                                       id_o, x > 0 ? 1u : more);
+                        }
+                        half = true;
+                        if (!test(&bars.p_full[s], gp & 1)) return true;
+                    } else if (!test(&bars.p_full[s], gp & 1)) {
+                        return false;
+                    }
+                    half = false;
+                    tc_fence_after();
                     if (el) {
 #pragma unroll
-                        for (int x = 0; x < 8; ++x)
+                        for (int x = 4; x < 8; ++x)
                             mma_ts(tm + cO, tm + cP + 8 * x, v + 128 * x, id_o,
-                                   x > 0 ? 1u : more);
+                                   1u);
                         mma_commit(&bars.o_done[s]);
                         if (up >= n_o || up_o > up)
                             mma_commit(&bars.v_empty[st]);
@@ -287,10 +342,10 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 unsigned long long t_last = 0;
                 uint32_t idle = 0;
                 while (ok && (up0 < n0 || up1 < n1)) {
-                    const bool x = step(S0{}, us0, up0, gp0, go0, n0, us1,
-                                        up1, n1);
-                    const bool y = ok && step(S1{}, us1, up1, gp1, go1, n1,
-                                              us0, up0, n0);
+                    const bool x = step(S0{}, us0, up0, half0, gp0, go0, n0,
+                                        us1, up1, n1);
+                    const bool y = ok && step(S1{}, us1, up1, half1, gp1, go1,
+                                              n1, us0, up0, n0);
                     if (x || y) {
                         idle = 0;
                     } else if ((++idle & 255u) == 0) {
@@ -328,17 +383,19 @@ __global__ void __launch_bounds__(kEfThreads, 1)
         for (int it = 0; ok; ++it) {
             ok = wwait(&bars.item_full[it & 1], (it >> 1) & 1, 408);
             if (!ok) break;
-            const EfItem w = item_s[it & 1];
+            const EfItem &w_s = item_s[it & 1];
+            const int item = w_s.item, n = w_s.n[s], parts = w_s.parts[s];
+            const int sp = w_s.sp, kt0 = w_s.kt0, wb = w_s.b, kvh = w_s.kvh;
+            const int ql = w_s.ql, kl = w_s.kl, slot0 = w_s.r0 + 128 * s;
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
-            if (w.item < 0) break;
-            const int n = w.n[s];
-            const int r = w.r0 + 128 * s + row, i = r % a.Nq;
-            const bool valid = r < a.G * a.Nq && i < w.ql;
+            if (item < 0) break;
+            const int r = slot0 + row, i = r % order.pitch;
+            const bool valid = r < order.rows && i < ql;
             int seen = 0;
             if (valid)
-                seen = a.causal ? max(0, min(w.kl, i + 1 + w.kl - w.ql))
-                                : w.kl;
+                seen = a.causal ? max(0, min(kl, i + 1 + kl - ql))
+                                : kl;
             float mref = kLowest, lsum = 0.0f;
             for (int kt = 0; kt < n; ++kt, ++g) {
                 ok = wwait(&bars.s_full[s], g & 1, 409);
@@ -360,7 +417,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                         v[96 + q] = __uint_as_float(e[q]);
                     }
                 }
-                const int lim = seen - 128 * kt;
+                const int lim = seen - 128 * (kt0 + kt);
                 if (__any_sync(0xffffffffu, lim < 128)) {
 #pragma unroll
                     for (int q = 0; q < 128; ++q)
@@ -381,17 +438,17 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 } else {
                     // these scores were issued behind the last tile's P V
                     // product: it is complete when they are
-                    const bool need = z > mref;
+                    const bool need = z > mref + kGrown;
                     if (__any_sync(0xffffffffu, need)) {
                         const float f = need ? ex2_approx(mref - z) : 1.0f;
                         const float2 f2 = make_float2(f, f);
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(tO + c, o);
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(tO + c, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int q = 0; q < 16; q += 2) {
+                            for (int q = 0; q < 32; q += 2) {
                                 const float2 y =
                                     mul2(make_float2(__uint_as_float(o[q]),
                                                      __uint_as_float(
@@ -400,7 +457,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                                 o[q] = __float_as_uint(y.x);
                                 o[q + 1] = __float_as_uint(y.y);
                             }
-                            tmem_st16(tO + c, o);
+                            tmem_st32(tO + c, o);
                         }
                         lsum *= f;
                         if (need) mref = z;
@@ -422,6 +479,11 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                         pw[q >> 1] = pack_bf16x2(p.x, p.y);
                     }
                     tmem_st16(tP + c / 2, pw);
+                    if (c == 32) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(&bars.p_half[s]);
+                    }
                 }
                 lsum += (ls[0].x + ls[1].x) + (ls[0].y + ls[1].y);
                 tmem_wait_st();
@@ -430,13 +492,40 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             }
             if (!ok) break;
             const size_t at =
-                (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq + r;
+                (size_t)(wb * a.H + kvh * a.G) * a.Nq +
+                order.row(r, a.Nq);
             uint16_t *o = (uint16_t *)a.out + at * D;
             if (n > 0) {
                 ok = wwait(&bars.o_done[s], (g - 1) & 1, 410);
                 if (!ok) break;
                 tc_fence_after();
             }
+            if (parts > 1) {
+                if (n == 0) continue;
+                const size_t to = sp * split.rows + at;
+                float *y = split.o + to * D;
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t x[32];
+                    tmem_ld32(tO + c, x);
+                    tmem_wait_ld();
+                    if (c + 32 == D) {
+                        tc_fence_before();
+                        mbar_arrive(&bars.o_empty[s]);
+                    }
+                    if (!valid) continue;
+#pragma unroll
+                    for (int q = 0; q < 32; q += 8) {
+                        uint32_t e[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) e[i] = x[q + i];
+                        st_global_v8(y + c + q, e);
+                    }
+                }
+                if (valid) split.ml[to] = make_float2(mref, lsum);
+                continue;
+            }
+            if (sp > 0) continue;
             // a row that sees nothing, or only scores of -inf: zeros
             const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
 #pragma unroll
@@ -478,19 +567,90 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     if (warp == 8) tmem_dealloc(tm, 512);
 }
 
+// Joins the chunks of the rows that have more than one: D / 8 lanes a row.
+template <int D>
+__global__ void __launch_bounds__(256)
+    k_exact_merge(const __grid_constant__ ExactView a,
+                  const __grid_constant__ EfSplit split,
+                  const __grid_constant__ ExactOrder order) {
+    wait_for_stream();
+    constexpr int L = D / 8;
+    const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int c = threadIdx.x % L * 8;
+    if (row >= split.rows) return;
+    const int group = a.G * a.Nq;  // rows of a K/V head's queries
+    const int x = (int)(row % group), i = x % a.Nq;
+    const ExactSeq seq(a, (int)(row / group) / a.Hkv);
+    if (i >= seq.ql) return;
+    // the slot that had the row
+    const int r0 = (x / a.Nq * order.pitch + i) / 128 * 128;
+    const int n = (exact_most(seq, r0, min(r0 + 128, order.rows),
+                              order.pitch) + 127) / 128;
+    const int parts = chunks_of(split, n);
+    if (parts < 2) return;
+    float m = kLowest;
+    for (int p = 0; p < parts; ++p)
+        m = fmaxf(m, split.ml[p * split.rows + row].x);
+    float l = 0.0f, o[8] = {};
+    for (int p = 0; p < parts; ++p) {
+        const float2 ml = split.ml[p * split.rows + row];
+        const float f = ex2_approx(ml.x - m);
+        l = fmaf(ml.y, f, l);
+        const float4 *x = reinterpret_cast<const float4 *>(
+            split.o + (p * split.rows + row) * D + c);
+        const float4 u = x[0], v = x[1];
+        const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = fmaf(e[i], f, o[i]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        y[i] = pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
+    *reinterpret_cast<uint4 *>((uint16_t *)a.out + row * D + c) =
+        make_uint4(y[0], y[1], y[2], y[3]);
+    if (a.lse && c == 0)
+        a.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Chunks of the keys, so that there are four items for each of a GB300's 152
+// SMs, and 4 tiles (512 keys) at least in a chunk. (Fixed, so that the
+// workspace does not depend on the device.)
+void divide_keys(const ExactView &a, int *splits, int *chunk) {
+    const long items = ExactOrder(a, 256).items(a);
+    const int tiles = (a.Nk + 127) / 128;
+    long n = (4 * 152 + items - 1) / items;
+    if (n > tiles / 4) n = tiles / 4;
+    if (n < 1) n = 1;
+    *chunk = (int)((tiles + n - 1) / n);
+    *splits = (tiles + *chunk - 1) / *chunk;
+}
+
 }  // namespace
 
+size_t exact_split_bytes(const ExactView &a) {
+    int splits, chunk;
+    divide_keys(a, &splits, &chunk);
+    if (splits == 1) return 0;
+    return sizeof(float) * (a.d + 2) * (size_t)splits * a.B * a.H * a.Nq;
+}
+
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
-                                cudaStream_t st) {
-    const int tiles = (int)(((long)a.G * a.Nq + 255) / 256);
-    const long items = (long)tiles * a.B * a.Hkv;
+                                float *part, cudaStream_t st) {
+    EfSplit split = {};
+    divide_keys(a, &split.splits, &split.chunk);
+    split.rows = (size_t)a.B * a.H * a.Nq;
+    split.o = part;
+    split.ml = (float2 *)(part + split.rows * split.splits * a.d);
+    const ExactOrder order(a, 256);
+    const long items = order.items(a) * split.splits;
     int dev = 0, sms = 152;
     if (cudaGetDevice(&dev) == cudaSuccess)
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     CUtensorMap tmQ, tmK, tmV;
-    const uint64_t nq = (uint64_t)a.B * a.H * a.Nq;
     const uint64_t nk = (uint64_t)a.B * a.Hkv * a.Nk;
-    cudaError_t e = make_tma_map_bf16(&tmQ, a.q, nq, a.d, 128);
+    cudaError_t e = make_tma_map_bf16(&tmQ, a.q, split.rows, a.d, 128);
     if (e == cudaSuccess) e = make_tma_map_bf16(&tmK, a.k, nk, a.d, 128);
     if (e == cudaSuccess) e = make_tma_map_bf16(&tmV, a.v, nk, a.d, 128);
     // more items than CTAs: they are taken from a counter
@@ -501,10 +661,16 @@ cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
         constexpr int D = decltype(dim)::value;
         const size_t smem =
             1024 + (size_t)(2 + 2 * kEfStages) * (D > 64 ? 2 : 1) * 16384;
-        return launch_after(
+        cudaError_t r = launch_after(
             k_exact_fwd_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
-            kEfThreads, smem, st, tmQ, tmK, tmV, a, tiles, (int)items,
-            items > sms ? next_item : nullptr);
+            kEfThreads, smem, st, tmQ, tmK, tmV, a, split, order,
+            (int)items, items > sms ? next_item : nullptr);
+        if (r == cudaSuccess && split.splits > 1)
+            r = launch_after(
+                k_exact_merge<D>,
+                dim3((unsigned)((split.rows * (D / 8) + 255) / 256)), 256, 0,
+                st, a, split, order);
+        return r;
     };
     return a.d == 128  ? launch(std::integral_constant<int, 128>{})
            : a.d == 64 ? launch(std::integral_constant<int, 64>{})

@@ -293,3 +293,33 @@ def test_argument_checks():
                                    :128])
     with pytest.raises(TypeError):
         E.elsaa_exact_forward(ex, None, k, v)
+
+
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d,causal,kl", [
+    (1, 1, 1, 1, 5000, 64, 1, None), (2, 8, 2, 2, 3000, 128, 1, [2999, 700]),
+    (1, 1, 1, 700, 2100, 64, 1, None), (1, 2, 1, 300, 1300, 32, 0, [1]),
+    (3, 2, 2, 1100, 1100, 64, 1, [1100, 513, 0])])
+def test_keys_in_chunks(B, H, Hkv, Nq, Nk, d, causal, kl):
+    """Few items: the keys of a row are split and joined."""
+    ql = None if kl is None else [Nq] + [max(1, Nq // 2)] * (B - 1)
+    run_case(B, H, Hkv, Nq, Nk, d, BF, causal, ql=ql, kl=kl, backward=False)
+    run_case(B, H, Hkv, Nq, Nk, d, F32, causal, ql=ql, kl=kl, backward=False)
+
+
+def test_long_rows_in_chunks():
+    """Rows of more keys than a chunk beside rows of few, chunks whose keys
+    none of a tile's rows sees, peaks in one chunk."""
+    q, k, v, _ = C.exact_inputs(1, 1, 1, 1600, 1600, 64, BF, 4)
+    k[0, 0, 777] *= 9.0
+    ref = C.exact_forward_ref(q, k, v, 0.125, 1, [1600], [1600], True)[0, 0]
+    ex = E.make_exact(1, 1, 1, 1600, 1600, 64, causal=True)
+    lse = torch.empty((1, 1, 1600), device="cuda")
+    o = E.elsaa_exact_forward(ex, q.cuda(), k.cuda(), v.cuda(), lse=lse)
+    C.close(o[0, 0], ref["o"], ref["o_tol"], "o")
+    C.close(lse[0, 0], ref["lse"], ref["lse_tol"], "lse")
+
+
+def test_many_short_sequences():
+    """More items than a grid's first CTAs, single tokens of grouped heads."""
+    run_case(200, 8, 2, 1, 40, 64, BF, 1, backward=False)
+    run_case(100, 4, 2, 3, 5, 32, BF, 1)
