@@ -20,10 +20,14 @@ namespace {
 
 using namespace tc;
 
-// 384 x 168 registers at launch = 256 x 208 (weights) + 128 x 88
-constexpr int kEbThreads = 384;
-constexpr int kEbRegsSoft = 208, kEbRegsOther = 88;
-static_assert(256 * kEbRegsSoft + 128 * kEbRegsOther <= kEbThreads * 168,
+// 16 warps make weights, four threads a row with 32 columns each; four others
+// issue and load. (With 8 warps, two threads a row, each iteration's waits,
+// loads and exponentials stood one behind the other.)
+constexpr int kEbWeights = 16;
+constexpr int kEbThreads = 32 * (kEbWeights + 4);
+// 640 x 96 registers at launch = 512 x 104 (weights) + 128 x 64
+constexpr int kEbRegsSoft = 104, kEbRegsOther = 64;
+static_assert(512 * kEbRegsSoft + 128 * kEbRegsOther <= kEbThreads * 96,
               "register shares within the launch's total");
 
 template <int D>
@@ -31,38 +35,52 @@ constexpr int kPanels = D > 64 ? 2 : 1;
 template <int D>
 constexpr uint32_t kTileBytes = kPanels<D> * 16384;  // 128 rows
 
+// A test of a barrier takes about 54 clocks, a try_wait 90.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t par,
                                           volatile int *abort,
                                           DeviceStatus *st, int site) {
+    if (__all_sync(0xffffffffu, mbar_test(bar, par))) return true;
     return __all_sync(0xffffffffu,
                       mbar_wait_or_abort(bar, par, abort, st, site));
 }
+// Two at once, tested side by side.
+__device__ __forceinline__ bool warp_wait2(uint64_t *a, uint32_t pa,
+                                           uint64_t *b, uint32_t pb,
+                                           volatile int *abort,
+                                           DeviceStatus *st, int site) {
+    const bool ready = mbar_test(a, pa) & mbar_test(b, pb);
+    if (__all_sync(0xffffffffu, ready)) return true;
+    return __all_sync(0xffffffffu,
+                      mbar_wait_or_abort(a, pa, abort, st, site) &&
+                          mbar_wait_or_abort(b, pb, abort, st, site));
+}
 
-// 64 columns of tensor memory
-__device__ __forceinline__ void load64(uint32_t t, float2 (&x)[32]) {
-    uint32_t a[32], b[32];
+// 32 columns of tensor memory
+__device__ __forceinline__ void load32(uint32_t t, float2 (&x)[16]) {
+    uint32_t a[32];
     tmem_ld32(t, a);
-    tmem_ld32(t + 32, b);
     tmem_wait_ld();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 16; ++i)
         x[i] = make_float2(__uint_as_float(a[2 * i]),
                            __uint_as_float(a[2 * i + 1]));
-        x[16 + i] = make_float2(__uint_as_float(b[2 * i]),
-                                __uint_as_float(b[2 * i + 1]));
-    }
 }
-// as bf16 (rounded to nearest) in 32 columns
-__device__ __forceinline__ void store64(uint32_t t, const float2 (&x)[32]) {
-    uint32_t y[32];
+// as bf16 (rounded to nearest) in 16 columns, for the products: one lane of
+// the warp then arrives on `bar`
+__device__ __forceinline__ void store32(uint32_t t, const float2 (&x)[16],
+                                        uint64_t *bar, int lane_id) {
+    uint32_t y[16];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) y[i] = pack_bf16x2(x[i].x, x[i].y);
-    tmem_st32(t, y);
+    for (int i = 0; i < 16; ++i) y[i] = pack_bf16x2(x[i].x, x[i].y);
+    tmem_st16(t, y);
     tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if (lane_id == 0) mbar_arrive(bar);
 }
 
 // One operand's product of K = D (both K-major) and of K = 128 (A from tensor
-// memory: columns 0..31 and 64..95, as the two halves' threads write them; B
+// memory: 16 columns of every 32, as the four quarters' threads write them; B
 // MN-major), issued by one lane.
 template <int D>
 __device__ __forceinline__ void mma_scores(uint32_t dst, uint64_t a,
@@ -80,7 +98,7 @@ __device__ __forceinline__ void mma_sums(uint32_t dst, uint32_t a, uint64_t b,
     const uint32_t id = idesc_bf16(128, D, false, true);
 #pragma unroll
     for (int x = 0; x < 8; ++x)
-        mma_ts(dst, a + (x >> 2) * 64 + (x & 3) * 8, b + 128 * x, id,
+        mma_ts(dst, a + (x >> 1) * 32 + (x & 1) * 8, b + 128 * x, id,
                x > 0 || more);
 }
 
@@ -95,12 +113,18 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int part,
     __syncwarp();
 }
 
-// D / 2 columns of sums in tensor memory, times f, to a row of bf16.
+// The columns of sums that a thread writes, and how many threads share a row.
+template <int D>
+constexpr int kOut = D > 64 ? 32 : 16;
+template <int D>
+constexpr int kOutShare = D / kOut<D>;
+
+// kOut columns of sums in tensor memory, times f, to a row of bf16.
 template <int D>
 __device__ __forceinline__ void store_sums(uint32_t t, float f, uint16_t *o,
                                            bool valid) {
 #pragma unroll
-    for (int c = 0; c < D / 2; c += 16) {
+    for (int c = 0; c < kOut<D>; c += 16) {
         uint32_t x[16], y[8];
         tmem_ld16(t + c, x);
         tmem_wait_ld();
@@ -118,7 +142,7 @@ __device__ __forceinline__ void store_sums(uint32_t t, float f, uint16_t *o,
 template <int D>
 __device__ __forceinline__ void store_zeros(uint16_t *o) {
 #pragma unroll
-    for (int c = 0; c < D / 2; c += 8)
+    for (int c = 0; c < kOut<D>; c += 8)
         *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
 }
 
@@ -181,10 +205,10 @@ struct BwdItem {
 };
 
 // A CTA holds Q and dO of 128 rows (of the heads that share a K/V head,
-// counted through) and walks key tiles. Warps 0-7: weights, two threads a row,
-// one for keys 0..63 of a tile, one for 64..127; warp 8 issues the products;
-// warp 9 takes the items and loads Q, dO and K, warp 10 V. Tensor memory: S of
-// two tiles, dP, dQ; dS goes over the S it came from.
+// counted through) and walks key tiles. Warps 0-15: weights, four threads a
+// row, for 32 keys of a tile each; warp 16 issues S and dQ, warp 17 dP; warp 18
+// takes the items and loads Q, dO and K, warp 19 V. Tensor memory: S of two
+// tiles, dP, dQ; dS goes over the S it came from.
 template <int D>
 __global__ void __launch_bounds__(kEbThreads, 1)
     k_exact_dq_tc(const __grid_constant__ CUtensorMap tmQ,
@@ -209,13 +233,13 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     const uint32_t sK = sG + kTile, sV = sK + kK * kTile;
     DeviceStatus *status = a.status;
 
-    if (warp == 8) tmem_alloc(&tbase, 512);
+    if (warp == kEbWeights) tmem_alloc(&tbase, 512);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], 10);
+            mbar_init(&bars.item_empty[s], kEbWeights + 3);
             mbar_init(&bars.s_full[s], 1);
-            mbar_init(&bars.ds_full[s], 256);
+            mbar_init(&bars.ds_full[s], kEbWeights);
         }
         for (int s = 0; s < kK; ++s) {
             mbar_init(&bars.k_full[s], 1);
@@ -226,11 +250,11 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             mbar_init(&bars.v_empty[s], 1);
         }
         mbar_init(&bars.q_full, 1);
-        mbar_init(&bars.q_empty, 1);
+        mbar_init(&bars.q_empty, 2);  // S and dP
         mbar_init(&bars.dp_full, 1);
-        mbar_init(&bars.dp_read, 256);
+        mbar_init(&bars.dp_read, kEbWeights);
         mbar_init(&bars.dq_full, 1);
-        mbar_init(&bars.dq_empty, 256);
+        mbar_init(&bars.dq_empty, 4 * kOutShare<D>);
         abort_flag = 0;
         fence_mbar_init();
     }
@@ -239,10 +263,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     tc_fence_after();
     const uint32_t tm = tbase;
 
-    if (warp >= 8) {
+    if (warp >= kEbWeights) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
             kEbRegsOther));
-        if (warp == 9 && lane_id == 0) {
+        if (warp == kEbWeights + 2 && lane_id == 0) {
             // ---------------------------------------------- items and loads
             int c = 0, qs = 0;  // key tiles and items loaded so far
             bool ok = true;
@@ -300,7 +324,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                          k0 + 128 * kt);
                 }
             }
-        } else if (warp == 10 && lane_id == 0) {
+        } else if (warp == kEbWeights + 3 && lane_id == 0) {
             // ------------------------------------------ loads of the values
             int c = 0;
             bool ok = true;
@@ -325,16 +349,18 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                     k0 + 128 * kt, &bars.v_full[vs]);
                 }
             }
-        } else if (warp == 8) {
+        } else if (warp < kEbWeights + 2) {
             // ---------------------------------------------------- MMA issue
-            // In the order S(j+2), dP(j+1), dQ(j): the weights of tile j are
-            // made while the products around them run. S(j+2) goes over dS(j)
+            // One warp for S and dQ, one for dP: a wait costs a warp about 150
+            // clocks even when there is nothing to wait for, and few products
+            // are queued behind those that run. S(j + 2) goes over dS(j)
             // behind dQ(j), which reads it: products of one thread run in the
             // order of their issue.
             const bool el = elect_one();
             auto wait = [&](uint64_t *bar, uint32_t par, int site) {
                 return warp_wait(bar, par, abort, status, site);
             };
+            const bool first = warp == kEbWeights;
             const uint64_t dQ = smem_desc(sQ, 16, 1024);
             const uint64_t dG = smem_desc(sG, 16, 1024);
             const uint64_t dK = smem_desc(sK, 16, 1024);
@@ -344,50 +370,54 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             bool ok = true;
             for (int it = 0; ok; ++it) {
                 if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 424)) break;
-                const BwdItem w = item_s[it & 1];
+                const int item = item_s[it & 1].item, n = item_s[it & 1].n;
+                const int kl = item_s[it & 1].kl;
                 __syncwarp();
                 if (el) mbar_arrive(&bars.item_empty[it & 1]);
-                if (w.item < 0) break;
-                const int n = w.n;
+                if (item < 0) break;
                 if (n == 0) continue;
                 if (!wait(&bars.q_full, qs & 1, 425)) break;
+                if (!first) {
+                    for (int j = 0; j < n; ++j) {
+                        const int x = c + j, vs = x % kV;
+                        ok = wait(&bars.v_full[vs], x / kV & 1, 427) &&
+                             (x == 0 ||
+                              wait(&bars.dp_read, (x - 1) & 1, 428));
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (el) {
+                            mma_scores<D>(tm + kP, dG, desc_at(dV, vs * kTile));
+                            mma_commit(&bars.dp_full);
+                            mma_commit(&bars.v_empty[vs]);
+                            if (j == n - 1) mma_commit(&bars.q_empty);
+                        }
+                    }
+                    c += n;
+                    ++qs;
+                    continue;
+                }
                 auto scores = [&](int j) {
                     const int x = c + j, ks = x % kK;
                     if (!wait(&bars.k_full[ks], x / kK & 1, 426))
                         return false;
                     // keys that the sequence does not have count with dS = 0
                     // in dQ and must be numbers
-                    if (w.kl - 128 * j < 128)
-                        zero_rows<D>(sK + ks * kTile, w.kl - 128 * j, lane_id);
+                    if (kl - 128 * j < 128)
+                        zero_rows<D>(sK + ks * kTile, kl - 128 * j, lane_id);
                     tc_fence_after();
                     if (el) {
                         mma_scores<D>(tm + kS + 128 * (x & 1), dQ,
                                       desc_at(dK, ks * kTile));
                         mma_commit(&bars.s_full[x & 1]);
-                    }
-                    return true;
-                };
-                auto products = [&](int j) {
-                    const int x = c + j, vs = x % kV;
-                    if (!wait(&bars.v_full[vs], x / kV & 1, 427))
-                        return false;
-                    if (x > 0 && !wait(&bars.dp_read, (x - 1) & 1, 428))
-                        return false;
-                    tc_fence_after();
-                    if (el) {
-                        mma_scores<D>(tm + kP, dG, desc_at(dV, vs * kTile));
-                        mma_commit(&bars.dp_full);
-                        mma_commit(&bars.v_empty[vs]);
                         if (j == n - 1) mma_commit(&bars.q_empty);
                     }
                     return true;
                 };
-                ok = scores(0) && (n < 2 || scores(1)) && products(0);
+                ok = scores(0) && (n < 2 || scores(1));
                 if (ok && qs > 0)
                     ok = wait(&bars.dq_empty, (qs - 1) & 1, 429);
                 for (int j = 0; j < n && ok; ++j) {
                     const int x = c + j, ks = x % kK;
-                    if (j + 1 < n && !(ok = products(j + 1))) break;
                     ok = wait(&bars.ds_full[x & 1], x / 2 & 1, 430);
                     if (!ok) break;
                     tc_fence_after();
@@ -407,9 +437,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     } else {
         // ---------------------------------------------------------- weights
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEbRegsSoft));
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane_id;
+        const int part = warp >> 2, row = (warp & 3) * 32 + lane_id;
         const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t0 = tm + lane + 64 * half;
+        const uint32_t t0 = tm + lane + 32 * part;
         const float sl2 = a.scale * kLog2e;
         const float2 sl22 = make_float2(sl2, sl2);
         int c = 0, qs = 0;
@@ -422,13 +452,14 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
             if (w.item < 0) break;
+            const bool writes = part < kOutShare<D>;
             const int r = w.r0 + row, i = r % order.pitch;
             const bool valid = r < order.rows && i < w.ql;
             const size_t at = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq +
                               order.row(r, a.Nq);
-            uint16_t *o = (uint16_t *)a.dq + at * D + D / 2 * half;
+            uint16_t *o = (uint16_t *)a.dq + at * D + kOut<D> * part;
             if (w.n == 0) {
-                if (valid) store_zeros<D>(o);
+                if (valid && writes) store_zeros<D>(o);
                 continue;
             }
             int seen = 0;
@@ -446,10 +477,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     break;
                 tc_fence_after();
                 const uint32_t tS = t0 + kS + 128 * (c & 1);
-                float2 p[32], g[32];
-                load64(tS, p);
+                float2 p[16], g[16];
+                load32(tS, p);
 #pragma unroll
-                for (int q = 0; q < 32; ++q) {
+                for (int q = 0; q < 16; ++q) {
                     p[q] = fma2(p[q], sl22, nl2);
                     p[q] = make_float2(ex2_approx(p[q].x), ex2_approx(p[q].y));
                 }
@@ -457,37 +488,38 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                      433)))
                     break;
                 tc_fence_after();
-                load64(t0 + kP, g);
+                load32(t0 + kP, g);
                 tc_fence_before();
-                mbar_arrive(&bars.dp_read);
+                __syncwarp();
+                if (lane_id == 0) mbar_arrive(&bars.dp_read);
 #pragma unroll
-                for (int q = 0; q < 32; ++q)
+                for (int q = 0; q < 16; ++q)
                     g[q] = mul2(p[q], add2(g[q], nd2));
-                const int lim = seen - 128 * j - 64 * half;
-                if (__any_sync(0xffffffffu, lim < 64)) {
+                const int lim = seen - 128 * j - 32 * part;
+                if (__any_sync(0xffffffffu, lim < 32)) {
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) {
+                    for (int q = 0; q < 16; ++q) {
                         if (2 * q >= lim) g[q].x = 0.0f;
                         if (2 * q + 1 >= lim) g[q].y = 0.0f;
                     }
                 }
-                store64(tS, g);
-                tc_fence_before();
-                mbar_arrive(&bars.ds_full[c & 1]);
+                store32(tS, g, &bars.ds_full[c & 1], lane_id);
             }
             if (!ok) break;
             if (!(ok = warp_wait(&bars.dq_full, qs & 1, abort, status, 434)))
                 break;
             ++qs;
             tc_fence_after();
-            store_sums<D>(tm + lane + kO + D / 2 * half, a.scale, o, valid);
+            if (!writes) continue;
+            store_sums<D>(tm + lane + kO + kOut<D> * part, a.scale, o, valid);
             tc_fence_before();
-            mbar_arrive(&bars.dq_empty);
+            __syncwarp();
+            if (lane_id == 0) mbar_arrive(&bars.dq_empty);
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) tmem_dealloc(tm, 512);
+    if (warp == kEbWeights) tmem_dealloc(tm, 512);
 }
 
 // --------------------------------------------------------------- dK and dV
@@ -506,7 +538,7 @@ struct DkvBars {
     uint64_t item_full[2], item_empty[2], kv_full, kv_empty;
     uint64_t q_full[Dkv<D>::kQ], q_empty[Dkv<D>::kQ];
     uint64_t g_full[Dkv<D>::kG], g_empty[Dkv<D>::kG];
-    uint64_t l_full[2], l_empty[2], s_full[2], p_full[2];
+    uint64_t l_empty[2], s_full[2], p_full[2];
     uint64_t dp_full, ds_full, sum_full, sum_empty;
 };
 
@@ -522,11 +554,11 @@ struct DkvShared {
 
 // A CTA holds K and V of 128 rows and walks tiles of 128 query rows of every
 // head that reads them; scores and weights stand transposed, a key a lane.
-// Warps 0-7: weights, two threads a key, for queries 0..63 and 64..127 of a
-// tile; warp 8 issues the products; warp 9 takes the items and loads K, V and
-// Q, warp 11 dO; warp 10 fetches the rows' lse and D. Tensor memory: S^T (two
-// for D <= 64), dP^T, dV, dK; P^T and dS^T go over the S^T and dP^T that they
-// came from.
+// Warps 0-15: weights, four threads a key, for 32 queries of a tile each; warp
+// 16 issues the products; warp 18 takes the items and loads K, V and Q; warp 19
+// loads dO and fetches the rows' lse and D. Tensor memory: S^T (two for
+// D <= 64), dP^T, dV, dK; P^T and dS^T go over the S^T and dP^T that they came
+// from.
 template <int D>
 __global__ void __launch_bounds__(kEbThreads, 1)
     k_exact_dkv_tc(const __grid_constant__ CUtensorMap tmQ,
@@ -557,15 +589,14 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     const uint32_t sQ = sV + kTile, sG = sQ + X::kQ * kTile;
     DeviceStatus *status = a.status;
 
-    if (warp == 8) tmem_alloc(&sh.tbase, 512);
+    if (warp == kEbWeights) tmem_alloc(&sh.tbase, 512);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], 11);
-            mbar_init(&bars.l_full[s], 32);
-            mbar_init(&bars.l_empty[s], 8);
-            mbar_init(&bars.s_full[s], 1);
-            mbar_init(&bars.p_full[s], 256);
+            mbar_init(&bars.item_empty[s], kEbWeights + 2);
+            mbar_init(&bars.l_empty[s], kEbWeights);
+            mbar_init(&bars.s_full[s], 2);  // the product, lse and D
+            mbar_init(&bars.p_full[s], kEbWeights);
         }
         for (int s = 0; s < X::kG; ++s) {
             mbar_init(&bars.g_full[s], 1);
@@ -578,9 +609,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         mbar_init(&bars.kv_full, 1);
         mbar_init(&bars.kv_empty, 1);
         mbar_init(&bars.dp_full, 1);
-        mbar_init(&bars.ds_full, 256);
+        mbar_init(&bars.ds_full, kEbWeights);
         mbar_init(&bars.sum_full, 1);
-        mbar_init(&bars.sum_empty, 256);
+        mbar_init(&bars.sum_empty, 4 * kOutShare<D>);
         sh.abort_flag = 0;
         fence_mbar_init();
     }
@@ -593,10 +624,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         return (w.ql - w.first + 127) / 128;
     };
 
-    if (warp >= 8) {
+    if (warp >= kEbWeights) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
             kEbRegsOther));
-        if (warp == 9 && lane_id == 0) {
+        if (warp == kEbWeights + 2 && lane_id == 0) {
             // ---------------------------------------------- items and loads
             int c = 0, ks = 0;  // query tiles and items loaded so far
             bool ok = true;
@@ -655,42 +686,23 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                              q0 + g * a.Nq + i);
                     }
             }
-        } else if (warp == 11 && lane_id == 0) {
-            // ---------------------------------------------- loads of dO
-            int c = 0;
-            bool ok = true;
-            for (int it = 0; ok; ++it) {
-                if (!mbar_wait_or_abort(&bars.item_full[it & 1], (it >> 1) & 1,
-                                        abort, status, 443))
-                    break;
-                const BwdItem w = item_s[it & 1];
-                mbar_arrive(&bars.item_empty[it & 1]);
-                if (w.item < 0) break;
-                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
-                for (int g = 0; g < a.G && ok; ++g)
-                    for (int i = w.first; i < w.ql; i += 128, ++c) {
-                        const int gs = c % X::kG;
-                        if (c >= X::kG &&
-                            !(ok = mbar_wait_or_abort(&bars.g_empty[gs],
-                                                      (c / X::kG - 1) & 1,
-                                                      abort, status, 458)))
-                            break;
-                        mbar_expect_tx(&bars.g_full[gs], kTile);
-                        for (int p = 0; p < kPanels<D>; ++p)
-                            tma_load_2d(sG + gs * kTile + p * 16384, &tmG,
-                                        64 * p, q0 + g * a.Nq + i,
-                                        &bars.g_full[gs]);
-                    }
-            }
-        } else if (warp == 8) {
+        } else if (warp == kEbWeights) {
             // ---------------------------------------------------- MMA issue
             // In the order dV(t), S(t + kS), dK(t), dP(t + 1): P(t + 1) is
             // made during dK(t) and dP(t + 1), dS(t) during dV(t) and
-            // S(t + kS). Products of one thread run in the order of their
-            // issue, which S over P and dP over dS rely on.
+            // S(t + kS). Few products are queued behind those that run, so
+            // that the tensor cores stand still during waits, even such that
+            // find their barrier complete: two products a wait. (A warp for
+            // each pair let the pairs' products run mixed, each of them later:
+            // 216 us instead of 201 at D = 128.) Products of one thread run in
+            // the order of their issue, which S over P and dP over dS rely on.
             const bool el = elect_one();
             auto wait = [&](uint64_t *bar, uint32_t par, int site) {
                 return warp_wait(bar, par, abort, status, site);
+            };
+            auto wait2 = [&](uint64_t *x, uint32_t px, uint64_t *y,
+                             uint32_t py, int site) {
+                return warp_wait2(x, px, y, py, abort, status, site);
             };
             const uint64_t dK = smem_desc(sK, 16, 1024);
             const uint64_t dV = smem_desc(sV, 16, 1024);
@@ -702,22 +714,19 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             bool ok = true;
             for (int it = 0; ok; ++it) {
                 if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 444)) break;
-                const BwdItem w = item_s[it & 1];
+                const int item = item_s[it & 1].item, n = item_s[it & 1].n;
+                // Rows that the sequence does not have count with weights of
+                // 0 and must be numbers: rows of the next Q or dO tile that
+                // it has.
+                const int all = item_s[it & 1].ql - item_s[it & 1].first;
                 __syncwarp();
                 if (el) mbar_arrive(&bars.item_empty[it & 1]);
-                if (w.item < 0) break;
-                const int n = w.n;
+                if (item < 0) break;
                 if (n == 0) continue;
-                if (!wait(&bars.kv_full, ks & 1, 445)) break;
-                // Rows that the sequence does not have count with weights of
-                // 0 and must be numbers: rows of the next Q and dO tile that
-                // it has.
-                const int all = w.ql - w.first;
                 int left_q = all, left_g = all;
+                // the tile of S(t) or dP(t) is there
                 auto scores = [&](int t) {
                     const int x = c + t, qs = x % X::kQ;
-                    if (!wait(&bars.q_full[qs], x / X::kQ & 1, 446))
-                        return false;
                     if (left_q < 128)
                         zero_rows<D>(sQ + qs * kTile, left_q, lane_id);
                     left_q = left_q > 128 ? left_q - 128 : all;
@@ -725,14 +734,11 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     if (el) {
                         mma_scores<D>(tm + X::cS + 128 * (x % X::kS), dK,
                                       desc_at(dQ, qs * kTile));
-                        mma_commit(&bars.s_full[x % X::kS]);
+                        mma_commit(&bars.s_full[x & 1]);
                     }
-                    return true;
                 };
                 auto products = [&](int t) {
                     const int x = c + t, gs = x % X::kG;
-                    if (!wait(&bars.g_full[gs], x / X::kG & 1, 447))
-                        return false;
                     if (left_g < 128)
                         zero_rows<D>(sG + gs * kTile, left_g, lane_id);
                     left_g = left_g > 128 ? left_g - 128 : all;
@@ -742,15 +748,29 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         mma_commit(&bars.dp_full);
                         if (t == n - 1) mma_commit(&bars.kv_empty);
                     }
-                    return true;
                 };
-                ok = scores(0) && products(0) &&
-                     (X::kS < 2 || n < 2 || scores(1));
-                if (ok && ks > 0)
-                    ok = wait(&bars.sum_empty, (ks - 1) & 1, 448);
+                auto q_at = [&](int t) { return &bars.q_full[(c + t) % X::kQ]; };
+                auto g_at = [&](int t) { return &bars.g_full[(c + t) % X::kG]; };
+                ok = wait2(&bars.kv_full, ks & 1, q_at(0), c / X::kQ & 1, 445);
+                if (!ok) break;
+                scores(0);
+                if (!(ok = wait(g_at(0), c / X::kG & 1, 447))) break;
+                products(0);
+                if (X::kS > 1 && n > 1) {
+                    ok = wait(q_at(1), (c + 1) / X::kQ & 1, 446);
+                    if (!ok) break;
+                    scores(1);
+                }
+                if (ks > 0 &&
+                    !(ok = wait(&bars.sum_empty, (ks - 1) & 1, 448)))
+                    break;
                 for (int t = 0; t < n && ok; ++t) {
                     const int x = c + t, qs = x % X::kQ, gs = x % X::kG;
-                    ok = wait(&bars.p_full[x % X::kS], x / X::kS & 1, 449);
+                    const int u = t + X::kS;
+                    uint64_t *p = &bars.p_full[x & 1];
+                    ok = u < n ? wait2(p, x / 2 & 1, q_at(u),
+                                       (c + u) / X::kQ & 1, 449)
+                               : wait(p, x / 2 & 1, 460);
                     if (!ok) break;
                     tc_fence_after();
                     if (el) {
@@ -759,8 +779,11 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                     desc_at(dGm, gs * kTile), t > 0);
                         mma_commit(&bars.g_empty[gs]);
                     }
-                    if (t + X::kS < n && !(ok = scores(t + X::kS))) break;
-                    ok = wait(&bars.ds_full, x & 1, 450);
+                    if (u < n) scores(u);
+                    ok = t + 1 < n
+                             ? wait2(&bars.ds_full, x & 1, g_at(t + 1),
+                                     (x + 1) / X::kG & 1, 450)
+                             : wait(&bars.ds_full, x & 1, 461);
                     if (!ok) break;
                     tc_fence_after();
                     if (el) {
@@ -769,13 +792,13 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         mma_commit(&bars.q_empty[qs]);
                         if (t == n - 1) mma_commit(&bars.sum_full);
                     }
-                    if (t + 1 < n) ok = products(t + 1);
+                    if (t + 1 < n) products(t + 1);
                 }
                 c += n;
                 ++ks;
             }
-        } else if (warp == 10) {
-            // ------------------------------------------------- lse and D
+        } else if (warp == kEbWeights + 3) {
+            // --------------------------------- loads of dO, of lse and D
             int c = 0;
             bool ok = true;
             for (int it = 0; ok; ++it) {
@@ -786,10 +809,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 __syncwarp();
                 if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
                 if (w.item < 0) break;
-                size_t head = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq;
-                int i0 = w.first;
+                int head = (w.b * a.H + w.kvh * a.G) * a.Nq, i0 = w.first;
                 for (int t = 0; t < w.n; ++t, ++c) {
-                    const size_t at = head + i0;
+                    const int gs = c % X::kG;
+                    const size_t at = (size_t)head + i0;
                     float l[4], d[4];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -800,6 +823,17 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                             d[q] = a.delta[at + i];
                         }
                     }
+                    if (c >= X::kG &&
+                        !(ok = warp_wait(&bars.g_empty[gs],
+                                         (c / X::kG - 1) & 1, abort, status,
+                                         443)))
+                        break;
+                    if (lane_id == 0) {
+                        mbar_expect_tx(&bars.g_full[gs], kTile);
+                        for (int p = 0; p < kPanels<D>; ++p)
+                            tma_load_2d(sG + gs * kTile + p * 16384, &tmG,
+                                        64 * p, head + i0, &bars.g_full[gs]);
+                    }
                     if (c >= 2 && !(ok = warp_wait(&bars.l_empty[c & 1],
                                                    (c / 2 - 1) & 1, abort,
                                                    status, 452)))
@@ -809,7 +843,8 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         row_l[c & 1][lane_id + 32 * q] = -l[q] * kLog2e;
                         row_d[c & 1][lane_id + 32 * q] = -d[q];
                     }
-                    mbar_arrive(&bars.l_full[c & 1]);
+                    __syncwarp();
+                    if (lane_id == 0) mbar_arrive(&bars.s_full[c & 1]);
                     i0 += 128;
                     if (i0 >= w.ql) {
                         i0 = w.first;
@@ -822,9 +857,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     } else {
         // ---------------------------------------------------------- weights
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEbRegsSoft));
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane_id;
+        const int part = warp >> 2, row = (warp & 3) * 32 + lane_id;
         const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t0 = tm + lane + 64 * half;
+        const uint32_t t0 = tm + lane + 32 * part;
         const float sl2 = a.scale * kLog2e;
         const float2 sl22 = make_float2(sl2, sl2);
         int c = 0, ks = 0;
@@ -838,12 +873,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
             if (w.item < 0) break;
             const int j = w.r0 + row;
-            const bool valid = j < w.kl;
-            const size_t at =
-                ((size_t)(w.b * a.Hkv + w.kvh) * a.Nk + j) * D + D / 2 * half;
+            const bool valid = j < w.kl, writes = part < kOutShare<D>;
+            const size_t at = ((size_t)(w.b * a.Hkv + w.kvh) * a.Nk + j) * D +
+                              kOut<D> * part;
             uint16_t *ok_ = (uint16_t *)a.dk + at, *ov = (uint16_t *)a.dv + at;
             if (w.n == 0) {
-                if (valid) {
+                if (valid && writes) {
                     store_zeros<D>(ok_);
                     store_zeros<D>(ov);
                 }
@@ -853,51 +888,46 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             const int first = !valid ? w.ql
                               : a.causal ? min(w.ql, max(0, j + w.ql - w.kl))
                                          : 0;
-            const int lo0 = first - w.first - 64 * half;
-            const int hi0 = w.ql - w.first - 64 * half;
-            int lo = lo0, hi = hi0;  // columns of this half that see the key
+            const int lo0 = first - w.first - 32 * part;
+            const int hi0 = w.ql - w.first - 32 * part;
+            int lo = lo0, hi = hi0;  // columns of this part that see the key
             for (int t = 0; t < w.n; ++t, ++c) {
-                const bool edge =
-                    __any_sync(0xffffffffu, lo > 0 || hi < 64);
-                if (!(ok = warp_wait(&bars.l_full[c & 1], c / 2 & 1, abort,
-                                     status, 454)) ||
-                    !(ok = warp_wait(&bars.s_full[c % X::kS], c / X::kS & 1,
-                                     abort, status, 455)))
+                const bool edge = __any_sync(0xffffffffu, lo > 0 || hi < 32);
+                if (!(ok = warp_wait(&bars.s_full[c & 1], c / 2 & 1, abort,
+                                     status, 455)))
                     break;
                 tc_fence_after();
                 const uint32_t tS = t0 + X::cS + 128 * (c % X::kS);
                 const float4 *nl = reinterpret_cast<const float4 *>(
-                    &row_l[c & 1][64 * half]);
+                    &row_l[c & 1][32 * part]);
                 const float4 *nd = reinterpret_cast<const float4 *>(
-                    &row_d[c & 1][64 * half]);
-                float2 p[32], g[32];
-                load64(tS, p);
+                    &row_d[c & 1][32 * part]);
+                float2 p[16], g[16];
+                load32(tS, p);
 #pragma unroll
-                for (int q = 0; q < 32; q += 2) {
+                for (int q = 0; q < 16; q += 2) {
                     const float4 l = nl[q / 2];
                     p[q] = fma2(p[q], sl22, make_float2(l.x, l.y));
                     p[q + 1] = fma2(p[q + 1], sl22, make_float2(l.z, l.w));
                 }
 #pragma unroll
-                for (int q = 0; q < 32; ++q)
+                for (int q = 0; q < 16; ++q)
                     p[q] = make_float2(ex2_approx(p[q].x), ex2_approx(p[q].y));
                 if (edge) {
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) {
+                    for (int q = 0; q < 16; ++q) {
                         if (2 * q < lo || 2 * q >= hi) p[q].x = 0.0f;
                         if (2 * q + 1 < lo || 2 * q + 1 >= hi) p[q].y = 0.0f;
                     }
                 }
-                store64(tS, p);
-                tc_fence_before();
-                mbar_arrive(&bars.p_full[c % X::kS]);
+                store32(tS, p, &bars.p_full[c & 1], lane_id);
                 if (!(ok = warp_wait(&bars.dp_full, c & 1, abort, status,
                                      456)))
                     break;
                 tc_fence_after();
-                load64(t0 + X::cP, g);
+                load32(t0 + X::cP, g);
 #pragma unroll
-                for (int q = 0; q < 32; q += 2) {
+                for (int q = 0; q < 16; q += 2) {
                     const float4 d = nd[q / 2];
                     g[q] = mul2(p[q], add2(g[q], make_float2(d.x, d.y)));
                     g[q + 1] =
@@ -905,19 +935,16 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 }
                 if (edge) {
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) {
+                    for (int q = 0; q < 16; ++q) {
                         if (2 * q < lo || 2 * q >= hi) g[q].x = 0.0f;
                         if (2 * q + 1 < lo || 2 * q + 1 >= hi) g[q].y = 0.0f;
                     }
                 }
-                store64(t0 + X::cP, g);
-                tc_fence_before();
-                mbar_arrive(&bars.ds_full);
-                __syncwarp();
+                store32(t0 + X::cP, g, &bars.ds_full, lane_id);
                 if (lane_id == 0) mbar_arrive(&bars.l_empty[c & 1]);
                 lo -= 128;
                 hi -= 128;
-                if (hi + 64 * half <= 0) {  // the next head
+                if (hi + 32 * part <= 0) {  // the next head
                     lo = lo0;
                     hi = hi0;
                 }
@@ -927,16 +954,18 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 break;
             ++ks;
             tc_fence_after();
-            const uint32_t t = tm + lane + D / 2 * half;
+            if (!writes) continue;
+            const uint32_t t = tm + lane + kOut<D> * part;
             store_sums<D>(t + X::cV, 1.0f, ov, valid);
             store_sums<D>(t + X::cK, a.scale, ok_, valid);
             tc_fence_before();
-            mbar_arrive(&bars.sum_empty);
+            __syncwarp();
+            if (lane_id == 0) mbar_arrive(&bars.sum_empty);
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) tmem_dealloc(tm, 512);
+    if (warp == kEbWeights) tmem_dealloc(tm, 512);
 }
 
 struct Maps {

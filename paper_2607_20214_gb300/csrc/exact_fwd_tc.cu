@@ -9,7 +9,7 @@
 //                   128 scores of a key tile in registers, so neither the row
 //                   maximum nor the sum needs another thread
 //   warp 8          issues every MMA: S = Q K^T, O += P V (P from TMEM)
-//   warp 9          takes the items, TMA loads of Q, K and V
+//   warp 9          takes the items, TMA loads of Q and K; warp 10 loads V
 // With few items the keys are split too: an item is then a chunk of the key
 // tiles, and k_exact_merge joins what the chunks of a row leave.
 // TMEM: S_s at 128 s, O_s at 256 + 128 s, P_s behind O_s for D <= 64, over S_s
@@ -39,14 +39,19 @@ static_assert(256 * kEfRegsSoft + 128 * kEfRegsOther <= kEfThreads * 168,
 // too. Rescaling for every new maximum: 753 us instead of 710 (B1 H16 H_kv4
 // N16384 d128 causal), since among 32 rows there is one in nearly every tile.
 constexpr float kGrown = 8.0f;
-constexpr int kEfStages = 2;  // key and value tiles held
+// Key and value tiles held.
+template <int D>
+constexpr int kEfK = D > 64 ? 3 : 4;
+template <int D>
+constexpr int kEfV = D > 64 ? 2 : 4;
 // a maximum below every score of a finite product
 constexpr float kLowest = -1e38f;
 
+template <int D>
 struct EfBars {
     uint64_t item_full[2], item_empty[2], q_full, q_empty;
-    uint64_t k_full[kEfStages], k_empty[kEfStages];
-    uint64_t v_full[kEfStages], v_empty[kEfStages];
+    uint64_t k_full[kEfK<D>], k_empty[kEfK<D>];
+    uint64_t v_full[kEfV<D>], v_empty[kEfV<D>];
     uint64_t s_full[2], p_half[2], p_full[2], o_done[2], o_empty[2];
 };
 
@@ -85,7 +90,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                    int *__restrict__ next_item) {
     wait_for_stream();
     extern __shared__ unsigned char smem_raw[];
-    __shared__ EfBars bars;
+    __shared__ EfBars<D> bars;
     __shared__ uint32_t tbase;
     __shared__ int abort_flag;
     __shared__ EfItem item_s[2];
@@ -95,7 +100,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     constexpr uint32_t kTileB = kPanels * 16384;
     const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
     const uint32_t sQ = align1k(smem_u32(smem_raw));
-    const uint32_t sK = sQ + 2 * kTileB, sV = sK + kEfStages * kTileB;
+    constexpr int kK = kEfK<D>, kV = kEfV<D>;
+    const uint32_t sK = sQ + 2 * kTileB, sV = sK + kK * kTileB;
     DeviceStatus *status = a.status;
 
     if (!next_item && blockIdx.x == 0 && tid < 4)
@@ -104,16 +110,18 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], 9);  // eight softmax warps, MMA
+            mbar_init(&bars.item_empty[s], 10);  // warps 0-8 and 10
             mbar_init(&bars.s_full[s], 1);
-            mbar_init(&bars.p_half[s], 128);
-            mbar_init(&bars.p_full[s], 128);
+            mbar_init(&bars.p_half[s], 4);
+            mbar_init(&bars.p_full[s], 4);
             mbar_init(&bars.o_done[s], 1);
-            mbar_init(&bars.o_empty[s], 128);
+            mbar_init(&bars.o_empty[s], 4);
         }
-        for (int s = 0; s < kEfStages; ++s) {
+        for (int s = 0; s < kK; ++s) {
             mbar_init(&bars.k_full[s], 1);
             mbar_init(&bars.k_empty[s], 1);
+        }
+        for (int s = 0; s < kV; ++s) {
             mbar_init(&bars.v_full[s], 1);
             mbar_init(&bars.v_empty[s], 1);
         }
@@ -130,24 +138,26 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
             kEfRegsOther));
+        // a tile of K or V
+        auto load = [&](uint64_t *full, uint64_t *empty, int c, int stages,
+                        uint32_t dst, const CUtensorMap *map, int row,
+                        int site) {
+            const int st = c % stages;
+            if (c >= stages &&
+                !mbar_wait_or_abort(&empty[st], (c / stages - 1) & 1, abort,
+                                    status, site))
+                return false;
+            mbar_expect_tx(&full[st], kTileB);
+            for (int p = 0; p < kPanels; ++p)
+                tma_load_2d(dst + st * kTileB + p * 16384, map, 64 * p, row,
+                            &full[st]);
+            return true;
+        };
         if (warp == 9 && lane_id == 0) {
-            // ---------------------------------------------- items and loads
+            // ------------------------------------ items, loads of Q and K
             int c = 0;   // key tiles loaded so far
             int qs = 0;  // items whose queries were loaded
             bool ok = true;
-            auto load = [&](uint64_t *full, uint64_t *empty, uint32_t dst,
-                            const CUtensorMap *map, int row, int site) {
-                const int st = c % kEfStages;
-                if (c >= kEfStages &&
-                    !mbar_wait_or_abort(&empty[st], (c / kEfStages - 1) & 1,
-                                        abort, status, site))
-                    return false;
-                mbar_expect_tx(&full[st], kTileB);
-                for (int p = 0; p < kPanels; ++p)
-                    tma_load_2d(dst + st * kTileB + p * 16384, map, 64 * p,
-                                row, &full[st]);
-                return true;
-            };
             const int heads = a.B * a.Hkv, rows = order.rows;
             for (int it = 0; ok; ++it) {
                 long item = blockIdx.x;
@@ -203,10 +213,26 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                                     q0 + order.row(w.r0 + 128 * s, a.Nq),
                                     &bars.q_full);
                 for (int kt = 0; kt < nk && ok; ++kt, ++c)
-                    ok = load(bars.k_full, bars.k_empty, sK, &tmK,
-                              k0 + 128 * kt, 402) &&
-                         load(bars.v_full, bars.v_empty, sV, &tmV,
-                              k0 + 128 * kt, 403);
+                    ok = load(bars.k_full, bars.k_empty, c, kK, sK, &tmK,
+                              k0 + 128 * kt, 402);
+            }
+        } else if (warp == 10 && lane_id == 0) {
+            // ------------------------------------------------ loads of V
+            int c = 0;
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!mbar_wait_or_abort(&bars.item_full[it & 1], (it >> 1) & 1,
+                                        abort, status, 403))
+                    break;
+                const EfItem w = item_s[it & 1];
+                mbar_arrive(&bars.item_empty[it & 1]);
+                if (w.item < 0) break;
+                const int nk = max(w.n[0], w.n[1]);
+                const int k0 =
+                    (w.b * a.Hkv + w.kvh) * a.Nk + 128 * w.kt0;
+                for (int kt = 0; kt < nk && ok; ++kt, ++c)
+                    ok = load(bars.v_full, bars.v_empty, c, kV, sV, &tmV,
+                              k0 + 128 * kt, 411);
             }
         } else if (warp == 8) {
             // ---------------------------------------------------- MMA issue
@@ -258,8 +284,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 auto scores = [&](auto slot, int &us, int n, int us_o,
                                   int n_o) {
                     constexpr int s = decltype(slot)::value;
-                    const int st = (c0 + us) % kEfStages;
-                    if (!wait(&bars.k_full[st], (c0 + us) / kEfStages & 1,
+                    const int st = (c0 + us) % kK;
+                    if (!wait(&bars.k_full[st], (c0 + us) / kK & 1,
                               406))
                         return false;
                     tc_fence_after();
@@ -286,16 +312,17 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     constexpr int s = decltype(slot)::value;
                     constexpr uint32_t cO = 128u * s + 256u;
                     constexpr uint32_t cP = D <= 64 ? cO + 64 : 128u * s;
-                    const int st = (c0 + up) % kEfStages;
+                    const int st = (c0 + up) % kV;
                     if (up == us) return false;
                     const uint64_t v = dV + st * kTile;
                     if (!half) {
-                        if (!test(&bars.p_half[s], gp & 1) ||
-                            !test(&bars.v_full[st],
-                                  (c0 + up) / kEfStages & 1) ||
-                            (up == 0 && go > 0 &&
-                             !test(&bars.o_empty[s], (go - 1) & 1)))
-                            return false;
+                        // the tests side by side, then one vote
+                        const bool ready =
+                            mbar_test(&bars.p_half[s], gp & 1) &
+                            mbar_test(&bars.v_full[st], (c0 + up) / kV & 1) &
+                            (up > 0 || go == 0 ||
+                             mbar_test(&bars.o_empty[s], (go - 1) & 1));
+                        if (!__all_sync(0xffffffffu, ready)) return false;
                         if (up == nk - 1 && part < 128) {
                             const uint32_t x = sV + st * kTileB;
                             for (int i = part * 8 + lane_id; i < 1024;
@@ -377,6 +404,13 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             return __all_sync(0xffffffffu,
                               mbar_wait_or_abort(bar, par, abort, status,
                                                  site));
+        };
+        // what the warp did in tensor memory comes before the products that
+        // wait for the barrier
+        auto warp_done = [=](uint64_t *bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane_id == 0) mbar_arrive(bar);
         };
         int g = 0;  // key tiles of this slot so far
         bool ok = true;
@@ -481,14 +515,12 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     tmem_st16(tP + c / 2, pw);
                     if (c == 32) {
                         tmem_wait_st();
-                        tc_fence_before();
-                        mbar_arrive(&bars.p_half[s]);
+                        warp_done(&bars.p_half[s]);
                     }
                 }
                 lsum += (ls[0].x + ls[1].x) + (ls[0].y + ls[1].y);
                 tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(&bars.p_full[s]);
+                warp_done(&bars.p_full[s]);
             }
             if (!ok) break;
             const size_t at =
@@ -510,8 +542,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     tmem_ld32(tO + c, x);
                     tmem_wait_ld();
                     if (c + 32 == D) {
-                        tc_fence_before();
-                        mbar_arrive(&bars.o_empty[s]);
+                        warp_done(&bars.o_empty[s]);
                     }
                     if (!valid) continue;
 #pragma unroll
@@ -535,8 +566,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     tmem_ld32(tO + c, x);
                     tmem_wait_ld();
                     if (c + 32 == D) {
-                        tc_fence_before();
-                        mbar_arrive(&bars.o_empty[s]);
+                        warp_done(&bars.o_empty[s]);
                     }
                 } else {
 #pragma unroll
@@ -660,7 +690,7 @@ cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
     auto launch = [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         const size_t smem =
-            1024 + (size_t)(2 + 2 * kEfStages) * (D > 64 ? 2 : 1) * 16384;
+            1024 + (size_t)(2 + kEfK<D> + kEfV<D>) * (D > 64 ? 2 : 1) * 16384;
         cudaError_t r = launch_after(
             k_exact_fwd_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
             kEfThreads, smem, st, tmQ, tmK, tmV, a, split, order,
