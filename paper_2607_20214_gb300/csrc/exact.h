@@ -77,16 +77,16 @@ __device__ __forceinline__ int exact_most(const ExactSeq &s, int r0, int r1,
                                           int N) {
     if (r0 >= r1 || s.ql == 0) return 0;
     const int i0 = r0 % N, i1 = (r1 - 1) % N;
-    // the last rows of a head are among them
-    if (r0 / N != (r1 - 1) / N)
-        return i0 < s.ql ? s.seen(s.ql - 1) : s.seen(min(i1, s.ql - 1));
-    return i0 < s.ql ? s.seen(min(i1, s.ql - 1)) : 0;
+    const int heads = (r1 - 1) / N - r0 / N;
+    // the last row of a head is among them
+    if (heads > 1 || (heads == 1 && i0 < s.ql)) return s.seen(s.ql - 1);
+    return heads == 1 || i0 < s.ql ? s.seen(min(i1, s.ql - 1)) : 0;
 }
 #endif
 
 // bf16 on the tensor cores; next_item: an int of scratch; part:
-// exact_split_bytes(a) of it, 256-byte aligned
-size_t exact_split_bytes(const ExactView &a);
+// exact_share_bytes(a) of it, 256-byte aligned
+size_t exact_share_bytes(const ExactView &a);
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
                                 float *part, cudaStream_t st);
 // Its backward pass: D_i first (which also clears the status and two work

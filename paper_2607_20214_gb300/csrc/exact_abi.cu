@@ -68,7 +68,7 @@ bool on_tensor_cores(const elsaa_exact *p) {
     return p->dtype == ELSAA_BF16 && p->impl == ELSAA_IMPL_AUTO;
 }
 
-// status and two work counters | D_i, or what the chunks of split keys leave
+// status and two work counters | D_i, or what CTAs leave of divided rows
 struct Layout {
     size_t next_item, scratch, total;
 };
@@ -76,7 +76,7 @@ Layout layout(const ExactView &a, bool tensor, bool backward) {
     Layout l;
     l.next_item = sizeof(DeviceStatus);
     l.scratch = align256(l.next_item + 2 * sizeof(int));
-    size_t most = tensor ? exact_split_bytes(a) : 0;
+    size_t most = tensor ? exact_share_bytes(a) : 0;
     const size_t delta = sizeof(float) * (size_t)a.B * a.H * a.Nq;
     if (backward && delta > most) most = delta;
     l.total = l.scratch + align256(most);

@@ -10,8 +10,8 @@
 //                   maximum nor the sum needs another thread
 //   warp 8          issues every MMA: S = Q K^T, O += P V (P from TMEM)
 //   warp 9          takes the items, TMA loads of Q and K; warp 10 loads V
-// With few items the keys are split too: an item is then a chunk of the key
-// tiles, and k_exact_merge joins what the chunks of a row leave.
+// With few items every CTA gets an equal share of all key tiles instead, in
+// order, and k_exact_merge joins what the CTAs of a divided item leave.
 // TMEM: S_s at 128 s, O_s at 256 + 128 s, P_s behind O_s for D <= 64, over S_s
 // at D = 128. O stays in tensor memory; a softmax warp rescales it when the
 // maximum of one of its rows has grown much.
@@ -62,21 +62,40 @@ struct EfItem {
     int ql, kl;
     int kt0;    // the first key tile
     int n[2];   // key tiles of each slot, from kt0 on
-    int parts[2];  // chunks that each slot's rows are split into
-    int sp;     // which of them this is
+    int part;   // where a divided item's sums go, -1: the item is whole
 };
 
-// How the keys are split: `splits` chunks at most, of `chunk` tiles. What a
-// chunk leaves of row r (over all heads): the sums of e^(z - m) v in
-// o[sp][r][D], and (m, sum of e^(z - m)) in ml[sp][r], z and m base 2.
-struct EfSplit {
-    int splits, chunk;
+// Shares. The items of a K/V head in their order, of all heads of a sequence,
+// of all sequences make one row of units: kEfHead for an item (what it costs
+// beside its tiles) and one for each of its key tiles (of 256 rows). CTA c of C
+// takes units [W c / C, W (c + 1) / C) of the W. Of an item that is divided,
+// every CTA leaves 256 rows of sums of e^(z - m) v in o[part][row][D] and
+// (m, sum of e^(z - m)) in ml[part][row], z and m base 2: part 2 c + 1 of the
+// CTA that begins it, part 2 c of the others. rec[c] tells k_exact_merge of
+// the item that CTA c begins.
+constexpr int kEfHead = 2;
+constexpr int kEfLeast = 6;     // units of a share at least, on average
+constexpr int kEfCtas = 152;    // one for each SM of a GB300
+constexpr int kEfMaxB = 256;
+struct EfRecord {
+    int b, kvh, r0, last;  // last: the CTA that ends it, -1: none
+};
+struct EfShares {
+    int on, tiles;  // tiles: items of a K/V head
     float *o;
     float2 *ml;
-    size_t rows;
+    EfRecord *rec;
 };
-__device__ __forceinline__ int chunks_of(const EfSplit &p, int tiles) {
-    return (tiles + p.chunk - 1) / p.chunk;
+
+// Units of item t of sequence `seq`, none if it has no row.
+__device__ __forceinline__ int ef_weight(const ExactSeq &seq,
+                                         const ExactOrder &order, int t) {
+    const int r0 = order.tile(t) * 256, r1 = min(r0 + 256, order.rows);
+    if (r0 >= r1 || seq.ql == 0) return 0;
+    if (r0 / order.pitch == (r1 - 1) / order.pitch &&
+        r0 % order.pitch >= seq.ql)
+        return 0;
+    return kEfHead + (exact_most(seq, r0, r1, order.pitch) + 127) / 128;
 }
 
 template <int D>
@@ -85,7 +104,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                    const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV,
                    const __grid_constant__ ExactView a,
-                   const __grid_constant__ EfSplit split,
+                   const __grid_constant__ EfShares shares,
                    const __grid_constant__ ExactOrder order, int items,
                    int *__restrict__ next_item) {
     wait_for_stream();
@@ -104,8 +123,35 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     const uint32_t sK = sQ + 2 * kTileB, sV = sK + kK * kTileB;
     DeviceStatus *status = a.status;
 
+    // units of all heads of the sequences up to b
+    __shared__ int upto[kEfMaxB];
     if (!next_item && blockIdx.x == 0 && tid < 4)
         (&status->code)[tid] = 0;  // a wait runs out much later
+    if (shares.on) {
+        for (int b = tid; b < a.B; b += kEfThreads) upto[b] = 0;
+        __syncthreads();
+        for (int i = tid; i < a.B * shares.tiles; i += kEfThreads) {
+            const int b = i / shares.tiles;
+            const int w =
+                ef_weight(ExactSeq(a, b), order, i - b * shares.tiles);
+            if (w) atomicAdd(&upto[b], w * a.Hkv);
+        }
+        __syncthreads();
+        if (warp == 0) {
+            int sum = 0;
+            for (int b = lane_id; b - lane_id < a.B; b += 32) {
+                int x = b < a.B ? upto[b] : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, x, o);
+                    if (lane_id >= o) x += y;
+                }
+                x += sum;
+                if (b < a.B) upto[b] = x;
+                sum = __shfl_sync(0xffffffffu, x, 31);
+            }
+        }
+    }
     if (warp == 8) tmem_alloc(&tbase, 512);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
@@ -153,46 +199,136 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                             &full[st]);
             return true;
         };
+        // of warp 9: where its share begins and how long it is
+        int sb = 0, skvh = 0, st = 0, at = 0, rest = 0;
+        long W = 0;
+        int C = 1;
+        if (shares.on && warp == 9) {
+            W = upto[a.B - 1];
+            C = (int)min((long)gridDim.x, max(1L, W / kEfLeast));
+            if (blockIdx.x < C) {
+                int u = (int)(W * blockIdx.x / C);
+                rest = (int)(W * (blockIdx.x + 1) / C) - u;
+                while (sb < a.B - 1 && upto[sb] <= u) ++sb;
+                if (sb > 0) u -= upto[sb - 1];
+                const int head =
+                    max(1, (upto[sb] - (sb > 0 ? upto[sb - 1] : 0)) / a.Hkv);
+                skvh = u / head;
+                u -= skvh * head;
+                const ExactSeq seq(a, sb);
+                for (;; st += 32) {
+                    int x = st + lane_id < shares.tiles
+                                ? ef_weight(seq, order, st + lane_id)
+                                : 0;
+                    const int own = x;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int y = __shfl_up_sync(0xffffffffu, x, o);
+                        if (lane_id >= o) x += y;
+                    }
+                    const uint32_t past =
+                        __ballot_sync(0xffffffffu, x > u);
+                    if (past || st + 32 >= shares.tiles) {
+                        const int k = past ? __ffs(past) - 1 : 31;
+                        at = u - __shfl_sync(0xffffffffu, x - own, k);
+                        st += k;
+                        break;
+                    }
+                    u -= __shfl_sync(0xffffffffu, x, 31);
+                }
+            }
+        }
         if (warp == 9 && lane_id == 0) {
             // ------------------------------------ items, loads of Q and K
             int c = 0;   // key tiles loaded so far
             int qs = 0;  // items whose queries were loaded
             bool ok = true;
             const int heads = a.B * a.Hkv, rows = order.rows;
+            EfRecord rec = {0, 0, 0, -1};
+            long unit = W * blockIdx.x / C;
+            // the next item, of key tiles [kt0, kt1)
+            auto fill = [&](EfItem &w, int b, int kvh, int t, int kt0,
+                            int kt1) {
+                w.item = 0;
+                w.b = b;
+                w.kvh = kvh;
+                w.r0 = order.tile(t) * 256;
+                w.kt0 = kt0;
+                w.part = -1;
+                const ExactSeq seq(a, b);
+                w.ql = seq.ql;
+                w.kl = seq.kl;
+                for (int s = 0; s < 2; ++s) {
+                    const int r = w.r0 + 128 * s;
+                    const int n = (exact_most(seq, r, min(r + 128, rows),
+                                              order.pitch) + 127) / 128;
+                    w.n[s] = max(0, min(n, kt1) - kt0);
+                }
+            };
+            auto next_share = [&](EfItem &w) {
+                while (rest > 0) {
+                    const int t = st, b = sb, kvh = skvh, a0 = at;
+                    const int all = ef_weight(ExactSeq(a, b), order, t);
+                    const int a1 = min(all, a0 + rest);
+                    const long begin = unit - a0;  // of the item
+                    rest -= a1 - a0;
+                    unit += a1 - a0;
+                    at = 0;
+                    if (++st == shares.tiles) {
+                        st = 0;
+                        if (++skvh == a.Hkv) {
+                            skvh = 0;
+                            // the next sequence that has rows (the last
+                            // one's end is that of the last share)
+                            while (sb < a.B - 1 && upto[++sb] == upto[sb - 1])
+                                ;
+                        }
+                    }
+                    if (all == 0) continue;
+                    const int kt0 = max(a0 - kEfHead, 0);
+                    const int kt1 = max(a1 - kEfHead, 0);
+                    // nothing of it but its head, unless it has no more
+                    if (kt0 == kt1 && (all > kEfHead || a0 > 0)) continue;
+                    fill(w, b, kvh, t, kt0, kt1);
+                    if (all > kEfHead) {
+                        const int first =
+                            (int)range_owner(begin + kEfHead, W, C);
+                        const int last =
+                            (int)range_owner(begin + all - 1, W, C);
+                        if (first != last) {
+                            w.part = 2 * (int)blockIdx.x;
+                            if (first == (int)blockIdx.x) {
+                                ++w.part;
+                                rec = {b, kvh, w.r0, last};
+                            }
+                        }
+                    }
+                    return true;
+                }
+                return false;
+            };
             for (int it = 0; ok; ++it) {
-                long item = blockIdx.x;
-                if (it > 0)
-                    item = next_item
-                               ? (long)gridDim.x + atomicAdd(next_item, 1)
-                               : items;
+                EfItem w = {-1};
+                if (shares.on) {
+                    if (!next_share(w)) w.item = -1;
+                } else {
+                    long item = blockIdx.x;
+                    if (it > 0)
+                        item = next_item ? (long)gridDim.x +
+                                               atomicAdd(next_item, 1)
+                                         : items;
+                    if (item < items) {
+                        // the last rows of every query head, which see most,
+                        // first
+                        const int h = (int)(item % heads);
+                        fill(w, h / a.Hkv, h % a.Hkv, (int)(item / heads), 0,
+                             1 << 30);
+                    }
+                }
                 if (it >= 2 && !mbar_wait_or_abort(&bars.item_empty[it & 1],
                                                    ((it >> 1) - 1) & 1, abort,
                                                    status, 400))
                     break;
-                EfItem w = {-1};
-                if (item < items) {
-                    // the last rows of every query head, which see most,
-                    // first
-                    const int h = (int)(item % heads);
-                    const int t = (int)(item / heads);
-                    w.item = (int)item;
-                    w.sp = t % split.splits;
-                    w.kt0 = w.sp * split.chunk;
-                    w.r0 = order.tile(t / split.splits) * 256;
-                    w.b = h / a.Hkv;
-                    w.kvh = h - w.b * a.Hkv;
-                    const ExactSeq seq(a, w.b);
-                    w.ql = seq.ql;
-                    w.kl = seq.kl;
-                    for (int s = 0; s < 2; ++s) {
-                        const int r = w.r0 + 128 * s;
-                        const int n =
-                            (exact_most(seq, r, min(r + 128, rows),
-                                        order.pitch) + 127) / 128;
-                        w.parts[s] = chunks_of(split, n);
-                        w.n[s] = max(0, min(n - w.kt0, split.chunk));
-                    }
-                }
                 item_s[it & 1] = w;
                 mbar_arrive(&bars.item_full[it & 1]);
                 if (w.item < 0) break;
@@ -216,6 +352,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     ok = load(bars.k_full, bars.k_empty, c, kK, sK, &tmK,
                               k0 + 128 * kt, 402);
             }
+            if (shares.on) shares.rec[blockIdx.x] = rec;
         } else if (warp == 10 && lane_id == 0) {
             // ------------------------------------------------ loads of V
             int c = 0;
@@ -418,8 +555,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             ok = wwait(&bars.item_full[it & 1], (it >> 1) & 1, 408);
             if (!ok) break;
             const EfItem &w_s = item_s[it & 1];
-            const int item = w_s.item, n = w_s.n[s], parts = w_s.parts[s];
-            const int sp = w_s.sp, kt0 = w_s.kt0, wb = w_s.b, kvh = w_s.kvh;
+            const int item = w_s.item, n = w_s.n[s], part = w_s.part;
+            const int kt0 = w_s.kt0, wb = w_s.b, kvh = w_s.kvh;
             const int ql = w_s.ql, kl = w_s.kl, slot0 = w_s.r0 + 128 * s;
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
@@ -532,18 +669,14 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 if (!ok) break;
                 tc_fence_after();
             }
-            if (parts > 1) {
-                if (n == 0) continue;
-                const size_t to = sp * split.rows + at;
-                float *y = split.o + to * D;
-#pragma unroll
-                for (int c = 0; c < D; c += 32) {
+            if (part >= 0) {
+                const size_t to = (size_t)part * 256 + 128 * s + row;
+                float *y = shares.o + to * D;
+                for (int c = 0; c < D && n > 0; c += 32) {
                     uint32_t x[32];
                     tmem_ld32(tO + c, x);
                     tmem_wait_ld();
-                    if (c + 32 == D) {
-                        warp_done(&bars.o_empty[s]);
-                    }
+                    if (c + 32 == D) warp_done(&bars.o_empty[s]);
                     if (!valid) continue;
 #pragma unroll
                     for (int q = 0; q < 32; q += 8) {
@@ -553,10 +686,9 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                         st_global_v8(y + c + q, e);
                     }
                 }
-                if (valid) split.ml[to] = make_float2(mref, lsum);
+                if (valid) shares.ml[to] = make_float2(mref, lsum);
                 continue;
             }
-            if (sp > 0) continue;
             // a row that sees nothing, or only scores of -inf: zeros
             const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
 #pragma unroll
@@ -597,94 +729,99 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     if (warp == 8) tmem_dealloc(tm, 512);
 }
 
-// Joins the chunks of the rows that have more than one: D / 8 lanes a row.
+// Joins the parts of divided items: blockIdx.y is the CTA that begins one,
+// D / 8 lanes a row.
 template <int D>
 __global__ void __launch_bounds__(256)
     k_exact_merge(const __grid_constant__ ExactView a,
-                  const __grid_constant__ EfSplit split,
+                  const __grid_constant__ EfShares shares,
                   const __grid_constant__ ExactOrder order) {
     wait_for_stream();
     constexpr int L = D / 8;
-    const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) / L;
-    const int c = threadIdx.x % L * 8;
-    if (row >= split.rows) return;
-    const int group = a.G * a.Nq;  // rows of a K/V head's queries
-    const int x = (int)(row % group), i = x % a.Nq;
-    const ExactSeq seq(a, (int)(row / group) / a.Hkv);
-    if (i >= seq.ql) return;
-    // the slot that had the row
-    const int r0 = (x / a.Nq * order.pitch + i) / 128 * 128;
-    const int n = (exact_most(seq, r0, min(r0 + 128, order.rows),
-                              order.pitch) + 127) / 128;
-    const int parts = chunks_of(split, n);
-    if (parts < 2) return;
+    const int first = blockIdx.y;
+    const EfRecord rec = shares.rec[first];
+    if (rec.last < 0) return;
+    const int row = (blockIdx.x * 256 + threadIdx.x) / L;
+    const int c = threadIdx.x % L * 8, r = rec.r0 + row;
+    if (r >= order.rows ||
+        r % order.pitch >= ExactSeq(a, rec.b).ql)
+        return;
+    auto at = [&](int cta) {
+        return (size_t)(2 * cta + (cta == first)) * 256 + row;
+    };
     float m = kLowest;
-    for (int p = 0; p < parts; ++p)
-        m = fmaxf(m, split.ml[p * split.rows + row].x);
+    for (int p = first; p <= rec.last; ++p)
+        m = fmaxf(m, shares.ml[at(p)].x);
     float l = 0.0f, o[8] = {};
-    for (int p = 0; p < parts; ++p) {
-        const float2 ml = split.ml[p * split.rows + row];
+    for (int p = first; p <= rec.last; ++p) {
+        const float2 ml = shares.ml[at(p)];
+        if (ml.y == 0.0f) continue;  // its sums may not have been written
         const float f = ex2_approx(ml.x - m);
         l = fmaf(ml.y, f, l);
-        const float4 *x = reinterpret_cast<const float4 *>(
-            split.o + (p * split.rows + row) * D + c);
+        const float4 *x =
+            reinterpret_cast<const float4 *>(shares.o + at(p) * D + c);
         const float4 u = x[0], v = x[1];
         const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = fmaf(e[i], f, o[i]);
     }
+    const size_t to = (size_t)(rec.b * a.H + rec.kvh * a.G) * a.Nq +
+                      order.row(r, a.Nq);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     uint32_t y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         y[i] = pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
-    *reinterpret_cast<uint4 *>((uint16_t *)a.out + row * D + c) =
+    *reinterpret_cast<uint4 *>((uint16_t *)a.out + to * D + c) =
         make_uint4(y[0], y[1], y[2], y[3]);
     if (a.lse && c == 0)
-        a.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+        a.lse[to] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Chunks of the keys, so that there are four items for each of a GB300's 152
-// SMs, and 4 tiles (512 keys) at least in a chunk. (Fixed, so that the
-// workspace does not depend on the device.)
-void divide_keys(const ExactView &a, int *splits, int *chunk) {
-    const long items = ExactOrder(a, 256).items(a);
-    const int tiles = (a.Nk + 127) / 128;
-    long n = (4 * 152 + items - 1) / items;
-    if (n > tiles / 4) n = tiles / 4;
-    if (n < 1) n = 1;
-    *chunk = (int)((tiles + n - 1) / n);
-    *splits = (tiles + *chunk - 1) / *chunk;
+// Shares instead of whole items: with fewer than four items for each SM, the
+// longest would run alone at the end. Not for short keys, where dividing costs
+// more. (Decided by the sizes alone, so that the workspace does not depend on
+// the device.)
+bool use_shares(const ExactView &a) {
+    const ExactOrder order(a, 256);
+    const long tiles = ((long)a.Nk + 127) / 128;
+    return order.items(a) < 4 * kEfCtas && tiles >= 8 && tiles <= 1 << 20 &&
+           a.B <= kEfMaxB;
 }
 
 }  // namespace
 
-size_t exact_split_bytes(const ExactView &a) {
-    int splits, chunk;
-    divide_keys(a, &splits, &chunk);
-    if (splits == 1) return 0;
-    return sizeof(float) * (a.d + 2) * (size_t)splits * a.B * a.H * a.Nq;
+size_t exact_share_bytes(const ExactView &a) {
+    if (!use_shares(a)) return 0;
+    return sizeof(EfRecord) * kEfCtas +
+           (size_t)2 * kEfCtas * 256 * sizeof(float) * (a.d + 2);
 }
 
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
                                 float *part, cudaStream_t st) {
-    EfSplit split = {};
-    divide_keys(a, &split.splits, &split.chunk);
-    split.rows = (size_t)a.B * a.H * a.Nq;
-    split.o = part;
-    split.ml = (float2 *)(part + split.rows * split.splits * a.d);
     const ExactOrder order(a, 256);
-    const long items = order.items(a) * split.splits;
+    const long items = order.items(a);
+    EfShares shares = {};
+    shares.on = use_shares(a);
+    shares.tiles = order.groups * order.per;
+    const size_t rows = (size_t)2 * kEfCtas * 256;
+    shares.o = part;
+    shares.ml = (float2 *)(part + rows * a.d);
+    shares.rec = (EfRecord *)(shares.ml + rows);
     int dev = 0, sms = 152;
     if (cudaGetDevice(&dev) == cudaSuccess)
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const int ctas = shares.on ? (sms < kEfCtas ? sms : kEfCtas)
+                               : (int)(items < sms ? items : sms);
+    // more items than CTAs: they are taken from a counter
+    const bool counted = !shares.on && items > sms;
     CUtensorMap tmQ, tmK, tmV;
+    const uint64_t nq = (uint64_t)a.B * a.H * a.Nq;
     const uint64_t nk = (uint64_t)a.B * a.Hkv * a.Nk;
-    cudaError_t e = make_tma_map_bf16(&tmQ, a.q, split.rows, a.d, 128);
+    cudaError_t e = make_tma_map_bf16(&tmQ, a.q, nq, a.d, 128);
     if (e == cudaSuccess) e = make_tma_map_bf16(&tmK, a.k, nk, a.d, 128);
     if (e == cudaSuccess) e = make_tma_map_bf16(&tmV, a.v, nk, a.d, 128);
-    // more items than CTAs: they are taken from a counter
-    if (e == cudaSuccess && items > sms)
+    if (e == cudaSuccess && counted)
         e = launch_clear(a.status, next_item, 1, st);
     if (e != cudaSuccess) return e;
     auto launch = [&](auto dim) {
@@ -692,14 +829,13 @@ cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
         const size_t smem =
             1024 + (size_t)(2 + kEfK<D> + kEfV<D>) * (D > 64 ? 2 : 1) * 16384;
         cudaError_t r = launch_after(
-            k_exact_fwd_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
-            kEfThreads, smem, st, tmQ, tmK, tmV, a, split, order,
-            (int)items, items > sms ? next_item : nullptr);
-        if (r == cudaSuccess && split.splits > 1)
-            r = launch_after(
-                k_exact_merge<D>,
-                dim3((unsigned)((split.rows * (D / 8) + 255) / 256)), 256, 0,
-                st, a, split, order);
+            k_exact_fwd_tc<D>, dim3((unsigned)ctas), kEfThreads, smem, st,
+            tmQ, tmK, tmV, a, shares, order, (int)items,
+            counted ? next_item : nullptr);
+        if (r == cudaSuccess && shares.on)
+            r = launch_after(k_exact_merge<D>,
+                             dim3(256 * (D / 8) / 256, (unsigned)ctas), 256, 0,
+                             st, a, shares, order);
         return r;
     };
     return a.d == 128  ? launch(std::integral_constant<int, 128>{})

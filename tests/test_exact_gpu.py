@@ -323,3 +323,26 @@ def test_many_short_sequences():
     """More items than a grid's first CTAs, single tokens of grouped heads."""
     run_case(200, 8, 2, 1, 40, 64, BF, 1, backward=False)
     run_case(100, 4, 2, 3, 5, 32, BF, 1)
+
+
+@pytest.mark.parametrize("dtype,impl", KINDS)
+@pytest.mark.parametrize("causal", [0, 1])
+def test_padded_groups_of_few_rows(causal, dtype, impl):
+    """Tiles that hold several heads with padding between them."""
+    run_case(5, 12, 2, 5, 70, 64, dtype, causal, ql=[3, 5, 0, 1, 4],
+             kl=[70, 2, 9, 69, 0], impl=impl)
+    run_case(2, 9, 3, 50, 300, 64, dtype, causal, ql=[20, 50], kl=[300, 41],
+             impl=impl)
+
+
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,kl", [
+    (1, 1, 1, 1, 9000, [9000]), (4, 4, 4, 3, 4000, [4000, 0, 1, 2600]),
+    (7, 2, 1, 300, 1100, [1100, 0, 0, 700, 3, 0, 0]),
+    (256, 1, 1, 2, 1030, [1030 - 4 * i for i in range(256)]),
+    (257, 1, 1, 2, 1030, [1030 - 4 * i for i in range(257)])])
+def test_shares(B, H, Hkv, Nq, Nk, kl):
+    """Rows divided among CTAs: few rows of many keys, sequences without any,
+    as many sequences as a share can be of."""
+    run_case(B, H, Hkv, Nq, Nk, 64, BF, 1, ql=[Nq] * B, kl=kl, backward=False)
+    run_case(B, H, Hkv, Nq, Nk, 64, BF, 0, ql=[(i % 2) * Nq for i in range(B)],
+             kl=kl, backward=False)
