@@ -20,20 +20,32 @@ namespace {
 
 using namespace tc;
 
-// 16 warps make weights, four threads a row with 32 columns each; four others
-// issue and load. (With 8 warps, two threads a row, each iteration's waits,
-// loads and exponentials stood one behind the other.)
-constexpr int kEbWeights = 16;
-constexpr int kEbThreads = 32 * (kEbWeights + 4);
-// 640 x 96 registers at launch = 512 x 104 (weights) + 128 x 64
-constexpr int kEbRegsSoft = 104, kEbRegsOther = 64;
-static_assert(512 * kEbRegsSoft + 128 * kEbRegsOther <= kEbThreads * 96,
-              "register shares within the launch's total");
-
+// What a CTA of either kernel is made of, by the head's size. It holds 128 rows
+// and walks tiles of `rows` others; weights are made by threads of 32 columns,
+// rows / 32 of them a held row; four more warps issue and load.
+//   D = 128: tiles of 128, 16 warps for the weights, one CTA an SM (it needs
+//            all of its tensor memory).
+//   D <= 64: tiles of 64, 8 warps, two CTAs an SM. A tile's waits, loads,
+//            exponentials and stores stand one behind the other; two CTAs fill
+//            each other's gaps.
 template <int D>
-constexpr int kPanels = D > 64 ? 2 : 1;
-template <int D>
-constexpr uint32_t kTileBytes = kPanels<D> * 16384;  // 128 rows
+struct Eb {
+    static constexpr int rows = D > 64 ? 128 : 64;
+    static constexpr int parts = rows / 32;
+    static constexpr int weights = 4 * parts;  // warps
+    static constexpr int threads = 32 * (weights + 4);
+    static constexpr int ctas = D > 64 ? 1 : 2;
+    static constexpr int columns = D > 64 ? 512 : 256;  // of tensor memory
+    static constexpr int out = D / parts;  // columns of sums a thread writes
+    // registers: at launch, of the weights' threads, of the others
+    static constexpr int regs = D > 64 ? 96 : 80;
+    static constexpr int soft = D > 64 ? 104 : 88, other = 64;
+    static_assert(32 * weights * soft + 128 * other <= threads * regs,
+                  "register shares within the launch's total");
+    static constexpr int panels = D > 64 ? 2 : 1;
+    static constexpr uint32_t held = panels * 16384;       // bytes of 128 rows
+    static constexpr uint32_t tile = panels * rows * 128;  // of a tile
+};
 
 // A test of a barrier takes about 54 clocks, a try_wait 90.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t par,
@@ -79,13 +91,13 @@ __device__ __forceinline__ void store32(uint32_t t, const float2 (&x)[16],
     if (lane_id == 0) mbar_arrive(bar);
 }
 
-// One operand's product of K = D (both K-major) and of K = 128 (A from tensor
-// memory: 16 columns of every 32, as the four quarters' threads write them; B
+// A product of K = D (both K-major) and one of K = rows (A from tensor
+// memory: 16 columns of every 32, as threads of 32 columns write them; B
 // MN-major), issued by one lane.
 template <int D>
 __device__ __forceinline__ void mma_scores(uint32_t dst, uint64_t a,
                                            uint64_t b) {
-    const uint32_t id = idesc_bf16(128, 128, false, false);
+    const uint32_t id = idesc_bf16(128, Eb<D>::rows, false, false);
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
         const uint32_t o = (x >> 2) * 1024 + (x & 3) * 2;
@@ -97,34 +109,29 @@ __device__ __forceinline__ void mma_sums(uint32_t dst, uint32_t a, uint64_t b,
                                          bool more) {
     const uint32_t id = idesc_bf16(128, D, false, true);
 #pragma unroll
-    for (int x = 0; x < 8; ++x)
+    for (int x = 0; x < Eb<D>::rows / 16; ++x)
         mma_ts(dst, a + (x >> 1) * 32 + (x & 1) * 8, b + 128 * x, id,
                x > 0 || more);
 }
 
-// Rows [part, 128) of a tile in shared memory become zeros (all lanes).
+// The rows of a tile in shared memory from `part` on become zeros (all lanes).
 template <int D>
 __device__ __forceinline__ void zero_rows(uint32_t tile, int part,
                                           int lane_id) {
-    for (int i = max(part, 0) * 8 + lane_id; i < 1024; i += 32)
-        for (int p = 0; p < kPanels<D>; ++p)
-            st_shared_zero16(tile + p * 16384 + i * 16);
+    using E = Eb<D>;
+    for (int i = max(part, 0) * 8 + lane_id; i < E::rows * 8; i += 32)
+        for (int p = 0; p < E::panels; ++p)
+            st_shared_zero16(tile + p * E::rows * 128 + i * 16);
     fence_proxy_async_smem();
     __syncwarp();
 }
 
-// The columns of sums that a thread writes, and how many threads share a row.
-template <int D>
-constexpr int kOut = D > 64 ? 32 : 16;
-template <int D>
-constexpr int kOutShare = D / kOut<D>;
-
-// kOut columns of sums in tensor memory, times f, to a row of bf16.
+// A thread's columns of sums in tensor memory, times f, to a row of bf16.
 template <int D>
 __device__ __forceinline__ void store_sums(uint32_t t, float f, uint16_t *o,
                                            bool valid) {
 #pragma unroll
-    for (int c = 0; c < kOut<D>; c += 16) {
+    for (int c = 0; c < Eb<D>::out; c += 16) {
         uint32_t x[16], y[8];
         tmem_ld16(t + c, x);
         tmem_wait_ld();
@@ -142,7 +149,7 @@ __device__ __forceinline__ void store_sums(uint32_t t, float f, uint16_t *o,
 template <int D>
 __device__ __forceinline__ void store_zeros(uint16_t *o) {
 #pragma unroll
-    for (int c = 0; c < kOut<D>; c += 8)
+    for (int c = 0; c < Eb<D>::out; c += 8)
         *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
 }
 
@@ -185,7 +192,7 @@ __global__ void __launch_bounds__(256)
 
 // Key and value tiles held: K(j) serves S(j) and dQ(j), behind S(j + 2).
 template <int D>
-constexpr int kDqK = D > 64 ? 3 : 6;
+constexpr int kDqK = D > 64 ? 3 : 5;
 template <int D>
 constexpr int kDqV = D > 64 ? 2 : 4;
 
@@ -205,12 +212,11 @@ struct BwdItem {
 };
 
 // A CTA holds Q and dO of 128 rows (of the heads that share a K/V head,
-// counted through) and walks key tiles. Warps 0-15: weights, four threads a
-// row, for 32 keys of a tile each; warp 16 issues S and dQ, warp 17 dP; warp 18
-// takes the items and loads Q, dO and K, warp 19 V. Tensor memory: S of two
-// tiles, dP, dQ; dS goes over the S it came from.
+// counted through) and walks key tiles. The first warps make the weights; then
+// one issues S and dQ, one dP, one takes the items and loads Q, dO and K, one V.
+// Tensor memory: S of two tiles, dP, dQ; dS goes over the S it came from.
 template <int D>
-__global__ void __launch_bounds__(kEbThreads, 1)
+__global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
     k_exact_dq_tc(const __grid_constant__ CUtensorMap tmQ,
                   const __grid_constant__ CUtensorMap tmG,
                   const __grid_constant__ CUtensorMap tmK,
@@ -226,20 +232,22 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     __shared__ int abort_flag;
     __shared__ BwdItem item_s[2];
     volatile int *abort = &abort_flag;
-    constexpr uint32_t kTile = kTileBytes<D>;
-    constexpr uint32_t kS = 0, kP = 256, kO = 384;  // tensor memory columns
+    using E = Eb<D>;
+    constexpr uint32_t kTile = E::tile;
+    // tensor memory columns
+    constexpr uint32_t kS = 0, kP = 2 * E::rows, kO = 3 * E::rows;
     const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
-    const uint32_t sQ = align1k(smem_u32(smem_raw)), sG = sQ + kTile;
-    const uint32_t sK = sG + kTile, sV = sK + kK * kTile;
+    const uint32_t sQ = align1k(smem_u32(smem_raw)), sG = sQ + E::held;
+    const uint32_t sK = sG + E::held, sV = sK + kK * kTile;
     DeviceStatus *status = a.status;
 
-    if (warp == kEbWeights) tmem_alloc(&tbase, 512);
+    if (warp == E::weights) tmem_alloc(&tbase, E::columns);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], kEbWeights + 3);
+            mbar_init(&bars.item_empty[s], E::weights + 3);
             mbar_init(&bars.s_full[s], 1);
-            mbar_init(&bars.ds_full[s], kEbWeights);
+            mbar_init(&bars.ds_full[s], E::weights);
         }
         for (int s = 0; s < kK; ++s) {
             mbar_init(&bars.k_full[s], 1);
@@ -252,9 +260,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         mbar_init(&bars.q_full, 1);
         mbar_init(&bars.q_empty, 2);  // S and dP
         mbar_init(&bars.dp_full, 1);
-        mbar_init(&bars.dp_read, kEbWeights);
+        mbar_init(&bars.dp_read, E::weights);
         mbar_init(&bars.dq_full, 1);
-        mbar_init(&bars.dq_empty, 4 * kOutShare<D>);
+        mbar_init(&bars.dq_empty, E::weights);
         abort_flag = 0;
         fence_mbar_init();
     }
@@ -263,18 +271,18 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     tc_fence_after();
     const uint32_t tm = tbase;
 
-    if (warp >= kEbWeights) {
+    if (warp >= E::weights) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
-            kEbRegsOther));
-        if (warp == kEbWeights + 2 && lane_id == 0) {
+            E::other));
+        if (warp == E::weights + 2 && lane_id == 0) {
             // ---------------------------------------------- items and loads
             int c = 0, qs = 0;  // key tiles and items loaded so far
             bool ok = true;
             const int heads = a.B * a.Hkv, rows = order.rows;
             auto tile = [&](uint64_t *full, uint32_t dst,
-                            const CUtensorMap *map, int row) {
-                for (int p = 0; p < kPanels<D>; ++p)
-                    tma_load_2d(dst + p * 16384, map, 64 * p, row, full);
+                            const CUtensorMap *map, int row, int rows_) {
+                for (int p = 0; p < E::panels; ++p)
+                    tma_load_2d(dst + p * rows_ * 128, map, 64 * p, row, full);
             };
             for (int it = 0; ok; ++it) {
                 const long item =
@@ -296,7 +304,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     w.ql = seq.ql;
                     w.kl = seq.kl;
                     w.n = (exact_most(seq, w.r0, min(w.r0 + 128, rows),
-                                      order.pitch) + 127) / 128;
+                                      order.pitch) + E::rows - 1) / E::rows;
                 }
                 item_s[it & 1] = w;
                 mbar_arrive(&bars.item_full[it & 1]);
@@ -309,9 +317,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq +
                                order.row(w.r0, a.Nq);
                 const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
-                mbar_expect_tx(&bars.q_full, 2 * kTile);
-                tile(&bars.q_full, sQ, &tmQ, q0);
-                tile(&bars.q_full, sG, &tmG, q0);
+                mbar_expect_tx(&bars.q_full, 2 * E::held);
+                tile(&bars.q_full, sQ, &tmQ, q0, 128);
+                tile(&bars.q_full, sG, &tmG, q0, 128);
                 for (int kt = 0; kt < w.n; ++kt, ++c) {
                     const int ks = c % kK;
                     if (c >= kK &&
@@ -321,10 +329,10 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         break;
                     mbar_expect_tx(&bars.k_full[ks], kTile);
                     tile(&bars.k_full[ks], sK + ks * kTile, &tmK,
-                         k0 + 128 * kt);
+                         k0 + E::rows * kt, E::rows);
                 }
             }
-        } else if (warp == kEbWeights + 3 && lane_id == 0) {
+        } else if (warp == E::weights + 3 && lane_id == 0) {
             // ------------------------------------------ loads of the values
             int c = 0;
             bool ok = true;
@@ -344,12 +352,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                                   status, 435)))
                         break;
                     mbar_expect_tx(&bars.v_full[vs], kTile);
-                    for (int p = 0; p < kPanels<D>; ++p)
-                        tma_load_2d(sV + vs * kTile + p * 16384, &tmV, 64 * p,
-                                    k0 + 128 * kt, &bars.v_full[vs]);
+                    for (int p = 0; p < E::panels; ++p)
+                        tma_load_2d(sV + vs * kTile + p * E::rows * 128, &tmV, 64 * p,
+                                    k0 + E::rows * kt, &bars.v_full[vs]);
                 }
             }
-        } else if (warp < kEbWeights + 2) {
+        } else if (warp < E::weights + 2) {
             // ---------------------------------------------------- MMA issue
             // One warp for S and dQ, one for dP: a wait costs a warp about 150
             // clocks even when there is nothing to wait for, and few products
@@ -360,7 +368,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             auto wait = [&](uint64_t *bar, uint32_t par, int site) {
                 return warp_wait(bar, par, abort, status, site);
             };
-            const bool first = warp == kEbWeights;
+            const bool first = warp == E::weights;
             const uint64_t dQ = smem_desc(sQ, 16, 1024);
             const uint64_t dG = smem_desc(sG, 16, 1024);
             const uint64_t dK = smem_desc(sK, 16, 1024);
@@ -402,11 +410,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         return false;
                     // keys that the sequence does not have count with dS = 0
                     // in dQ and must be numbers
-                    if (kl - 128 * j < 128)
-                        zero_rows<D>(sK + ks * kTile, kl - 128 * j, lane_id);
+                    if (kl - E::rows * j < E::rows)
+                        zero_rows<D>(sK + ks * kTile, kl - E::rows * j,
+                                     lane_id);
                     tc_fence_after();
                     if (el) {
-                        mma_scores<D>(tm + kS + 128 * (x & 1), dQ,
+                        mma_scores<D>(tm + kS + E::rows * (x & 1), dQ,
                                       desc_at(dK, ks * kTile));
                         mma_commit(&bars.s_full[x & 1]);
                         if (j == n - 1) mma_commit(&bars.q_empty);
@@ -422,7 +431,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     if (!ok) break;
                     tc_fence_after();
                     if (el) {
-                        mma_sums<D>(tm + kO, tm + kS + 128 * (x & 1),
+                        mma_sums<D>(tm + kO, tm + kS + E::rows * (x & 1),
                                     desc_at(dKm, ks * kTile), j > 0);
                         mma_commit(&bars.k_empty[ks]);
                         if (j == n - 1) mma_commit(&bars.dq_full);
@@ -436,7 +445,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         __syncwarp();
     } else {
         // ---------------------------------------------------------- weights
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEbRegsSoft));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(E::soft));
         const int part = warp >> 2, row = (warp & 3) * 32 + lane_id;
         const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t0 = tm + lane + 32 * part;
@@ -452,14 +461,13 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
             if (w.item < 0) break;
-            const bool writes = part < kOutShare<D>;
             const int r = w.r0 + row, i = r % order.pitch;
             const bool valid = r < order.rows && i < w.ql;
             const size_t at = (size_t)(w.b * a.H + w.kvh * a.G) * a.Nq +
                               order.row(r, a.Nq);
-            uint16_t *o = (uint16_t *)a.dq + at * D + kOut<D> * part;
+            uint16_t *o = (uint16_t *)a.dq + at * D + E::out * part;
             if (w.n == 0) {
-                if (valid && writes) store_zeros<D>(o);
+                if (valid) store_zeros<D>(o);
                 continue;
             }
             int seen = 0;
@@ -476,7 +484,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                      status, 432)))
                     break;
                 tc_fence_after();
-                const uint32_t tS = t0 + kS + 128 * (c & 1);
+                const uint32_t tS = t0 + kS + E::rows * (c & 1);
                 float2 p[16], g[16];
                 load32(tS, p);
 #pragma unroll
@@ -495,7 +503,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
 #pragma unroll
                 for (int q = 0; q < 16; ++q)
                     g[q] = mul2(p[q], add2(g[q], nd2));
-                const int lim = seen - 128 * j - 32 * part;
+                const int lim = seen - E::rows * j - 32 * part;
                 if (__any_sync(0xffffffffu, lim < 32)) {
 #pragma unroll
                     for (int q = 0; q < 16; ++q) {
@@ -510,8 +518,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 break;
             ++qs;
             tc_fence_after();
-            if (!writes) continue;
-            store_sums<D>(tm + lane + kO + kOut<D> * part, a.scale, o, valid);
+            store_sums<D>(tm + lane + kO + E::out * part, a.scale, o, valid);
             tc_fence_before();
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.dq_empty);
@@ -519,18 +526,16 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == kEbWeights) tmem_dealloc(tm, 512);
+    if (warp == E::weights) tmem_dealloc(tm, E::columns);
 }
 
 // --------------------------------------------------------------- dK and dV
 
 template <int D>
 struct Dkv {
-    static constexpr int kS = D > 64 ? 1 : 2;  // S in tensor memory
-    // query tiles and dO tiles held: Q(j) serves S(j) and dK(j), behind
-    // S(j + kS)
-    static constexpr int kQ = D > 64 ? 3 : 4, kG = D > 64 ? 2 : 4;
-    static constexpr uint32_t cS = 0, cP = 128 * kS, cV = cP + 128,
+    static constexpr int kQ = D > 64 ? 3 : 4, kG = D > 64 ? 2 : 4;  // tiles held
+    // tensor memory columns
+    static constexpr uint32_t cS = 0, cP = Eb<D>::rows, cV = 2 * Eb<D>::rows,
                               cK = cV + D;
 };
 template <int D>
@@ -545,22 +550,22 @@ struct DkvBars {
 // What lies behind the tiles in shared memory (there are 3 KB).
 template <int D>
 struct DkvShared {
-    float row_l[2][128], row_d[2][128];  // -lse (base 2) and -D of the rows
+    // -lse (base 2) and -D of the rows
+    float row_l[2][Eb<D>::rows], row_d[2][Eb<D>::rows];
     DkvBars<D> bars;
     BwdItem item[2];
     uint32_t tbase;
     int abort_flag;
 };
 
-// A CTA holds K and V of 128 rows and walks tiles of 128 query rows of every
-// head that reads them; scores and weights stand transposed, a key a lane.
-// Warps 0-15: weights, four threads a key, for 32 queries of a tile each; warp
-// 16 issues the products; warp 18 takes the items and loads K, V and Q; warp 19
-// loads dO and fetches the rows' lse and D. Tensor memory: S^T (two for
-// D <= 64), dP^T, dV, dK; P^T and dS^T go over the S^T and dP^T that they came
-// from.
+// A CTA holds K and V of 128 rows and walks tiles of query rows of every head
+// that reads them; scores and weights stand transposed, a key a lane. The first
+// warps make the weights; then one issues the products, one (behind one that
+// has nothing to do) takes the items and loads K, V and Q, and one loads dO and
+// fetches the rows' lse and D. Tensor memory: S^T, dP^T, dV, dK; P^T and dS^T go
+// over the S^T and dP^T that they came from.
 template <int D>
-__global__ void __launch_bounds__(kEbThreads, 1)
+__global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
     k_exact_dkv_tc(const __grid_constant__ CUtensorMap tmQ,
                    const __grid_constant__ CUtensorMap tmG,
                    const __grid_constant__ CUtensorMap tmK,
@@ -570,8 +575,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     wait_for_stream();
     using X = Dkv<D>;
     extern __shared__ unsigned char smem_raw[];
-    constexpr uint32_t kTile = kTileBytes<D>;
-    constexpr uint32_t kTiles = (2 + X::kQ + X::kG) * kTile;
+    using E = Eb<D>;
+    constexpr uint32_t kTile = E::tile;
+    constexpr uint32_t kTiles = 2 * E::held + (X::kQ + X::kG) * kTile;
     // there is no room for a whole KB of padding: dynamic shared memory begins
     // on one, as the kernel has no other
     const uint32_t pad = align1k(smem_u32(smem_raw)) - smem_u32(smem_raw);
@@ -585,18 +591,18 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     auto &row_l = sh.row_l, &row_d = sh.row_d;
     volatile int *abort = &sh.abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
-    const uint32_t sK = smem_u32(smem_raw), sV = sK + kTile;
-    const uint32_t sQ = sV + kTile, sG = sQ + X::kQ * kTile;
+    const uint32_t sK = smem_u32(smem_raw), sV = sK + E::held;
+    const uint32_t sQ = sV + E::held, sG = sQ + X::kQ * kTile;
     DeviceStatus *status = a.status;
 
-    if (warp == kEbWeights) tmem_alloc(&sh.tbase, 512);
+    if (warp == E::weights) tmem_alloc(&sh.tbase, E::columns);
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], kEbWeights + 2);
-            mbar_init(&bars.l_empty[s], kEbWeights);
+            mbar_init(&bars.item_empty[s], E::weights + 2);
+            mbar_init(&bars.l_empty[s], E::weights);
             mbar_init(&bars.s_full[s], 2);  // the product, lse and D
-            mbar_init(&bars.p_full[s], kEbWeights);
+            mbar_init(&bars.p_full[s], E::weights);
         }
         for (int s = 0; s < X::kG; ++s) {
             mbar_init(&bars.g_full[s], 1);
@@ -609,9 +615,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         mbar_init(&bars.kv_full, 1);
         mbar_init(&bars.kv_empty, 1);
         mbar_init(&bars.dp_full, 1);
-        mbar_init(&bars.ds_full, kEbWeights);
+        mbar_init(&bars.ds_full, E::weights);
         mbar_init(&bars.sum_full, 1);
-        mbar_init(&bars.sum_empty, 4 * kOutShare<D>);
+        mbar_init(&bars.sum_empty, E::weights);
         sh.abort_flag = 0;
         fence_mbar_init();
     }
@@ -621,21 +627,21 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     const uint32_t tm = sh.tbase;
     // tiles of a query head's rows, walked head by head
     auto tiles_of = [](const BwdItem &w) {
-        return (w.ql - w.first + 127) / 128;
+        return (w.ql - w.first + E::rows - 1) / E::rows;
     };
 
-    if (warp >= kEbWeights) {
+    if (warp >= E::weights) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(
-            kEbRegsOther));
-        if (warp == kEbWeights + 2 && lane_id == 0) {
+            E::other));
+        if (warp == E::weights + 2 && lane_id == 0) {
             // ---------------------------------------------- items and loads
             int c = 0, ks = 0;  // query tiles and items loaded so far
             bool ok = true;
             const int heads = a.B * a.Hkv;
             auto tile = [&](uint64_t *full, uint32_t dst,
-                            const CUtensorMap *map, int row) {
-                for (int p = 0; p < kPanels<D>; ++p)
-                    tma_load_2d(dst + p * 16384, map, 64 * p, row, full);
+                            const CUtensorMap *map, int row, int rows_) {
+                for (int p = 0; p < E::panels; ++p)
+                    tma_load_2d(dst + p * rows_ * 128, map, 64 * p, row, full);
             };
             for (int it = 0; ok; ++it) {
                 const long item =
@@ -669,12 +675,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     break;
                 ++ks;
                 const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk + w.r0;
-                mbar_expect_tx(&bars.kv_full, 2 * kTile);
-                tile(&bars.kv_full, sK, &tmK, k0);
-                tile(&bars.kv_full, sV, &tmV, k0);
+                mbar_expect_tx(&bars.kv_full, 2 * E::held);
+                tile(&bars.kv_full, sK, &tmK, k0, 128);
+                tile(&bars.kv_full, sV, &tmV, k0, 128);
                 const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
                 for (int g = 0; g < a.G && ok; ++g)
-                    for (int i = w.first; i < w.ql; i += 128, ++c) {
+                    for (int i = w.first; i < w.ql; i += E::rows, ++c) {
                         const int qs = c % X::kQ;
                         if (c >= X::kQ &&
                             !(ok = mbar_wait_or_abort(&bars.q_empty[qs],
@@ -683,14 +689,14 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                             break;
                         mbar_expect_tx(&bars.q_full[qs], kTile);
                         tile(&bars.q_full[qs], sQ + qs * kTile, &tmQ,
-                             q0 + g * a.Nq + i);
+                             q0 + g * a.Nq + i, E::rows);
                     }
             }
-        } else if (warp == kEbWeights) {
+        } else if (warp == E::weights) {
             // ---------------------------------------------------- MMA issue
-            // In the order dV(t), S(t + kS), dK(t), dP(t + 1): P(t + 1) is
+            // In the order dV(t), S(t + 1), dK(t), dP(t + 1): P(t + 1) is
             // made during dK(t) and dP(t + 1), dS(t) during dV(t) and
-            // S(t + kS). Few products are queued behind those that run, so
+            // S(t + 1). Few products are queued behind those that run, so
             // that the tensor cores stand still during waits, even such that
             // find their barrier complete: two products a wait. (A warp for
             // each pair let the pairs' products run mixed, each of them later:
@@ -727,21 +733,21 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 // the tile of S(t) or dP(t) is there
                 auto scores = [&](int t) {
                     const int x = c + t, qs = x % X::kQ;
-                    if (left_q < 128)
+                    if (left_q < E::rows)
                         zero_rows<D>(sQ + qs * kTile, left_q, lane_id);
-                    left_q = left_q > 128 ? left_q - 128 : all;
+                    left_q = left_q > E::rows ? left_q - E::rows : all;
                     tc_fence_after();
                     if (el) {
-                        mma_scores<D>(tm + X::cS + 128 * (x % X::kS), dK,
+                        mma_scores<D>(tm + X::cS, dK,
                                       desc_at(dQ, qs * kTile));
                         mma_commit(&bars.s_full[x & 1]);
                     }
                 };
                 auto products = [&](int t) {
                     const int x = c + t, gs = x % X::kG;
-                    if (left_g < 128)
+                    if (left_g < E::rows)
                         zero_rows<D>(sG + gs * kTile, left_g, lane_id);
-                    left_g = left_g > 128 ? left_g - 128 : all;
+                    left_g = left_g > E::rows ? left_g - E::rows : all;
                     tc_fence_after();
                     if (el) {
                         mma_scores<D>(tm + X::cP, dV, desc_at(dG, gs * kTile));
@@ -756,17 +762,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 scores(0);
                 if (!(ok = wait(g_at(0), c / X::kG & 1, 447))) break;
                 products(0);
-                if (X::kS > 1 && n > 1) {
-                    ok = wait(q_at(1), (c + 1) / X::kQ & 1, 446);
-                    if (!ok) break;
-                    scores(1);
-                }
                 if (ks > 0 &&
                     !(ok = wait(&bars.sum_empty, (ks - 1) & 1, 448)))
                     break;
                 for (int t = 0; t < n && ok; ++t) {
                     const int x = c + t, qs = x % X::kQ, gs = x % X::kG;
-                    const int u = t + X::kS;
+                    const int u = t + 1;
                     uint64_t *p = &bars.p_full[x & 1];
                     ok = u < n ? wait2(p, x / 2 & 1, q_at(u),
                                        (c + u) / X::kQ & 1, 449)
@@ -774,8 +775,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                     if (!ok) break;
                     tc_fence_after();
                     if (el) {
-                        mma_sums<D>(tm + X::cV,
-                                    tm + X::cS + 128 * (x % X::kS),
+                        mma_sums<D>(tm + X::cV, tm + X::cS,
                                     desc_at(dGm, gs * kTile), t > 0);
                         mma_commit(&bars.g_empty[gs]);
                     }
@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 c += n;
                 ++ks;
             }
-        } else if (warp == kEbWeights + 3) {
+        } else if (warp == E::weights + 3) {
             // --------------------------------- loads of dO, of lse and D
             int c = 0;
             bool ok = true;
@@ -813,9 +813,9 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 for (int t = 0; t < w.n; ++t, ++c) {
                     const int gs = c % X::kG;
                     const size_t at = (size_t)head + i0;
-                    float l[4], d[4];
+                    float l[E::parts], d[E::parts];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < E::parts; ++q) {
                         const int i = lane_id + 32 * q;
                         l[q] = d[q] = 0.0f;
                         if (i0 + i < w.ql) {
@@ -830,8 +830,8 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                         break;
                     if (lane_id == 0) {
                         mbar_expect_tx(&bars.g_full[gs], kTile);
-                        for (int p = 0; p < kPanels<D>; ++p)
-                            tma_load_2d(sG + gs * kTile + p * 16384, &tmG,
+                        for (int p = 0; p < E::panels; ++p)
+                            tma_load_2d(sG + gs * kTile + p * E::rows * 128, &tmG,
                                         64 * p, head + i0, &bars.g_full[gs]);
                     }
                     if (c >= 2 && !(ok = warp_wait(&bars.l_empty[c & 1],
@@ -839,13 +839,13 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                                    status, 452)))
                         break;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < E::parts; ++q) {
                         row_l[c & 1][lane_id + 32 * q] = -l[q] * kLog2e;
                         row_d[c & 1][lane_id + 32 * q] = -d[q];
                     }
                     __syncwarp();
                     if (lane_id == 0) mbar_arrive(&bars.s_full[c & 1]);
-                    i0 += 128;
+                    i0 += E::rows;
                     if (i0 >= w.ql) {
                         i0 = w.first;
                         head += a.Nq;
@@ -856,7 +856,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
         __syncwarp();
     } else {
         // ---------------------------------------------------------- weights
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEbRegsSoft));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(E::soft));
         const int part = warp >> 2, row = (warp & 3) * 32 + lane_id;
         const uint32_t lane = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t0 = tm + lane + 32 * part;
@@ -873,12 +873,12 @@ __global__ void __launch_bounds__(kEbThreads, 1)
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
             if (w.item < 0) break;
             const int j = w.r0 + row;
-            const bool valid = j < w.kl, writes = part < kOutShare<D>;
+            const bool valid = j < w.kl;
             const size_t at = ((size_t)(w.b * a.Hkv + w.kvh) * a.Nk + j) * D +
-                              kOut<D> * part;
+                              E::out * part;
             uint16_t *ok_ = (uint16_t *)a.dk + at, *ov = (uint16_t *)a.dv + at;
             if (w.n == 0) {
-                if (valid && writes) {
+                if (valid) {
                     store_zeros<D>(ok_);
                     store_zeros<D>(ov);
                 }
@@ -897,7 +897,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                                      status, 455)))
                     break;
                 tc_fence_after();
-                const uint32_t tS = t0 + X::cS + 128 * (c % X::kS);
+                const uint32_t tS = t0 + X::cS;
                 const float4 *nl = reinterpret_cast<const float4 *>(
                     &row_l[c & 1][32 * part]);
                 const float4 *nd = reinterpret_cast<const float4 *>(
@@ -942,8 +942,8 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 }
                 store32(t0 + X::cP, g, &bars.ds_full, lane_id);
                 if (lane_id == 0) mbar_arrive(&bars.l_empty[c & 1]);
-                lo -= 128;
-                hi -= 128;
+                lo -= E::rows;
+                hi -= E::rows;
                 if (hi + 32 * part <= 0) {  // the next head
                     lo = lo0;
                     hi = hi0;
@@ -954,8 +954,7 @@ __global__ void __launch_bounds__(kEbThreads, 1)
                 break;
             ++ks;
             tc_fence_after();
-            if (!writes) continue;
-            const uint32_t t = tm + lane + kOut<D> * part;
+            const uint32_t t = tm + lane + E::out * part;
             store_sums<D>(t + X::cV, 1.0f, ov, valid);
             store_sums<D>(t + X::cK, a.scale, ok_, valid);
             tc_fence_before();
@@ -965,19 +964,20 @@ __global__ void __launch_bounds__(kEbThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == kEbWeights) tmem_dealloc(tm, 512);
+    if (warp == E::weights) tmem_dealloc(tm, E::columns);
 }
 
 struct Maps {
     CUtensorMap q, g, k, v;
 };
-cudaError_t make_maps(const ExactView &a, Maps *m) {
+// q_rows, k_rows: of the tiles of Q and dO, of K and V
+cudaError_t make_maps(const ExactView &a, int q_rows, int k_rows, Maps *m) {
     const uint64_t nq = (uint64_t)a.B * a.H * a.Nq;
     const uint64_t nk = (uint64_t)a.B * a.Hkv * a.Nk;
-    cudaError_t e = make_tma_map_bf16(&m->q, a.q, nq, a.d, 128);
-    if (e == cudaSuccess) e = make_tma_map_bf16(&m->g, a.d_o, nq, a.d, 128);
-    if (e == cudaSuccess) e = make_tma_map_bf16(&m->k, a.k, nk, a.d, 128);
-    if (e == cudaSuccess) e = make_tma_map_bf16(&m->v, a.v, nk, a.d, 128);
+    cudaError_t e = make_tma_map_bf16(&m->q, a.q, nq, a.d, q_rows);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&m->g, a.d_o, nq, a.d, q_rows);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&m->k, a.k, nk, a.d, k_rows);
+    if (e == cudaSuccess) e = make_tma_map_bf16(&m->v, a.v, nk, a.d, k_rows);
     return e;
 }
 int sm_count() {
@@ -1009,17 +1009,18 @@ cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
                                cudaStream_t st) {
     const ExactOrder order(a, 128);
     const long items = order.items(a);
-    const int sms = sm_count();
-    Maps m;
-    const cudaError_t e = make_maps(a, &m);
-    if (e != cudaSuccess) return e;
     return by_width(a.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
+        using E = Eb<D>;
+        const long most = (long)sm_count() * E::ctas;
+        Maps m;
+        const cudaError_t e = make_maps(a, 128, E::rows, &m);
+        if (e != cudaSuccess) return e;
         const size_t smem =
-            1024 + (size_t)(2 + kDqK<D> + kDqV<D>) * kTileBytes<D>;
+            1024 + 2 * E::held + (size_t)(kDqK<D> + kDqV<D>) * E::tile;
         return launch_after(
-            k_exact_dq_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
-            kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, order, (int)items,
+            k_exact_dq_tc<D>, dim3((unsigned)(items < most ? items : most)),
+            E::threads, smem, st, m.q, m.g, m.k, m.v, a, order, (int)items,
             next_item);
     });
 }
@@ -1027,19 +1028,20 @@ cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
 cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
                                 cudaStream_t st) {
     const long items = (long)((a.Nk + 127) / 128) * a.B * a.Hkv;
-    const int sms = sm_count();
-    Maps m;
-    const cudaError_t e = make_maps(a, &m);
-    if (e != cudaSuccess) return e;
     return by_width(a.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
+        using E = Eb<D>;
+        const long most = (long)sm_count() * E::ctas;
+        Maps m;
+        const cudaError_t e = make_maps(a, E::rows, 128, &m);
+        if (e != cudaSuccess) return e;
         constexpr size_t smem =
-            sizeof(DkvShared<D>) +
-            (size_t)(2 + Dkv<D>::kQ + Dkv<D>::kG) * kTileBytes<D>;
+            2 * E::held + (size_t)(Dkv<D>::kQ + Dkv<D>::kG) * E::tile +
+            sizeof(DkvShared<D>);
         static_assert(smem <= 232448, "shared memory of a CTA");
         return launch_after(
-            k_exact_dkv_tc<D>, dim3((unsigned)(items < sms ? items : sms)),
-            kEbThreads, smem, st, m.q, m.g, m.k, m.v, a, (int)items,
+            k_exact_dkv_tc<D>, dim3((unsigned)(items < most ? items : most)),
+            E::threads, smem, st, m.q, m.g, m.k, m.v, a, (int)items,
             next_item);
     });
 }
