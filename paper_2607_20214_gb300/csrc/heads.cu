@@ -27,9 +27,9 @@ namespace {
 
 constexpr int kHeadWarps = 8;
 // CTAs of the backward kernel at most, each of which leaves a partial of dw:
-// eight of 8 warps on each of the 152 SMs of a GB300. Fixed, so that the
+// six of 8 warps for each of the 152 SMs of a GB300. Fixed, so that the
 // workspace does not depend on the device.
-constexpr int kHeadCtas = 1216;
+constexpr int kHeadCtas = 912;
 
 struct RowsView {
     char *p;
@@ -99,19 +99,34 @@ struct Turn {
     float c[VE], s[VE];
 };
 
-// Sines and cosines of the token at (b, n), two pairs a lane, handed to the
-// lanes whose channels they turn.
-template <int VE, int LPH, bool IL>
+// Sine and cosine of h half turns, h in [-1, 1). For heads of bf16 the
+// hardware's: an absolute error of 2^-21 where the result is rounded to 2^-8.
+// (With sincospif the backward pass of B8 H12 N8192 d64 took 5 us more.)
+template <typename T>
+__device__ __forceinline__ void half_turns(float h, float *s, float *c) {
+    if (sizeof(T) == 4) {
+        sincospif(h, s, c);
+    } else {
+        const float x = h * 3.14159265f;
+        *s = __sinf(x);
+        *c = __cosf(x);
+    }
+}
+
+// Sines and cosines of the token at (b, n), a pair a lane or two (D = 128),
+// handed to the lanes whose channels they turn.
+template <typename T, int D, int VE, int LPH, bool IL>
 __device__ __forceinline__ void make_turn(const HeadsArgs &a, int b, int n,
                                           int n_new, int lane,
                                           Turn<VE> &t) {
-    float c0[2], s0[2];
+    constexpr int PL = D > 64 ? 2 : 1;
+    float c0[PL], s0[PL];
     const int pairs = a.dim >> 1;
     int64_t start = n;
     if (a.lengths) start += (int64_t)a.lengths[b] - n_new;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int p = 2 * lane + i;
+    for (int i = 0; i < PL; ++i) {
+        const int p = PL * lane + i;
         c0[i] = 1.0f;
         s0[i] = 0.0f;
         if (p < pairs) {
@@ -119,9 +134,9 @@ __device__ __forceinline__ void make_turn(const HeadsArgs &a, int b, int n,
             if (a.positions)
                 pos = a.positions[((size_t)a.axis[p] * a.B + b) * a.N + n];
             const uint64_t f = (uint64_t)pos * a.turns[p];
-            // half turns in [-1, 1): the 32 leading bits of the fraction
+            // the 32 leading bits of the fraction
             const float h = (float)(int32_t)(f >> 32) * 0x1p-31f;
-            sincospif(h, &s0[i], &c0[i]);
+            half_turns<T>(h, &s0[i], &c0[i]);
         }
     }
     const int ch = (lane % LPH) * VE;
@@ -139,11 +154,11 @@ __device__ __forceinline__ void make_turn(const HeadsArgs &a, int b, int n,
     }
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-        // the pair of channel ch + e, in lane pair / 2
+        // the pair of channel ch + e, in lane pair / PL
         const int q = IL ? e >> 1 : e;
-        const int src = ((base + q) >> 1) & 31;
-        const float c = __shfl_sync(~0u, c0[q & 1], src);
-        const float s = __shfl_sync(~0u, s0[q & 1], src);
+        const int src = ((base + q) / PL) & 31;
+        const float c = __shfl_sync(~0u, c0[q % PL], src);
+        const float s = __shfl_sync(~0u, s0[q % PL], src);
         const bool rot = IL ? ch + e < a.dim : t.on;
         t.c[e] = rot ? c : 1.0f;
         t.s[e] = rot ? (IL ? (e & 1 ? s : -s) : sign * s) : 0.0f;
@@ -183,9 +198,10 @@ __device__ __forceinline__ float2 two(const float (&x)[VE], int i) {
     return make_float2(x[2 * i], x[2 * i + 1]);
 }
 
-// __launch_bounds__: four CTAs an SM
+// Five CTAs an SM: B2 H16 N16384 d128 bf16 142 us, with four 149, with six and
+// two groups a time 146.
 template <typename T, int D, bool IL>
-__global__ void __launch_bounds__(kHeadWarps * 32, 4)
+__global__ void __launch_bounds__(kHeadWarps * 32, 5)
     k_heads_forward(const __grid_constant__ HeadsArgs a) {
     wait_for_stream();
     using V = Vec<T>;
@@ -237,7 +253,7 @@ __global__ void __launch_bounds__(kHeadWarps * 32, 4)
     bool rot;
     {
         Turn<VE> t;
-        make_turn<VE, LPH, IL>(a, b, n, n_new, lane, t);
+        make_turn<T, D, VE, LPH, IL>(a, b, n, n_new, lane, t);
         float w[VE];
 #pragma unroll
         for (int e = 0; e < VE; ++e)
@@ -315,15 +331,45 @@ __device__ __forceinline__ void load_grad(const char *p, float *g) {
                         g + n * i);
 }
 
+// The gradients of copies 1 .. cp - 1, three loads at a time.
+template <typename T, typename GT>
+__device__ __forceinline__ void add_copies(const char *p, size_t step, int cp,
+                                           float (&g)[Vec<T>::n]) {
+    constexpr int VE = Vec<T>::n;
+    for (int i = 1; i < cp; i += 3) {
+        float m[3][VE];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) m[k][e] = 0.0f;
+            if (i + k < cp) load_grad<T, GT>(p + (i + k) * step, m[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) g[e] += m[k][e];
+    }
+}
+
+// Groups of heads that a warp of the backward kernel reads at a time, and CTAs
+// an SM, by the bytes of a lane's gradients: fp32 ones of bf16 rows (32) fill
+// the registers of two CTAs, and three groups in flight serve memory better than
+// more warps (B8 H12 N8192 d64 214 us; two groups 251, one group and three CTAs
+// 240; half the channels a lane 287; asking for the next groups before working
+// on those at hand 219). 16-bit ones do best the other way (padded B2 H16 H_kv4
+// N2047 d128, copied heads: 35 us; two groups and two CTAs 42).
+template <typename T, typename GT>
+constexpr bool kWide = sizeof(GT) * Vec<T>::n > 16;
+
 // The backward pass. A CTA's warps walk the tokens; dw is summed in
 // registers, then over the CTA's warps, and leaves as one partial of the CTA
 // that k_heads_weights adds up in order.
 template <typename T, typename GT, int D, bool IL>
-__global__ void __launch_bounds__(kHeadWarps * 32, 2)
+__global__ void __launch_bounds__(kHeadWarps * 32, (kWide<T, GT> ? 2 : 3))
     k_heads_backward(const __grid_constant__ HeadsArgs a) {
     wait_for_stream();
     using V = Vec<T>;
-    constexpr int VE = V::n, LPH = D / VE, HPW = 32 / LPH, U = 2;
+    constexpr int VE = V::n, LPH = D / VE, HPW = 32 / LPH, U = kWide<T, GT> ? 3 : 1;
     __shared__ float sums[kHeadWarps][D];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ch = (lane % LPH) * VE;
@@ -349,7 +395,7 @@ __global__ void __launch_bounds__(kHeadWarps * 32, 2)
         const int n_new = a.new_len ? min(max(a.new_len[b], 0), a.N) : a.N;
         if (n >= n_new) continue;
         Turn<VE> t;
-        if (kind < 2) make_turn<VE, LPH, IL>(a, b, n, n_new, lane, t);
+        if (kind < 2) make_turn<T, D, VE, LPH, IL>(a, b, n, n_new, lane, t);
         const char *gp = a.out[kind] +
                          ((((size_t)b * heads + h0) * cp * a.N + n) * D + ch) *
                              sizeof(GT);
@@ -376,13 +422,7 @@ __global__ void __launch_bounds__(kHeadWarps * 32, 2)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (h0 + g + u * HPW < h1)
-                        for (int i = 1; i < cp; ++i) {
-                            float more[VE];
-                            load_grad<T, GT>(gp + u * g_step + i * g_head,
-                                             more);
-#pragma unroll
-                            for (int e = 0; e < VE; ++e) gr[u][e] += more[e];
-                        }
+                        add_copies<T, GT>(gp + u * g_step, g_head, cp, gr[u]);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
