@@ -98,7 +98,10 @@ cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
 cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
                                 cudaStream_t st);
 // CUDA cores (fp32, and bf16 with impl = SIMT)
-cudaError_t launch_exact_fwd_simt(const ExactView &a, cudaStream_t st);
+// part: exact_chunk_bytes(a) of scratch
+size_t exact_chunk_bytes(const ExactView &a);
+cudaError_t launch_exact_fwd_simt(const ExactView &a, float *part,
+                                  cudaStream_t st);
 cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys,
                                   cudaStream_t st);
 

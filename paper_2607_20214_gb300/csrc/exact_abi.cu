@@ -76,7 +76,7 @@ Layout layout(const ExactView &a, bool tensor, bool backward) {
     Layout l;
     l.next_item = sizeof(DeviceStatus);
     l.scratch = align256(l.next_item + 2 * sizeof(int));
-    size_t most = tensor ? exact_share_bytes(a) : 0;
+    size_t most = tensor ? exact_share_bytes(a) : exact_chunk_bytes(a);
     const size_t delta = sizeof(float) * (size_t)a.B * a.H * a.Nq;
     if (backward && delta > most) most = delta;
     l.total = l.scratch + align256(most);
@@ -143,7 +143,8 @@ extern "C" int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
                                                st));
     else
         ELSAA_EXACT_LAUNCH("exact_fwd_simt", st,
-                           launch_exact_fwd_simt(a, st));
+                           launch_exact_fwd_simt(
+                               a, (float *)(ws + l.scratch), st));
     return ELSAA_OK;
 }
 

@@ -9,7 +9,8 @@
 // scores of rows 4 y .. 4 y + 3 with x, x + 16, x + 32, x + 48, and of the sums
 // the same rows with d / 16 channels. Every four channels cost 8 16-byte reads
 // from shared memory for 64 multiply-adds (32 packed ones): bound by the
-// CUDA cores' multiply-adds.
+// CUDA cores' multiply-adds. With few tiles of rows the keys of the forward pass
+// are divided too, and k_exact_join adds up what the chunks of a row leave.
 #include <type_traits>
 
 #include "device_common.cuh"
@@ -145,13 +146,24 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
+// How the keys are divided: `splits` chunks at most, of `chunk` keys. What a
+// chunk leaves of row r (over all heads): the sums of e^(z - m) v in
+// o[part][r][D], and (m, sum of e^(z - m)) in ml[part][r], z and m base 2.
+struct Split {
+    int splits, chunk;
+    size_t rows;
+    float *o;
+    float2 *ml;
+};
+
 // Tile `t` (the last ones first: they see most) of K/V head `kvh`, b-major.
 struct Item {
-    int b, kvh, tile;
-    __device__ Item(const ExactView &a, int tiles) {
+    int b, kvh, tile, part;
+    __device__ Item(const ExactView &a, int tiles, int splits = 1) {
         const int heads = a.B * a.Hkv;
-        const int h = blockIdx.x % heads;
-        tile = tiles - 1 - (int)(blockIdx.x / heads);
+        const int h = blockIdx.x % heads, t = (int)(blockIdx.x / heads);
+        tile = tiles - 1 - t / splits;
+        part = t % splits;
         b = h / a.Hkv;
         kvh = h % a.Hkv;
     }
@@ -159,21 +171,25 @@ struct Item {
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads)
-    k_exact_fwd(const __grid_constant__ ExactView a, int tiles) {
+    k_exact_fwd(const __grid_constant__ ExactView a,
+                const __grid_constant__ Split split, int tiles) {
     wait_for_stream();
     extern __shared__ __align__(16) float sm[];
     float *sQ = sm, *sK = sQ + kHeld * D, *sV = sK + kPass * (D + 4);
     float *sP = sV + kPass * (D + 4);
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
     if (blockIdx.x == 0 && threadIdx.x < 4) (&a.status->code)[threadIdx.x] = 0;
-    const Item it(a, tiles);
+    const Item it(a, tiles, split.splits);
     const ExactSeq seq(a, it.b);
     const int rows = a.G * a.Nq, r0 = it.tile * kHeld;
     const int r1 = min(r0 + kHeld, rows);
     const size_t head0 = (size_t)it.b * a.H + (size_t)it.kvh * a.G;
     const T *q = (const T *)a.q + (head0 * a.Nq + r0) * D;
     const size_t kv = ((size_t)it.b * a.Hkv + it.kvh) * a.Nk;
-    const int most = exact_most(seq, r0, r1, a.Nq);
+    const int all = exact_most(seq, r0, r1, a.Nq);
+    const int first = it.part * split.chunk;
+    if (it.part > 0 && first >= all) return;
+    const int most = min(all, first + split.chunk);
     load_rows<T, D>(sQ, D, q, kHeld, [&](int r) {
         return r0 + r < r1 && (r0 + r) % a.Nq < seq.ql;
     });
@@ -190,7 +206,7 @@ __global__ void __launch_bounds__(kThreads)
         for (int c = 0; c < D / 32; ++c) acc[i][c] = make_float2(0.f, 0.f);
     }
     const float sl2 = a.scale * kLog2e;
-    for (int j0 = 0; j0 < most; j0 += kPass) {
+    for (int j0 = first; j0 < most; j0 += kPass) {
         __syncthreads();
         auto have = [&](int r) { return j0 + r < most; };
         load_rows<T, D>(sK, D + 4, (const T *)a.k + (kv + j0) * D, kPass, have);
@@ -230,6 +246,14 @@ __global__ void __launch_bounds__(kThreads)
     for (int i = 0; i < 4; ++i) {
         const int r = r0 + 4 * y + i;
         if (r >= r1 || r % a.Nq >= seq.ql) continue;
+        if (all > split.chunk) {
+            const size_t to = it.part * split.rows + head0 * a.Nq + r;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                store2(split.o + to * D + 2 * x + 32 * c, acc[i][c]);
+            if (x == 0) split.ml[to] = make_float2(m[i], l[i]);
+            continue;
+        }
         const float inv = l[i] > 0.f ? 1.0f / l[i] : l[i] == 0.f ? 0.f : l[i];
         T *o = (T *)a.out + (head0 * a.Nq + r) * D + 2 * x;
 #pragma unroll
@@ -239,6 +263,48 @@ __global__ void __launch_bounds__(kThreads)
             a.lse[head0 * a.Nq + r] =
                 l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
     }
+}
+
+// Joins the chunks of the rows that have more than one: D / 4 lanes a row.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+    k_exact_join(const __grid_constant__ ExactView a,
+                 const __grid_constant__ Split split) {
+    wait_for_stream();
+    constexpr int L = D / 4;
+    const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int c = threadIdx.x % L * 4;
+    if (row >= split.rows) return;
+    const int group = a.G * a.Nq, r = (int)(row % group);
+    const ExactSeq seq(a, (int)(row / group) / a.Hkv);
+    if (r % a.Nq >= seq.ql) return;
+    const int r0 = r / kHeld * kHeld;
+    const int all = exact_most(seq, r0, min(r0 + kHeld, group), a.Nq);
+    if (all <= split.chunk) return;
+    const int parts = (all + split.chunk - 1) / split.chunk;
+    float m = -INFINITY;
+    for (int p = 0; p < parts; ++p)
+        m = fmaxf(m, split.ml[p * split.rows + row].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < parts; ++p) {
+        const float2 ml = split.ml[p * split.rows + row];
+        const float f = exp2f(ml.x - ref);
+        const float4 v = *reinterpret_cast<const float4 *>(
+            split.o + (p * split.rows + row) * D + c);
+        l = fmaf(ml.y, f, l);
+        o.x = fmaf(v.x, f, o.x);
+        o.y = fmaf(v.y, f, o.y);
+        o.z = fmaf(v.z, f, o.z);
+        o.w = fmaf(v.w, f, o.w);
+    }
+    const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+    T *to = (T *)a.out + row * D + c;
+    store2(to, make_float2(o.x * inv, o.y * inv));
+    store2(to + 2, make_float2(o.z * inv, o.w * inv));
+    if (a.lse && c == 0)
+        a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // KEYS = 0: query rows held; dQ, and D_i = <dO_i, O_i> for the other kernel.
@@ -405,14 +471,51 @@ cudaError_t by_type(const ExactView &a, F f) {
 
 }  // namespace
 
-cudaError_t launch_exact_fwd_simt(const ExactView &a, cudaStream_t st) {
+namespace {
+
+// Eight CTAs for each of a GB300's 152 SMs, two tiles of keys in a chunk at
+// least. (By the sizes alone: the workspace does not depend on the device.)
+Split divide_keys(const ExactView &a) {
+    const long tiles = ((long)a.G * a.Nq + kHeld - 1) / kHeld;
+    const long items = tiles * a.B * a.Hkv;
+    const long passes = ((long)a.Nk + kPass - 1) / kPass;
+    long n = (8 * 152 + items - 1) / items;
+    if (n > passes / 2) n = passes / 2;
+    if (n < 1) n = 1;
+    Split s = {};
+    s.chunk = (int)((passes + n - 1) / n) * kPass;
+    s.splits = (int)(((long)a.Nk + s.chunk - 1) / s.chunk);
+    s.rows = (size_t)a.B * a.H * a.Nq;
+    return s;
+}
+
+}  // namespace
+
+size_t exact_chunk_bytes(const ExactView &a) {
+    const Split s = divide_keys(a);
+    return s.splits > 1 ? sizeof(float) * (a.d + 2) * s.splits * s.rows : 0;
+}
+
+cudaError_t launch_exact_fwd_simt(const ExactView &a, float *part,
+                                  cudaStream_t st) {
+    Split split = divide_keys(a);
+    split.o = part;
+    split.ml = (float2 *)(part + split.rows * split.splits * a.d);
     const int tiles = (int)(((long)a.G * a.Nq + kHeld - 1) / kHeld);
-    const dim3 grid((unsigned)((long)tiles * a.B * a.Hkv));
+    const dim3 grid((unsigned)((long)tiles * a.B * a.Hkv * split.splits));
     const size_t smem = sizeof(float) * (kHeld * a.d + 2 * kPass * (a.d + 4) +
                                          kHeld * kPass);
     return by_type(a, [&](auto t, auto dim) {
-        return launch_after(k_exact_fwd<decltype(t), decltype(dim)::value>,
-                            grid, kThreads, smem, st, a, tiles);
+        using T = decltype(t);
+        constexpr int D = decltype(dim)::value;
+        cudaError_t e = launch_after(k_exact_fwd<T, D>, grid, kThreads, smem,
+                                     st, a, split, tiles);
+        if (e == cudaSuccess && split.splits > 1)
+            e = launch_after(
+                k_exact_join<T, D>,
+                dim3((unsigned)((split.rows * (D / 4) + 255) / 256)), 256, 0,
+                st, a, split);
+        return e;
     });
 }
 

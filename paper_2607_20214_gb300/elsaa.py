@@ -1023,6 +1023,7 @@ def make_heads(B, H, H_kv, N, d_h, dtype="bf16", norm=True, rotary=None,
     h.rows = (B, N, H, d_h), (B, N, H_kv, d_h)
     h.out = (B, H, N, d_h), (B, kv, N, d_h)
     h.axes = h.rotary.axes
+    h.weights, h.batch = (d_h,), (B,)
     return h
 
 
@@ -1039,66 +1040,82 @@ def new_heads_workspace(heads: elsaa_heads, device) -> torch.Tensor:
                        dtype=torch.uint8, device=device)
 
 
-class _On:
+def _index(t, name):
     """The device of a call's tensors, which must be the current one."""
-
-    def __init__(self, t, name):
-        if not isinstance(t, torch.Tensor):
-            raise TypeError("%s must be a torch.Tensor" % name)
-        if not t.is_cuda:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    index = t.get_device()
+    if index != _current_device():
+        if index < 0:
             raise ValueError("%s must be a CUDA tensor" % name)
-        self.device, self.index = t.device, t.get_device()
-        if _current_device() != self.index:
-            raise ValueError("%s is on %s, which is not the current device"
-                             % (name, self.device))
+        raise ValueError("%s is on %s, which is not the current device"
+                         % (name, t.device))
+    return index
 
 
-def _whole(t, name, dtype, shape, on):
-    """Pointer of a contiguous tensor of this type and shape; None stays."""
+class _On:
+    """A device, as _own wants it."""
+
+    def __init__(self, index):
+        self.index, self.device = index, torch.device("cuda", index)
+
+
+def _whole(t, name, dtype, shape, index):
+    """Pointer of a contiguous tensor of this type and shape; None stays. (The
+    checks that pass cost least: a small call makes a dozen of them.)"""
     if t is None:
         return None
     if isinstance(t, torch.Tensor) and t.dtype is dtype and \
-            t.get_device() == on.index and t.shape == shape and \
+            t.shape == shape and t.get_device() == index and \
             t.is_contiguous():
         return t.data_ptr()
     n = 1
     for x in shape:
         n *= x
-    _ptr(t, name, dtype, n, on.device)
+    _ptr(t, name, dtype, n, torch.device("cuda", index))
     raise ValueError("%s must be %s (got %s)" % (name, list(shape),
                                                  list(t.shape)))
 
 
-def _strided(t, name, dtype, shape, on):
+def _strided(t, name, dtype, shape, index):
     """elsaa_rows of [B, N, heads, d_h], whose channels lie side by side."""
     if t is None:
         return None
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if t.get_device() != on.index:
-        raise ValueError("%s must be on %s (got %s)" % (name, on.device,
-                                                        t.device))
-    if t.dtype is not dtype:
-        raise ValueError("%s must be %s (got %s)" % (name, dtype, t.dtype))
-    if t.shape != shape:
-        raise ValueError("%s must be %s (got %s)" % (name, list(shape),
-                                                     list(t.shape)))
-    sb, sn, sh, sd = t.stride()
-    if sd != 1:
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index:
+        sb, sn, sh, sd = t.stride()
+        if sd == 1:
+            return elsaa_rows(t.data_ptr(), sb, sn, sh)
         raise ValueError("%s must have its channels side by side" % name)
-    return elsaa_rows(t.data_ptr(), sb, sn, sh)
+    if t.get_device() != index:
+        raise ValueError("%s must be on cuda:%d (got %s)" % (name, index,
+                                                            t.device))
+    raise ValueError("%s must be %s %s (got %s %s)" % (
+        name, dtype, list(shape), t.dtype, list(t.shape)))
 
 
-def _tokens(heads, positions, lengths, new_len, on):
-    """Pointers of positions, lengths, new_len."""
-    i32, B = torch.int32, (heads.B,)
-    if positions is not None:
-        shape = (heads.axes, heads.B, heads.N)
-        if heads.axes == 1 and positions.dim() == 2:
-            shape = shape[1:]
-        positions = _whole(positions, "positions", i32, shape, on)
-    return (positions, _whole(lengths, "lengths", i32, B, on),
-            _whole(new_len, "new_len", i32, B, on))
+def _raw(stream, index):
+    """cudaStream_t of `stream`, by default torch's current one."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(index)
+    return _stream_of(stream, torch.device("cuda", index))
+
+
+def _space(workspace, index):
+    """(pointer, bytes) of a workspace."""
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on cuda:%d" % index)
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def _positions(heads, positions, index):
+    if positions is None:
+        return None
+    shape = (heads.axes, heads.B, heads.N)
+    if heads.axes == 1 and positions.dim() == 2:
+        shape = shape[1:]
+    return _whole(positions, "positions", torch.int32, shape, index)
 
 
 def elsaa_heads_forward(heads: elsaa_heads, q=None, k=None, v=None, w_q=None,
@@ -1108,29 +1125,31 @@ def elsaa_heads_forward(heads: elsaa_heads, q=None, k=None, v=None, w_q=None,
     [B, N, H_kv, d_h] (strided views of a projection's output; None: not
     wanted) to normed and rotated heads. Returns (q_out, k_out, v_out),
     allocated here when not given (rows behind new_len then undefined)."""
-    first = q if q is not None else k if k is not None else v
-    on = _On(first, "q")
-    dt, f32, w = heads.torch_dtype, torch.float32, (heads.d_h,)
+    on = _index(q if q is not None else k if k is not None else v, "q")
+    dt, f32, i32 = heads.torch_dtype, torch.float32, torch.int32
+    w, B = heads.weights, heads.batch
     rq, rk = heads.rows
     oq, ok = heads.out
-    rows = (_strided(q, "q", dt, rq, on), _strided(k, "k", dt, rk, on),
-            _strided(v, "v", dt, rk, on))
+    rows_q = _strided(q, "q", dt, rq, on)
+    rows_k = _strided(k, "k", dt, rk, on)
+    rows_v = _strided(v, "v", dt, rk, on)
     if (q is not None and q_out is None) or (
             k is not None and k_out is None) or (
             v is not None and v_out is None):
-        with _own(stream, on):
+        with _own(stream, _On(on)):
             def new(x, out, shape):
                 if x is None or out is not None:
                     return out
-                return torch.empty(shape, dtype=dt, device=on.device)
+                return torch.empty(shape, dtype=dt, device=x.device)
             q_out, k_out, v_out = (new(q, q_out, oq), new(k, k_out, ok),
                                    new(v, v_out, ok))
     _check(load_library().elsaa_heads_forward(
-        heads.ref, *rows, _whole(w_q, "w_q", f32, w, on),
-        _whole(w_k, "w_k", f32, w, on),
-        *_tokens(heads, positions, lengths, new_len, on),
+        heads.ref, rows_q, rows_k, rows_v, _whole(w_q, "w_q", f32, w, on),
+        _whole(w_k, "w_k", f32, w, on), _positions(heads, positions, on),
+        _whole(lengths, "lengths", i32, B, on),
+        _whole(new_len, "new_len", i32, B, on),
         _whole(q_out, "q_out", dt, oq, on), _whole(k_out, "k_out", dt, ok, on),
-        _whole(v_out, "v_out", dt, ok, on), _stream_of(stream, on.device)))
+        _whole(v_out, "v_out", dt, ok, on), _raw(stream, on)))
     return q_out, k_out, v_out
 
 
@@ -1144,10 +1163,9 @@ def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
     dw_k): the rows of the gradients given, allocated here when not given
     (rows behind new_len then undefined); dw_q and dw_k likewise where the
     weights are given."""
-    first = dq if dq is not None else dk if dk is not None else dv
-    on = _On(first, "dq")
+    on = _index(dq if dq is not None else dk if dk is not None else dv, "dq")
     dt, gt, f32 = heads.torch_dtype, heads.grad_dtype, torch.float32
-    w = (heads.d_h,)
+    i32, w, B = torch.int32, heads.weights, heads.batch
     rq, rk = heads.rows
     oq, ok = heads.out
     if w_q is not None and dw_q is None and dq is not None or \
@@ -1156,11 +1174,12 @@ def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
             dk is not None and dk_rows is None or \
             dv is not None and dv_rows is None or \
             workspace is None and not (dw_q is None and dw_k is None):
-        with _own(stream, on):
+        own = _On(on)
+        with _own(stream, own):
             def new(x, out, shape, t):
                 if x is None or out is not None:
                     return out
-                return torch.empty(shape, dtype=t, device=on.device)
+                return torch.empty(shape, dtype=t, device=own.device)
             dq_rows, dk_rows, dv_rows = (
                 new(dq, dq_rows, rq, dt), new(dk, dk_rows, rk, dt),
                 new(dv, dv_rows, rk, dt))
@@ -1169,19 +1188,20 @@ def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
             if dk is not None:
                 dw_k = new(w_k, dw_k, w, f32)
             if workspace is None:
-                workspace = new_heads_workspace(heads, on.device)
-    ws, nbytes = (None, 0) if workspace is None else _scratch(workspace, on)
+                workspace = new_heads_workspace(heads, own.device)
+    ws, nbytes = (None, 0) if workspace is None else _space(workspace, on)
     _check(load_library().elsaa_heads_backward(
         heads.ref, _whole(dq, "dq", gt, oq, on), _whole(dk, "dk", gt, ok, on),
         _whole(dv, "dv", gt, ok, on), _strided(q, "q", dt, rq, on),
         _strided(k, "k", dt, rk, on), _whole(w_q, "w_q", f32, w, on),
-        _whole(w_k, "w_k", f32, w, on),
-        *_tokens(heads, positions, lengths, new_len, on),
+        _whole(w_k, "w_k", f32, w, on), _positions(heads, positions, on),
+        _whole(lengths, "lengths", i32, B, on),
+        _whole(new_len, "new_len", i32, B, on),
         _strided(dq_rows, "dq_rows", dt, rq, on),
         _strided(dk_rows, "dk_rows", dt, rk, on),
         _strided(dv_rows, "dv_rows", dt, rk, on),
         _whole(dw_q, "dw_q", f32, w, on), _whole(dw_k, "dw_k", f32, w, on),
-        ws, nbytes, _stream_of(stream, on.device)))
+        ws, nbytes, _raw(stream, on)))
     return dq_rows, dk_rows, dv_rows, dw_q, dw_k
 
 
@@ -1195,6 +1215,7 @@ def make_exact(B, H, H_kv, N_q, N_k, d_h, dtype="bf16", causal=False,
     e.ref = ctypes.byref(e)
     e.torch_dtype = _torch_dtype(code)
     e.q, e.kv, e.rows = ((B, H, N_q, d_h), (B, H_kv, N_k, d_h), (B, H, N_q))
+    e.batch = (B,)
     return e
 
 
@@ -1218,22 +1239,23 @@ def elsaa_exact_forward(exact: elsaa_exact, q, k, v, q_len=None, k_len=None,
     """Enqueue elsaa_exact_forward: q [B, H, N_q, d_h] over k, v
     [B, H_kv, N_k, d_h]. Returns o (allocated here when not given, rows behind
     q_len then undefined); lse [B, H, N_q] fp32 is written when given."""
-    on = _On(q, "q")
-    dt, i32, B = exact.torch_dtype, torch.int32, (exact.B,)
+    on = _index(q, "q")
+    dt, i32, B = exact.torch_dtype, torch.int32, exact.batch
     if o is None or workspace is None:
-        with _own(stream, on):
+        own = _On(on)
+        with _own(stream, own):
             if o is None:
-                o = torch.empty(exact.q, dtype=dt, device=on.device)
+                o = torch.empty(exact.q, dtype=dt, device=own.device)
             if workspace is None:
-                workspace = new_exact_workspace(exact, on.device)
-    ws, nbytes = _scratch(workspace, on)
+                workspace = new_exact_workspace(exact, own.device)
+    ws, nbytes = _space(workspace, on)
     _check(load_library().elsaa_exact_forward(
         exact.ref, _whole(q, "q", dt, exact.q, on),
         _whole(k, "k", dt, exact.kv, on), _whole(v, "v", dt, exact.kv, on),
         _whole(q_len, "q_len", i32, B, on), _whole(k_len, "k_len", i32, B, on),
         _whole(o, "o", dt, exact.q, on),
         _whole(lse, "lse", torch.float32, exact.rows, on), ws, nbytes,
-        _stream_of(stream, on.device)))
+        _raw(stream, on)))
     return o
 
 
@@ -1243,18 +1265,19 @@ def elsaa_exact_backward(exact: elsaa_exact, q, k, v, o, lse, d_o, q_len=None,
     """Enqueue elsaa_exact_backward: the gradients of q, k and v from d_o, with
     o and lse of elsaa_exact_forward. Returns (dq, dk, dv), allocated here when
     not given (rows behind q_len and k_len then undefined)."""
-    on = _On(q, "q")
-    dt, i32, B = exact.torch_dtype, torch.int32, (exact.B,)
+    on = _index(q, "q")
+    dt, i32, B = exact.torch_dtype, torch.int32, exact.batch
     if dq is None or dk is None or dv is None or workspace is None:
-        with _own(stream, on):
+        own = _On(on)
+        with _own(stream, own):
             def new(out, shape):
                 return out if out is not None else torch.empty(
-                    shape, dtype=dt, device=on.device)
+                    shape, dtype=dt, device=own.device)
             dq, dk, dv = (new(dq, exact.q), new(dk, exact.kv),
                           new(dv, exact.kv))
             if workspace is None:
-                workspace = new_exact_workspace(exact, on.device, True)
-    ws, nbytes = _scratch(workspace, on)
+                workspace = new_exact_workspace(exact, own.device, True)
+    ws, nbytes = _space(workspace, on)
     _check(load_library().elsaa_exact_backward(
         exact.ref, _whole(q, "q", dt, exact.q, on),
         _whole(k, "k", dt, exact.kv, on), _whole(v, "v", dt, exact.kv, on),
@@ -1264,5 +1287,5 @@ def elsaa_exact_backward(exact: elsaa_exact, q, k, v, o, lse, d_o, q_len=None,
         _whole(q_len, "q_len", i32, B, on), _whole(k_len, "k_len", i32, B, on),
         _whole(dq, "dq", dt, exact.q, on), _whole(dk, "dk", dt, exact.kv, on),
         _whole(dv, "dv", dt, exact.kv, on), ws, nbytes,
-        _stream_of(stream, on.device)))
+        _raw(stream, on)))
     return dq, dk, dv
