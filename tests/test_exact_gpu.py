@@ -346,3 +346,60 @@ def test_shares(B, H, Hkv, Nq, Nk, kl):
     run_case(B, H, Hkv, Nq, Nk, 64, BF, 1, ql=[Nq] * B, kl=kl, backward=False)
     run_case(B, H, Hkv, Nq, Nk, 64, BF, 0, ql=[(i % 2) * Nq for i in range(B)],
              kl=kl, backward=False)
+
+
+def test_offsets_past_32_bits():
+    """K and V of more than 2^31 elements each: the last head's rows."""
+    Hkv, Nk, d = 16, 1_060_000, 128
+    k = torch.zeros((1, Hkv, Nk, d), dtype=BF, device="cuda")
+    v = torch.zeros_like(k)
+    assert k.numel() > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(0)
+    at = torch.randint(0, Nk, (3000,), generator=g, device="cuda").unique()
+    k[0, -1, at] = torch.randn(len(at), d, generator=g, device="cuda").to(BF)
+    v[0, -1, at] = torch.randn(len(at), d, generator=g, device="cuda").to(BF)
+    q = (4 * torch.randn(1, Hkv, 2, d, generator=g, device="cuda")).to(BF)
+    ex = E.make_exact(1, Hkv, Hkv, 2, Nk, d)
+    lse = torch.empty((1, Hkv, 2), device="cuda")
+    o = E.elsaa_exact_forward(ex, q, k, v, lse=lse)
+    s = (q[0, -1].double() @ k[0, -1, at].double().t()) / math.sqrt(d)
+    e = torch.exp(s)
+    total = e.sum(1) + Nk - len(at)  # the other scores are 0
+    want = (e @ v[0, -1, at].double()) / total[:, None]
+    mag = (e @ v[0, -1, at].double().abs()) / total[:, None]
+    # weights and result rounded to bf16, sums over a million terms in fp32 of
+    # which each CTA adds at most a few thousand in a row
+    tol = 2.0 ** -8 * (mag + want.abs()) + 2.0 ** -10 * mag
+    assert bool(((o[0, -1].double() - want).abs() <= tol).all())
+    assert bool(((lse[0, -1].double() - torch.log(total)).abs() < 1e-3).all())
+    assert not o[0, :-1].any()
+
+
+def test_another_current_device_is_refused(monkeypatch):
+    q, k, v, _ = (x.cuda() for x in C.exact_inputs(1, 1, 1, 8, 8, 64, BF))
+    ex = E.make_exact(1, 1, 1, 8, 8, 64)
+    monkeypatch.setattr(E, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        E.elsaa_exact_forward(ex, q, k, v)
+
+
+def test_backward_of_one_leaf_in_a_graph_beside_an_eager_one():
+    """torch's graph of the leaves lives while the calls are captured."""
+    q, k, v, do = (x.cuda() for x in C.exact_inputs(1, 2, 1, 96, 96, 64, BF))
+    leaf = q.clone().requires_grad_()
+    eager = (leaf.float() ** 2).sum()
+    ex = E.make_exact(1, 2, 1, 96, 96, 64, causal=True)
+    ws = E.new_exact_workspace(ex, "cuda", backward=True)
+    lse = torch.empty((1, 2, 96), device="cuda")
+    x = leaf.detach()
+    o = E.elsaa_exact_forward(ex, x, k, v, lse=lse, workspace=ws)
+    want = E.elsaa_exact_backward(ex, x, k, v, o, lse, do, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = E.elsaa_exact_backward(ex, x, k, v, o, lse, do, workspace=ws)
+    graph.replay()
+    eager.backward()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(leaf.grad, (2 * q.float()).to(BF))

@@ -339,3 +339,22 @@ def test_argument_checks():
     with pytest.raises(E.ElsaaError):
         E.elsaa_heads_backward(h, torch.zeros(1, 2, 8, 64, device="cuda",
                                               dtype=BF))
+
+
+def test_offsets_past_32_bits():
+    """Rows of more than 2^31 elements: the last tokens against a call of
+    their own."""
+    H, N, d = 256, 66_000, 128
+    h = E.make_heads(1, H, H, N, d, rotary=E.make_rotary(d))
+    g = torch.Generator(device="cuda").manual_seed(0)
+    q = torch.randint(-100, 100, (1, N, H, d), generator=g, device="cuda",
+                      dtype=torch.int8).to(BF)
+    assert q.numel() > 2 ** 31
+    o = E.elsaa_heads_forward(h, q)[0]
+    few = E.make_heads(1, H, H, 5, d, rotary=E.make_rotary(d))
+    pos = torch.arange(N - 5, N, dtype=torch.int32, device="cuda")[None]
+    want = E.elsaa_heads_forward(few, q[:, -5:], positions=pos)[0]
+    assert torch.equal(o[:, :, -5:], want)
+    rows = E.elsaa_heads_backward(h, o, q=q)[0]
+    part = E.elsaa_heads_backward(few, want, q=q[:, -5:], positions=pos)[0]
+    assert torch.equal(rows[:, -5:], part)
