@@ -90,13 +90,17 @@ size_t exact_share_bytes(const ExactView &a);
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
                                 float *part, cudaStream_t st);
 // Its backward pass: D_i first (which also clears the status and two work
-// counters), then dQ, and dK with dV.
+// counters), then dQ, and dK with dV, and the sums of walks that were divided.
+// part: exact_part_bytes(a) of scratch, 256-byte aligned.
+size_t exact_part_bytes(const ExactView &a);
 cudaError_t launch_exact_delta(const ExactView &a, int *counters,
                                cudaStream_t st);
 cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
-                               cudaStream_t st);
+                               float *part, cudaStream_t st);
 cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
-                                cudaStream_t st);
+                                float *part, cudaStream_t st);
+cudaError_t launch_exact_sum(const ExactView &a, float *part,
+                             cudaStream_t st);
 // CUDA cores (fp32, and bf16 with impl = SIMT)
 // part: exact_chunk_bytes(a) of scratch
 size_t exact_chunk_bytes(const ExactView &a);

@@ -68,9 +68,10 @@ bool on_tensor_cores(const elsaa_exact *p) {
     return p->dtype == ELSAA_BF16 && p->impl == ELSAA_IMPL_AUTO;
 }
 
-// status and two work counters | D_i, or what CTAs leave of divided rows
+// status and two work counters | D_i, or what CTAs leave of divided rows | the
+// same of the backward pass
 struct Layout {
-    size_t next_item, scratch, total;
+    size_t next_item, scratch, part, total;
 };
 Layout layout(const ExactView &a, bool tensor, bool backward) {
     Layout l;
@@ -79,7 +80,8 @@ Layout layout(const ExactView &a, bool tensor, bool backward) {
     size_t most = tensor ? exact_share_bytes(a) : exact_chunk_bytes(a);
     const size_t delta = sizeof(float) * (size_t)a.B * a.H * a.Nq;
     if (backward && delta > most) most = delta;
-    l.total = l.scratch + align256(most);
+    l.part = l.total = l.scratch + align256(most);
+    if (backward && tensor) l.total += align256(exact_part_bytes(a));
     return l;
 }
 
@@ -185,10 +187,12 @@ extern "C" int elsaa_exact_backward(
         int *next_item = (int *)((char *)workspace + l.next_item);
         ELSAA_EXACT_LAUNCH("exact_delta", st,
                            launch_exact_delta(a, next_item, st));
+        float *part = (float *)((char *)workspace + l.part);
         ELSAA_EXACT_LAUNCH("exact_dq_tc", st,
-                           launch_exact_dq_tc(a, next_item, st));
+                           launch_exact_dq_tc(a, next_item, part, st));
         ELSAA_EXACT_LAUNCH("exact_dkv_tc", st,
-                           launch_exact_dkv_tc(a, next_item + 1, st));
+                           launch_exact_dkv_tc(a, next_item + 1, part, st));
+        ELSAA_EXACT_LAUNCH("exact_sum", st, launch_exact_sum(a, part, st));
         return ELSAA_OK;
     }
     ELSAA_EXACT_LAUNCH("exact_dq_simt", st,

@@ -6,7 +6,9 @@
 // holds 128 query rows and walks the keys, k_exact_dkv_tc holds 128 keys and
 // walks the query rows of every head that reads them. That is seven products
 // instead of five, but every sum stays in tensor memory, in one order: no fp32
-// dQ in memory, no atomics, the same bits on every call.
+// dQ in memory, no atomics, the same bits on every call. With fewer items than
+// places for CTAs the walks are divided too, and k_exact_sum adds up, in order,
+// what the parts leave.
 #include <type_traits>
 
 #include "device_common.cuh"
@@ -153,6 +155,23 @@ __device__ __forceinline__ void store_zeros(uint16_t *o) {
         *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
 }
 
+// The same columns as they are.
+template <int D>
+__device__ __forceinline__ void store_part(uint32_t t, float *o) {
+#pragma unroll
+    for (int c = 0; c < Eb<D>::out; c += 16) {
+        uint32_t x[16], y[8];
+        tmem_ld16(t + c, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = x[h + e];
+            st_global_v8(o + c + h, y);
+        }
+    }
+}
+
 // D_i = <dO_i, O_i>, D / 8 lanes a row; clears the status and two counters.
 template <int D>
 __global__ void __launch_bounds__(256)
@@ -209,7 +228,32 @@ struct BwdItem {
     int ql, kl;
     int n;     // tiles to walk
     int first; // keys held: the first query row that sees one
+    int t0;    // the first tile of the walk
+    int part;  // where a divided walk's sums go, -1: the walk is whole
+    int rest;  // 1: a part of nothing, whose item others write
 };
+
+// Walks of n tiles in at most `splits` parts of kEbLeast tiles and more. Part p
+// of item i of the call leaves its sums in o[i splits + p][128][D] (keys: dK,
+// then dV, [2][128][D]).
+constexpr int kEbLeast = 4;
+struct EbSplit {
+    int splits;
+    float *o;
+};
+__device__ __forceinline__ int parts_of(const EbSplit &s, int n) {
+    return min(s.splits, max(1, n / kEbLeast));
+}
+// Part p of a walk: sets t0, n, part and rest.
+__device__ __forceinline__ void take_part(const EbSplit &s, int p, int index,
+                                          BwdItem &w) {
+    const int parts = parts_of(s, w.n);
+    w.rest = p >= parts;
+    const int end = w.rest ? 0 : (int)((long)w.n * (p + 1) / parts);
+    w.t0 = w.rest ? 0 : (int)((long)w.n * p / parts);
+    w.part = parts > 1 ? index * s.splits + p : -1;
+    w.n = end - w.t0;
+}
 
 // A CTA holds Q and dO of 128 rows (of the heads that share a K/V head,
 // counted through) and walks key tiles. The first warps make the weights; then
@@ -222,7 +266,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                   const __grid_constant__ CUtensorMap tmK,
                   const __grid_constant__ CUtensorMap tmV,
                   const __grid_constant__ ExactView a,
-                  const __grid_constant__ ExactOrder order, int items,
+                  const __grid_constant__ ExactOrder order,
+                  const __grid_constant__ EbSplit split, int items,
                   int *__restrict__ next_item) {
     wait_for_stream();
     extern __shared__ unsigned char smem_raw[];
@@ -297,7 +342,9 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                     // the last rows of every query head, which see most, first
                     const int h = (int)(item % heads);
                     w.item = (int)item;
-                    w.r0 = order.tile((int)(item / heads)) * 128;
+                    const int x = order.tile((int)(item / heads) /
+                                             split.splits);
+                    w.r0 = x * 128;
                     w.b = h / a.Hkv;
                     w.kvh = h - w.b * a.Hkv;
                     const ExactSeq seq(a, w.b);
@@ -305,6 +352,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                     w.kl = seq.kl;
                     w.n = (exact_most(seq, w.r0, min(w.r0 + 128, rows),
                                       order.pitch) + E::rows - 1) / E::rows;
+                    take_part(split, (int)(item / heads) % split.splits,
+                              h * order.groups * order.per + x, w);
                 }
                 item_s[it & 1] = w;
                 mbar_arrive(&bars.item_full[it & 1]);
@@ -316,7 +365,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                 ++qs;
                 const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq +
                                order.row(w.r0, a.Nq);
-                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
+                const int k0 =
+                    (w.b * a.Hkv + w.kvh) * a.Nk + E::rows * w.t0;
                 mbar_expect_tx(&bars.q_full, 2 * E::held);
                 tile(&bars.q_full, sQ, &tmQ, q0, 128);
                 tile(&bars.q_full, sG, &tmG, q0, 128);
@@ -343,7 +393,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                 const BwdItem w = item_s[it & 1];
                 mbar_arrive(&bars.item_empty[it & 1]);
                 if (w.item < 0) break;
-                const int k0 = (w.b * a.Hkv + w.kvh) * a.Nk;
+                const int k0 =
+                    (w.b * a.Hkv + w.kvh) * a.Nk + E::rows * w.t0;
                 for (int kt = 0; kt < w.n; ++kt, ++c) {
                     const int vs = c % kV;
                     if (c >= kV &&
@@ -379,7 +430,9 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
             for (int it = 0; ok; ++it) {
                 if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 424)) break;
                 const int item = item_s[it & 1].item, n = item_s[it & 1].n;
-                const int kl = item_s[it & 1].kl;
+                // keys of the sequence from the walk's first tile on
+                const int kl =
+                    item_s[it & 1].kl - E::rows * item_s[it & 1].t0;
                 __syncwarp();
                 if (el) mbar_arrive(&bars.item_empty[it & 1]);
                 if (item < 0) break;
@@ -467,7 +520,7 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                               order.row(r, a.Nq);
             uint16_t *o = (uint16_t *)a.dq + at * D + E::out * part;
             if (w.n == 0) {
-                if (valid) store_zeros<D>(o);
+                if (valid && !w.rest) store_zeros<D>(o);
                 continue;
             }
             int seen = 0;
@@ -503,7 +556,7 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
 #pragma unroll
                 for (int q = 0; q < 16; ++q)
                     g[q] = mul2(p[q], add2(g[q], nd2));
-                const int lim = seen - E::rows * j - 32 * part;
+                const int lim = seen - E::rows * (w.t0 + j) - 32 * part;
                 if (__any_sync(0xffffffffu, lim < 32)) {
 #pragma unroll
                     for (int q = 0; q < 16; ++q) {
@@ -518,7 +571,12 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                 break;
             ++qs;
             tc_fence_after();
-            store_sums<D>(tm + lane + kO + E::out * part, a.scale, o, valid);
+            const uint32_t to = tm + lane + kO + E::out * part;
+            if (w.part >= 0)
+                store_part<D>(to, split.o + ((size_t)w.part * 128 + row) * D +
+                                      E::out * part);
+            else
+                store_sums<D>(to, a.scale, o, valid);
             tc_fence_before();
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.dq_empty);
@@ -570,7 +628,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                    const __grid_constant__ CUtensorMap tmG,
                    const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV,
-                   const __grid_constant__ ExactView a, int items,
+                   const __grid_constant__ ExactView a,
+                   const __grid_constant__ EbSplit split, int items,
                    int *__restrict__ next_item) {
     wait_for_stream();
     using X = Dkv<D>;
@@ -656,7 +715,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                     // the first keys, which are seen most, first
                     const int h = (int)(item % heads);
                     w.item = (int)item;
-                    w.r0 = (int)(item / heads) * 128;
+                    const int x = (int)(item / heads) / split.splits;
+                    w.r0 = x * 128;
                     w.b = h / a.Hkv;
                     w.kvh = h - w.b * a.Hkv;
                     const ExactSeq seq(a, w.b);
@@ -664,6 +724,8 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                     w.kl = seq.kl;
                     w.first = seq.first_row(w.r0);
                     w.n = a.G * tiles_of(w);
+                    take_part(split, (int)(item / heads) % split.splits,
+                              h * ((a.Nk + 127) / 128) + x, w);
                 }
                 item_s[it & 1] = w;
                 mbar_arrive(&bars.item_full[it & 1]);
@@ -678,19 +740,25 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                 mbar_expect_tx(&bars.kv_full, 2 * E::held);
                 tile(&bars.kv_full, sK, &tmK, k0, 128);
                 tile(&bars.kv_full, sV, &tmV, k0, 128);
-                const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
-                for (int g = 0; g < a.G && ok; ++g)
-                    for (int i = w.first; i < w.ql; i += E::rows, ++c) {
-                        const int qs = c % X::kQ;
-                        if (c >= X::kQ &&
-                            !(ok = mbar_wait_or_abort(&bars.q_empty[qs],
-                                                      (c / X::kQ - 1) & 1,
-                                                      abort, status, 442)))
-                            break;
-                        mbar_expect_tx(&bars.q_full[qs], kTile);
-                        tile(&bars.q_full[qs], sQ + qs * kTile, &tmQ,
-                             q0 + g * a.Nq + i, E::rows);
+                const int per = tiles_of(w);
+                int head = (w.b * a.H + w.kvh * a.G + w.t0 / per) * a.Nq;
+                int i = w.first + w.t0 % per * E::rows;
+                for (int t = 0; t < w.n; ++t, ++c) {
+                    const int qs = c % X::kQ;
+                    if (c >= X::kQ &&
+                        !(ok = mbar_wait_or_abort(&bars.q_empty[qs],
+                                                  (c / X::kQ - 1) & 1, abort,
+                                                  status, 442)))
+                        break;
+                    mbar_expect_tx(&bars.q_full[qs], kTile);
+                    tile(&bars.q_full[qs], sQ + qs * kTile, &tmQ, head + i,
+                         E::rows);
+                    i += E::rows;
+                    if (i >= w.ql) {
+                        i = w.first;
+                        head += a.Nq;
                     }
+                }
             }
         } else if (warp == E::weights) {
             // ---------------------------------------------------- MMA issue
@@ -725,11 +793,14 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                 // 0 and must be numbers: rows of the next Q or dO tile that
                 // it has.
                 const int all = item_s[it & 1].ql - item_s[it & 1].first;
+                const int t0 = item_s[it & 1].t0;
                 __syncwarp();
                 if (el) mbar_arrive(&bars.item_empty[it & 1]);
                 if (item < 0) break;
                 if (n == 0) continue;
-                int left_q = all, left_g = all;
+                int left_q =
+                    all - t0 % ((all + E::rows - 1) / E::rows) * E::rows;
+                int left_g = left_q;
                 // the tile of S(t) or dP(t) is there
                 auto scores = [&](int t) {
                     const int x = c + t, qs = x % X::kQ;
@@ -809,7 +880,10 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                 __syncwarp();
                 if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
                 if (w.item < 0) break;
-                int head = (w.b * a.H + w.kvh * a.G) * a.Nq, i0 = w.first;
+                if (w.n == 0) continue;
+                const int per = tiles_of(w);
+                int head = (w.b * a.H + w.kvh * a.G + w.t0 / per) * a.Nq;
+                int i0 = w.first + w.t0 % per * E::rows;
                 for (int t = 0; t < w.n; ++t, ++c) {
                     const int gs = c % X::kG;
                     const size_t at = (size_t)head + i0;
@@ -878,7 +952,7 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                               E::out * part;
             uint16_t *ok_ = (uint16_t *)a.dk + at, *ov = (uint16_t *)a.dv + at;
             if (w.n == 0) {
-                if (valid) {
+                if (valid && !w.rest) {
                     store_zeros<D>(ok_);
                     store_zeros<D>(ov);
                 }
@@ -890,7 +964,9 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                                          : 0;
             const int lo0 = first - w.first - 32 * part;
             const int hi0 = w.ql - w.first - 32 * part;
-            int lo = lo0, hi = hi0;  // columns of this part that see the key
+            const int skip = w.t0 % tiles_of(w) * E::rows;
+            // columns of this part that see the key
+            int lo = lo0 - skip, hi = hi0 - skip;
             for (int t = 0; t < w.n; ++t, ++c) {
                 const bool edge = __any_sync(0xffffffffu, lo > 0 || hi < 32);
                 if (!(ok = warp_wait(&bars.s_full[c & 1], c / 2 & 1, abort,
@@ -955,8 +1031,15 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
             ++ks;
             tc_fence_after();
             const uint32_t t = tm + lane + E::out * part;
-            store_sums<D>(t + X::cV, 1.0f, ov, valid);
-            store_sums<D>(t + X::cK, a.scale, ok_, valid);
+            if (w.part >= 0) {
+                float *o = split.o + ((size_t)w.part * 256 + row) * D +
+                           E::out * part;
+                store_part<D>(t + X::cK, o);
+                store_part<D>(t + X::cV, o + 128 * D);
+            } else {
+                store_sums<D>(t + X::cV, 1.0f, ov, valid);
+                store_sums<D>(t + X::cK, a.scale, ok_, valid);
+            }
             tc_fence_before();
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.sum_empty);
@@ -965,6 +1048,74 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
     tc_fence_before();
     __syncthreads();
     if (warp == E::weights) tmem_dealloc(tm, E::columns);
+}
+
+// The sums of walks that were divided: rows of dQ, then of dK and dV, D / 8
+// lanes a row.
+template <int D>
+__global__ void __launch_bounds__(256)
+    k_exact_sum(const __grid_constant__ ExactView a,
+                const __grid_constant__ ExactOrder order,
+                const __grid_constant__ EbSplit sq,
+                const __grid_constant__ EbSplit sk) {
+    wait_for_stream();
+    using E = Eb<D>;
+    constexpr int L = D / 8;
+    long row = ((long)blockIdx.x * 256 + threadIdx.x) / L;
+    const int c = threadIdx.x % L * 8;
+    const long nq = sq.splits > 1 ? (long)a.B * a.H * a.Nq : 0;
+    const bool keys = row >= nq;
+    const float *from;
+    size_t step;
+    int parts;
+    uint16_t *to;
+    if (!keys) {
+        const int group = a.G * a.Nq, head = (int)(row / group);
+        const int x = (int)(row % group), i = x % a.Nq;
+        const ExactSeq seq(a, head / a.Hkv);
+        if (i >= seq.ql) return;
+        const int r = x / a.Nq * order.pitch + i, r0 = r / 128 * 128;
+        const int n = (exact_most(seq, r0, min(r0 + 128, order.rows),
+                                  order.pitch) + E::rows - 1) / E::rows;
+        parts = parts_of(sq, n);
+        const size_t index = (size_t)head * order.groups * order.per + r / 128;
+        from = sq.o + (index * sq.splits * 128 + (r - r0)) * D + c;
+        step = 128 * D;
+        to = (uint16_t *)a.dq + row * D + c;
+    } else {
+        row -= nq;
+        if (sk.splits == 1 || row >= (long)a.B * a.Hkv * a.Nk) return;
+        const int head = (int)(row / a.Nk), j = (int)(row % a.Nk);
+        const ExactSeq seq(a, head / a.Hkv);
+        if (j >= seq.kl) return;
+        const int r0 = j / 128 * 128;
+        const int n =
+            a.G * ((seq.ql - seq.first_row(r0) + E::rows - 1) / E::rows);
+        parts = parts_of(sk, n);
+        const size_t index = (size_t)head * ((a.Nk + 127) / 128) + j / 128;
+        from = sk.o + (index * sk.splits * 256 + (j - r0)) * D + c;
+        step = 256 * D;
+        to = (uint16_t *)a.dk + row * D + c;
+    }
+    if (parts == 1) return;
+    for (int which = 0; which < (keys ? 2 : 1); ++which) {
+        float x[8] = {};
+        for (int p = 0; p < parts; ++p) {
+            const float4 *y = reinterpret_cast<const float4 *>(
+                from + p * step + which * 128 * D);
+            const float4 u = y[0], v = y[1];
+            const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] += e[i];
+        }
+        const float f = which ? 1.0f : a.scale;
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = pack_bf16x2(x[2 * i] * f, x[2 * i + 1] * f);
+        if (which) to = (uint16_t *)a.dv + row * D + c;
+        *reinterpret_cast<uint4 *>(to) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
 }
 
 struct Maps {
@@ -1005,10 +1156,69 @@ cudaError_t launch_exact_delta(const ExactView &a, int *counters,
     });
 }
 
+namespace {
+
+// Parts of a walk of at most n tiles: one and a half for each place for a CTA (a
+// GB300 has 152 SMs) when the items fill less than half of them; two of long
+// walks when there are fewer items than places, since with causal = 1 the
+// longest walk is twice the average. Otherwise none, as what parts leave is
+// written and read again. B1 H8 H_kv1 N2048 d64 (16 items of dK, dV): the
+// backward pass takes 60 us, undivided 238; B64 H8 H_kv2 N256 d64 (256 items,
+// walks of 16 tiles) 52 undivided, 69 in three parts. (By the sizes alone: the
+// workspace does not depend on the device.)
+int divide_walks(long items, long n, int d) {
+    const long places = 152 * (d > 64 ? 1 : 2);
+    long parts = 1;
+    if (items < places / 2)
+        parts = (places * 3 / 2 + items - 1) / items;
+    else if (items < places && n >= 32)
+        parts = 2;
+    if (parts > n / kEbLeast) parts = n / kEbLeast;
+    return parts < 1 ? 1 : (int)parts;
+}
+// of the walks over keys (dQ) and over query rows (dK, dV)
+int query_parts(const ExactView &a) {
+    const int rows = a.d > 64 ? 128 : 64;
+    return divide_walks(ExactOrder(a, 128).items(a),
+                        ((long)a.Nk + rows - 1) / rows, a.d);
+}
+long key_items(const ExactView &a) {
+    return (long)((a.Nk + 127) / 128) * a.B * a.Hkv;
+}
+int key_parts(const ExactView &a) {
+    const int rows = a.d > 64 ? 128 : 64;
+    return divide_walks(key_items(a), a.G * (((long)a.Nq + rows - 1) / rows),
+                        a.d);
+}
+// Floats that the parts of dQ and of dK, dV leave.
+void part_floats(const ExactView &a, size_t *q, size_t *k) {
+    const long nq = ExactOrder(a, 128).items(a), nk = key_items(a);
+    const int sq = query_parts(a), sk = key_parts(a);
+    *q = sq > 1 ? (size_t)nq * sq * 128 * a.d : 0;
+    *k = sk > 1 ? (size_t)nk * sk * 256 * a.d : 0;
+}
+EbSplit query_split(const ExactView &a, float *part) {
+    return EbSplit{query_parts(a), part};
+}
+EbSplit key_split(const ExactView &a, float *part) {
+    size_t q, k;
+    part_floats(a, &q, &k);
+    return EbSplit{key_parts(a), part + q};
+}
+
+}  // namespace
+
+size_t exact_part_bytes(const ExactView &a) {
+    size_t q, k;
+    part_floats(a, &q, &k);
+    return sizeof(float) * (q + k);
+}
+
 cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
-                               cudaStream_t st) {
+                               float *part, cudaStream_t st) {
     const ExactOrder order(a, 128);
-    const long items = order.items(a);
+    const EbSplit split = query_split(a, part);
+    const long items = order.items(a) * split.splits;
     return by_width(a.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         using E = Eb<D>;
@@ -1020,14 +1230,15 @@ cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
             1024 + 2 * E::held + (size_t)(kDqK<D> + kDqV<D>) * E::tile;
         return launch_after(
             k_exact_dq_tc<D>, dim3((unsigned)(items < most ? items : most)),
-            E::threads, smem, st, m.q, m.g, m.k, m.v, a, order, (int)items,
-            next_item);
+            E::threads, smem, st, m.q, m.g, m.k, m.v, a, order, split,
+            (int)items, next_item);
     });
 }
 
 cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
-                                cudaStream_t st) {
-    const long items = (long)((a.Nk + 127) / 128) * a.B * a.Hkv;
+                                float *part, cudaStream_t st) {
+    const EbSplit split = key_split(a, part);
+    const long items = key_items(a) * split.splits;
     return by_width(a.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         using E = Eb<D>;
@@ -1041,8 +1252,22 @@ cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
         static_assert(smem <= 232448, "shared memory of a CTA");
         return launch_after(
             k_exact_dkv_tc<D>, dim3((unsigned)(items < most ? items : most)),
-            E::threads, smem, st, m.q, m.g, m.k, m.v, a, (int)items,
+            E::threads, smem, st, m.q, m.g, m.k, m.v, a, split, (int)items,
             next_item);
+    });
+}
+
+cudaError_t launch_exact_sum(const ExactView &a, float *part,
+                             cudaStream_t st) {
+    const EbSplit sq = query_split(a, part), sk = key_split(a, part);
+    long rows = sq.splits > 1 ? (long)a.B * a.H * a.Nq : 0;
+    if (sk.splits > 1) rows += (long)a.B * a.Hkv * a.Nk;
+    if (rows == 0) return cudaSuccess;
+    const long threads = rows * (a.d / 8);
+    return by_width(a.d, [&](auto dim) {
+        return launch_after(k_exact_sum<decltype(dim)::value>,
+                            dim3((unsigned)((threads + 255) / 256)), 256, 0,
+                            st, a, ExactOrder(a, 128), sq, sk);
     });
 }
 

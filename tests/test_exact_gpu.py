@@ -403,3 +403,13 @@ def test_backward_of_one_leaf_in_a_graph_beside_an_eager_one():
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.equal(leaf.grad, (2 * q.float()).to(BF))
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,causal,ql,kl", [
+    (1, 8, 1, 260, 1300, 0, None, None), (1, 8, 1, 600, 600, 1, None, None),
+    (2, 4, 2, 333, 1100, 1, [333, 200], [1100, 900]),
+    (3, 6, 1, 300, 1024, 0, [300, 0, 129], [1, 1024, 0])])
+def test_divided_walks(B, H, Hkv, Nq, Nk, causal, ql, kl, d):
+    """Few items: the sums of the backward pass are divided and added up."""
+    run_case(B, H, Hkv, Nq, Nk, d, BF, causal, ql=ql, kl=kl)
