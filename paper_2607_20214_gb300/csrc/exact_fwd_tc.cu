@@ -8,8 +8,9 @@
 //   warps 0-3, 4-7  softmax of slot 0 / 1: one thread per query row holds all
 //                   128 scores of a key tile in registers, so neither the row
 //                   maximum nor the sum needs another thread
-//   warp 8          issues every MMA: S = Q K^T, O += P V (P from TMEM)
-//   warp 9          takes the items, TMA loads of Q and K; warp 10 loads V
+//   warp 8          issues the products: S = Q K^T, O += P V (P from TMEM); for
+//                   D <= 64 those of slot 0, and warp 9 those of slot 1
+//   warp 10         takes the items, TMA loads of Q and K; warp 11 loads V
 // With few items every CTA gets an equal share of all key tiles instead, in
 // order, and k_exact_merge joins what the CTAs of a divided item leave.
 // TMEM: S_s at 128 s, O_s at 256 + 128 s, P_s behind O_s for D <= 64, over S_s
@@ -39,6 +40,13 @@ static_assert(256 * kEfRegsSoft + 128 * kEfRegsOther <= kEfThreads * 168,
 // too. Rescaling for every new maximum: 753 us instead of 710 (B1 H16 H_kv4
 // N16384 d128 causal), since among 32 rows there is one in nearly every tile.
 constexpr float kGrown = 8.0f;
+// Scores go ahead of the last tile's P V product, as soon as the softmax has
+// read the scores before them, where they do not lie over P; each slot's
+// products then have a warp of their own. B4 H12 N4096 d64 causal: 125 us
+// without, 114 with. (At D = 128 two warps let the slots' products run mixed,
+// each of them later: B1 H16 H_kv4 N16384 735 us instead of 703.)
+template <int D>
+constexpr bool kEfAhead = D <= 64;
 // Key and value tiles held.
 template <int D>
 constexpr int kEfK = D > 64 ? 3 : 4;
@@ -52,7 +60,8 @@ struct EfBars {
     uint64_t item_full[2], item_empty[2], q_full, q_empty;
     uint64_t k_full[kEfK<D>], k_empty[kEfK<D>];
     uint64_t v_full[kEfV<D>], v_empty[kEfV<D>];
-    uint64_t s_full[2], p_half[2], p_full[2], o_done[2], o_empty[2];
+    uint64_t s_full[2], s_read[2], p_half[2], p_full[2];
+    uint64_t o_done[2], o_empty[2];
 };
 
 // What the roles know of an item.
@@ -120,6 +129,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     const int tid = threadIdx.x, warp = tid >> 5, lane_id = tid & 31;
     const uint32_t sQ = align1k(smem_u32(smem_raw));
     constexpr int kK = kEfK<D>, kV = kEfV<D>;
+    constexpr bool kAhead = kEfAhead<D>;
     const uint32_t sK = sQ + 2 * kTileB, sV = sK + kK * kTileB;
     DeviceStatus *status = a.status;
 
@@ -156,8 +166,10 @@ __global__ void __launch_bounds__(kEfThreads, 1)
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(&bars.item_full[s], 1);
-            mbar_init(&bars.item_empty[s], 10);  // warps 0-8 and 10
+            // warps 0-8 and 11, and 9 where it issues products
+            mbar_init(&bars.item_empty[s], 10 + kAhead);
             mbar_init(&bars.s_full[s], 1);
+            mbar_init(&bars.s_read[s], 4);
             mbar_init(&bars.p_half[s], 4);
             mbar_init(&bars.p_full[s], 4);
             mbar_init(&bars.o_done[s], 1);
@@ -165,14 +177,14 @@ __global__ void __launch_bounds__(kEfThreads, 1)
         }
         for (int s = 0; s < kK; ++s) {
             mbar_init(&bars.k_full[s], 1);
-            mbar_init(&bars.k_empty[s], 1);
+            mbar_init(&bars.k_empty[s], 1 + kAhead);
         }
         for (int s = 0; s < kV; ++s) {
             mbar_init(&bars.v_full[s], 1);
-            mbar_init(&bars.v_empty[s], 1);
+            mbar_init(&bars.v_empty[s], 1 + kAhead);
         }
         mbar_init(&bars.q_full, 1);
-        mbar_init(&bars.q_empty, 1);
+        mbar_init(&bars.q_empty, 1 + kAhead);
         abort_flag = 0;
         fence_mbar_init();
     }
@@ -199,11 +211,11 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                             &full[st]);
             return true;
         };
-        // of warp 9: where its share begins and how long it is
+        // of warp 10: where its share begins and how long it is
         int sb = 0, skvh = 0, st = 0, at = 0, rest = 0;
         long W = 0;
         int C = 1;
-        if (shares.on && warp == 9) {
+        if (shares.on && warp == 10) {
             W = upto[a.B - 1];
             C = (int)min((long)gridDim.x, max(1L, W / kEfLeast));
             if (blockIdx.x < C) {
@@ -238,7 +250,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 }
             }
         }
-        if (warp == 9 && lane_id == 0) {
+        if (warp == 10 && lane_id == 0) {
             // ------------------------------------ items, loads of Q and K
             int c = 0;   // key tiles loaded so far
             int qs = 0;  // items whose queries were loaded
@@ -353,7 +365,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                               k0 + 128 * kt, 402);
             }
             if (shares.on) shares.rec[blockIdx.x] = rec;
-        } else if (warp == 10 && lane_id == 0) {
+        } else if (warp == 11 && lane_id == 0) {
             // ------------------------------------------------ loads of V
             int c = 0;
             bool ok = true;
@@ -371,7 +383,110 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     ok = load(bars.v_full, bars.v_empty, c, kV, sV, &tmV,
                               k0 + 128 * kt, 411);
             }
-        } else if (warp == 8) {
+        } else if (kAhead && warp < 10) {
+            // --------------------------------------- MMA issue of one slot
+            const int s = warp - 8;
+            const bool el = elect_one();
+            auto wait = [&](uint64_t *bar, uint32_t par, int site) -> bool {
+                if (__all_sync(0xffffffffu, mbar_test(bar, par))) return true;
+                return __all_sync(0xffffffffu,
+                                  mbar_wait_or_abort(bar, par, abort, status,
+                                                     site));
+            };
+            const uint32_t id_s = idesc_bf16(128, 128, false, false);
+            const uint32_t id_o = idesc_bf16(128, D, false, true);
+            const uint64_t dQ = smem_desc(sQ + s * kTileB, 16, 1024);
+            const uint64_t dK = smem_desc(sK, 16, 1024);
+            const uint64_t dV = smem_desc(sV, 16384, 1024);
+            const uint32_t tS = tm + 128 * s, tO = tS + 256, tP = tO + 64;
+            int c = 0, qs = 0;  // key tiles and items before
+            int g = 0, go = 0;  // of which this slot had
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 380)) break;
+                const EfItem &w = item_s[it & 1];
+                const int item = w.item, n = w.n[s];
+                const int nk = max(w.n[0], w.n[1]);
+                const int part = w.kl - 128 * (w.kt0 + nk - 1);
+                __syncwarp();
+                if (el) mbar_arrive(&bars.item_empty[it & 1]);
+                if (item < 0) break;
+                if (nk == 0) continue;
+                if (!(ok = wait(&bars.q_full, qs & 1, 381))) break;
+                ++qs;
+                auto scores = [&](int kt) {
+                    const int st = (c + kt) % kK;
+                    if (!wait(&bars.k_full[st], (c + kt) / kK & 1, 382))
+                        return false;
+                    tc_fence_after();
+                    const uint64_t k = desc_at(dK, st * kTileB);
+                    if (el) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x)
+                            mma_ss(tS, dQ + 2 * x, k + 2 * x, id_s, x > 0);
+                        mma_commit(&bars.s_full[s]);
+                        mma_commit(&bars.k_empty[st]);
+                        if (kt + 1 == n) mma_commit(&bars.q_empty);
+                    }
+                    return true;
+                };
+                if (n > 0) {
+                    ok = scores(0) &&
+                         (go == 0 ||
+                          wait(&bars.o_empty[s], (go - 1) & 1, 383));
+                    ++go;
+                } else if (el) {
+                    mbar_arrive(&bars.q_empty);
+                }
+                for (int kt = 0; kt < n && ok; ++kt, ++g) {
+                    const int st = (c + kt) % kV;
+                    if (kt + 1 < n)
+                        ok = wait(&bars.s_read[s], g & 1, 384) &&
+                             scores(kt + 1);
+                    ok = ok && wait(&bars.v_full[st], (c + kt) / kV & 1, 385);
+                    if (!ok) break;
+                    if (kt == nk - 1 && part < 128) {
+                        // (both slots write the same zeros)
+                        const uint32_t x = sV + st * kTileB;
+                        for (int i = part * 8 + lane_id; i < 1024; i += 32)
+                            st_shared_zero16(x + i * 16);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    const uint64_t v = desc_at(dV, st * kTileB);
+                    ok = wait(&bars.p_half[s], g & 1, 386);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (el) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            mma_ts(tO, tP + 8 * x, v + 128 * x, id_o,
+                                   x > 0 || kt > 0);
+                    }
+                    ok = wait(&bars.p_full[s], g & 1, 387);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (el) {
+#pragma unroll
+                        for (int x = 4; x < 8; ++x)
+                            mma_ts(tO, tP + 8 * x, v + 128 * x, id_o, 1u);
+                        mma_commit(&bars.o_done[s]);
+                        mma_commit(&bars.v_empty[st]);
+                    }
+                }
+                // tiles that only the other slot has
+                for (int kt = n; kt < nk && ok; ++kt) {
+                    const int ks = (c + kt) % kK, vs = (c + kt) % kV;
+                    ok = wait(&bars.k_full[ks], (c + kt) / kK & 1, 388);
+                    if (!ok) break;
+                    if (el) mbar_arrive(&bars.k_empty[ks]);
+                    ok = wait(&bars.v_full[vs], (c + kt) / kV & 1, 389);
+                    if (!ok) break;
+                    if (el) mbar_arrive(&bars.v_empty[vs]);
+                }
+                c += nk;
+            }
+        } else if (!kAhead && warp == 8) {
             // ---------------------------------------------------- MMA issue
             // Whenever half of a slot's P is ready: that half of its P V
             // product; then the other half, and right behind it the scores of its next key tile; the softmax sees these only
@@ -588,6 +703,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                         v[96 + q] = __uint_as_float(e[q]);
                     }
                 }
+                if (kAhead) warp_done(&bars.s_read[s]);
                 const int lim = seen - 128 * (kt0 + kt);
                 if (__any_sync(0xffffffffu, lim < 128)) {
 #pragma unroll
@@ -607,8 +723,14 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 if (kt == 0) {
                     mref = fmaxf(z, kLowest);
                 } else {
-                    // these scores were issued behind the last tile's P V
-                    // product: it is complete when they are
+                    // P and O are free: the last tile's P V product is
+                    // complete (at D = 128 these scores were issued behind it
+                    // and it is complete when they are)
+                    if (kAhead) {
+                        ok = wwait(&bars.o_done[s], (g - 1) & 1, 417);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
                     const bool need = z > mref + kGrown;
                     if (__any_sync(0xffffffffu, need)) {
                         const float f = need ? ex2_approx(mref - z) : 1.0f;
