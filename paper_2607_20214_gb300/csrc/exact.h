@@ -28,9 +28,11 @@ struct ExactView {
 // are past the last row.
 struct ExactOrder {
     int pitch, rows, groups, per;
-    ExactOrder(const ExactView &a, int tile) {
+    ExactOrder(const ExactView &a, int tile)
+        : ExactOrder(a, tile, a.q_len != nullptr) {}
+    ExactOrder(const ExactView &a, int tile, bool padded) {
         pitch = a.Nq;
-        if (a.q_len && a.Nq > 128) pitch = (a.Nq + 127) / 128 * 128;
+        if (padded && a.Nq > 128) pitch = (a.Nq + 127) / 128 * 128;
         rows = a.G * pitch;
         const int tiles = (rows + tile - 1) / tile;
         groups = tiles < a.G ? 1 : a.G;

@@ -1177,10 +1177,9 @@ int divide_walks(long items, long n, int d) {
     return parts < 1 ? 1 : (int)parts;
 }
 // of the walks over keys (dQ) and over query rows (dK, dV)
-int query_parts(const ExactView &a) {
+int query_parts(const ExactView &a, const ExactOrder &order) {
     const int rows = a.d > 64 ? 128 : 64;
-    return divide_walks(ExactOrder(a, 128).items(a),
-                        ((long)a.Nk + rows - 1) / rows, a.d);
+    return divide_walks(order.items(a), ((long)a.Nk + rows - 1) / rows, a.d);
 }
 long key_items(const ExactView &a) {
     return (long)((a.Nk + 127) / 128) * a.B * a.Hkv;
@@ -1190,28 +1189,29 @@ int key_parts(const ExactView &a) {
     return divide_walks(key_items(a), a.G * (((long)a.Nq + rows - 1) / rows),
                         a.d);
 }
-// Floats that the parts of dQ and of dK, dV leave.
-void part_floats(const ExactView &a, size_t *q, size_t *k) {
-    const long nq = ExactOrder(a, 128).items(a), nk = key_items(a);
-    const int sq = query_parts(a), sk = key_parts(a);
-    *q = sq > 1 ? (size_t)nq * sq * 128 * a.d : 0;
-    *k = sk > 1 ? (size_t)nk * sk * 256 * a.d : 0;
+// Floats that the parts of dK, dV and of dQ leave.
+size_t key_floats(const ExactView &a) {
+    const int parts = key_parts(a);
+    return parts > 1 ? (size_t)key_items(a) * parts * 256 * a.d : 0;
 }
-EbSplit query_split(const ExactView &a, float *part) {
-    return EbSplit{query_parts(a), part};
+size_t query_floats(const ExactView &a, bool padded) {
+    const ExactOrder order(a, 128, padded);
+    const int parts = query_parts(a, order);
+    return parts > 1 ? (size_t)order.items(a) * parts * 128 * a.d : 0;
 }
 EbSplit key_split(const ExactView &a, float *part) {
-    size_t q, k;
-    part_floats(a, &q, &k);
-    return EbSplit{key_parts(a), part + q};
+    return EbSplit{key_parts(a), part};
+}
+EbSplit query_split(const ExactView &a, float *part) {
+    return EbSplit{query_parts(a, ExactOrder(a, 128)), part + key_floats(a)};
 }
 
 }  // namespace
 
 size_t exact_part_bytes(const ExactView &a) {
-    size_t q, k;
-    part_floats(a, &q, &k);
-    return sizeof(float) * (q + k);
+    // with and without q_len, which the workspace's size does not know of
+    const size_t x = query_floats(a, false), y = query_floats(a, true);
+    return sizeof(float) * (key_floats(a) + (x > y ? x : y));
 }
 
 cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,

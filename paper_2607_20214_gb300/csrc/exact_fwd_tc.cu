@@ -29,7 +29,7 @@ namespace {
 
 using namespace tc;
 
-// 384 x 168 registers at launch = 256 x 208 (softmax) + 128 x 88
+// 384 x 168 registers at launch = 256 x 200 (softmax) + 128 x 104
 constexpr int kEfThreads = 384;
 constexpr int kEfRegsSoft = 200, kEfRegsOther = 104;
 static_assert(256 * kEfRegsSoft + 128 * kEfRegsOther <= kEfThreads * 168,
@@ -900,21 +900,43 @@ __global__ void __launch_bounds__(256)
         a.lse[to] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Shares instead of whole items: with fewer than four items for each SM, the
-// longest would run alone at the end. Not for short keys, where dividing costs
-// more. (Decided by the sizes alone, so that the workspace does not depend on
-// the device.)
-bool use_shares(const ExactView &a) {
-    const ExactOrder order(a, 256);
+// Shares may be used with fewer than four items for each SM, and not for short
+// keys, where dividing costs more. (By the sizes alone, whether q_len is given
+// or not: with it there are as many items or more.)
+bool may_share(const ExactView &a, bool padded) {
     const long tiles = ((long)a.Nk + 127) / 128;
-    return order.items(a) < 4 * kEfCtas && tiles >= 8 && tiles <= 1 << 20 &&
-           a.B <= kEfMaxB;
+    return ExactOrder(a, 256, padded).items(a) < 4 * kEfCtas && tiles >= 8 &&
+           tiles <= 1 << 20 && a.B <= kEfMaxB;
+}
+
+// Shares instead of whole items, the longest first. A share's parts cost a CTA
+// about 7 tiles' time and k_exact_merge; whole items cost what the longest has
+// beyond an equal share. In padded batches that is known to the device alone:
+// shares. (B1 H16 H_kv4 N4096 d128 causal, longest 32 tiles, shares 28.6: whole
+// items ES_WHOLE us, shares ES_SHARES.)
+bool use_shares(const ExactView &a) {
+    if (!may_share(a, a.q_len != nullptr)) return false;
+    if (a.q_len || a.k_len) return true;
+    const ExactOrder order(a, 256);
+    long sum = 0, longest = 0;
+    for (long r0 = 0; r0 < order.rows; r0 += 256) {
+        const long r1 = r0 + 256 < order.rows ? r0 + 256 : order.rows;
+        // the last row of a head, if there is one, else the tile's last
+        const long last = r0 / a.Nq != (r1 - 1) / a.Nq || r1 % a.Nq == 0
+                              ? a.Nq - 1 : (r1 - 1) % a.Nq;
+        long seen = a.causal ? last + 1 + a.Nk - a.Nq : a.Nk;
+        if (seen > a.Nk) seen = a.Nk;
+        const long n = seen > 0 ? (seen + 127) / 128 : 0;
+        sum += n;
+        if (n > longest) longest = n;
+    }
+    return longest - sum * a.B * a.Hkv / kEfCtas > 7;
 }
 
 }  // namespace
 
 size_t exact_share_bytes(const ExactView &a) {
-    if (!use_shares(a)) return 0;
+    if (!may_share(a, false)) return 0;
     return sizeof(EfRecord) * kEfCtas +
            (size_t)2 * kEfCtas * 256 * sizeof(float) * (a.d + 2);
 }

@@ -413,3 +413,30 @@ def test_backward_of_one_leaf_in_a_graph_beside_an_eager_one():
 def test_divided_walks(B, H, Hkv, Nq, Nk, causal, ql, kl, d):
     """Few items: the sums of the backward pass are divided and added up."""
     run_case(B, H, Hkv, Nq, Nk, d, BF, causal, ql=ql, kl=kl)
+
+
+@pytest.mark.parametrize("H,Hkv,Nq,Nk,d", [
+    (75, 1, 129, 4100, 128), (70, 1, 129, 4100, 128), (150, 1, 129, 2100, 64),
+    (20, 5, 257, 1100, 64)])
+@pytest.mark.parametrize("padded", [False, True])
+def test_the_workspace_is_large_enough(H, Hkv, Nq, Nk, d, padded):
+    """Its size does not know of q_len, with which rows lie on more tiles: what
+    lies behind it stays."""
+    q, k, v, do = (x.cuda() for x in C.exact_inputs(1, H, Hkv, Nq, Nk, d, BF))
+    ex = E.make_exact(1, H, Hkv, Nq, Nk, d)
+    size = E.elsaa_exact_workspace_size(ex, True)
+    room = torch.full((size + (1 << 26),), 77, dtype=torch.uint8,
+                      device="cuda")
+    ws = room[:size]
+    n = lens([Nq], 1) if padded else None
+    lse = torch.zeros((1, H, Nq), device="cuda")
+    o = E.elsaa_exact_forward(ex, q, k, v, q_len=n, lse=lse, workspace=ws)
+    g = E.elsaa_exact_backward(ex, q, k, v, o, lse, do, q_len=n, workspace=ws)
+    E.elsaa_check_status(ws)
+    assert (room[size:] == 77).all()
+    s = (q.double().view(1, Hkv, -1, d) @ k.double().transpose(2, 3)) * d ** -.5
+    p = torch.softmax(s, -1)
+    dv = p.transpose(2, 3) @ do.double().view(1, Hkv, -1, d)
+    # weights of 2^-8 and sums of thousands of terms, in fp32 or bf16
+    scale = (p.transpose(2, 3) @ do.double().abs().view(1, Hkv, -1, d))
+    assert bool(((g[2].double() - dv).abs() <= 2.0 ** -6 * scale).all())
