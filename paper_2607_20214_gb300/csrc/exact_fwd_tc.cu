@@ -16,6 +16,7 @@
 // TMEM: S_s at 128 s, O_s at 256 + 128 s, P_s behind O_s for D <= 64, over S_s
 // at D = 128. O stays in tensor memory; a softmax warp rescales it when the
 // maximum of one of its rows has grown much.
+#include <algorithm>
 #include <type_traits>
 
 #include "device_common.cuh"
@@ -910,27 +911,36 @@ bool may_share(const ExactView &a, bool padded) {
 }
 
 // Shares instead of whole items, the longest first. A share's parts cost a CTA
-// about 7 tiles' time and k_exact_merge; whole items cost what the longest has
-// beyond an equal share. In padded batches that is known to the device alone:
-// shares. (B1 H16 H_kv4 N4096 d128 causal, longest 32 tiles, shares 28.6: whole
-// items ES_WHOLE us, shares ES_SHARES.)
+// about 7 tiles' time and k_exact_merge; whole items cost what the last CTA takes
+// beyond an equal share: at least (j + 1) times the item of rank j C among the C
+// CTAs'. In padded batches that is known to the device alone: shares. Causal
+// B1 H16 H_kv4 N4096 d128 (32 tiles, equal shares 29): whole items 59 us, shares
+// 70; B1 H4 N8192 (64 tiles, shares 28): 107 and 66; B2 H8 H_kv1 N3000, not
+// causal (two items of 24 tiles one behind the other, shares 30): 87 and 73.
 bool use_shares(const ExactView &a) {
     if (!may_share(a, a.q_len != nullptr)) return false;
     if (a.q_len || a.k_len) return true;
     const ExactOrder order(a, 256);
-    long sum = 0, longest = 0;
-    for (long r0 = 0; r0 < order.rows; r0 += 256) {
+    int n[4 * kEfCtas], items = 0;
+    long sum = 0;
+    for (long r0 = 0; r0 < order.rows && items < 4 * kEfCtas; r0 += 256) {
         const long r1 = r0 + 256 < order.rows ? r0 + 256 : order.rows;
         // the last row of a head, if there is one, else the tile's last
-        const long last = r0 / a.Nq != (r1 - 1) / a.Nq || r1 % a.Nq == 0
-                              ? a.Nq - 1 : (r1 - 1) % a.Nq;
+        const long last =
+            r0 / a.Nq != (r1 - 1) / a.Nq ? a.Nq - 1 : (r1 - 1) % a.Nq;
         long seen = a.causal ? last + 1 + a.Nk - a.Nq : a.Nk;
         if (seen > a.Nk) seen = a.Nk;
-        const long n = seen > 0 ? (seen + 127) / 128 : 0;
-        sum += n;
-        if (n > longest) longest = n;
+        n[items] = seen > 0 ? (int)((seen + 127) / 128) : 0;
+        sum += n[items++];
     }
-    return longest - sum * a.B * a.Hkv / kEfCtas > 7;
+    std::sort(n, n + items, [](int x, int y) { return x > y; });
+    const long heads = (long)a.B * a.Hkv;
+    long most = 0;
+    for (long j = 0; j * kEfCtas < items * heads; ++j) {
+        const long t = (j + 1) * n[j * kEfCtas / heads];
+        if (t > most) most = t;
+    }
+    return most - sum * heads / kEfCtas > 7;
 }
 
 }  // namespace
