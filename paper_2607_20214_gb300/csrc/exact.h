@@ -84,6 +84,54 @@ __device__ __forceinline__ int exact_most(const ExactSeq &s, int r0, int r1,
     if (heads > 1 || (heads == 1 && i0 < s.ql)) return s.seen(s.ql - 1);
     return heads == 1 || i0 < s.ql ? s.seen(min(i1, s.ql - 1)) : 0;
 }
+
+// Row and first of eight channels of thread t, of D / 8 threads a row: a warp
+// has 8 rows and 4 pieces of 8 channels of each, so that its reads of sums laid
+// out [D / 8][rows][8] cover 256 bytes and its writes of a bf16 row 64.
+template <int D>
+__device__ __forceinline__ long piece_of(long t, int *c) {
+    const int lane = (int)(t & 31);
+    const long warp = t >> 5;
+    *c = (int)(warp % (D / 32)) * 32 + (lane & 3) * 8;
+    return warp / (D / 32) * 8 + (lane >> 2);
+}
+
+// Writes CH 16-byte pieces (2 or 4) of every lane's row, rows D elements apart:
+// y is the lane's own row from `row` on. Lanes first exchange pieces in groups
+// of CH, so that a store covers 16 CH bytes of 32 / CH rows; with a row a lane
+// each store met 32 lines, and the memory unit took them one after the other.
+template <int D, int CH>
+__device__ __forceinline__ void store_rows(uint32_t (&y)[4 * CH],
+                                           uint16_t *row, bool valid,
+                                           int lane) {
+    const uint32_t rows = __ballot_sync(0xffffffffu, valid);
+#pragma unroll
+    for (int bit = 1; bit < CH; bit <<= 1) {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if (k & bit) continue;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t &a = y[4 * k + w], &b = y[4 * (k | bit) + w];
+                const uint32_t r =
+                    __shfl_xor_sync(0xffffffffu, up ? a : b, bit);
+                if (up)
+                    a = r;
+                else
+                    b = r;
+            }
+        }
+    }
+    // piece p of row (group + i) now is piece i of lane p of the group
+    const int p = lane & (CH - 1), first = lane - p;
+    uint16_t *to = row - p * D + 8 * p;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+        if (rows >> (first + i) & 1)
+            *reinterpret_cast<uint4 *>(to + i * D) = make_uint4(
+                y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+}
 #endif
 
 // bf16 on the tensor cores; next_item: an int of scratch; part:

@@ -128,25 +128,23 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int part,
     __syncwarp();
 }
 
-// A thread's columns of sums in tensor memory, times f, to a row of bf16.
+// A thread's columns of sums in tensor memory, times f, to a row of bf16 (the
+// whole warp).
 template <int D>
 __device__ __forceinline__ void store_sums(uint32_t t, float f, uint16_t *o,
-                                           bool valid) {
+                                           bool valid, int lane_id) {
+    constexpr int n = Eb<D>::out;
+    uint32_t x[n], y[n / 2];
+    if constexpr (n == 32)
+        tmem_ld32(t, x);
+    else
+        tmem_ld16(t, x);
+    tmem_wait_ld();
 #pragma unroll
-    for (int c = 0; c < Eb<D>::out; c += 16) {
-        uint32_t x[16], y[8];
-        tmem_ld16(t + c, x);
-        tmem_wait_ld();
-        if (!valid) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            y[e] = pack_bf16x2(__uint_as_float(x[2 * e]) * f,
-                               __uint_as_float(x[2 * e + 1]) * f);
-        reinterpret_cast<uint4 *>(o + c)[0] =
-            make_uint4(y[0], y[1], y[2], y[3]);
-        reinterpret_cast<uint4 *>(o + c)[1] =
-            make_uint4(y[4], y[5], y[6], y[7]);
-    }
+    for (int e = 0; e < n / 2; ++e)
+        y[e] = pack_bf16x2(__uint_as_float(x[2 * e]) * f,
+                           __uint_as_float(x[2 * e + 1]) * f);
+    store_rows<D, n / 8>(y, o, valid, lane_id);
 }
 template <int D>
 __device__ __forceinline__ void store_zeros(uint16_t *o) {
@@ -155,11 +153,12 @@ __device__ __forceinline__ void store_zeros(uint16_t *o) {
         *reinterpret_cast<uint4 *>(o + c) = make_uint4(0, 0, 0, 0);
 }
 
-// The same columns as they are.
+// The same columns as they are, to [D / 8][128 rows][8].
 template <int D>
 __device__ __forceinline__ void store_part(uint32_t t, float *o) {
+    constexpr int n = Eb<D>::out;
 #pragma unroll
-    for (int c = 0; c < Eb<D>::out; c += 16) {
+    for (int c = 0; c < n; c += 16) {
         uint32_t x[16], y[8];
         tmem_ld16(t + c, x);
         tmem_wait_ld();
@@ -167,7 +166,7 @@ __device__ __forceinline__ void store_part(uint32_t t, float *o) {
         for (int h = 0; h < 16; h += 8) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = x[h + e];
-            st_global_v8(o + c + h, y);
+            st_global_v8(o + (c + h) * 128, y);
         }
     }
 }
@@ -234,8 +233,8 @@ struct BwdItem {
 };
 
 // Walks of n tiles in at most `splits` parts of kEbLeast tiles and more. Part p
-// of item i of the call leaves its sums in o[i splits + p][128][D] (keys: dK,
-// then dV, [2][128][D]).
+// of item i of the call leaves its sums in o[i splits + p][D / 8][128][8] (keys:
+// dK, then dV).
 constexpr int kEbLeast = 4;
 struct EbSplit {
     int splits;
@@ -573,10 +572,10 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
             tc_fence_after();
             const uint32_t to = tm + lane + kO + E::out * part;
             if (w.part >= 0)
-                store_part<D>(to, split.o + ((size_t)w.part * 128 + row) * D +
-                                      E::out * part);
+                store_part<D>(to, split.o + (size_t)w.part * 128 * D +
+                                      E::out * part * 128 + row * 8);
             else
-                store_sums<D>(to, a.scale, o, valid);
+                store_sums<D>(to, a.scale, o, valid, lane_id);
             tc_fence_before();
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.dq_empty);
@@ -1032,13 +1031,13 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
             tc_fence_after();
             const uint32_t t = tm + lane + E::out * part;
             if (w.part >= 0) {
-                float *o = split.o + ((size_t)w.part * 256 + row) * D +
-                           E::out * part;
+                float *o = split.o + (size_t)w.part * 256 * D +
+                           E::out * part * 128 + row * 8;
                 store_part<D>(t + X::cK, o);
                 store_part<D>(t + X::cV, o + 128 * D);
             } else {
-                store_sums<D>(t + X::cV, 1.0f, ov, valid);
-                store_sums<D>(t + X::cK, a.scale, ok_, valid);
+                store_sums<D>(t + X::cV, 1.0f, ov, valid, lane_id);
+                store_sums<D>(t + X::cK, a.scale, ok_, valid, lane_id);
             }
             tc_fence_before();
             __syncwarp();
@@ -1060,9 +1059,8 @@ __global__ void __launch_bounds__(256)
                 const __grid_constant__ EbSplit sk) {
     wait_for_stream();
     using E = Eb<D>;
-    constexpr int L = D / 8;
-    long row = ((long)blockIdx.x * 256 + threadIdx.x) / L;
-    const int c = threadIdx.x % L * 8;
+    int c;
+    long row = piece_of<D>((long)blockIdx.x * 256 + threadIdx.x, &c);
     const long nq = sq.splits > 1 ? (long)a.B * a.H * a.Nq : 0;
     const bool keys = row >= nq;
     const float *from;
@@ -1079,7 +1077,7 @@ __global__ void __launch_bounds__(256)
                                   order.pitch) + E::rows - 1) / E::rows;
         parts = parts_of(sq, n);
         const size_t index = (size_t)head * order.groups * order.per + r / 128;
-        from = sq.o + (index * sq.splits * 128 + (r - r0)) * D + c;
+        from = sq.o + index * sq.splits * 128 * D + c * 128 + (r - r0) * 8;
         step = 128 * D;
         to = (uint16_t *)a.dq + row * D + c;
     } else {
@@ -1093,7 +1091,7 @@ __global__ void __launch_bounds__(256)
             a.G * ((seq.ql - seq.first_row(r0) + E::rows - 1) / E::rows);
         parts = parts_of(sk, n);
         const size_t index = (size_t)head * ((a.Nk + 127) / 128) + j / 128;
-        from = sk.o + (index * sk.splits * 256 + (j - r0)) * D + c;
+        from = sk.o + index * sk.splits * 256 * D + c * 128 + (j - r0) * 8;
         step = 256 * D;
         to = (uint16_t *)a.dk + row * D + c;
     }
@@ -1263,7 +1261,7 @@ cudaError_t launch_exact_sum(const ExactView &a, float *part,
     long rows = sq.splits > 1 ? (long)a.B * a.H * a.Nq : 0;
     if (sk.splits > 1) rows += (long)a.B * a.Hkv * a.Nk;
     if (rows == 0) return cudaSuccess;
-    const long threads = rows * (a.d / 8);
+    const long threads = (rows + 7) / 8 * a.d;  // 8 rows a warp
     return by_width(a.d, [&](auto dim) {
         return launch_after(k_exact_sum<decltype(dim)::value>,
                             dim3((unsigned)((threads + 255) / 256)), 256, 0,

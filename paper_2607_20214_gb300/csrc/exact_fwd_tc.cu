@@ -79,7 +79,7 @@ struct EfItem {
 // of all sequences make one row of units: kEfHead for an item (what it costs
 // beside its tiles) and one for each of its key tiles (of 256 rows). CTA c of C
 // takes units [W c / C, W (c + 1) / C) of the W. Of an item that is divided,
-// every CTA leaves 256 rows of sums of e^(z - m) v in o[part][row][D] and
+// every CTA leaves 256 rows of sums of e^(z - m) v in o[part][D / 8][row][8] and
 // (m, sum of e^(z - m)) in ml[part][row], z and m base 2: part 2 c + 1 of the
 // CTA that begins it, part 2 c of the others. rec[c] tells k_exact_merge of
 // the item that CTA c begins.
@@ -793,8 +793,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 tc_fence_after();
             }
             if (part >= 0) {
-                const size_t to = (size_t)part * 256 + 128 * s + row;
-                float *y = shares.o + to * D;
+                const int at_row = 128 * s + row;
+                float *y = shares.o + (size_t)part * 256 * D + at_row * 8;
                 for (int c = 0; c < D && n > 0; c += 32) {
                     uint32_t x[32];
                     tmem_ld32(tO + c, x);
@@ -806,10 +806,12 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                         uint32_t e[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) e[i] = x[q + i];
-                        st_global_v8(y + c + q, e);
+                        st_global_v8(y + (c + q) * 256, e);
                     }
                 }
-                if (valid) shares.ml[to] = make_float2(mref, lsum);
+                if (valid)
+                    shares.ml[(size_t)part * 256 + at_row] =
+                        make_float2(mref, lsum);
                 continue;
             }
             // a row that sees nothing, or only scores of -inf: zeros
@@ -827,20 +829,12 @@ __global__ void __launch_bounds__(kEfThreads, 1)
 #pragma unroll
                     for (int q = 0; q < 32; ++q) x[q] = 0;
                 }
-                if (!valid) continue;
+                uint32_t y[16];
 #pragma unroll
-                for (int q = 0; q < 32; q += 16) {
-                    uint32_t y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        y[e] = pack_bf16x2(
-                            __uint_as_float(x[q + 2 * e]) * inv,
-                            __uint_as_float(x[q + 2 * e + 1]) * inv);
-                    reinterpret_cast<uint4 *>(o + c + q)[0] =
-                        make_uint4(y[0], y[1], y[2], y[3]);
-                    reinterpret_cast<uint4 *>(o + c + q)[1] =
-                        make_uint4(y[4], y[5], y[6], y[7]);
-                }
+                for (int e = 0; e < 16; ++e)
+                    y[e] = pack_bf16x2(__uint_as_float(x[2 * e]) * inv,
+                                       __uint_as_float(x[2 * e + 1]) * inv);
+                store_rows<D, 4>(y, o + c, valid, lane_id);
             }
             if (valid && a.lse)
                 a.lse[at] = lsum == 0.0f ? -INFINITY
@@ -860,29 +854,28 @@ __global__ void __launch_bounds__(256)
                   const __grid_constant__ EfShares shares,
                   const __grid_constant__ ExactOrder order) {
     wait_for_stream();
-    constexpr int L = D / 8;
     const int first = blockIdx.y;
     const EfRecord rec = shares.rec[first];
     if (rec.last < 0) return;
-    const int row = (blockIdx.x * 256 + threadIdx.x) / L;
-    const int c = threadIdx.x % L * 8, r = rec.r0 + row;
+    int c;
+    const int row = (int)piece_of<D>(blockIdx.x * 256 + threadIdx.x, &c);
+    const int r = rec.r0 + row;
     if (r >= order.rows ||
         r % order.pitch >= ExactSeq(a, rec.b).ql)
         return;
-    auto at = [&](int cta) {
-        return (size_t)(2 * cta + (cta == first)) * 256 + row;
-    };
+    auto at = [&](int cta) { return (size_t)(2 * cta + (cta == first)); };
     float m = kLowest;
     for (int p = first; p <= rec.last; ++p)
-        m = fmaxf(m, shares.ml[at(p)].x);
+        m = fmaxf(m, shares.ml[at(p) * 256 + row].x);
     float l = 0.0f, o[8] = {};
     for (int p = first; p <= rec.last; ++p) {
-        const float2 ml = shares.ml[at(p)];
+        const float2 ml = shares.ml[at(p) * 256 + row];
         if (ml.y == 0.0f) continue;  // its sums may not have been written
         const float f = ex2_approx(ml.x - m);
         l = fmaf(ml.y, f, l);
         const float4 *x =
-            reinterpret_cast<const float4 *>(shares.o + at(p) * D + c);
+            reinterpret_cast<const float4 *>(shares.o + at(p) * 256 * D +
+                                             c * 256 + row * 8);
         const float4 u = x[0], v = x[1];
         const float e[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
