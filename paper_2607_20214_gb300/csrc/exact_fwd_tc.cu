@@ -58,7 +58,7 @@ constexpr float kLowest = -1e38f;
 
 template <int D>
 struct EfBars {
-    uint64_t item_full[2], item_empty[2], q_full, q_empty;
+    uint64_t item_full[2], item_empty[2], q_full[2], q_empty[2];
     uint64_t k_full[kEfK<D>], k_empty[kEfK<D>];
     uint64_t v_full[kEfV<D>], v_empty[kEfV<D>];
     uint64_t s_full[2], s_read[2], p_half[2], p_full[2];
@@ -169,6 +169,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             mbar_init(&bars.item_full[s], 1);
             // warps 0-8 and 11, and 9 where it issues products
             mbar_init(&bars.item_empty[s], 10 + kAhead);
+            mbar_init(&bars.q_full[s], 1);
+            mbar_init(&bars.q_empty[s], 1);
             mbar_init(&bars.s_full[s], 1);
             mbar_init(&bars.s_read[s], 4);
             mbar_init(&bars.p_half[s], 4);
@@ -184,8 +186,6 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             mbar_init(&bars.v_full[s], 1);
             mbar_init(&bars.v_empty[s], 1 + kAhead);
         }
-        mbar_init(&bars.q_full, 1);
-        mbar_init(&bars.q_empty, 1 + kAhead);
         abort_flag = 0;
         fence_mbar_init();
     }
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
         if (warp == 10 && lane_id == 0) {
             // ------------------------------------ items, loads of Q and K
             int c = 0;   // key tiles loaded so far
-            int qs = 0;  // items whose queries were loaded
+            int qs[2] = {0, 0};  // items whose queries were loaded
             bool ok = true;
             const int heads = a.B * a.Hkv, rows = order.rows;
             EfRecord rec = {0, 0, 0, -1};
@@ -320,24 +320,31 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 }
                 return false;
             };
-            for (int it = 0; ok; ++it) {
+            // An item is drawn when the last one's key tiles are on their way:
+            // earlier, and the longest items' CTAs draw others that they come
+            // to late (B1 H16 H_kv4 N4096 d128 causal: 83 us instead of 58).
+            bool begun = false;
+            auto next = [&]() {
                 EfItem w = {-1};
                 if (shares.on) {
                     if (!next_share(w)) w.item = -1;
-                } else {
-                    long item = blockIdx.x;
-                    if (it > 0)
-                        item = next_item ? (long)gridDim.x +
-                                               atomicAdd(next_item, 1)
-                                         : items;
-                    if (item < items) {
-                        // the last rows of every query head, which see most,
-                        // first
-                        const int h = (int)(item % heads);
-                        fill(w, h / a.Hkv, h % a.Hkv, (int)(item / heads), 0,
-                             1 << 30);
-                    }
+                    return w;
                 }
+                const long item = !begun      ? blockIdx.x
+                                  : next_item ? (long)gridDim.x +
+                                                    atomicAdd(next_item, 1)
+                                              : items;
+                begun = true;
+                if (item < items) {
+                    // the last rows of every query head, which see most,
+                    // first
+                    const int h = (int)item % heads, t = (int)item / heads;
+                    fill(w, h / a.Hkv, h % a.Hkv, t, 0, 1 << 30);
+                }
+                return w;
+            };
+            for (int it = 0; ok; ++it) {
+                const EfItem w = next();
                 if (it >= 2 && !mbar_wait_or_abort(&bars.item_empty[it & 1],
                                                    ((it >> 1) - 1) & 1, abort,
                                                    status, 400))
@@ -346,22 +353,30 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 mbar_arrive(&bars.item_full[it & 1]);
                 if (w.item < 0) break;
                 const int nk = max(w.n[0], w.n[1]);
-                if (nk == 0) continue;
-                if (qs >= 1 && !mbar_wait_or_abort(&bars.q_empty, (qs - 1) & 1,
-                                                   abort, status, 401))
-                    break;
-                ++qs;
                 const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
                 const int k0 =
                     (w.b * a.Hkv + w.kvh) * a.Nk + 128 * w.kt0;
-                mbar_expect_tx(&bars.q_full,
-                               ((w.n[0] > 0) + (w.n[1] > 0)) * kTileB);
-                for (int s = 0; s < 2; ++s)
-                    for (int p = 0; p < kPanels && w.n[s] > 0; ++p)
+                int kt = 0;
+                for (int s = 0; s < 2 && ok; ++s) {
+                    if (w.n[s] == 0) continue;
+                    ok = qs[s] == 0 ||
+                         mbar_wait_or_abort(&bars.q_empty[s], (qs[s] - 1) & 1,
+                                            abort, status, 401);
+                    if (!ok) break;
+                    ++qs[s];
+                    mbar_expect_tx(&bars.q_full[s], kTileB);
+                    for (int p = 0; p < kPanels; ++p)
                         tma_load_2d(sQ + s * kTileB + p * 16384, &tmQ, 64 * p,
                                     q0 + order.row(w.r0 + 128 * s, a.Nq),
-                                    &bars.q_full);
-                for (int kt = 0; kt < nk && ok; ++kt, ++c)
+                                    &bars.q_full[s]);
+                    if (kt == 0) {
+                        ok = load(bars.k_full, bars.k_empty, c, kK, sK, &tmK,
+                                  k0, 402);
+                        ++kt;
+                        ++c;
+                    }
+                }
+                for (; kt < nk && ok; ++kt, ++c)
                     ok = load(bars.k_full, bars.k_empty, c, kK, sK, &tmK,
                               k0 + 128 * kt, 402);
             }
@@ -400,8 +415,8 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             const uint64_t dK = smem_desc(sK, 16, 1024);
             const uint64_t dV = smem_desc(sV, 16384, 1024);
             const uint32_t tS = tm + 128 * s, tO = tS + 256, tP = tO + 64;
-            int c = 0, qs = 0;  // key tiles and items before
-            int g = 0, go = 0;  // of which this slot had
+            int c = 0;          // key tiles before
+            int g = 0, go = 0;  // tiles and items that this slot had
             bool ok = true;
             for (int it = 0; ok; ++it) {
                 if (!wait(&bars.item_full[it & 1], (it >> 1) & 1, 380)) break;
@@ -413,8 +428,6 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 if (el) mbar_arrive(&bars.item_empty[it & 1]);
                 if (item < 0) break;
                 if (nk == 0) continue;
-                if (!(ok = wait(&bars.q_full, qs & 1, 381))) break;
-                ++qs;
                 auto scores = [&](int kt) {
                     const int st = (c + kt) % kK;
                     if (!wait(&bars.k_full[st], (c + kt) / kK & 1, 382))
@@ -427,17 +440,15 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                             mma_ss(tS, dQ + 2 * x, k + 2 * x, id_s, x > 0);
                         mma_commit(&bars.s_full[s]);
                         mma_commit(&bars.k_empty[st]);
-                        if (kt + 1 == n) mma_commit(&bars.q_empty);
+                        if (kt + 1 == n) mma_commit(&bars.q_empty[s]);
                     }
                     return true;
                 };
                 if (n > 0) {
-                    ok = scores(0) &&
+                    ok = wait(&bars.q_full[s], go & 1, 381) && scores(0) &&
                          (go == 0 ||
                           wait(&bars.o_empty[s], (go - 1) & 1, 383));
                     ++go;
-                } else if (el) {
-                    mbar_arrive(&bars.q_empty);
                 }
                 for (int kt = 0; kt < n && ok; ++kt, ++g) {
                     const int st = (c + kt) % kV;
@@ -512,7 +523,6 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             const uint64_t dV = smem_desc(sV, 16384, 1024);
             constexpr uint32_t kTile = kTileB >> 4;  // in descriptor units
             int c0 = 0;                // key tiles of earlier items
-            int qs = 0;
             int gp0 = 0, gp1 = 0;      // P V products issued per slot
             int go0 = 0, go1 = 0;      // items finished per slot
             bool ok = true;
@@ -525,9 +535,6 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 if (w.item < 0) break;
                 const int n0 = w.n[0], n1 = w.n[1], nk = max(n0, n1);
                 if (nk == 0) continue;
-                ok = wait(&bars.q_full, qs & 1, 405);
-                if (!ok) break;
-                ++qs;
                 int us0 = 0, us1 = 0, up0 = 0, up1 = 0;
                 // keys of the last tile that the sequence has: values of
                 // others count with weights of 0 and must be numbers
@@ -553,8 +560,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                         // both slots have used the tile
                         if (us >= n_o || us_o > us)
                             mma_commit(&bars.k_empty[st]);
-                        if (us + 1 == n && us_o == n_o)
-                            mma_commit(&bars.q_empty);
+                        if (us + 1 == n) mma_commit(&bars.q_empty[s]);
                     }
                     ++us;
                     return true;
@@ -617,8 +623,12 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 };
                 using S0 = std::integral_constant<int, 0>;
                 using S1 = std::integral_constant<int, 1>;
-                if (n0 > 0) ok = scores(S0{}, us0, n0, us1, n1);
-                if (ok && n1 > 0) ok = scores(S1{}, us1, n1, us0, n0);
+                if (n0 > 0)
+                    ok = wait(&bars.q_full[0], go0 & 1, 405) &&
+                         scores(S0{}, us0, n0, us1, n1);
+                if (ok && n1 > 0)
+                    ok = wait(&bars.q_full[1], go1 & 1, 418) &&
+                         scores(S1{}, us1, n1, us0, n0);
                 unsigned long long t_last = 0;
                 uint32_t idle = 0;
                 while (ok && (up0 < n0 || up1 < n1)) {
