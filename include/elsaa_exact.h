@@ -16,8 +16,13 @@
  * of its k_len (all N_k) when causal = 0 or j <= i + k_len - q_len: the last
  * query sees every key. With s_ij = scale <q_i, k_j> over those j,
  *     lse_i = log sum_j exp(s_ij),   O_i = sum_j exp(s_ij - lse_i) v_j;
- * a query that sees nothing has O_i = 0 and lse_i = -inf. Lengths outside
- * [0, N_q] and [0, N_k] are clipped.
+ * a query that sees nothing has O_i = 0 and lse_i = -inf, and so has one whose
+ * scores are all -inf. Lengths outside [0, N_q] and [0, N_k] are clipped.
+ *
+ * Rows behind the lengths may hold anything, NaN too. A NaN or an infinity in a
+ * row that a sequence has may, with causal = 1, also reach rows that do not see
+ * it or that it does not see, within 128 rows of the diagonal (v in the forward
+ * pass; q, k, v and d_o in the backward pass): a weight of 0 times it is NaN.
  */
 #ifndef ELSAA_EXACT_H
 #define ELSAA_EXACT_H
@@ -55,14 +60,18 @@ int elsaa_exact_workspace_size(const elsaa_exact *exact, int backward,
 
 /*
  * q        [B, H, N_q, d_h], k, v [B, H_kv, N_k, d_h], contiguous, 16-byte
- *          aligned, as all tensors here.
- * q_len, k_len  [B] int32, or NULL. Rows behind them may hold anything, NaN
- *          too, and those of o and lse are left as they were.
+ *          aligned, as all tensors here. Outputs must not overlap inputs.
+ * q_len, k_len  [B] int32, or NULL. Rows of o and lse behind q_len are left as
+ *          they were.
  * o        [B, H, N_q, d_h] (written).
  * lse      [B, H, N_q] fp32 (written), or NULL.
  *
- * bf16: scores and sums in fp32, weights rounded to bf16 for their product
- * with V.
+ * bf16 on the tensor cores: scores and sums in fp32, weights (relative to a
+ * reference within 2^8 of the row's largest) rounded to bf16 for their product
+ * with V, their sum taken before that; o rounded once. A score below -6.9e37
+ * counts as -inf. The results do not depend on timing, but the division of rows
+ * over CTAs, and with it the last bits, depends on the sizes, the lengths and
+ * the number of SMs.
  */
 int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
                         const void *k, const void *v, const int32_t *q_len,
@@ -79,7 +88,9 @@ int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
  *     dK = scale dS^T Q,
  * summed over the query heads of a K/V head in a fixed order: a call gives the
  * same bits every time. Rows behind the lengths are left as they were; those
- * of queries that see nothing and of keys that no query sees are zeros.
+ * of queries that see nothing and of keys that no query sees are zeros. bf16 on
+ * the tensor cores: P and dS in fp32, each rounded to bf16 for its products,
+ * sums in fp32, results rounded once.
  */
 int elsaa_exact_backward(const elsaa_exact *exact, const void *q,
                          const void *k, const void *v, const void *o,

@@ -156,7 +156,9 @@ cudaError_t launch_exact_sum(const ExactView &a, float *part,
 size_t exact_chunk_bytes(const ExactView &a);
 cudaError_t launch_exact_fwd_simt(const ExactView &a, float *part,
                                   cudaStream_t st);
-cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys,
+// part: exact_add_bytes(a) of scratch
+size_t exact_add_bytes(const ExactView &a);
+cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys, float *part,
                                   cudaStream_t st);
 
 }  // namespace elsaa

@@ -81,7 +81,9 @@ Layout layout(const ExactView &a, bool tensor, bool backward) {
     const size_t delta = sizeof(float) * (size_t)a.B * a.H * a.Nq;
     if (backward && delta > most) most = delta;
     l.part = l.total = l.scratch + align256(most);
-    if (backward && tensor) l.total += align256(exact_part_bytes(a));
+    if (backward)
+        l.total +=
+            align256(tensor ? exact_part_bytes(a) : exact_add_bytes(a));
     return l;
 }
 
@@ -183,11 +185,11 @@ extern "C" int elsaa_exact_backward(
     a.status = (DeviceStatus *)workspace;
     a.delta = (float *)((char *)workspace + l.scratch);
     cudaStream_t st = (cudaStream_t)stream;
+    float *part = (float *)((char *)workspace + l.part);
     if (tensor) {
         int *next_item = (int *)((char *)workspace + l.next_item);
         ELSAA_EXACT_LAUNCH("exact_delta", st,
                            launch_exact_delta(a, next_item, st));
-        float *part = (float *)((char *)workspace + l.part);
         ELSAA_EXACT_LAUNCH("exact_dq_tc", st,
                            launch_exact_dq_tc(a, next_item, part, st));
         ELSAA_EXACT_LAUNCH("exact_dkv_tc", st,
@@ -196,8 +198,8 @@ extern "C" int elsaa_exact_backward(
         return ELSAA_OK;
     }
     ELSAA_EXACT_LAUNCH("exact_dq_simt", st,
-                       launch_exact_bwd_simt(a, false, st));
+                       launch_exact_bwd_simt(a, false, part, st));
     ELSAA_EXACT_LAUNCH("exact_dkv_simt", st,
-                       launch_exact_bwd_simt(a, true, st));
+                       launch_exact_bwd_simt(a, true, part, st));
     return ELSAA_OK;
 }

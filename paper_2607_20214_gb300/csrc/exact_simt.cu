@@ -9,8 +9,9 @@
 // scores of rows 4 y .. 4 y + 3 with x, x + 16, x + 32, x + 48, and of the sums
 // the same rows with d / 16 channels. Every four channels cost 8 16-byte reads
 // from shared memory for 64 multiply-adds (32 packed ones): bound by the
-// CUDA cores' multiply-adds. With few tiles of rows the keys of the forward pass
-// are divided too, and k_exact_join adds up what the chunks of a row leave.
+// CUDA cores' multiply-adds. With few tiles of held rows the walks are divided
+// into chunks, and k_exact_join and k_exact_add add up, in order, what these
+// leave.
 #include <type_traits>
 
 #include "device_common.cuh"
@@ -146,9 +147,11 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-// How the keys are divided: `splits` chunks at most, of `chunk` keys. What a
-// chunk leaves of row r (over all heads): the sums of e^(z - m) v in
-// o[part][r][D], and (m, sum of e^(z - m)) in ml[part][r], z and m base 2.
+// How walks are divided: `splits` chunks at most, of `chunk` keys, or (dK, dV) of
+// `chunk` passing rows over all heads. What a chunk leaves of held row r (over
+// all heads): the sums in o[part][r][D], of the forward pass those of e^(z - m) v
+// with (m, sum of e^(z - m)) in ml[part][r], z and m base 2; of dK and dV
+// [part][r][2][D].
 struct Split {
     int splits, chunk;
     size_t rows;
@@ -311,7 +314,8 @@ __global__ void __launch_bounds__(256)
 // KEYS = 1: key rows held; dK, dV.
 template <typename T, int D, bool KEYS>
 __global__ void __launch_bounds__(kThreads)
-    k_exact_bwd(const __grid_constant__ ExactView a, int tiles) {
+    k_exact_bwd(const __grid_constant__ ExactView a,
+                const __grid_constant__ Split split, int tiles) {
     wait_for_stream();
     extern __shared__ __align__(16) float sm[];
     // held: Q, dO or K, V; passing: K, V or Q, dO
@@ -324,7 +328,7 @@ __global__ void __launch_bounds__(kThreads)
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
     if (!KEYS && blockIdx.x == 0 && threadIdx.x < 4)
         (&a.status->code)[threadIdx.x] = 0;
-    const Item it(a, tiles);
+    const Item it(a, tiles, split.splits);
     const ExactSeq seq(a, it.b);
     const size_t head0 = (size_t)it.b * a.H + (size_t)it.kvh * a.G;
     const size_t qrow = head0 * a.Nq;
@@ -344,6 +348,10 @@ __global__ void __launch_bounds__(kThreads)
         }
     if constexpr (!KEYS) {
         const int rows = a.G * a.Nq, r1 = min(r0 + kHeld, rows);
+        const int all = exact_most(seq, r0, r1, a.Nq);
+        const int begin = it.part * split.chunk;
+        if (it.part > 0 && begin >= all) return;
+        const int most = min(all, begin + split.chunk);
         auto valid = [&](int r) {
             return r0 + r < r1 && (r0 + r) % a.Nq < seq.ql;
         };
@@ -367,11 +375,11 @@ __global__ void __launch_bounds__(kThreads)
             if (valid(r)) {
                 seen[i] = seq.seen((r0 + r) % a.Nq);
                 lse2[i] = a.lse[qrow + r0 + r] * kLog2e;
-                if (x == 0) a.delta[qrow + r0 + r] = delta[i];
+                if (x == 0 && it.part == 0)
+                    a.delta[qrow + r0 + r] = delta[i];
             }
         }
-        const int most = exact_most(seq, r0, r1, a.Nq);
-        for (int j0 = 0; j0 < most; j0 += kPass) {
+        for (int j0 = begin; j0 < most; j0 += kPass) {
             __syncthreads();
             auto have = [&](int r) { return j0 + r < most; };
             load_rows<T, D>(sC, D + 4, K + (size_t)j0 * D, kPass, have);
@@ -396,6 +404,13 @@ __global__ void __launch_bounds__(kThreads)
         for (int i = 0; i < 4; ++i) {
             const int r = r0 + 4 * y + i;
             if (!valid(4 * y + i)) continue;
+            if (all > split.chunk) {
+                float *o = split.o + (it.part * split.rows + qrow + r) * D +
+                           2 * x;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) store2(o + 32 * c, acc[i][c]);
+                continue;
+            }
             T *o = (T *)a.dq + (qrow + r) * D + 2 * x;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
@@ -407,8 +422,15 @@ __global__ void __launch_bounds__(kThreads)
         auto valid = [&](int r) { return r0 + r < seq.kl; };
         load_rows<T, D>(sA, D, K + (size_t)r0 * D, kHeld, valid);
         load_rows<T, D>(sB, D, V + (size_t)r0 * D, kHeld, valid);
-        for (int g = 0; g < a.G; ++g)
-            for (int i0 = seq.first_row(r0); i0 < seq.ql; i0 += kPass) {
+        // passing tiles of a head, of all heads, of this chunk
+        const int first = seq.first_row(r0);
+        const int per = (seq.ql - first + kPass - 1) / kPass;
+        const int all = a.G * per, t0 = it.part * (split.chunk / kPass);
+        if (it.part > 0 && t0 >= all) return;
+        const int t1 = min(all, t0 + split.chunk / kPass);
+        if (t0 < t1) {
+            int g = t0 / per, i0 = first + t0 % per * kPass;
+            for (int t = t0; t < t1; ++t) {
                 const size_t at = (size_t)g * a.Nq + i0;
                 __syncthreads();
                 auto have = [&](int r) { return i0 + r < seq.ql; };
@@ -440,10 +462,26 @@ __global__ void __launch_bounds__(kThreads)
                 __syncwarp();
                 weighted<D>(sW, sC, y, x, acc);
                 weighted<D>(sP, sE, y, x, acc2);
+                i0 += kPass;
+                if (i0 >= seq.ql) {
+                    i0 = first;
+                    ++g;
+                }
             }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (!valid(4 * y + i)) continue;
+            if (all * kPass > split.chunk) {
+                float *o = split.o + (it.part * split.rows + kv + r0 + 4 * y +
+                                      i) * 2 * D + 2 * x;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    store2(o + 32 * c, acc[i][c]);
+                    store2(o + D + 32 * c, acc2[i][c]);
+                }
+                continue;
+            }
             const size_t at = (kv + r0 + 4 * y + i) * D + 2 * x;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -452,6 +490,53 @@ __global__ void __launch_bounds__(kThreads)
                 store2((T *)a.dv + at + 32 * c, acc2[i][c]);
             }
         }
+    }
+}
+
+// The sums of dQ's rows, or of dK's and dV's, that were divided: D / 4 lanes a
+// row.
+template <typename T, int D, bool KEYS>
+__global__ void __launch_bounds__(256)
+    k_exact_add(const __grid_constant__ ExactView a,
+                const __grid_constant__ Split split) {
+    wait_for_stream();
+    constexpr int L = D / 4, n = KEYS ? 2 : 1;
+    const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int c = threadIdx.x % L * 4;
+    if (row >= split.rows) return;
+    int parts;
+    if constexpr (KEYS) {
+        const int j = (int)(row % a.Nk);
+        const ExactSeq seq(a, (int)(row / a.Nk) / a.Hkv);
+        if (j >= seq.kl) return;
+        const int first = seq.first_row(j / kHeld * kHeld);
+        const int all =
+            a.G * ((seq.ql - first + kPass - 1) / kPass) * kPass;
+        parts = (all + split.chunk - 1) / split.chunk;
+    } else {
+        const int group = a.G * a.Nq, r = (int)(row % group);
+        const ExactSeq seq(a, (int)(row / group) / a.Hkv);
+        if (r % a.Nq >= seq.ql) return;
+        const int r0 = r / kHeld * kHeld;
+        const int all = exact_most(seq, r0, min(r0 + kHeld, group), a.Nq);
+        parts = (all + split.chunk - 1) / split.chunk;
+    }
+    if (parts < 2) return;
+#pragma unroll
+    for (int w = 0; w < n; ++w) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 0; p < parts; ++p) {
+            const float4 v = *reinterpret_cast<const float4 *>(
+                split.o + ((p * split.rows + row) * n + w) * D + c);
+            o.x += v.x;
+            o.y += v.y;
+            o.z += v.z;
+            o.w += v.w;
+        }
+        const float f = w ? 1.0f : a.scale;
+        T *to = (T *)(w ? a.dv : KEYS ? a.dk : a.dq) + row * D + c;
+        store2(to, make_float2(o.x * f, o.y * f));
+        store2(to + 2, make_float2(o.z * f, o.w * f));
     }
 }
 
@@ -473,20 +558,32 @@ cudaError_t by_type(const ExactView &a, F f) {
 
 namespace {
 
-// Eight CTAs for each of a GB300's 152 SMs, two tiles of keys in a chunk at
-// least. (By the sizes alone: the workspace does not depend on the device.)
-Split divide_keys(const ExactView &a) {
-    const long tiles = ((long)a.G * a.Nq + kHeld - 1) / kHeld;
-    const long items = tiles * a.B * a.Hkv;
-    const long passes = ((long)a.Nk + kPass - 1) / kPass;
-    long n = (8 * 152 + items - 1) / items;
+// Walks of `passing` rows of `rows` held ones in `tiles` tiles: chunks so that
+// there are eight CTAs for each of a GB300's 152 SMs, of two tiles at least. (By
+// the sizes alone: the workspace does not depend on the device.)
+Split divide(long tiles, long passing, size_t rows) {
+    const long passes = (passing + kPass - 1) / kPass;
+    long n = (8 * 152 + tiles - 1) / tiles;
     if (n > passes / 2) n = passes / 2;
     if (n < 1) n = 1;
     Split s = {};
     s.chunk = (int)((passes + n - 1) / n) * kPass;
-    s.splits = (int)(((long)a.Nk + s.chunk - 1) / s.chunk);
-    s.rows = (size_t)a.B * a.H * a.Nq;
+    s.splits = (int)((passing + s.chunk - 1) / s.chunk);
+    s.rows = rows;
     return s;
+}
+long query_tiles(const ExactView &a) {
+    return ((long)a.G * a.Nq + kHeld - 1) / kHeld;
+}
+Split divide_keys(const ExactView &a) {
+    return divide(query_tiles(a) * a.B * a.Hkv, a.Nk,
+                  (size_t)a.B * a.H * a.Nq);
+}
+// dK, dV: the rows of every head in tiles of their own
+Split divide_queries(const ExactView &a) {
+    return divide((long)((a.Nk + kHeld - 1) / kHeld) * a.B * a.Hkv,
+                  a.G * (((long)a.Nq + kPass - 1) / kPass) * kPass,
+                  (size_t)a.B * a.Hkv * a.Nk);
 }
 
 }  // namespace
@@ -519,21 +616,36 @@ cudaError_t launch_exact_fwd_simt(const ExactView &a, float *part,
     });
 }
 
-cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys,
+size_t exact_add_bytes(const ExactView &a) {
+    const Split q = divide_keys(a), k = divide_queries(a);
+    const size_t x = q.splits > 1 ? q.splits * q.rows : 0;
+    const size_t y = k.splits > 1 ? 2 * k.splits * k.rows : 0;
+    return sizeof(float) * a.d * (x > y ? x : y);
+}
+
+cudaError_t launch_exact_bwd_simt(const ExactView &a, bool keys, float *part,
                                   cudaStream_t st) {
-    const long rows = keys ? a.Nk : (long)a.G * a.Nq;
-    const int tiles = (int)((rows + kHeld - 1) / kHeld);
-    const dim3 grid((unsigned)((long)tiles * a.B * a.Hkv));
+    Split split = keys ? divide_queries(a) : divide_keys(a);
+    split.o = part;
+    const long tiles = keys ? (a.Nk + kHeld - 1) / kHeld : query_tiles(a);
+    const dim3 grid((unsigned)(tiles * a.B * a.Hkv * split.splits));
     const size_t smem =
         sizeof(float) * (2 * kHeld * a.d + 2 * kPass * (a.d + 4) +
                          (keys ? 2 : 1) * kHeld * kPass + 3 * kPass);
     return by_type(a, [&](auto t, auto dim) {
         using T = decltype(t);
         constexpr int D = decltype(dim)::value;
-        return keys ? launch_after(k_exact_bwd<T, D, true>, grid, kThreads,
-                                   smem, st, a, tiles)
-                    : launch_after(k_exact_bwd<T, D, false>, grid, kThreads,
-                                   smem, st, a, tiles);
+        const dim3 rows((unsigned)((split.rows * (D / 4) + 255) / 256));
+        auto run = [&](auto which) {
+            constexpr bool K = decltype(which)::value;
+            cudaError_t e = launch_after(k_exact_bwd<T, D, K>, grid, kThreads,
+                                         smem, st, a, split, (int)tiles);
+            if (e == cudaSuccess && split.splits > 1)
+                e = launch_after(k_exact_add<T, D, K>, rows, 256, 0, st, a,
+                                 split);
+            return e;
+        };
+        return keys ? run(std::true_type{}) : run(std::false_type{});
     });
 }
 

@@ -440,3 +440,11 @@ def test_the_workspace_is_large_enough(H, Hkv, Nq, Nk, d, padded):
     # weights of 2^-8 and sums of thousands of terms, in fp32 or bf16
     scale = (p.transpose(2, 3) @ do.double().abs().view(1, Hkv, -1, d))
     assert bool(((g[2].double() - dv).abs() <= 2.0 ** -6 * scale).all())
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,causal,ql,kl", [
+    (1, 4, 1, 200, 600, 1, None, None), (2, 6, 2, 150, 400, 0, [150, 40],
+                                         [1, 400])])
+def test_divided_walks_on_the_cuda_cores(B, H, Hkv, Nq, Nk, causal, ql, kl, d):
+    run_case(B, H, Hkv, Nq, Nk, d, F32, causal, ql=ql, kl=kl)
