@@ -9,6 +9,12 @@
 // dQ in memory, no atomics, the same bits on every call. With fewer items than
 // places for CTAs the walks are divided too, and k_exact_sum adds up, in order,
 // what the parts leave.
+//
+// What bounds them. At D = 128 the products and the shared memory that feeds
+// them: tensor pipe 73 % (dQ) and 67 % (dK, dV). B4 H12 N4096 causal: both 490 us,
+// 1.06 PFLOP/s counting five products, 0.55 of the measured bf16 rate. For D <= 64
+// the weights' warps, whose steps of a tile stand one behind the other: B4 H12
+// N4096 d64 causal, dQ 134 us, dK and dV 203.
 #include <type_traits>
 
 #include "device_common.cuh"

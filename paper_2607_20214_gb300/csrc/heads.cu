@@ -10,7 +10,8 @@
 //     out = r (x A + x' B),  A = w cos a,  B = +-w' sin a,
 // x' the pair's other channel (of lane +- dim / 2 VE, or next to x), r the
 // head's 1 / sqrt(mean x^2 + eps). Memory bound: every row is read once and
-// every head written once.
+// every head written once. B2 H16 N16384 d128 bf16 136 us, 5.9 TB/s, 0.88 of the
+// measured copy rate; backward B8 H12 N8192 d64 from fp32 gradients 210 us, 0.79.
 #include <stdlib.h>
 
 #include <type_traits>
