@@ -299,8 +299,10 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                             skvh = 0;
                             // the next sequence that has rows (the last
                             // one's end is that of the last share)
-                            while (sb < a.B - 1 && upto[++sb] == upto[sb - 1])
-                                ;
+                            while (sb < a.B - 1) {
+                                ++sb;
+                                if (upto[sb] != upto[sb - 1]) break;
+                            }
                         }
                     }
                     if (all == 0) continue;

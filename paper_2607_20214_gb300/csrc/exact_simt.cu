@@ -8,11 +8,12 @@
 // operands in shared memory as fp32. Thread (y, x) of 8 x 16 computes the
 // scores of rows 4 y .. 4 y + 3 with x, x + 16, x + 32, x + 48, and of the sums
 // the same rows with d / 16 channels. Every four channels cost 8 16-byte reads
-// from shared memory for 64 multiply-adds (32 packed ones): bound by the
-// CUDA cores' multiply-adds. With few tiles of held rows the walks are divided
-// into chunks, and k_exact_join and k_exact_add add up, in order, what these
-// leave. B8 H8 N1000 d64 fp32 465 us forward, 35 TFLOP/s of 74; its backward pass
-// 1524, 27.
+// from shared memory for 64 multiply-adds (32 packed ones). Shared memory's
+// wavefronts run at 64 % of their peak, the multiply-adds at 46 %: B8 H8 N1000
+// d64 fp32 465 us forward, 35 TFLOP/s of 74; its backward pass 1524, 27. (8 rows a
+// thread, or warps of 4 x 8, save wavefronts and were no faster.) With few
+// tiles of held rows the walks are divided into chunks, and k_exact_join and
+// k_exact_add add up, in order, what these leave.
 #include <type_traits>
 
 #include "device_common.cuh"

@@ -30,7 +30,7 @@ constexpr int kDevSortRange = 1;     // a scatter position fell outside [0, N)
 constexpr int kDevPermRange = 2;     // a permutation entry fell outside [0, N)
 constexpr int kDevWaitTimeout = 3;   // a bounded mbarrier wait ran out
 constexpr int kDevTmem = 4;          // tensor-memory allocation failed
-constexpr int kDevLayout = 5;        // shared memory begins elsewhere
+constexpr int kDevLayout = 7;        // shared memory begins elsewhere (5, 6: cache.h)
 
 // The CTA (of `grid` over `total` work items, CTA c taking items
 // [total c / grid, total (c + 1) / grid)) that works on item t.
