@@ -43,7 +43,7 @@ typedef struct elsaa_exact {
     int d_h;         /* 32, 64 or 128                                        */
     int dtype;       /* ELSAA_BF16 or ELSAA_FP32, of every tensor but lse    */
     int causal;
-    float scale;     /* score scale; 0 -> 1/sqrt(d_h)                        */
+    float scale;     /* score scale, at most 1e38; 0 -> 1/sqrt(d_h)         */
     int impl;        /* ELSAA_IMPL_AUTO (bf16 on the tensor cores) or
                         ELSAA_IMPL_SIMT                                      */
 } elsaa_exact;

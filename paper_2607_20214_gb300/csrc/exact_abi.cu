@@ -42,8 +42,9 @@ int make_view(const elsaa_exact *p, ExactView *a) {
         return bad("causal must be 0 or 1");
     if (p->impl != ELSAA_IMPL_AUTO && p->impl != ELSAA_IMPL_SIMT)
         return bad("impl must be AUTO or SIMT");
-    if (!(p->scale >= 0.f) || !isfinite(p->scale))
-        return bad("scale must be finite and >= 0");
+    // (times log2 e it must still be finite)
+    if (!(p->scale >= 0.f && p->scale <= 1e38f))
+        return bad("scale must be at least 0 and at most 1e38");
     if (p->d_h != 32 && p->d_h != 64 && p->d_h != 128)
         return no("d_h must be 32, 64 or 128");
     if (p->H > 65535) return no("H must be at most 65535");

@@ -57,7 +57,8 @@ EXACT_BAD = [
     (dict(causal=2), INV, "causal"), (dict(impl=3), INV, "impl"),
     (dict(scale=-1.0), INV, "scale"),
     (dict(scale=float("inf")), INV, "scale"),
-    (dict(scale=float("nan")), INV, "scale"), (dict(d_h=96), UNS, "d_h"),
+    (dict(scale=float("nan")), INV, "scale"),
+    (dict(scale=2e38), INV, "scale"), (dict(d_h=96), UNS, "d_h"),
     (dict(N_q=1 << 29), UNS, "2^30"), (dict(N_k=1 << 30), UNS, "2^30"),
     (dict(B=1 << 30, H=1 << 15, H_kv=1 << 15), UNS, "2^30"),
     (dict(H=1 << 16, H_kv=1 << 16), UNS, "65535"),
