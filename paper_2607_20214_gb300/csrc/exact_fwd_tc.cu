@@ -509,10 +509,11 @@ __global__ void __launch_bounds__(kEfThreads, 1)
         } else if (!kAhead && warp == 8) {
             // ---------------------------------------------------- MMA issue
             // Whenever half of a slot's P is ready: that half of its P V
-            // product; then the other half, and right behind it the scores of its next key tile; the softmax sees these only
-            // when both are complete (a commit covers all that was issued
-            // before it). At D = 128 the scores go over P, which relies on
-            // products of one thread running in the order of their issue.
+            // product; then the other half, and right behind it the scores of
+            // its next key tile; the softmax sees these only when both are
+            // complete (a commit covers all that was issued before it). The
+            // scores go over P, which relies on products of one thread
+            // running in the order of their issue.
             // The whole warp runs the loop, so that its state and the
             // operands' descriptors are warp-uniform; one lane issues.
             const bool el = elect_one();
@@ -578,7 +579,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                                 int n_o) {
                     constexpr int s = decltype(slot)::value;
                     constexpr uint32_t cO = 128u * s + 256u;
-                    constexpr uint32_t cP = D <= 64 ? cO + 64 : 128u * s;
+                    constexpr uint32_t cP = 128u * s;
                     const int st = (c0 + up) % kV;
                     if (up == us) return false;
                     const uint64_t v = dV + st * kTile;
