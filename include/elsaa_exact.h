@@ -88,9 +88,9 @@ int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
  *     dK = scale dS^T Q,
  * summed over the query heads of a K/V head in a fixed order: a call gives the
  * same bits every time. Rows behind the lengths are left as they were; those
- * of queries that see nothing and of keys that no query sees are zeros. bf16 on
- * the tensor cores: P and dS in fp32, each rounded to bf16 for its products,
- * sums in fp32, results rounded once.
+ * of queries that see nothing and of keys that no query sees are zeros; a query
+ * with lse = -inf has weights of 0. bf16 on the tensor cores: P and dS in fp32,
+ * each rounded to bf16 for its products, sums in fp32, results rounded once.
  */
 int elsaa_exact_backward(const elsaa_exact *exact, const void *q,
                          const void *k, const void *v, const void *o,

@@ -72,6 +72,13 @@ struct ExactSeq {
     }
 };
 
+// A row without a weight above 0 has lse = -inf: as +inf it makes
+// exp(s - lse) = 0 also where scores of finite q and k overflow to -inf.
+__device__ __forceinline__ float exact_lse(const float *lse) {
+    const float x = *lse;
+    return x == -INFINITY ? INFINITY : x;
+}
+
 // Rows of the query heads that share a K/V head, counted through: row r is row
 // r mod N of head r / N of the group. `most` is the largest seen() among rows
 // [r0, r1).

@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
             if (valid) {
                 seen = a.causal ? max(0, min(w.kl, i + 1 + w.kl - w.ql))
                                 : w.kl;
-                nl = -a.lse[at] * kLog2e;
+                nl = -exact_lse(a.lse + at) * kLog2e;
                 nd = -a.delta[at];
             }
             const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(nd, nd);
@@ -898,7 +898,7 @@ __global__ void __launch_bounds__(Eb<D>::threads, Eb<D>::ctas)
                         const int i = lane_id + 32 * q;
                         l[q] = d[q] = 0.0f;
                         if (i0 + i < w.ql) {
-                            l[q] = a.lse[at + i];
+                            l[q] = exact_lse(a.lse + at + i);
                             d[q] = a.delta[at + i];
                         }
                     }

@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kThreads)
             lse2[i] = 0.f;
             if (valid(r)) {
                 seen[i] = seq.seen((r0 + r) % a.Nq);
-                lse2[i] = a.lse[qrow + r0 + r] * kLog2e;
+                lse2[i] = exact_lse(a.lse + qrow + r0 + r) * kLog2e;
                 if (x == 0 && it.part == 0)
                     a.delta[qrow + r0 + r] = delta[i];
             }
@@ -440,7 +440,8 @@ __global__ void __launch_bounds__(kThreads)
                 load_rows<T, D>(sE, D + 4, dO + at * D, kPass, have);
                 if (threadIdx.x < kPass) {
                     const int r = threadIdx.x;
-                    sL[r] = have(r) ? a.lse[qrow + at + r] * kLog2e : 0.f;
+                    sL[r] = have(r) ? exact_lse(a.lse + qrow + at + r) * kLog2e
+                                    : 0.f;
                     sD[r] = have(r) ? a.delta[qrow + at + r] : 0.f;
                     sN[r] = seq.seen(i0 + r);
                 }

@@ -156,6 +156,38 @@ def test_scores_of_minus_infinity_are_no_weight(dtype, impl):
     assert not o.any() and (lse == -math.inf).all()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("dtype,impl", KINDS)
+def test_gradients_where_finite_rows_score_minus_infinity(dtype, impl, d,
+                                                          causal):
+    """A query whose scores with every key overflow has no weights: its
+    gradient is 0, and the others' are those without it (in the same order,
+    so the same bits)."""
+    q, k, v, do = C.exact_inputs(1, 2, 1, 70, 150, d, dtype)
+    q[..., 0] = 0
+    k[..., 0] = -1e20
+    ex = E.make_exact(1, 2, 1, 70, 150, d, dtype=NAME[dtype], causal=causal,
+                      impl=impl)
+
+    def run(q, do):
+        x = [t.cuda() for t in (q, k, v)]
+        lse = torch.empty((1, 2, 70), device="cuda")
+        o = E.elsaa_exact_forward(ex, *x, lse=lse)
+        return o, lse, E.elsaa_exact_backward(ex, *x, o, lse, do.cuda())
+    q1 = q.clone()
+    q1[0, 1, 5, 0] = 1e20
+    o, lse, got = run(q1, do)
+    assert not o[0, 1, 5].any() and lse[0, 1, 5] == -math.inf
+    do[0, 1, 5] = 0
+    o0, lse0, want = run(q, do)
+    assert lse0[0, 1, 5] > -math.inf
+    assert not got[0][0, 1, 5].any()
+    want[0][0, 1, 5] = 0
+    for x, y in zip(got, want):
+        assert torch.equal(x, y) and x.isfinite().all()
+
+
 def test_infinite_scores_do_not_reach_other_rows():
     q, k, v, _ = (x.cuda() for x in C.exact_inputs(1, 2, 1, 200, 200, 64, BF))
     ex = E.make_exact(1, 2, 1, 200, 200, 64)
