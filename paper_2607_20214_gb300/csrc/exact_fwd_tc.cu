@@ -105,7 +105,9 @@ struct EfShares {
 
 // Units of item t of sequence `seq`, none if it has no row.
 __device__ __forceinline__ int ef_weight(const ExactSeq &seq,
-                                         const ExactOrder &order, int t) {
+                                         const ExactOrder &batch, int t) {
+    const ExactOrder order = batch.of(seq.ql);
+    if (t >= order.groups * order.per) return 0;
     const int r0 = order.tile(t) * 256, r1 = min(r0 + 256, order.rows);
     if (r0 >= r1 || seq.ql == 0) return 0;
     if (r0 / order.pitch == (r1 - 1) / order.pitch &&
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             int c = 0;   // key tiles loaded so far
             int qs[2] = {0, 0};  // items whose queries were loaded
             bool ok = true;
-            const int heads = a.B * a.Hkv, rows = order.rows;
+            const int heads = a.B * a.Hkv;
             EfRecord rec = {0, 0, 0, -1};
             long unit = W * blockIdx.x / C;
             // the next item, of key tiles [kt0, kt1)
@@ -271,16 +273,18 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 w.item = 0;
                 w.b = b;
                 w.kvh = kvh;
-                w.r0 = order.tile(t) * 256;
                 w.kt0 = kt0;
                 w.part = -1;
                 const ExactSeq seq(a, b);
                 w.ql = seq.ql;
                 w.kl = seq.kl;
+                const ExactOrder own = order.of(seq.ql);
+                w.r0 = (t < own.groups * own.per ? own.tile(t)
+                                                 : own.groups * own.per) * 256;
                 for (int s = 0; s < 2; ++s) {
                     const int r = w.r0 + 128 * s;
-                    const int n = (exact_most(seq, r, min(r + 128, rows),
-                                              order.pitch) + 127) / 128;
+                    const int n = (exact_most(seq, r, min(r + 128, own.rows),
+                                              own.pitch) + 127) / 128;
                     w.n[s] = max(0, min(n, kt1) - kt0);
                 }
             };
@@ -364,6 +368,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                 const int q0 = (w.b * a.H + w.kvh * a.G) * a.Nq;
                 const int k0 =
                     (w.b * a.Hkv + w.kvh) * a.Nk + 128 * w.kt0;
+                const ExactOrder own = order.of(w.ql);
                 int kt = 0;
                 for (int s = 0; s < 2 && ok; ++s) {
                     if (w.n[s] == 0) continue;
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
                     mbar_expect_tx(&bars.q_full[s], kTileB);
                     for (int p = 0; p < kPanels; ++p)
                         tma_load_2d(sQ + s * kTileB + p * 16384, &tmQ, 64 * p,
-                                    q0 + order.row(w.r0 + 128 * s, a.Nq),
+                                    q0 + own.row(w.r0 + 128 * s, a.Nq),
                                     &bars.q_full[s]);
                     if (kt == 0) {
                         ok = load(bars.k_full, bars.k_empty, c, kK, sK, &tmK,
@@ -696,8 +701,9 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             __syncwarp();
             if (lane_id == 0) mbar_arrive(&bars.item_empty[it & 1]);
             if (item < 0) break;
-            const int r = slot0 + row, i = r % order.pitch;
-            const bool valid = r < order.rows && i < ql;
+            const ExactOrder own = order.of(ql);
+            const int r = slot0 + row, i = r % own.pitch;
+            const bool valid = r < own.rows && i < ql;
             int seen = 0;
             if (valid)
                 seen = a.causal ? max(0, min(kl, i + 1 + kl - ql))
@@ -803,8 +809,7 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             }
             if (!ok) break;
             const size_t at =
-                (size_t)(wb * a.H + kvh * a.G) * a.Nq +
-                order.row(r, a.Nq);
+                (size_t)(wb * a.H + kvh * a.G) * a.Nq + own.row(r, a.Nq);
             uint16_t *o = (uint16_t *)a.out + at * D;
             if (n > 0) {
                 ok = wwait(&bars.o_done[s], (g - 1) & 1, 410);
@@ -879,9 +884,9 @@ __global__ void __launch_bounds__(256)
     int c;
     const int row = (int)piece_of<D>(blockIdx.x * 256 + threadIdx.x, &c);
     const int r = rec.r0 + row;
-    if (r >= order.rows ||
-        r % order.pitch >= ExactSeq(a, rec.b).ql)
-        return;
+    const int ql = ExactSeq(a, rec.b).ql;
+    const ExactOrder own = order.of(ql);
+    if (r >= own.rows || r % own.pitch >= ql) return;
     auto at = [&](int cta) { return (size_t)(2 * cta + (cta == first)); };
     float m = kLowest;
     for (int p = first; p <= rec.last; ++p)
@@ -901,7 +906,7 @@ __global__ void __launch_bounds__(256)
         for (int i = 0; i < 8; ++i) o[i] = fmaf(e[i], f, o[i]);
     }
     const size_t to = (size_t)(rec.b * a.H + rec.kvh * a.G) * a.Nq +
-                      order.row(r, a.Nq);
+                      own.row(r, a.Nq);
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     uint32_t y[4];
 #pragma unroll

@@ -156,6 +156,34 @@ def test_scores_of_minus_infinity_are_no_weight(dtype, impl):
     assert not o.any() and (lse == -math.inf).all()
 
 
+@pytest.mark.parametrize("G,Nq", [(2, 300), (1, 1000), (3, 129)])
+def test_many_padded_sequences(G, Nq):
+    """More items than are divided into shares, of sequences that need fewer
+    tiles than the batch: every row is written, some sequences against the
+    oracle, and nothing behind the lengths."""
+    B, Hkv, d, Nk = 90, 8, 32, 260
+    q, k, v, _ = C.exact_inputs(B, Hkv * G, Hkv, Nq, Nk, d, BF)
+    ql = [(b * 37) % (Nq + 1) for b in range(B)]
+    kl = [(b * 101) % (Nk + 1) for b in range(B)]
+    ql[1], ql[2], kl[3] = 128, Nq, Nk
+    ex = E.make_exact(B, Hkv * G, Hkv, Nq, Nk, d, causal=True)
+    o = torch.full(q.shape, 7.0, dtype=BF, device="cuda")
+    lse = torch.full(q.shape[:3], math.nan, device="cuda")
+    E.elsaa_exact_forward(ex, q.cuda(), k.cuda(), v.cuda(), o=o, lse=lse,
+                          q_len=lens(ql, B), k_len=lens(kl, B))
+    for b in range(B):
+        n = ql[b]
+        assert not lse[b, :, :n].isnan().any()
+        assert lse[b, :, n:].isnan().all() and (o[b, :, n:] == 7).all()
+    for b in (1, 2, 3, 40):
+        one = [x[b:b + 1] for x in (q, k, v)]
+        ref = C.exact_forward_ref(*one, 1 / math.sqrt(d), True, [ql[b]],
+                                  [kl[b]], True)
+        for (_, h), r in ref.items():
+            C.close(o[b, h, :ql[b]], r["o"], r["o_tol"], ("o", b, h))
+            C.close(lse[b, h, :ql[b]], r["lse"], r["lse_tol"], ("lse", b, h))
+
+
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("d", [32, 64, 128])
 @pytest.mark.parametrize("dtype,impl", KINDS)
