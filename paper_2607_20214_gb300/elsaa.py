@@ -106,7 +106,30 @@ class elsaa_rotary(ctypes.Structure):
     ]
 
 
-class elsaa_heads(ctypes.Structure):
+class _Described(ctypes.Structure):
+    """A structure whose fields say all that a call checks its tensors by.
+
+    _of works that out; it is kept beside the bytes that it came from, and
+    looked up by them, so that a copy or a structure with an edited field (or
+    whose memory was written in another way) is what its fields say. ref is
+    the structure's own address, a copy's that of the copy.
+    """
+    _known = (None, None)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self)
+
+    def facts(self):
+        now = bytes(self)
+        known, facts = self._known
+        if known != now:
+            facts = self._of()
+            self._known = now, facts
+        return facts
+
+
+class elsaa_heads(_Described):
     """Mirror of struct elsaa_heads; make_heads fills it."""
     _fields_ = [
         ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
@@ -116,6 +139,17 @@ class elsaa_heads(ctypes.Structure):
         ("rotary", elsaa_rotary),
     ]
 
+    def _of(self):
+        """Types of rows and heads and of the heads' gradients; shapes of the
+        rows of q and of k and v, of their heads, of weights, lengths and
+        positions."""
+        dt = _torch_dtype(self.dtype)
+        B, H, N, d = self.B, self.H, self.N, self.d_h
+        kv = H if self.expand else self.H_kv
+        return (dt, torch.float32 if self.grad_fp32 else dt,
+                (B, N, H, d), (B, N, self.H_kv, d), (B, H, N, d),
+                (B, kv, N, d), (d,), (B,), (self.rotary.axes, B, N))
+
 
 class elsaa_rows(ctypes.Structure):
     """Mirror of struct elsaa_rows (strides in elements)."""
@@ -123,7 +157,7 @@ class elsaa_rows(ctypes.Structure):
                 ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
-class elsaa_exact(ctypes.Structure):
+class elsaa_exact(_Described):
     """Mirror of struct elsaa_exact; make_exact fills it."""
     _fields_ = [
         ("B", ctypes.c_int), ("H", ctypes.c_int), ("H_kv", ctypes.c_int),
@@ -131,6 +165,12 @@ class elsaa_exact(ctypes.Structure):
         ("dtype", ctypes.c_int), ("causal", ctypes.c_int),
         ("scale", ctypes.c_float), ("impl", ctypes.c_int),
     ]
+
+    def _of(self):
+        """Type of the tensors; shapes of q, of k and v, of lse, of lengths."""
+        B, H, Nq = self.B, self.H, self.N_q
+        return (_torch_dtype(self.dtype), (B, H, Nq, self.d_h),
+                (B, self.H_kv, self.N_k, self.d_h), (B, H, Nq), (B,))
 
 
 class ElsaaError(RuntimeError):
@@ -1011,20 +1051,12 @@ def make_rotary(dim, base=10000.0, interleaved=False, sections=None,
 def make_heads(B, H, H_kv, N, d_h, dtype="bf16", norm=True, rotary=None,
                expand=False, grad_fp32=False, eps=1e-6) -> elsaa_heads:
     """What elsaa_heads_forward and elsaa_heads_backward are about (fields:
-    include/elsaa_heads.h). rotary: as make_rotary returns it, or None."""
-    code = _dtype_code(dtype)
-    h = elsaa_heads(B, H, H_kv, N, d_h, code, int(bool(norm)),
-                    int(bool(expand)), int(bool(grad_fp32)), eps,
-                    make_rotary(0) if rotary is None else rotary)
-    h.ref = ctypes.byref(h)
-    h.torch_dtype = _torch_dtype(code)
-    h.grad_dtype = torch.float32 if grad_fp32 else h.torch_dtype
-    kv = H if expand else H_kv
-    h.rows = (B, N, H, d_h), (B, N, H_kv, d_h)
-    h.out = (B, H, N, d_h), (B, kv, N, d_h)
-    h.axes = h.rotary.axes
-    h.weights, h.batch = (d_h,), (B,)
-    return h
+    include/elsaa_heads.h; a call goes by what they are then). rotary: as
+    make_rotary returns it (copied), or None."""
+    return elsaa_heads(B, H, H_kv, N, d_h, _dtype_code(dtype),
+                       int(bool(norm)), int(bool(expand)),
+                       int(bool(grad_fp32)), eps,
+                       make_rotary(0) if rotary is None else rotary)
 
 
 def elsaa_heads_workspace_size(heads: elsaa_heads) -> int:
@@ -1109,11 +1141,10 @@ def _space(workspace, index):
     return workspace.data_ptr(), workspace.nbytes
 
 
-def _positions(heads, positions, index):
+def _positions(positions, shape, index):
     if positions is None:
         return None
-    shape = (heads.axes, heads.B, heads.N)
-    if heads.axes == 1 and positions.dim() == 2:
+    if shape[0] == 1 and positions.dim() == 2:
         shape = shape[1:]
     return _whole(positions, "positions", torch.int32, shape, index)
 
@@ -1126,10 +1157,8 @@ def elsaa_heads_forward(heads: elsaa_heads, q=None, k=None, v=None, w_q=None,
     wanted) to normed and rotated heads. Returns (q_out, k_out, v_out),
     allocated here when not given (rows behind new_len then undefined)."""
     on = _index(q if q is not None else k if k is not None else v, "q")
-    dt, f32, i32 = heads.torch_dtype, torch.float32, torch.int32
-    w, B = heads.weights, heads.batch
-    rq, rk = heads.rows
-    oq, ok = heads.out
+    f32, i32 = torch.float32, torch.int32
+    dt, _, rq, rk, oq, ok, w, B, at = heads.facts()
     rows_q = _strided(q, "q", dt, rq, on)
     rows_k = _strided(k, "k", dt, rk, on)
     rows_v = _strided(v, "v", dt, rk, on)
@@ -1145,7 +1174,7 @@ def elsaa_heads_forward(heads: elsaa_heads, q=None, k=None, v=None, w_q=None,
                                    new(v, v_out, ok))
     _check(load_library().elsaa_heads_forward(
         heads.ref, rows_q, rows_k, rows_v, _whole(w_q, "w_q", f32, w, on),
-        _whole(w_k, "w_k", f32, w, on), _positions(heads, positions, on),
+        _whole(w_k, "w_k", f32, w, on), _positions(positions, at, on),
         _whole(lengths, "lengths", i32, B, on),
         _whole(new_len, "new_len", i32, B, on),
         _whole(q_out, "q_out", dt, oq, on), _whole(k_out, "k_out", dt, ok, on),
@@ -1164,10 +1193,8 @@ def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
     (rows behind new_len then undefined); dw_q and dw_k likewise where the
     weights are given."""
     on = _index(dq if dq is not None else dk if dk is not None else dv, "dq")
-    dt, gt, f32 = heads.torch_dtype, heads.grad_dtype, torch.float32
-    i32, w, B = torch.int32, heads.weights, heads.batch
-    rq, rk = heads.rows
-    oq, ok = heads.out
+    f32, i32 = torch.float32, torch.int32
+    dt, gt, rq, rk, oq, ok, w, B, at = heads.facts()
     if w_q is not None and dw_q is None and dq is not None or \
             w_k is not None and dw_k is None and dk is not None or \
             dq is not None and dq_rows is None or \
@@ -1194,7 +1221,7 @@ def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
         heads.ref, _whole(dq, "dq", gt, oq, on), _whole(dk, "dk", gt, ok, on),
         _whole(dv, "dv", gt, ok, on), _strided(q, "q", dt, rq, on),
         _strided(k, "k", dt, rk, on), _whole(w_q, "w_q", f32, w, on),
-        _whole(w_k, "w_k", f32, w, on), _positions(heads, positions, on),
+        _whole(w_k, "w_k", f32, w, on), _positions(positions, at, on),
         _whole(lengths, "lengths", i32, B, on),
         _whole(new_len, "new_len", i32, B, on),
         _strided(dq_rows, "dq_rows", dt, rq, on),
@@ -1208,15 +1235,9 @@ def elsaa_heads_backward(heads: elsaa_heads, dq=None, dk=None, dv=None,
 def make_exact(B, H, H_kv, N_q, N_k, d_h, dtype="bf16", causal=False,
                scale=0.0, impl=ELSAA_IMPL_AUTO) -> elsaa_exact:
     """What elsaa_exact_forward and elsaa_exact_backward are about (fields:
-    include/elsaa_exact.h)."""
-    code = _dtype_code(dtype)
-    e = elsaa_exact(B, H, H_kv, N_q, N_k, d_h, code, int(bool(causal)), scale,
-                    impl)
-    e.ref = ctypes.byref(e)
-    e.torch_dtype = _torch_dtype(code)
-    e.q, e.kv, e.rows = ((B, H, N_q, d_h), (B, H_kv, N_k, d_h), (B, H, N_q))
-    e.batch = (B,)
-    return e
+    include/elsaa_exact.h; a call goes by what they are then)."""
+    return elsaa_exact(B, H, H_kv, N_q, N_k, d_h, _dtype_code(dtype),
+                       int(bool(causal)), scale, impl)
 
 
 def elsaa_exact_workspace_size(exact: elsaa_exact, backward=False) -> int:
@@ -1240,21 +1261,22 @@ def elsaa_exact_forward(exact: elsaa_exact, q, k, v, q_len=None, k_len=None,
     [B, H_kv, N_k, d_h]. Returns o (allocated here when not given, rows behind
     q_len then undefined); lse [B, H, N_q] fp32 is written when given."""
     on = _index(q, "q")
-    dt, i32, B = exact.torch_dtype, torch.int32, exact.batch
+    i32 = torch.int32
+    dt, rows, kv, row, B = exact.facts()
     if o is None or workspace is None:
         own = _On(on)
         with _own(stream, own):
             if o is None:
-                o = torch.empty(exact.q, dtype=dt, device=own.device)
+                o = torch.empty(rows, dtype=dt, device=own.device)
             if workspace is None:
                 workspace = new_exact_workspace(exact, own.device)
     ws, nbytes = _space(workspace, on)
     _check(load_library().elsaa_exact_forward(
-        exact.ref, _whole(q, "q", dt, exact.q, on),
-        _whole(k, "k", dt, exact.kv, on), _whole(v, "v", dt, exact.kv, on),
+        exact.ref, _whole(q, "q", dt, rows, on),
+        _whole(k, "k", dt, kv, on), _whole(v, "v", dt, kv, on),
         _whole(q_len, "q_len", i32, B, on), _whole(k_len, "k_len", i32, B, on),
-        _whole(o, "o", dt, exact.q, on),
-        _whole(lse, "lse", torch.float32, exact.rows, on), ws, nbytes,
+        _whole(o, "o", dt, rows, on),
+        _whole(lse, "lse", torch.float32, row, on), ws, nbytes,
         _raw(stream, on)))
     return o
 
@@ -1266,26 +1288,26 @@ def elsaa_exact_backward(exact: elsaa_exact, q, k, v, o, lse, d_o, q_len=None,
     o and lse of elsaa_exact_forward. Returns (dq, dk, dv), allocated here when
     not given (rows behind q_len and k_len then undefined)."""
     on = _index(q, "q")
-    dt, i32, B = exact.torch_dtype, torch.int32, exact.batch
+    i32 = torch.int32
+    dt, rows, kv, row, B = exact.facts()
     if dq is None or dk is None or dv is None or workspace is None:
         own = _On(on)
         with _own(stream, own):
             def new(out, shape):
                 return out if out is not None else torch.empty(
                     shape, dtype=dt, device=own.device)
-            dq, dk, dv = (new(dq, exact.q), new(dk, exact.kv),
-                          new(dv, exact.kv))
+            dq, dk, dv = new(dq, rows), new(dk, kv), new(dv, kv)
             if workspace is None:
                 workspace = new_exact_workspace(exact, own.device, True)
     ws, nbytes = _space(workspace, on)
     _check(load_library().elsaa_exact_backward(
-        exact.ref, _whole(q, "q", dt, exact.q, on),
-        _whole(k, "k", dt, exact.kv, on), _whole(v, "v", dt, exact.kv, on),
-        _whole(o, "o", dt, exact.q, on),
-        _whole(lse, "lse", torch.float32, exact.rows, on),
-        _whole(d_o, "d_o", dt, exact.q, on),
+        exact.ref, _whole(q, "q", dt, rows, on),
+        _whole(k, "k", dt, kv, on), _whole(v, "v", dt, kv, on),
+        _whole(o, "o", dt, rows, on),
+        _whole(lse, "lse", torch.float32, row, on),
+        _whole(d_o, "d_o", dt, rows, on),
         _whole(q_len, "q_len", i32, B, on), _whole(k_len, "k_len", i32, B, on),
-        _whole(dq, "dq", dt, exact.q, on), _whole(dk, "dk", dt, exact.kv, on),
-        _whole(dv, "dv", dt, exact.kv, on), ws, nbytes,
+        _whole(dq, "dq", dt, rows, on), _whole(dk, "dk", dt, kv, on),
+        _whole(dv, "dv", dt, kv, on), ws, nbytes,
         _raw(stream, on)))
     return dq, dk, dv
