@@ -67,11 +67,11 @@ int elsaa_exact_workspace_size(const elsaa_exact *exact, int backward,
  * lse      [B, H, N_q] fp32 (written), or NULL.
  *
  * bf16 on the tensor cores: scores and sums in fp32, weights (relative to a
- * reference within 2^8 of the row's largest) rounded to bf16 for their product
+ * reference within 2^9 of the row's largest) rounded to bf16 for their product
  * with V, their sum taken before that; o rounded once. A score below -6.9e37
- * counts as -inf. The results do not depend on timing, but the division of rows
- * over CTAs, and with it the last bits, depends on the sizes, the lengths and
- * the number of SMs.
+ * counts as -inf; with either dtype one above 2.3e38 is infinite. The results
+ * do not depend on timing, but the division of rows over CTAs, and with it the
+ * last bits, depends on the sizes, the lengths and the number of SMs.
  */
 int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
                         const void *k, const void *v, const int32_t *q_len,

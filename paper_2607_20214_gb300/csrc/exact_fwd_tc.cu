@@ -59,8 +59,19 @@ template <int D>
 constexpr int kEfK = D > 64 ? 3 : 4;
 template <int D>
 constexpr int kEfV = D > 64 ? 2 : 4;
-// a maximum below every score of a finite product
+// a score (base 2) of this or less counts as -inf
 constexpr float kLowest = -1e38f;
+// The reference of a row's weights is a rounded product, score * sl2, and
+// fma(score, sl2, -reference) does not round it: the largest weight comes out
+// as 2^d, d up to half a unit in the reference's last place. Up to 2^24 that is
+// 2^0.5, which the sum of the weights takes out again; behind 2^31 the weights
+// would overflow, or none be left. A warp that meets a reference behind 2^24
+// goes on in a second loop, where such rows have the reference's score
+// subtracted from the others before the product. The vote that it takes costs
+// 1 % (B1 H16 H_kv4 N16384 d128 causal 699 -> 707 us; single rows of 16384 keys
+// 101 -> 106); the subtraction in the same loop, behind a branch, 2 (715), and
+// padded chunks of 500 rows 61 instead of 57.
+constexpr float kFar = 16777216.0f;
 
 template <int D>
 struct EfBars {
@@ -708,105 +719,144 @@ __global__ void __launch_bounds__(kEfThreads, 1)
             if (valid)
                 seen = a.causal ? max(0, min(kl, i + 1 + kl - ql))
                                 : kl;
-            float mref = kLowest, lsum = 0.0f;
-            for (int kt = 0; kt < n; ++kt, ++g) {
-                ok = wwait(&bars.s_full[s], g & 1, 409);
-                if (!ok) break;
-                tc_fence_after();
-                float v[128];
-                {
-                    uint32_t x[32], b[32], c[32], e[32];
-                    tmem_ld32(tS, x);
-                    tmem_ld32(tS + 32, b);
-                    tmem_ld32(tS + 64, c);
-                    tmem_ld32(tS + 96, e);
-                    tmem_wait_ld();
+            // the reference; behind kFar the score that it comes from, else 0
+            float mref = kLowest, from = 0.0f, lsum = 0.0f;
+            auto refer = [&](float top, float z) {
+                mref = fmaxf(z, kLowest);
+                from = fabsf(z) > kFar && z > kLowest ? top : 0.0f;
+            };
+            int kt = 0;
+            // key tiles from kt on; without kFarRows up to the one with such a
+            // row's reference, which is read again
+            auto walk = [&](auto far_rows) {
+                constexpr bool kFarRows = decltype(far_rows)::value;
+                for (; kt < n; ++kt, ++g) {
+                    ok = wwait(&bars.s_full[s], g & 1, 409);
+                    if (!ok) break;
+                    tc_fence_after();
+                    float v[128];
+                    {
+                        uint32_t x[32], b[32], c[32], e[32];
+                        tmem_ld32(tS, x);
+                        tmem_ld32(tS + 32, b);
+                        tmem_ld32(tS + 64, c);
+                        tmem_ld32(tS + 96, e);
+                        tmem_wait_ld();
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) {
-                        v[q] = __uint_as_float(x[q]);
-                        v[32 + q] = __uint_as_float(b[q]);
-                        v[64 + q] = __uint_as_float(c[q]);
-                        v[96 + q] = __uint_as_float(e[q]);
-                    }
-                }
-                if (kAhead) warp_done(&bars.s_read[s]);
-                const int lim = seen - 128 * (kt0 + kt);
-                if (__any_sync(0xffffffffu, lim < 128)) {
-#pragma unroll
-                    for (int q = 0; q < 128; ++q)
-                        if (q >= lim) v[q] = -INFINITY;
-                }
-                float mx[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                for (int q = 4; q < 124; q += 8)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        mx[x] = max3(mx[x], v[q + 2 * x], v[q + 2 * x + 1]);
-                mx[0] = max3(mx[0], v[124], v[125]);
-                mx[1] = max3(mx[1], v[126], v[127]);
-                const float z =
-                    fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
-                if (kt == 0) {
-                    mref = fmaxf(z, kLowest);
-                } else {
-                    // P and O are free: the last tile's P V product is
-                    // complete (at D = 128 these scores were issued behind it
-                    // and it is complete when they are)
-                    if (kAhead) {
-                        ok = wwait(&bars.o_done[s], (g - 1) & 1, 417);
-                        if (!ok) break;
-                        tc_fence_after();
-                    }
-                    const bool need = z > mref + kGrown;
-                    if (__any_sync(0xffffffffu, need)) {
-                        const float f = need ? ex2_approx(mref - z) : 1.0f;
-                        const float2 f2 = make_float2(f, f);
-#pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(tO + c, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int q = 0; q < 32; q += 2) {
-                                const float2 y =
-                                    mul2(make_float2(__uint_as_float(o[q]),
-                                                     __uint_as_float(
-                                                         o[q + 1])),
-                                         f2);
-                                o[q] = __float_as_uint(y.x);
-                                o[q + 1] = __float_as_uint(y.y);
-                            }
-                            tmem_st32(tO + c, o);
+                        for (int q = 0; q < 32; ++q) {
+                            v[q] = __uint_as_float(x[q]);
+                            v[32 + q] = __uint_as_float(b[q]);
+                            v[64 + q] = __uint_as_float(c[q]);
+                            v[96 + q] = __uint_as_float(e[q]);
                         }
-                        lsum *= f;
-                        if (need) mref = z;
                     }
-                }
-                const float2 nm = make_float2(-mref, -mref);
-                float2 ls[2] = {make_float2(0.0f, 0.0f),
-                                make_float2(0.0f, 0.0f)};
+                    if (kAhead && kFarRows) warp_done(&bars.s_read[s]);
+                    const int lim = seen - 128 * (kt0 + kt);
+                    if (__any_sync(0xffffffffu, lim < 128)) {
 #pragma unroll
-                for (int c = 0; c < 128; c += 32) {
-                    uint32_t pw[16];
+                        for (int q = 0; q < 128; ++q)
+                            if (q >= lim) v[q] = -INFINITY;
+                    }
+                    float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-                    for (int q = 0; q < 32; q += 2) {
-                        const float2 x = fma2(
-                            make_float2(v[c + q], v[c + q + 1]), sl22, nm);
-                        const float2 p =
-                            make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                        ls[(q >> 1) & 1] = add2(ls[(q >> 1) & 1], p);
-                        pw[q >> 1] = pack_bf16x2(p.x, p.y);
+                    for (int q = 4; q < 124; q += 8)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            mx[x] = max3(mx[x], v[q + 2 * x], v[q + 2 * x + 1]);
+                    mx[0] = max3(mx[0], v[124], v[125]);
+                    mx[1] = max3(mx[1], v[126], v[127]);
+                    const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+                    // (rounded by itself, also where it is subtracted)
+                    const float z = __fmul_rn(top, sl2);
+                    bool need = kt == 0 ? z > -INFINITY : z >= mref + kGrown;
+                    if (!kFarRows) {
+                        if (__any_sync(0xffffffffu, need && fabsf(z) > kFar))
+                            return;
+                        if (kAhead) warp_done(&bars.s_read[s]);
                     }
-                    tmem_st16(tP + c / 2, pw);
-                    if (c == 32) {
-                        tmem_wait_st();
-                        warp_done(&bars.p_half[s]);
+                    if (kt == 0) {
+                        if (kFarRows)
+                            refer(top, z);
+                        else
+                            mref = fmaxf(z, kLowest);
+                    } else {
+                        // P and O are free: the last tile's P V product is
+                        // complete (at D = 128 these scores were issued
+                        // behind it and it is complete when they are)
+                        if (kAhead) {
+                            ok = wwait(&bars.o_done[s], (g - 1) & 1, 417);
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
+                        float less = mref - z;
+                        if (kFarRows && from != 0.0f) {
+                            need = top > from;
+                            less = (from - top) * sl2;
+                        }
+                        if (__any_sync(0xffffffffu, need)) {
+                            const float f = need ? ex2_approx(less) : 1.0f;
+                            const float2 f2 = make_float2(f, f);
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(tO + c, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int q = 0; q < 32; q += 2) {
+                                    const float2 y = mul2(
+                                        make_float2(__uint_as_float(o[q]),
+                                                    __uint_as_float(o[q + 1])),
+                                        f2);
+                                    o[q] = __float_as_uint(y.x);
+                                    o[q + 1] = __float_as_uint(y.y);
+                                }
+                                tmem_st32(tO + c, o);
+                            }
+                            lsum *= f;
+                            if (need) {
+                                if (kFarRows)
+                                    refer(top, z);
+                                else
+                                    mref = z;
+                            }
+                        }
                     }
+                    float nref = -mref;
+                    if (kFarRows) {
+                        nref = from != 0.0f     ? 0.0f
+                               : mref > kLowest ? -mref
+                                                : -INFINITY;
+#pragma unroll
+                        for (int q = 0; q < 128; ++q) v[q] -= from;
+                    }
+                    const float2 nm = make_float2(nref, nref);
+                    float2 ls[2] = {make_float2(0.0f, 0.0f),
+                                    make_float2(0.0f, 0.0f)};
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        uint32_t pw[16];
+#pragma unroll
+                        for (int q = 0; q < 32; q += 2) {
+                            const float2 x = fma2(
+                                make_float2(v[c + q], v[c + q + 1]), sl22, nm);
+                            const float2 p =
+                                make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                            ls[(q >> 1) & 1] = add2(ls[(q >> 1) & 1], p);
+                            pw[q >> 1] = pack_bf16x2(p.x, p.y);
+                        }
+                        tmem_st16(tP + c / 2, pw);
+                        if (c == 32) {
+                            tmem_wait_st();
+                            warp_done(&bars.p_half[s]);
+                        }
+                    }
+                    lsum += (ls[0].x + ls[1].x) + (ls[0].y + ls[1].y);
+                    tmem_wait_st();
+                    warp_done(&bars.p_full[s]);
                 }
-                lsum += (ls[0].x + ls[1].x) + (ls[0].y + ls[1].y);
-                tmem_wait_st();
-                warp_done(&bars.p_full[s]);
-            }
+            };
+            walk(std::false_type{});
+            if (ok && kt < n) walk(std::true_type{});
             if (!ok) break;
             const size_t at =
                 (size_t)(wb * a.H + kvh * a.G) * a.Nq + own.row(r, a.Nq);

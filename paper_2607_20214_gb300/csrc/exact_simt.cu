@@ -224,7 +224,9 @@ __global__ void __launch_bounds__(kThreads)
             float z = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[i][e] = j0 + x + 16 * e < seen[i] ? s[i][e] * sl2
+                // (rounded before the maximum, itself one of them, is
+                // subtracted: large scores' weights stay below 1)
+                s[i][e] = j0 + x + 16 * e < seen[i] ? __fmul_rn(s[i][e], sl2)
                                                     : -INFINITY;
                 z = fmaxf(z, s[i][e]);
             }
