@@ -91,6 +91,11 @@ int elsaa_exact_forward(const elsaa_exact *exact, const void *q,
  * of queries that see nothing and of keys that no query sees are zeros; a query
  * with lse = -inf has weights of 0. bf16 on the tensor cores: P and dS in fp32,
  * each rounded to bf16 for its products, sums in fp32, results rounded once.
+ *
+ * lse is fp32, and so a weight is off by a factor of up to e^(|lse| 2^-22).
+ * Where |lse| is above 2^16 ln 2, one within that factor squared of 1 counts as
+ * 1: the gradients of a row that one key has to itself are right at any size of
+ * its scores; how several share a row is lost from |lse| = 2^22 on.
  */
 int elsaa_exact_backward(const elsaa_exact *exact, const void *q,
                          const void *k, const void *v, const void *o,

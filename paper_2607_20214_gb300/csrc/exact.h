@@ -98,6 +98,23 @@ __device__ __forceinline__ float exact_lse(const float *lse) {
     return x == -INFINITY ? INFINITY : x;
 }
 
+// The backward pass makes weights again as 2^x, x = fma(s, sl2, -lse2), from an
+// lse that was rounded on its way: the forward pass's product, lse itself and
+// lse2, with log2 e and ln 2 as fp32. x is off by up to 2^-22.3 |lse2|, which
+// below kFarLse is a factor of 1.01 of the weight. Behind it the largest one, 1
+// or a little less, could come out as any power of two, or infinite: there x
+// counts as 0 from -2^-21 |lse2| on. exact_edge: where that begins, +inf for
+// rows that need none of it.
+constexpr float kFarLse = 65536.0f;
+__device__ __forceinline__ float exact_edge(float lse2) {
+    const float z = fabsf(lse2);
+    return z > kFarLse && z < INFINITY ? -0x1p-21f * z : INFINITY;
+}
+// (a NaN stays one)
+__device__ __forceinline__ float exact_exponent(float x, float edge) {
+    return x > edge ? 0.0f : x;
+}
+
 // Rows of the query heads that share a K/V head, counted through: row r is row
 // r mod N of head r / N of the group. `most` is the largest seen() among rows
 // [r0, r1).
@@ -165,16 +182,17 @@ __device__ __forceinline__ void store_rows(uint32_t (&y)[4 * CH],
 size_t exact_share_bytes(const ExactView &a);
 cudaError_t launch_exact_fwd_tc(const ExactView &a, int *next_item,
                                 float *part, cudaStream_t st);
-// Its backward pass: D_i first (which also clears the status and two work
-// counters), then dQ, and dK with dV, and the sums of walks that were divided.
-// part: exact_part_bytes(a) of scratch, 256-byte aligned.
+// Its backward pass: D_i first (which also clears the status, two work counters
+// and `far`), then dQ (which sets `far` where a row's lse is behind kFarLse),
+// and dK with dV, and the sums of walks that were divided. part:
+// exact_part_bytes(a) of scratch, 256-byte aligned.
 size_t exact_part_bytes(const ExactView &a);
 cudaError_t launch_exact_delta(const ExactView &a, int *counters,
                                cudaStream_t st);
-cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item,
+cudaError_t launch_exact_dq_tc(const ExactView &a, int *next_item, int *far,
                                float *part, cudaStream_t st);
 cudaError_t launch_exact_dkv_tc(const ExactView &a, int *next_item,
-                                float *part, cudaStream_t st);
+                                const int *far, float *part, cudaStream_t st);
 cudaError_t launch_exact_sum(const ExactView &a, float *part,
                              cudaStream_t st);
 // CUDA cores (fp32, and bf16 with impl = SIMT)

@@ -69,7 +69,7 @@ bool on_tensor_cores(const elsaa_exact *p) {
     return p->dtype == ELSAA_BF16 && p->impl == ELSAA_IMPL_AUTO;
 }
 
-// status and two work counters | D_i, or what CTAs leave of divided rows | the
+// status, two work counters and a flag | D_i, or what CTAs leave of divided rows | the
 // same of the backward pass
 struct Layout {
     size_t next_item, scratch, part, total;
@@ -77,7 +77,7 @@ struct Layout {
 Layout layout(const ExactView &a, bool tensor, bool backward) {
     Layout l;
     l.next_item = sizeof(DeviceStatus);
-    l.scratch = align256(l.next_item + 2 * sizeof(int));
+    l.scratch = align256(l.next_item + 3 * sizeof(int));
     size_t most = tensor ? exact_share_bytes(a) : exact_chunk_bytes(a);
     const size_t delta = sizeof(float) * (size_t)a.B * a.H * a.Nq;
     if (backward && delta > most) most = delta;
@@ -189,12 +189,13 @@ extern "C" int elsaa_exact_backward(
     float *part = (float *)((char *)workspace + l.part);
     if (tensor) {
         int *next_item = (int *)((char *)workspace + l.next_item);
+        int *far = next_item + 2;
         ELSAA_EXACT_LAUNCH("exact_delta", st,
                            launch_exact_delta(a, next_item, st));
         ELSAA_EXACT_LAUNCH("exact_dq_tc", st,
-                           launch_exact_dq_tc(a, next_item, part, st));
+                           launch_exact_dq_tc(a, next_item, far, part, st));
         ELSAA_EXACT_LAUNCH("exact_dkv_tc", st,
-                           launch_exact_dkv_tc(a, next_item + 1, part, st));
+                           launch_exact_dkv_tc(a, next_item + 1, far, part, st));
         ELSAA_EXACT_LAUNCH("exact_sum", st, launch_exact_sum(a, part, st));
         return ELSAA_OK;
     }

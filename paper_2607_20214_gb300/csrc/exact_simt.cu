@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(kThreads)
         load_rows<T, D>(sC, D + 4, (const T *)a.o + (qrow + r0) * D, kHeld,
                         valid);
         __syncthreads();
-        float lse2[4], delta[4];
+        float lse2[4], edge[4], delta[4];
         int seen[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(kThreads)
                 if (x == 0 && it.part == 0)
                     a.delta[qrow + r0 + r] = delta[i];
             }
+            edge[i] = exact_edge(lse2[i]);
         }
         for (int j0 = begin; j0 < most; j0 += kPass) {
             __syncthreads();
@@ -396,7 +397,8 @@ __global__ void __launch_bounds__(kThreads)
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = exp2f(fmaf(s[i][e], sl2, -lse2[i]));
+                    const float p = exp2f(exact_exponent(
+                        fmaf(s[i][e], sl2, -lse2[i]), edge[i]));
                     sW[(4 * y + i) * kPass + x + 16 * e] =
                         j0 + x + 16 * e < seen[i]
                             ? p * (dp[i][e] - delta[i]) : 0.f;
@@ -454,11 +456,14 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = x + 16 * e;
+                    const float edge = exact_edge(sL[j]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const bool on = r0 + 4 * y + i < sN[j];
                         const float p =
-                            on ? exp2f(fmaf(s[i][e], sl2, -sL[j])) : 0.f;
+                            on ? exp2f(exact_exponent(
+                                     fmaf(s[i][e], sl2, -sL[j]), edge))
+                               : 0.f;
                         sP[(4 * y + i) * kPass + j] = p;
                         sW[(4 * y + i) * kPass + j] =
                             on ? p * (dp[i][e] - sD[j]) : 0.f;

@@ -129,3 +129,64 @@ def test_large_scores_rise_from_tile_to_tile(sign, dtype, impl):
     alone, key = check_forward(q[0, 0], k[0, 0], v[0, 0], o[0, 0], lse[0, 0],
                                64.0, True, True)
     assert alone.all() and (key == np.arange(130) + 1370).all()
+
+
+@pytest.mark.parametrize("dtype,impl", KINDS)
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind", SIZES)
+def test_gradients_of_large_scores(kind, shape, d, dtype, impl):
+    """Rows whose weights go to one key: dV gets d_o whole, dS is what the
+    rounding of o leaves. (The others' d_o is 0: whether a tie is one is more
+    than lse holds.)"""
+    B, H, Hkv = (shape.get(n, 1) for n in ("B", "H", "Hkv"))
+    Nq, Nk, causal = shape["Nq"], shape["Nk"], shape.get("causal", False)
+    q, k, v, do, scale = large(d, dtype, kind, **shape)
+    ql, kl = shape.get("ql", [Nq] * B), shape.get("kl", [Nk] * B)
+    ex = E.make_exact(B, H, Hkv, Nq, Nk, d, dtype=NAME[dtype], causal=causal,
+                      scale=scale, impl=impl)
+    kw = {}
+    if "ql" in shape:
+        kw = dict(q_len=torch.tensor(ql, dtype=torch.int32, device="cuda"),
+                  k_len=torch.tensor(kl, dtype=torch.int32, device="cuda"))
+    x = [t.cuda() for t in (q, k, v)]
+    o = torch.zeros_like(x[0])
+    lse = torch.zeros((B, H, Nq), device="cuda")
+    E.elsaa_exact_forward(ex, *x, o=o, lse=lse, **kw)
+    sc = scale or 1 / math.sqrt(d)
+    G, exact = H // Hkv, not isinstance(kind, tuple)
+    rows = {}
+    for b in range(B):
+        for h in range(H):
+            rows[b, h] = check_forward(
+                q[b, h, :ql[b]], k[b, h // G, :kl[b]], v[b, h // G, :kl[b]],
+                o[b, h, :ql[b]], lse[b, h, :ql[b]], sc, causal, exact)
+            do[b, h, :ql[b]][torch.tensor(~rows[b, h][0])] = 0
+    got = E.elsaa_exact_backward(ex, *x, o, lse, do.cuda(), **kw)
+    u = C.half_step(dtype)
+    rnd = 2.0 ** -8 if dtype == BF and impl == 0 else 0.0
+    for b in range(B):
+        n, m = ql[b], kl[b]
+        for j in range(Hkv):
+            K, V = C.f64(k[b, j, :m]), C.f64(v[b, j, :m])
+            dk, dv, dkt, dvt = (np.zeros((m, d)) for _ in range(4))
+            for h in range(j * G, j * G + G):
+                alone, key = rows[b, h]
+                Q, DO, O = (C.f64(t[b, h, :n]) for t in (q, do, o))
+                # P is 1, or within 0.01 of it where lse is below 2^16, and
+                # rounded; dS = <d_o, v - o>
+                p = alone * 1.0
+                ds = p * (DO * (V[key] - O)).sum(1)
+                mag = (np.abs(DO) * (np.abs(V[key]) + np.abs(O))).sum(1)
+                off = p * ((d + 8) * C.U32 * mag) + (rnd + 0.02) * np.abs(ds)
+                dq = sc * ds[:, None] * K[key]
+                tol = sc * off[:, None] * np.abs(K[key]) + 2 * u * np.abs(dq)
+                C.close(got[0][b, h, :n], dq, tol, ("dq", b, h))
+                np.add.at(dk, key, sc * ds[:, None] * Q)
+                np.add.at(dkt, key, sc * (off + n * G * C.U32 * np.abs(ds))[
+                    :, None] * np.abs(Q))
+                np.add.at(dv, key, p[:, None] * DO)
+                np.add.at(dvt, key, (0.02 + n * G * C.U32) *
+                          p[:, None] * np.abs(DO))
+            C.close(got[1][b, j, :m], dk, dkt + 2 * u * np.abs(dk), "dk")
+            C.close(got[2][b, j, :m], dv, dvt + 2 * u * np.abs(dv), "dv")
