@@ -82,6 +82,11 @@ struct EfBars {
     uint64_t o_done[2], o_empty[2];
 };
 
+// How long a slot's softmax waits for its next item: as long as the other slot
+// may take for its own, which can have 2^23 tiles more (2^30 keys; a tile takes
+// 1.2 to 1.8 us). The CTA's other waits are of kWaitLimitNs, and end this one.
+constexpr unsigned long long kEfItemNs = 30 * kWaitLimitNs;
+
 // What the roles know of an item.
 struct EfItem {
     int item;   // -1: no more
@@ -703,7 +708,10 @@ __global__ void __launch_bounds__(kEfThreads, 1)
         int g = 0;  // key tiles of this slot so far
         bool ok = true;
         for (int it = 0; ok; ++it) {
-            ok = wwait(&bars.item_full[it & 1], (it >> 1) & 1, 408);
+            ok = __all_sync(0xffffffffu,
+                            mbar_wait_or_abort_for(
+                                kEfItemNs, &bars.item_full[it & 1],
+                                (it >> 1) & 1, abort, status, 408));
             if (!ok) break;
             const EfItem &w_s = item_s[it & 1];
             const int item = w_s.item, n = w_s.n[s], part = w_s.part;

@@ -123,22 +123,27 @@ __device__ __forceinline__ void mbar_arrive(uint64_t *bar) {
 // Bounded wait that also gives up as soon as another thread of the CTA has
 // set *abort (after its own wait ran out), so a stalled pipeline drains in
 // one wait limit instead of one per pending stage.
-__device__ __forceinline__ bool mbar_wait_or_abort(uint64_t *bar,
-                                                   uint32_t parity,
-                                                   volatile int *abort,
-                                                   DeviceStatus *st,
-                                                   int site) {
+__device__ __forceinline__ bool mbar_wait_or_abort_for(
+    unsigned long long limit_ns, uint64_t *bar, uint32_t parity,
+    volatile int *abort, DeviceStatus *st, int site) {
     if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long t0 = global_ns();
     while (!mbar_try_wait(bar, parity)) {
         if (*abort) return false;
-        if (global_ns() - t0 > kWaitLimitNs) {
+        if (global_ns() - t0 > limit_ns) {
             *abort = 1;
             record_timeout(st, site);
             return false;
         }
     }
     return true;
+}
+__device__ __forceinline__ bool mbar_wait_or_abort(uint64_t *bar,
+                                                   uint32_t parity,
+                                                   volatile int *abort,
+                                                   DeviceStatus *st,
+                                                   int site) {
+    return mbar_wait_or_abort_for(kWaitLimitNs, bar, parity, abort, st, site);
 }
 
 // Named barrier over `count` threads (id 0 is __syncthreads).
