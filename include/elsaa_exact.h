@@ -21,8 +21,12 @@
  *
  * Rows behind the lengths may hold anything, NaN too. A NaN or an infinity in a
  * row that a sequence has may, with causal = 1, also reach rows that do not see
- * it or that it does not see, within 128 rows of the diagonal (v in the forward
- * pass; q, k, v and d_o in the backward pass): a weight of 0 times it is NaN.
+ * it or that it does not see, as a weight of 0 times it is NaN:
+ *     v in the forward pass and k of dq: query rows in one tile of 128 with a
+ *     row that sees it or one of its 128 keys. Tiles hold the rows of a K/V
+ *     head's query heads one behind the other, so that a head's first rows may
+ *     share one with the last of the head before;
+ *     q and d_o of dk and dv: the keys of the same 128 as one that they see.
  */
 #ifndef ELSAA_EXACT_H
 #define ELSAA_EXACT_H
