@@ -24,8 +24,9 @@
  *     a = 2 pi frac(position * turns[p] / 2^64),
  * position that of the pair's axis: the product is taken modulo 2^64, so that
  * a far position's angle is as exact as a near one's. Sines and cosines are
- * those of fp32 (dtype fp32) or off by 2^-21 at most (bf16, whose results are
- * rounded to 2^-8). mean(x^2) is taken in fp32: rows of numbers near 2^64
+ * those of fp32 (dtype fp32) or off by 2^-20 at most (bf16, whose heads and rows
+ * are rounded to 2^-8; the fp32 dw_q and dw_k of bf16 rows are off by 2^-20 of
+ * their terms' sizes for it). mean(x^2) is taken in fp32: rows of numbers near 2^64
  * overflow to 0.
  */
 #ifndef ELSAA_HEADS_H

@@ -101,8 +101,11 @@ struct Turn {
 };
 
 // Sine and cosine of h half turns, h in [-1, 1). For heads of bf16 the
-// hardware's: an absolute error of 2^-21 where the result is rounded to 2^-8.
-// (With sincospif the backward pass of B8 H12 N8192 d64 took 5 us more.)
+// hardware's, 2^-21.41 and 2^-21.19 off for arguments up to pi, which are off
+// themselves by 2^-21.6 (h, pi and their product as fp32): 2^-20.4, where heads
+// and rows are rounded to 2^-8. dw, in fp32, is off by that times its terms'
+// sizes, as by a dozen roundings, of the many that its sum has. (With sincospif
+// the backward pass of B8 H12 N8192 d64 took 5 us more.)
 template <typename T>
 __device__ __forceinline__ void half_turns(float h, float *s, float *c) {
     if (sizeof(T) == 4) {
