@@ -55,10 +55,18 @@ struct ExactOrder {
     // Of a sequence of ql rows in a padded batch of short ones, heads as far
     // apart as these rows need: then no 128 rows are without one, and tile()
     // holds for the first groups * per of the tiles that the batch's own order
-    // gives. B8 H16 H_kv4 N_q 500 N_k 4096 d128, 20 or 300 rows each: 66 -> 52
-    // us, 113 -> 102. Longer batches have few such rows and gained nothing:
-    // sequences of 4099 and 1500 to 3300 rows, causal, 119-137 us so and
-    // 126-138 fitted.
+    // gives. B8 H16 H_kv4 N_k 4096 d128 causal, us, heads as the batch has them
+    // and fitted, by the rows of a sequence:
+    //   N_q    20 rows   20 to 300   1 to N_q    0.85 N_q to N_q
+    //    500   31   27   47    42    49    49       67    67
+    //    900   31   27   47    42    78    80      106    99
+    //   1100   41   35   55    42   104   103      124   126
+    //   2048   41   35   56    42   153   154      237   239
+    //   4096   53   37   68    50   311   306      440   431
+    // B32, and B8 with 12 heads of 64, gain and lose likewise; half of the
+    // sequences short and half long loses up to 6 % (N_q 2048, d64: 89 and 94).
+    // So the rule gives away what long batches of short sequences alone would
+    // gain.
     __device__ __forceinline__ ExactOrder of(int ql) const {
         ExactOrder x = *this;
         if (padded && pitch <= 1024) x.lay(max(ql + 127, 128) / 128 * 128);
