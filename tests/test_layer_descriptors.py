@@ -25,8 +25,8 @@ class Library:
         self.seen = []
 
     def __getattr__(self, name):
-        def call(ref, *args):
-            x = ref._obj
+        def call(x, *args):
+            assert isinstance(x, ctypes.Structure)
             self.seen.append({f[0]: getattr(x, f[0]) for f in x._fields_})
             return 0
         return call
