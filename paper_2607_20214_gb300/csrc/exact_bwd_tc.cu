@@ -14,7 +14,7 @@
 // them: tensor pipe 73 % (dQ) and 67 % (dK, dV). B4 H12 N4096 causal: both 490 us,
 // 1.06 PFLOP/s counting five products, 0.55 of the measured bf16 rate. For D <= 64
 // the weights' warps, whose steps of a tile stand one behind the other: B4 H12
-// N4096 d64 causal, dQ 134 us, dK and dV 203.
+// N4096 d64 causal, dQ 137 us, dK and dV 205.
 #include <type_traits>
 
 #include "device_common.cuh"

@@ -17,11 +17,11 @@
 // at D = 128. O stays in tensor memory; a softmax warp rescales it when the
 // maximum of one of its rows has grown much.
 //
-// What bounds it: at D = 128 the products, 2048 of a tile's 2870 clocks (256 rows,
+// What bounds it: at D = 128 the products, 2048 of a tile's 2900 clocks (256 rows,
 // 128 keys), and the steps of a slot between them, of which the softmax takes
-// 1260: B1 H16 H_kv4 N16384 causal 0.70 ms, 1.57 PFLOP/s, 0.82 of the measured bf16
-// rate. For D <= 64 the softmax: B4 H12 N4096 d64 without a mask 199 us, 1.03
-// PFLOP/s.
+// 1260: B1 H16 H_kv4 N16384 causal 0.71 ms, 1.56 PFLOP/s, 0.81 of the measured bf16
+// rate. For D <= 64 the waits between a slot's steps, no pipe is full: B4 H12 N4096
+// d64 without a mask 200 us, 1.03 PFLOP/s.
 #include <algorithm>
 #include <type_traits>
 

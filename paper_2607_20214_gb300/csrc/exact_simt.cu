@@ -10,7 +10,7 @@
 // the same rows with d / 16 channels. Every four channels cost 8 16-byte reads
 // from shared memory for 64 multiply-adds (32 packed ones). Shared memory's
 // wavefronts run at 64 % of their peak, the multiply-adds at 46 %: B8 H8 N1000
-// d64 fp32 465 us forward, 35 TFLOP/s of 74; its backward pass 1524, 27. (8 rows a
+// d64 fp32 464 us forward, 35 TFLOP/s of 74; its backward pass 1559, 26. (8 rows a
 // thread, or warps of 4 x 8, save wavefronts and were no faster.) With few
 // tiles of held rows the walks are divided into chunks, and k_exact_join and
 // k_exact_add add up, in order, what these leave.
